@@ -305,6 +305,154 @@ ADAMA_API adama_status adama_apply_sharded_peers(adama_ctx *ctx, float *const *w
                                                  int world_size, int rank, size_t n, double lr,
                                                  void *cuda_stream);
 
+/* ---- the end of a fine-tuning step ------------------------------------------------------- */
+
+/* The mini-batch's LAST fold and its update in one pass over a list of tensors (Algorithm 2: the
+ * inner loop body for the last micro-batch, "Update", and the next mini-batch's decay):
+ *     g <- factor*g,  m <- m + a*g,  v <- v + b*g^2,  then as adama_apply
+ * With one micro-batch per mini-batch this is a whole Adam (with adama_set_weight_decay: AdamW)
+ * step: 26 B/param with bf16 gradients where a fold and an apply move 18 + 24.  Results are
+ * bit-identical to adama_fold_multi followed by adama_apply_multi when grad_factor is NULL.
+ *   grads, w, m, v, n : HOST arrays of `count` entries, as for adama_fold_multi / adama_apply_multi;
+ *            up to 512 tensors share a launch, of any lengths (0 included)
+ *   w_bf16 : NULL, or a HOST array of `count` device pointers (entries may be NULL) that receive
+ *            the updated weights rounded to bf16, as adama_apply_bf16_copy
+ *   grad_factor : NULL (1), or ONE fp32 in DEVICE memory that every gradient is multiplied by, e.g.
+ *            adama_grad_norm.factor.  If it is NaN the kernel leaves w, m, v and the copies as they
+ *            are (t has been counted all the same): a step with a non-finite gradient is skipped
+ *            without a host round trip.
+ * Any element-aligned pointers are accepted; 128-bit accesses are used for a tensor whose w, m, v
+ * reach a 16-byte boundary after the same number of elements and whose gradient (and copy) reach a
+ * 4-element boundary there, element accesses otherwise.  Tensors must not overlap.
+ * Errors: INVALID_ARG, BAD_STATE, MISALIGNED (element alignment), CUDA. */
+ADAMA_API adama_status adama_fold_apply_multi(adama_ctx *ctx, const void *const *grads,
+                                              adama_dtype gdt, float *const *w, float *const *m,
+                                              float *const *v, void *const *w_bf16, const size_t *n,
+                                              int count, double lr, const float *grad_factor,
+                                              void *cuda_stream);
+
+/* Moments in 8 bits: per block of 256 consecutive elements of a tensor (the last block may be
+ * shorter) one fp32 scale for m and one for v,
+ *     m[i] = M(m_codes[i]) * m_scale[i/256]   M: e4m3 (sign, 4 exponent bits, 3 mantissa bits; NaN
+ *                                             0x7f, 0xff), largest value 448
+ *     v[i] = V(v_codes[i]) * v_scale[i/256]   V(0) = 0, V(c) = (1 + (c mod 8)/8) * 2^(c/8 - 31),
+ *                                             largest value 1.875
+ * 2.03 B/param instead of 8.  All-zero codes and scales are the initial state m = v = 0.  Writing a
+ * block puts its largest |m| and v at the largest code value, rounds the others to the nearest code
+ * (ties to the even one), and never rounds a v > 0 to 0. */
+#define ADAMA_STATE8_BLOCK 256
+typedef struct adama_state8 {
+    uint8_t *m_codes; /* n bytes */
+    float *m_scale;   /* ceil(n/256) fp32 */
+    uint8_t *v_codes;
+    float *v_scale;
+} adama_state8;
+
+/* adama_fold_apply_multi with moments in 8 bits: 14.06 B/param with bf16 gradients.  The same
+ * formula, evaluated in fp32 on the values that the codes stand for; the beta decay multiplies the
+ * scales, the codes are those of the undecayed m_t, v_t.
+ *   states : HOST array of `count` descriptions of device buffers
+ * It is meant for ONE gradient per mini-batch.  There is deliberately no 8-bit form of adama_fold:
+ * a micro-batch changes v by less than half of a code's width, so rounding after each of N folds
+ * would lose most of them.  To accumulate several micro-batches, sum them first (adama_sgdm_fold
+ * into an fp32 buffer), then make this call.
+ * Up to 448 tensors share a launch; 16-byte aligned grads, w and copies and 8-byte aligned codes
+ * take 64- and 128-bit accesses, others element accesses.  grad_factor, w_bf16 and errors as
+ * adama_fold_apply_multi. */
+ADAMA_API adama_status adama_fold_apply8_multi(adama_ctx *ctx, const void *const *grads,
+                                               adama_dtype gdt, float *const *w,
+                                               const adama_state8 *states, void *const *w_bf16,
+                                               const size_t *n, int count, double lr,
+                                               const float *grad_factor, void *cuda_stream);
+
+/* fp32 moments into codes and scales (a run that moves from 32 to 8 bits, a checkpoint read back),
+ * and codes and scales into the fp32 values that they stand for.  m, v follow the state convention
+ * above (decayed between mini-batches).  Packing the result of an unpack gives the same values back
+ * to the last bit of the scales.  Errors: INVALID_ARG, MISALIGNED, CUDA. */
+ADAMA_API adama_status adama_state8_pack_multi(adama_ctx *ctx, const float *const *m,
+                                               const float *const *v, const adama_state8 *states,
+                                               const size_t *n, int count, void *cuda_stream);
+ADAMA_API adama_status adama_state8_unpack_multi(adama_ctx *ctx, const adama_state8 *states,
+                                                 float *const *m, float *const *v, const size_t *n,
+                                                 int count, void *cuda_stream);
+
+/* Scratch of the two reductions below: caller-owned device memory, 16-byte aligned, zero-filled
+ * once before its first use (each call leaves it ready for the next).  Calls that may overlap on the
+ * GPU (different streams) need one each. */
+#define ADAMA_WORKSPACE_BYTES 65536
+
+/* Global 2-norm of a list of gradients, and the factor that clips it to max_norm, both left in
+ * device memory:
+ *     sumsq = sum over all tensors of g^2  (+ out->sumsq if `accumulate`),  norm = sqrt(sumsq),
+ *     factor = max_norm/norm where norm > max_norm, else 1; NaN where norm is not finite
+ * `accumulate` joins lists of different dtypes (or of several ranks, the caller having summed
+ * sumsq) in one norm.  Squares are formed and summed in fp32 within 16 elements of a thread, in
+ * double from there on; entries beyond 1.8e19 count as infinite.  The result does not depend on
+ * scheduling.  An empty list gives norm 0, factor 1.  max_norm > 0, may be infinite (no clipping).
+ * One launch for up to 1024 tensors, any element-aligned pointers.
+ *   out : one adama_grad_norm in DEVICE memory, 8-byte aligned
+ * Errors: INVALID_ARG, MISALIGNED, CUDA. */
+typedef struct adama_grad_norm {
+    float norm;
+    float factor;
+    double sumsq;
+} adama_grad_norm;
+ADAMA_API adama_status adama_grad_norm_multi(adama_ctx *ctx, const void *const *grads,
+                                             adama_dtype gdt, const size_t *n, int count,
+                                             double max_norm, int accumulate, adama_grad_norm *out,
+                                             void *workspace, void *cuda_stream);
+
+/* Log-probability of one target per row of logits, with z = logit_scale * logits (logit_scale is
+ * the inverse temperature):
+ *     lse = log sum_j exp(z_j),  logp = z_target - lse,  entropy = lse - sum_j p_j z_j
+ *   logits  : [rows, vocab] fp32 or bf16, row pitch ld elements (>= vocab), device, read-only;
+ *             -inf entries have probability 0
+ *   targets : rows int64, device.  A row with a negative target is not read; its outputs are 0.  A
+ *             target >= vocab gives NaN, and the next adama_sync_status reports INVALID_ARG.
+ *   logp, lse, entropy : rows fp32 each; lse and entropy may be NULL
+ * Any element-aligned logits and any pitch.  Errors: INVALID_ARG, MISALIGNED, CUDA. */
+ADAMA_API adama_status adama_token_logprobs(adama_ctx *ctx, const void *logits, adama_dtype dt,
+                                            int64_t rows, int64_t vocab, int64_t ld,
+                                            const int64_t *targets, double logit_scale, float *logp,
+                                            float *lse, float *entropy, void *cuda_stream);
+
+/* Clipped policy loss with a KL term, and its gradient with respect to the logits.  Per row, with
+ * logp as in adama_token_logprobs, A the advantage and w the row's weight:
+ *     r  = exp(logp - old_logp)
+ *     pg = -min(r*A, clamp(r, 1-clip_low, 1+clip_high)*A)
+ *     d  = ref_logp - logp,  kl = exp(d) - d - 1            (0 without ref_logp)
+ *     stats = sum over rows of w*{pg + kl_coef*kl, pg, kl, [r*A > the clamped product]}
+ *     dlogits_j = w*logit_scale*c*([j = target] - p_j),
+ *         c = (r*A <= the clamped product ? -r*A : 0) + kl_coef*(1 - exp(d))
+ * so that stats[0] is the loss and dlogits its gradient; w carries the mask and the normalisation
+ * (e.g. 1/number of answer tokens).  A row with w = 0 or a negative target is not read: its dlogits
+ * are 0, its logp is 0 and it adds nothing to stats.  dlogits in bf16 is the dY that
+ * adama_linear_wgrad_fold takes for the output layer (its pitch must then be a multiple of 8).
+ *   logits   : [rows, vocab] fp32 or bf16, pitch ld_logits; read-only unless dlogits is the same
+ *              buffer, which is allowed with equal dtype and pitch (the gradient replaces the logits)
+ *   dlogits  : [rows, vocab] fp32 or bf16, pitch ld_dlogits, or NULL (loss and logp only)
+ *   old_logp, ref_logp (or NULL), advantages, weights : rows fp32 each
+ *   logp     : rows fp32, or NULL;   stats : 4 fp32;   workspace : ADAMA_WORKSPACE_BYTES
+ * logit_scale > 0, 0 <= clip_low <= 1, clip_high >= 0, kl_coef finite.  Deterministic.
+ * Errors: INVALID_ARG, MISALIGNED, CUDA; targets >= vocab as in adama_token_logprobs. */
+typedef struct adama_policy_args {
+    const void *logits;
+    void *dlogits;
+    adama_dtype logits_dtype, dlogits_dtype;
+    int64_t rows, vocab, ld_logits, ld_dlogits;
+    const int64_t *targets;
+    const float *old_logp;
+    const float *ref_logp;
+    const float *advantages;
+    const float *weights;
+    double logit_scale, clip_low, clip_high, kl_coef;
+    float *logp;
+    float *stats;
+    void *workspace;
+} adama_policy_args;
+ADAMA_API adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args *args,
+                                         void *cuda_stream);
+
 /* ---- host-buffer variants (same arithmetic, copies included) --------------------------- */
 
 /* adama_fold with the gradient in HOST memory (pinned memory for full copy
@@ -438,7 +586,8 @@ ADAMA_API adama_status adama_set_weight_decay(adama_ctx *ctx, double weight_deca
 
 /* Waits for `cuda_stream`, then reads and clears the device status block.
  * Returns ADAMA_OK, ADAMA_ERR_TIMEOUT (a bounded wait inside the fused kernel
- * expired; m and v of that call are incomplete) or ADAMA_ERR_CUDA. */
+ * expired; m and v of that call are incomplete), ADAMA_ERR_INVALID_ARG (a row of
+ * adama_token_logprobs or adama_policy_loss had a target >= vocab) or ADAMA_ERR_CUDA. */
 ADAMA_API adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream);
 
 /* Test hook: writes {code, wait, tile} into the device status block exactly as a kernel whose

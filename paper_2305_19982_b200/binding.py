@@ -25,6 +25,8 @@ EXPORTED_SYMBOLS = [
     "adama_debug_set_wgrad_variant", "adama_debug_setup_state", "adama_last_error", "adama_launch_count", "adama_host_constants",
     "adama_host_constants_allreduced", "adama_host_constants_sharded",
     "adama_version",
+    "adama_fold_apply_multi", "adama_fold_apply8_multi", "adama_state8_pack_multi", "adama_state8_unpack_multi",
+    "adama_grad_norm_multi", "adama_token_logprobs", "adama_policy_loss",
 ]
 
 
@@ -42,6 +44,9 @@ F32, BF16 = 0, 1
 GRADS_PRESCALED = 1
 ASYNC_COPYBACK = 2
 INPUTS_SETTLED = 4
+STATE8_BLOCK = 256        # ADAMA_STATE8_BLOCK
+WORKSPACE_BYTES = 65536   # ADAMA_WORKSPACE_BYTES
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 class AdamAError(RuntimeError):
@@ -55,6 +60,23 @@ class _LinearItem(ctypes.Structure):
                 ("d_in", ctypes.c_int), ("d_out", ctypes.c_int), ("ldx", ctypes.c_int64),
                 ("ldy", ctypes.c_int64), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
                 ("ldmv", ctypes.c_int64), ("m_bias", ctypes.c_void_p), ("v_bias", ctypes.c_void_p)]
+
+
+class _State8(ctypes.Structure):
+    _fields_ = [("m_codes", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _PolicyArgs(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("dlogits", ctypes.c_void_p),
+                ("logits_dtype", ctypes.c_int), ("dlogits_dtype", ctypes.c_int),
+                ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ld_logits", ctypes.c_int64),
+                ("ld_dlogits", ctypes.c_int64), ("targets", ctypes.c_void_p),
+                ("old_logp", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p),
+                ("advantages", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("logit_scale", ctypes.c_double), ("clip_low", ctypes.c_double),
+                ("clip_high", ctypes.c_double), ("kl_coef", ctypes.c_double),
+                ("logp", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("workspace", ctypes.c_void_p)]
 
 
 class _Config(ctypes.Structure):
@@ -118,6 +140,14 @@ def load_library() -> ctypes.CDLL:
     L.adama_sgdm_fold.argtypes = [vp, vp, ci, vp, sz, vp]
     L.adama_sgdm_apply.argtypes = [vp, vp, vp, sz, dbl, dbl, vp]
     L.adama_coefficient_stats.argtypes = [vp, vp, vp, vp, vp, sz, vp, vp]
+    vpp, szp = ctypes.POINTER(vp), ctypes.POINTER(sz)
+    L.adama_fold_apply_multi.argtypes = [vp, vpp, ci, vpp, vpp, vpp, vpp, szp, ci, dbl, vp, vp]
+    L.adama_fold_apply8_multi.argtypes = [vp, vpp, ci, vpp, ctypes.POINTER(_State8), vpp, szp, ci, dbl, vp, vp]
+    L.adama_state8_pack_multi.argtypes = [vp, vpp, vpp, ctypes.POINTER(_State8), szp, ci, vp]
+    L.adama_state8_unpack_multi.argtypes = [vp, ctypes.POINTER(_State8), vpp, vpp, szp, ci, vp]
+    L.adama_grad_norm_multi.argtypes = [vp, vpp, ci, szp, ci, dbl, ci, vp, vp, vp]
+    L.adama_token_logprobs.argtypes = [vp, vp, ci, i64, i64, i64, vp, dbl, vp, vp, vp, vp]
+    L.adama_policy_loss.argtypes = [vp, ctypes.POINTER(_PolicyArgs), vp]
     L.adama_get_step.argtypes = [vp]
     L.adama_get_step.restype = i64
     L.adama_set_step.argtypes = [vp, i64]
@@ -185,6 +215,47 @@ class TensorList:
         return len(self.tensors)
 
 
+class State8:
+    """Adam moments of one tensor in 8 bits (adama_state8): `m_codes` float8_e4m3fn and `v_codes`
+    uint8, one element each per parameter, `m_scale` and `v_scale` fp32, one per 256 elements.  All
+    contiguous CUDA tensors owned by the caller; `State8.zeros(n)` makes the initial state."""
+
+    def __init__(self, m_codes: torch.Tensor, m_scale: torch.Tensor, v_codes: torch.Tensor,
+                 v_scale: torch.Tensor):
+        n = m_codes.numel()
+        blocks = -(-n // STATE8_BLOCK)
+        if v_codes.numel() != n or m_scale.numel() != blocks or v_scale.numel() != blocks:
+            raise ValueError("v_codes must match m_codes; scales have one element per 256 codes")
+        if not all(t.is_contiguous() for t in (m_codes, m_scale, v_codes, v_scale)):
+            raise ValueError("an 8-bit state needs contiguous tensors")
+        self.m_codes, self.m_scale, self.v_codes, self.v_scale = m_codes, m_scale, v_codes, v_scale
+        self.numel = n
+        self._item = _State8(_dev_ptr(m_codes, torch.float8_e4m3fn, "m_codes"),
+                             _dev_ptr(m_scale, torch.float32, "m_scale"),
+                             _dev_ptr(v_codes, torch.uint8, "v_codes"),
+                             _dev_ptr(v_scale, torch.float32, "v_scale"))
+
+    @classmethod
+    def zeros(cls, n: int, device="cuda") -> "State8":
+        blocks = -(-n // STATE8_BLOCK)
+        zeros = lambda k, dtype: torch.zeros(k, dtype=torch.uint8, device=device).view(dtype)  # noqa: E731
+        return cls(zeros(n, torch.float8_e4m3fn), zeros(4 * blocks, torch.float32),
+                   zeros(n, torch.uint8), zeros(4 * blocks, torch.float32))
+
+
+class State8List:
+    """Descriptions of a list of State8, marshalled once for repeated calls (keeps them alive)."""
+
+    def __init__(self, states):
+        self.states = list(states)
+        self.items = (_State8 * len(self.states))(*[s._item for s in self.states])
+        self.numels = [s.numel for s in self.states]
+        self.ns = (ctypes.c_size_t * len(self.states))(*self.numels)
+
+    def __len__(self):
+        return len(self.states)
+
+
 class AdamA:
     """One AdamA context (adama_ctx) bound to a CUDA device.
 
@@ -200,6 +271,7 @@ class AdamA:
                  async_copyback=False, inputs_settled=False):
         self._L = load_library()
         self._h = ctypes.c_void_p()
+        self._workspaces = {}
         self.device = torch.device("cuda", int(device))
         cfg = _Config(beta1, beta2, eps, int(device),
                       (GRADS_PRESCALED if grads_prescaled else 0) |
@@ -471,6 +543,172 @@ class AdamA:
             self._h, _dev_ptr(w, torch.float32, "w"), _dev_ptr(m, torch.float32, "m"),
             _dev_ptr(v, torch.float32, "v"), n, float(lr), int(world_size),
             _stream_ptr(self.device)))
+
+    # -- the end of a fine-tuning step -------------------------------------------------------
+    def _workspace(self, stream: int) -> int:
+        """Scratch of the reductions: one zero-filled buffer for each stream that uses them."""
+        t = self._workspaces.get(stream)
+        if t is None:
+            t = torch.zeros(WORKSPACE_BYTES, dtype=torch.uint8, device=self.device)
+            self._workspaces[stream] = t
+        return t.data_ptr()
+
+    @staticmethod
+    def _copies(w_bf16, numels):
+        """Pointer array of the optional bf16 copies: None, or a list whose entries may be None."""
+        if w_bf16 is None:
+            return None
+        if isinstance(w_bf16, TensorList):
+            if w_bf16.dtype != torch.bfloat16 or w_bf16.numels != numels:
+                raise ValueError("w_bf16 must be bfloat16 tensors of the sizes of the weights")
+            return w_bf16.ptrs
+        if len(w_bf16) != len(numels):
+            raise ValueError("lists must have equal length")
+        arr = (ctypes.c_void_p * len(numels))()
+        for i, (t, n) in enumerate(zip(w_bf16, numels)):
+            if t is None:
+                continue
+            if t.numel() != n or not t.is_contiguous():
+                raise ValueError("w_bf16 must be contiguous tensors of the sizes of the weights")
+            arr[i] = _dev_ptr(t, torch.bfloat16, "w_bf16")
+        return arr
+
+    @staticmethod
+    def _factor(grad_factor):
+        if grad_factor is None:
+            return None
+        if grad_factor.numel() != 1:
+            raise ValueError("grad_factor must hold one value")
+        return _dev_ptr(grad_factor, torch.float32, "grad_factor")
+
+    def fold_apply_multi(self, ws, grads, ms, vs, lr: float, w_bf16=None,
+                         grad_factor: Optional[torch.Tensor] = None) -> None:
+        """adama_fold_apply_multi: the mini-batch's last gradient and the update in one pass over
+        lists of tensors (or TensorList objects).  `w_bf16` (list, entries may be None) receives
+        the weights as bf16; `grad_factor` is one fp32 on the device (NaN skips the step)."""
+        ws = ws if isinstance(ws, TensorList) else TensorList(ws, torch.float32)
+        grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+        ms = ms if isinstance(ms, TensorList) else TensorList(ms, torch.float32)
+        vs = vs if isinstance(vs, TensorList) else TensorList(vs, torch.float32)
+        if not ws.numels == grads.numels == ms.numels == vs.numels:
+            raise ValueError("w, grad, m, v must be lists of equal sizes")
+        for t in (ws, ms, vs):
+            if t.dtype != torch.float32:
+                raise TypeError("w, m, v must be float32")
+        if grads.dtype not in _DTYPES:
+            raise TypeError("grads must be float32 or bfloat16")
+        self._check(self._L.adama_fold_apply_multi(
+            self._h, grads.ptrs, _DTYPES[grads.dtype], ws.ptrs, ms.ptrs, vs.ptrs,
+            self._copies(w_bf16, ws.numels), ws.ns, len(ws), float(lr), self._factor(grad_factor),
+            _stream_ptr(self.device)))
+
+    def fold_apply8_multi(self, ws, grads, states, lr: float, w_bf16=None,
+                          grad_factor: Optional[torch.Tensor] = None) -> None:
+        """adama_fold_apply8_multi: the same with moments in 8 bits (a list of State8, or a
+        State8List).  For one gradient per mini-batch; see include/adama.h."""
+        ws = ws if isinstance(ws, TensorList) else TensorList(ws, torch.float32)
+        grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+        states = states if isinstance(states, State8List) else State8List(states)
+        if not ws.numels == grads.numels == states.numels:
+            raise ValueError("w, grad, states must be lists of equal sizes")
+        if ws.dtype != torch.float32:
+            raise TypeError("w must be float32")
+        if grads.dtype not in _DTYPES:
+            raise TypeError("grads must be float32 or bfloat16")
+        self._check(self._L.adama_fold_apply8_multi(
+            self._h, grads.ptrs, _DTYPES[grads.dtype], ws.ptrs, states.items,
+            self._copies(w_bf16, ws.numels), ws.ns, len(ws), float(lr), self._factor(grad_factor),
+            _stream_ptr(self.device)))
+
+    def _state8_convert(self, fn, states, ms, vs, pack: bool) -> None:
+        states = states if isinstance(states, State8List) else State8List(states)
+        ms = ms if isinstance(ms, TensorList) else TensorList(ms, torch.float32)
+        vs = vs if isinstance(vs, TensorList) else TensorList(vs, torch.float32)
+        if not states.numels == ms.numels == vs.numels:
+            raise ValueError("states, m, v must be lists of equal sizes")
+        if ms.dtype != torch.float32 or vs.dtype != torch.float32:
+            raise TypeError("m, v must be float32")
+        lists = (ms.ptrs, vs.ptrs, states.items) if pack else (states.items, ms.ptrs, vs.ptrs)
+        self._check(fn(self._h, *lists, states.ns, len(states), _stream_ptr(self.device)))
+
+    def state8_pack_multi(self, ms, vs, states) -> None:
+        """adama_state8_pack_multi: fp32 moments into 8-bit states."""
+        self._state8_convert(self._L.adama_state8_pack_multi, states, ms, vs, True)
+
+    def state8_unpack_multi(self, states, ms, vs) -> None:
+        """adama_state8_unpack_multi: the fp32 values that 8-bit states stand for."""
+        self._state8_convert(self._L.adama_state8_unpack_multi, states, ms, vs, False)
+
+    def grad_norm_multi(self, grads, max_norm: float, out: torch.Tensor, accumulate: bool = False) -> None:
+        """adama_grad_norm_multi: `out` (4 fp32 on the device) receives norm in out[0], the clip
+        factor in out[1] (the grad_factor of a step: out[1:2]) and the sum of squares as a float64
+        in out[2:4]."""
+        grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+        if grads.dtype not in _DTYPES:
+            raise TypeError("grads must be float32 or bfloat16")
+        if out.numel() != 4 or not out.is_contiguous():
+            raise ValueError("out must hold 4 contiguous float32 values")
+        stream = _stream_ptr(self.device)
+        self._check(self._L.adama_grad_norm_multi(
+            self._h, grads.ptrs, _DTYPES[grads.dtype], grads.ns, len(grads), float(max_norm),
+            int(accumulate), _dev_ptr(out, torch.float32, "out"), self._workspace(stream), stream))
+
+    @staticmethod
+    def _rows(t: torch.Tensor, name: str):
+        """(pointer, dtype, pitch) of a [rows, vocab] tensor with unit stride in its last dimension."""
+        if t.dim() != 2:
+            raise ValueError(f"{name} must be [rows, vocab]")
+        if t.dtype not in _DTYPES:
+            raise TypeError(f"{name} must be float32 or bfloat16")
+        rows, vocab = t.shape
+        if vocab > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name} must have unit stride in its last dimension")
+        return _dev_ptr(t, t.dtype, name), _DTYPES[t.dtype], t.stride(0) if rows > 1 else max(vocab, t.stride(0))
+
+    @staticmethod
+    def _per_row(t: Optional[torch.Tensor], rows: int, name: str, dtype=torch.float32):
+        if t is None:
+            return None
+        if t.numel() != rows or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous with one element per row")
+        return _dev_ptr(t, dtype, name)
+
+    def token_logprobs(self, logits: torch.Tensor, targets: torch.Tensor, logp: torch.Tensor,
+                       lse: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                       logit_scale: float = 1.0) -> None:
+        """adama_token_logprobs: log-probability of `targets` (int64; negative = ignored) under the
+        rows of `logits` (fp32 or bf16), written to `logp`; log-sum-exp and entropy on request."""
+        ptr, dt, ld = self._rows(logits, "logits")
+        rows, vocab = logits.shape
+        self._check(self._L.adama_token_logprobs(
+            self._h, ptr, dt, rows, vocab, ld, self._per_row(targets, rows, "targets", torch.int64),
+            float(logit_scale), self._per_row(logp, rows, "logp"), self._per_row(lse, rows, "lse"),
+            self._per_row(entropy, rows, "entropy"), _stream_ptr(self.device)))
+
+    def policy_loss(self, logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Tensor,
+                    advantages: torch.Tensor, weights: torch.Tensor, dlogits: Optional[torch.Tensor],
+                    stats: torch.Tensor, ref_logp: Optional[torch.Tensor] = None,
+                    logp: Optional[torch.Tensor] = None, clip_low: float = 0.2, clip_high: float = 0.2,
+                    kl_coef: float = 0.0, logit_scale: float = 1.0) -> None:
+        """adama_policy_loss: `stats` (4 fp32) receives {loss, policy part, KL, clipped share}, each
+        weighted by `weights`; `dlogits` (fp32 or bf16, `logits` itself, or None) the gradient."""
+        ptr, dt, ld = self._rows(logits, "logits")
+        rows, vocab = logits.shape
+        dptr, ddt, dld = None, dt, 0
+        if dlogits is not None:
+            if tuple(dlogits.shape) != (rows, vocab):
+                raise ValueError("dlogits must have the shape of logits")
+            dptr, ddt, dld = self._rows(dlogits, "dlogits")
+        if stats.numel() != 4 or not stats.is_contiguous():
+            raise ValueError("stats must hold 4 contiguous float32 values")
+        stream = _stream_ptr(self.device)
+        args = _PolicyArgs(
+            ptr, dptr, dt, ddt, rows, vocab, ld, dld, self._per_row(targets, rows, "targets", torch.int64),
+            self._per_row(old_logp, rows, "old_logp"), self._per_row(ref_logp, rows, "ref_logp"),
+            self._per_row(advantages, rows, "advantages"), self._per_row(weights, rows, "weights"),
+            float(logit_scale), float(clip_low), float(clip_high), float(kl_coef),
+            self._per_row(logp, rows, "logp"), _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream))
+        self._check(self._L.adama_policy_loss(self._h, ctypes.byref(args), stream))
 
     # -- host-buffer variants ---------------------------------------------------------------
     def fold_host(self, grad_host: torch.Tensor, m: torch.Tensor, v: torch.Tensor,

@@ -14,7 +14,7 @@ CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libadama.so"
 SOURCES = ["adama_api.cu", "fold_apply.cu", "multi_tensor.cu", "bias_grad.cu", "peer_apply.cu", "extensions.cu",
-           "wgrad_fold.cu"]
+           "wgrad_fold.cu", "fold_apply_multi.cu", "state8.cu", "grad_norm.cu", "policy_loss.cu"]
 
 
 def _nvcc() -> str:

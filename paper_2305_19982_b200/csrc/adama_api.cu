@@ -151,6 +151,17 @@ adama_status check_apply_args(adama_ctx *ctx, float *w, float *m, float *v, size
     return ADAMA_OK;
 }
 
+// Walks a list in ranges of at most `most` tensors: launch(first, count) for each.
+template <typename Launch>
+adama_status for_ranges(adama_ctx *ctx, int count, int most, const char *what, Launch launch) {
+    for (int first = 0; first < count; first += most) {
+        const int k = count - first < most ? count - first : most;
+        cudaError_t e = launch(first, k);
+        if (e != cudaSuccess) return cuda_fail(ctx, what, e);
+    }
+    return ADAMA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -539,6 +550,260 @@ adama_status adama_apply_multi(adama_ctx *ctx, float *const *w, float *const *m,
     return ADAMA_OK;
 }
 
+// ---- the end of a fine-tuning step ------------------------------------------------------------
+
+static bool any_element(const size_t *n, int first, int count) {
+    for (int i = first; i < first + count; ++i)
+        if (n[i] > 0) return true;
+    return false;
+}
+
+static adama_status check_state8(adama_ctx *ctx, const adama_state8 &s, size_t n) {
+    if (n > 0 && (!s.m_codes || !s.m_scale || !s.v_codes || !s.v_scale))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "state8: null pointer");
+    if (!aligned_to(s.m_scale, 4) || !aligned_to(s.v_scale, 4))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "state8: scales not aligned to 4 bytes");
+    return ADAMA_OK;
+}
+
+static adama_status fold_apply_impl(adama_ctx *ctx, const void *const *grads, adama_dtype gdt,
+                                    float *const *w, float *const *m, float *const *v,
+                                    const adama_state8 *states, void *const *w_bf16, const size_t *n,
+                                    int count, double lr, const float *grad_factor, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    const bool packed = states != nullptr;
+    if (count < 0 || (count > 0 && (!grads || !w || !n || (!packed && (!m || !v)))))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "fold_apply: null list or negative count");
+    if (gdt != ADAMA_F32 && gdt != ADAMA_BF16)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "fold_apply: unknown gradient dtype");
+    if (!isfinite(lr)) return fail(ctx, ADAMA_ERR_INVALID_ARG, "fold_apply: lr is not finite");
+    if (ctx->n_micro < 1 || ctx->t < 1)
+        return fail(ctx, ADAMA_ERR_BAD_STATE, "fold_apply: adama_begin_minibatch has not been called");
+    if (!aligned_to(grad_factor, 4))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "fold_apply: grad_factor not aligned to 4 bytes");
+    for (int i = 0; i < count; ++i) {
+        if (n[i] > 0 && (!grads[i] || !w[i] || (!packed && (!m[i] || !v[i]))))
+            return fail(ctx, ADAMA_ERR_INVALID_ARG, "fold_apply: null pointer");
+        if (!aligned_to(grads[i], dtype_size(gdt)) || !aligned_to(w[i], 4) ||
+            (!packed && (!aligned_to(m[i], 4) || !aligned_to(v[i], 4))) ||
+            (w_bf16 && !aligned_to(w_bf16[i], 2)))
+            return fail(ctx, ADAMA_ERR_MISALIGNED, "fold_apply: pointer not aligned to its element size");
+        if (packed) {
+            adama_status st = check_state8(ctx, states[i], n[i]);
+            if (st != ADAMA_OK) return st;
+        }
+    }
+    DeviceGuard guard(ctx->cfg.device);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const adama::ApplyConstants c = adama::make_apply_constants(
+        ctx->cfg.beta1, ctx->cfg.beta2, ctx->cfg.eps, ctx->t, lr, 1, false, ctx->weight_decay);
+    cudaError_t e = join_copyback(ctx, stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, "fold_apply", e);
+    adama::StepList list;
+    list.g = grads;
+    list.w = w;
+    list.m = m;
+    list.v = v;
+    list.s8 = states;
+    list.copy = w_bf16;
+    list.n = n;
+    return for_ranges(ctx, count, packed ? adama::kStep8Max : adama::kStepMax, "fold_apply launch",
+                      [&](int first, int k) {
+        if (!any_element(n, first, k)) return cudaSuccess;
+        ctx->launches += 1;
+        return packed ? adama::launch_fold_apply8_multi(list, gdt, first, k, ctx->fold_c, c, grad_factor,
+                                                        ctx->sm_count, stream)
+                      : adama::launch_fold_apply_multi(list, gdt, first, k, ctx->fold_c, c, grad_factor,
+                                                       ctx->sm_count, stream);
+    });
+}
+
+adama_status adama_fold_apply_multi(adama_ctx *ctx, const void *const *grads, adama_dtype gdt,
+                                    float *const *w, float *const *m, float *const *v,
+                                    void *const *w_bf16, const size_t *n, int count, double lr,
+                                    const float *grad_factor, void *cuda_stream) {
+    return fold_apply_impl(ctx, grads, gdt, w, m, v, nullptr, w_bf16, n, count, lr, grad_factor, cuda_stream);
+}
+
+adama_status adama_fold_apply8_multi(adama_ctx *ctx, const void *const *grads, adama_dtype gdt,
+                                     float *const *w, const adama_state8 *states, void *const *w_bf16,
+                                     const size_t *n, int count, double lr, const float *grad_factor,
+                                     void *cuda_stream) {
+    static const adama_state8 none = {nullptr, nullptr, nullptr, nullptr};
+    if (ctx && count > 0 && !states)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "fold_apply8: null list of states");
+    return fold_apply_impl(ctx, grads, gdt, w, nullptr, nullptr, states ? states : &none, w_bf16, n, count, lr,
+                           grad_factor, cuda_stream);
+}
+
+static adama_status state8_convert(adama_ctx *ctx, bool pack, float *const *m, float *const *v,
+                                   const adama_state8 *states, const size_t *n, int count,
+                                   void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (count < 0 || (count > 0 && (!m || !v || !states || !n)))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "state8: null list or negative count");
+    for (int i = 0; i < count; ++i) {
+        if (n[i] > 0 && (!m[i] || !v[i])) return fail(ctx, ADAMA_ERR_INVALID_ARG, "state8: null pointer");
+        if (!aligned_to(m[i], 4) || !aligned_to(v[i], 4))
+            return fail(ctx, ADAMA_ERR_MISALIGNED, "state8: moments not aligned to 4 bytes");
+        adama_status st = check_state8(ctx, states[i], n[i]);
+        if (st != ADAMA_OK) return st;
+    }
+    DeviceGuard guard(ctx->cfg.device);
+    adama::StepList list;
+    list.m = m;
+    list.v = v;
+    list.s8 = states;
+    list.n = n;
+    return for_ranges(ctx, count, adama::kStep8Max, "state8 launch", [&](int first, int k) {
+        if (!any_element(n, first, k)) return cudaSuccess;
+        ctx->launches += 1;
+        return adama::launch_state8_convert(list, pack, first, k, ctx->sm_count,
+                                            static_cast<cudaStream_t>(cuda_stream));
+    });
+}
+
+adama_status adama_state8_pack_multi(adama_ctx *ctx, const float *const *m, const float *const *v,
+                                     const adama_state8 *states, const size_t *n, int count,
+                                     void *cuda_stream) {
+    // the kernel only reads m and v in this direction
+    return state8_convert(ctx, true, const_cast<float *const *>(m), const_cast<float *const *>(v), states, n,
+                          count, cuda_stream);
+}
+
+adama_status adama_state8_unpack_multi(adama_ctx *ctx, const adama_state8 *states, float *const *m,
+                                       float *const *v, const size_t *n, int count, void *cuda_stream) {
+    return state8_convert(ctx, false, m, v, states, n, count, cuda_stream);
+}
+
+adama_status adama_grad_norm_multi(adama_ctx *ctx, const void *const *grads, adama_dtype gdt,
+                                   const size_t *n, int count, double max_norm, int accumulate,
+                                   adama_grad_norm *out, void *workspace, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (count < 0 || (count > 0 && (!grads || !n)) || !out || !workspace)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "grad_norm: null pointer or negative count");
+    if (gdt != ADAMA_F32 && gdt != ADAMA_BF16)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "grad_norm: unknown gradient dtype");
+    if (!(max_norm > 0.0)) return fail(ctx, ADAMA_ERR_INVALID_ARG, "grad_norm: max_norm must be > 0");
+    if (!aligned_to(out, 8) || !aligned_to(workspace, 16))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "grad_norm: out needs 8-byte, workspace 16-byte alignment");
+    for (int i = 0; i < count; ++i) {
+        if (n[i] > 0 && !grads[i]) return fail(ctx, ADAMA_ERR_INVALID_ARG, "grad_norm: null pointer");
+        if (!aligned_to(grads[i], dtype_size(gdt)))
+            return fail(ctx, ADAMA_ERR_MISALIGNED, "grad_norm: pointer not aligned to its element size");
+    }
+    DeviceGuard guard(ctx->cfg.device);
+    auto launch = [&](int first, int k) {
+        ctx->launches += 1;
+        return adama::launch_grad_norm(grads + first, gdt, n + first, k, (float)max_norm,
+                                       accumulate || first > 0, out, workspace, ctx->sm_count,
+                                       static_cast<cudaStream_t>(cuda_stream));
+    };
+    if (count == 0) {  // still writes the result of the empty sum
+        static const void *const no_grads[1] = {nullptr};
+        static const size_t no_n[1] = {0};
+        grads = no_grads;
+        n = no_n;
+        count = 1;
+    }
+    return for_ranges(ctx, count, adama::kNormMax, "grad_norm launch", launch);
+}
+
+static adama_status check_logits(adama_ctx *ctx, const void *logits, adama_dtype dt, int64_t rows,
+                                 int64_t vocab, int64_t ld, const int64_t *targets, double logit_scale) {
+    if (rows < 0 || vocab < 1 || vocab > INT32_MAX || ld < vocab)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: bad shape or a row pitch smaller than the row");
+    if (dt != ADAMA_F32 && dt != ADAMA_BF16)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: unknown dtype");
+    if (rows > 0 && (!logits || !targets)) return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: null pointer");
+    if (!(logit_scale > 0.0) || !isfinite(logit_scale))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: logit_scale must be finite and > 0");
+    if (!aligned_to(logits, dtype_size(dt)) || !aligned_to(targets, 8))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "logits: pointer not aligned to its element size");
+    return ADAMA_OK;
+}
+
+adama_status adama_token_logprobs(adama_ctx *ctx, const void *logits, adama_dtype dt, int64_t rows,
+                                  int64_t vocab, int64_t ld, const int64_t *targets, double logit_scale,
+                                  float *logp, float *lse, float *entropy, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    adama_status st = check_logits(ctx, logits, dt, rows, vocab, ld, targets, logit_scale);
+    if (st != ADAMA_OK) return st;
+    if (rows > 0 && !logp) return fail(ctx, ADAMA_ERR_INVALID_ARG, "token_logprobs: null output");
+    if (!aligned_to(logp, 4) || !aligned_to(lse, 4) || !aligned_to(entropy, 4))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "token_logprobs: output not aligned to 4 bytes");
+    if (rows == 0) return ADAMA_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    adama::LogprobArgs a;
+    a.logits = logits;
+    a.dtype = dt;
+    a.rows = rows;
+    a.vocab = vocab;
+    a.ld = ld;
+    a.targets = targets;
+    a.scale = logit_scale;
+    a.logp = logp;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.status = ctx->status_dev;
+    cudaError_t e = adama::launch_token_logprobs(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(ctx, "token_logprobs launch", e);
+    ctx->launches += 1;
+    return ADAMA_OK;
+}
+
+adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args *p, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (!p) return fail(ctx, ADAMA_ERR_INVALID_ARG, "policy_loss: null arguments");
+    adama_status st = check_logits(ctx, p->logits, p->logits_dtype, p->rows, p->vocab, p->ld_logits,
+                                   p->targets, p->logit_scale);
+    if (st != ADAMA_OK) return st;
+    if (p->dlogits_dtype != ADAMA_F32 && p->dlogits_dtype != ADAMA_BF16)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "policy_loss: unknown gradient dtype");
+    if (!p->stats || !p->workspace ||
+        (p->rows > 0 && (!p->old_logp || !p->advantages || !p->weights)))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "policy_loss: null pointer");
+    if (p->dlogits && p->ld_dlogits < p->vocab)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "policy_loss: row pitch of dlogits smaller than the row");
+    if (p->dlogits == p->logits && p->rows > 0 &&
+        (p->dlogits_dtype != p->logits_dtype || p->ld_dlogits != p->ld_logits))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "policy_loss: in place needs one dtype and one pitch");
+    if (!(p->clip_low >= 0.0) || !(p->clip_low <= 1.0) || !(p->clip_high >= 0.0) || !isfinite(p->kl_coef))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "policy_loss: clip range or kl_coef out of range");
+    if (!aligned_to(p->dlogits, dtype_size(p->dlogits_dtype)) || !aligned_to(p->old_logp, 4) ||
+        !aligned_to(p->ref_logp, 4) || !aligned_to(p->advantages, 4) || !aligned_to(p->weights, 4) ||
+        !aligned_to(p->logp, 4) || !aligned_to(p->stats, 4) || !aligned_to(p->workspace, 16))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "policy_loss: pointer not aligned");
+    DeviceGuard guard(ctx->cfg.device);
+    adama::PolicyArgs a;
+    a.logits = p->logits;
+    a.dlogits = p->dlogits;
+    a.logits_dtype = p->logits_dtype;
+    a.dlogits_dtype = p->dlogits_dtype;
+    a.rows = p->rows;
+    a.vocab = p->vocab;
+    a.ld_logits = p->ld_logits;
+    a.ld_dlogits = p->ld_dlogits;
+    a.targets = p->targets;
+    a.old_logp = p->old_logp;
+    a.ref_logp = p->ref_logp;
+    a.advantages = p->advantages;
+    a.weights = p->weights;
+    a.scale_exact = p->logit_scale;
+    a.scale = (float)p->logit_scale;
+    a.ratio_min = (float)(1.0 - p->clip_low);
+    a.ratio_max = (float)(1.0 + p->clip_high);
+    a.kl_coef = (float)p->kl_coef;
+    a.logp = p->logp;
+    a.stats = p->stats;
+    a.workspace = p->workspace;
+    a.status = ctx->status_dev;
+    cudaError_t e = adama::launch_policy_loss(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(ctx, "policy_loss launch", e);
+    ctx->launches += 1;
+    return ADAMA_OK;
+}
+
 // ---- host-buffer variants -------------------------------------------------------------------
 
 adama_status adama_fold_host(adama_ctx *ctx, const void *grad_host, adama_dtype gdt, float *m,
@@ -745,6 +1010,11 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
     if (host[0] != adama::kDevOk) {
         e = cudaMemsetAsync(ctx->status_dev, 0, 256, stream);
         if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+        if (host[0] == adama::kDevBadTarget) {
+            snprintf(ctx->err, sizeof(ctx->err), "a row of logits had a target outside the vocabulary (row %llu)",
+                     (unsigned long long)host[2] << 32 | host[1]);
+            return ADAMA_ERR_INVALID_ARG;
+        }
         snprintf(ctx->err, sizeof(ctx->err),
                  "device-side wait expired in the fused weight-gradient kernel "
                  "(code %u, wait %u, tile %u)",

@@ -50,8 +50,9 @@ ApplyConstants make_apply_constants(double beta1, double beta2, double eps, int6
                                     int world = 1, bool sharded = false, double weight_decay = 0.0);
 
 // Status block in device memory (256 bytes): word 0 = first error code recorded
-// by a kernel (0 = none), word 1 = which wait, word 2 = tile; rest reserved.
-enum DeviceErr : unsigned { kDevOk = 0, kDevTimeout = 1 };
+// by a kernel (0 = none), word 1 = which wait, word 2 = tile (bad target: the row, low and high
+// half); rest reserved.
+enum DeviceErr : unsigned { kDevOk = 0, kDevTimeout = 1, kDevBadTarget = 2 };
 
 // streaming kernels (fold_apply.cu)
 cudaError_t launch_fold(const void *grad, adama_dtype gdt, float *m, float *v, size_t n,
@@ -78,6 +79,73 @@ cudaError_t launch_fold_multi(const void *const *g, adama_dtype gdt, float *cons
                               int sm_count, cudaStream_t stream);
 cudaError_t launch_apply_multi(float *const *w, float *const *m, float *const *v, const size_t *n,
                                int count, ApplyConstants c, int sm_count, cudaStream_t stream);
+
+// one-pass fold + apply over many tensors, states in 32 bits (fold_apply_multi.cu) or in 8 (state8.cu).
+// Tables of up to kStepSmall tensors travel as 3-4 KB of kernel parameters, larger ones as 20-30 KB.
+constexpr int kStepSmall = 64;
+constexpr int kStepMax = 512;
+constexpr int kStep8Max = 448;
+constexpr int kStateBlock = ADAMA_STATE8_BLOCK;
+struct StepList {  // host arrays; each launch takes a range of them
+    const void *const *g = nullptr;
+    float *const *w = nullptr;
+    float *const *m = nullptr;
+    float *const *v = nullptr;
+    const adama_state8 *s8 = nullptr;
+    void *const *copy = nullptr;  // bf16 weight copies; may be null, entries may be null
+    const size_t *n = nullptr;
+};
+cudaError_t launch_fold_apply_multi(const StepList &s, adama_dtype gdt, int first, int count,
+                                    FoldConstants f, ApplyConstants c, const float *factor,
+                                    int sm_count, cudaStream_t stream);
+cudaError_t launch_fold_apply8_multi(const StepList &s, adama_dtype gdt, int first, int count,
+                                     FoldConstants f, ApplyConstants c, const float *factor,
+                                     int sm_count, cudaStream_t stream);
+// pack: m, v -> s8; otherwise s8 -> m, v
+cudaError_t launch_state8_convert(const StepList &s, bool pack, int first, int count, int sm_count,
+                                  cudaStream_t stream);
+
+// Workspace of the reductions: zero before its first use, the ticket is zero again after each launch.
+constexpr int kWorkspaceParts = (ADAMA_WORKSPACE_BYTES - 64) / 8;
+struct Workspace {
+    unsigned ticket;
+    unsigned reserved[15];
+    double part[kWorkspaceParts];
+};
+static_assert(sizeof(Workspace) == ADAMA_WORKSPACE_BYTES, "as the header states");
+
+// gradient norm over a list (grad_norm.cu)
+constexpr int kNormMax = 1024;
+cudaError_t launch_grad_norm(const void *const *g, adama_dtype gdt, const size_t *n, int count,
+                             float max_norm, int accumulate, adama_grad_norm *out, void *workspace,
+                             int sm_count, cudaStream_t stream);
+
+// rows of logits (policy_loss.cu)
+struct LogprobArgs {
+    const void *logits;
+    adama_dtype dtype;
+    int64_t rows, vocab, ld;
+    const int64_t *targets;
+    double scale;
+    float *logp, *lse, *entropy;  // lse, entropy may be null
+    unsigned *status;
+};
+cudaError_t launch_token_logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream);
+struct PolicyArgs {
+    const void *logits;
+    void *dlogits;  // may be null: no gradient
+    adama_dtype logits_dtype, dlogits_dtype;
+    int64_t rows, vocab, ld_logits, ld_dlogits;
+    const int64_t *targets;
+    const float *old_logp, *ref_logp, *advantages, *weights;  // ref_logp may be null
+    double scale_exact;
+    float scale, ratio_min, ratio_max, kl_coef;
+    float *logp;  // may be null
+    float *stats;
+    void *workspace;
+    unsigned *status;
+};
+cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream);
 
 // fused reduce-scatter + sharded apply + all-gather over peer-mapped buffers (peer_apply.cu)
 constexpr int kMaxPeers = 16;
