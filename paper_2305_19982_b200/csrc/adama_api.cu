@@ -1016,9 +1016,9 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
             return ADAMA_ERR_INVALID_ARG;
         }
         snprintf(ctx->err, sizeof(ctx->err),
-                 "device-side wait expired in the fused weight-gradient kernel "
-                 "(code %u, wait %u, tile %u)",
-                 host[0], host[1], host[2]);
+                 "device-side wait expired in the %s kernel (code %u, wait %u, tile %u)",
+                 host[1] == adama::kWaitPolicyRing ? "policy-loss" : "fused weight-gradient", host[0], host[1],
+                 host[2]);
         return ADAMA_ERR_TIMEOUT;
     }
     return ADAMA_OK;

@@ -53,6 +53,7 @@ ApplyConstants make_apply_constants(double beta1, double beta2, double eps, int6
 // by a kernel (0 = none), word 1 = which wait, word 2 = tile (bad target: the row, low and high
 // half); rest reserved.
 enum DeviceErr : unsigned { kDevOk = 0, kDevTimeout = 1, kDevBadTarget = 2 };
+constexpr unsigned kWaitPolicyRing = 100;  // word 1 for the waits of the policy loss's ring
 
 // streaming kernels (fold_apply.cu)
 cudaError_t launch_fold(const void *grad, adama_dtype gdt, float *m, float *v, size_t n,

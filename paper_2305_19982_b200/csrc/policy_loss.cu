@@ -4,123 +4,19 @@
 //     r = exp(logp - old),  pg = -min(r*A, clamp(r, 1-cl, 1+ch)*A),  d = ref - logp,
 //     kl = exp(d) - d - 1,  loss += w*(pg + beta*kl)
 //     dlogits_j = w*s*c*([j = target] - p_j),  c = -(r*A while r*A <= the clamped product) + beta*(1 - exp(d))
-#include <math_constants.h>
+// A row is read once (loss: and its gradient written once); what bounds every form is HBM.
+#include <atomic>
 
 #include "adama_device.cuh"
+#include "bulk_copy.cuh"
+#include "softmax_rows.cuh"
 #include "tensor_table.cuh"
 
 namespace adama {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 512;  // that work on rows, in every kernel here
 constexpr int kWarps = kThreads / 32;
-
-// Softmax statistics of a set of logits, with k = s*log2(e): the largest one, the sum of
-// 2^(k*(x - top)) and that of the same times k*(x - top).  The difference is formed first: a common
-// offset of the logits, or the lowest value of their type as a mask, then costs neither precision
-// nor range.  An empty set, or one of -inf alone, has top = -inf and sums of zero.
-struct Stats {
-    float top, sum, wsum;
-};
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
-// Statistics of a union: both brought to the larger top.
-__device__ __forceinline__ Stats join(const Stats &a, const Stats &b, float k) {
-    Stats r;
-    r.top = fmaxf(a.top, b.top);
-    const float da = a.top == r.top ? 0.f : k * (a.top - r.top), db = b.top == r.top ? 0.f : k * (b.top - r.top);
-    const float ea = exp2_fast(da), eb = exp2_fast(db);
-    r.sum = a.sum * ea + b.sum * eb;
-    // an empty side has weight 0 and distance -inf: its product is left out
-    r.wsum = (ea > 0.f ? ea * (a.wsum + a.sum * da) : 0.f) + (eb > 0.f ? eb * (b.wsum + b.sum * db) : 0.f);
-    return r;
-}
-
-template <int N>
-__device__ __forceinline__ void add(Stats &s, const float (&x)[N], float k) {
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
-    if (top > s.top) {
-        const float d = s.top == -CUDART_INF_F ? 0.f : k * (s.top - top), e = exp2_fast(d);
-        s.wsum = e > 0.f ? e * (s.wsum + s.sum * d) : 0.f;
-        s.sum *= e;
-        s.top = top;
-    }
-    const float ref = s.top == -CUDART_INF_F ? 0.f : s.top;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float d = k * (x[i] - ref), e = exp2_fast(d);
-        s.sum += e;
-        s.wsum += e * fmaxf(d, -1e30f);  // -inf has e = 0
-    }
-}
-
-// eight consecutive logits, widened exactly; the pointer is 16-byte aligned.  Not a read-only load:
-// the gradient may be written over the logits.
-__device__ __forceinline__ void load_row8(const float *p, float (&x)[8]) {
-    const float4 a = ld_stream(reinterpret_cast<const float4 *>(p)), b = ld_stream(reinterpret_cast<const float4 *>(p) + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void load_row8(const __nv_bfloat16 *p, float (&x)[8]) {
-    const float4 t = ld_stream(reinterpret_cast<const float4 *>(p));
-    const unsigned u[4] = {__float_as_uint(t.x), __float_as_uint(t.y), __float_as_uint(t.z), __float_as_uint(t.w)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {  // bf16 -> fp32 is a 16-bit left shift
-        x[2 * i] = __uint_as_float(u[i] << 16);
-        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-}
-
-__device__ __forceinline__ Stats shfl_join(Stats s, float k) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Stats b;
-        b.top = __shfl_xor_sync(0xffffffffu, s.top, o);
-        b.sum = __shfl_xor_sync(0xffffffffu, s.sum, o);
-        b.wsum = __shfl_xor_sync(0xffffffffu, s.wsum, o);
-        s = join(s, b, k);
-    }
-    return s;
-}
-
-template <typename T>
-__device__ __forceinline__ int head_of_row(const T *x, int64_t vocab) {
-    const int mis = (int)((reinterpret_cast<uintptr_t>(x) % 16) / sizeof(T));
-    const int64_t head = mis ? 16 / sizeof(T) - mis : 0;
-    return (int)(head < vocab ? head : vocab);
-}
-
-// Statistics of a whole row by the CTA; every thread gets them.
-template <typename T>
-__device__ __forceinline__ Stats row_stats(const T *x, int64_t vocab, float k, Stats *shared) {
-    Stats s = {-CUDART_INF_F, 0.f, 0.f};
-    const int head = head_of_row(x, vocab);
-    const int64_t body = (vocab - head) / 8;
-    for (int64_t i = threadIdx.x; i < body; i += kThreads) {
-        float v[8];
-        load_row8(x + head + 8 * i, v);
-        add(s, v, k);
-    }
-    const int64_t tail0 = head + 8 * body;
-    for (int64_t i = threadIdx.x; i < head + (vocab - tail0); i += kThreads) {
-        const float v[1] = {widen(x[i < head ? i : tail0 + (i - head)])};
-        add(s, v, k);
-    }
-    s = shfl_join(s, k);
-    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = s;
-    __syncthreads();
-    s = shared[0];
-    for (int i = 1; i < kWarps; ++i) s = join(s, shared[i], k);
-    __syncthreads();
-    return s;
-}
 
 __device__ __forceinline__ void record_bad_target(unsigned *status, int64_t row) {
     if (atomicCAS(status, (unsigned)kDevOk, (unsigned)kDevBadTarget) == (unsigned)kDevOk) {
@@ -129,190 +25,629 @@ __device__ __forceinline__ void record_bad_target(unsigned *status, int64_t row)
     }
 }
 
-template <typename T>
+// Barrier of the W warps that share a row: group g of the CTA.
+template <int W>
+__device__ __forceinline__ void group_sync(int g) {
+    if (W == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(W * 32) : "memory");
+}
+
+// Union over the W warps of a group, in every thread; `slots` (W of them) are the group's own, and
+// are free again after the caller's next group_sync.
+template <int W, bool ENT>
+__device__ __forceinline__ Stats group_join(Stats s, float k, Stats *slots, int g) {
+    s = warp_join<ENT>(s, k);
+    if (W == 1) return s;
+    const int lane = threadIdx.x % 32;
+    if (lane == 0) slots[threadIdx.x / 32 % W] = s;
+    group_sync<W>(g);
+    const Stats none = {-CUDART_INF_F, 0.f, 0.f};
+    return warp_join<ENT>(lane < W ? slots[lane] : none, k);
+}
+
+__device__ __forceinline__ float logp_of(float x_target, const Stats &s, float log2sum, float k) {
+    return CUDART_LN2_F * (k * (x_target - s.top) - log2sum);
+}
+
+// ---- token log-probabilities -----------------------------------------------------------------
+
+// W warps to a row, kLoads units of each thread in flight; a CTA holds 16/W rows.
+constexpr int kLoads = 4;
+
+template <typename T, int W, bool ENT>
 __global__ void __launch_bounds__(kThreads)
 token_logprobs_kernel(const LogprobArgs a, float k) {
+    constexpr int kGroupThreads = 32 * W, kGroups = kWarps / W;
     __shared__ Stats shared[kWarps];
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int g = threadIdx.x / kGroupThreads, t = threadIdx.x % kGroupThreads;
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + g; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
         const int64_t target = a.targets[row];
         const T *x = static_cast<const T *>(a.logits) + row * a.ld;
         float logp = 0.f, lse = 0.f, entropy = 0.f;
         if (target >= 0) {
-            const Stats s = row_stats(x, a.vocab, k, shared);
+            const bool inside = target < a.vocab;
+            const float x_target = inside ? widen(x[target]) : CUDART_NAN_F;
+            const RowShape shape = row_shape(x, (int)a.vocab);
+            const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
+            Running<ENT> run;
+            int i = t;
+            for (; i + (kLoads - 1) * kGroupThreads < shape.units; i += kLoads * kGroupThreads) {
+                uint4 u[kLoads];
+#pragma unroll
+                for (int j = 0; j < kLoads; ++j) u[j] = ld_unit(body + i + j * kGroupThreads);
+                run.template add_units<T>(u, k);
+            }
+            for (; i < shape.units; i += kGroupThreads) {
+                const uint4 u[1] = {ld_unit(body + i)};
+                run.template add_units<T>(u, k);
+            }
+            if (t < shape.head + shape.tail) run.add_one(widen(x[extra_index<T>(shape, t)]), k);
+            const Stats s = group_join<W, ENT>(run.stats(), k, shared + g * W, g);
             const float log2sum = log2f(s.sum);
             lse = fmaf(s.top, (float)a.scale, CUDART_LN2_F * log2sum);
-            logp = target < a.vocab ? CUDART_LN2_F * (k * (widen(x[target]) - s.top) - log2sum) : CUDART_NAN_F;
-            entropy = CUDART_LN2_F * (log2sum - s.wsum / s.sum);
-            if (target >= a.vocab && threadIdx.x == 0) record_bad_target(a.status, row);
+            logp = logp_of(x_target, s, log2sum, k);
+            if (ENT) entropy = CUDART_LN2_F * (log2sum - s.wsum / s.sum);
+            if (!inside && t == 0) record_bad_target(a.status, row);
         }
-        if (threadIdx.x == 0) {
+        if (t == 0) {
             a.logp[row] = logp;
             if (a.lse) a.lse[row] = lse;
-            if (a.entropy) a.entropy[row] = entropy;
+            if (ENT) a.entropy[row] = entropy;
         }
+        if (W > 1) group_sync<W>(g);  // the slots are used again
     }
 }
 
-// Loss terms of one row and its slope dloss/dlogp (without weight and scale).
-struct Terms {
-    float pg, kl, cut, slope;
+// ---- policy loss: parts shared by its forms ---------------------------------------------------
+
+// What a row brings beside its logits.
+struct RowIn {
+    int64_t target;
+    float weight, old, adv, ref;
+
+    __device__ __forceinline__ bool live() const { return weight != 0.f && target >= 0; }
 };
-__device__ __forceinline__ Terms loss_terms(float logp, float old, float adv, const float *ref, int64_t row,
-                                            const PolicyArgs &a) {
-    Terms t;
-    const float r = expf(logp - old), plain = r * adv;
-    const float clipped = fminf(fmaxf(r, a.ratio_min), a.ratio_max) * adv;
-    const bool cut = plain > clipped;
-    t.pg = -(cut ? clipped : plain);
-    t.cut = cut ? 1.f : 0.f;
-    t.slope = cut ? 0.f : -plain;
-    t.kl = 0.f;
-    if (ref) {
-        const float d = ref[row] - logp, e = expf(d);
-        t.kl = e - d - 1.f;
-        t.slope += a.kl_coef * (1.f - e);
-    }
-    if (r != r) t.pg = t.slope = r;  // a NaN log-probability stays visible
-    return t;
+__device__ __forceinline__ RowIn row_in(const PolicyArgs &a, int64_t row) {
+    RowIn r;
+    r.target = a.targets[row];
+    r.weight = a.weights[row];
+    r.old = a.old_logp[row];
+    r.adv = a.advantages[row];
+    r.ref = a.ref_logp ? a.ref_logp[row] : 0.f;
+    return r;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_out8(T *p, const float (&y)[8]);
+// One row's loss terms and its gradient: dlogits_j = unit*[j = target] + per_e*2^(k*(x_j - top)).
+struct RowOut {
+    float logp, pg, kl, cut, unit, per_e;
+};
+__device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, const Stats &s, float x_target, float k) {
+    RowOut o;
+    o.logp = logp_of(x_target, s, log2f(s.sum), k);
+    const float r = expf(o.logp - in.old), plain = r * in.adv;
+    const float clipped = fminf(fmaxf(r, a.ratio_min), a.ratio_max) * in.adv;
+    const bool cut = plain > clipped;
+    o.pg = -(cut ? clipped : plain);
+    o.cut = cut ? 1.f : 0.f;
+    float slope = cut ? 0.f : -plain;
+    o.kl = 0.f;
+    if (a.ref_logp) {
+        const float d = in.ref - o.logp, e = expf(d);
+        o.kl = e - d - 1.f;
+        slope += a.kl_coef * (1.f - e);
+    }
+    if (r != r) o.pg = slope = r;  // a NaN log-probability stays visible
+    o.unit = in.weight * slope * a.scale;
+    o.per_e = -o.unit / s.sum;
+    return o;
+}
+
+// Sums of one thread over its rows; in double, so that their order does not show in fp32.
+struct Sums {
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+
+    __device__ __forceinline__ void add(const PolicyArgs &a, const RowIn &in, const RowOut &o) {
+        const double w = in.weight;
+        v[0] += w * (o.pg + (a.ref_logp ? a.kl_coef * o.kl : 0.f));
+        v[1] += w * o.pg;
+        v[2] += w * o.kl;
+        v[3] += w * o.cut;
+    }
+};
+
+// The threads' sums -> the CTA's in the workspace -> stats, by the last CTA, in the CTAs' order.
+// All kThreads call it; `slots` holds kWarps doubles.
+__device__ __forceinline__ void finish_stats(const PolicyArgs &a, Sums s, double (*slots)[4], volatile int *last,
+                                             int t) {
+    Workspace *ws = static_cast<Workspace *>(a.workspace);
+    const auto cta_sum = [&]() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            for (int o = 16; o > 0; o >>= 1) s.v[i] += __shfl_down_sync(0xffffffffu, s.v[i], o);
+            if (t % 32 == 0) slots[t / 32][i] = s.v[i];
+        }
+        asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+    };
+    cta_sum();
+    if (t < 4) {
+        double sum = 0.0;
+        for (int w = 0; w < kWarps; ++w) sum += slots[w][t];
+        ws->part[4 * blockIdx.x + t] = sum;
+        __threadfence();
+    }
+    asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+    if (t == 0) *last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
+    asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+    if (!*last) return;
+    __threadfence();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s.v[i] = 0.0;
+        for (unsigned b = t; b < gridDim.x; b += kThreads) s.v[i] += __ldcg(&ws->part[4 * b + i]);
+    }
+    cta_sum();
+    if (t < 4) {
+        double sum = 0.0;
+        for (int w = 0; w < kWarps; ++w) sum += slots[w][t];
+        a.stats[t] = (float)sum;
+    }
+    if (t == 0) ws->ticket = 0;
+}
+
+template <typename O>
+__device__ __forceinline__ O narrow(float y);
 template <>
-__device__ __forceinline__ void store_out8(float *p, const float (&y)[8]) {
+__device__ __forceinline__ float narrow<float>(float y) { return y; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
+
+__device__ __forceinline__ void store_wide(float *p, const float (&y)[4]) {
+    st_stream(reinterpret_cast<float4 *>(p), make_float4(y[0], y[1], y[2], y[3]));
+}
+__device__ __forceinline__ void store_wide(float *p, const float (&y)[8]) {
     st_stream(reinterpret_cast<float4 *>(p), make_float4(y[0], y[1], y[2], y[3]));
     st_stream(reinterpret_cast<float4 *>(p) + 1, make_float4(y[4], y[5], y[6], y[7]));
 }
-template <>
-__device__ __forceinline__ void store_out8(__nv_bfloat16 *p, const float (&y)[8]) {
+__device__ __forceinline__ void store_wide(__nv_bfloat16 *p, const float (&y)[4]) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]));
+}
+__device__ __forceinline__ void store_wide(__nv_bfloat16 *p, const float (&y)[8]) {
     *reinterpret_cast<uint4 *>(p) = make_uint4(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]),
                                                pack2_bf16(y[4], y[5]), pack2_bf16(y[6], y[7]));
 }
-__device__ __forceinline__ void store1(float *p, float y) { *p = y; }
-__device__ __forceinline__ void store1(__nv_bfloat16 *p, float y) { *p = __float2bfloat16_rn(y); }
+
+// How a row's gradient is written.
+template <typename T, typename O>
+struct RowWriter {
+    static constexpr int N = kUnit<T>;
+    O *y;  // null: no gradient
+    bool wide;
+    int target;
+    float top, unit, per_e;
+    bool live;
+
+    __device__ __forceinline__ RowWriter(O *row, const RowShape &shape, bool live_, int64_t target_, float top_,
+                                         const RowOut &o)
+        : y(row), target((int)target_), top(top_), unit(o.unit), per_e(o.per_e), live(live_) {
+        constexpr int align = N * sizeof(O) < 16 ? N * sizeof(O) : 16;
+        wide = reinterpret_cast<uintptr_t>(row + shape.head) % align == 0;
+    }
+    // the unit of logits that begins at element j
+    __device__ __forceinline__ void put(const uint4 &u, int j, float k) const {
+        float v[N];
+        if (live) {
+            const Pair minus = pair(-top, -top), k2 = pair(k, k), per = pair(per_e, per_e);
+#pragma unroll
+            for (int q = 0; q < N / 2; ++q) {
+                float d0, d1;
+                split(mul2(add2(unit_pair<T>(u, q), minus), k2), d0, d1);
+                split(mul2(pair(exp2_fast(d0), exp2_fast(d1)), per), v[2 * q], v[2 * q + 1]);
+            }
+            if ((unsigned)(target - j) < (unsigned)N) {
+#pragma unroll
+                for (int q = 0; q < N; ++q)
+                    if (target - j == q) v[q] += unit;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < N; ++q) v[q] = 0.f;
+        }
+        if (wide) {
+            store_wide(y + j, v);
+        } else {
+#pragma unroll
+            for (int q = 0; q < N; ++q) y[j + q] = narrow<O>(v[q]);
+        }
+    }
+    __device__ __forceinline__ void put_one(float x, int j, float k) const {
+        float v = 0.f;
+        if (live) {
+            v = per_e * exp2_fast(k * (x - top));
+            if (j == target) v += unit;
+        }
+        y[j] = narrow<O>(v);
+    }
+};
+
+// ---- rows that fit a few warps' registers ------------------------------------------------------
+
+constexpr int kRowUnits = 8;  // units of a thread
+
+template <typename T, typename O, int W>
+__global__ void __launch_bounds__(kThreads)
+policy_loss_rows_kernel(const PolicyArgs a, float k) {
+    constexpr int kGroupThreads = 32 * W, kGroups = kWarps / W;
+    __shared__ Stats shared[kWarps];
+    __shared__ double sums[kWarps][4];
+    __shared__ int last;
+    const int g = threadIdx.x / kGroupThreads, t = threadIdx.x % kGroupThreads;
+    Sums acc;
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + g; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
+        const RowIn in = row_in(a, row);
+        const bool live = in.live();
+        const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+        const RowShape shape = row_shape(x, (int)a.vocab);
+        const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
+        const bool has_extra = t < shape.head + shape.tail;
+        const int extra = has_extra ? extra_index<T>(shape, t) : 0;
+        uint4 u[kRowUnits];
+        float x_extra = 0.f, top = 0.f;
+        RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (live) {
+            const bool inside = in.target < a.vocab;
+            const float x_target = inside ? widen(x[in.target]) : CUDART_NAN_F;
+#pragma unroll
+            for (int i = 0; i < kRowUnits; ++i)
+                if (t + i * kGroupThreads < shape.units) u[i] = ld_unit(body + t + i * kGroupThreads);
+            if (has_extra) x_extra = widen(x[extra]);
+            Running<false> run;
+#pragma unroll
+            for (int i = 0; i < kRowUnits; ++i) {
+                if (t + i * kGroupThreads < shape.units) {
+                    const uint4 one[1] = {u[i]};
+                    run.template add_units<T>(one, k);
+                }
+            }
+            if (has_extra) run.add_one(x_extra, k);
+            // the gradient may replace the logits: all have been read when the join is through
+            const Stats s = group_join<W, false>(run.stats(), k, shared + g * W, g);
+            top = s.top;
+            o = row_out(a, in, s, x_target, k);
+            if (t == 0) {
+                acc.add(a, in, o);
+                if (!inside) record_bad_target(a.status, row);
+            }
+        }
+        if (t == 0 && a.logp) a.logp[row] = o.logp;
+        if (a.dlogits) {
+            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, live, in.target, top, o);
+#pragma unroll
+            for (int i = 0; i < kRowUnits; ++i)
+                if (t + i * kGroupThreads < shape.units) out.put(u[i], shape.head + (t + i * kGroupThreads) * kUnit<T>, k);
+            if (has_extra) out.put_one(x_extra, extra, k);
+        }
+        if (W > 1) group_sync<W>(g);  // the slots are used again
+    }
+    finish_stats(a, acc, sums, &last, threadIdx.x);
+}
+
+// ---- longer rows: a ring in shared memory ------------------------------------------------------
+// A row, or its slice where a cluster of CTAs shares one, is brought to shared memory by bulk
+// copies, in stages of kStageBytes; the statistics are taken from the stages as they arrive, then the
+// gradient is computed from the same stages, each of which is refilled as soon as it has been used:
+// the next row streams in while this one's gradient streams out, and every logit crosses the HBM bus
+// once.  One producer warp, kThreads that compute.
+
+constexpr int kStageBytes = 16384;
+constexpr int kStages = 13;
+constexpr int kRingThreads = kThreads + 32;
+constexpr int kStageUnits = kStageBytes / 16;
+constexpr int kMaxCluster = 8;
+
+struct RingShared {
+    alignas(128) unsigned char stage[kStages][kStageBytes];
+    alignas(16) float4 peer[2][kMaxCluster];  // {top, sum, x_target} of the cluster's CTAs, for even and odd rows
+    unsigned long long full[kStages], empty[kStages], joined[2];
+    Stats slots[2][kWarps];  // for even and odd rows: a warp may be a row ahead of another
+    double sums[kWarps][4];
+    int last, give_up;
+};
+
+// The slice of a row's units that CTA `rank` of `size` takes.
+__device__ __forceinline__ void slice_of(int units, int rank, int size, int &from, int &count) {
+    from = (int)((int64_t)units * rank / size);
+    count = (int)((int64_t)units * (rank + 1) / size) - from;
+}
+
+template <typename T, typename O>
+__global__ void __launch_bounds__(kRingThreads, 1)
+policy_loss_ring_kernel(const PolicyArgs a, float k, int cluster) {
+    extern __shared__ unsigned char raw[];
+    RingShared &sh = *reinterpret_cast<RingShared *>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
+    const int t = threadIdx.x, lane = t % 32, warp = t / 32;
+    const int rank = cluster > 1 ? (int)cluster_rank() : 0;
+    const int64_t first = blockIdx.x / cluster, step = gridDim.x / cluster;
+    if (t == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            barrier_init(shared_addr(&sh.full[i]), 1);
+            barrier_init(shared_addr(&sh.empty[i]), kWarps);
+        }
+        for (int i = 0; i < 2; ++i) barrier_init(shared_addr(&sh.joined[i]), 1);
+        sh.give_up = 0;
+        barrier_init_fence();
+    }
+    __syncthreads();
+    if (cluster > 1) cluster_sync();  // the peers' barriers are ready before the first message
+
+    if (warp == kWarps) {
+        // ---- producer
+        if (lane == 0) {
+            uint32_t n = 0;  // stages issued
+            for (int64_t row = first; row < a.rows && !*(volatile int *)&sh.give_up; row += step) {
+                if (a.weights[row] == 0.f || a.targets[row] < 0) continue;
+                const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+                const RowShape shape = row_shape(x, (int)a.vocab);
+                int from, count;
+                slice_of(shape.units, rank, cluster, from, count);
+                const unsigned char *src = reinterpret_cast<const unsigned char *>(x + shape.head) + (size_t)from * 16;
+                for (int at = 0; at < count; at += kStageUnits, ++n) {
+                    const uint32_t slot = n % kStages, turn = n / kStages;
+                    if (turn > 0 && !barrier_wait(shared_addr(&sh.empty[slot]), (turn - 1) & 1, &sh.give_up)) break;
+                    const uint32_t bytes = 16u * (uint32_t)(count - at < kStageUnits ? count - at : kStageUnits);
+                    barrier_expect(shared_addr(&sh.full[slot]), bytes);
+                    bulk_load(shared_addr(sh.stage[slot]), src + (size_t)at * 16, bytes, shared_addr(&sh.full[slot]));
+                }
+            }
+            if (*(volatile int *)&sh.give_up) {  // copies in flight end before the CTA does
+                int none = 0;
+                for (uint32_t i = n > kStages ? n - kStages : 0; i < n; ++i)
+                    barrier_wait(shared_addr(&sh.full[i % kStages]), (i / kStages) & 1, &none);
+            }
+        }
+    } else {
+        Sums acc;
+        uint32_t n = 0, joins = 0;  // stages used, rows joined
+        RowIn next = {-1, 0.f, 0.f, 0.f, 0.f};
+        if (first < a.rows) next = row_in(a, first);
+        for (int64_t row = first; row < a.rows; row += step) {
+            const RowIn in = next;
+            if (row + step < a.rows) next = row_in(a, row + step);
+            const bool live = in.live();
+            const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+            const RowShape shape = row_shape(x, (int)a.vocab);
+            int from, count;
+            slice_of(shape.units, rank, cluster, from, count);
+            const bool has_extra = rank == 0 && t < shape.head + shape.tail;
+            const int extra = has_extra ? extra_index<T>(shape, t) : 0;
+            const uint32_t n0 = n;
+            float x_extra = 0.f, top = 0.f;
+            RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (live) {
+                const bool inside = in.target < a.vocab;
+                const float x_target = t == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
+                if (has_extra) x_extra = widen(x[extra]);
+                Running<false> run;
+                for (int at = 0; at < count; at += kStageUnits, ++n) {
+                    const uint32_t slot = n % kStages;
+                    barrier_wait(shared_addr(&sh.full[slot]), (n / kStages) & 1, &sh.give_up);
+                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[slot]);
+                    if (count - at >= kStageUnits) {
+                        uint4 u[kStageUnits / kThreads];
+#pragma unroll
+                        for (int i = 0; i < kStageUnits / kThreads; ++i) u[i] = units[t + i * kThreads];
+                        run.template add_units<T>(u, k);
+                    } else {
+                        for (int i = t; i < count - at; i += kThreads) {
+                            const uint4 u[1] = {units[i]};
+                            run.template add_units<T>(u, k);
+                        }
+                    }
+                }
+                if (has_extra) run.add_one(x_extra, k);
+                // the CTA's statistics, then the cluster's; thread 0's x_target travels with them
+                Stats s = warp_join<false>(run.stats(), k);
+                const int b = joins & 1;
+                if (lane == 0) sh.slots[b][warp] = {s.top, s.sum, x_target};
+                asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+                const Stats none = {-CUDART_INF_F, 0.f, 0.f};
+                const Stats mine = lane < kWarps ? sh.slots[b][lane] : none;
+                s = warp_join<false>(mine, k);
+                float xt = __shfl_sync(0xffffffffu, mine.wsum, 0);
+                if (cluster > 1) {
+                    const uint32_t bar = shared_addr(&sh.joined[b]);
+                    if (t == 0) barrier_expect(bar, 16u * cluster);
+                    if (t < cluster) send16(shared_addr(&sh.peer[b][rank]), bar, t, s.top, s.sum, xt, 0.f);
+                    barrier_wait(bar, (joins >> 1) & 1, &sh.give_up);
+                    Stats p = none;
+                    if (lane < cluster) {
+                        const float4 q = sh.peer[b][lane];
+                        p = {q.x, q.y, q.z};
+                    }
+                    s = warp_join<false>(p, k);
+                }
+                ++joins;
+                top = s.top;
+                o = row_out(a, in, s, xt, k);
+                if (t == 0 && rank == 0) {
+                    acc.add(a, in, o);
+                    if (!inside) record_bad_target(a.status, row);
+                }
+            }
+            if (t == 0 && rank == 0 && a.logp) a.logp[row] = o.logp;
+            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, live, in.target, top, o);
+            n = n0;
+            for (int at = 0; at < count; at += kStageUnits) {
+                const int here = count - at < kStageUnits ? count - at : kStageUnits;
+                const uint32_t slot = n % kStages;
+                const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[slot]);
+                const int j0 = shape.head + (from + at) * kUnit<T>;
+                if (a.dlogits)
+                    for (int i = t; i < here; i += kThreads) {
+                        uint4 u = make_uint4(0, 0, 0, 0);
+                        if (live) u = units[i];
+                        out.put(u, j0 + i * kUnit<T>, k);
+                    }
+                if (live) {
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
+                    ++n;
+                }
+            }
+            if (a.dlogits && has_extra) out.put_one(x_extra, extra, k);
+        }
+        if (t == 0 && sh.give_up && atomicCAS(a.status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
+            a.status[1] = kWaitPolicyRing;
+        finish_stats(a, acc, sh.sums, &sh.last, t);
+    }
+    if (cluster > 1) {
+        __syncwarp();
+        cluster_sync();  // no CTA ends while a peer may still send to it
+    }
+}
+
+// ---- rows that no cluster's shared memory holds: read twice --------------------------------------
 
 template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads)
-policy_loss_kernel(const PolicyArgs a, float k) {
+policy_loss_long_kernel(const PolicyArgs a, float k) {
     __shared__ Stats shared[kWarps];
-    __shared__ double sums[4][kWarps];
-    __shared__ bool last;
-    Workspace *ws = static_cast<Workspace *>(a.workspace);
-    double acc[4] = {0.0, 0.0, 0.0, 0.0};  // thread 0's
+    __shared__ double sums[kWarps][4];
+    __shared__ int last;
+    const int t = threadIdx.x;
+    Sums acc;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const int64_t target = a.targets[row];
-        const float weight = a.weights[row];
+        const RowIn in = row_in(a, row);
+        const bool live = in.live();
         const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
-        O *y = a.dlogits ? static_cast<O *>(a.dlogits) + row * a.ld_dlogits : nullptr;
-        float logp = 0.f, unit = 0.f, top = 0.f, per_e = 0.f;  // gradient: unit*one-hot + per_e*2^(k*(x - top))
-        const bool live = weight != 0.f && target >= 0;
+        const RowShape shape = row_shape(x, (int)a.vocab);
+        const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
+        const bool has_extra = t < shape.head + shape.tail;
+        const int extra = has_extra ? extra_index<T>(shape, t) : 0;
+        float x_extra = 0.f, top = 0.f;
+        RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (live) {
-            const Stats s = row_stats(x, a.vocab, k, shared);
-            const float log2sum = log2f(s.sum);
-            logp = target < a.vocab ? CUDART_LN2_F * (k * (widen(x[target]) - s.top) - log2sum) : CUDART_NAN_F;
+            const bool inside = in.target < a.vocab;
+            const float x_target = inside ? widen(x[in.target]) : CUDART_NAN_F;
+            if (has_extra) x_extra = widen(x[extra]);
+            Running<false> run;
+            for (int i = t; i < shape.units; i += kThreads) {
+                const uint4 u[1] = {ld_unit(body + i)};
+                run.template add_units<T>(u, k);
+            }
+            if (has_extra) run.add_one(x_extra, k);
+            const Stats s = group_join<kWarps, false>(run.stats(), k, shared, 0);
             top = s.top;
-            const Terms t = loss_terms(logp, a.old_logp[row], a.advantages[row], a.ref_logp, row, a);
-            unit = weight * t.slope * a.scale;
-            per_e = -unit / s.sum;
-            if (threadIdx.x == 0) {
-                acc[0] += (double)weight * (t.pg + (a.ref_logp ? a.kl_coef * t.kl : 0.f));
-                acc[1] += (double)weight * t.pg;
-                acc[2] += (double)weight * t.kl;
-                acc[3] += (double)weight * t.cut;
-                if (target >= a.vocab) record_bad_target(a.status, row);
+            o = row_out(a, in, s, x_target, k);
+            if (t == 0) {
+                acc.add(a, in, o);
+                if (!inside) record_bad_target(a.status, row);
             }
         }
-        if (threadIdx.x == 0 && a.logp) a.logp[row] = logp;
-        if (!y) continue;
-        const int head = head_of_row(x, a.vocab);
-        const int64_t body = (a.vocab - head) / 8, tail0 = head + 8 * body;
-        const bool wide = reinterpret_cast<uintptr_t>(y + head) % 16 == 0;
-        __syncthreads();  // in place: every thread has read the target's logit
-        for (int64_t i = threadIdx.x; i < body; i += kThreads) {
-            const int64_t j = head + 8 * i;
-            float v[8];
-            if (live) {
-                load_row8(x + j, v);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    v[q] = per_e * exp2_fast(k * (v[q] - top));
-                    if (j + q == target) v[q] += unit;
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] = 0.f;
+        if (t == 0 && a.logp) a.logp[row] = o.logp;
+        if (a.dlogits) {
+            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, live, in.target, top, o);
+            for (int i = t; i < shape.units; i += kThreads) {
+                uint4 u = make_uint4(0, 0, 0, 0);
+                if (live) u = ld_unit(body + i);
+                out.put(u, shape.head + i * kUnit<T>, k);
             }
-            if (wide) {
-                store_out8(y + j, v);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) store1(y + j + q, v[q]);
-            }
+            if (has_extra) out.put_one(x_extra, extra, k);
         }
-        for (int64_t i = threadIdx.x; i < head + (a.vocab - tail0); i += kThreads) {
-            const int64_t j = i < head ? i : tail0 + (i - head);
-            float v = live ? per_e * exp2_fast(k * (widen(x[j]) - top)) : 0.f;
-            if (live && j == target) v += unit;
-            store1(y + j, v);
-        }
+        group_sync<kWarps>(0);  // the slots are used again
     }
-    // the CTAs' sums, added in their order by the last CTA to finish
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < 4; ++i) ws->part[4 * blockIdx.x + i] = acc[i];
-        __threadfence();
-        last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    double all[4] = {0.0, 0.0, 0.0, 0.0};
-    for (unsigned b = threadIdx.x; b < gridDim.x; b += kThreads)
-        for (int i = 0; i < 4; ++i) all[i] += __ldcg(&ws->part[4 * b + i]);
-    for (int i = 0; i < 4; ++i) {
-        for (int o = 16; o > 0; o >>= 1) all[i] += __shfl_down_sync(0xffffffffu, all[i], o);
-        if (threadIdx.x % 32 == 0) sums[i][threadIdx.x / 32] = all[i];
-    }
-    __syncthreads();
-    if (threadIdx.x < 4) {
-        double s = 0.0;
-        for (int i = 0; i < kWarps; ++i) s += sums[threadIdx.x][i];
-        a.stats[threadIdx.x] = (float)s;
-    }
-    if (threadIdx.x == 0) ws->ticket = 0;
+    finish_stats(a, acc, sums, &last, t);
 }
 
-unsigned row_grid(int64_t rows, int sm_count, int per_sm) {
-    int64_t cap = (int64_t)sm_count * per_sm;
-    if (cap > kWorkspaceParts / 4) cap = kWorkspaceParts / 4;
-    return (unsigned)(rows < 1 ? 1 : rows < cap ? rows : cap);
-}
+// ---- launches --------------------------------------------------------------------------------------
 
 constexpr double kLog2e = 1.4426950408889634074;
+
+unsigned grid_of(int64_t work, int64_t cap) {
+    if (cap > kWorkspaceParts / 4) cap = kWorkspaceParts / 4;
+    return (unsigned)(work < 1 ? 1 : work < cap ? work : cap);
+}
+
+template <typename T, int W>
+cudaError_t logprobs_groups(const LogprobArgs &a, float k, int sm_count, cudaStream_t stream) {
+    const int64_t ctas = (a.rows + kWarps / W - 1) / (kWarps / W);
+    const unsigned grid = (unsigned)(ctas < (int64_t)sm_count * 4 ? ctas : (int64_t)sm_count * 4);
+    if (a.entropy) token_logprobs_kernel<T, W, true><<<grid, kThreads, 0, stream>>>(a, k);
+    else token_logprobs_kernel<T, W, false><<<grid, kThreads, 0, stream>>>(a, k);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
+    const float k = (float)(a.scale * kLog2e);
+    const int64_t units = a.vocab / kUnit<T>;
+    if (units <= 32 * kRowUnits) return logprobs_groups<T, 1>(a, k, sm_count, stream);
+    if (units <= 128 * kRowUnits) return logprobs_groups<T, 4>(a, k, sm_count, stream);
+    return logprobs_groups<T, 16>(a, k, sm_count, stream);
+}
+
+template <typename T, typename O, int W>
+cudaError_t policy_rows(const PolicyArgs &a, float k, int sm_count, cudaStream_t stream) {
+    const int64_t ctas = (a.rows + kWarps / W - 1) / (kWarps / W);
+    policy_loss_rows_kernel<T, O, W><<<grid_of(ctas, (int64_t)sm_count * 2), kThreads, 0, stream>>>(a, k);
+    return cudaGetLastError();
+}
+
+template <typename T, typename O>
+cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count, cudaStream_t stream) {
+    constexpr size_t bytes = sizeof(RingShared) + 128;
+    static std::atomic<unsigned long long> ready{0};  // one bit per device: the attribute is set
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (!(ready.load() & bit)) {
+        e = cudaFuncSetAttribute(policy_loss_ring_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != cudaSuccess) return e;
+        ready.fetch_or(bit);
+    }
+    cudaLaunchConfig_t cfg = {};
+    const int64_t most = sm_count / cluster;
+    cfg.gridDim = dim3((unsigned)((a.rows < 1 ? 1 : a.rows < most ? a.rows : most) * cluster));
+    cfg.blockDim = dim3(kRingThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim = {(unsigned)cluster, 1, 1};
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O>, a, k, cluster);
+}
+
+template <typename T, typename O>
+cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
+    const float k = (float)(a.scale_exact * kLog2e);
+    const int64_t units = a.vocab / kUnit<T>;
+    if (units <= 32 * kRowUnits) return policy_rows<T, O, 1>(a, k, sm_count, stream);
+    if (units <= 128 * kRowUnits) return policy_rows<T, O, 4>(a, k, sm_count, stream);
+    // slices of at most half the ring, so that the next row's first half is in when this one's is used;
+    // more CTAs to a row while there are fewer rows than SMs
+    constexpr int64_t kHalf = (int64_t)kStages * kStageUnits / 2;
+    int cluster = 1;
+    while (cluster < kMaxCluster && ((units + cluster - 1) / cluster > kHalf || a.rows * cluster * 2 <= sm_count)) cluster *= 2;
+    if ((units + cluster - 1) / cluster <= (int64_t)(kStages - 1) * kStageUnits)
+        return policy_ring<T, O>(a, k, cluster, sm_count, stream);
+    policy_loss_long_kernel<T, O><<<grid_of(a.rows, (int64_t)sm_count * 4), kThreads, 0, stream>>>(a, k);
+    return cudaGetLastError();
+}
 
 }  // namespace
 
 cudaError_t launch_token_logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
-    const float k = (float)(a.scale * kLog2e);
-    const unsigned grid = row_grid(a.rows, sm_count, 4);
-    if (a.dtype == ADAMA_F32)
-        token_logprobs_kernel<float><<<grid, kThreads, 0, stream>>>(a, k);
-    else
-        token_logprobs_kernel<__nv_bfloat16><<<grid, kThreads, 0, stream>>>(a, k);
-    return cudaGetLastError();
+    return a.dtype == ADAMA_F32 ? logprobs<float>(a, sm_count, stream) : logprobs<__nv_bfloat16>(a, sm_count, stream);
 }
 
 cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
-    const float k = (float)(a.scale_exact * kLog2e);
-    const unsigned grid = row_grid(a.rows, sm_count, 4);
-    if (a.logits_dtype == ADAMA_F32 && a.dlogits_dtype == ADAMA_F32)
-        policy_loss_kernel<float, float><<<grid, kThreads, 0, stream>>>(a, k);
-    else if (a.logits_dtype == ADAMA_F32)
-        policy_loss_kernel<float, __nv_bfloat16><<<grid, kThreads, 0, stream>>>(a, k);
-    else if (a.dlogits_dtype == ADAMA_F32)
-        policy_loss_kernel<__nv_bfloat16, float><<<grid, kThreads, 0, stream>>>(a, k);
-    else
-        policy_loss_kernel<__nv_bfloat16, __nv_bfloat16><<<grid, kThreads, 0, stream>>>(a, k);
-    return cudaGetLastError();
+    if (a.logits_dtype == ADAMA_F32)
+        return a.dlogits_dtype == ADAMA_F32 ? policy<float, float>(a, sm_count, stream)
+                                            : policy<float, __nv_bfloat16>(a, sm_count, stream);
+    return a.dlogits_dtype == ADAMA_F32 ? policy<__nv_bfloat16, float>(a, sm_count, stream)
+                                        : policy<__nv_bfloat16, __nv_bfloat16>(a, sm_count, stream);
 }
 
 }  // namespace adama
