@@ -156,7 +156,8 @@ struct Sums {
 };
 
 // The threads' sums -> the CTA's in the workspace -> stats, by the last CTA, in the CTAs' order.
-// All kThreads call it; `slots` holds kWarps doubles.
+// All THREADS call it.
+template <int THREADS>
 __device__ __forceinline__ void finish_stats(const PolicyArgs &a, Sums s, double (*slots)[4], volatile int *last,
                                              int t) {
     Workspace *ws = static_cast<Workspace *>(a.workspace);
@@ -166,29 +167,29 @@ __device__ __forceinline__ void finish_stats(const PolicyArgs &a, Sums s, double
             for (int o = 16; o > 0; o >>= 1) s.v[i] += __shfl_down_sync(0xffffffffu, s.v[i], o);
             if (t % 32 == 0) slots[t / 32][i] = s.v[i];
         }
-        asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+        asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory");
     };
     cta_sum();
     if (t < 4) {
         double sum = 0.0;
-        for (int w = 0; w < kWarps; ++w) sum += slots[w][t];
+        for (int w = 0; w < THREADS / 32; ++w) sum += slots[w][t];
         ws->part[4 * blockIdx.x + t] = sum;
         __threadfence();
     }
-    asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+    asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory");
     if (t == 0) *last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
-    asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory");
+    asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory");
     if (!*last) return;
     __threadfence();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         s.v[i] = 0.0;
-        for (unsigned b = t; b < gridDim.x; b += kThreads) s.v[i] += __ldcg(&ws->part[4 * b + i]);
+        for (unsigned b = t; b < gridDim.x; b += THREADS) s.v[i] += __ldcg(&ws->part[4 * b + i]);
     }
     cta_sum();
     if (t < 4) {
         double sum = 0.0;
-        for (int w = 0; w < kWarps; ++w) sum += slots[w][t];
+        for (int w = 0; w < THREADS / 32; ++w) sum += slots[w][t];
         a.stats[t] = (float)sum;
     }
     if (t == 0) ws->ticket = 0;
@@ -216,42 +217,21 @@ __device__ __forceinline__ void store_wide(__nv_bfloat16 *p, const float (&y)[8]
                                                pack2_bf16(y[4], y[5]), pack2_bf16(y[6], y[7]));
 }
 
-// How a row's gradient is written.
+// How a row's gradient is written.  The units are written without the target's extra term; the
+// thread that wrote the target's element writes it again, with the term.
 template <typename T, typename O>
 struct RowWriter {
     static constexpr int N = kUnit<T>;
-    O *y;  // null: no gradient
+    O *y;
     bool wide;
-    int target;
-    float top, unit, per_e;
-    bool live;
+    float top, unit, per_e, k;
 
-    __device__ __forceinline__ RowWriter(O *row, const RowShape &shape, bool live_, int64_t target_, float top_,
-                                         const RowOut &o)
-        : y(row), target((int)target_), top(top_), unit(o.unit), per_e(o.per_e), live(live_) {
+    __device__ __forceinline__ RowWriter(O *row, const RowShape &shape, float top_, const RowOut &o, float k_)
+        : y(row), top(top_), unit(o.unit), per_e(o.per_e), k(k_) {
         constexpr int align = N * sizeof(O) < 16 ? N * sizeof(O) : 16;
         wide = reinterpret_cast<uintptr_t>(row + shape.head) % align == 0;
     }
-    // the unit of logits that begins at element j
-    __device__ __forceinline__ void put(const uint4 &u, int j, float k) const {
-        float v[N];
-        if (live) {
-            const Pair minus = pair(-top, -top), k2 = pair(k, k), per = pair(per_e, per_e);
-#pragma unroll
-            for (int q = 0; q < N / 2; ++q) {
-                float d0, d1;
-                split(mul2(add2(unit_pair<T>(u, q), minus), k2), d0, d1);
-                split(mul2(pair(exp2_fast(d0), exp2_fast(d1)), per), v[2 * q], v[2 * q + 1]);
-            }
-            if ((unsigned)(target - j) < (unsigned)N) {
-#pragma unroll
-                for (int q = 0; q < N; ++q)
-                    if (target - j == q) v[q] += unit;
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < N; ++q) v[q] = 0.f;
-        }
+    __device__ __forceinline__ void store(int j, const float (&v)[N]) const {
         if (wide) {
             store_wide(y + j, v);
         } else {
@@ -259,22 +239,46 @@ struct RowWriter {
             for (int q = 0; q < N; ++q) y[j + q] = narrow<O>(v[q]);
         }
     }
-    __device__ __forceinline__ void put_one(float x, int j, float k) const {
-        float v = 0.f;
-        if (live) {
-            v = per_e * exp2_fast(k * (x - top));
-            if (j == target) v += unit;
+    // the unit of logits that begins at element j
+    __device__ __forceinline__ void put(const uint4 &u, int j) const {
+        float v[N];
+        const Pair minus = pair(-top, -top), k2 = pair(k, k), per = pair(per_e, per_e);
+#pragma unroll
+        for (int q = 0; q < N / 2; ++q) {
+            float d0, d1;
+            split(mul2(add2(unit_pair<T>(u, q), minus), k2), d0, d1);
+            split(mul2(pair(exp2_fast(d0), exp2_fast(d1)), per), v[2 * q], v[2 * q + 1]);
         }
-        y[j] = narrow<O>(v);
+        store(j, v);
+    }
+    __device__ __forceinline__ void put_zeros(int j) const {
+        float v[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = 0.f;
+        store(j, v);
+    }
+    __device__ __forceinline__ void put_one(float x, int j) const { y[j] = narrow<O>(per_e * exp2_fast(k * (x - top))); }
+    __device__ __forceinline__ void put_target(float x, int64_t j) const {
+        y[j] = narrow<O>(per_e * exp2_fast(k * (x - top)) + unit);
     }
 };
+
+// Thread of a group of `threads` that writes element j of a row: units go round the threads from the
+// first unit of the slice on (stages hold a multiple of `threads` units), extra i belongs to thread i.
+template <typename T>
+__device__ __forceinline__ int owner_of(const RowShape &shape, int64_t j, int from, int threads) {
+    const int at = (int)j - shape.head;
+    if (at < 0) return (int)j;
+    if (at >= shape.units * kUnit<T>) return shape.head + at - shape.units * kUnit<T>;
+    return (at / kUnit<T> - from) % threads;
+}
 
 // ---- rows that fit a few warps' registers ------------------------------------------------------
 
 constexpr int kRowUnits = 8;  // units of a thread
 
 template <typename T, typename O, int W>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 policy_loss_rows_kernel(const PolicyArgs a, float k) {
     constexpr int kGroupThreads = 32 * W, kGroups = kWarps / W;
     __shared__ Stats shared[kWarps];
@@ -291,11 +295,11 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
         const bool has_extra = t < shape.head + shape.tail;
         const int extra = has_extra ? extra_index<T>(shape, t) : 0;
         uint4 u[kRowUnits];
-        float x_extra = 0.f, top = 0.f;
+        float x_extra = 0.f, x_target = CUDART_NAN_F, top = 0.f;
         RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (live) {
             const bool inside = in.target < a.vocab;
-            const float x_target = inside ? widen(x[in.target]) : CUDART_NAN_F;
+            if (inside) x_target = widen(x[in.target]);
 #pragma unroll
             for (int i = 0; i < kRowUnits; ++i)
                 if (t + i * kGroupThreads < shape.units) u[i] = ld_unit(body + t + i * kGroupThreads);
@@ -320,15 +324,22 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
         }
         if (t == 0 && a.logp) a.logp[row] = o.logp;
         if (a.dlogits) {
-            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, live, in.target, top, o);
+            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
 #pragma unroll
-            for (int i = 0; i < kRowUnits; ++i)
-                if (t + i * kGroupThreads < shape.units) out.put(u[i], shape.head + (t + i * kGroupThreads) * kUnit<T>, k);
-            if (has_extra) out.put_one(x_extra, extra, k);
+            for (int i = 0; i < kRowUnits; ++i) {
+                const int at = t + i * kGroupThreads;
+                if (at < shape.units) {
+                    if (live) out.put(u[i], shape.head + at * kUnit<T>);
+                    else out.put_zeros(shape.head + at * kUnit<T>);
+                }
+            }
+            if (has_extra) out.put_one(x_extra, extra);
+            if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, 0, kGroupThreads))
+                out.put_target(x_target, in.target);
         }
         if (W > 1) group_sync<W>(g);  // the slots are used again
     }
-    finish_stats(a, acc, sums, &last, threadIdx.x);
+    finish_stats<kThreads>(a, acc, sums, &last, threadIdx.x);
 }
 
 // ---- longer rows: a ring in shared memory ------------------------------------------------------
@@ -336,11 +347,14 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
 // copies, in stages of kStageBytes; the statistics are taken from the stages as they arrive, then the
 // gradient is computed from the same stages, each of which is refilled as soon as it has been used:
 // the next row streams in while this one's gradient streams out, and every logit crosses the HBM bus
-// once.  One producer warp, kThreads that compute.
+// once.  One producer warp, kRingWork threads that compute.
 
-constexpr int kStageBytes = 16384;
-constexpr int kStages = 13;
-constexpr int kRingThreads = kThreads + 32;
+constexpr int kStageBytes = 12288;
+constexpr int kStages = 9;
+constexpr int kRingsPerSm = 2;
+constexpr int kRingWork = 256;
+constexpr int kRingWarps = kRingWork / 32;
+constexpr int kRingThreads = kRingWork + 32;
 constexpr int kStageUnits = kStageBytes / 16;
 constexpr int kMaxCluster = 8;
 
@@ -348,29 +362,42 @@ struct RingShared {
     alignas(128) unsigned char stage[kStages][kStageBytes];
     alignas(16) float4 peer[2][kMaxCluster];  // {top, sum, x_target} of the cluster's CTAs, for even and odd rows
     unsigned long long full[kStages], empty[kStages], joined[2];
-    Stats slots[2][kWarps];  // for even and odd rows: a warp may be a row ahead of another
-    double sums[kWarps][4];
+    Stats slots[2][kRingWarps];  // for even and odd rows: a warp may be a row ahead of another
+    double sums[kRingWarps][4];
     int last, give_up;
 };
 
-// The slice of a row's units that CTA `rank` of `size` takes.
-__device__ __forceinline__ void slice_of(int units, int rank, int size, int &from, int &count) {
-    from = (int)((int64_t)units * rank / size);
-    count = (int)((int64_t)units * (rank + 1) / size) - from;
+// The slice of a row's units that CTA `rank` of 2^log_size takes (units < 2^29, so 32 bits hold it).
+__device__ __forceinline__ void slice_of(int units, int rank, int log_size, int &from, int &count) {
+    from = (int)(((unsigned)units * (unsigned)rank) >> log_size);
+    count = (int)(((unsigned)units * (unsigned)(rank + 1)) >> log_size) - from;
 }
 
+// Place in the ring: a stage, and the parity of the barrier phase that its current use completes.
+struct Cursor {
+    uint32_t slot = 0, parity = 0;
+
+    __device__ __forceinline__ void advance() {
+        if (++slot == kStages) {
+            slot = 0;
+            parity ^= 1;
+        }
+    }
+};
+
 template <typename T, typename O>
-__global__ void __launch_bounds__(kRingThreads, 1)
-policy_loss_ring_kernel(const PolicyArgs a, float k, int cluster) {
+__global__ void __launch_bounds__(kRingThreads, kRingsPerSm)
+policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
     extern __shared__ unsigned char raw[];
     RingShared &sh = *reinterpret_cast<RingShared *>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
     const int t = threadIdx.x, lane = t % 32, warp = t / 32;
+    const int cluster = 1 << log_cluster;
     const int rank = cluster > 1 ? (int)cluster_rank() : 0;
-    const int64_t first = blockIdx.x / cluster, step = gridDim.x / cluster;
+    const int64_t first = blockIdx.x >> log_cluster, step = gridDim.x >> log_cluster;
     if (t == 0) {
         for (int i = 0; i < kStages; ++i) {
             barrier_init(shared_addr(&sh.full[i]), 1);
-            barrier_init(shared_addr(&sh.empty[i]), kWarps);
+            barrier_init(shared_addr(&sh.empty[i]), kRingWarps);
         }
         for (int i = 0; i < 2; ++i) barrier_init(shared_addr(&sh.joined[i]), 1);
         sh.give_up = 0;
@@ -379,34 +406,41 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int cluster) {
     __syncthreads();
     if (cluster > 1) cluster_sync();  // the peers' barriers are ready before the first message
 
-    if (warp == kWarps) {
+    if (warp == kRingWarps) {
         // ---- producer
         if (lane == 0) {
-            uint32_t n = 0;  // stages issued
+            Cursor c;
+            uint32_t issued = 0;  // stages, up to kStages
             for (int64_t row = first; row < a.rows && !*(volatile int *)&sh.give_up; row += step) {
                 if (a.weights[row] == 0.f || a.targets[row] < 0) continue;
                 const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
                 const RowShape shape = row_shape(x, (int)a.vocab);
                 int from, count;
-                slice_of(shape.units, rank, cluster, from, count);
+                slice_of(shape.units, rank, log_cluster, from, count);
                 const unsigned char *src = reinterpret_cast<const unsigned char *>(x + shape.head) + (size_t)from * 16;
-                for (int at = 0; at < count; at += kStageUnits, ++n) {
-                    const uint32_t slot = n % kStages, turn = n / kStages;
-                    if (turn > 0 && !barrier_wait(shared_addr(&sh.empty[slot]), (turn - 1) & 1, &sh.give_up)) break;
+                for (int at = 0; at < count; at += kStageUnits, c.advance()) {
+                    const uint32_t full = shared_addr(&sh.full[c.slot]);
+                    // used before: wait until that use, of the other parity, is over
+                    if (issued == kStages && !barrier_wait(shared_addr(&sh.empty[c.slot]), c.parity ^ 1, &sh.give_up)) break;
                     const uint32_t bytes = 16u * (uint32_t)(count - at < kStageUnits ? count - at : kStageUnits);
-                    barrier_expect(shared_addr(&sh.full[slot]), bytes);
-                    bulk_load(shared_addr(sh.stage[slot]), src + (size_t)at * 16, bytes, shared_addr(&sh.full[slot]));
+                    barrier_expect(full, bytes);
+                    bulk_load(shared_addr(sh.stage[c.slot]), src + (size_t)at * 16, bytes, full);
+                    if (issued < kStages) ++issued;
                 }
             }
             if (*(volatile int *)&sh.give_up) {  // copies in flight end before the CTA does
                 int none = 0;
-                for (uint32_t i = n > kStages ? n - kStages : 0; i < n; ++i)
-                    barrier_wait(shared_addr(&sh.full[i % kStages]), (i / kStages) & 1, &none);
+                for (uint32_t i = 0; i < issued; ++i) {  // backwards from the last one issued
+                    if (c.slot == 0) c.parity ^= 1;
+                    c.slot = c.slot ? c.slot - 1 : kStages - 1;
+                    barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &none);
+                }
             }
         }
     } else {
         Sums acc;
-        uint32_t n = 0, joins = 0;  // stages used, rows joined
+        Cursor c;
+        uint32_t joins = 0;  // rows joined
         RowIn next = {-1, 0.f, 0.f, 0.f, 0.f};
         if (first < a.rows) next = row_in(a, first);
         for (int64_t row = first; row < a.rows; row += step) {
@@ -416,28 +450,27 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int cluster) {
             const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
             const RowShape shape = row_shape(x, (int)a.vocab);
             int from, count;
-            slice_of(shape.units, rank, cluster, from, count);
+            slice_of(shape.units, rank, log_cluster, from, count);
             const bool has_extra = rank == 0 && t < shape.head + shape.tail;
             const int extra = has_extra ? extra_index<T>(shape, t) : 0;
-            const uint32_t n0 = n;
-            float x_extra = 0.f, top = 0.f;
+            const Cursor c0 = c;
+            float x_extra = 0.f, xt = 0.f, top = 0.f;
             RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (live) {
                 const bool inside = in.target < a.vocab;
                 const float x_target = t == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
                 if (has_extra) x_extra = widen(x[extra]);
                 Running<false> run;
-                for (int at = 0; at < count; at += kStageUnits, ++n) {
-                    const uint32_t slot = n % kStages;
-                    barrier_wait(shared_addr(&sh.full[slot]), (n / kStages) & 1, &sh.give_up);
-                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[slot]);
+                for (int at = 0; at < count; at += kStageUnits, c.advance()) {
+                    barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &sh.give_up);
+                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]);
                     if (count - at >= kStageUnits) {
-                        uint4 u[kStageUnits / kThreads];
+                        uint4 u[kStageUnits / kRingWork];
 #pragma unroll
-                        for (int i = 0; i < kStageUnits / kThreads; ++i) u[i] = units[t + i * kThreads];
+                        for (int i = 0; i < kStageUnits / kRingWork; ++i) u[i] = units[t + i * kRingWork];
                         run.template add_units<T>(u, k);
                     } else {
-                        for (int i = t; i < count - at; i += kThreads) {
+                        for (int i = t; i < count - at; i += kRingWork) {
                             const uint4 u[1] = {units[i]};
                             run.template add_units<T>(u, k);
                         }
@@ -448,11 +481,11 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int cluster) {
                 Stats s = warp_join<false>(run.stats(), k);
                 const int b = joins & 1;
                 if (lane == 0) sh.slots[b][warp] = {s.top, s.sum, x_target};
-                asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(kRingWork) : "memory");
                 const Stats none = {-CUDART_INF_F, 0.f, 0.f};
-                const Stats mine = lane < kWarps ? sh.slots[b][lane] : none;
+                const Stats mine = lane < kRingWarps ? sh.slots[b][lane] : none;
                 s = warp_join<false>(mine, k);
-                float xt = __shfl_sync(0xffffffffu, mine.wsum, 0);
+                xt = __shfl_sync(0xffffffffu, mine.wsum, 0);
                 if (cluster > 1) {
                     const uint32_t bar = shared_addr(&sh.joined[b]);
                     if (t == 0) barrier_expect(bar, 16u * cluster);
@@ -474,30 +507,42 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int cluster) {
                 }
             }
             if (t == 0 && rank == 0 && a.logp) a.logp[row] = o.logp;
-            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, live, in.target, top, o);
-            n = n0;
-            for (int at = 0; at < count; at += kStageUnits) {
-                const int here = count - at < kStageUnits ? count - at : kStageUnits;
-                const uint32_t slot = n % kStages;
-                const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[slot]);
-                const int j0 = shape.head + (from + at) * kUnit<T>;
-                if (a.dlogits)
-                    for (int i = t; i < here; i += kThreads) {
-                        uint4 u = make_uint4(0, 0, 0, 0);
-                        if (live) u = units[i];
-                        out.put(u, j0 + i * kUnit<T>, k);
+            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
+            const int j0 = shape.head + from * kUnit<T>;
+            if (live) {
+                c = c0;
+                for (int at = 0; at < count; at += kStageUnits, c.advance()) {
+                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]);
+                    if (a.dlogits) {
+                        if (count - at >= kStageUnits) {
+                            uint4 u[kStageUnits / kRingWork];
+#pragma unroll
+                            for (int i = 0; i < kStageUnits / kRingWork; ++i) u[i] = units[t + i * kRingWork];
+#pragma unroll
+                            for (int i = 0; i < kStageUnits / kRingWork; ++i)
+                                out.put(u[i], j0 + (at + t + i * kRingWork) * kUnit<T>);
+                        } else {
+                            for (int i = t; i < count - at; i += kRingWork) out.put(units[i], j0 + (at + i) * kUnit<T>);
+                        }
                     }
-                if (live) {
                     __syncwarp();
-                    if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
-                    ++n;
+                    if (lane == 0) barrier_arrive(shared_addr(&sh.empty[c.slot]));
+                }
+            } else if (a.dlogits) {
+                for (int i = t; i < count; i += kRingWork) out.put_zeros(j0 + i * kUnit<T>);
+            }
+            if (a.dlogits) {
+                if (has_extra) out.put_one(x_extra, extra);
+                if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, from, kRingWork)) {
+                    const int at = ((int)in.target - shape.head) / kUnit<T> - from;
+                    const bool extra_one = in.target < shape.head || in.target >= shape.head + shape.units * kUnit<T>;
+                    if (extra_one ? rank == 0 : at >= 0 && at < count) out.put_target(xt, in.target);
                 }
             }
-            if (a.dlogits && has_extra) out.put_one(x_extra, extra, k);
         }
         if (t == 0 && sh.give_up && atomicCAS(a.status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
             a.status[1] = kWaitPolicyRing;
-        finish_stats(a, acc, sh.sums, &sh.last, t);
+        finish_stats<kRingWork>(a, acc, sh.sums, &sh.last, t);
     }
     if (cluster > 1) {
         __syncwarp();
@@ -523,11 +568,11 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
         const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
         const bool has_extra = t < shape.head + shape.tail;
         const int extra = has_extra ? extra_index<T>(shape, t) : 0;
-        float x_extra = 0.f, top = 0.f;
+        float x_extra = 0.f, x_target = CUDART_NAN_F, top = 0.f;
         RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (live) {
             const bool inside = in.target < a.vocab;
-            const float x_target = inside ? widen(x[in.target]) : CUDART_NAN_F;
+            if (inside) x_target = widen(x[in.target]);
             if (has_extra) x_extra = widen(x[extra]);
             Running<false> run;
             for (int i = t; i < shape.units; i += kThreads) {
@@ -545,17 +590,18 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
         }
         if (t == 0 && a.logp) a.logp[row] = o.logp;
         if (a.dlogits) {
-            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, live, in.target, top, o);
+            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
             for (int i = t; i < shape.units; i += kThreads) {
-                uint4 u = make_uint4(0, 0, 0, 0);
-                if (live) u = ld_unit(body + i);
-                out.put(u, shape.head + i * kUnit<T>, k);
+                if (live) out.put(ld_unit(body + i), shape.head + i * kUnit<T>);
+                else out.put_zeros(shape.head + i * kUnit<T>);
             }
-            if (has_extra) out.put_one(x_extra, extra, k);
+            if (has_extra) out.put_one(x_extra, extra);
+            if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, 0, kThreads))
+                out.put_target(x_target, in.target);
         }
         group_sync<kWarps>(0);  // the slots are used again
     }
-    finish_stats(a, acc, sums, &last, t);
+    finish_stats<kThreads>(a, acc, sums, &last, t);
 }
 
 // ---- launches --------------------------------------------------------------------------------------
@@ -606,17 +652,19 @@ cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count,
         ready.fetch_or(bit);
     }
     cudaLaunchConfig_t cfg = {};
-    const int64_t most = sm_count / cluster;
+    const int64_t most = sm_count * kRingsPerSm / cluster;
     cfg.gridDim = dim3((unsigned)((a.rows < 1 ? 1 : a.rows < most ? a.rows : most) * cluster));
     cfg.blockDim = dim3(kRingThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
+    int log_cluster = 0;
+    while (1 << log_cluster < cluster) ++log_cluster;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim = {(unsigned)cluster, 1, 1};
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O>, a, k, cluster);
+    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O>, a, k, log_cluster);
 }
 
 template <typename T, typename O>
@@ -625,12 +673,11 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
     const int64_t units = a.vocab / kUnit<T>;
     if (units <= 32 * kRowUnits) return policy_rows<T, O, 1>(a, k, sm_count, stream);
     if (units <= 128 * kRowUnits) return policy_rows<T, O, 4>(a, k, sm_count, stream);
-    // slices of at most half the ring, so that the next row's first half is in when this one's is used;
-    // more CTAs to a row while there are fewer rows than SMs
-    constexpr int64_t kHalf = (int64_t)kStages * kStageUnits / 2;
+    // as few CTAs to a row as hold it, more while there are fewer rows than SMs
+    constexpr int64_t kRing = (int64_t)kStages * kStageUnits;
     int cluster = 1;
-    while (cluster < kMaxCluster && ((units + cluster - 1) / cluster > kHalf || a.rows * cluster * 2 <= sm_count)) cluster *= 2;
-    if ((units + cluster - 1) / cluster <= (int64_t)(kStages - 1) * kStageUnits)
+    while (cluster < kMaxCluster && ((units + cluster - 1) / cluster > kRing || a.rows * cluster * 2 <= sm_count)) cluster *= 2;
+    if ((units + cluster - 1) / cluster <= kRing)
         return policy_ring<T, O>(a, k, cluster, sm_count, stream);
     policy_loss_long_kernel<T, O><<<grid_of(a.rows, (int64_t)sm_count * 4), kThreads, 0, stream>>>(a, k);
     return cudaGetLastError();

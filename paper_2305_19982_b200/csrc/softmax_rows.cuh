@@ -143,9 +143,8 @@ __device__ __forceinline__ Stats raised(Stats s, float top, float k) {
 // Statistics of the union over the 32 lanes of a warp, in every lane.
 template <bool ENT>
 __device__ __forceinline__ Stats warp_join(Stats s, float k) {
-    float top = s.top;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float top;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(top) : "f"(s.top));
     s = raised(s, top, k);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
