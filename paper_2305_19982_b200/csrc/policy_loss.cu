@@ -6,6 +6,7 @@
 //     dlogits_j = w*s*c*([j = target] - p_j),  c = -(r*A while r*A <= the clamped product) + beta*(1 - exp(d))
 // A row is read once (loss: and its gradient written once); what bounds every form is HBM.
 #include <atomic>
+#include <type_traits>
 
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"
@@ -138,7 +139,7 @@ __device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, 
     }
     if (r != r) o.pg = slope = r;  // a NaN log-probability stays visible
     o.unit = in.weight * slope * a.scale;
-    o.per_e = -o.unit / s.sum;
+    o.per_e = __fdividef(-o.unit, s.sum);  // 2 ulp; sum >= 1 or NaN
     return o;
 }
 
@@ -231,16 +232,18 @@ struct RowWriter {
         constexpr int align = N * sizeof(O) < 16 ? N * sizeof(O) : 16;
         wide = reinterpret_cast<uintptr_t>(row + shape.head) % align == 0;
     }
-    __device__ __forceinline__ void store(int j, const float (&v)[N]) const {
-        if (wide) {
-            store_wide(y + j, v);
+    template <bool WIDE>
+    __device__ __forceinline__ static void store(O *p, const float (&v)[N]) {
+        if (WIDE) {
+            store_wide(p, v);
         } else {
 #pragma unroll
-            for (int q = 0; q < N; ++q) y[j + q] = narrow<O>(v[q]);
+            for (int q = 0; q < N; ++q) p[q] = narrow<O>(v[q]);
         }
     }
-    // the unit of logits that begins at element j
-    __device__ __forceinline__ void put(const uint4 &u, int j) const {
+    // a unit of logits whose gradient goes to p
+    template <bool WIDE>
+    __device__ __forceinline__ void put(const uint4 &u, O *p) const {
         float v[N];
         const Pair minus = pair(-top, -top), k2 = pair(k, k), per = pair(per_e, per_e);
 #pragma unroll
@@ -249,13 +252,14 @@ struct RowWriter {
             split(mul2(add2(unit_pair<T>(u, q), minus), k2), d0, d1);
             split(mul2(pair(exp2_fast(d0), exp2_fast(d1)), per), v[2 * q], v[2 * q + 1]);
         }
-        store(j, v);
+        store<WIDE>(p, v);
     }
-    __device__ __forceinline__ void put_zeros(int j) const {
+    template <bool WIDE>
+    __device__ __forceinline__ static void put_zeros(O *p) {
         float v[N];
 #pragma unroll
         for (int q = 0; q < N; ++q) v[q] = 0.f;
-        store(j, v);
+        store<WIDE>(p, v);
     }
     __device__ __forceinline__ void put_one(float x, int j) const { y[j] = narrow<O>(per_e * exp2_fast(k * (x - top))); }
     __device__ __forceinline__ void put_target(float x, int64_t j) const {
@@ -325,14 +329,18 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
         if (t == 0 && a.logp) a.logp[row] = o.logp;
         if (a.dlogits) {
             const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
+            O *p = out.y + shape.head + t * kUnit<T>;
+            const auto units = [&](auto wide) {
 #pragma unroll
-            for (int i = 0; i < kRowUnits; ++i) {
-                const int at = t + i * kGroupThreads;
-                if (at < shape.units) {
-                    if (live) out.put(u[i], shape.head + at * kUnit<T>);
-                    else out.put_zeros(shape.head + at * kUnit<T>);
+                for (int i = 0; i < kRowUnits; ++i) {
+                    if (t + i * kGroupThreads < shape.units) {
+                        if (live) out.template put<decltype(wide)::value>(u[i], p + i * kGroupThreads * kUnit<T>);
+                        else out.template put_zeros<decltype(wide)::value>(p + i * kGroupThreads * kUnit<T>);
+                    }
                 }
-            }
+            };
+            if (out.wide) units(std::true_type());
+            else units(std::false_type());
             if (has_extra) out.put_one(x_extra, extra);
             if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, 0, kGroupThreads))
                 out.put_target(x_target, in.target);
@@ -508,28 +516,39 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             }
             if (t == 0 && rank == 0 && a.logp) a.logp[row] = o.logp;
             const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
-            const int j0 = shape.head + from * kUnit<T>;
+            O *p = out.y + shape.head + (int64_t)(from + t) * kUnit<T>;
             if (live) {
                 c = c0;
-                for (int at = 0; at < count; at += kStageUnits, c.advance()) {
-                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]);
-                    if (a.dlogits) {
+                const auto release = [&]() {
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive(shared_addr(&sh.empty[c.slot]));
+                };
+                const auto stages = [&](auto wide) {
+                    for (int at = 0; at < count; at += kStageUnits, c.advance(), p += kStageUnits * kUnit<T>) {
+                        const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]) + t;
                         if (count - at >= kStageUnits) {
                             uint4 u[kStageUnits / kRingWork];
 #pragma unroll
-                            for (int i = 0; i < kStageUnits / kRingWork; ++i) u[i] = units[t + i * kRingWork];
+                            for (int i = 0; i < kStageUnits / kRingWork; ++i) u[i] = units[i * kRingWork];
 #pragma unroll
                             for (int i = 0; i < kStageUnits / kRingWork; ++i)
-                                out.put(u[i], j0 + (at + t + i * kRingWork) * kUnit<T>);
+                                out.template put<decltype(wide)::value>(u[i], p + i * kRingWork * kUnit<T>);
                         } else {
-                            for (int i = t; i < count - at; i += kRingWork) out.put(units[i], j0 + (at + i) * kUnit<T>);
+                            for (int i = 0; i < count - at - t; i += kRingWork)
+                                out.template put<decltype(wide)::value>(units[i], p + i * kUnit<T>);
                         }
+                        release();
                     }
-                    __syncwarp();
-                    if (lane == 0) barrier_arrive(shared_addr(&sh.empty[c.slot]));
-                }
+                };
+                if (!a.dlogits)
+                    for (int at = 0; at < count; at += kStageUnits, c.advance()) release();
+                else if (out.wide) stages(std::true_type());
+                else stages(std::false_type());
             } else if (a.dlogits) {
-                for (int i = t; i < count; i += kRingWork) out.put_zeros(j0 + i * kUnit<T>);
+                for (int i = 0; i < count - t; i += kRingWork) {
+                    if (out.wide) out.template put_zeros<true>(p + (int64_t)i * kUnit<T>);
+                    else out.template put_zeros<false>(p + (int64_t)i * kUnit<T>);
+                }
             }
             if (a.dlogits) {
                 if (has_extra) out.put_one(x_extra, extra);
@@ -591,10 +610,15 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
         if (t == 0 && a.logp) a.logp[row] = o.logp;
         if (a.dlogits) {
             const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
-            for (int i = t; i < shape.units; i += kThreads) {
-                if (live) out.put(ld_unit(body + i), shape.head + i * kUnit<T>);
-                else out.put_zeros(shape.head + i * kUnit<T>);
-            }
+            O *p = out.y + shape.head;
+            const auto units = [&](auto wide) {
+                for (int i = t; i < shape.units; i += kThreads) {
+                    if (live) out.template put<decltype(wide)::value>(ld_unit(body + i), p + (int64_t)i * kUnit<T>);
+                    else out.template put_zeros<decltype(wide)::value>(p + (int64_t)i * kUnit<T>);
+                }
+            };
+            if (out.wide) units(std::true_type());
+            else units(std::false_type());
             if (has_extra) out.put_one(x_extra, extra);
             if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, 0, kThreads))
                 out.put_target(x_target, in.target);
