@@ -356,8 +356,8 @@ typedef struct adama_state8 {
  * a micro-batch changes v by less than half of a code's width, so rounding after each of N folds
  * would lose most of them.  To accumulate several micro-batches, sum them first (adama_sgdm_fold
  * into an fp32 buffer), then make this call.
- * Up to 448 tensors share a launch; 16-byte aligned grads, w and copies and 8-byte aligned codes
- * take 64- and 128-bit accesses, others element accesses.  grad_factor, w_bf16 and errors as
+ * Up to 448 tensors share a launch; tensors whose buffers are all 16-byte aligned are streamed in
+ * whole blocks, others (and the last, shorter block) element by element.  grad_factor, w_bf16 and errors as
  * adama_fold_apply_multi. */
 ADAMA_API adama_status adama_fold_apply8_multi(adama_ctx *ctx, const void *const *grads,
                                                adama_dtype gdt, float *const *w,

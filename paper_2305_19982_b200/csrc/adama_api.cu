@@ -612,7 +612,7 @@ static adama_status fold_apply_impl(adama_ctx *ctx, const void *const *grads, ad
         if (!any_element(n, first, k)) return cudaSuccess;
         ctx->launches += 1;
         return packed ? adama::launch_fold_apply8_multi(list, gdt, first, k, ctx->fold_c, c, grad_factor,
-                                                        ctx->sm_count, stream)
+                                                        ctx->status_dev, ctx->sm_count, stream)
                       : adama::launch_fold_apply_multi(list, gdt, first, k, ctx->fold_c, c, grad_factor,
                                                        ctx->sm_count, stream);
     });
@@ -1017,8 +1017,11 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
         }
         snprintf(ctx->err, sizeof(ctx->err),
                  "device-side wait expired in the %s kernel (code %u, wait %u, tile %u)",
-                 host[1] == adama::kWaitPolicyRing ? "policy-loss" : "fused weight-gradient", host[0], host[1],
-                 host[2]);
+                 host[1] == adama::kWaitPolicyRing   ? "policy-loss"
+                 : host[1] == adama::kWaitState8Ring ? "8-bit update"
+                 : host[1] == adama::kWaitStepRing   ? "update"
+                                                     : "fused weight-gradient",
+                 host[0], host[1], host[2]);
         return ADAMA_ERR_TIMEOUT;
     }
     return ADAMA_OK;

@@ -53,7 +53,8 @@ ApplyConstants make_apply_constants(double beta1, double beta2, double eps, int6
 // by a kernel (0 = none), word 1 = which wait, word 2 = tile (bad target: the row, low and high
 // half); rest reserved.
 enum DeviceErr : unsigned { kDevOk = 0, kDevTimeout = 1, kDevBadTarget = 2 };
-constexpr unsigned kWaitPolicyRing = 100;  // word 1 for the waits of the policy loss's ring
+// word 1 for the waits of the kernels that stream through a ring of bulk copies
+constexpr unsigned kWaitPolicyRing = 100, kWaitState8Ring = 101, kWaitStepRing = 102;
 
 // streaming kernels (fold_apply.cu)
 cudaError_t launch_fold(const void *grad, adama_dtype gdt, float *m, float *v, size_t n,
@@ -101,7 +102,7 @@ cudaError_t launch_fold_apply_multi(const StepList &s, adama_dtype gdt, int firs
                                     int sm_count, cudaStream_t stream);
 cudaError_t launch_fold_apply8_multi(const StepList &s, adama_dtype gdt, int first, int count,
                                      FoldConstants f, ApplyConstants c, const float *factor,
-                                     int sm_count, cudaStream_t stream);
+                                     unsigned *status, int sm_count, cudaStream_t stream);
 // pack: m, v -> s8; otherwise s8 -> m, v
 cudaError_t launch_state8_convert(const StepList &s, bool pack, int first, int count, int sm_count,
                                   cudaStream_t stream);

@@ -9,7 +9,10 @@
 #include <cuda_fp8.h>
 #include <float.h>
 
+#include <atomic>
+
 #include "adama_device.cuh"
+#include "bulk_copy.cuh"
 #include "tensor_table.cuh"
 
 namespace adama {
@@ -18,8 +21,12 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kPerLane = kStateBlock / 32;                      // elements of a block that one lane holds
-constexpr int kBlocksPerWarp = kChunk / (kStateBlock * kWarps); // blocks of a chunk that one warp takes
-static_assert(kPerLane == 8, "one 64-bit access per lane moves its codes");
+constexpr int kBlocks = kChunk / kStateBlock;                   // blocks of a chunk
+// A lane holds elements 4*lane .. 4*lane+3 of the block's first half and of its second half: every
+// access of a warp is then contiguous (512 bytes of fp32, 256 of bf16, 128 of codes).
+constexpr int kHalf = kStateBlock / 2;
+static_assert(kPerLane == 8, "two groups of four");
+static_assert(kBlocks == 16, "one lane of the producer warp to each of a chunk's scales");
 
 constexpr float kMTop = 448.f, kVTop = 1.875f;
 constexpr float kMTopInv = (float)(1.0 / 448.0), kVTopInv = (float)(1.0 / 1.875);
@@ -110,7 +117,15 @@ __device__ __forceinline__ void step8_1(float g, float &w, float &m, float &v, c
     w = fmaf(-c.step, m * rcp_fast(denom), w * c.w_keep);
 }
 
-// Byte i of a lane's eight codes lies at element 8*lane + i (vector form) or lane + 32*i.
+// What a lane moves: eight values of four arrays; group h of it lies kHalf*h further on.  In the
+// element form value i lies at element lane + 32*i and elements from n on are left alone.
+__device__ __forceinline__ uint2 load_codes(const uint8_t *p) {
+    return make_uint2(*reinterpret_cast<const unsigned *>(p), *reinterpret_cast<const unsigned *>(p + kHalf));
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, uint2 c) {
+    *reinterpret_cast<unsigned *>(p) = c.x;
+    *reinterpret_cast<unsigned *>(p + kHalf) = c.y;
+}
 __device__ __forceinline__ uint2 gather_codes(const uint8_t *p, size_t at, size_t n, int lane) {
     unsigned x[2] = {0, 0};
 #pragma unroll
@@ -124,20 +139,117 @@ __device__ __forceinline__ void scatter_codes(uint8_t *p, size_t at, size_t n, i
     for (int i = 0; i < kPerLane; ++i)
         if (at + lane + 32 * i < n) p[at + lane + 32 * i] = (uint8_t)(x[i / 4] >> (8 * (i % 4)));
 }
-__device__ __forceinline__ uint2 load_codes(const uint8_t *p) { return *reinterpret_cast<const uint2 *>(p); }
-__device__ __forceinline__ void store_codes(uint8_t *p, uint2 c) { *reinterpret_cast<uint2 *>(p) = c; }
-
+__device__ __forceinline__ Grad4 shared_grad4(const float *p) {
+    const float4 t = *reinterpret_cast<const float4 *>(p);
+    return {t.x, t.y, t.z, t.w};
+}
+__device__ __forceinline__ Grad4 shared_grad4(const __nv_bfloat16 *p) {
+    const uint2 t = *reinterpret_cast<const uint2 *>(p);
+    return {__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xffff0000u),
+            __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xffff0000u)};
+}
+__device__ __forceinline__ void put4(float (&x)[kPerLane], int h, float4 a) {
+    x[4 * h] = a.x;
+    x[4 * h + 1] = a.y;
+    x[4 * h + 2] = a.z;
+    x[4 * h + 3] = a.w;
+}
 __device__ __forceinline__ void load8(const float *p, float (&x)[kPerLane]) {
-    const float4 a = ld_stream(reinterpret_cast<const float4 *>(p));
-    const float4 b = ld_stream(reinterpret_cast<const float4 *>(p) + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) put4(x, h, ld_stream(reinterpret_cast<const float4 *>(p + kHalf * h)));
+}
+template <typename G>
+__device__ __forceinline__ void load_grads(const G *p, float (&x)[kPerLane]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const Grad4 a = load_grad4(p + kHalf * h, 0);
+        put4(x, h, make_float4(a.x, a.y, a.z, a.w));
+    }
 }
 __device__ __forceinline__ void store8(float *p, const float (&x)[kPerLane]) {
-    st_stream(reinterpret_cast<float4 *>(p), make_float4(x[0], x[1], x[2], x[3]));
-    st_stream(reinterpret_cast<float4 *>(p) + 1, make_float4(x[4], x[5], x[6], x[7]));
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        st_stream(reinterpret_cast<float4 *>(p + kHalf * h), make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]));
+}
+__device__ __forceinline__ void store_copy(__nv_bfloat16 *p, const float (&x)[kPerLane]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<uint2 *>(p + kHalf * h) =
+            make_uint2(pack2_bf16(x[4 * h], x[4 * h + 1]), pack2_bf16(x[4 * h + 2], x[4 * h + 3]));
 }
 
+// One block by one warp: the update of what has been loaded, and the stores.
+struct Block8 {
+    float g[kPerLane], w[kPerLane];
+    uint2 mc, vc;
+    float sm, sv;
+
+    __device__ __forceinline__ float2 update(float factor, const FoldConstants &f, const ApplyConstants &c) {
+        Lane x;
+        x.decode(mc, vc, sm, sv);
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) step8_1(__fmul_rn(g[i], factor), w[i], x.m[i], x.v[i], f, c);
+        return x.encode(mc, vc);
+    }
+    __device__ __forceinline__ static void store_scales(const adama_state8 &s, size_t blk, float2 top, int lane,
+                                                        const ApplyConstants &c) {
+        if (lane == 0) {
+            s.m_scale[blk] = __fmul_rn(__fmul_rn(top.x, kMTopInv), c.beta1_hi);
+            s.v_scale[blk] = __fmul_rn(__fmul_rn(top.y, kVTopInv), c.beta2_hi);
+        }
+    }
+    // element i0 = the block's first + 4*lane
+    __device__ __forceinline__ void store_wide(const adama_state8 &s, float *w_out, __nv_bfloat16 *copy, size_t i0) const {
+        store8(w_out + i0, w);
+        store_codes(s.m_codes + i0, mc);
+        store_codes(s.v_codes + i0, vc);
+        if (copy) store_copy(copy + i0, w);
+    }
+};
+
+// A block straight from global memory, of any length and alignment.
+template <typename G>
+__device__ __forceinline__ void block_direct(const G *g, float *w, __nv_bfloat16 *copy, const adama_state8 &s, size_t at,
+                                             size_t n, bool wide, int lane, float factor, const FoldConstants &f,
+                                             const ApplyConstants &c) {
+    const size_t blk = at / kStateBlock, i0 = at + 4 * lane;
+    Block8 x;
+    x.sm = s.m_scale[blk];
+    x.sv = s.v_scale[blk];
+    if (wide) {
+        load_grads(g + i0, x.g);
+        load8(w + i0, x.w);
+        x.mc = load_codes(s.m_codes + i0);
+        x.vc = load_codes(s.v_codes + i0);
+    } else {
+        x.mc = gather_codes(s.m_codes, at, n, lane);
+        x.vc = gather_codes(s.v_codes, at, n, lane);
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) {
+            const size_t j = at + lane + 32 * i;
+            x.g[i] = j < n ? widen(g[j]) : 0.f;
+            x.w[i] = j < n ? w[j] : 0.f;
+        }
+    }
+    const float2 top = x.update(factor, f, c);
+    if (wide) {
+        x.store_wide(s, w, copy, i0);
+    } else {
+        scatter_codes(s.m_codes, at, n, lane, x.mc);
+        scatter_codes(s.v_codes, at, n, lane, x.vc);
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) {
+            const size_t j = at + lane + 32 * i;
+            if (j < n) {
+                w[j] = x.w[i];
+                if (copy) copy[j] = __float2bfloat16_rn(x.w[i]);
+            }
+        }
+    }
+    Block8::store_scales(s, blk, top, lane, c);
+}
+
+// Short lists: one warp to a block, straight from global memory.
 template <typename G, int CAP>
 __global__ void __launch_bounds__(kThreads)
 fold_apply8_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f, ApplyConstants c,
@@ -146,68 +258,143 @@ fold_apply8_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f, App
     if (factor != factor) return;  // a NaN factor (non-finite gradient norm) skips the step
     const unsigned total = tab.chunk_start[tab.count];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x) {
+    for (unsigned i = blockIdx.x; i < total * (kBlocks / kWarps); i += gridDim.x) {
+        const unsigned chunk = i / (kBlocks / kWarps);
         const int t = tensor_of_chunk(tab.chunk_start, tab.count, chunk);
-        const size_t n = (size_t)tab.n[t], first = (size_t)(chunk - tab.chunk_start[t]) * kChunk;
-        const adama_state8 s = tab.s[t];
-        const G *g = static_cast<const G *>(tab.g[t]);
-        float *w = tab.w[t];
-        __nv_bfloat16 *copy = tab.copy[t];
-        for (int b = 0; b < kBlocksPerWarp; ++b) {
-            const size_t at = first + (size_t)(warp + b * kWarps) * kStateBlock;
-            if (at >= n) break;
-            const size_t blk = at / kStateBlock;
-            const float sm = s.m_scale[blk], sv = s.v_scale[blk];
-            Lane x;
-            uint2 mc, vc;
-            float gg[kPerLane], ww[kPerLane];
-            const bool wide = tab.vec[t] && at + kStateBlock <= n;
-            const size_t i0 = at + lane * kPerLane;
-            if (wide) {
-                load_grad8(g + i0, gg);
-                load8(w + i0, ww);
-                mc = load_codes(s.m_codes + i0);
-                vc = load_codes(s.v_codes + i0);
-            } else {
-                mc = gather_codes(s.m_codes, at, n, lane);
-                vc = gather_codes(s.v_codes, at, n, lane);
-#pragma unroll
-                for (int i = 0; i < kPerLane; ++i) {
-                    const size_t j = at + lane + 32 * i;
-                    gg[i] = j < n ? widen(g[j]) : 0.f;
-                    ww[i] = j < n ? w[j] : 0.f;
-                }
-            }
-            x.decode(mc, vc, sm, sv);
-#pragma unroll
-            for (int i = 0; i < kPerLane; ++i) step8_1(__fmul_rn(gg[i], factor), ww[i], x.m[i], x.v[i], f, c);
-            const float2 top = x.encode(mc, vc);
-            if (wide) {
-                store8(w + i0, ww);
-                store_codes(s.m_codes + i0, mc);
-                store_codes(s.v_codes + i0, vc);
-                if (copy)
-                    *reinterpret_cast<uint4 *>(copy + i0) =
-                        make_uint4(pack2_bf16(ww[0], ww[1]), pack2_bf16(ww[2], ww[3]),
-                                   pack2_bf16(ww[4], ww[5]), pack2_bf16(ww[6], ww[7]));
-            } else {
-                scatter_codes(s.m_codes, at, n, lane, mc);
-                scatter_codes(s.v_codes, at, n, lane, vc);
-#pragma unroll
-                for (int i = 0; i < kPerLane; ++i) {
-                    const size_t j = at + lane + 32 * i;
-                    if (j < n) {
-                        w[j] = ww[i];
-                        if (copy) copy[j] = __float2bfloat16_rn(ww[i]);
-                    }
-                }
-            }
+        const size_t n = (size_t)tab.n[t];
+        const size_t at = (size_t)(chunk - tab.chunk_start[t]) * kChunk +
+                          (size_t)(i % (kBlocks / kWarps) * kWarps + warp) * kStateBlock;
+        if (at < n)
+            block_direct(static_cast<const G *>(tab.g[t]), tab.w[t], tab.copy[t], tab.s[t], at, n,
+                         tab.vec[t] && at + kStateBlock <= n, lane, factor, f, c);
+    }
+}
+
+// Long lists: a producer warp keeps several chunks' gradients, weights, codes and scales on their way
+// to shared memory by bulk copies; each of the other warps takes one block of a chunk.
+template <typename G>
+struct Stage8 {
+    alignas(16) float w[kChunk];
+    alignas(16) G g[kChunk];
+    alignas(16) uint8_t m[kChunk], v[kChunk];
+    alignas(16) float sm[kBlocks], sv[kBlocks];
+};
+template <typename G>
+struct Ring8 {
+    static constexpr int kStages = sizeof(G) == 2 ? 6 : 5;
+    Stage8<G> stage[kStages];
+    unsigned long long full[kStages], empty[kStages];
+    int tensor[kStages];
+    int give_up;
+};
+constexpr int kRingWarps = kBlocks;
+constexpr int kRingThreads = 32 * (kRingWarps + 1);
+
+template <typename G, int CAP>
+__global__ void __launch_bounds__(kRingThreads, 1)
+fold_apply8_ring_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f, ApplyConstants c,
+                        const float *__restrict__ factor_ptr, unsigned *status) {
+    extern __shared__ unsigned char raw[];
+    Ring8<G> &sh = *reinterpret_cast<Ring8<G> *>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
+    constexpr int kStages = Ring8<G>::kStages;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const float factor = factor_ptr ? *factor_ptr : 1.f;
+    if (factor != factor) return;  // a NaN factor (non-finite gradient norm) skips the step
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            barrier_init(shared_addr(&sh.full[i]), 1 + 32);  // the bulk copies, and each lane's scales
+            barrier_init(shared_addr(&sh.empty[i]), kRingWarps);
+        }
+        sh.give_up = 0;
+        barrier_init_fence();
+    }
+    __syncthreads();
+    const unsigned total = tab.chunk_start[tab.count];
+    int slot = 0;
+    uint32_t parity = 0;
+    const auto advance = [&]() {
+        if (++slot == kStages) {
+            slot = 0;
+            parity ^= 1;
+        }
+    };
+    if (warp == kRingWarps) {
+        int issued = 0;
+        for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x, advance()) {
+            const int t = tensor_of_chunk(tab.chunk_start, tab.count, chunk);
+            const size_t first = (size_t)(chunk - tab.chunk_start[t]) * kChunk, left = (size_t)tab.n[t] - first;
+            const adama_state8 &s = tab.s[t];
+            Stage8<G> &st = sh.stage[slot];
+            const uint32_t full = shared_addr(&sh.full[slot]);
+            if (issued == kStages && !barrier_wait(shared_addr(&sh.empty[slot]), parity ^ 1, &sh.give_up)) break;
+            __syncwarp();
             if (lane == 0) {
-                s.m_scale[blk] = __fmul_rn(__fmul_rn(top.x, kMTopInv), c.beta1_hi);
-                s.v_scale[blk] = __fmul_rn(__fmul_rn(top.y, kVTopInv), c.beta2_hi);
+                sh.tensor[slot] = t;
+                // whole blocks of an aligned tensor; the warps fetch the rest themselves
+                const uint32_t blocks = tab.vec[t] ? (uint32_t)(left < kChunk ? left / kStateBlock : kBlocks) : 0;
+                const uint32_t k = blocks * kStateBlock;
+                barrier_expect(full, k * (6 + (uint32_t)sizeof(G)));
+                if (k) {
+                    bulk_load(shared_addr(st.w), tab.w[t] + first, 4 * k, full);
+                    bulk_load(shared_addr(st.g), static_cast<const G *>(tab.g[t]) + first, k * (uint32_t)sizeof(G), full);
+                    bulk_load(shared_addr(st.m), s.m_codes + first, k, full);
+                    bulk_load(shared_addr(st.v), s.v_codes + first, k, full);
+                }
+            }
+            const int b = lane % kBlocks;
+            if ((size_t)b * kStateBlock < left) {
+                if (lane < kBlocks) small_load(shared_addr(st.sm + b), s.m_scale + first / kStateBlock + b);
+                else small_load(shared_addr(st.sv + b), s.v_scale + first / kStateBlock + b);
+            }
+            small_loads_arrive(full);
+            if (issued < kStages) ++issued;
+        }
+        if (*(volatile int *)&sh.give_up) {  // copies in flight end before the CTA does
+            small_loads_wait();
+            int none = 0;
+            for (int i = 0; i < issued; ++i) {
+                if (slot == 0) parity ^= 1;
+                slot = slot ? slot - 1 : kStages - 1;
+                barrier_wait(shared_addr(&sh.full[slot]), parity, &none);
             }
         }
+        return;
     }
+    for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x, advance()) {
+        if (!barrier_wait(shared_addr(&sh.full[slot]), parity, &sh.give_up)) break;  // nothing of this chunk is written
+        const int t = sh.tensor[slot];
+        const size_t n = (size_t)tab.n[t], first = (size_t)(chunk - tab.chunk_start[t]) * kChunk;
+        const size_t at = first + (size_t)warp * kStateBlock;
+        const adama_state8 s = tab.s[t];
+        if (tab.vec[t] && at + kStateBlock <= n) {
+            const Stage8<G> &st = sh.stage[slot];
+            const int o = warp * kStateBlock + 4 * lane;
+            const size_t blk = at / kStateBlock;
+            Block8 x;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                put4(x.w, h, *reinterpret_cast<const float4 *>(st.w + o + kHalf * h));
+                const Grad4 q = shared_grad4(st.g + o + kHalf * h);
+                put4(x.g, h, make_float4(q.x, q.y, q.z, q.w));
+            }
+            x.mc = load_codes(st.m + o);
+            x.vc = load_codes(st.v + o);
+            x.sm = st.sm[warp];
+            x.sv = st.sv[warp];
+            __syncwarp();
+            if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
+            const float2 top = x.update(factor, f, c);
+            x.store_wide(s, tab.w[t], tab.copy[t], at + 4 * lane);
+            Block8::store_scales(s, blk, top, lane, c);
+        } else {
+            if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
+            if (at < n)
+                block_direct(static_cast<const G *>(tab.g[t]), tab.w[t], tab.copy[t], s, at, n, false, lane, factor, f, c);
+        }
+    }
+    if (threadIdx.x == 0 && *(volatile int *)&sh.give_up &&
+        atomicCAS(status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
+        status[1] = kWaitState8Ring;
 }
 
 template <int CAP>
@@ -222,63 +409,95 @@ struct ConvertTable {
 };
 static_assert(sizeof(ConvertTable<kStep8Max>) <= 32000, "table must fit the kernel parameter space");
 
-// PACK: fp32 moments -> codes and scales; otherwise codes and scales -> the values they stand for.
-template <bool PACK, int CAP>
+// fp32 moments -> codes and scales; one warp to a block.
+template <int CAP>
 __global__ void __launch_bounds__(kThreads)
-state8_convert_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
+state8_pack_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
     const unsigned total = tab.chunk_start[tab.count];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x) {
         const int t = tensor_of_chunk(tab.chunk_start, tab.count, chunk);
         const size_t n = (size_t)tab.n[t], first = (size_t)(chunk - tab.chunk_start[t]) * kChunk;
         const adama_state8 s = tab.s[t];
-        float *m = tab.m[t], *v = tab.v[t];
-        for (int b = 0; b < kBlocksPerWarp; ++b) {
+        const float *m = tab.m[t], *v = tab.v[t];
+        for (int b = 0; b < kBlocks / kWarps; ++b) {
             const size_t at = first + (size_t)(warp + b * kWarps) * kStateBlock;
             if (at >= n) break;
-            const size_t blk = at / kStateBlock, i0 = at + lane * kPerLane;
+            const size_t blk = at / kStateBlock, i0 = at + 4 * lane;
             const bool wide = tab.vec[t] && at + kStateBlock <= n;
             Lane x;
             uint2 mc, vc;
-            if (PACK) {
-                if (wide) {
-                    load8(m + i0, x.m);
-                    load8(v + i0, x.v);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kPerLane; ++i) {
-                        const size_t j = at + lane + 32 * i;
-                        x.m[i] = j < n ? m[j] : 0.f;
-                        x.v[i] = j < n ? v[j] : 0.f;
-                    }
-                }
-                const float2 top = x.encode(mc, vc);
-                if (wide) {
-                    store_codes(s.m_codes + i0, mc);
-                    store_codes(s.v_codes + i0, vc);
-                } else {
-                    scatter_codes(s.m_codes, at, n, lane, mc);
-                    scatter_codes(s.v_codes, at, n, lane, vc);
-                }
-                if (lane == 0) {
-                    s.m_scale[blk] = __fmul_rn(top.x, kMTopInv);
-                    s.v_scale[blk] = __fmul_rn(top.y, kVTopInv);
-                }
+            if (wide) {
+                load8(m + i0, x.m);
+                load8(v + i0, x.v);
             } else {
-                mc = wide ? load_codes(s.m_codes + i0) : gather_codes(s.m_codes, at, n, lane);
-                vc = wide ? load_codes(s.v_codes + i0) : gather_codes(s.v_codes, at, n, lane);
-                x.decode(mc, vc, s.m_scale[blk], s.v_scale[blk]);
-                if (wide) {
-                    store8(m + i0, x.m);
-                    store8(v + i0, x.v);
-                } else {
 #pragma unroll
-                    for (int i = 0; i < kPerLane; ++i) {
-                        const size_t j = at + lane + 32 * i;
-                        if (j < n) {
-                            m[j] = x.m[i];
-                            v[j] = x.v[i];
-                        }
+                for (int i = 0; i < kPerLane; ++i) {
+                    const size_t j = at + lane + 32 * i;
+                    x.m[i] = j < n ? m[j] : 0.f;
+                    x.v[i] = j < n ? v[j] : 0.f;
+                }
+            }
+            const float2 top = x.encode(mc, vc);
+            if (wide) {
+                store_codes(s.m_codes + i0, mc);
+                store_codes(s.v_codes + i0, vc);
+            } else {
+                scatter_codes(s.m_codes, at, n, lane, mc);
+                scatter_codes(s.v_codes, at, n, lane, vc);
+            }
+            if (lane == 0) {
+                s.m_scale[blk] = __fmul_rn(top.x, kMTopInv);
+                s.v_scale[blk] = __fmul_rn(top.y, kVTopInv);
+            }
+        }
+    }
+}
+
+// Codes and scales -> the values they stand for; one warp to kUnpackBlocks consecutive blocks, whose
+// loads are all issued before the first store.
+constexpr int kUnpackBlocks = kBlocks / kWarps;
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads)
+state8_unpack_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
+    const unsigned total = tab.chunk_start[tab.count];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x) {
+        const int t = tensor_of_chunk(tab.chunk_start, tab.count, chunk);
+        const size_t n = (size_t)tab.n[t];
+        const size_t first = (size_t)(chunk - tab.chunk_start[t]) * kChunk + (size_t)warp * kUnpackBlocks * kStateBlock;
+        const adama_state8 s = tab.s[t];
+        float *m = tab.m[t], *v = tab.v[t];
+        uint2 mc[kUnpackBlocks], vc[kUnpackBlocks];
+        float sm[kUnpackBlocks], sv[kUnpackBlocks];
+#pragma unroll
+        for (int b = 0; b < kUnpackBlocks; ++b) {
+            const size_t at = first + b * kStateBlock, blk = at / kStateBlock;
+            if (at < n) {
+                const bool wide = tab.vec[t] && at + kStateBlock <= n;
+                mc[b] = wide ? load_codes(s.m_codes + at + 4 * lane) : gather_codes(s.m_codes, at, n, lane);
+                vc[b] = wide ? load_codes(s.v_codes + at + 4 * lane) : gather_codes(s.v_codes, at, n, lane);
+                sm[b] = s.m_scale[blk];
+                sv[b] = s.v_scale[blk];
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kUnpackBlocks; ++b) {
+            const size_t at = first + b * kStateBlock;
+            if (at >= n) continue;
+            Lane x;
+            x.decode(mc[b], vc[b], sm[b], sv[b]);
+            if (tab.vec[t] && at + kStateBlock <= n) {
+                store8(m + at + 4 * lane, x.m);
+                store8(v + at + 4 * lane, x.v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPerLane; ++i) {
+                    const size_t j = at + lane + 32 * i;
+                    if (j < n) {
+                        m[j] = x.m[i];
+                        v[j] = x.v[i];
                     }
                 }
             }
@@ -286,16 +505,42 @@ state8_convert_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
     }
 }
 
-bool state_wide(const adama_state8 &s) { return aligned(s.m_codes, 8) && aligned(s.v_codes, 8); }
+bool state_wide(const adama_state8 &s) { return aligned(s.m_codes, 16) && aligned(s.v_codes, 16); }
+
+constexpr unsigned kRingFrom = 2;  // chunks per SM from which the ring is used
 
 unsigned grid_of(unsigned chunks, int sm_count, int per_sm) {
     const unsigned cap = (unsigned)(sm_count * per_sm);
     return chunks < cap ? chunks : cap;
 }
 
+template <typename G, int CAP>
+cudaError_t launch_kernels(const Table8<CAP> &tab, unsigned chunks, FoldConstants f, ApplyConstants c, const float *factor,
+                           unsigned *status, int sm_count, cudaStream_t stream) {
+    if (chunks < kRingFrom * (unsigned)sm_count) {
+        const unsigned ctas = chunks * (kBlocks / kWarps);
+        fold_apply8_kernel<G, CAP><<<grid_of(ctas, sm_count, 4), kThreads, 0, stream>>>(tab, f, c, factor);
+        return cudaGetLastError();
+    }
+    constexpr int bytes = (int)sizeof(Ring8<G>) + 128;
+    static std::atomic<unsigned long long> ready{0};  // one bit per device: the attribute is set
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (!(ready.load() & bit)) {
+        e = cudaFuncSetAttribute(fold_apply8_ring_kernel<G, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != cudaSuccess) return e;
+        ready.fetch_or(bit);
+    }
+    fold_apply8_ring_kernel<G, CAP><<<grid_of(chunks, sm_count, 1), kRingThreads, bytes, stream>>>(tab, f, c, factor, status);
+    return cudaGetLastError();
+}
+
 template <int CAP>
 cudaError_t launch_step(const StepList &s, adama_dtype gdt, int first, int count, FoldConstants f,
-                        ApplyConstants c, const float *factor, int sm_count, cudaStream_t stream) {
+                        ApplyConstants c, const float *factor, unsigned *status, int sm_count,
+                        cudaStream_t stream) {
     Table8<CAP> tab;
     for (int i = 0; i < count; ++i) {
         tab.g[i] = s.g[first + i];
@@ -307,12 +552,8 @@ cudaError_t launch_step(const StepList &s, adama_dtype gdt, int first, int count
     tab.count = count;
     const unsigned chunks = fill_chunks(tab.n, tab.chunk_start, s.n + first, count);
     if (chunks == 0) return cudaSuccess;
-    const unsigned grid = grid_of(chunks, sm_count, 4);
-    if (gdt == ADAMA_F32)
-        fold_apply8_kernel<float, CAP><<<grid, kThreads, 0, stream>>>(tab, f, c, factor);
-    else
-        fold_apply8_kernel<__nv_bfloat16, CAP><<<grid, kThreads, 0, stream>>>(tab, f, c, factor);
-    return cudaGetLastError();
+    return gdt == ADAMA_F32 ? launch_kernels<float>(tab, chunks, f, c, factor, status, sm_count, stream)
+                            : launch_kernels<__nv_bfloat16>(tab, chunks, f, c, factor, status, sm_count, stream);
 }
 
 template <bool PACK, int CAP>
@@ -327,7 +568,8 @@ cudaError_t launch_convert(const StepList &s, int first, int count, int sm_count
     tab.count = count;
     const unsigned chunks = fill_chunks(tab.n, tab.chunk_start, s.n + first, count);
     if (chunks == 0) return cudaSuccess;
-    state8_convert_kernel<PACK, CAP><<<grid_of(chunks, sm_count, 8), kThreads, 0, stream>>>(tab);
+    if (PACK) state8_pack_kernel<CAP><<<grid_of(chunks, sm_count, 8), kThreads, 0, stream>>>(tab);
+    else state8_unpack_kernel<CAP><<<grid_of(chunks, sm_count, 8), kThreads, 0, stream>>>(tab);
     return cudaGetLastError();
 }
 
@@ -335,9 +577,9 @@ cudaError_t launch_convert(const StepList &s, int first, int count, int sm_count
 
 cudaError_t launch_fold_apply8_multi(const StepList &s, adama_dtype gdt, int first, int count,
                                      FoldConstants f, ApplyConstants c, const float *factor,
-                                     int sm_count, cudaStream_t stream) {
-    return count <= kStepSmall ? launch_step<kStepSmall>(s, gdt, first, count, f, c, factor, sm_count, stream)
-                               : launch_step<kStep8Max>(s, gdt, first, count, f, c, factor, sm_count, stream);
+                                     unsigned *status, int sm_count, cudaStream_t stream) {
+    return count <= kStepSmall ? launch_step<kStepSmall>(s, gdt, first, count, f, c, factor, status, sm_count, stream)
+                               : launch_step<kStep8Max>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
 }
 
 cudaError_t launch_state8_convert(const StepList &s, bool pack, int first, int count, int sm_count,
