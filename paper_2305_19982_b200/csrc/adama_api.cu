@@ -614,7 +614,7 @@ static adama_status fold_apply_impl(adama_ctx *ctx, const void *const *grads, ad
         return packed ? adama::launch_fold_apply8_multi(list, gdt, first, k, ctx->fold_c, c, grad_factor,
                                                         ctx->status_dev, ctx->sm_count, stream)
                       : adama::launch_fold_apply_multi(list, gdt, first, k, ctx->fold_c, c, grad_factor,
-                                                       ctx->sm_count, stream);
+                                                       ctx->status_dev, ctx->sm_count, stream);
     });
 }
 

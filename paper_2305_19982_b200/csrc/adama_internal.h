@@ -99,7 +99,7 @@ struct StepList {  // host arrays; each launch takes a range of them
 };
 cudaError_t launch_fold_apply_multi(const StepList &s, adama_dtype gdt, int first, int count,
                                     FoldConstants f, ApplyConstants c, const float *factor,
-                                    int sm_count, cudaStream_t stream);
+                                    unsigned *status, int sm_count, cudaStream_t stream);
 cudaError_t launch_fold_apply8_multi(const StepList &s, adama_dtype gdt, int first, int count,
                                      FoldConstants f, ApplyConstants c, const float *factor,
                                      unsigned *status, int sm_count, cudaStream_t stream);

@@ -5,7 +5,6 @@
 //     kl = exp(d) - d - 1,  loss += w*(pg + beta*kl)
 //     dlogits_j = w*s*c*([j = target] - p_j),  c = -(r*A while r*A <= the clamped product) + beta*(1 - exp(d))
 // A row is read once (loss: and its gradient written once); what bounds every form is HBM.
-#include <atomic>
 #include <type_traits>
 
 #include "adama_device.cuh"
@@ -665,16 +664,9 @@ cudaError_t policy_rows(const PolicyArgs &a, float k, int sm_count, cudaStream_t
 template <typename T, typename O>
 cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count, cudaStream_t stream) {
     constexpr size_t bytes = sizeof(RingShared) + 128;
-    static std::atomic<unsigned long long> ready{0};  // one bit per device: the attribute is set
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
+    static std::atomic<unsigned long long> ready{0};
+    cudaError_t e = allow_shared(policy_loss_ring_kernel<T, O>, (int)bytes, ready);
     if (e != cudaSuccess) return e;
-    const unsigned long long bit = device < 64 ? 1ull << device : 0;
-    if (!(ready.load() & bit)) {
-        e = cudaFuncSetAttribute(policy_loss_ring_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e != cudaSuccess) return e;
-        ready.fetch_or(bit);
-    }
     cudaLaunchConfig_t cfg = {};
     const int64_t most = sm_count * kRingsPerSm / cluster;
     cfg.gridDim = dim3((unsigned)((a.rows < 1 ? 1 : a.rows < most ? a.rows : most) * cluster));

@@ -1,8 +1,11 @@
-// Lists of tensors in a kernel's parameter space: the work of one launch is the list's chunks of
-// kChunk elements, numbered through all tensors; a CTA finds the tensor of a chunk by bisection.
+// Lists of tensors in a kernel's parameter space: the work of one launch is the list's chunks (of
+// kChunk elements, or what the kernel states), numbered through all tensors; a CTA finds the tensor
+// of a chunk by bisection.
 #pragma once
 
 #include <cuda_bf16.h>
+
+#include <atomic>
 
 #include "adama_internal.h"
 #include "stream_access.cuh"
@@ -22,13 +25,22 @@ __device__ __forceinline__ int tensor_of_chunk(const unsigned *chunk_start, int 
     return lo;
 }
 
+// The same for a chunk behind one that lies in tensor t: steps forward from there (a loop over chunks
+// passes few tensor borders at a time; bisecting anew for each chunk cost the producers of the rings
+// more than the copies that they issue).
+__device__ __forceinline__ int tensor_from(const unsigned *chunk_start, int t, unsigned c) {
+    while (chunk_start[t + 1] <= c) ++t;
+    return t;
+}
+
 // Fills n and chunk_start for `count` tensors; returns the number of chunks.
-inline unsigned fill_chunks(unsigned long long *n_out, unsigned *chunk_start, const size_t *n, int count) {
+inline unsigned fill_chunks(unsigned long long *n_out, unsigned *chunk_start, const size_t *n, int count,
+                            size_t chunk = kChunk) {
     unsigned acc = 0;
     for (int i = 0; i < count; ++i) {
         n_out[i] = (unsigned long long)n[i];
         chunk_start[i] = acc;
-        acc += (unsigned)((n[i] + kChunk - 1) / kChunk);
+        acc += (unsigned)((n[i] + chunk - 1) / chunk);
     }
     chunk_start[count] = acc;
     return acc;
@@ -49,6 +61,30 @@ __device__ __forceinline__ void load_grad8(const __nv_bfloat16 *g, float (&x)[8]
         x[2 * i] = __uint_as_float(u[i] << 16);
         x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
     }
+}
+
+// four gradient values from shared memory, widened exactly
+__device__ __forceinline__ Grad4 shared_grad4(const float *p) {
+    const float4 t = *reinterpret_cast<const float4 *>(p);
+    return {t.x, t.y, t.z, t.w};
+}
+__device__ __forceinline__ Grad4 shared_grad4(const __nv_bfloat16 *p) {
+    const uint2 t = *reinterpret_cast<const uint2 *>(p);
+    return {__uint_as_float(t.x << 16), __uint_as_float(t.x & 0xffff0000u),
+            __uint_as_float(t.y << 16), __uint_as_float(t.y & 0xffff0000u)};
+}
+
+// Sets a kernel's limit of dynamic shared memory once per device (`ready`: one bit per device).
+template <typename Kernel>
+inline cudaError_t allow_shared(Kernel kernel, int bytes, std::atomic<unsigned long long> &ready) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (ready.load() & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) ready.fetch_or(bit);
+    return e;
 }
 
 // two fp32 -> packed bf16x2, round to nearest even (the weight copy a bf16 forward pass reads)
