@@ -2,13 +2,17 @@
 // device for the step that multiplies by it.  One pass, 2 or 4 B/element; each CTA's sum goes to
 // the workspace as a double, the last CTA to finish adds them in the CTAs' order, so that the
 // result does not depend on scheduling.
+#include "softmax_rows.cuh"
 #include "tensor_table.cuh"
 
 namespace adama {
 namespace {
 
 constexpr int kThreads = 256;
+// 4 CTAs per SM with 8 units of each thread in flight: 369 M bf16 gradients take 107.7 us (6.85 TB/s);
+// 4 x 4 109.3, 8 x 4 111.6, 2 x 8 109.4, 2 x 16 106.3 but 8.4 instead of 5.7 us for short lists.
 constexpr int kCtasPerSm = 4;
+constexpr int kLongUnits = 8, kShortUnits = 2;
 
 template <int CAP>
 struct NormTable {
@@ -30,45 +34,55 @@ __device__ __forceinline__ double block_sum(double x, double *shared) {
     return sum;
 }
 
-template <typename G, int CAP>
+// A chunk is UNITS 16-byte units of each thread, all loaded before the first is used.
+template <typename G, int UNITS, int CAP>
 __global__ void __launch_bounds__(kThreads)
 grad_norm_kernel(const __grid_constant__ NormTable<CAP> tab, float max_norm, int accumulate,
                  adama_grad_norm *out, Workspace *ws) {
-    constexpr int kVec = 16 / sizeof(G);
+    constexpr int kVec = 16 / sizeof(G), kNormChunk = UNITS * kThreads * kVec;
     __shared__ double shared[kThreads / 32];
     __shared__ bool last;
     const unsigned total = tab.chunk_start[tab.count];
     double sum = 0.0;
+    int t = tensor_of_chunk(tab.chunk_start, tab.count, blockIdx.x);
     for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x) {
-        const int t = tensor_of_chunk(tab.chunk_start, tab.count, chunk);
-        const size_t n = (size_t)tab.n[t], first = (size_t)(chunk - tab.chunk_start[t]) * kChunk;
+        t = tensor_from(tab.chunk_start, t, chunk);
+        const size_t n = (size_t)tab.n[t], first = (size_t)(chunk - tab.chunk_start[t]) * kNormChunk;
         const G *g = static_cast<const G *>(tab.g[t]);
         const size_t mis = (reinterpret_cast<uintptr_t>(g) % 16) / sizeof(G);
-        const size_t head = mis ? kVec - mis : 0;  // chunk c covers [head + c*kChunk, ...), the first one the head too
+        const size_t head = mis ? kVec - mis : 0;  // chunk c covers [head + c*kNormChunk, ...), the first one the head too
+        const size_t base = head + first + (size_t)threadIdx.x * kVec;
         float part = 0.f;
+        uint4 u[UNITS];
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            u[i] = make_uint4(0, 0, 0, 0);
+            if (base + (size_t)i * kThreads * kVec + kVec <= n)
+                u[i] = ld_unit_ro(reinterpret_cast<const uint4 *>(g + base + (size_t)i * kThreads * kVec));
+        }
         if (first == 0 && threadIdx.x < head && threadIdx.x < n) {
             const float x = widen(g[threadIdx.x]);
             part = fmaf(x, x, part);
         }
-#pragma unroll
-        for (int u = 0; u < kChunk / (kVec * kThreads); ++u) {
-            const size_t i = head + first + (size_t)(u * kThreads + threadIdx.x) * kVec;
-            if (i + kVec <= n) {
-                if (sizeof(G) == 2) {
-                    float x[8];
-                    load_grad8(g + i, x);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) part = fmaf(x[j], x[j], part);
-                } else {
-                    const Grad4 x = load_grad4(g + i, 0);
-                    part = fmaf(x.x, x.x, fmaf(x.y, x.y, fmaf(x.z, x.z, fmaf(x.w, x.w, part))));
-                }
-            } else {
-                for (size_t j = i; j < n && j < i + kVec; ++j) {
+        if (base + kNormChunk > n) {  // the unit that the tensor's end cuts, if it is one of this thread's
+            const size_t end = n > head ? head + (n - head) / kVec * kVec : n;
+            if (end >= base && (end - base) % (kThreads * kVec) == 0)
+                for (size_t j = end; j < n; ++j) {
                     const float x = widen(g[j]);
                     part = fmaf(x, x, part);
                 }
+        }
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            Pair p = 0;
+#pragma unroll
+            for (int q = 0; q < kVec / 2; ++q) {
+                const Pair x = unit_pair<G>(u[i], q);
+                p = fma2(x, x, p);
             }
+            float lo, hi;
+            split(p, lo, hi);
+            part += lo + hi;
         }
         sum += (double)part;
     }
@@ -94,21 +108,39 @@ grad_norm_kernel(const __grid_constant__ NormTable<CAP> tab, float max_norm, int
     }
 }
 
-template <int CAP>
-cudaError_t launch(const void *const *g, adama_dtype gdt, const size_t *n, int count, float max_norm,
-                   int accumulate, adama_grad_norm *out, Workspace *ws, int sm_count, cudaStream_t stream) {
-    NormTable<CAP> tab;
-    for (int i = 0; i < count; ++i) tab.g[i] = g[i];
-    tab.count = count;
-    const unsigned chunks = fill_chunks(tab.n, tab.chunk_start, n, count);
+template <typename G, int UNITS, int CAP>
+cudaError_t launch_kernel(NormTable<CAP> &tab, const size_t *n, int count, float max_norm, int accumulate,
+                          adama_grad_norm *out, Workspace *ws, int sm_count, cudaStream_t stream) {
+    const unsigned chunks = fill_chunks(tab.n, tab.chunk_start, n, count, UNITS * kThreads * 16 / sizeof(G));
     unsigned cap = (unsigned)(sm_count * kCtasPerSm);
     if (cap > kWorkspaceParts) cap = kWorkspaceParts;
     const unsigned grid = chunks == 0 ? 1 : chunks < cap ? chunks : cap;
-    if (gdt == ADAMA_F32)
-        grad_norm_kernel<float, CAP><<<grid, kThreads, 0, stream>>>(tab, max_norm, accumulate, out, ws);
-    else
-        grad_norm_kernel<__nv_bfloat16, CAP><<<grid, kThreads, 0, stream>>>(tab, max_norm, accumulate, out, ws);
+    grad_norm_kernel<G, UNITS, CAP><<<grid, kThreads, 0, stream>>>(tab, max_norm, accumulate, out, ws);
     return cudaGetLastError();
+}
+
+template <typename G, int CAP>
+cudaError_t launch(const void *const *g, const size_t *n, int count, float max_norm, int accumulate,
+                   adama_grad_norm *out, Workspace *ws, int sm_count, cudaStream_t stream) {
+    NormTable<CAP> tab;
+    size_t all = 0;
+    for (int i = 0; i < count; ++i) {
+        tab.g[i] = g[i];
+        all += n[i];
+    }
+    tab.count = count;
+    // long chunks where every CTA has several of them, else as many CTAs as there is work for
+    const size_t several = (size_t)kLongUnits * kThreads * 16 / sizeof(G) * (size_t)sm_count * kCtasPerSm * 4;
+    return all >= several
+               ? launch_kernel<G, kLongUnits, CAP>(tab, n, count, max_norm, accumulate, out, ws, sm_count, stream)
+               : launch_kernel<G, kShortUnits, CAP>(tab, n, count, max_norm, accumulate, out, ws, sm_count, stream);
+}
+
+template <typename G>
+cudaError_t launch(const void *const *g, const size_t *n, int count, float max_norm, int accumulate,
+                   adama_grad_norm *out, Workspace *ws, int sm_count, cudaStream_t stream) {
+    return count <= kStepSmall ? launch<G, kStepSmall>(g, n, count, max_norm, accumulate, out, ws, sm_count, stream)
+                               : launch<G, kNormMax>(g, n, count, max_norm, accumulate, out, ws, sm_count, stream);
 }
 
 }  // namespace
@@ -117,9 +149,9 @@ cudaError_t launch_grad_norm(const void *const *g, adama_dtype gdt, const size_t
                              float max_norm, int accumulate, adama_grad_norm *out, void *workspace,
                              int sm_count, cudaStream_t stream) {
     Workspace *ws = static_cast<Workspace *>(workspace);
-    return count <= kStepSmall
-               ? launch<kStepSmall>(g, gdt, n, count, max_norm, accumulate, out, ws, sm_count, stream)
-               : launch<kNormMax>(g, gdt, n, count, max_norm, accumulate, out, ws, sm_count, stream);
+    return gdt == ADAMA_F32
+               ? launch<float>(g, n, count, max_norm, accumulate, out, ws, sm_count, stream)
+               : launch<__nv_bfloat16>(g, n, count, max_norm, accumulate, out, ws, sm_count, stream);
 }
 
 }  // namespace adama

@@ -59,6 +59,14 @@ __device__ __forceinline__ uint4 ld_unit(const uint4 *p) {
     return r;
 }
 
+__device__ __forceinline__ uint4 ld_unit_ro(const uint4 *p) {
+    uint4 r;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+                 : "l"(p));
+    return r;
+}
+
 // ---- 16-byte units -------------------------------------------------------------------------------
 template <typename T>
 constexpr int kUnit = 16 / sizeof(T);  // values in a unit
