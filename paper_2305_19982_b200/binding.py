@@ -184,7 +184,14 @@ def host_constants(beta1, beta2, eps, n_micro, t, lr, flags=0, world_size=1, sha
     return [float(x) for x in out]
 
 
+# the current stream's handle without building a Stream object around it (2 us of a 6 us call), where
+# torch offers that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_ptr(device) -> int:
+    if _raw_stream is not None:
+        return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
 
 
@@ -210,6 +217,7 @@ class TensorList:
             self.ptrs[i] = _dev_ptr(t, self.dtype, f"tensor {i}")
         self.numels = [t.numel() for t in self.tensors]
         self.ns = (ctypes.c_size_t * len(self.tensors))(*self.numels)
+        self.sizes = bytes(self.ns)  # for comparing lists of sizes at once
 
     def __len__(self):
         return len(self.tensors)
@@ -251,6 +259,7 @@ class State8List:
         self.items = (_State8 * len(self.states))(*[s._item for s in self.states])
         self.numels = [s.numel for s in self.states]
         self.ns = (ctypes.c_size_t * len(self.states))(*self.numels)
+        self.sizes = bytes(self.ns)
 
     def __len__(self):
         return len(self.states)
@@ -554,14 +563,15 @@ class AdamA:
         return t.data_ptr()
 
     @staticmethod
-    def _copies(w_bf16, numels):
+    def _copies(w_bf16, ws):
         """Pointer array of the optional bf16 copies: None, or a list whose entries may be None."""
         if w_bf16 is None:
             return None
         if isinstance(w_bf16, TensorList):
-            if w_bf16.dtype != torch.bfloat16 or w_bf16.numels != numels:
+            if w_bf16.dtype != torch.bfloat16 or w_bf16.sizes != ws.sizes:
                 raise ValueError("w_bf16 must be bfloat16 tensors of the sizes of the weights")
             return w_bf16.ptrs
+        numels = ws.numels
         if len(w_bf16) != len(numels):
             raise ValueError("lists must have equal length")
         arr = (ctypes.c_void_p * len(numels))()
@@ -590,7 +600,7 @@ class AdamA:
         grads = grads if isinstance(grads, TensorList) else TensorList(grads)
         ms = ms if isinstance(ms, TensorList) else TensorList(ms, torch.float32)
         vs = vs if isinstance(vs, TensorList) else TensorList(vs, torch.float32)
-        if not ws.numels == grads.numels == ms.numels == vs.numels:
+        if not ws.sizes == grads.sizes == ms.sizes == vs.sizes:
             raise ValueError("w, grad, m, v must be lists of equal sizes")
         for t in (ws, ms, vs):
             if t.dtype != torch.float32:
@@ -599,7 +609,7 @@ class AdamA:
             raise TypeError("grads must be float32 or bfloat16")
         self._check(self._L.adama_fold_apply_multi(
             self._h, grads.ptrs, _DTYPES[grads.dtype], ws.ptrs, ms.ptrs, vs.ptrs,
-            self._copies(w_bf16, ws.numels), ws.ns, len(ws), float(lr), self._factor(grad_factor),
+            self._copies(w_bf16, ws), ws.ns, len(ws), float(lr), self._factor(grad_factor),
             _stream_ptr(self.device)))
 
     def fold_apply8_multi(self, ws, grads, states, lr: float, w_bf16=None,
@@ -609,7 +619,7 @@ class AdamA:
         ws = ws if isinstance(ws, TensorList) else TensorList(ws, torch.float32)
         grads = grads if isinstance(grads, TensorList) else TensorList(grads)
         states = states if isinstance(states, State8List) else State8List(states)
-        if not ws.numels == grads.numels == states.numels:
+        if not ws.sizes == grads.sizes == states.sizes:
             raise ValueError("w, grad, states must be lists of equal sizes")
         if ws.dtype != torch.float32:
             raise TypeError("w must be float32")
@@ -617,14 +627,14 @@ class AdamA:
             raise TypeError("grads must be float32 or bfloat16")
         self._check(self._L.adama_fold_apply8_multi(
             self._h, grads.ptrs, _DTYPES[grads.dtype], ws.ptrs, states.items,
-            self._copies(w_bf16, ws.numels), ws.ns, len(ws), float(lr), self._factor(grad_factor),
+            self._copies(w_bf16, ws), ws.ns, len(ws), float(lr), self._factor(grad_factor),
             _stream_ptr(self.device)))
 
     def _state8_convert(self, fn, states, ms, vs, pack: bool) -> None:
         states = states if isinstance(states, State8List) else State8List(states)
         ms = ms if isinstance(ms, TensorList) else TensorList(ms, torch.float32)
         vs = vs if isinstance(vs, TensorList) else TensorList(vs, torch.float32)
-        if not states.numels == ms.numels == vs.numels:
+        if not states.sizes == ms.sizes == vs.sizes:
             raise ValueError("states, m, v must be lists of equal sizes")
         if ms.dtype != torch.float32 or vs.dtype != torch.float32:
             raise TypeError("m, v must be float32")
@@ -669,9 +679,10 @@ class AdamA:
     def _per_row(t: Optional[torch.Tensor], rows: int, name: str, dtype=torch.float32):
         if t is None:
             return None
-        if t.numel() != rows or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous with one element per row")
-        return _dev_ptr(t, dtype, name)
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == rows:
+            return t.data_ptr()
+        _dev_ptr(t, dtype, name)
+        raise ValueError(f"{name} must be contiguous with one element per row")
 
     def token_logprobs(self, logits: torch.Tensor, targets: torch.Tensor, logp: torch.Tensor,
                        lse: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
