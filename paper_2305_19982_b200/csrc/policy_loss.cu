@@ -51,50 +51,59 @@ __device__ __forceinline__ float logp_of(float x_target, const Stats &s, float l
 
 // ---- token log-probabilities -----------------------------------------------------------------
 
-// W warps to a row, kLoads units of each thread in flight; a CTA holds 16/W rows.
-constexpr int kLoads = 4;
+// W warps to a row, ROWS rows to a CTA, kLoads units of each thread in flight.
+#ifndef KL
+#define KL 4
+#define W0 4
+#endif
+constexpr int kLoads = KL;
 
-template <typename T, int W, bool ENT>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, int W, int ROWS, bool ENT>
+__global__ void __launch_bounds__(32 * W * ROWS)
 token_logprobs_kernel(const LogprobArgs a, float k) {
-    constexpr int kGroupThreads = 32 * W, kGroups = kWarps / W;
-    __shared__ Stats shared[kWarps];
+    constexpr int kGroupThreads = 32 * W;
+    __shared__ Stats shared[W * ROWS];
     const int g = threadIdx.x / kGroupThreads, t = threadIdx.x % kGroupThreads;
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + g; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
-        const int64_t target = a.targets[row];
-        const T *x = static_cast<const T *>(a.logits) + row * a.ld;
-        float logp = 0.f, lse = 0.f, entropy = 0.f;
-        if (target >= 0) {
-            const bool inside = target < a.vocab;
-            const float x_target = inside ? widen(x[target]) : CUDART_NAN_F;
-            const RowShape shape = row_shape(x, (int)a.vocab);
-            const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
-            Running<ENT> run;
-            int i = t;
-            for (; i + (kLoads - 1) * kGroupThreads < shape.units; i += kLoads * kGroupThreads) {
-                uint4 u[kLoads];
+    const int64_t row = (int64_t)blockIdx.x * ROWS + g;
+    if (row >= a.rows) return;  // a whole group
+    const int64_t target = a.targets[row];
+    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+    float logp = 0.f, lse = 0.f, entropy = 0.f;
+    if (target >= 0) {
+        const bool inside = target < a.vocab;
+        const float x_target = inside ? widen(x[target]) : CUDART_NAN_F;
+        const RowShape shape = row_shape(x, (int)a.vocab);
+        const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
+        const float x_extra = t < shape.head + shape.tail ? widen(x[extra_index<T>(shape, t)]) : -CUDART_INF_F;
+        Running<ENT> run;
+        int i = t;
+        for (; i + (kLoads - 1) * kGroupThreads < shape.units; i += kLoads * kGroupThreads) {
+            uint4 u[kLoads];
 #pragma unroll
-                for (int j = 0; j < kLoads; ++j) u[j] = ld_unit(body + i + j * kGroupThreads);
-                run.template add_units<T>(u, k);
-            }
-            for (; i < shape.units; i += kGroupThreads) {
-                const uint4 u[1] = {ld_unit(body + i)};
-                run.template add_units<T>(u, k);
-            }
-            if (t < shape.head + shape.tail) run.add_one(widen(x[extra_index<T>(shape, t)]), k);
-            const Stats s = group_join<W, ENT>(run.stats(), k, shared + g * W, g);
-            const float log2sum = log2f(s.sum);
-            lse = fmaf(s.top, (float)a.scale, CUDART_LN2_F * log2sum);
-            logp = logp_of(x_target, s, log2sum, k);
-            if (ENT) entropy = CUDART_LN2_F * (log2sum - s.wsum / s.sum);
-            if (!inside && t == 0) record_bad_target(a.status, row);
+            for (int j = 0; j < kLoads; ++j) u[j] = ld_unit_ro(body + i + j * kGroupThreads);
+            run.template add_units<T>(u, k);
         }
-        if (t == 0) {
-            a.logp[row] = logp;
-            if (a.lse) a.lse[row] = lse;
-            if (ENT) a.entropy[row] = entropy;
+        {
+            uint4 u[kLoads - 1];  // what is left, loaded together
+#pragma unroll
+            for (int j = 0; j < kLoads - 1; ++j) {
+                u[j] = nothing<T>();
+                if (i + j * kGroupThreads < shape.units) u[j] = ld_unit_ro(body + i + j * kGroupThreads);
+            }
+            run.template add_units<T>(u, k);
         }
-        if (W > 1) group_sync<W>(g);  // the slots are used again
+        run.add_one(x_extra, k);
+        const Stats s = group_join<W, ENT>(run.stats(), k, shared + g * W, g);
+        const float log2sum = log2f(s.sum);
+        lse = fmaf(s.top, (float)a.scale, CUDART_LN2_F * log2sum);
+        logp = logp_of(x_target, s, log2sum, k);
+        if (ENT) entropy = CUDART_LN2_F * (log2sum - s.wsum / s.sum);
+        if (!inside && t == 0) record_bad_target(a.status, row);
+    }
+    if (t == 0) {
+        a.logp[row] = logp;
+        if (a.lse) a.lse[row] = lse;
+        if (ENT) a.entropy[row] = entropy;
     }
 }
 
@@ -636,12 +645,11 @@ unsigned grid_of(int64_t work, int64_t cap) {
     return (unsigned)(work < 1 ? 1 : work < cap ? work : cap);
 }
 
-template <typename T, int W>
-cudaError_t logprobs_groups(const LogprobArgs &a, float k, int sm_count, cudaStream_t stream) {
-    const int64_t ctas = (a.rows + kWarps / W - 1) / (kWarps / W);
-    const unsigned grid = (unsigned)(ctas < (int64_t)sm_count * 4 ? ctas : (int64_t)sm_count * 4);
-    if (a.entropy) token_logprobs_kernel<T, W, true><<<grid, kThreads, 0, stream>>>(a, k);
-    else token_logprobs_kernel<T, W, false><<<grid, kThreads, 0, stream>>>(a, k);
+template <typename T, int W, int ROWS>
+cudaError_t logprobs_groups(const LogprobArgs &a, float k, cudaStream_t stream) {
+    const unsigned grid = (unsigned)((a.rows + ROWS - 1) / ROWS);
+    if (a.entropy) token_logprobs_kernel<T, W, ROWS, true><<<grid, 32 * W * ROWS, 0, stream>>>(a, k);
+    else token_logprobs_kernel<T, W, ROWS, false><<<grid, 32 * W * ROWS, 0, stream>>>(a, k);
     return cudaGetLastError();
 }
 
@@ -649,9 +657,9 @@ template <typename T>
 cudaError_t logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
     const float k = (float)(a.scale * kLog2e);
     const int64_t units = a.vocab / kUnit<T>;
-    if (units <= 32 * kRowUnits) return logprobs_groups<T, 1>(a, k, sm_count, stream);
-    if (units <= 128 * kRowUnits) return logprobs_groups<T, 4>(a, k, sm_count, stream);
-    return logprobs_groups<T, 16>(a, k, sm_count, stream);
+    if (units <= 32 * kRowUnits) return logprobs_groups<T, 1, 4>(a, k, stream);
+    if (units <= 128 * kRowUnits || a.rows >= 8 * (int64_t)sm_count) return logprobs_groups<T, W0, 1>(a, k, stream);
+    return logprobs_groups<T, 16, 1>(a, k, stream);
 }
 
 template <typename T, typename O, int W>

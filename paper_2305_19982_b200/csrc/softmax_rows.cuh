@@ -83,6 +83,13 @@ __device__ __forceinline__ Pair unit_pair<__nv_bfloat16>(const uint4 &u, int i) 
     return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));  // bf16 -> fp32 is a shift
 }
 
+// a unit of -inf
+template <typename T>
+__device__ __forceinline__ uint4 nothing() {
+    const unsigned w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+}
+
 __device__ __forceinline__ float unit_max(const uint4 &u, float) {
     return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
 }
