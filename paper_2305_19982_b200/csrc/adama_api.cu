@@ -713,6 +713,7 @@ static adama_status check_logits(adama_ctx *ctx, const void *logits, adama_dtype
                                  int64_t vocab, int64_t ld, const int64_t *targets, double logit_scale) {
     if (rows < 0 || vocab < 1 || vocab > INT32_MAX || ld < vocab)
         return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: bad shape or a row pitch smaller than the row");
+    if (rows > INT32_MAX) return fail(ctx, ADAMA_ERR_UNSUPPORTED, "logits: more than 2^31-1 rows");
     if (dt != ADAMA_F32 && dt != ADAMA_BF16)
         return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: unknown dtype");
     if (rows > 0 && (!logits || !targets)) return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: null pointer");

@@ -75,8 +75,19 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
+}
+// Three words into the shared memory of CTA `rank` of the cluster; ordered by the next cluster_sync.
+__device__ __forceinline__ void store12(uint32_t dst, uint32_t rank, float a, float b, float c) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(dst), "r"(rank));
+    asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;"
+                 ::"r"(r), "f"(a), "f"(b), "f"(c)
+                 : "memory");
 }
 // 16 bytes into the shared memory of CTA `rank` of the cluster, announced on its barrier; dst and bar
 // are this CTA's addresses of the same variables.

@@ -49,35 +49,52 @@ __device__ __forceinline__ float logp_of(float x_target, const Stats &s, float l
     return CUDART_LN2_F * (k * (x_target - s.top) - log2sum);
 }
 
+constexpr int kMaxCluster = 8;  // CTAs that may share a row
+
+// The slice of a row's units that CTA `rank` of 2^log_size takes (units < 2^29, so 32 bits hold it).
+__device__ __forceinline__ void slice_of(int units, int rank, int log_size, int &from, int &count) {
+    from = (int)(((unsigned)units * (unsigned)rank) >> log_size);
+    count = (int)(((unsigned)units * (unsigned)(rank + 1)) >> log_size) - from;
+}
+
+__device__ __forceinline__ void store_peer(const Stats *slot, uint32_t rank, const Stats &s) {
+    store12(shared_addr(slot), rank, s.top, s.sum, s.wsum);
+}
+
 // ---- token log-probabilities -----------------------------------------------------------------
 
-// W warps to a row, ROWS rows to a CTA, kLoads units of each thread in flight.
-#ifndef KL
-#define KL 4
-#define W0 4
-#endif
-constexpr int kLoads = KL;
+// W warps to a row (or to the slice of a row that a cluster of CTAs shares), ROWS rows to a CTA, kLoads
+// units of each thread in flight.
+constexpr int kLoads = 4;
 
-template <typename T, int W, int ROWS, bool ENT>
+template <typename T, int W, int ROWS, bool ENT, bool CLUSTER>
 __global__ void __launch_bounds__(32 * W * ROWS)
-token_logprobs_kernel(const LogprobArgs a, float k) {
+token_logprobs_kernel(const LogprobArgs a, float k, int log_cluster) {
     constexpr int kGroupThreads = 32 * W;
-    __shared__ Stats shared[W * ROWS];
+    __shared__ Stats shared[W * ROWS], peers[kMaxCluster];
     const int g = threadIdx.x / kGroupThreads, t = threadIdx.x % kGroupThreads;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + g;
+    const int rank = CLUSTER ? (int)cluster_rank() : 0;
+    const int64_t row = CLUSTER ? blockIdx.x >> log_cluster : (int64_t)blockIdx.x * ROWS + g;
     if (row >= a.rows) return;  // a whole group
     const int64_t target = a.targets[row];
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     float logp = 0.f, lse = 0.f, entropy = 0.f;
     if (target >= 0) {
+        if (CLUSTER) cluster_arrive();
         const bool inside = target < a.vocab;
         const float x_target = inside ? widen(x[target]) : CUDART_NAN_F;
         const RowShape shape = row_shape(x, (int)a.vocab);
         const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
-        const float x_extra = t < shape.head + shape.tail ? widen(x[extra_index<T>(shape, t)]) : -CUDART_INF_F;
+        const bool has_extra = rank == 0 && t < shape.head + shape.tail;
+        const float x_extra = has_extra ? widen(x[extra_index<T>(shape, t)]) : -CUDART_INF_F;
+        int i = t, end = shape.units;
+        if (CLUSTER) {
+            slice_of(shape.units, rank, log_cluster, i, end);
+            end += i;
+            i += t;
+        }
         Running<ENT> run;
-        int i = t;
-        for (; i + (kLoads - 1) * kGroupThreads < shape.units; i += kLoads * kGroupThreads) {
+        for (; i + (kLoads - 1) * kGroupThreads < end; i += kLoads * kGroupThreads) {
             uint4 u[kLoads];
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) u[j] = ld_unit_ro(body + i + j * kGroupThreads);
@@ -88,19 +105,28 @@ token_logprobs_kernel(const LogprobArgs a, float k) {
 #pragma unroll
             for (int j = 0; j < kLoads - 1; ++j) {
                 u[j] = nothing<T>();
-                if (i + j * kGroupThreads < shape.units) u[j] = ld_unit_ro(body + i + j * kGroupThreads);
+                if (i + j * kGroupThreads < end) u[j] = ld_unit_ro(body + i + j * kGroupThreads);
             }
             run.template add_units<T>(u, k);
         }
         run.add_one(x_extra, k);
-        const Stats s = group_join<W, ENT>(run.stats(), k, shared + g * W, g);
+        Stats s = group_join<W, ENT>(run.stats(), k, shared + g * W, g);
+        if (CLUSTER) {  // to the first CTA's shared memory
+            cluster_wait();  // it has begun
+            if (t == 0) store_peer(&peers[rank], 0, s);
+            cluster_sync();
+            if (rank != 0) return;
+            const Stats none = {-CUDART_INF_F, 0.f, 0.f};
+            const int lane = t % 32;
+            s = warp_join<ENT>(lane < 1 << log_cluster ? peers[lane] : none, k);
+        }
         const float log2sum = log2f(s.sum);
         lse = fmaf(s.top, (float)a.scale, CUDART_LN2_F * log2sum);
         logp = logp_of(x_target, s, log2sum, k);
         if (ENT) entropy = CUDART_LN2_F * (log2sum - s.wsum / s.sum);
         if (!inside && t == 0) record_bad_target(a.status, row);
     }
-    if (t == 0) {
+    if (t == 0 && rank == 0) {
         a.logp[row] = logp;
         if (a.lse) a.lse[row] = lse;
         if (ENT) a.entropy[row] = entropy;
@@ -372,7 +398,6 @@ constexpr int kRingWork = 256;
 constexpr int kRingWarps = kRingWork / 32;
 constexpr int kRingThreads = kRingWork + 32;
 constexpr int kStageUnits = kStageBytes / 16;
-constexpr int kMaxCluster = 8;
 
 struct RingShared {
     alignas(128) unsigned char stage[kStages][kStageBytes];
@@ -382,12 +407,6 @@ struct RingShared {
     double sums[kRingWarps][4];
     int last, give_up;
 };
-
-// The slice of a row's units that CTA `rank` of 2^log_size takes (units < 2^29, so 32 bits hold it).
-__device__ __forceinline__ void slice_of(int units, int rank, int log_size, int &from, int &count) {
-    from = (int)(((unsigned)units * (unsigned)rank) >> log_size);
-    count = (int)(((unsigned)units * (unsigned)(rank + 1)) >> log_size) - from;
-}
 
 // Place in the ring: a stage, and the parity of the barrier phase that its current use completes.
 struct Cursor {
@@ -648,9 +667,30 @@ unsigned grid_of(int64_t work, int64_t cap) {
 template <typename T, int W, int ROWS>
 cudaError_t logprobs_groups(const LogprobArgs &a, float k, cudaStream_t stream) {
     const unsigned grid = (unsigned)((a.rows + ROWS - 1) / ROWS);
-    if (a.entropy) token_logprobs_kernel<T, W, ROWS, true><<<grid, 32 * W * ROWS, 0, stream>>>(a, k);
-    else token_logprobs_kernel<T, W, ROWS, false><<<grid, 32 * W * ROWS, 0, stream>>>(a, k);
+    if (a.entropy) token_logprobs_kernel<T, W, ROWS, true, false><<<grid, 32 * W * ROWS, 0, stream>>>(a, k, 0);
+    else token_logprobs_kernel<T, W, ROWS, false, false><<<grid, 32 * W * ROWS, 0, stream>>>(a, k, 0);
     return cudaGetLastError();
+}
+
+int log2_of(int n) {
+    int l = 0;
+    while (1 << l < n) ++l;
+    return l;
+}
+
+template <typename T>
+cudaError_t logprobs_cluster(const LogprobArgs &a, float k, int cluster, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.rows * cluster));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim = {(unsigned)cluster, 1, 1};
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return a.entropy ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kWarps, 1, true, true>, a, k, log2_of(cluster))
+                     : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kWarps, 1, false, true>, a, k, log2_of(cluster));
 }
 
 template <typename T>
@@ -658,8 +698,10 @@ cudaError_t logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
     const float k = (float)(a.scale * kLog2e);
     const int64_t units = a.vocab / kUnit<T>;
     if (units <= 32 * kRowUnits) return logprobs_groups<T, 1, 4>(a, k, stream);
-    if (units <= 128 * kRowUnits || a.rows >= 8 * (int64_t)sm_count) return logprobs_groups<T, W0, 1>(a, k, stream);
-    return logprobs_groups<T, 16, 1>(a, k, stream);
+    if (units <= 128 * kRowUnits || a.rows >= 8 * (int64_t)sm_count) return logprobs_groups<T, 4, 1>(a, k, stream);
+    int cluster = 1;  // more CTAs to a row while there are fewer rows than SMs and work for their threads
+    while (cluster < kMaxCluster && a.rows * cluster * 2 <= sm_count && units >= cluster * 2 * kThreads) cluster *= 2;
+    return cluster > 1 ? logprobs_cluster<T>(a, k, cluster, stream) : logprobs_groups<T, kWarps, 1>(a, k, stream);
 }
 
 template <typename T, typename O, int W>
@@ -681,14 +723,12 @@ cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count,
     cfg.blockDim = dim3(kRingThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
-    int log_cluster = 0;
-    while (1 << log_cluster < cluster) ++log_cluster;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim = {(unsigned)cluster, 1, 1};
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O>, a, k, log_cluster);
+    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O>, a, k, log2_of(cluster));
 }
 
 template <typename T, typename O>
