@@ -666,14 +666,15 @@ class AdamA:
     @staticmethod
     def _rows(t: torch.Tensor, name: str):
         """(pointer, dtype, pitch) of a [rows, vocab] tensor with unit stride in its last dimension."""
-        if t.dim() != 2:
+        shape, stride, dt = t.shape, t.stride(), _DTYPES.get(t.dtype)
+        if len(shape) != 2:
             raise ValueError(f"{name} must be [rows, vocab]")
-        if t.dtype not in _DTYPES:
+        if dt is None:
             raise TypeError(f"{name} must be float32 or bfloat16")
-        rows, vocab = t.shape
-        if vocab > 1 and t.stride(1) != 1:
+        rows, vocab = shape
+        if vocab > 1 and stride[1] != 1:
             raise ValueError(f"{name} must have unit stride in its last dimension")
-        return _dev_ptr(t, t.dtype, name), _DTYPES[t.dtype], t.stride(0) if rows > 1 else max(vocab, t.stride(0))
+        return _dev_ptr(t, t.dtype, name), dt, stride[0] if rows > 1 else max(vocab, stride[0])
 
     @staticmethod
     def _per_row(t: Optional[torch.Tensor], rows: int, name: str, dtype=torch.float32):

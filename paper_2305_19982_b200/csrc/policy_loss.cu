@@ -190,40 +190,43 @@ struct Sums {
     }
 };
 
-// The threads' sums -> the CTA's in the workspace -> stats, by the last CTA, in the CTAs' order.
-// All THREADS call it.
-template <int THREADS>
-__device__ __forceinline__ void finish_stats(const PolicyArgs &a, Sums s, double (*slots)[4], volatile int *last,
+// The leaders' sums -> the CTA's in the workspace -> stats, by the last CTA, in the CTAs' order.  All
+// THREADS call it; thread LEADER*i holds the sums of leader i.
+template <int THREADS, int LEADER>
+__device__ __forceinline__ void finish_stats(const PolicyArgs &a, const Sums &s, double (*slots)[4], volatile int *last,
                                              int t) {
+    static_assert(THREADS / 32 <= kWarps, "slots");
+    constexpr int kLeaders = THREADS / LEADER;
     Workspace *ws = static_cast<Workspace *>(a.workspace);
-    const auto cta_sum = [&]() {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            for (int o = 16; o > 0; o >>= 1) s.v[i] += __shfl_down_sync(0xffffffffu, s.v[i], o);
-            if (t % 32 == 0) slots[t / 32][i] = s.v[i];
-        }
-        asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory");
-    };
-    cta_sum();
+    const auto sync = []() { asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory"); };
+    if (t % LEADER == 0)
+        for (int i = 0; i < 4; ++i) slots[t / LEADER][i] = s.v[i];
+    if (kLeaders > 1) sync();
+    else __syncwarp();
+    double sum = 0.0;
     if (t < 4) {
-        double sum = 0.0;
-        for (int w = 0; w < THREADS / 32; ++w) sum += slots[w][t];
-        ws->part[4 * blockIdx.x + t] = sum;
-        __threadfence();
+        for (int w = 0; w < kLeaders; ++w) sum += slots[w][t];
+        if (gridDim.x == 1) a.stats[t] = (float)sum;
     }
-    asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory");
-    if (t == 0) *last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
-    asm volatile("bar.sync 0, %0;" ::"n"(THREADS) : "memory");
+    if (gridDim.x == 1) return;
+    if (t < 32) {
+        if (t < 4) {
+            ws->part[4 * blockIdx.x + t] = sum;
+            __threadfence();
+        }
+        __syncwarp();
+        if (t == 0) *last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
+    }
+    sync();
     if (!*last) return;
     __threadfence();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        s.v[i] = 0.0;
-        for (unsigned b = t; b < gridDim.x; b += THREADS) s.v[i] += __ldcg(&ws->part[4 * b + i]);
-    }
-    cta_sum();
+    sum = 0.0;  // threads of one remainder mod 4 add up the same of the four sums
+    for (unsigned i = t; i < 4 * gridDim.x; i += THREADS) sum += __ldcg(&ws->part[i]);
+    for (int o = 16; o >= 4; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
+    if (t % 32 < 4) slots[t / 32][t % 32] = sum;
+    sync();
     if (t < 4) {
-        double sum = 0.0;
+        sum = 0.0;
         for (int w = 0; w < THREADS / 32; ++w) sum += slots[w][t];
         a.stats[t] = (float)sum;
     }
@@ -381,7 +384,7 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
         }
         if (W > 1) group_sync<W>(g);  // the slots are used again
     }
-    finish_stats<kThreads>(a, acc, sums, &last, threadIdx.x);
+    finish_stats<kThreads, 32 * W>(a, acc, sums, &last, threadIdx.x);
 }
 
 // ---- longer rows: a ring in shared memory ------------------------------------------------------
@@ -588,7 +591,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
         }
         if (t == 0 && sh.give_up && atomicCAS(a.status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
             a.status[1] = kWaitPolicyRing;
-        finish_stats<kRingWork>(a, acc, sh.sums, &sh.last, t);
+        finish_stats<kRingWork, kRingWork>(a, acc, sh.sums, &sh.last, t);
     }
     if (cluster > 1) {
         __syncwarp();
@@ -652,7 +655,7 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
         }
         group_sync<kWarps>(0);  // the slots are used again
     }
-    finish_stats<kThreads>(a, acc, sums, &last, t);
+    finish_stats<kThreads, kThreads>(a, acc, sums, &last, t);
 }
 
 // ---- launches --------------------------------------------------------------------------------------
