@@ -5,7 +5,6 @@
 //     kl = exp(d) - d - 1,  loss += w*(pg + beta*kl)
 //     dlogits_j = w*s*c*([j = target] - p_j),  c = -(r*A while r*A <= the clamped product) + beta*(1 - exp(d))
 // A row is read once (loss: and its gradient written once); what bounds every form is HBM.
-#include <type_traits>
 
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"
@@ -240,48 +239,68 @@ __device__ __forceinline__ float narrow<float>(float y) { return y; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
 
-__device__ __forceinline__ void store_wide(float *p, const float (&y)[4]) {
-    st_stream(reinterpret_cast<float4 *>(p), make_float4(y[0], y[1], y[2], y[3]));
+// N values as 32-bit words of their type
+__device__ __forceinline__ void to_words(const float (&v)[4], unsigned (&w)[4], float) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
 }
-__device__ __forceinline__ void store_wide(float *p, const float (&y)[8]) {
-    st_stream(reinterpret_cast<float4 *>(p), make_float4(y[0], y[1], y[2], y[3]));
-    st_stream(reinterpret_cast<float4 *>(p) + 1, make_float4(y[4], y[5], y[6], y[7]));
+__device__ __forceinline__ void to_words(const float (&v)[8], unsigned (&w)[8], float) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
 }
-__device__ __forceinline__ void store_wide(__nv_bfloat16 *p, const float (&y)[4]) {
-    *reinterpret_cast<uint2 *>(p) = make_uint2(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]));
+__device__ __forceinline__ void to_words(const float (&v)[4], unsigned (&w)[2], __nv_bfloat16) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w[i] = pack2_bf16(v[2 * i], v[2 * i + 1]);
 }
-__device__ __forceinline__ void store_wide(__nv_bfloat16 *p, const float (&y)[8]) {
-    *reinterpret_cast<uint4 *>(p) = make_uint4(pack2_bf16(y[0], y[1]), pack2_bf16(y[2], y[3]),
-                                               pack2_bf16(y[4], y[5]), pack2_bf16(y[6], y[7]));
+__device__ __forceinline__ void to_words(const float (&v)[8], unsigned (&w)[4], __nv_bfloat16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack2_bf16(v[2 * i], v[2 * i + 1]);
+}
+__device__ __forceinline__ void store_words(void *p, const unsigned (&w)[2]) { *static_cast<uint2 *>(p) = make_uint2(w[0], w[1]); }
+__device__ __forceinline__ void store_words(void *p, const unsigned (&w)[4]) {
+    *static_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_words(void *p, const unsigned (&w)[8]) {
+    static_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    static_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+
+// Zeros to p[0 .. n) by `threads` threads.
+template <typename O>
+__device__ __forceinline__ void fill_zeros(O *p, int64_t n, int t, int threads) {
+    constexpr int kPer = 16 / sizeof(O);
+    const int mis = (int)(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(O));
+    const int64_t head = mis ? (kPer - mis < n ? kPer - mis : n) : 0, body = (n - head) / kPer;
+    for (int64_t i = t; i < body; i += threads) reinterpret_cast<uint4 *>(p + head)[i] = make_uint4(0, 0, 0, 0);
+    const int64_t tail0 = head + body * kPer;
+    if (t < head) p[t] = narrow<O>(0.f);
+    if (t < n - tail0) p[tail0 + t] = narrow<O>(0.f);
 }
 
 // How a row's gradient is written.  The units are written without the target's extra term; the
 // thread that wrote the target's element writes it again, with the term.
+//
+// A unit's gradient is one aligned store where logits and gradient have the same alignment.  Where they
+// have not, a thread takes the window of N logits from `shift` on, which ends in the next unit: the
+// raw words of both are shifted into place before anything is computed, and only the first `shift`
+// elements of a slice and the last N - shift are stored one by one.  (Then logits and gradient are
+// different buffers: in place they share their pitch.)
 template <typename T, typename O>
 struct RowWriter {
     static constexpr int N = kUnit<T>;
-    O *y;
-    bool wide;
+    static constexpr int kWords = N * sizeof(O) / 4;             // a unit's gradient
+    static constexpr int kStoreWords = kWords < 4 ? kWords : 4;  // one store
+    int shift;  // elements between a unit's first one and the next aligned address; 0: aligned stores
     float top, unit, per_e, k;
 
-    __device__ __forceinline__ RowWriter(O *row, const RowShape &shape, float top_, const RowOut &o, float k_)
-        : y(row), top(top_), unit(o.unit), per_e(o.per_e), k(k_) {
-        constexpr int align = N * sizeof(O) < 16 ? N * sizeof(O) : 16;
-        wide = reinterpret_cast<uintptr_t>(row + shape.head) % align == 0;
+    __device__ __forceinline__ RowWriter(const O *row, const RowShape &shape, float top_, float unit_, float per_e_, float k_)
+        : top(top_), unit(unit_), per_e(per_e_), k(k_) {
+        constexpr int kPer = kStoreWords * 4 / sizeof(O);
+        const int mis = (int)(reinterpret_cast<uintptr_t>(row + shape.head) % (kStoreWords * 4) / sizeof(O));
+        shift = mis ? kPer - mis : 0;
     }
-    template <bool WIDE>
-    __device__ __forceinline__ static void store(O *p, const float (&v)[N]) {
-        if (WIDE) {
-            store_wide(p, v);
-        } else {
-#pragma unroll
-            for (int q = 0; q < N; ++q) p[q] = narrow<O>(v[q]);
-        }
-    }
-    // a unit of logits whose gradient goes to p
-    template <bool WIDE>
-    __device__ __forceinline__ void put(const uint4 &u, O *p) const {
-        float v[N];
+    // the gradient of N logits
+    __device__ __forceinline__ void values(const uint4 &u, float (&v)[N]) const {
         const Pair minus = pair(-top, -top), k2 = pair(k, k), per = pair(per_e, per_e);
 #pragma unroll
         for (int q = 0; q < N / 2; ++q) {
@@ -289,30 +308,52 @@ struct RowWriter {
             split(mul2(add2(unit_pair<T>(u, q), minus), k2), d0, d1);
             split(mul2(pair(exp2_fast(d0), exp2_fast(d1)), per), v[2 * q], v[2 * q + 1]);
         }
-        store<WIDE>(p, v);
     }
-    template <bool WIDE>
-    __device__ __forceinline__ static void put_zeros(O *p) {
+    __device__ __forceinline__ void put(const uint4 &u, O *p) const {
         float v[N];
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = 0.f;
-        store<WIDE>(p, v);
+        values(u, v);
+        unsigned w[kWords];
+        to_words(v, w, O());
+        store_words(p, w);
     }
-    __device__ __forceinline__ void put_one(float x, int j) const { y[j] = narrow<O>(per_e * exp2_fast(k * (x - top))); }
-    __device__ __forceinline__ void put_target(float x, int64_t j) const {
-        y[j] = narrow<O>(per_e * exp2_fast(k * (x - top)) + unit);
+    // shift > 0: u goes to p; `first`: the slice begins with it, `last`: it ends with it, else `next` follows
+    __device__ __forceinline__ void put_shifted(const uint4 &u, const uint4 &next, O *p, bool first, bool last) const {
+        unsigned z[8] = {u.x, u.y, u.z, u.w, next.x, next.y, next.z, next.w};
+        const int words = shift * (int)sizeof(T) / 4;
+        if (words & 2) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) z[i] = z[i + 2];
+        }
+        if (words & 1) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) z[i] = z[i + 1];
+        }
+        if (sizeof(T) == 2 && (shift & 1)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = __funnelshift_r(z[i], z[i + 1], 16);
+        }
+        if (!last) put(make_uint4(z[0], z[1], z[2], z[3]), p + shift);
+        if (first || last) {
+            float v[N];
+            values(u, v);
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                if (q < shift ? first : last) p[q] = narrow<O>(v[q]);
+        }
+    }
+    __device__ __forceinline__ O value(float x, bool is_target) const {
+        const float p = per_e * exp2_fast(k * (x - top));
+        return narrow<O>(is_target ? p + unit : p);
+    }
+    // Thread of a group of `threads` that wrote element j, of a slice of `count` units from unit `from`
+    // on that go round the threads; -1: it is not among the slice's units.
+    __device__ __forceinline__ int writer_of(const RowShape &shape, int64_t j, int from, int count, int threads) const {
+        const int64_t at = j - shape.head - (int64_t)from * N;
+        if (at < 0 || at >= (int64_t)count * N) return -1;
+        const int u = (int)(at / N);
+        return (at % N < shift && u > 0 ? u - 1 : u) % threads;
     }
 };
-
-// Thread of a group of `threads` that writes element j of a row: units go round the threads from the
-// first unit of the slice on (stages hold a multiple of `threads` units), extra i belongs to thread i.
-template <typename T>
-__device__ __forceinline__ int owner_of(const RowShape &shape, int64_t j, int from, int threads) {
-    const int at = (int)j - shape.head;
-    if (at < 0) return (int)j;
-    if (at >= shape.units * kUnit<T>) return shape.head + at - shape.units * kUnit<T>;
-    return (at / kUnit<T> - from) % threads;
-}
 
 // ---- rows that fit a few warps' registers ------------------------------------------------------
 
@@ -365,22 +406,29 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
         }
         if (t == 0 && a.logp) a.logp[row] = o.logp;
         if (a.dlogits) {
-            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
-            O *p = out.y + shape.head + t * kUnit<T>;
-            const auto units = [&](auto wide) {
+            O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+            if (live) {
+                const RowWriter<T, O> out(y, shape, top, o.unit, o.per_e, k);
+                O *p = y + shape.head + t * kUnit<T>;
+                if (out.shift == 0) {
 #pragma unroll
-                for (int i = 0; i < kRowUnits; ++i) {
-                    if (t + i * kGroupThreads < shape.units) {
-                        if (live) out.template put<decltype(wide)::value>(u[i], p + i * kGroupThreads * kUnit<T>);
-                        else out.template put_zeros<decltype(wide)::value>(p + i * kGroupThreads * kUnit<T>);
+                    for (int i = 0; i < kRowUnits; ++i)
+                        if (t + i * kGroupThreads < shape.units) out.put(u[i], p + i * kGroupThreads * kUnit<T>);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kRowUnits; ++i) {
+                        const int at = t + i * kGroupThreads;
+                        if (at < shape.units)
+                            out.put_shifted(u[i], ld_unit(body + (at + 1 < shape.units ? at + 1 : at)),
+                                            p + i * kGroupThreads * kUnit<T>, at == 0, at + 1 == shape.units);
                     }
                 }
-            };
-            if (out.wide) units(std::true_type());
-            else units(std::false_type());
-            if (has_extra) out.put_one(x_extra, extra);
-            if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, 0, kGroupThreads))
-                out.put_target(x_target, in.target);
+                if (has_extra) y[extra] = out.value(x_extra, extra == in.target);
+                if (in.target < a.vocab && t == out.writer_of(shape, in.target, 0, shape.units, kGroupThreads))
+                    y[in.target] = out.value(x_target, true);
+            } else {
+                fill_zeros(y, a.vocab, t, kGroupThreads);
+            }
         }
         if (W > 1) group_sync<W>(g);  // the slots are used again
     }
@@ -388,28 +436,42 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
 }
 
 // ---- longer rows: a ring in shared memory ------------------------------------------------------
-// A row, or its slice where a cluster of CTAs shares one, is brought to shared memory by bulk
-// copies, in stages of kStageBytes; the statistics are taken from the stages as they arrive, then the
-// gradient is computed from the same stages, each of which is refilled as soon as it has been used:
-// the next row streams in while this one's gradient streams out, and every logit crosses the HBM bus
-// once.  One producer warp, kRingWork threads that compute.
+// A row, or its slice where a cluster of CTAs shares one, is brought to shared memory by bulk copies,
+// in stages; the statistics are taken from the stages as they arrive, then the gradient is computed
+// from the same stages, each of which is refilled as soon as it has been used: every logit crosses the
+// HBM bus once.  The warps that compute take row i+1's statistics BEFORE they write row i's gradient:
+// between a row's statistics and its gradient lie the joins over warps and CTAs and the loss itself,
+// which one warp of its own does meanwhile, and nobody waits for them.  The ring therefore holds two
+// rows (slices).  One more warp issues the copies.
 
-constexpr int kStageBytes = 12288;
-constexpr int kStages = 9;
-constexpr int kRingsPerSm = 2;
-constexpr int kRingWork = 256;
+constexpr int kStageBytes = 16384;
+constexpr int kStages = 14;
+constexpr int kRingWork = 512;
 constexpr int kRingWarps = kRingWork / 32;
-constexpr int kRingThreads = kRingWork + 32;
+constexpr int kProducerWarp = kRingWarps, kScalarWarp = kRingWarps + 1;
+constexpr int kRingThreads = kRingWork + 64;
 constexpr int kStageUnits = kStageBytes / 16;
+constexpr int kEach = kStageUnits / kRingWork;                 // units of a stage that a thread takes
+constexpr int kSliceUnits = kStages / 2 * kStageUnits;         // largest slice of a row
 
+// What the gradient of a row needs.
+struct Verdict {
+    float top, unit, per_e, x_target;
+    int64_t target;
+    int writer;  // the thread that writes the target's element, or -1
+};
+
+// Two of each, for even and odd live rows: nobody is more than one row ahead.
 struct RingShared {
     alignas(128) unsigned char stage[kStages][kStageBytes];
-    alignas(16) float4 peer[2][kMaxCluster];  // {top, sum, x_target} of the cluster's CTAs, for even and odd rows
-    unsigned long long full[kStages], empty[kStages], joined[2];
-    Stats slots[2][kRingWarps];  // for even and odd rows: a warp may be a row ahead of another
-    double sums[kRingWarps][4];
+    alignas(16) float4 peer[2][kMaxCluster];  // {top, sum, x_target} of the cluster's CTAs
+    Verdict verdict[2];
+    float2 slots[2][kRingWarps];              // {top, sum} of the warps
+    unsigned long long full[kStages], empty[kStages], joined[2], peered[2], ready[2];
+    double sums[1][4];
     int last, give_up;
 };
+static_assert(sizeof(RingShared) + 128 <= 232448, "shared memory of a CTA");
 
 // Place in the ring: a stage, and the parity of the barrier phase that its current use completes.
 struct Cursor {
@@ -423,8 +485,14 @@ struct Cursor {
     }
 };
 
+__device__ __forceinline__ Stats join2(const Stats &a, const Stats &b, float k) {
+    const float top = fmaxf(a.top, b.top);
+    const Stats p = raised(a, top, k), q = raised(b, top, k);
+    return {top, p.sum + q.sum, 0.f};
+}
+
 template <typename T, typename O>
-__global__ void __launch_bounds__(kRingThreads, kRingsPerSm)
+__global__ void __launch_bounds__(kRingThreads, 1)
 policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
     extern __shared__ unsigned char raw[];
     RingShared &sh = *reinterpret_cast<RingShared *>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
@@ -437,15 +505,18 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             barrier_init(shared_addr(&sh.full[i]), 1);
             barrier_init(shared_addr(&sh.empty[i]), kRingWarps);
         }
-        for (int i = 0; i < 2; ++i) barrier_init(shared_addr(&sh.joined[i]), 1);
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(shared_addr(&sh.joined[i]), kRingWarps);
+            barrier_init(shared_addr(&sh.peered[i]), 1);
+            barrier_init(shared_addr(&sh.ready[i]), 1);
+        }
         sh.give_up = 0;
         barrier_init_fence();
     }
     __syncthreads();
     if (cluster > 1) cluster_sync();  // the peers' barriers are ready before the first message
 
-    if (warp == kRingWarps) {
-        // ---- producer
+    if (warp == kProducerWarp) {
         if (lane == 0) {
             Cursor c;
             uint32_t issued = 0;  // stages, up to kStages
@@ -475,123 +546,177 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 }
             }
         }
-    } else {
+    } else if (warp == kScalarWarp) {
         Sums acc;
-        Cursor c;
-        uint32_t joins = 0;  // rows joined
+        uint32_t n = 0;  // live rows
         RowIn next = {-1, 0.f, 0.f, 0.f, 0.f};
         if (first < a.rows) next = row_in(a, first);
         for (int64_t row = first; row < a.rows; row += step) {
             const RowIn in = next;
             if (row + step < a.rows) next = row_in(a, row + step);
-            const bool live = in.live();
+            if (!in.live()) {
+                if (lane == 0 && rank == 0 && a.logp) a.logp[row] = 0.f;
+                continue;
+            }
             const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
             const RowShape shape = row_shape(x, (int)a.vocab);
             int from, count;
             slice_of(shape.units, rank, log_cluster, from, count);
-            const bool has_extra = rank == 0 && t < shape.head + shape.tail;
-            const int extra = has_extra ? extra_index<T>(shape, t) : 0;
-            const Cursor c0 = c;
-            float x_extra = 0.f, xt = 0.f, top = 0.f;
-            RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (live) {
-                const bool inside = in.target < a.vocab;
-                const float x_target = t == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
-                if (has_extra) x_extra = widen(x[extra]);
-                Running<false> run;
-                for (int at = 0; at < count; at += kStageUnits, c.advance()) {
-                    barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &sh.give_up);
-                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]);
-                    if (count - at >= kStageUnits) {
-                        uint4 u[kStageUnits / kRingWork];
-#pragma unroll
-                        for (int i = 0; i < kStageUnits / kRingWork; ++i) u[i] = units[t + i * kRingWork];
-                        run.template add_units<T>(u, k);
-                    } else {
-                        for (int i = t; i < count - at; i += kRingWork) {
-                            const uint4 u[1] = {units[i]};
-                            run.template add_units<T>(u, k);
-                        }
-                    }
-                }
-                if (has_extra) run.add_one(x_extra, k);
-                // the CTA's statistics, then the cluster's; thread 0's x_target travels with them
-                Stats s = warp_join<false>(run.stats(), k);
-                const int b = joins & 1;
-                if (lane == 0) sh.slots[b][warp] = {s.top, s.sum, x_target};
-                asm volatile("bar.sync 1, %0;" ::"n"(kRingWork) : "memory");
-                const Stats none = {-CUDART_INF_F, 0.f, 0.f};
-                const Stats mine = lane < kRingWarps ? sh.slots[b][lane] : none;
-                s = warp_join<false>(mine, k);
-                xt = __shfl_sync(0xffffffffu, mine.wsum, 0);
-                if (cluster > 1) {
-                    const uint32_t bar = shared_addr(&sh.joined[b]);
-                    if (t == 0) barrier_expect(bar, 16u * cluster);
-                    if (t < cluster) send16(shared_addr(&sh.peer[b][rank]), bar, t, s.top, s.sum, xt, 0.f);
-                    barrier_wait(bar, (joins >> 1) & 1, &sh.give_up);
-                    Stats p = none;
-                    if (lane < cluster) {
-                        const float4 q = sh.peer[b][lane];
-                        p = {q.x, q.y, q.z};
-                    }
-                    s = warp_join<false>(p, k);
-                }
-                ++joins;
-                top = s.top;
-                o = row_out(a, in, s, xt, k);
-                if (t == 0 && rank == 0) {
+            const int b = n & 1;
+            const uint32_t parity = n >> 1 & 1;
+            const bool inside = in.target < a.vocab, has_extra = rank == 0 && lane < shape.head + shape.tail;
+            const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
+            // the gradient may replace the logits: what is read here travels with this CTA's message,
+            // before which nobody writes
+            float x_target = rank == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
+            const float x_extra = has_extra ? widen(x[extra]) : -CUDART_INF_F;
+            Running<false> run;
+            run.add_one(x_extra, k);
+            barrier_wait(shared_addr(&sh.joined[b]), parity, &sh.give_up);
+            const Stats none = {-CUDART_INF_F, 0.f, 0.f};
+            Stats s = none;
+            if (lane < kRingWarps) s = {sh.slots[b][lane].x, sh.slots[b][lane].y, 0.f};
+            s = warp_join<false>(join2(s, run.stats(), k), k);
+            if (cluster > 1) {
+                const uint32_t bar = shared_addr(&sh.peered[b]);
+                if (lane == 0) barrier_expect(bar, 16u * cluster);
+                if (lane < cluster) send16(shared_addr(&sh.peer[b][rank]), bar, lane, s.top, s.sum, x_target, 0.f);
+                barrier_wait(bar, parity, &sh.give_up);
+                float4 q = make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+                if (lane < cluster) q = sh.peer[b][lane];
+                x_target = __shfl_sync(0xffffffffu, q.z, 0);
+                s = warp_join<false>({q.x, q.y, 0.f}, k);
+            }
+            const RowOut o = row_out(a, in, s, x_target, k);
+            O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+            const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
+            if (lane == 0) {
+                const int writer = inside ? out.writer_of(shape, in.target, from, count, kRingWork) : -1;
+                sh.verdict[b] = {s.top, o.unit, o.per_e, x_target, in.target, writer};
+                barrier_arrive(shared_addr(&sh.ready[b]));
+                if (rank == 0) {
                     acc.add(a, in, o);
+                    if (a.logp) a.logp[row] = o.logp;
                     if (!inside) record_bad_target(a.status, row);
                 }
             }
-            if (t == 0 && rank == 0 && a.logp) a.logp[row] = o.logp;
-            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
-            O *p = out.y + shape.head + (int64_t)(from + t) * kUnit<T>;
-            if (live) {
-                c = c0;
-                const auto release = [&]() {
-                    __syncwarp();
-                    if (lane == 0) barrier_arrive(shared_addr(&sh.empty[c.slot]));
-                };
-                const auto stages = [&](auto wide) {
-                    for (int at = 0; at < count; at += kStageUnits, c.advance(), p += kStageUnits * kUnit<T>) {
-                        const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]) + t;
-                        if (count - at >= kStageUnits) {
-                            uint4 u[kStageUnits / kRingWork];
-#pragma unroll
-                            for (int i = 0; i < kStageUnits / kRingWork; ++i) u[i] = units[i * kRingWork];
-#pragma unroll
-                            for (int i = 0; i < kStageUnits / kRingWork; ++i)
-                                out.template put<decltype(wide)::value>(u[i], p + i * kRingWork * kUnit<T>);
-                        } else {
-                            for (int i = 0; i < count - at - t; i += kRingWork)
-                                out.template put<decltype(wide)::value>(units[i], p + i * kUnit<T>);
-                        }
-                        release();
-                    }
-                };
-                if (!a.dlogits)
-                    for (int at = 0; at < count; at += kStageUnits, c.advance()) release();
-                else if (out.wide) stages(std::true_type());
-                else stages(std::false_type());
-            } else if (a.dlogits) {
-                for (int i = 0; i < count - t; i += kRingWork) {
-                    if (out.wide) out.template put_zeros<true>(p + (int64_t)i * kUnit<T>);
-                    else out.template put_zeros<false>(p + (int64_t)i * kUnit<T>);
-                }
-            }
-            if (a.dlogits) {
-                if (has_extra) out.put_one(x_extra, extra);
-                if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, from, kRingWork)) {
-                    const int at = ((int)in.target - shape.head) / kUnit<T> - from;
-                    const bool extra_one = in.target < shape.head || in.target >= shape.head + shape.units * kUnit<T>;
-                    if (extra_one ? rank == 0 : at >= 0 && at < count) out.put_target(xt, in.target);
-                }
-            }
+            if (has_extra && a.dlogits) y[extra] = out.value(x_extra, extra == in.target);
+            ++n;
         }
-        if (t == 0 && sh.give_up && atomicCAS(a.status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
+        if (lane == 0 && *(volatile int *)&sh.give_up &&
+            atomicCAS(a.status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
             a.status[1] = kWaitPolicyRing;
-        finish_stats<kRingWork, kRingWork>(a, acc, sh.sums, &sh.last, t);
+        __syncwarp();
+        finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane);
+    } else {
+        Cursor c;
+        uint32_t n = 0;              // live rows whose statistics have been taken
+        int64_t due = -1;            // the row whose gradient is to be written next
+        Cursor due_at;
+        const auto write_due = [&]() {
+            const T *x = static_cast<const T *>(a.logits) + due * a.ld_logits;
+            const RowShape shape = row_shape(x, (int)a.vocab);
+            int from, count;
+            slice_of(shape.units, rank, log_cluster, from, count);
+            const int b = (n - 1) & 1;
+            const bool ok = barrier_wait(shared_addr(&sh.ready[b]), (n - 1) >> 1 & 1, &sh.give_up);
+            const Verdict q = sh.verdict[b];
+            O *y = static_cast<O *>(a.dlogits) + due * a.ld_dlogits;
+            const RowWriter<T, O> out(y, shape, q.top, q.unit, q.per_e, k);
+            Cursor at_stage = due_at;
+            const auto release = [&]() {
+                __syncwarp();
+                if (lane == 0) barrier_arrive(shared_addr(&sh.empty[at_stage.slot]));
+            };
+            O *p = y + shape.head + (int64_t)(from + t) * kUnit<T>;
+            if (!a.dlogits || !ok) {
+                for (int at = 0; at < count; at += kStageUnits, at_stage.advance()) release();
+                return;
+            }
+            if (out.shift == 0) {
+                for (int at = 0; at < count; at += kStageUnits, at_stage.advance(), p += kStageUnits * kUnit<T>) {
+                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]) + t;
+                    if (count - at >= kStageUnits) {
+                        uint4 u[kEach];
+#pragma unroll
+                        for (int i = 0; i < kEach; ++i) u[i] = units[i * kRingWork];
+#pragma unroll
+                        for (int i = 0; i < kEach; ++i) out.put(u[i], p + i * kRingWork * kUnit<T>);
+                    } else {
+#pragma unroll 1
+                        for (int i = 0; i < count - at - t; i += kRingWork) out.put(units[i], p + i * kUnit<T>);
+                    }
+                    release();
+                }
+            } else {
+                for (int at = 0; at < count; at += kStageUnits, p += kStageUnits * kUnit<T>) {
+                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]);
+                    const int slot = at_stage.slot + 1 == kStages ? 0 : at_stage.slot + 1;
+                    const uint4 *after = reinterpret_cast<const uint4 *>(sh.stage[slot]);  // still the row's: nobody releases it before this stage
+#pragma unroll 1
+                    for (int i = t; i < kStageUnits && at + i < count; i += kRingWork) {
+                        const bool last = at + i + 1 == count;
+                        const uint4 *next = i + 1 < kStageUnits ? units + i + 1 : after;
+                        out.put_shifted(units[i], last ? units[i] : *next, p + (i - t) * kUnit<T>, at + i == 0, last);
+                    }
+                    release();
+                    at_stage.advance();
+                }
+            }
+            if (t == q.writer) y[q.target] = out.value(q.x_target, true);
+        };
+        float next_weight = 0.f;
+        int64_t next_target = -1;
+        if (first < a.rows) {
+            next_weight = a.weights[first];
+            next_target = a.targets[first];
+        }
+        for (int64_t row = first; row < a.rows; row += step) {
+            const bool live = next_weight != 0.f && next_target >= 0;
+            if (row + step < a.rows) {
+                next_weight = a.weights[row + step];
+                next_target = a.targets[row + step];
+            }
+            const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+            const RowShape shape = row_shape(x, (int)a.vocab);
+            int from, count;
+            slice_of(shape.units, rank, log_cluster, from, count);
+            if (!live) {
+                if (a.dlogits) {  // the first CTA's part has the row's head, the last one's its tail
+                    const int64_t begin = rank == 0 ? 0 : shape.head + (int64_t)from * kUnit<T>;
+                    const int64_t end = rank == cluster - 1 ? a.vocab : shape.head + (int64_t)(from + count) * kUnit<T>;
+                    fill_zeros(static_cast<O *>(a.dlogits) + row * a.ld_dlogits + begin, end - begin, t, kRingWork);
+                }
+                continue;
+            }
+            const Cursor begin = c;
+            Running<false> run;
+            for (int at = 0; at < count; at += kStageUnits, c.advance()) {
+                barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &sh.give_up);
+                const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]) + t;
+                const int here = count - at;
+                uint4 u[kEach];
+                if (here >= kStageUnits) {
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) u[i] = units[i * kRingWork];
+                    run.template add_units<T>(u, k);
+                } else if (t < here) {
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) u[i] = t + i * kRingWork < here ? units[i * kRingWork] : nothing<T>();
+                    run.template add_units<T>(u, k);
+                }
+            }
+            const Stats s = warp_join<false>(run.stats(), k);
+            if (lane == 0) {
+                sh.slots[n & 1][warp] = make_float2(s.top, s.sum);
+                barrier_arrive(shared_addr(&sh.joined[n & 1]));
+            }
+            if (due >= 0) write_due();
+            due = row;
+            due_at = begin;
+            ++n;
+        }
+        if (due >= 0) write_due();
     }
     if (cluster > 1) {
         __syncwarp();
@@ -639,19 +764,23 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
         }
         if (t == 0 && a.logp) a.logp[row] = o.logp;
         if (a.dlogits) {
-            const RowWriter<T, O> out(static_cast<O *>(a.dlogits) + row * a.ld_dlogits, shape, top, o, k);
-            O *p = out.y + shape.head;
-            const auto units = [&](auto wide) {
-                for (int i = t; i < shape.units; i += kThreads) {
-                    if (live) out.template put<decltype(wide)::value>(ld_unit(body + i), p + (int64_t)i * kUnit<T>);
-                    else out.template put_zeros<decltype(wide)::value>(p + (int64_t)i * kUnit<T>);
+            O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+            if (live) {
+                const RowWriter<T, O> out(y, shape, top, o.unit, o.per_e, k);
+                O *p = y + shape.head;
+                if (out.shift == 0) {
+                    for (int i = t; i < shape.units; i += kThreads) out.put(ld_unit(body + i), p + (int64_t)i * kUnit<T>);
+                } else {
+                    for (int i = t; i < shape.units; i += kThreads)
+                        out.put_shifted(ld_unit(body + i), ld_unit(body + (i + 1 < shape.units ? i + 1 : i)),
+                                        p + (int64_t)i * kUnit<T>, i == 0, i + 1 == shape.units);
                 }
-            };
-            if (out.wide) units(std::true_type());
-            else units(std::false_type());
-            if (has_extra) out.put_one(x_extra, extra);
-            if (live && in.target < a.vocab && t == owner_of<T>(shape, in.target, 0, kThreads))
-                out.put_target(x_target, in.target);
+                if (has_extra) y[extra] = out.value(x_extra, extra == in.target);
+                if (in.target < a.vocab && t == out.writer_of(shape, in.target, 0, shape.units, kThreads))
+                    y[in.target] = out.value(x_target, true);
+            } else {
+                fill_zeros(y, a.vocab, t, kThreads);
+            }
         }
         group_sync<kWarps>(0);  // the slots are used again
     }
@@ -721,7 +850,32 @@ cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count,
     cudaError_t e = allow_shared(policy_loss_ring_kernel<T, O>, (int)bytes, ready);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    const int64_t most = sm_count * kRingsPerSm / cluster;
+    int64_t most = sm_count / cluster;
+    if (cluster > 1) {
+        // a GPC's SMs need not be a multiple of the cluster's; a cluster that waits for its turn would
+        // leave its share of the rows to the end
+        static std::atomic<int> resident[64][4];
+        const int l = log2_of(cluster);
+        int device = 0;
+        e = cudaGetDevice(&device);
+        if (e != cudaSuccess) return e;
+        int m = device < 64 ? resident[device][l].load() : 0;
+        if (m == 0) {
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim = {(unsigned)cluster, 1, 1};
+            cfg.gridDim = dim3((unsigned)(most * cluster));
+            cfg.blockDim = dim3(kRingThreads);
+            cfg.dynamicSmemBytes = bytes;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O>, &cfg);
+            if (e != cudaSuccess) return e;
+            if (m < 1) m = 1;
+            if (device < 64) resident[device][l].store(m);
+        }
+        if (m < most) most = m;
+    }
     cfg.gridDim = dim3((unsigned)((a.rows < 1 ? 1 : a.rows < most ? a.rows : most) * cluster));
     cfg.blockDim = dim3(kRingThreads);
     cfg.dynamicSmemBytes = bytes;
@@ -740,8 +894,8 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
     const int64_t units = a.vocab / kUnit<T>;
     if (units <= 32 * kRowUnits) return policy_rows<T, O, 1>(a, k, sm_count, stream);
     if (units <= 128 * kRowUnits) return policy_rows<T, O, 4>(a, k, sm_count, stream);
-    // as few CTAs to a row as hold it, more while there are fewer rows than SMs
-    constexpr int64_t kRing = (int64_t)kStages * kStageUnits;
+    // as few CTAs to a row as hold two of its slices, more while there are fewer rows than SMs
+    constexpr int64_t kRing = kSliceUnits;
     int cluster = 1;
     while (cluster < kMaxCluster && ((units + cluster - 1) / cluster > kRing || a.rows * cluster * 2 <= sm_count)) cluster *= 2;
     if ((units + cluster - 1) / cluster <= kRing)
