@@ -301,11 +301,11 @@ struct RowWriter {
     }
     // the gradient of N logits
     __device__ __forceinline__ void values(const uint4 &u, float (&v)[N]) const {
-        const Pair minus = pair(-top, -top), k2 = pair(k, k), per = pair(per_e, per_e);
+        const Pair k2 = pair(k, k), per = pair(per_e, per_e);
 #pragma unroll
         for (int q = 0; q < N / 2; ++q) {
             float d0, d1;
-            split(mul2(add2(unit_pair<T>(u, q), minus), k2), d0, d1);
+            split(mul2(unit_less<T>(u, q, top), k2), d0, d1);
             split(mul2(pair(exp2_fast(d0), exp2_fast(d1)), per), v[2 * q], v[2 * q + 1]);
         }
     }
@@ -613,11 +613,9 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
         uint32_t n = 0;              // live rows whose statistics have been taken
         int64_t due = -1;            // the row whose gradient is to be written next
         Cursor due_at;
+        RowShape shape = {0, 0, 0};  // the due row's, and its slice
+        int from = 0, count = 0;
         const auto write_due = [&]() {
-            const T *x = static_cast<const T *>(a.logits) + due * a.ld_logits;
-            const RowShape shape = row_shape(x, (int)a.vocab);
-            int from, count;
-            slice_of(shape.units, rank, log_cluster, from, count);
             const int b = (n - 1) & 1;
             const bool ok = barrier_wait(shared_addr(&sh.ready[b]), (n - 1) >> 1 & 1, &sh.give_up);
             const Verdict q = sh.verdict[b];
@@ -634,7 +632,21 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 return;
             }
             if (out.shift == 0) {
-                for (int at = 0; at < count; at += kStageUnits, at_stage.advance(), p += kStageUnits * kUnit<T>) {
+                int at = 0;
+                for (; count - at >= 2 * kStageUnits; at += 2 * kStageUnits, p += 2 * kStageUnits * kUnit<T>) {
+                    uint4 u[2 * kEach];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]) + t;
+#pragma unroll
+                        for (int i = 0; i < kEach; ++i) u[j * kEach + i] = units[i * kRingWork];
+                        release();
+                        at_stage.advance();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2 * kEach; ++i) out.put(u[i], p + i * kRingWork * kUnit<T>);
+                }
+                for (; at < count; at += kStageUnits, at_stage.advance(), p += kStageUnits * kUnit<T>) {
                     const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]) + t;
                     if (count - at >= kStageUnits) {
                         uint4 u[kEach];
@@ -652,7 +664,8 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 for (int at = 0; at < count; at += kStageUnits, p += kStageUnits * kUnit<T>) {
                     const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]);
                     const int slot = at_stage.slot + 1 == kStages ? 0 : at_stage.slot + 1;
-                    const uint4 *after = reinterpret_cast<const uint4 *>(sh.stage[slot]);  // still the row's: nobody releases it before this stage
+                    // the row's next stage: nobody releases it before this one
+                    const uint4 *after = reinterpret_cast<const uint4 *>(sh.stage[slot]);
 #pragma unroll 1
                     for (int i = t; i < kStageUnits && at + i < count; i += kRingWork) {
                         const bool last = at + i + 1 == count;
@@ -678,29 +691,38 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 next_target = a.targets[row + step];
             }
             const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
-            const RowShape shape = row_shape(x, (int)a.vocab);
-            int from, count;
-            slice_of(shape.units, rank, log_cluster, from, count);
+            const RowShape new_shape = row_shape(x, (int)a.vocab);
+            int new_from, new_count;
+            slice_of(new_shape.units, rank, log_cluster, new_from, new_count);
             if (!live) {
                 if (a.dlogits) {  // the first CTA's part has the row's head, the last one's its tail
-                    const int64_t begin = rank == 0 ? 0 : shape.head + (int64_t)from * kUnit<T>;
-                    const int64_t end = rank == cluster - 1 ? a.vocab : shape.head + (int64_t)(from + count) * kUnit<T>;
+                    const int64_t begin = rank == 0 ? 0 : new_shape.head + (int64_t)new_from * kUnit<T>;
+                    const int64_t end =
+                        rank == cluster - 1 ? a.vocab : new_shape.head + (int64_t)(new_from + new_count) * kUnit<T>;
                     fill_zeros(static_cast<O *>(a.dlogits) + row * a.ld_dlogits + begin, end - begin, t, kRingWork);
                 }
                 continue;
             }
             const Cursor begin = c;
             Running<false> run;
-            for (int at = 0; at < count; at += kStageUnits, c.advance()) {
-                barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &sh.give_up);
-                const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]) + t;
-                const int here = count - at;
-                uint4 u[kEach];
-                if (here >= kStageUnits) {
+            int at = 0;
+            for (; new_count - at >= 2 * kStageUnits; at += 2 * kStageUnits) {
+                uint4 u[2 * kEach];
 #pragma unroll
-                    for (int i = 0; i < kEach; ++i) u[i] = units[i * kRingWork];
-                    run.template add_units<T>(u, k);
-                } else if (t < here) {
+                for (int j = 0; j < 2; ++j, c.advance()) {
+                    barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &sh.give_up);
+                    const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]) + t;
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) u[j * kEach + i] = units[i * kRingWork];
+                }
+                run.template add_units<T>(u, k);
+            }
+            for (; at < new_count; at += kStageUnits, c.advance()) {
+                barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &sh.give_up);
+                const int here = new_count - at;
+                const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]) + t;
+                if (t < here) {
+                    uint4 u[kEach];
 #pragma unroll
                     for (int i = 0; i < kEach; ++i) u[i] = t + i * kRingWork < here ? units[i * kRingWork] : nothing<T>();
                     run.template add_units<T>(u, k);
@@ -713,6 +735,9 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             }
             if (due >= 0) write_due();
             due = row;
+            shape = new_shape;
+            from = new_from;
+            count = new_count;
             due_at = begin;
             ++n;
         }

@@ -83,6 +83,23 @@ __device__ __forceinline__ Pair unit_pair<__nv_bfloat16>(const uint4 &u, int i) 
     return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));  // bf16 -> fp32 is a shift
 }
 
+// values 2i and 2i+1, less r: for bf16 one instruction each widens and subtracts
+template <typename T>
+__device__ __forceinline__ Pair unit_less(const uint4 &u, int i, float r);
+template <>
+__device__ __forceinline__ Pair unit_less<float>(const uint4 &u, int i, float r) {
+    return add2(unit_pair<float>(u, i), pair(-r, -r));
+}
+template <>
+__device__ __forceinline__ Pair unit_less<__nv_bfloat16>(const uint4 &u, int i, float r) {
+    const unsigned w = i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
+    float lo, hi;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.bf16 %0, a, %3;\n\tadd.rn.f32.bf16 %1, b, %3;\n\t}"
+        : "=f"(lo), "=f"(hi)
+        : "r"(w), "f"(-r));
+    return pair(lo, hi);
+}
+
 // a unit of -inf
 template <typename T>
 __device__ __forceinline__ uint4 nothing() {
@@ -113,13 +130,10 @@ struct Running {
             top = t;
         }
     }
-    __device__ __forceinline__ Pair minus_ref() const {
-        const float r = top == -CUDART_INF_F ? 0.f : -top;
-        return pair(r, r);
-    }
-    __device__ __forceinline__ void add_pair(Pair x, Pair minus, Pair k2) {
+    __device__ __forceinline__ float ref() const { return top == -CUDART_INF_F ? 0.f : top; }
+    __device__ __forceinline__ void add_pair(Pair x_less_ref, Pair k2) {
         float d0, d1;
-        split(mul2(add2(x, minus), k2), d0, d1);
+        split(mul2(x_less_ref, k2), d0, d1);
         const Pair e = pair(exp2_fast(d0), exp2_fast(d1));
         sum = add2(sum, e);
         if (ENT) wsum = fma2(e, pair(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f)), wsum);  // -inf has e = 0
@@ -130,15 +144,16 @@ struct Running {
 #pragma unroll
         for (int i = 1; i < N; ++i) t = fmaxf(t, unit_max(u[i], T()));
         raise(t, k);
-        const Pair minus = minus_ref(), k2 = pair(k, k);
+        const float r = ref();
+        const Pair k2 = pair(k, k);
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int q = 0; q < kUnit<T> / 2; ++q) add_pair(unit_pair<T>(u[i], q), minus, k2);
+            for (int q = 0; q < kUnit<T> / 2; ++q) add_pair(unit_less<T>(u[i], q, r), k2);
     }
     __device__ __forceinline__ void add_one(float x, float k) {
         raise(x, k);
-        add_pair(pair(x, -CUDART_INF_F), minus_ref(), pair(k, k));
+        add_pair(pair(x - ref(), -CUDART_INF_F), pair(k, k));
     }
     __device__ __forceinline__ Stats stats() const {
         float a, b, c = 0.f, d = 0.f;
