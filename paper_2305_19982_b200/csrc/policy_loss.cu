@@ -444,15 +444,24 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
 // which one warp of its own does meanwhile, and nobody waits for them.  The ring therefore holds two
 // rows (slices).  One more warp issues the copies.
 
-constexpr int kStageBytes = 16384;
-constexpr int kStages = 14;
-constexpr int kRingWork = 512;
-constexpr int kRingWarps = kRingWork / 32;
-constexpr int kProducerWarp = kRingWarps, kScalarWarp = kRingWarps + 1;
-constexpr int kRingThreads = kRingWork + 64;
-constexpr int kStageUnits = kStageBytes / 16;
-constexpr int kEach = kStageUnits / kRingWork;                 // units of a stage that a thread takes
-constexpr int kSliceUnits = kStages / 2 * kStageUnits;         // largest slice of a row
+// How the ring is cut: WORK threads compute, a stage holds two units of each.  A stage that a row fills
+// in part costs nearly as much as a full one, so a launch takes the cut that fills better.
+template <int WORK, int STAGES>
+struct RingCut {
+    static constexpr int kWork = WORK, kStages = STAGES;
+    static constexpr int kEach = 2;                              // units of a stage that a thread takes
+    static constexpr int kWarps = WORK / 32, kThreads = WORK + 64;
+    static constexpr int kProducerWarp = kWarps, kScalarWarp = kWarps + 1;
+    static constexpr int kStageUnits = kEach * WORK, kStageBytes = 16 * kStageUnits;
+    static constexpr int kSliceUnits = STAGES / 2 * kStageUnits;  // largest slice of a row
+
+    // stages of a slice times their units, in percent of the slice
+    static int fill_cost(int64_t slice) {
+        return (int)((slice + kStageUnits - 1) / kStageUnits * kStageUnits * 100 / slice);
+    }
+};
+using Cut512 = RingCut<512, 14>;  // 14 x 16 KB: slices of up to 7168 units
+using Cut640 = RingCut<640, 11>;  // 11 x 20 KB: up to 6400
 
 // What the gradient of a row needs.
 struct Verdict {
@@ -462,23 +471,25 @@ struct Verdict {
 };
 
 // Two of each, for even and odd live rows: nobody is more than one row ahead.
+template <typename Cut>
 struct RingShared {
-    alignas(128) unsigned char stage[kStages][kStageBytes];
+    alignas(128) unsigned char stage[Cut::kStages][Cut::kStageBytes];
     alignas(16) float4 peer[2][kMaxCluster];  // {top, sum, x_target} of the cluster's CTAs
     Verdict verdict[2];
-    float2 slots[2][kRingWarps];              // {top, sum} of the warps
-    unsigned long long full[kStages], empty[kStages], joined[2], peered[2], ready[2];
+    float2 slots[2][Cut::kWarps];             // {top, sum} of the warps
+    unsigned long long full[Cut::kStages], empty[Cut::kStages], joined[2], peered[2], ready[2];
     double sums[1][4];
     int last, give_up;
 };
-static_assert(sizeof(RingShared) + 128 <= 232448, "shared memory of a CTA");
+static_assert(sizeof(RingShared<Cut512>) + 128 <= 232448 && sizeof(RingShared<Cut640>) + 128 <= 232448, "shared memory of a CTA");
 
 // Place in the ring: a stage, and the parity of the barrier phase that its current use completes.
+template <int STAGES>
 struct Cursor {
     uint32_t slot = 0, parity = 0;
 
     __device__ __forceinline__ void advance() {
-        if (++slot == kStages) {
+        if (++slot == STAGES) {
             slot = 0;
             parity ^= 1;
         }
@@ -491,11 +502,12 @@ __device__ __forceinline__ Stats join2(const Stats &a, const Stats &b, float k) 
     return {top, p.sum + q.sum, 0.f};
 }
 
-template <typename T, typename O>
-__global__ void __launch_bounds__(kRingThreads, 1)
+template <typename T, typename O, typename Cut>
+__global__ void __launch_bounds__(Cut::kThreads, 1)
 policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
+    constexpr int kStages = Cut::kStages, kStageUnits = Cut::kStageUnits, kRingWork = Cut::kWork, kEach = Cut::kEach;
     extern __shared__ unsigned char raw[];
-    RingShared &sh = *reinterpret_cast<RingShared *>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
+    RingShared<Cut> &sh = *reinterpret_cast<RingShared<Cut> *>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
     const int t = threadIdx.x, lane = t % 32, warp = t / 32;
     const int cluster = 1 << log_cluster;
     const int rank = cluster > 1 ? (int)cluster_rank() : 0;
@@ -503,10 +515,10 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
     if (t == 0) {
         for (int i = 0; i < kStages; ++i) {
             barrier_init(shared_addr(&sh.full[i]), 1);
-            barrier_init(shared_addr(&sh.empty[i]), kRingWarps);
+            barrier_init(shared_addr(&sh.empty[i]), Cut::kWarps);
         }
         for (int i = 0; i < 2; ++i) {
-            barrier_init(shared_addr(&sh.joined[i]), kRingWarps);
+            barrier_init(shared_addr(&sh.joined[i]), Cut::kWarps);
             barrier_init(shared_addr(&sh.peered[i]), 1);
             barrier_init(shared_addr(&sh.ready[i]), 1);
         }
@@ -516,9 +528,9 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
     __syncthreads();
     if (cluster > 1) cluster_sync();  // the peers' barriers are ready before the first message
 
-    if (warp == kProducerWarp) {
+    if (warp == Cut::kProducerWarp) {
         if (lane == 0) {
-            Cursor c;
+            Cursor<kStages> c;
             uint32_t issued = 0;  // stages, up to kStages
             for (int64_t row = first; row < a.rows && !*(volatile int *)&sh.give_up; row += step) {
                 if (a.weights[row] == 0.f || a.targets[row] < 0) continue;
@@ -546,7 +558,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 }
             }
         }
-    } else if (warp == kScalarWarp) {
+    } else if (warp == Cut::kScalarWarp) {
         Sums acc;
         uint32_t n = 0;  // live rows
         RowIn next = {-1, 0.f, 0.f, 0.f, 0.f};
@@ -575,7 +587,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             barrier_wait(shared_addr(&sh.joined[b]), parity, &sh.give_up);
             const Stats none = {-CUDART_INF_F, 0.f, 0.f};
             Stats s = none;
-            if (lane < kRingWarps) s = {sh.slots[b][lane].x, sh.slots[b][lane].y, 0.f};
+            if (lane < Cut::kWarps) s = {sh.slots[b][lane].x, sh.slots[b][lane].y, 0.f};
             s = warp_join<false>(join2(s, run.stats(), k), k);
             if (cluster > 1) {
                 const uint32_t bar = shared_addr(&sh.peered[b]);
@@ -609,10 +621,10 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
         __syncwarp();
         finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane);
     } else {
-        Cursor c;
+        Cursor<kStages> c;
         uint32_t n = 0;              // live rows whose statistics have been taken
         int64_t due = -1;            // the row whose gradient is to be written next
-        Cursor due_at;
+        Cursor<kStages> due_at;
         RowShape shape = {0, 0, 0};  // the due row's, and its slice
         int from = 0, count = 0;
         const auto write_due = [&]() {
@@ -621,7 +633,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             const Verdict q = sh.verdict[b];
             O *y = static_cast<O *>(a.dlogits) + due * a.ld_dlogits;
             const RowWriter<T, O> out(y, shape, q.top, q.unit, q.per_e, k);
-            Cursor at_stage = due_at;
+            Cursor<kStages> at_stage = due_at;
             const auto release = [&]() {
                 __syncwarp();
                 if (lane == 0) barrier_arrive(shared_addr(&sh.empty[at_stage.slot]));
@@ -703,7 +715,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 }
                 continue;
             }
-            const Cursor begin = c;
+            const Cursor<kStages> begin = c;
             Running<false> run;
             int at = 0;
             for (; new_count - at >= 2 * kStageUnits; at += 2 * kStageUnits) {
@@ -721,7 +733,12 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &sh.give_up);
                 const int here = new_count - at;
                 const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[c.slot]) + t;
-                if (t < here) {
+                if (here <= kRingWork) {
+                    if (t < here) {
+                        const uint4 u[1] = {units[0]};
+                        run.template add_units<T>(u, k);
+                    }
+                } else if (t < here) {
                     uint4 u[kEach];
 #pragma unroll
                     for (int i = 0; i < kEach; ++i) u[i] = t + i * kRingWork < here ? units[i * kRingWork] : nothing<T>();
@@ -868,11 +885,11 @@ cudaError_t policy_rows(const PolicyArgs &a, float k, int sm_count, cudaStream_t
     return cudaGetLastError();
 }
 
-template <typename T, typename O>
+template <typename T, typename O, typename Cut>
 cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count, cudaStream_t stream) {
-    constexpr size_t bytes = sizeof(RingShared) + 128;
+    constexpr size_t bytes = sizeof(RingShared<Cut>) + 128;
     static std::atomic<unsigned long long> ready{0};
-    cudaError_t e = allow_shared(policy_loss_ring_kernel<T, O>, (int)bytes, ready);
+    cudaError_t e = allow_shared(policy_loss_ring_kernel<T, O, Cut>, (int)bytes, ready);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     int64_t most = sm_count / cluster;
@@ -890,11 +907,11 @@ cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count,
             attr.id = cudaLaunchAttributeClusterDimension;
             attr.val.clusterDim = {(unsigned)cluster, 1, 1};
             cfg.gridDim = dim3((unsigned)(most * cluster));
-            cfg.blockDim = dim3(kRingThreads);
+            cfg.blockDim = dim3(Cut::kThreads);
             cfg.dynamicSmemBytes = bytes;
             cfg.attrs = &attr;
             cfg.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O>, &cfg);
+            e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O, Cut>, &cfg);
             if (e != cudaSuccess) return e;
             if (m < 1) m = 1;
             if (device < 64) resident[device][l].store(m);
@@ -902,7 +919,7 @@ cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count,
         if (m < most) most = m;
     }
     cfg.gridDim = dim3((unsigned)((a.rows < 1 ? 1 : a.rows < most ? a.rows : most) * cluster));
-    cfg.blockDim = dim3(kRingThreads);
+    cfg.blockDim = dim3(Cut::kThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr;
@@ -910,7 +927,7 @@ cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count,
     attr.val.clusterDim = {(unsigned)cluster, 1, 1};
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O>, a, k, log2_of(cluster));
+    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O, Cut>, a, k, log2_of(cluster));
 }
 
 template <typename T, typename O>
@@ -920,11 +937,15 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
     if (units <= 32 * kRowUnits) return policy_rows<T, O, 1>(a, k, sm_count, stream);
     if (units <= 128 * kRowUnits) return policy_rows<T, O, 4>(a, k, sm_count, stream);
     // as few CTAs to a row as hold two of its slices, more while there are fewer rows than SMs
-    constexpr int64_t kRing = kSliceUnits;
     int cluster = 1;
-    while (cluster < kMaxCluster && ((units + cluster - 1) / cluster > kRing || a.rows * cluster * 2 <= sm_count)) cluster *= 2;
-    if ((units + cluster - 1) / cluster <= kRing)
-        return policy_ring<T, O>(a, k, cluster, sm_count, stream);
+    while (cluster < kMaxCluster && ((units + cluster - 1) / cluster > Cut512::kSliceUnits || a.rows * cluster * 2 <= sm_count))
+        cluster *= 2;
+    // 8192 x 50257 bf16 (6282 units, 114 % against 101 %): 260 and 248 us; 8192 x 32000 (4000 units, 102 %
+    // against 128 %): 158 and 175 us.  On a tie the deeper ring.
+    const int64_t slice = (units + cluster - 1) / cluster;
+    if (slice <= Cut640::kSliceUnits && Cut640::fill_cost(slice) < Cut512::fill_cost(slice))
+        return policy_ring<T, O, Cut640>(a, k, cluster, sm_count, stream);
+    if (slice <= Cut512::kSliceUnits) return policy_ring<T, O, Cut512>(a, k, cluster, sm_count, stream);
     policy_loss_long_kernel<T, O><<<grid_of(a.rows, (int64_t)sm_count * 4), kThreads, 0, stream>>>(a, k);
     return cudaGetLastError();
 }
