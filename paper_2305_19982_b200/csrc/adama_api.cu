@@ -174,15 +174,18 @@ adama_status adama_init(adama_ctx **out, const adama_config *cfg) {
     if (!config_ok(cfg)) return ADAMA_ERR_INVALID_ARG;
     int count = 0;
     if (cudaGetDeviceCount(&count) != cudaSuccess || cfg->device >= count) return ADAMA_ERR_CUDA;
-    cudaDeviceProp prop;
-    if (cudaGetDeviceProperties(&prop, cfg->device) != cudaSuccess) return ADAMA_ERR_CUDA;
-    if (prop.major != 10) return ADAMA_ERR_UNSUPPORTED;  // kernels are built for sm_100a only
+    // the two attributes alone: a whole cudaDeviceProp takes milliseconds to fill
+    int major = 0, sm_count = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, cfg->device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess)
+        return ADAMA_ERR_CUDA;
+    if (major != 10) return ADAMA_ERR_UNSUPPORTED;  // kernels are built for sm_100a only
 
     adama_ctx *ctx = new (std::nothrow) adama_ctx();
     if (!ctx) return ADAMA_ERR_CUDA;
     memset(ctx, 0, sizeof(*ctx));
     ctx->cfg = *cfg;
-    ctx->sm_count = prop.multiProcessorCount;
+    ctx->sm_count = sm_count;
 
     DeviceGuard guard(cfg->device);
     const char *msg = "";
