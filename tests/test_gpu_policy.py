@@ -198,6 +198,59 @@ def test_policy_loss_and_gradient(T, V, dtype, out, pitch, offset, scale, ref):
         assert torch.equal(stats, second) and torch.equal(x, d)
 
 
+LONG = [(160, 16_385), (150, 51_200), (150, 51_203), (160, 57_345), (152, 65_537), (80, 131_073), (2, 229_381), (2, 458_760), (3, 459_001)]
+
+
+@pytest.mark.parametrize("dtype,out", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("T,V", LONG)
+@pytest.mark.parametrize("pitch,out_pitch", [(0, 0), (1, 7)])
+def test_policy_loss_of_long_rows(T, V, dtype, out, pitch, out_pitch):
+    """Rows of one CTA, of a cluster, and longer than a cluster holds; with the gradient's rows
+    aligned like the logits' and otherwise.  Same bounds as above; the reference in 64 bits is
+    evaluated on the GPU."""
+    opt = adama.AdamA()
+    gen = torch.Generator(device="cuda").manual_seed(T + V)
+    rows = torch.randn(T, V + pitch, generator=gen, device="cuda").to(dtype).mul_(2)
+    x = rows[:, :V]
+    targets = torch.randint(0, V, (T,), generator=gen, device="cuda")
+    targets[:4 if T > 4 else 1] = torch.tensor([0, V - 1, V // 2, 7], device="cuda")[:4 if T > 4 else 1]
+    logp = torch.stack([r.double()[t] - torch.logsumexp(r.double(), 0) for r, t in zip(x, targets)])
+    step = lambda s: ((torch.randn(T, generator=gen, device="cuda") * s * 512).round() + 0.5) / 512  # noqa: E731
+    old, ref = (logp - step(0.2)).float(), (logp - step(0.4)).float()
+    adv, weights = torch.randn(T, generator=gen, device="cuda"), torch.rand(T, generator=gen, device="cuda")
+    weights[2::5] = 0
+    whole = torch.full((T, V + out_pitch), 777.0, dtype=out, device="cuda")
+    d, stats, got = whole[:, :V], torch.empty(4, device="cuda"), torch.empty(T, device="cuda")
+    opt.policy_loss(x, targets, old, adv, weights, d, stats, ref_logp=ref, logp=got, kl_coef=0.1)
+    opt.sync_status()
+    r, dd = torch.exp(logp - old.double()), ref.double() - logp
+    A, w = adv.double(), weights.double()
+    clipped = r.clamp(0.8, 1.2) * A
+    cut = r * A > clipped
+    slope = torch.where(cut, 0.0, -r * A) + 0.1 * (1 - torch.exp(dd))
+    size = (torch.where(cut, 0.0, (r * A).abs()) + 0.1 * (1 + torch.exp(dd))) * w
+    assert float((got.double() - torch.where(w != 0, logp, 0.0)).abs().max()) <= LOGP
+    pg, kl = -torch.minimum(r * A, clipped), torch.exp(dd) - dd - 1
+    for value, terms in zip(stats.tolist(), (pg + 0.1 * kl, pg, kl, cut.double())):
+        assert abs(value - float((w * terms).sum())) <= 2 * LOGP * float((w * (4 * A.abs() + 2)).sum()) + 1e-6
+    for i in range(T):
+        p = torch.softmax(x[i].double(), 0)
+        grad = -p
+        grad[targets[i]] += 1
+        grad = grad * (w[i] * slope[i])
+        p[targets[i]] += 1
+        bound = GRAD * size[i] * p + HALF_ULP[out] * grad.abs() + 1e-30
+        err = (d[i].double() - grad).abs()
+        assert bool((err <= bound).all()), (i, float((err - bound).max()))
+        if float(w[i]) == 0:
+            assert not bool(d[i].any())
+    assert bool((whole[:, V:] == 777.0).all())
+    if dtype == out and pitch == 0:
+        second = torch.empty(4, device="cuda")
+        opt.policy_loss(x, targets, old, adv, weights, x, second, ref_logp=ref, kl_coef=0.1)
+        assert torch.equal(second, stats) and torch.equal(x, d)
+
+
 def test_gradient_against_differences():
     """Directional derivative: (loss(x + h*u) - loss(x - h*u))/2h with h = 1/64 against <dlogits, u>;
     u has unit entries, the truncation is h^2/6 of a third derivative of order |unit| and the loss's

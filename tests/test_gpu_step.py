@@ -109,6 +109,53 @@ def test_fold_apply_writes_nothing_outside_its_tensors(n):
     assert bool((bufs[0].view != 0).all())
 
 
+LONG = [2_500_001, 1, 6, 2048, 700_003, 4095, 1_048_576, 3]     # long enough to be streamed through shared memory
+
+
+@pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset,g_offset", [(0, 0), (1, 1), (3, 3), (2, 6), (1, 5), (0, 2), (1, 0)])
+def test_long_lists_equal_fold_then_apply(gdtype, offset, g_offset):
+    """Heads before the first boundary, ragged ends, gradients that reach their boundary with the
+    weights or not, chunks of one tensor beside those of the next; nothing outside is written."""
+    bufs = [[Guarded(n, offset=offset) for n in LONG] for _ in range(3)]
+    copies = [Guarded(n, dtype=torch.bfloat16, offset=offset) if i != 4 else None for i, n in enumerate(LONG)]
+    grads = [Guarded(n, dtype=gdtype, offset=g_offset) for n in LONG]
+    gen = torch.Generator(device="cuda").manual_seed(offset + 10 * g_offset)
+    for k, bs in enumerate(bufs):
+        for b in bs:
+            b.view.copy_(torch.randn(b.n, generator=gen, device="cuda") * 0.02)
+            if k == 2:
+                b.view.square_()
+    for g in grads:
+        g.view.copy_((torch.randn(g.n, generator=gen, device="cuda") * 1e-2).to(gdtype))
+    for c in copies:
+        if c is not None:
+            c.zero()
+    w2, m2, v2 = ([b.view.clone() for b in bs] for bs in bufs)
+    a, b = adama.AdamA(), adama.AdamA()
+    for opt in (a, b):
+        opt.set_step(5)
+        opt.begin_minibatch(1)
+        opt.set_weight_decay(0.01)
+    gs = [g.view for g in grads]
+    a.fold_apply_multi(*([x.view for x in bs] for bs in bufs[:1]), gs, *([x.view for x in bs] for bs in bufs[1:]), wl.LR,
+                       w_bf16=[c.view if c is not None else None for c in copies])
+    assert a.launch_count == 1
+    b.fold_multi(gs, m2, v2)
+    b.apply_multi(w2, m2, v2, wl.LR)
+    a.sync_status()
+    for bs, want in zip(bufs, (w2, m2, v2)):
+        for x, y in zip(bs, want):
+            assert torch.equal(x.view, y)
+            x.check()
+    for c, y in zip(copies, w2):
+        if c is not None:
+            assert torch.equal(c.view, y.bfloat16())
+            c.check()
+    for g in grads:
+        g.check()
+
+
 def test_factor_multiplies_the_gradient_and_nan_skips_the_step():
     n = 10_001
     g = wl.normal((n,), 1e-2, torch.float32, 1).cuda()
@@ -283,6 +330,53 @@ def test_fold_apply8_is_the_formula_operation_by_operation(n, offset, gdtype):
         for b in (w, copy, gg):
             b.check()
     assert not bool(raw.m_codes.view(torch.uint8)[offset + n:].any()) and not bool(raw.v_codes[offset + n:].any())
+
+
+@pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0, 8, 1])
+def test_long_8_bit_lists_equal_one_tensor_at_a_time(gdtype, offset):
+    """A long list is streamed through shared memory, single tensors of up to a million elements are
+    not: the same codes, scales and weights, whole blocks or ragged, aligned (offset 0 and 8 elements
+    of 16 bytes) or element by element (offset 1)."""
+    sizes = [1_000_000, 255, 256, 4097, 900_001, 3, 70_000]
+    gen = torch.Generator(device="cuda").manual_seed(offset)
+    off8 = 16 if offset == 8 else offset                        # codes are bytes
+    ws = [Guarded(n, offset=offset) for n in sizes]
+    gs = [Guarded(n, dtype=gdtype, offset=offset) for n in sizes]
+    cs = [Guarded(n, dtype=torch.bfloat16, offset=offset) for n in sizes]
+    for w, g in zip(ws, gs):
+        w.view.copy_(torch.randn(w.n, generator=gen, device="cuda") * 0.02)
+        g.view.copy_((torch.randn(w.n, generator=gen, device="cuda") * 1e-3).to(gdtype))
+    w2 = [w.view.clone() for w in ws]
+
+    def states():
+        raw = [State8.zeros(n + 32) for n in sizes]
+        return raw, [State8(r.m_codes[off8:off8 + n], r.m_scale[1:1 - (-n // 256)] if n + 32 > 256 * -(-n // 256) else
+                            r.m_scale[:-(-n // 256)], r.v_codes[off8:off8 + n], r.v_scale[:-(-n // 256)]) for r, n in zip(raw, sizes)]
+
+    raw1, s1 = states()
+    raw2, s2 = states()
+    a, b = adama.AdamA(), adama.AdamA()
+    for step in range(3):
+        a.begin_minibatch(1)
+        b.begin_minibatch(1)
+        a.fold_apply8_multi([w.view for w in ws], [g.view for g in gs], s1, wl.LR, w_bf16=[c.view for c in cs])
+        for w, g, s in zip(w2, gs, s2):
+            b.fold_apply8_multi([w], [g.view], [s], wl.LR)
+    a.sync_status()
+    assert a.launch_count == 3
+    for w, y, c, g in zip(ws, w2, cs, gs):
+        assert torch.equal(w.view, y) and torch.equal(c.view, y.bfloat16())
+        for x in (w, c, g):
+            x.check()
+    for x, y in zip(raw1, raw2):      # the bytes around the states too: untouched zeros
+        assert torch.equal(x.m_codes.view(torch.uint8), y.m_codes.view(torch.uint8)) and torch.equal(x.v_codes, y.v_codes)
+        assert torch.equal(x.m_scale, y.m_scale) and torch.equal(x.v_scale, y.v_scale)
+    ms, vs = [torch.empty(n, device="cuda") for n in sizes], [torch.empty(n, device="cuda") for n in sizes]
+    a.state8_unpack_multi(s1, ms, vs)
+    for s, m, v in zip(s1, ms, vs):
+        dm, dv = _decode(s)
+        assert np.array_equal(f64(m), dm.astype(F).astype(float)) and np.array_equal(f64(v), dv.astype(F).astype(float))
 
 
 def test_fold_apply8_tracks_32_bit_states():
