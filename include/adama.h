@@ -322,8 +322,8 @@ ADAMA_API adama_status adama_apply_sharded_peers(adama_ctx *ctx, float *const *w
  *            are (t has been counted all the same): a step with a non-finite gradient is skipped
  *            without a host round trip.
  * Any element-aligned pointers are accepted; 128-bit accesses are used for a tensor whose w, m, v
- * reach a 16-byte boundary after the same number of elements and whose gradient (and copy) reach a
- * 4-element boundary there, element accesses otherwise.  Tensors must not overlap.
+ * reach a 16-byte boundary after the same number of elements (at most 7) and whose gradient and copy
+ * reach a 4-element boundary there, element accesses otherwise.  Tensors must not overlap.
  * Errors: INVALID_ARG, BAD_STATE, MISALIGNED (element alignment), CUDA. */
 ADAMA_API adama_status adama_fold_apply_multi(adama_ctx *ctx, const void *const *grads,
                                               adama_dtype gdt, float *const *w, float *const *m,

@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroups = kChunk / (4 * kThreads);  // float4 groups of one thread in a chunk
-constexpr unsigned char kScalar = 255;            // no common 16-byte alignment: element by element
+constexpr unsigned char kScalar = 255;            // no common alignment: element by element
 
 template <int CAP>
 struct StepTable {
@@ -24,7 +24,8 @@ struct StepTable {
     __nv_bfloat16 *copy[CAP];  // entries may be null
     unsigned long long n[CAP];
     unsigned chunk_start[CAP + 1];
-    unsigned char head[CAP];  // elements before the first 16-byte boundary of w, m, v; or kScalar
+    unsigned char head[CAP];  // elements before the vector accesses begin (0..7), or kScalar
+    unsigned char bulk[CAP];  // 1: the gradient is 16-byte aligned there too
     int count;
 };
 static_assert(sizeof(StepTable<kStepMax>) <= 32000, "table must fit the kernel parameter space");
@@ -50,6 +51,36 @@ __device__ __forceinline__ void scalar_element(const G *g, float *w, float *m, f
     m[i] = mi;
     v[i] = vi;
     if (copy) copy[i] = __float2bfloat16_rn(wi);
+}
+
+// Elements [i, end) at a distance of `stride`, four of them on their way at a time.
+template <typename G>
+__device__ __forceinline__ void scalar_run(const G *g, float *w, float *m, float *v, __nv_bfloat16 *copy, size_t i, size_t end,
+                                           size_t stride, float factor, const FoldConstants &f, const ApplyConstants &c) {
+    for (; i < end; i += 4 * stride) {
+        float gg[4], ww[4], mm[4], vv[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const size_t j = i + q * stride;
+            if (j < end) {
+                gg[q] = widen(g[j]);
+                ww[q] = w[j];
+                mm[q] = m[j];
+                vv[q] = v[j];
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const size_t j = i + q * stride;
+            if (j < end) {
+                step1(gg[q] * factor, ww[q], mm[q], vv[q], f, c);
+                w[j] = ww[q];
+                m[j] = mm[q];
+                v[j] = vv[q];
+                if (copy) copy[j] = __float2bfloat16_rn(ww[q]);
+            }
+        }
+    }
 }
 
 __device__ __forceinline__ void step4(const Grad4 &g, float factor, float4 &x, float4 &y, float4 &z, const FoldConstants &f,
@@ -84,11 +115,10 @@ fold_apply_multi_kernel(const __grid_constant__ StepTable<CAP> tab, FoldConstant
         const unsigned char head = tab.head[t];
         if (head == kScalar) {
             const size_t end = (k + 1) * kChunk < n ? (k + 1) * kChunk : n;
-            for (size_t i = k * kChunk + threadIdx.x; i < end; i += kThreads)
-                scalar_element(g, w, m, v, copy, i, factor, f, c);
+            scalar_run(g, w, m, v, copy, k * kChunk + threadIdx.x, end, kThreads, factor, f, c);
             continue;
         }
-        if (k == 0 && threadIdx.x < head) scalar_element(g, w, m, v, copy, threadIdx.x, factor, f, c);
+        if (k == 0 && threadIdx.x < head && threadIdx.x < n) scalar_element(g, w, m, v, copy, threadIdx.x, factor, f, c);
         const size_t base = head + k * kChunk + 4 * threadIdx.x;
         Group r[kGroups];
 #pragma unroll
@@ -176,8 +206,7 @@ fold_apply_ring_kernel(const __grid_constant__ StepTable<CAP> tab, FoldConstants
             const G *g = static_cast<const G *>(tab.g[t]) + base;
             const size_t left = n > base ? n - base : 0;
             // whole units of eight elements of an aligned tensor; the threads fetch the rest themselves
-            const bool bulk = head != kScalar && reinterpret_cast<uintptr_t>(g) % 16 == 0;
-            const uint32_t k = bulk ? (uint32_t)(left < kRingChunk ? left : kRingChunk) & ~7u : 0;
+            const uint32_t k = tab.bulk[t] ? (uint32_t)(left < kRingChunk ? left : kRingChunk) & ~7u : 0;
             if (issued == kStages && !barrier_wait(shared_addr(&sh.empty[slot]), parity ^ 1, &sh.give_up)) break;
             const uint32_t full = shared_addr(&sh.full[slot]);
             sh.tensor[slot] = t;
@@ -230,25 +259,42 @@ fold_apply_ring_kernel(const __grid_constant__ StepTable<CAP> tab, FoldConstants
         // before the first boundary, behind the last whole unit, or all of an unaligned tensor's chunk
         if (k == 0 && head != kScalar && tid < head && (size_t)tid < n) scalar_element(g, w, m, v, copy, tid, factor, f, c);
         const size_t end = base + kRingChunk < n ? base + kRingChunk : n;
-        for (size_t i = base + loaded + tid; i < end; i += kRingWork) scalar_element(g, w, m, v, copy, i, factor, f, c);
+        if (!tab.bulk[t] && head != kScalar && end >= base + 4 * tid + 4) {  // aligned, but not for bulk copies
+            const size_t i = base + 4 * tid;
+            r.g = load_grad4(g + i, 0);
+            r.w = ld_stream(reinterpret_cast<float4 *>(w + i));
+            r.m = ld_stream(reinterpret_cast<float4 *>(m + i));
+            r.v = ld_stream(reinterpret_cast<float4 *>(v + i));
+            step4(r.g, factor, r.w, r.m, r.v, f, c);
+            store4(w, m, v, copy, i, r.w, r.m, r.v);
+        }
+        const size_t done = tab.bulk[t] ? base + loaded : head == kScalar ? base : end > base ? base + (end - base) / 4 * 4 : end;
+        scalar_run(g, w, m, v, copy, done + tid, end, kRingWork, factor, f, c);
     }
     if (tid == 0 && *(volatile int *)&sh.give_up &&
         atomicCAS(status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
         status[1] = kWaitStepRing;
 }
 
-// Elements up to the first 16-byte boundary when w, m, v reach it together and the gradient (and
-// the copy) reach their own 4-element boundary there too; kScalar otherwise.
-unsigned char head_of(const void *g, adama_dtype gdt, const float *w, const float *m, const float *v,
-                      const void *copy) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(w) & 15;
-    const uintptr_t head = at ? (16 - at) / 4 : 0;
+// Elements before w, m, v are at a 16-byte boundary, the gradient at one too (bulk copies need it) or
+// at least at its own 4-element boundary, and the copy at 8 bytes; kScalar where there is no such place.
+void place_of(const void *g, adama_dtype gdt, const float *w, const float *m, const float *v, const void *copy,
+              unsigned char &head, unsigned char &bulk) {
     const uintptr_t gs = gdt == ADAMA_F32 ? 4 : 2;
-    if ((reinterpret_cast<uintptr_t>(m) & 15) != at || (reinterpret_cast<uintptr_t>(v) & 15) != at ||
-        (reinterpret_cast<uintptr_t>(g) + head * gs) % (4 * gs) != 0 ||
-        (copy && (reinterpret_cast<uintptr_t>(copy) + head * 2) % 8 != 0))
-        return kScalar;
-    return (unsigned char)head;
+    const auto at = [](const void *p, uintptr_t bytes, uintptr_t align) {
+        return (reinterpret_cast<uintptr_t>(p) + bytes) % align == 0;
+    };
+    for (int whole = 1; whole >= 0; --whole) {
+        for (uintptr_t h = 0; h < 8; ++h) {
+            if (!at(w, 4 * h, 16) || !at(m, 4 * h, 16) || !at(v, 4 * h, 16) || !at(g, gs * h, whole ? 16 : 4 * gs)) continue;
+            if (copy && !at(copy, 2 * h, 8)) continue;
+            head = (unsigned char)h;
+            bulk = (unsigned char)whole;
+            return;
+        }
+    }
+    head = kScalar;
+    bulk = 0;
 }
 
 constexpr unsigned kRingFrom = 4;  // chunks of the ring per SM from which it is used
@@ -282,7 +328,7 @@ cudaError_t launch(const StepList &s, adama_dtype gdt, int first, int count, Fol
         tab.m[i] = s.m[first + i];
         tab.v[i] = s.v[first + i];
         tab.copy[i] = s.copy ? static_cast<__nv_bfloat16 *>(s.copy[first + i]) : nullptr;
-        tab.head[i] = head_of(tab.g[i], gdt, tab.w[i], tab.m[i], tab.v[i], tab.copy[i]);
+        place_of(tab.g[i], gdt, tab.w[i], tab.m[i], tab.v[i], tab.copy[i], tab.head[i], tab.bulk[i]);
     }
     tab.count = count;
     return gdt == ADAMA_F32

@@ -44,8 +44,9 @@ __device__ __forceinline__ Stats group_join(Stats s, float k, Stats *slots, int 
     return warp_join<ENT>(lane < W ? slots[lane] : none, k);
 }
 
-__device__ __forceinline__ float logp_of(float x_target, const Stats &s, float log2sum, float k) {
-    return CUDART_LN2_F * (k * (x_target - s.top) - log2sum);
+// In natural units: the rounding of k does not show but through the sum.
+__device__ __forceinline__ float logp_of(float x_target, const Stats &s, float log_sum, float scale) {
+    return fmaf(scale, x_target - s.top, -log_sum);
 }
 
 constexpr int kMaxCluster = 8;  // CTAs that may share a row
@@ -119,10 +120,10 @@ token_logprobs_kernel(const LogprobArgs a, float k, int log_cluster) {
             const int lane = t % 32;
             s = warp_join<ENT>(lane < 1 << log_cluster ? peers[lane] : none, k);
         }
-        const float log2sum = log2f(s.sum);
-        lse = fmaf(s.top, (float)a.scale, CUDART_LN2_F * log2sum);
-        logp = logp_of(x_target, s, log2sum, k);
-        if (ENT) entropy = CUDART_LN2_F * (log2sum - s.wsum / s.sum);
+        const float log_sum = logf(s.sum), scale = (float)a.scale;
+        lse = fmaf(s.top, scale, log_sum);
+        logp = logp_of(x_target, s, log_sum, scale);
+        if (ENT) entropy = log_sum - CUDART_LN2_F * (s.wsum / s.sum);
         if (!inside && t == 0) record_bad_target(a.status, row);
     }
     if (t == 0 && rank == 0) {
@@ -155,9 +156,9 @@ __device__ __forceinline__ RowIn row_in(const PolicyArgs &a, int64_t row) {
 struct RowOut {
     float logp, pg, kl, cut, unit, per_e;
 };
-__device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, const Stats &s, float x_target, float k) {
+__device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, const Stats &s, float x_target) {
     RowOut o;
-    o.logp = logp_of(x_target, s, log2f(s.sum), k);
+    o.logp = logp_of(x_target, s, logf(s.sum), a.scale);
     const float r = expf(o.logp - in.old), plain = r * in.adv;
     const float clipped = fminf(fmaxf(r, a.ratio_min), a.ratio_max) * in.adv;
     const bool cut = plain > clipped;
@@ -398,7 +399,7 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
             // the gradient may replace the logits: all have been read when the join is through
             const Stats s = group_join<W, false>(run.stats(), k, shared + g * W, g);
             top = s.top;
-            o = row_out(a, in, s, x_target, k);
+            o = row_out(a, in, s, x_target);
             if (t == 0) {
                 acc.add(a, in, o);
                 if (!inside) record_bad_target(a.status, row);
@@ -599,7 +600,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 x_target = __shfl_sync(0xffffffffu, q.z, 0);
                 s = warp_join<false>({q.x, q.y, 0.f}, k);
             }
-            const RowOut o = row_out(a, in, s, x_target, k);
+            const RowOut o = row_out(a, in, s, x_target);
             O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
             const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
             if (lane == 0) {
@@ -798,7 +799,7 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
             if (has_extra) run.add_one(x_extra, k);
             const Stats s = group_join<kWarps, false>(run.stats(), k, shared, 0);
             top = s.top;
-            o = row_out(a, in, s, x_target, k);
+            o = row_out(a, in, s, x_target);
             if (t == 0) {
                 acc.add(a, in, o);
                 if (!inside) record_bad_target(a.status, row);

@@ -96,13 +96,16 @@ def test_fold_apply_more_tensors_than_one_launch_holds():
         assert torch.equal(x, y)
 
 
-@pytest.mark.parametrize("n", [1, 7, 4099, 70_001])
-def test_fold_apply_writes_nothing_outside_its_tensors(n):
+@pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset,g_offset", [(1, 3), (1, 1), (3, 3), (2, 6), (3, 7)])
+@pytest.mark.parametrize("n", [1, 2, 4, 7, 4099, 70_001])
+def test_fold_apply_writes_nothing_outside_its_tensors(n, offset, g_offset, gdtype):
+    """Among them tensors that end before the first boundary that their vector accesses wait for."""
     opt = adama.AdamA()
     opt.begin_minibatch(1)
-    bufs = [Guarded(n, offset=o).zero() for o in (1, 1, 1)]
-    copy = Guarded(n, dtype=torch.bfloat16, offset=3).zero()
-    g = Guarded(n, dtype=torch.bfloat16, offset=3).fill(wl.normal((n,), 1e-2, torch.bfloat16, 5).cuda())
+    bufs = [Guarded(n, offset=offset).zero() for _ in range(3)]
+    copy = Guarded(n, dtype=torch.bfloat16, offset=g_offset).zero()
+    g = Guarded(n, dtype=gdtype, offset=g_offset).fill(wl.normal((n,), 1e-2, gdtype, 5).cuda())
     opt.fold_apply_multi([bufs[0].view], [g.view], [bufs[1].view], [bufs[2].view], wl.LR, w_bf16=[copy.view])
     for b in bufs + [copy, g]:
         b.check()
@@ -113,7 +116,7 @@ LONG = [2_500_001, 1, 6, 2048, 700_003, 4095, 1_048_576, 3]     # long enough to
 
 
 @pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("offset,g_offset", [(0, 0), (1, 1), (3, 3), (2, 6), (1, 5), (0, 2), (1, 0)])
+@pytest.mark.parametrize("offset,g_offset", [(0, 0), (1, 1), (3, 3), (2, 6), (1, 5), (0, 2), (1, 0), (0, 4), (3, 1)])
 def test_long_lists_equal_fold_then_apply(gdtype, offset, g_offset):
     """Heads before the first boundary, ragged ends, gradients that reach their boundary with the
     weights or not, chunks of one tensor beside those of the next; nothing outside is written."""
