@@ -446,23 +446,25 @@ state8_pack_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
     }
 }
 
-// Codes and scales -> the values they stand for; one warp to kUnpackBlocks consecutive blocks, whose
-// loads are all issued before the first store.
+// Codes and scales -> the values they stand for; one warp to kUnpackBlocks consecutive blocks of a
+// chunk.  The next chunk's codes are on their way while this one's values are written.
 constexpr int kUnpackBlocks = kBlocks / kWarps;
+// 405 M parameters take 651 us (4/5 of it writes) with 3 CTAs per SM, 725 with 2, 713 with 4, 712 with 6,
+// 684 without the look-ahead at 8, 690 with the codes streamed through shared memory.
+constexpr int kUnpackCtas = 3;
 
-template <int CAP>
-__global__ void __launch_bounds__(kThreads)
-state8_unpack_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
-    const unsigned total = tab.chunk_start[tab.count];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x) {
-        const int t = tensor_of_chunk(tab.chunk_start, tab.count, chunk);
-        const size_t n = (size_t)tab.n[t];
-        const size_t first = (size_t)(chunk - tab.chunk_start[t]) * kChunk + (size_t)warp * kUnpackBlocks * kStateBlock;
-        const adama_state8 s = tab.s[t];
-        float *m = tab.m[t], *v = tab.v[t];
-        uint2 mc[kUnpackBlocks], vc[kUnpackBlocks];
-        float sm[kUnpackBlocks], sv[kUnpackBlocks];
+struct UnpackBlocks {
+    size_t first, n;  // of the warp's elements; n: where the tensor ends (0: no chunk)
+    int t;
+    uint2 mc[kUnpackBlocks], vc[kUnpackBlocks];
+    float sm[kUnpackBlocks], sv[kUnpackBlocks];
+
+    template <int CAP>
+    __device__ __forceinline__ void load(const ConvertTable<CAP> &tab, unsigned chunk, int from, int warp, int lane) {
+        t = tensor_from(tab.chunk_start, from, chunk);
+        n = (size_t)tab.n[t];
+        first = (size_t)(chunk - tab.chunk_start[t]) * kChunk + (size_t)warp * kUnpackBlocks * kStateBlock;
+        const adama_state8 &s = tab.s[t];
 #pragma unroll
         for (int b = 0; b < kUnpackBlocks; ++b) {
             const size_t at = first + b * kStateBlock, blk = at / kStateBlock;
@@ -474,6 +476,10 @@ state8_unpack_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
                 sv[b] = s.v_scale[blk];
             }
         }
+    }
+    template <int CAP>
+    __device__ __forceinline__ void store(const ConvertTable<CAP> &tab, int lane) const {
+        float *m = tab.m[t], *v = tab.v[t];
 #pragma unroll
         for (int b = 0; b < kUnpackBlocks; ++b) {
             const size_t at = first + b * kStateBlock;
@@ -494,6 +500,27 @@ state8_unpack_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
                 }
             }
         }
+    }
+};
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads)
+state8_unpack_kernel(const __grid_constant__ ConvertTable<CAP> tab) {
+    const unsigned total = tab.chunk_start[tab.count];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    unsigned chunk = blockIdx.x;
+    if (chunk >= total) return;
+    UnpackBlocks a, b;
+    a.load(tab, chunk, tensor_of_chunk(tab.chunk_start, tab.count, chunk), warp, lane);
+    for (;;) {
+        chunk += gridDim.x;
+        if (chunk < total) b.load(tab, chunk, a.t, warp, lane);
+        a.store(tab, lane);
+        if (chunk >= total) return;
+        chunk += gridDim.x;
+        if (chunk < total) a.load(tab, chunk, b.t, warp, lane);
+        b.store(tab, lane);
+        if (chunk >= total) return;
     }
 }
 
@@ -554,7 +581,7 @@ cudaError_t launch_convert(const StepList &s, int first, int count, int sm_count
     const unsigned chunks = fill_chunks(tab.n, tab.chunk_start, s.n + first, count);
     if (chunks == 0) return cudaSuccess;
     if (PACK) state8_pack_kernel<CAP><<<grid_of(chunks, sm_count, 8), kThreads, 0, stream>>>(tab);
-    else state8_unpack_kernel<CAP><<<grid_of(chunks, sm_count, 8), kThreads, 0, stream>>>(tab);
+    else state8_unpack_kernel<CAP><<<grid_of(chunks, sm_count, kUnpackCtas), kThreads, 0, stream>>>(tab);
     return cudaGetLastError();
 }
 
