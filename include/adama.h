@@ -352,10 +352,10 @@ typedef struct adama_state8 {
  * formula, evaluated in fp32 on the values that the codes stand for; the beta decay multiplies the
  * scales, the codes are those of the undecayed m_t, v_t.
  *   states : HOST array of `count` descriptions of device buffers
- * It is meant for ONE gradient per mini-batch.  There is deliberately no 8-bit form of adama_fold:
- * a micro-batch changes v by less than half of a code's width, so rounding after each of N folds
- * would lose most of them.  To accumulate several micro-batches, sum them first (adama_sgdm_fold
- * into an fp32 buffer), then make this call.
+ * It is meant for ONE gradient per mini-batch.  There is deliberately no 8-bit form of adama_fold: a
+ * single micro-batch changes most entries of v by far less than half of a code's width, and rounding
+ * after each of N folds would lose those changes.  To accumulate several micro-batches, sum them
+ * first (adama_sgdm_fold into an fp32 buffer), then make this call.
  * Up to 448 tensors share a launch; tensors whose buffers are all 16-byte aligned are streamed in
  * whole blocks, others (and the last, shorter block) element by element.  grad_factor, w_bf16 and errors as
  * adama_fold_apply_multi. */
@@ -367,8 +367,8 @@ ADAMA_API adama_status adama_fold_apply8_multi(adama_ctx *ctx, const void *const
 
 /* fp32 moments into codes and scales (a run that moves from 32 to 8 bits, a checkpoint read back),
  * and codes and scales into the fp32 values that they stand for.  m, v follow the state convention
- * above (decayed between mini-batches).  Packing the result of an unpack gives the same values back
- * to the last bit of the scales.  Errors: INVALID_ARG, MISALIGNED, CUDA. */
+ * above (decayed between mini-batches).  Packing the result of an unpack gives the same codes back,
+ * with scales that differ by a few units in the last place at most.  Errors: INVALID_ARG, MISALIGNED, CUDA. */
 ADAMA_API adama_status adama_state8_pack_multi(adama_ctx *ctx, const float *const *m,
                                                const float *const *v, const adama_state8 *states,
                                                const size_t *n, int count, void *cuda_stream);
@@ -386,8 +386,8 @@ ADAMA_API adama_status adama_state8_unpack_multi(adama_ctx *ctx, const adama_sta
  *     sumsq = sum over all tensors of g^2  (+ out->sumsq if `accumulate`),  norm = sqrt(sumsq),
  *     factor = max_norm/norm where norm > max_norm, else 1; NaN where norm is not finite
  * `accumulate` joins lists of different dtypes (or of several ranks, the caller having summed
- * sumsq) in one norm.  Squares are formed and summed in fp32 within 16 elements of a thread, in
- * double from there on; entries beyond 1.8e19 count as infinite.  The result does not depend on
+ * sumsq) in one norm.  Squares are formed and summed in fp32 within up to 64 elements of a thread (13
+ * roundings at most), in double from there on; entries beyond 1.8e19 count as infinite.  The result does not depend on
  * scheduling.  An empty list gives norm 0, factor 1.  max_norm > 0, may be infinite (no clipping).
  * One launch for up to 1024 tensors, any element-aligned pointers.
  *   out : one adama_grad_norm in DEVICE memory, 8-byte aligned

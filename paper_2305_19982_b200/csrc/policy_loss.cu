@@ -454,7 +454,8 @@ struct RingCut {
     static constexpr int kWarps = WORK / 32, kThreads = WORK + 64;
     static constexpr int kProducerWarp = kWarps, kScalarWarp = kWarps + 1;
     static constexpr int kStageUnits = kEach * WORK, kStageBytes = 16 * kStageUnits;
-    static constexpr int kSliceUnits = STAGES / 2 * kStageUnits;  // largest slice of a row
+    static constexpr int kRingUnits = STAGES * kStageUnits;
+    static constexpr int kSliceUnits = STAGES / 2 * kStageUnits;  // largest slice of which two fit
 
     // stages of a slice times their units, in percent of the slice
     static int fill_cost(int64_t slice) {
@@ -887,49 +888,60 @@ cudaError_t policy_rows(const PolicyArgs &a, float k, int sm_count, cudaStream_t
 }
 
 template <typename T, typename O, typename Cut>
-cudaError_t policy_ring(const PolicyArgs &a, float k, int cluster, int sm_count, cudaStream_t stream) {
-    constexpr size_t bytes = sizeof(RingShared<Cut>) + 128;
-    static std::atomic<unsigned long long> ready{0};
-    cudaError_t e = allow_shared(policy_loss_ring_kernel<T, O, Cut>, (int)bytes, ready);
-    if (e != cudaSuccess) return e;
+struct RingLaunch {
+    static constexpr int kBytes = (int)sizeof(RingShared<Cut>) + 128;
     cudaLaunchConfig_t cfg = {};
-    int64_t most = sm_count / cluster;
-    if (cluster > 1) {
-        // a GPC's SMs need not be a multiple of the cluster's; a cluster that waits for its turn would
-        // leave its share of the rows to the end
-        static std::atomic<int> resident[64][4];
-        const int l = log2_of(cluster);
+    cudaLaunchAttribute attr;
+
+    RingLaunch(int cluster, int64_t clusters, cudaStream_t stream) {
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim = {(unsigned)cluster, 1, 1};
+        cfg.gridDim = dim3((unsigned)(clusters * cluster));
+        cfg.blockDim = dim3(Cut::kThreads);
+        cfg.dynamicSmemBytes = kBytes;
+        cfg.stream = stream;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+    }
+    RingLaunch(const RingLaunch &) = delete;  // cfg points at attr
+
+    static cudaError_t prepare() {
+        static std::atomic<unsigned long long> ready{0};
+        return allow_shared(policy_loss_ring_kernel<T, O, Cut>, kBytes, ready);
+    }
+    // Clusters that run at a time.  A GPC's SMs need not be a multiple of the cluster's (132 of 148 SMs
+    // take part in clusters of 4, 120 in clusters of 8), and a cluster that waits for its turn would leave
+    // its share of the rows to the end.  Asked for once per device.
+    static cudaError_t resident(int cluster, int sm_count, int *out) {
+        static std::atomic<int> known[64][4];
+        *out = sm_count;
+        if (cluster == 1) return cudaSuccess;
         int device = 0;
-        e = cudaGetDevice(&device);
+        cudaError_t e = cudaGetDevice(&device);
         if (e != cudaSuccess) return e;
-        int m = device < 64 ? resident[device][l].load() : 0;
+        std::atomic<int> *slot = device < 64 ? &known[device][log2_of(cluster)] : nullptr;
+        int m = slot ? slot->load() : 0;
         if (m == 0) {
-            cudaLaunchAttribute attr;
-            attr.id = cudaLaunchAttributeClusterDimension;
-            attr.val.clusterDim = {(unsigned)cluster, 1, 1};
-            cfg.gridDim = dim3((unsigned)(most * cluster));
-            cfg.blockDim = dim3(Cut::kThreads);
-            cfg.dynamicSmemBytes = bytes;
-            cfg.attrs = &attr;
-            cfg.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O, Cut>, &cfg);
+            e = prepare();
+            if (e != cudaSuccess) return e;
+            RingLaunch l(cluster, sm_count / cluster, nullptr);
+            e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O, Cut>, &l.cfg);
             if (e != cudaSuccess) return e;
             if (m < 1) m = 1;
-            if (device < 64) resident[device][l].store(m);
+            if (slot) slot->store(m);
         }
-        if (m < most) most = m;
+        *out = m;
+        return cudaSuccess;
     }
-    cfg.gridDim = dim3((unsigned)((a.rows < 1 ? 1 : a.rows < most ? a.rows : most) * cluster));
-    cfg.blockDim = dim3(Cut::kThreads);
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim = {(unsigned)cluster, 1, 1};
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, policy_loss_ring_kernel<T, O, Cut>, a, k, log2_of(cluster));
-}
+    static cudaError_t launch(const PolicyArgs &a, float k, int cluster, int sm_count, cudaStream_t stream) {
+        int most = 0;
+        cudaError_t e = prepare();
+        if (e == cudaSuccess) e = resident(cluster, sm_count, &most);
+        if (e != cudaSuccess) return e;
+        RingLaunch l(cluster, a.rows < 1 ? 1 : a.rows < most ? a.rows : most, stream);
+        return cudaLaunchKernelEx(&l.cfg, policy_loss_ring_kernel<T, O, Cut>, a, k, log2_of(cluster));
+    }
+};
 
 template <typename T, typename O>
 cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
@@ -937,16 +949,28 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
     const int64_t units = a.vocab / kUnit<T>;
     if (units <= 32 * kRowUnits) return policy_rows<T, O, 1>(a, k, sm_count, stream);
     if (units <= 128 * kRowUnits) return policy_rows<T, O, 4>(a, k, sm_count, stream);
-    // as few CTAs to a row as hold two of its slices, more while there are fewer rows than SMs
+    // As few CTAs to a row as hold two of its slices.  Few rows are dealt out at once, one to a cluster as
+    // large as that allows, which then has to hold one slice (33 x 131072 fp32: 8.9 us with 4 CTAs to a
+    // row, 10.9 with 8 in three turns).
+    using Ring = RingLaunch<T, O, Cut512>;
     int cluster = 1;
-    while (cluster < kMaxCluster && ((units + cluster - 1) / cluster > Cut512::kSliceUnits || a.rows * cluster * 2 <= sm_count))
-        cluster *= 2;
-    // 8192 x 50257 bf16 (6282 units, 114 % against 101 %): 260 and 248 us; 8192 x 32000 (4000 units, 102 %
-    // against 128 %): 158 and 175 us.  On a tie the deeper ring.
+    while (cluster < kMaxCluster && (units + cluster - 1) / cluster > Cut512::kSliceUnits) cluster *= 2;
+    bool one_turn = false;
+    for (int c = kMaxCluster; c >= 1 && !one_turn; c /= 2) {
+        int most = 0;
+        const cudaError_t e = a.rows * c <= sm_count ? Ring::resident(c, sm_count, &most) : cudaSuccess;
+        if (e != cudaSuccess) return e;
+        if (a.rows <= most && (units + c - 1) / c <= Cut640::kRingUnits) {
+            cluster = c;
+            one_turn = true;
+        }
+    }
+    // 8192 x 50257 bf16 (6282 units, 114 % against 101 %): 260 and 255 us, with odd pitches 159 and 146;
+    // 8192 x 32000 (4000 units, 102 % against 128 %): 158 and 175 us.  On a tie the deeper ring.
     const int64_t slice = (units + cluster - 1) / cluster;
-    if (slice <= Cut640::kSliceUnits && Cut640::fill_cost(slice) < Cut512::fill_cost(slice))
-        return policy_ring<T, O, Cut640>(a, k, cluster, sm_count, stream);
-    if (slice <= Cut512::kSliceUnits) return policy_ring<T, O, Cut512>(a, k, cluster, sm_count, stream);
+    if ((one_turn || slice <= Cut640::kSliceUnits) && Cut640::fill_cost(slice) < Cut512::fill_cost(slice))
+        return RingLaunch<T, O, Cut640>::launch(a, k, cluster, sm_count, stream);
+    if (one_turn || slice <= Cut512::kSliceUnits) return Ring::launch(a, k, cluster, sm_count, stream);
     policy_loss_long_kernel<T, O><<<grid_of(a.rows, (int64_t)sm_count * 4), kThreads, 0, stream>>>(a, k);
     return cudaGetLastError();
 }

@@ -471,8 +471,8 @@ def test_many_8_bit_tensors_in_several_launches_equal_one_by_one():
 @pytest.mark.parametrize("sizes,offset", [([1], 0), ([3, 1, 2], 1), ([4096, 5, 0, 4097], 3), ([100_003, 17], 1),
                                           ([(31 * i) % 200 for i in range(2100)], 1), ([3_000_001], 0)])
 def test_grad_norm_against_64_bits(sizes, offset, gdtype):
-    """Squares and sums of 16 in fp32, the rest in double: relative error of the sum <= 17*2^-24 =
-    1.0e-6, half of it on the norm, one more rounding on the factor."""
+    """Squares and sums of up to 64 elements in fp32 (13 roundings at most), the rest in double: relative
+    error of the sum <= 1.0e-6 (17*2^-24), half of it on the norm, one more rounding on the factor."""
     opt = adama.AdamA()
     gs = _views(sizes, offset, gdtype)
     for i, g in enumerate(gs):
