@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import enum
+import struct
 from pathlib import Path
 from typing import Optional
 
@@ -67,16 +68,9 @@ class _State8(ctypes.Structure):
                 ("v_codes", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
-class _PolicyArgs(ctypes.Structure):
-    _fields_ = [("logits", ctypes.c_void_p), ("dlogits", ctypes.c_void_p),
-                ("logits_dtype", ctypes.c_int), ("dlogits_dtype", ctypes.c_int),
-                ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ld_logits", ctypes.c_int64),
-                ("ld_dlogits", ctypes.c_int64), ("targets", ctypes.c_void_p),
-                ("old_logp", ctypes.c_void_p), ("ref_logp", ctypes.c_void_p),
-                ("advantages", ctypes.c_void_p), ("weights", ctypes.c_void_p),
-                ("logit_scale", ctypes.c_double), ("clip_low", ctypes.c_double),
-                ("clip_high", ctypes.c_double), ("kl_coef", ctypes.c_double),
-                ("logp", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("workspace", ctypes.c_void_p)]
+# adama_policy_args in native layout: logits, dlogits, two dtypes, rows, vocab, two pitches, five per-row
+# pointers, four doubles, logp, stats, workspace (packing costs a third of filling a ctypes structure)
+_POLICY_ARGS = struct.Struct("@PPii4qPPPPP4dPPP")
 
 
 class _Config(ctypes.Structure):
@@ -140,14 +134,14 @@ def load_library() -> ctypes.CDLL:
     L.adama_sgdm_fold.argtypes = [vp, vp, ci, vp, sz, vp]
     L.adama_sgdm_apply.argtypes = [vp, vp, vp, sz, dbl, dbl, vp]
     L.adama_coefficient_stats.argtypes = [vp, vp, vp, vp, vp, sz, vp, vp]
-    vpp, szp = ctypes.POINTER(vp), ctypes.POINTER(sz)
-    L.adama_fold_apply_multi.argtypes = [vp, vpp, ci, vpp, vpp, vpp, vpp, szp, ci, dbl, vp, vp]
-    L.adama_fold_apply8_multi.argtypes = [vp, vpp, ci, vpp, ctypes.POINTER(_State8), vpp, szp, ci, dbl, vp, vp]
-    L.adama_state8_pack_multi.argtypes = [vp, vpp, vpp, ctypes.POINTER(_State8), szp, ci, vp]
-    L.adama_state8_unpack_multi.argtypes = [vp, ctypes.POINTER(_State8), vpp, vpp, szp, ci, vp]
-    L.adama_grad_norm_multi.argtypes = [vp, vpp, ci, szp, ci, dbl, ci, vp, vp, vp]
+    # the lists of these calls are passed by address (TensorList.at, State8List.at)
+    L.adama_fold_apply_multi.argtypes = [vp, vp, ci, vp, vp, vp, vp, vp, ci, dbl, vp, vp]
+    L.adama_fold_apply8_multi.argtypes = [vp, vp, ci, vp, vp, vp, vp, ci, dbl, vp, vp]
+    L.adama_state8_pack_multi.argtypes = [vp, vp, vp, vp, vp, ci, vp]
+    L.adama_state8_unpack_multi.argtypes = [vp, vp, vp, vp, vp, ci, vp]
+    L.adama_grad_norm_multi.argtypes = [vp, vp, ci, vp, ci, dbl, ci, vp, vp, vp]
     L.adama_token_logprobs.argtypes = [vp, vp, ci, i64, i64, i64, vp, dbl, vp, vp, vp, vp]
-    L.adama_policy_loss.argtypes = [vp, ctypes.POINTER(_PolicyArgs), vp]
+    L.adama_policy_loss.argtypes = [vp, ctypes.c_char_p, vp]
     L.adama_get_step.argtypes = [vp]
     L.adama_get_step.restype = i64
     L.adama_set_step.argtypes = [vp, i64]
@@ -218,6 +212,7 @@ class TensorList:
         self.numels = [t.numel() for t in self.tensors]
         self.ns = (ctypes.c_size_t * len(self.tensors))(*self.numels)
         self.sizes = bytes(self.ns)  # for comparing lists of sizes at once
+        self.at, self.ns_at = ctypes.addressof(self.ptrs), ctypes.addressof(self.ns)
 
     def __len__(self):
         return len(self.tensors)
@@ -260,6 +255,7 @@ class State8List:
         self.numels = [s.numel for s in self.states]
         self.ns = (ctypes.c_size_t * len(self.states))(*self.numels)
         self.sizes = bytes(self.ns)
+        self.at, self.ns_at = ctypes.addressof(self.items), ctypes.addressof(self.ns)
 
     def __len__(self):
         return len(self.states)
@@ -563,6 +559,15 @@ class AdamA:
         return t.data_ptr()
 
     @staticmethod
+    def _list(x, dtype=None):
+        """x as a TensorList (of the dtype, where one is asked for)."""
+        if type(x) is not TensorList:
+            return TensorList(x, dtype)
+        if dtype is not None and x.dtype is not dtype:
+            raise TypeError(f"a list of {dtype} tensors is needed, got {x.dtype}")
+        return x
+
+    @staticmethod
     def _copies(w_bf16, ws):
         """Pointer array of the optional bf16 copies: None, or a list whose entries may be None."""
         if w_bf16 is None:
@@ -591,77 +596,70 @@ class AdamA:
             raise ValueError("grad_factor must hold one value")
         return _dev_ptr(grad_factor, torch.float32, "grad_factor")
 
+    @staticmethod
+    def _grad_dtype(grads) -> int:
+        dt = _DTYPES.get(grads.dtype)
+        if dt is None:
+            raise TypeError("grads must be float32 or bfloat16")
+        return dt
+
     def fold_apply_multi(self, ws, grads, ms, vs, lr: float, w_bf16=None,
                          grad_factor: Optional[torch.Tensor] = None) -> None:
         """adama_fold_apply_multi: the mini-batch's last gradient and the update in one pass over
         lists of tensors (or TensorList objects).  `w_bf16` (list, entries may be None) receives
         the weights as bf16; `grad_factor` is one fp32 on the device (NaN skips the step)."""
-        ws = ws if isinstance(ws, TensorList) else TensorList(ws, torch.float32)
-        grads = grads if isinstance(grads, TensorList) else TensorList(grads)
-        ms = ms if isinstance(ms, TensorList) else TensorList(ms, torch.float32)
-        vs = vs if isinstance(vs, TensorList) else TensorList(vs, torch.float32)
+        ws, grads = self._list(ws, torch.float32), self._list(grads)
+        ms, vs = self._list(ms, torch.float32), self._list(vs, torch.float32)
         if not ws.sizes == grads.sizes == ms.sizes == vs.sizes:
             raise ValueError("w, grad, m, v must be lists of equal sizes")
-        for t in (ws, ms, vs):
-            if t.dtype != torch.float32:
-                raise TypeError("w, m, v must be float32")
-        if grads.dtype not in _DTYPES:
-            raise TypeError("grads must be float32 or bfloat16")
+        copies = self._copies(w_bf16, ws)
         self._check(self._L.adama_fold_apply_multi(
-            self._h, grads.ptrs, _DTYPES[grads.dtype], ws.ptrs, ms.ptrs, vs.ptrs,
-            self._copies(w_bf16, ws), ws.ns, len(ws), float(lr), self._factor(grad_factor),
-            _stream_ptr(self.device)))
+            self._h, grads.at, self._grad_dtype(grads), ws.at, ms.at, vs.at, copies, ws.ns_at, len(ws.tensors), lr,
+            self._factor(grad_factor), _stream_ptr(self.device)))
 
     def fold_apply8_multi(self, ws, grads, states, lr: float, w_bf16=None,
                           grad_factor: Optional[torch.Tensor] = None) -> None:
         """adama_fold_apply8_multi: the same with moments in 8 bits (a list of State8, or a
         State8List).  For one gradient per mini-batch; see include/adama.h."""
-        ws = ws if isinstance(ws, TensorList) else TensorList(ws, torch.float32)
-        grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+        ws, grads = self._list(ws, torch.float32), self._list(grads)
         states = states if isinstance(states, State8List) else State8List(states)
         if not ws.sizes == grads.sizes == states.sizes:
             raise ValueError("w, grad, states must be lists of equal sizes")
-        if ws.dtype != torch.float32:
-            raise TypeError("w must be float32")
-        if grads.dtype not in _DTYPES:
-            raise TypeError("grads must be float32 or bfloat16")
+        copies = self._copies(w_bf16, ws)
         self._check(self._L.adama_fold_apply8_multi(
-            self._h, grads.ptrs, _DTYPES[grads.dtype], ws.ptrs, states.items,
-            self._copies(w_bf16, ws), ws.ns, len(ws), float(lr), self._factor(grad_factor),
-            _stream_ptr(self.device)))
+            self._h, grads.at, self._grad_dtype(grads), ws.at, states.at, copies, ws.ns_at, len(ws.tensors), lr,
+            self._factor(grad_factor), _stream_ptr(self.device)))
 
-    def _state8_convert(self, fn, states, ms, vs, pack: bool) -> None:
+    def _state8_lists(self, states, ms, vs):
         states = states if isinstance(states, State8List) else State8List(states)
-        ms = ms if isinstance(ms, TensorList) else TensorList(ms, torch.float32)
-        vs = vs if isinstance(vs, TensorList) else TensorList(vs, torch.float32)
+        ms, vs = self._list(ms, torch.float32), self._list(vs, torch.float32)
         if not states.sizes == ms.sizes == vs.sizes:
             raise ValueError("states, m, v must be lists of equal sizes")
-        if ms.dtype != torch.float32 or vs.dtype != torch.float32:
-            raise TypeError("m, v must be float32")
-        lists = (ms.ptrs, vs.ptrs, states.items) if pack else (states.items, ms.ptrs, vs.ptrs)
-        self._check(fn(self._h, *lists, states.ns, len(states), _stream_ptr(self.device)))
+        return states, ms, vs
 
     def state8_pack_multi(self, ms, vs, states) -> None:
         """adama_state8_pack_multi: fp32 moments into 8-bit states."""
-        self._state8_convert(self._L.adama_state8_pack_multi, states, ms, vs, True)
+        states, ms, vs = self._state8_lists(states, ms, vs)
+        self._check(self._L.adama_state8_pack_multi(self._h, ms.at, vs.at, states.at, states.ns_at,
+                                                    len(states.states), _stream_ptr(self.device)))
 
     def state8_unpack_multi(self, states, ms, vs) -> None:
         """adama_state8_unpack_multi: the fp32 values that 8-bit states stand for."""
-        self._state8_convert(self._L.adama_state8_unpack_multi, states, ms, vs, False)
+        states, ms, vs = self._state8_lists(states, ms, vs)
+        self._check(self._L.adama_state8_unpack_multi(self._h, states.at, ms.at, vs.at, states.ns_at,
+                                                      len(states.states), _stream_ptr(self.device)))
 
     def grad_norm_multi(self, grads, max_norm: float, out: torch.Tensor, accumulate: bool = False) -> None:
         """adama_grad_norm_multi: `out` (4 fp32 on the device) receives norm in out[0], the clip
         factor in out[1] (the grad_factor of a step: out[1:2]) and the sum of squares as a float64
         in out[2:4]."""
-        grads = grads if isinstance(grads, TensorList) else TensorList(grads)
-        if grads.dtype not in _DTYPES:
-            raise TypeError("grads must be float32 or bfloat16")
+        grads = self._list(grads)
         if out.numel() != 4 or not out.is_contiguous():
             raise ValueError("out must hold 4 contiguous float32 values")
         stream = _stream_ptr(self.device)
         self._check(self._L.adama_grad_norm_multi(
-            self._h, grads.ptrs, _DTYPES[grads.dtype], grads.ns, len(grads), float(max_norm),
-            int(accumulate), _dev_ptr(out, torch.float32, "out"), self._workspace(stream), stream))
+            self._h, grads.at, self._grad_dtype(grads), grads.ns_at, len(grads.tensors), max_norm, int(accumulate),
+            _dev_ptr(out, torch.float32, "out"), self._workspace(stream), stream))
 
     @staticmethod
     def _rows(t: torch.Tensor, name: str):
@@ -679,7 +677,7 @@ class AdamA:
     @staticmethod
     def _per_row(t: Optional[torch.Tensor], rows: int, name: str, dtype=torch.float32):
         if t is None:
-            return None
+            return 0
         if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == rows:
             return t.data_ptr()
         _dev_ptr(t, dtype, name)
@@ -706,21 +704,21 @@ class AdamA:
         weighted by `weights`; `dlogits` (fp32 or bf16, `logits` itself, or None) the gradient."""
         ptr, dt, ld = self._rows(logits, "logits")
         rows, vocab = logits.shape
-        dptr, ddt, dld = None, dt, 0
+        dptr, ddt, dld = 0, dt, 0
         if dlogits is not None:
-            if tuple(dlogits.shape) != (rows, vocab):
+            if dlogits.shape != logits.shape:
                 raise ValueError("dlogits must have the shape of logits")
             dptr, ddt, dld = self._rows(dlogits, "dlogits")
         if stats.numel() != 4 or not stats.is_contiguous():
             raise ValueError("stats must hold 4 contiguous float32 values")
         stream = _stream_ptr(self.device)
-        args = _PolicyArgs(
-            ptr, dptr, dt, ddt, rows, vocab, ld, dld, self._per_row(targets, rows, "targets", torch.int64),
-            self._per_row(old_logp, rows, "old_logp"), self._per_row(ref_logp, rows, "ref_logp"),
-            self._per_row(advantages, rows, "advantages"), self._per_row(weights, rows, "weights"),
-            float(logit_scale), float(clip_low), float(clip_high), float(kl_coef),
-            self._per_row(logp, rows, "logp"), _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream))
-        self._check(self._L.adama_policy_loss(self._h, ctypes.byref(args), stream))
+        row = self._per_row
+        args = _POLICY_ARGS.pack(
+            ptr, dptr, dt, ddt, rows, vocab, ld, dld, row(targets, rows, "targets", torch.int64),
+            row(old_logp, rows, "old_logp"), row(ref_logp, rows, "ref_logp"), row(advantages, rows, "advantages"),
+            row(weights, rows, "weights"), logit_scale, clip_low, clip_high, kl_coef, row(logp, rows, "logp"),
+            _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream))
+        self._check(self._L.adama_policy_loss(self._h, args, stream))
 
     # -- host-buffer variants ---------------------------------------------------------------
     def fold_host(self, grad_host: torch.Tensor, m: torch.Tensor, v: torch.Tensor,

@@ -117,6 +117,7 @@ struct Workspace {
 static_assert(sizeof(Workspace) == ADAMA_WORKSPACE_BYTES, "as the header states");
 
 // gradient norm over a list (grad_norm.cu)
+constexpr int kNormMid = 256;
 constexpr int kNormMax = 1024;
 cudaError_t launch_grad_norm(const void *const *g, adama_dtype gdt, const size_t *n, int count,
                              float max_norm, int accumulate, adama_grad_norm *out, void *workspace,

@@ -313,6 +313,23 @@ def test_rows_with_infinite_entries_and_masked_rows_of_nan():
         assert abs(float(d[i].double().sum())) <= 3e-2 * float(d[i].double().abs().sum())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,V", [(3, 100), (2, 3001), (2, 40_003), (200, 20_001), (2, 131_074)])
+def test_rows_at_the_lowest_value_are_uniform(T, V, dtype):
+    """A row that a mask has set to the type's lowest value throughout is a uniform one."""
+    opt = adama.AdamA()
+    x = torch.full((T, V), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+    targets = torch.arange(T, device="cuda") % V
+    logp, lse, ent = (torch.empty(T, device="cuda") for _ in range(3))
+    opt.token_logprobs(x, targets, logp, lse=lse, entropy=ent)
+    assert float((logp + math.log(V)).abs().max()) <= LOGP and float((ent - math.log(V)).abs().max()) <= 10 * LOGP
+    one, d, stats = torch.ones(T, device="cuda"), torch.empty(T, V, dtype=dtype, device="cuda"), torch.empty(4, device="cuda")
+    opt.policy_loss(x, targets, logp, one, one, d, stats)
+    want = torch.full((T, V), 1.0 / V, dtype=torch.float64, device="cuda")
+    want[torch.arange(T, device="cuda"), targets] -= 1
+    assert bool(((d.double() - want).abs() <= GRAD * want.abs() + HALF_ULP[dtype] * want.abs()).all())
+
+
 def test_large_logits_saturate_without_overflow():
     opt = adama.AdamA()
     T, V = 3, 300
