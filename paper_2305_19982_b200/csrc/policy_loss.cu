@@ -360,87 +360,75 @@ struct RowWriter {
     }
 };
 
-// ---- rows that fit a few warps' registers ------------------------------------------------------
+// ---- rows that fit a warp's registers -----------------------------------------------------------
 
-constexpr int kRowUnits = 8;  // units of a thread: rows of up to 4 KB to a warp, 16 KB to four
+// One row at a time to a warp, 32 warps to an SM hide its latencies: 100000 x 2000 bf16 150 us (73 % of a
+// copy's rate), 333333 x 600 262 us (42 %), where a row's loss terms cost more than its elements.
+constexpr int kRowUnits = 8;  // units of a lane: rows of up to 4 KB
 
-// One row at a time per group, several groups to an SM hide its latencies: 12500 x 8000 bf16 80 us = 4.4
-// TB/s, 200000 x 500 150 us, where a row's joins and loss terms cost more than its elements.
-
-template <typename T, typename O, int W>
+template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 2)
 policy_loss_rows_kernel(const PolicyArgs a, float k) {
-    constexpr int kGroupThreads = 32 * W, kGroups = kWarps / W;
-    __shared__ Stats shared[kWarps];
     __shared__ double sums[kWarps][4];
     __shared__ int last;
-    const int g = threadIdx.x / kGroupThreads, t = threadIdx.x % kGroupThreads;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     Sums acc;
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + g; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
+    for (int64_t row = (int64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (int64_t)gridDim.x * kWarps) {
         const RowIn in = row_in(a, row);
-        const bool live = in.live();
+        O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+        if (!in.live()) {
+            if (lane == 0 && a.logp) a.logp[row] = 0.f;
+            if (a.dlogits) fill_zeros(y, a.vocab, lane, 32);
+            continue;
+        }
         const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
         const RowShape shape = row_shape(x, (int)a.vocab);
         const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
-        const bool has_extra = t < shape.head + shape.tail;
-        const int extra = has_extra ? extra_index<T>(shape, t) : 0;
+        const bool has_extra = lane < shape.head + shape.tail, inside = in.target < a.vocab;
+        const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
+        const float x_target = inside ? widen(x[in.target]) : CUDART_NAN_F;
         uint4 u[kRowUnits];
-        float x_extra = 0.f, x_target = CUDART_NAN_F, top = 0.f;
-        RowOut o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live) {
-            const bool inside = in.target < a.vocab;
-            if (inside) x_target = widen(x[in.target]);
+#pragma unroll
+        for (int i = 0; i < kRowUnits; ++i)
+            if (lane + 32 * i < shape.units) u[i] = ld_unit(body + lane + 32 * i);
+        const float x_extra = has_extra ? widen(x[extra]) : 0.f;
+        Running<false> run;
+#pragma unroll
+        for (int i = 0; i < kRowUnits; ++i) {
+            if (lane + 32 * i < shape.units) {
+                const uint4 one[1] = {u[i]};
+                run.template add_units<T>(one, k);
+            }
+        }
+        if (has_extra) run.add_one(x_extra, k);
+        // the gradient may replace the logits: every lane has read its own when the join is through
+        const Stats s = warp_join<false>(run.stats(), k);
+        const RowOut o = row_out(a, in, s, x_target);
+        if (lane == 0) {
+            acc.add(a, in, o);
+            if (!inside) record_bad_target(a.status, row);
+            if (a.logp) a.logp[row] = o.logp;
+        }
+        if (!a.dlogits) continue;
+        const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
+        O *p = y + shape.head + lane * kUnit<T>;
+        if (out.shift == 0) {
 #pragma unroll
             for (int i = 0; i < kRowUnits; ++i)
-                if (t + i * kGroupThreads < shape.units) u[i] = ld_unit(body + t + i * kGroupThreads);
-            if (has_extra) x_extra = widen(x[extra]);
-            Running<false> run;
+                if (lane + 32 * i < shape.units) out.put(u[i], p + 32 * i * kUnit<T>);
+        } else {
 #pragma unroll
             for (int i = 0; i < kRowUnits; ++i) {
-                if (t + i * kGroupThreads < shape.units) {
-                    const uint4 one[1] = {u[i]};
-                    run.template add_units<T>(one, k);
-                }
-            }
-            if (has_extra) run.add_one(x_extra, k);
-            // the gradient may replace the logits: all have been read when the join is through
-            const Stats s = group_join<W, false>(run.stats(), k, shared + g * W, g);
-            top = s.top;
-            o = row_out(a, in, s, x_target);
-            if (t == 0) {
-                acc.add(a, in, o);
-                if (!inside) record_bad_target(a.status, row);
+                const int at = lane + 32 * i;
+                if (at < shape.units)
+                    out.put_shifted(u[i], ld_unit(body + (at + 1 < shape.units ? at + 1 : at)), p + 32 * i * kUnit<T>, at == 0,
+                                    at + 1 == shape.units);
             }
         }
-        if (t == 0 && a.logp) a.logp[row] = o.logp;
-        if (a.dlogits) {
-            O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
-            if (live) {
-                const RowWriter<T, O> out(y, shape, top, o.unit, o.per_e, k);
-                O *p = y + shape.head + t * kUnit<T>;
-                if (out.shift == 0) {
-#pragma unroll
-                    for (int i = 0; i < kRowUnits; ++i)
-                        if (t + i * kGroupThreads < shape.units) out.put(u[i], p + i * kGroupThreads * kUnit<T>);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kRowUnits; ++i) {
-                        const int at = t + i * kGroupThreads;
-                        if (at < shape.units)
-                            out.put_shifted(u[i], ld_unit(body + (at + 1 < shape.units ? at + 1 : at)),
-                                            p + i * kGroupThreads * kUnit<T>, at == 0, at + 1 == shape.units);
-                    }
-                }
-                if (has_extra) y[extra] = out.value(x_extra, extra == in.target);
-                if (in.target < a.vocab && t == out.writer_of(shape, in.target, 0, shape.units, kGroupThreads))
-                    y[in.target] = out.value(x_target, true);
-            } else {
-                fill_zeros(y, a.vocab, t, kGroupThreads);
-            }
-        }
-        if (W > 1) group_sync<W>(g);  // the slots are used again
+        if (has_extra) y[extra] = out.value(x_extra, extra == in.target);
+        if (inside && lane == out.writer_of(shape, in.target, 0, shape.units, 32)) y[in.target] = out.value(x_target, true);
     }
-    finish_stats<kThreads, 32 * W>(a, acc, sums, &last, threadIdx.x);
+    finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x);
 }
 
 // ---- longer rows: a ring in shared memory ------------------------------------------------------
@@ -454,14 +442,13 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
 
 // How the ring is cut: WORK threads compute, a stage holds two units of each.  A stage that a row fills
 // in part costs nearly as much as a full one, so a launch takes the cut that fills better.
-template <int WORK, int STAGES>
+template <int WORK, int STAGES, int PER_SM>
 struct RingCut {
-    static constexpr int kWork = WORK, kStages = STAGES;
+    static constexpr int kWork = WORK, kStages = STAGES, kPerSm = PER_SM;
     static constexpr int kEach = 2;                              // units of a stage that a thread takes
     static constexpr int kWarps = WORK / 32, kThreads = WORK + 64;
     static constexpr int kProducerWarp = kWarps, kScalarWarp = kWarps + 1;
     static constexpr int kStageUnits = kEach * WORK, kStageBytes = 16 * kStageUnits;
-    static constexpr int kRingUnits = STAGES * kStageUnits;
     static constexpr int kSliceUnits = STAGES / 2 * kStageUnits;  // largest slice of which two fit
 
     // stages of a slice times their units, in percent of the slice
@@ -469,8 +456,14 @@ struct RingCut {
         return (int)((slice + kStageUnits - 1) / kStageUnits * kStageUnits * 100 / slice);
     }
 };
-using Cut512 = RingCut<512, 14>;  // 14 x 16 KB: slices of up to 7168 units
-using Cut640 = RingCut<640, 11>;  // 11 x 20 KB: up to 6400
+// The shorter the slice, the fewer threads to it and the more CTAs to an SM: a row's joins and barriers
+// then cost fewer warps, and other rows' work hides its latencies (24390 x 8200 bf16: 238 us with 512
+// threads, 160 with 256, 132 with 128; 48828 x 4096: 149 with 128, 131 with 64).
+using Cut640 = RingCut<640, 11, 1>;  // 11 stages of 20 KB: slices of up to 6400 units
+using Cut512 = RingCut<512, 14, 1>;  // 14 of 16 KB: 7168
+using Cut256 = RingCut<256, 13, 2>;  // 13 of 8 KB: 3072
+using Cut128 = RingCut<128, 13, 4>;  // 13 of 4 KB: 1536
+using Cut64 = RingCut<64, 13, 8>;    // 13 of 2 KB: 768
 
 // What the gradient of a row needs.
 struct Verdict {
@@ -491,6 +484,10 @@ struct RingShared {
     int last, give_up;
 };
 static_assert(sizeof(RingShared<Cut512>) + 128 <= 232448 && sizeof(RingShared<Cut640>) + 128 <= 232448, "shared memory of a CTA");
+static_assert(2 * (sizeof(RingShared<Cut256>) + 128 + 1024) <= 233472 &&
+                  4 * (sizeof(RingShared<Cut128>) + 128 + 1024) <= 233472 &&
+                  8 * (sizeof(RingShared<Cut64>) + 128 + 1024) <= 233472,
+              "shared memory of an SM");
 
 // Place in the ring: a stage, and the parity of the barrier phase that its current use completes.
 template <int STAGES>
@@ -512,7 +509,7 @@ __device__ __forceinline__ Stats join2(const Stats &a, const Stats &b, float k) 
 }
 
 template <typename T, typename O, typename Cut>
-__global__ void __launch_bounds__(Cut::kThreads, 1)
+__global__ void __launch_bounds__(Cut::kThreads, Cut::kPerSm)
 policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
     constexpr int kStages = Cut::kStages, kStageUnits = Cut::kStageUnits, kRingWork = Cut::kWork, kEach = Cut::kEach;
     extern __shared__ unsigned char raw[];
@@ -887,10 +884,9 @@ cudaError_t logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
     return cluster > 1 ? logprobs_cluster<T>(a, k, cluster, stream) : logprobs_groups<T, kWarps, 1>(a, k, stream);
 }
 
-template <typename T, typename O, int W>
+template <typename T, typename O>
 cudaError_t policy_rows(const PolicyArgs &a, float k, int sm_count, cudaStream_t stream) {
-    const int64_t ctas = (a.rows + kWarps / W - 1) / (kWarps / W);
-    policy_loss_rows_kernel<T, O, W><<<grid_of(ctas, (int64_t)sm_count * 2), kThreads, 0, stream>>>(a, k);
+    policy_loss_rows_kernel<T, O><<<grid_of((a.rows + kWarps - 1) / kWarps, (int64_t)sm_count * 2), kThreads, 0, stream>>>(a, k);
     return cudaGetLastError();
 }
 
@@ -921,7 +917,7 @@ struct RingLaunch {
     // its share of the rows to the end.  Asked for once per device.
     static cudaError_t resident(int cluster, int sm_count, int *out) {
         static std::atomic<int> known[64][4];
-        *out = sm_count;
+        *out = sm_count * Cut::kPerSm;
         if (cluster == 1) return cudaSuccess;
         int device = 0;
         cudaError_t e = cudaGetDevice(&device);
@@ -931,7 +927,7 @@ struct RingLaunch {
         if (m == 0) {
             e = prepare();
             if (e != cudaSuccess) return e;
-            RingLaunch l(cluster, sm_count / cluster, nullptr);
+            RingLaunch l(cluster, sm_count * Cut::kPerSm / cluster, nullptr);
             e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O, Cut>, &l.cfg);
             if (e != cudaSuccess) return e;
             if (m < 1) m = 1;
@@ -954,11 +950,10 @@ template <typename T, typename O>
 cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
     const float k = (float)(a.scale_exact * kLog2e);
     const int64_t units = a.vocab / kUnit<T>;
-    if (units <= 32 * kRowUnits) return policy_rows<T, O, 1>(a, k, sm_count, stream);
-    if (units <= 128 * kRowUnits) return policy_rows<T, O, 4>(a, k, sm_count, stream);
+    if (units <= 32 * kRowUnits) return policy_rows<T, O>(a, k, sm_count, stream);
     // As few CTAs to a row as hold two of its slices.  Few rows are dealt out at once, one to a cluster as
-    // large as that allows, which then has to hold one slice (33 x 131072 fp32: 8.9 us with 4 CTAs to a
-    // row, 10.9 with 8 in three turns).
+    // large as that and the row's length allow, which then has to hold one slice (33 x 131072 fp32: 8.9 us
+    // with 4 CTAs to a row, 10.9 with 8 in three turns).
     using Ring = RingLaunch<T, O, Cut512>;
     int cluster = 1;
     while (cluster < kMaxCluster && (units + cluster - 1) / cluster > Cut512::kSliceUnits) cluster *= 2;
@@ -967,14 +962,20 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
         int most = 0;
         const cudaError_t e = a.rows * c <= sm_count ? Ring::resident(c, sm_count, &most) : cudaSuccess;
         if (e != cudaSuccess) return e;
-        if (a.rows <= most && (units + c - 1) / c <= Cut640::kRingUnits) {
+        if (a.rows <= most && (units + c - 1) / c <= Cut640::kStages * Cut640::kStageUnits && (c == 1 || units >= (int64_t)c * Cut512::kWork)) {
             cluster = c;
             one_turn = true;
         }
     }
-    // 8192 x 50257 bf16 (6282 units, 114 % against 102 %): 260 and 256 us, with odd pitches 159 and 146;
-    // 8192 x 32000 (4000 units, 102 % against 128 %): 158 and 175 us.  On a tie the deeper ring.
     const int64_t slice = (units + cluster - 1) / cluster;
+    if (!one_turn && slice <= Cut64::kSliceUnits) return RingLaunch<T, O, Cut64>::launch(a, k, 1, sm_count, stream);
+    if (!one_turn && slice <= Cut128::kSliceUnits) return RingLaunch<T, O, Cut128>::launch(a, k, 1, sm_count, stream);
+    // (only whole rows: the halves of 6250 x 32000 in clusters take 129 us, whole rows with Cut512 123)
+    if (!one_turn && cluster == 1 && slice <= Cut256::kSliceUnits)
+        return RingLaunch<T, O, Cut256>::launch(a, k, 1, sm_count, stream);
+    // The two cuts of a whole SM: 8192 x 50257 bf16 (6282 units, 114 % against 102 %) 260 and 256 us, 4096 of
+    // them with odd pitches 159 and 146; 8192 x 32000 (4000 units, 102 % against 128 %) 158 and 175 us.  On a
+    // tie the deeper ring.
     if ((one_turn || slice <= Cut640::kSliceUnits) && Cut640::fill_cost(slice) < Cut512::fill_cost(slice))
         return RingLaunch<T, O, Cut640>::launch(a, k, cluster, sm_count, stream);
     if (one_turn || slice <= Cut512::kSliceUnits) return Ring::launch(a, k, cluster, sm_count, stream);

@@ -198,7 +198,7 @@ def test_policy_loss_and_gradient(T, V, dtype, out, pitch, offset, scale, ref):
         assert torch.equal(stats, second) and torch.equal(x, d)
 
 
-LONG = [(160, 16_385), (150, 51_200), (150, 51_203), (160, 57_345), (152, 65_537), (80, 131_073), (2, 229_381), (2, 458_760), (3, 459_001), (2, 460_001), (1, 920_003)]
+LONG = [(1300, 5_003), (700, 9_001), (400, 20_001), (160, 16_385), (150, 51_200), (150, 51_203), (160, 57_345), (152, 65_537), (80, 131_073), (2, 229_381), (2, 458_760), (3, 459_001), (2, 460_001), (1, 920_003)]
 
 
 @pytest.mark.parametrize("dtype,out", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32)])
