@@ -440,8 +440,7 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
 // which one warp of its own does meanwhile, and nobody waits for them.  The ring therefore holds two
 // rows (slices).  One more warp issues the copies.
 
-// How the ring is cut: WORK threads compute, a stage holds two units of each.  A stage that a row fills
-// in part costs nearly as much as a full one, so a launch takes the cut that fills better.
+// How the ring is cut: WORK threads compute, a stage holds two units of each, PER_SM such CTAs share an SM.
 template <int WORK, int STAGES, int PER_SM>
 struct RingCut {
     static constexpr int kWork = WORK, kStages = STAGES, kPerSm = PER_SM;
@@ -917,7 +916,8 @@ struct RingLaunch {
     // its share of the rows to the end.  Asked for once per device.
     static cudaError_t resident(int cluster, int sm_count, int *out) {
         static std::atomic<int> known[64][4];
-        *out = sm_count * Cut::kPerSm;
+        const int most = kWorkspaceParts / 4;  // each CTA's sums have a place there
+        *out = sm_count * Cut::kPerSm < most ? sm_count * Cut::kPerSm : most;
         if (cluster == 1) return cudaSuccess;
         int device = 0;
         cudaError_t e = cudaGetDevice(&device);
@@ -962,7 +962,8 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
         int most = 0;
         const cudaError_t e = a.rows * c <= sm_count ? Ring::resident(c, sm_count, &most) : cudaSuccess;
         if (e != cudaSuccess) return e;
-        if (a.rows <= most && (units + c - 1) / c <= Cut640::kStages * Cut640::kStageUnits && (c == 1 || units >= (int64_t)c * Cut512::kWork)) {
+        const bool fits = (units + c - 1) / c <= Cut640::kStages * Cut640::kStageUnits;
+        if (a.rows <= most && fits && (c == 1 || units >= (int64_t)c * Cut512::kWork)) {
             cluster = c;
             one_turn = true;
         }
@@ -973,9 +974,10 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
     // (only whole rows: the halves of 6250 x 32000 in clusters take 129 us, whole rows with Cut512 123)
     if (!one_turn && cluster == 1 && slice <= Cut256::kSliceUnits)
         return RingLaunch<T, O, Cut256>::launch(a, k, 1, sm_count, stream);
-    // The two cuts of a whole SM: 8192 x 50257 bf16 (6282 units, 114 % against 102 %) 260 and 256 us, 4096 of
-    // them with odd pitches 159 and 146; 8192 x 32000 (4000 units, 102 % against 128 %) 158 and 175 us.  On a
-    // tie the deeper ring.
+    // The two cuts of a whole SM: a stage that a row fills in part costs nearly as much as a full one, so the
+    // cut that fills better: 8192 x 50257 bf16 (6282 units, 114 % with Cut512, 102 % with Cut640) 260 and
+    // 256 us, 4096 of them with odd pitches 159 and 146; 8192 x 32000 (4000 units, 102 % and 128 %) 158 and
+    // 175 us.  On a tie the deeper ring.
     if ((one_turn || slice <= Cut640::kSliceUnits) && Cut640::fill_cost(slice) < Cut512::fill_cost(slice))
         return RingLaunch<T, O, Cut640>::launch(a, k, cluster, sm_count, stream);
     if (one_turn || slice <= Cut512::kSliceUnits) return Ring::launch(a, k, cluster, sm_count, stream);
