@@ -2,7 +2,7 @@
 // device for the step that multiplies by it.  One pass, 2 or 4 B/element; each CTA's sum goes to
 // the workspace as a double, the last CTA to finish adds them in the CTAs' order, so that the
 // result does not depend on scheduling.  Bound by HBM: 369 M bf16 gradients take 107.9 us = 6.84 TB/s
-// (reads alone run above a copy's rate); 150 short tensors 6 us, two dependent reductions.
+// (reads alone run above a copy's rate); 150 short tensors 4.9 us, two dependent reductions.
 #include "softmax_rows.cuh"
 #include "tensor_table.cuh"
 
@@ -11,9 +11,10 @@ namespace {
 
 constexpr int kThreads = 256;
 // 4 CTAs per SM with 8 units of each thread in flight: 369 M bf16 gradients take 107.7 us (6.85 TB/s);
-// 4 x 4 109.3, 8 x 4 111.6, 2 x 8 109.4, 2 x 16 106.3 but 8.4 instead of 5.7 us for short lists.
+// 4 x 4 109.3, 8 x 4 111.6, 2 x 8 109.4, 2 x 16 106.3 but 8.4 instead of 5.7 us for short lists.  Lists of
+// 16 M elements (50 MB and less) want the bytes in flight most: 10.7 us with 8 units, 14.1 with 2.
 constexpr int kCtasPerSm = 4;
-constexpr int kLongUnits = 8, kShortUnits = 2;
+constexpr int kUnits = 8;
 
 template <int CAP>
 struct NormTable {
@@ -35,12 +36,12 @@ __device__ __forceinline__ double block_sum(double x, double *shared) {
     return sum;
 }
 
-// A chunk is UNITS 16-byte units of each thread, all loaded before the first is used.
-template <typename G, int UNITS, int CAP>
+// A chunk is kUnits 16-byte units of each thread, all loaded before the first is used.
+template <typename G, int CAP>
 __global__ void __launch_bounds__(kThreads)
 grad_norm_kernel(const __grid_constant__ NormTable<CAP> tab, float max_norm, int accumulate,
                  adama_grad_norm *out, Workspace *ws) {
-    constexpr int kVec = 16 / sizeof(G), kNormChunk = UNITS * kThreads * kVec;
+    constexpr int kVec = 16 / sizeof(G), kNormChunk = kUnits * kThreads * kVec;
     __shared__ double shared[kThreads / 32];
     __shared__ bool last;
     const unsigned total = tab.chunk_start[tab.count];
@@ -54,9 +55,9 @@ grad_norm_kernel(const __grid_constant__ NormTable<CAP> tab, float max_norm, int
         const size_t head = mis ? kVec - mis : 0;  // chunk c covers [head + c*kNormChunk, ...), the first one the head too
         const size_t base = head + first + (size_t)threadIdx.x * kVec;
         float part = 0.f;
-        uint4 u[UNITS];
+        uint4 u[kUnits];
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
+        for (int i = 0; i < kUnits; ++i) {
             u[i] = make_uint4(0, 0, 0, 0);
             if (base + (size_t)i * kThreads * kVec + kVec <= n)
                 u[i] = ld_unit_ro(reinterpret_cast<const uint4 *>(g + base + (size_t)i * kThreads * kVec));
@@ -65,16 +66,15 @@ grad_norm_kernel(const __grid_constant__ NormTable<CAP> tab, float max_norm, int
             const float x = widen(g[threadIdx.x]);
             part = fmaf(x, x, part);
         }
-        if (base + kNormChunk > n) {  // the unit that the tensor's end cuts, if it is one of this thread's
-            const size_t end = n > head ? head + (n - head) / kVec * kVec : n;
-            if (end >= base && (end - base) % (kThreads * kVec) == 0)
-                for (size_t j = end; j < n; ++j) {
-                    const float x = widen(g[j]);
-                    part = fmaf(x, x, part);
-                }
+        if (first + kNormChunk >= n && n > head) {  // the tensor's last chunk: what its end cuts off a unit
+            const size_t j = head + (n - head) / kVec * kVec + threadIdx.x;
+            if (j < n) {
+                const float x = widen(g[j]);
+                part = fmaf(x, x, part);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
+        for (int i = 0; i < kUnits; ++i) {
             Pair p = 0;
 #pragma unroll
             for (int q = 0; q < kVec / 2; ++q) {
@@ -109,32 +109,18 @@ grad_norm_kernel(const __grid_constant__ NormTable<CAP> tab, float max_norm, int
     }
 }
 
-template <typename G, int UNITS, int CAP>
-cudaError_t launch_kernel(NormTable<CAP> &tab, const size_t *n, int count, float max_norm, int accumulate,
-                          adama_grad_norm *out, Workspace *ws, int sm_count, cudaStream_t stream) {
-    const unsigned chunks = fill_chunks(tab.n, tab.chunk_start, n, count, UNITS * kThreads * 16 / sizeof(G));
-    unsigned cap = (unsigned)(sm_count * kCtasPerSm);
-    if (cap > kWorkspaceParts) cap = kWorkspaceParts;
-    const unsigned grid = chunks == 0 ? 1 : chunks < cap ? chunks : cap;
-    grad_norm_kernel<G, UNITS, CAP><<<grid, kThreads, 0, stream>>>(tab, max_norm, accumulate, out, ws);
-    return cudaGetLastError();
-}
-
 template <typename G, int CAP>
 cudaError_t launch(const void *const *g, const size_t *n, int count, float max_norm, int accumulate,
                    adama_grad_norm *out, Workspace *ws, int sm_count, cudaStream_t stream) {
     NormTable<CAP> tab;
-    size_t all = 0;
-    for (int i = 0; i < count; ++i) {
-        tab.g[i] = g[i];
-        all += n[i];
-    }
+    for (int i = 0; i < count; ++i) tab.g[i] = g[i];
     tab.count = count;
-    // long chunks where every CTA has several of them, else as many CTAs as there is work for
-    const size_t several = (size_t)kLongUnits * kThreads * 16 / sizeof(G) * (size_t)sm_count * kCtasPerSm * 4;
-    return all >= several
-               ? launch_kernel<G, kLongUnits, CAP>(tab, n, count, max_norm, accumulate, out, ws, sm_count, stream)
-               : launch_kernel<G, kShortUnits, CAP>(tab, n, count, max_norm, accumulate, out, ws, sm_count, stream);
+    const unsigned chunks = fill_chunks(tab.n, tab.chunk_start, n, count, kUnits * kThreads * 16 / sizeof(G));
+    unsigned cap = (unsigned)(sm_count * kCtasPerSm);
+    if (cap > kWorkspaceParts) cap = kWorkspaceParts;
+    const unsigned grid = chunks == 0 ? 1 : chunks < cap ? chunks : cap;
+    grad_norm_kernel<G, CAP><<<grid, kThreads, 0, stream>>>(tab, max_norm, accumulate, out, ws);
+    return cudaGetLastError();
 }
 
 template <typename G>

@@ -195,10 +195,10 @@ struct Sums {
 };
 
 // The leaders' sums -> the CTA's in the workspace -> stats, by the last CTA, in the CTAs' order.  All
-// THREADS call it; thread LEADER*i holds the sums of leader i.
+// THREADS call it; thread LEADER*i holds the sums of leader i.  CTA `index` of `count` that have sums.
 template <int THREADS, int LEADER>
 __device__ __forceinline__ void finish_stats(const PolicyArgs &a, const Sums &s, double (*slots)[4], volatile int *last,
-                                             int t) {
+                                             int t, unsigned index, unsigned count) {
     static_assert(THREADS / 32 <= kWarps, "slots");
     constexpr int kLeaders = THREADS / LEADER;
     Workspace *ws = static_cast<Workspace *>(a.workspace);
@@ -210,22 +210,22 @@ __device__ __forceinline__ void finish_stats(const PolicyArgs &a, const Sums &s,
     double sum = 0.0;
     if (t < 4) {
         for (int w = 0; w < kLeaders; ++w) sum += slots[w][t];
-        if (gridDim.x == 1) a.stats[t] = (float)sum;
+        if (count == 1) a.stats[t] = (float)sum;
     }
-    if (gridDim.x == 1) return;
+    if (count == 1) return;
     if (t < 32) {
         if (t < 4) {
-            ws->part[4 * blockIdx.x + t] = sum;
+            ws->part[4 * index + t] = sum;
             __threadfence();
         }
         __syncwarp();
-        if (t == 0) *last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
+        if (t == 0) *last = atomicAdd(&ws->ticket, 1u) == count - 1;
     }
     sync();
     if (!*last) return;
     __threadfence();
     sum = 0.0;  // threads of one remainder mod 4 add up the same of the four sums
-    for (unsigned i = t; i < 4 * gridDim.x; i += THREADS) sum += __ldcg(&ws->part[i]);
+    for (unsigned i = t; i < 4 * count; i += THREADS) sum += __ldcg(&ws->part[i]);
     for (int o = 16; o >= 4; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);
     if (t % 32 < 4) slots[t / 32][t % 32] = sum;
     sync();
@@ -428,7 +428,7 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
         if (has_extra) y[extra] = out.value(x_extra, extra == in.target);
         if (inside && lane == out.writer_of(shape, in.target, 0, shape.units, 32)) y[in.target] = out.value(x_target, true);
     }
-    finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x);
+    finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
 }
 
 // ---- longer rows: a ring in shared memory ------------------------------------------------------
@@ -624,7 +624,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             atomicCAS(a.status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
             a.status[1] = kWaitPolicyRing;
         __syncwarp();
-        finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane);
+        if (rank == 0) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, (unsigned)first, (unsigned)step);
     } else {
         Cursor<kStages> c;
         uint32_t n = 0;              // live rows whose statistics have been taken
@@ -831,7 +831,7 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
         }
         group_sync<kWarps>(0);  // the slots are used again
     }
-    finish_stats<kThreads, kThreads>(a, acc, sums, &last, t);
+    finish_stats<kThreads, kThreads>(a, acc, sums, &last, t, blockIdx.x, gridDim.x);
 }
 
 // ---- launches --------------------------------------------------------------------------------------

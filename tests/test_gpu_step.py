@@ -489,6 +489,22 @@ def test_grad_norm_against_64_bits(sizes, offset, gdtype):
         assert abs(float(out[2:4].view(torch.float64)) - want * want) <= 1.1e-6 * want * want
 
 
+@pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
+def test_grad_norm_counts_every_element_once(gdtype):
+    """Of ones, whose sums are exact at any order, at every alignment and around the lengths where a tensor
+    ends near the 32 KB that one thread block takes at a time."""
+    opt = adama.AdamA()
+    chunk = 32768 // (2 if gdtype == torch.bfloat16 else 4)
+    x = torch.ones(2 * chunk + 64, dtype=gdtype, device="cuda")
+    out = torch.zeros(4, device="cuda")
+    for n in [*range(1, 20), *range(chunk - 9, chunk + 10), *range(2 * chunk - 9, 2 * chunk + 10)]:
+        for offset in range(8):
+            x.fill_(math.nan)
+            x[offset:offset + n] = 1
+            opt.grad_norm_multi([x[offset:offset + n]], 1.0, out)
+            assert float(out[2:4].view(torch.float64)) == n, (n, offset)
+
+
 def test_grad_norm_joins_lists_and_reports_what_is_not_finite():
     opt = adama.AdamA()
     a, b = wl.normal((5000,), 1.0, torch.float32, 1).cuda(), wl.normal((777,), 1.0, torch.bfloat16, 2).cuda()
