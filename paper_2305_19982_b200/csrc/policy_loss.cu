@@ -67,8 +67,8 @@ __device__ __forceinline__ void store_peer(const Stats *slot, uint32_t rank, con
 // ---- token log-probabilities -----------------------------------------------------------------
 
 // W warps to a row (or to the slice of a row that a cluster of CTAs shares), ROWS rows to a CTA, kLoads
-// units of each thread in flight.  4096 x 50304: 70.0 us with 4 warps, 76.7 with 2, 72.4 with 8; 70.5 with 8
-// units in flight; 94 when CTAs of 16 warps walked the rows.
+// units of each thread in flight.  4096 x 50304: 69.5 us with 4 warps, 76.7 with 2; 70.5 with 8 units in
+// flight; 94 when CTAs of 16 warps walked the rows.
 constexpr int kLoads = 4;
 
 template <typename T, int W, int ROWS, bool ENT, bool CLUSTER>
@@ -877,10 +877,25 @@ cudaError_t logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
     const float k = (float)(a.scale * kLog2e);
     const int64_t units = a.vocab / kUnit<T>;
     if (units <= 32 * kRowUnits) return logprobs_groups<T, 1, 4>(a, k, stream);
-    if (units <= 128 * kRowUnits || a.rows >= 8 * (int64_t)sm_count) return logprobs_groups<T, 4, 1>(a, k, stream);
-    int cluster = 1;  // more CTAs to a row while there are fewer rows than SMs and work for their threads
-    while (cluster < kMaxCluster && a.rows * cluster * 2 <= sm_count && units >= cluster * 2 * kThreads) cluster *= 2;
-    return cluster > 1 ? logprobs_cluster<T>(a, k, cluster, stream) : logprobs_groups<T, kWarps, 1>(a, k, stream);
+    // Warps to a row, us with 4 / 8 / 16.  Short rows: 592 x 9000 bf16 4.8 / 5.5 / 6.0, 74 of them 3.6 / 3.2 / 3.1.
+    const int64_t per_sm = a.rows / sm_count;
+    if (units <= 3 * kThreads)
+        return per_sm < 1 ? logprobs_groups<T, 8, 1>(a, k, stream) : logprobs_groups<T, 4, 1>(a, k, stream);
+    // Few long rows: a cluster of CTAs to each while there are fewer rows than SMs and work for their threads
+    // (20 x 50257 bf16 4.5 with 8 CTAs, 5.4 with 1; 20 x 20000 3.9 and 3.6), then 16 warps (296 x 131072
+    // fp32 50.7 / 31.3 / 24.9).
+    if (per_sm < 3 && units > 6 * kThreads) {
+        int cluster = 1;
+        if (units >= 8 * kThreads)
+            while (cluster < kMaxCluster && a.rows * cluster * 2 <= sm_count && units >= cluster * 2 * kThreads) cluster *= 2;
+        return cluster > 1 ? logprobs_cluster<T>(a, k, cluster, stream) : logprobs_groups<T, kWarps, 1>(a, k, stream);
+    }
+    // More rows: 4 warps, of which the fewest wait at a row's end (1024 x 50257 bf16 22.0 / 24.3 / 25.3, 6000 x
+    // 20000 bf16 47.1 / 52.4 / 85.6); 8 for the numbers of rows that leave an SM with too few resident warps
+    // (450 x 50257 fp32 23.0 / 17.0 / 20.5), or at 4 warps with all its rows resident at once and so with more
+    // or fewer of them than the next SM (2048 x 128256 fp32 162.6 / 149.4 / 149.4).
+    return per_sm < 5 || (per_sm >= 10 && per_sm < 16) ? logprobs_groups<T, 8, 1>(a, k, stream)
+                                                       : logprobs_groups<T, 4, 1>(a, k, stream);
 }
 
 template <typename T, typename O>

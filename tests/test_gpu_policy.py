@@ -63,6 +63,23 @@ def test_token_logprobs(T, V, dtype, pitch, offset, scale):
     opt.sync_status()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,V", [(20, 9001), (100, 26_001), (300, 9001), (300, 30_011), (470, 26_001), (760, 26_001), (1600, 26_001)])
+def test_token_logprobs_at_every_number_of_warps_to_a_row(T, V, dtype):
+    opt = adama.AdamA()
+    buf, x = _logits(T, V, dtype, T + V, V + 1, 1)
+    targets = torch.randint(-1, V, (T,), generator=torch.Generator().manual_seed(V)).cuda()
+    logp, lse, ent = (torch.full((T,), -7.0, device="cuda") for _ in range(3))
+    opt.token_logprobs(x, targets, logp, lse=lse, entropy=ent)
+    live = targets.cpu() >= 0
+    rl, rp, re, _ = (r[live] for r in _reference(x, targets, 1.0))
+    assert float((lse.cpu().double()[live] - rl).abs().max()) <= LOGP
+    assert float((logp.cpu().double()[live] - rp).abs().max()) <= LOGP
+    assert float((ent.cpu().double()[live] - re).abs().max()) <= LOGP * 10
+    assert not (~live).any() or float(logp.cpu()[~live].abs().max()) == 0.0
+    opt.sync_status()
+
+
 def test_token_logprobs_of_rows_with_infinite_entries():
     opt = adama.AdamA()
     T, V = 6, 3001
