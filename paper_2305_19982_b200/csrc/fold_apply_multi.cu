@@ -344,9 +344,9 @@ cudaError_t launch(const StepList &s, adama_dtype gdt, int first, int count, Fol
 cudaError_t launch_fold_apply_multi(const StepList &s, adama_dtype gdt, int first, int count,
                                     FoldConstants f, ApplyConstants c, const float *factor,
                                     unsigned *status, int sm_count, cudaStream_t stream) {
-    return count <= kStepSmall
-               ? launch<kStepSmall>(s, gdt, first, count, f, c, factor, status, sm_count, stream)
-               : launch<kStepMax>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
+    if (count <= kStepSmall) return launch<kStepSmall>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
+    if (count <= kStepMid) return launch<kStepMid>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
+    return launch<kStepMax>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
 }
 
 }  // namespace adama

@@ -593,17 +593,21 @@ cudaError_t launch_convert(const StepList &s, int first, int count, int sm_count
 cudaError_t launch_fold_apply8_multi(const StepList &s, adama_dtype gdt, int first, int count,
                                      FoldConstants f, ApplyConstants c, const float *factor,
                                      unsigned *status, int sm_count, cudaStream_t stream) {
-    return count <= kStepSmall ? launch_step<kStepSmall>(s, gdt, first, count, f, c, factor, status, sm_count, stream)
-                               : launch_step<kStep8Max>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
+    if (count <= kStepSmall) return launch_step<kStepSmall>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
+    if (count <= kStepMid) return launch_step<kStepMid>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
+    return launch_step<kStep8Max>(s, gdt, first, count, f, c, factor, status, sm_count, stream);
+}
+
+template <bool PACK>
+static cudaError_t convert(const StepList &s, int first, int count, int sm_count, cudaStream_t stream) {
+    if (count <= kStepSmall) return launch_convert<PACK, kStepSmall>(s, first, count, sm_count, stream);
+    if (count <= kStepMid) return launch_convert<PACK, kStepMid>(s, first, count, sm_count, stream);
+    return launch_convert<PACK, kStep8Max>(s, first, count, sm_count, stream);
 }
 
 cudaError_t launch_state8_convert(const StepList &s, bool pack, int first, int count, int sm_count,
                                   cudaStream_t stream) {
-    if (pack)
-        return count <= kStepSmall ? launch_convert<true, kStepSmall>(s, first, count, sm_count, stream)
-                                   : launch_convert<true, kStep8Max>(s, first, count, sm_count, stream);
-    return count <= kStepSmall ? launch_convert<false, kStepSmall>(s, first, count, sm_count, stream)
-                               : launch_convert<false, kStep8Max>(s, first, count, sm_count, stream);
+    return pack ? convert<true>(s, first, count, sm_count, stream) : convert<false>(s, first, count, sm_count, stream);
 }
 
 }  // namespace adama

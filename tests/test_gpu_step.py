@@ -465,6 +465,37 @@ def test_many_8_bit_tensors_in_several_launches_equal_one_by_one():
         assert torch.equal(x.m_codes.view(torch.uint8), y.m_codes.view(torch.uint8))
 
 
+@pytest.mark.parametrize("large", [0, 3_000_017])
+@pytest.mark.parametrize("count", [64, 65, 192, 193])
+def test_lists_around_the_sizes_of_the_launch_tables(count, large):
+    """The same tensors in one list and one by one; with one large tensor in the list's middle they stream."""
+    sizes = [1 + (53 * i) % 700 for i in range(count)]
+    sizes[count // 2] += large
+    lists = lambda: [[wl.normal((n,), 0.02, torch.float32, k * 1000 + i).cuda() for i, n in enumerate(sizes)]  # noqa: E731
+                     for k in range(3)]
+    gs = [wl.normal((n,), 1e-3, torch.bfloat16, 9000 + i).cuda() for i, n in enumerate(sizes)]
+    opt, ref = adama.AdamA(), adama.AdamA()
+    opt.begin_minibatch(1)
+    ref.begin_minibatch(1)
+    (w, m, v), (w2, m2, v2) = lists(), lists()
+    v, v2 = [x.abs() for x in v], [x.abs() for x in v2]
+    a, b = [State8.zeros(n) for n in sizes], [State8.zeros(n) for n in sizes]
+    opt.state8_pack_multi(m, v, State8List(a))
+    opt.fold_apply_multi(w, gs, m, v, wl.LR)
+    opt.fold_apply8_multi(w, gs, State8List(a), wl.LR)
+    m8, v8, m9, v9 = ([torch.full((n,), -1.0, device="cuda") for n in sizes] for _ in range(4))
+    opt.state8_unpack_multi(State8List(a), m8, v8)
+    for i in range(count):
+        ref.state8_pack_multi([m2[i]], [v2[i]], [b[i]])
+        ref.fold_apply_multi([w2[i]], [gs[i]], [m2[i]], [v2[i]], wl.LR)
+        ref.fold_apply8_multi([w2[i]], [gs[i]], [b[i]], wl.LR)
+        ref.state8_unpack_multi([b[i]], [m9[i]], [v9[i]])
+    assert opt.launch_count == 4
+    for x, y in zip(w + m + v + m8 + v8, w2 + m2 + v2 + m9 + v9):
+        assert torch.equal(x, y)
+    opt.sync_status()
+
+
 # ---- gradient norm ---------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
