@@ -496,6 +496,43 @@ def test_lists_around_the_sizes_of_the_launch_tables(count, large):
     opt.sync_status()
 
 
+def test_one_tensor_of_more_than_2_31_elements():
+    """32-bit states (34 GB), then 8-bit ones in place of the moments: what lies around and behind element
+    2^31 becomes what the same values become in tensors of their own; the norm counts every element."""
+    n = 2 ** 31 + 12_345
+    if torch.cuda.mem_get_info()[0] < 48 * 2 ** 30:
+        pytest.skip("needs 48 GB of free device memory")
+    parts = [slice(0, 4096), slice(2 ** 31 - 8192, 2 ** 31 + 4096), slice(2 ** 31 + 8192, n)]
+    opt, ref = adama.AdamA(), adama.AdamA()
+    opt.begin_minibatch(1)
+    ref.begin_minibatch(1)
+    g = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros(4, device="cuda")
+    opt.grad_norm_multi([g], 1.0, out)
+    assert float(out[2:4].view(torch.float64)) == n
+    w, m, v = (torch.zeros(n, device="cuda") for _ in range(3))
+    for k, p in enumerate(parts):
+        size = (p.stop - p.start,)
+        for j, t in enumerate((w, m, v, g)):
+            t[p] = wl.normal(size, 0.02, torch.float32, 10 * k + j).abs().cuda()
+    small = [[t[p].clone() for t in (w, g, m, v)] for p in parts]
+    opt.fold_apply_multi([w], [g], [m], [v], wl.LR)
+    for p, (w1, g1, m1, v1) in zip(parts, small):
+        ref.fold_apply_multi([w1], [g1], [m1], [v1], wl.LR)
+        assert torch.equal(w[p], w1) and torch.equal(m[p], m1) and torch.equal(v[p], v1)
+    state = State8.zeros(n)
+    opt.state8_pack_multi([m], [v], [state])
+    opt.fold_apply8_multi([w], [g], [state], wl.LR)
+    opt.state8_unpack_multi([state], [m], [v])
+    for p, (w1, g1, m1, v1) in zip(parts, small):
+        one = State8.zeros(w1.numel())
+        ref.state8_pack_multi([m1], [v1], [one])
+        ref.fold_apply8_multi([w1], [g1], [one], wl.LR)
+        ref.state8_unpack_multi([one], [m1], [v1])
+        assert torch.equal(w[p], w1) and torch.equal(m[p], m1) and torch.equal(v[p], v1)
+    opt.sync_status()
+
+
 # ---- gradient norm ---------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
