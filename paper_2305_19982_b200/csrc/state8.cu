@@ -382,6 +382,7 @@ fold_apply8_ring_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f
             x.store_wide(s, tab.w[t], tab.copy[t], at + 4 * lane);
             Block8::store_scales(s, blk, top, lane, c);
         } else {
+            __syncwarp();  // every lane is past the wait and has read tensor[slot] before the slot is given back
             if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
             if (at < n)
                 block_direct(static_cast<const G *>(tab.g[t]), tab.w[t], tab.copy[t], s, at, n, false, lane, factor, f, c);

@@ -1,0 +1,27 @@
+"""Where one lane acts for its warp in the kernels that stream through shared memory, the warp is
+brought together first.  The lanes of a warp may run apart: a lane 0 that gives a stage back before
+the others have read it, or that is still busy when the others reach a cluster barrier, is an error
+that a run hardly ever shows, so the order of the statements is checked in the sources."""
+import re
+from pathlib import Path
+
+import pytest
+
+CSRC = Path(__file__).resolve().parent.parent / "paper_2305_19982_b200" / "csrc"
+RINGS = ["fold_apply_multi.cu", "state8.cu", "policy_loss.cu"]
+
+
+def _statements(name):
+    """The file's lines without comments, blank lines left out."""
+    text = re.sub(r"//[^\n]*", "", (CSRC / name).read_text())
+    return [line.strip() for line in text.splitlines() if line.strip()]
+
+
+@pytest.mark.parametrize("name", RINGS)
+def test_a_stage_is_given_back_by_the_whole_warp(name):
+    lines = _statements(name)
+    arrivals = [i for i, line in enumerate(lines) if "barrier_arrive" in line and "empty[" in line]
+    assert arrivals
+    for i in arrivals:
+        assert lines[i].startswith("if (lane == 0)")
+        assert lines[i - 1] == "__syncwarp();", f"{name}: {lines[i - 1]} / {lines[i]}"
