@@ -118,6 +118,7 @@ token_logprobs_kernel(const LogprobArgs a, float k, int log_cluster) {
         if (CLUSTER) {  // to the first CTA's shared memory
             cluster_wait();  // it has begun
             if (t == 0) store_peer(&peers[rank], 0, s);
+            __syncwarp();  // the cluster's barrier is for whole warps
             cluster_sync();
             if (rank != 0) return;
             const Stats none = {-CUDART_INF_F, 0.f, 0.f};

@@ -25,3 +25,12 @@ def test_a_stage_is_given_back_by_the_whole_warp(name):
     for i in arrivals:
         assert lines[i].startswith("if (lane == 0)")
         assert lines[i - 1] == "__syncwarp();", f"{name}: {lines[i - 1]} / {lines[i]}"
+
+
+def test_cluster_barriers_are_reached_by_whole_warps():
+    """They are the .aligned form, which all lanes of a warp execute together."""
+    lines = _statements("policy_loss.cu")
+    places = [i for i, line in enumerate(lines) if "cluster_sync();" in line]
+    assert len(places) == 3
+    for i in places:
+        assert lines[i - 1] in ("__syncwarp();", "__syncthreads();"), f"{lines[i - 1]} / {lines[i]}"
