@@ -402,8 +402,8 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
             }
         }
         if (has_extra) run.add_one(x_extra, k);
-        // the gradient may replace the logits: every lane has read its own when the join is through
         const Stats s = warp_join<false>(run.stats(), k);
+        __syncwarp();  // the gradient may replace the logits: no lane writes before all have read (a join alone orders no memory)
         const RowOut o = row_out(a, in, s, x_target);
         if (lane == 0) {
             acc.add(a, in, o);

@@ -34,3 +34,12 @@ def test_cluster_barriers_are_reached_by_whole_warps():
     assert len(places) == 3
     for i in places:
         assert lines[i - 1] in ("__syncwarp();", "__syncthreads();"), f"{lines[i - 1]} / {lines[i]}"
+
+
+def test_a_gradient_over_the_logits_waits_for_the_warp():
+    """Rows in a warp's registers: every lane reads the target's logit, which another lane overwrites."""
+    lines = _statements("policy_loss.cu")
+    begin = next(i for i, line in enumerate(lines) if line.startswith("policy_loss_rows_kernel("))
+    join = next(i for i in range(begin, len(lines)) if "warp_join" in lines[i])
+    store = next(i for i in range(begin, len(lines)) if lines[i].startswith("const RowWriter"))
+    assert join < store and "__syncwarp();" in lines[join:store]
