@@ -608,6 +608,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             const RowOut o = row_out(a, in, s, x_target);
             O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
             const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
+            __syncwarp();  // all lanes have read x_target, which the verdict's readers may overwrite
             if (lane == 0) {
                 const int writer = inside ? out.writer_of(shape, in.target, from, count, kRingWork) : -1;
                 sh.verdict[b] = {s.top, o.unit, o.per_e, x_target, in.target, writer};

@@ -43,3 +43,12 @@ def test_a_gradient_over_the_logits_waits_for_the_warp():
     join = next(i for i in range(begin, len(lines)) if "warp_join" in lines[i])
     store = next(i for i in range(begin, len(lines)) if lines[i].startswith("const RowWriter"))
     assert join < store and "__syncwarp();" in lines[join:store]
+
+
+def test_the_verdict_on_a_row_waits_for_the_warp():
+    """Longer rows: the warp that does the joins reads the target's logit in every lane; its lane 0 then
+    lets the other warps write over it."""
+    lines = _statements("policy_loss.cu")
+    arrive = next(i for i, line in enumerate(lines) if "barrier_arrive(shared_addr(&sh.ready" in line)
+    begin = max(i for i in range(arrive) if lines[i] == "if (lane == 0) {")
+    assert lines[begin - 1] == "__syncwarp();"
