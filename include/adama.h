@@ -378,7 +378,9 @@ ADAMA_API adama_status adama_state8_unpack_multi(adama_ctx *ctx, const adama_sta
 
 /* Scratch of the two reductions below: caller-owned device memory, 16-byte aligned, zero-filled
  * once before its first use (each call leaves it ready for the next).  Calls that may overlap on the
- * GPU (different streams) need one each. */
+ * GPU (different streams) need one each.  A call that is captured into a CUDA graph keeps the address:
+ * give each graph a workspace of its own, with the zero-fill captured in the same graph before its first
+ * use, or filled before the first replay.  A captured zero-fill has not run when the capture ends. */
 #define ADAMA_WORKSPACE_BYTES 65536
 
 /* Global 2-norm of a list of gradients, and the factor that clips it to max_norm, both left in
@@ -452,6 +454,10 @@ typedef struct adama_policy_args {
 } adama_policy_args;
 ADAMA_API adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args *args,
                                          void *cuda_stream);
+
+/* The id of the capture that `cuda_stream` is taking part in, 0 if it is not being captured: what a
+ * caller who keeps a workspace per stream tells graphs apart by.  Ids are unique in the process. */
+ADAMA_API uint64_t adama_stream_capture_id(void *cuda_stream);
 
 /* ---- host-buffer variants (same arithmetic, copies included) --------------------------- */
 

@@ -27,7 +27,7 @@ EXPORTED_SYMBOLS = [
     "adama_host_constants_allreduced", "adama_host_constants_sharded",
     "adama_version",
     "adama_fold_apply_multi", "adama_fold_apply8_multi", "adama_state8_pack_multi", "adama_state8_unpack_multi",
-    "adama_grad_norm_multi", "adama_token_logprobs", "adama_policy_loss",
+    "adama_grad_norm_multi", "adama_token_logprobs", "adama_policy_loss", "adama_stream_capture_id",
 ]
 
 
@@ -142,6 +142,8 @@ def load_library() -> ctypes.CDLL:
     L.adama_grad_norm_multi.argtypes = [vp, vp, ci, vp, ci, dbl, ci, vp, vp, vp]
     L.adama_token_logprobs.argtypes = [vp, vp, ci, i64, i64, i64, vp, dbl, vp, vp, vp, vp]
     L.adama_policy_loss.argtypes = [vp, ctypes.c_char_p, vp]
+    L.adama_stream_capture_id.argtypes = [vp]
+    L.adama_stream_capture_id.restype = ctypes.c_uint64
     L.adama_get_step.argtypes = [vp]
     L.adama_get_step.restype = i64
     L.adama_set_step.argtypes = [vp, i64]
@@ -276,7 +278,7 @@ class AdamA:
                  async_copyback=False, inputs_settled=False):
         self._L = load_library()
         self._h = ctypes.c_void_p()
-        self._workspaces = {}
+        self._workspaces, self._captured = {}, {}
         self.device = torch.device("cuda", int(device))
         cfg = _Config(beta1, beta2, eps, int(device),
                       (GRADS_PRESCALED if grads_prescaled else 0) |
@@ -551,7 +553,17 @@ class AdamA:
 
     # -- the end of a fine-tuning step -------------------------------------------------------
     def _workspace(self, stream: int) -> int:
-        """Scratch of the reductions: one zero-filled buffer for each stream that uses them."""
+        """Scratch of the reductions, zero-filled: one buffer for each stream that uses them.  While the
+        stream is being captured into a graph, one for that graph alone, whose zero-fill the graph carries;
+        it comes from the graph's memory and is let go when the stream's next capture begins to use one."""
+        if stream:  # the legacy default stream cannot be captured
+            capture = self._L.adama_stream_capture_id(stream)
+            if capture:
+                known, t = self._captured.get(stream, (0, None))
+                if known != capture:
+                    t = torch.zeros(WORKSPACE_BYTES, dtype=torch.uint8, device=self.device)
+                    self._captured[stream] = (capture, t)
+                return t.data_ptr()
         t = self._workspaces.get(stream)
         if t is None:
             t = torch.zeros(WORKSPACE_BYTES, dtype=torch.uint8, device=self.device)

@@ -1072,6 +1072,16 @@ int adama_debug_setup_state(int device) { return adama::wgrad_setup_state(device
 
 const char *adama_last_error(const adama_ctx *ctx) { return ctx ? ctx->err : ""; }
 
+uint64_t adama_stream_capture_id(void *cuda_stream) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (cudaStreamGetCaptureInfo(static_cast<cudaStream_t>(cuda_stream), &status, &id) != cudaSuccess) {
+        cudaGetLastError();  // e.g. the legacy stream while another one captures: it is not captured itself
+        return 0;
+    }
+    return status == cudaStreamCaptureStatusActive ? id : 0;
+}
+
 int64_t adama_launch_count(const adama_ctx *ctx) { return ctx ? ctx->launches : -1; }
 
 adama_status adama_host_constants(const adama_config *cfg, int n_micro, int64_t t, double lr,
