@@ -590,10 +590,11 @@ ADAMA_API int adama_get_n_micro(const adama_ctx *ctx);
  * (the factor is 1.0f, results are bit-identical).  Errors: INVALID_ARG (negative or not finite). */
 ADAMA_API adama_status adama_set_weight_decay(adama_ctx *ctx, double weight_decay);
 
-/* Waits for `cuda_stream`, then reads and clears the device status block.
- * Returns ADAMA_OK, ADAMA_ERR_TIMEOUT (a bounded wait inside the fused kernel
- * expired; m and v of that call are incomplete), ADAMA_ERR_INVALID_ARG (a row of
- * adama_token_logprobs or adama_policy_loss had a target >= vocab) or ADAMA_ERR_CUDA. */
+/* Waits for `cuda_stream`, then reads the device status block.  Returns ADAMA_OK,
+ * ADAMA_ERR_TIMEOUT (a bounded wait inside a kernel expired: the fused weight gradient, a streamed
+ * update or the policy loss, as adama_last_error says; what that call writes is incomplete),
+ * ADAMA_ERR_INVALID_ARG (a row of adama_token_logprobs or adama_policy_loss had a target >= vocab) or
+ * ADAMA_ERR_CUDA.  Each call reports and clears one of them, an expired wait first: call again for the other. */
 ADAMA_API adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream);
 
 /* Test hook: writes {code, wait, tile} into the device status block exactly as a kernel whose

@@ -791,8 +791,9 @@ class AdamA:
         return int(self._L.adama_get_n_micro(self._h))
 
     def sync_status(self) -> None:
-        """Waits for the current stream and raises AdamAError(ERR_TIMEOUT) if a bounded
-        device-side wait expired."""
+        """Waits for the current stream and raises AdamAError: ERR_TIMEOUT if a bounded device-side wait
+        expired, else ERR_INVALID_ARG if a row of logits had a target outside the vocabulary.  One report
+        a call, which clears it."""
         self._check(self._L.adama_sync_status(self._h, _stream_ptr(self.device)))
 
     def debug_set_status(self, code: int, wait: int = 0, tile: int = 0) -> None:

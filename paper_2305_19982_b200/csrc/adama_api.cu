@@ -1005,20 +1005,21 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
     if (!ctx) return ADAMA_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->cfg.device);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    unsigned host[4] = {0, 0, 0, 0};
+    unsigned host[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     cudaError_t e = join_copyback(ctx, stream);
     if (e == cudaSuccess)
         e = cudaMemcpyAsync(host, ctx->status_dev, sizeof(host), cudaMemcpyDeviceToHost, stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
     if (e != cudaSuccess) return cuda_fail(ctx, "sync_status", e);
+    // One report a call, an expired wait first; what is not reported yet stays for the next call.
+    const auto clear = [&](int first) {
+        cudaError_t c = cudaMemsetAsync(ctx->status_dev + first, 0, 4 * sizeof(unsigned), stream);
+        if (c == cudaSuccess) c = cudaStreamSynchronize(stream);
+        return c;
+    };
     if (host[0] != adama::kDevOk) {
-        e = cudaMemsetAsync(ctx->status_dev, 0, 256, stream);
-        if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
-        if (host[0] == adama::kDevBadTarget) {
-            snprintf(ctx->err, sizeof(ctx->err), "a row of logits had a target outside the vocabulary (row %llu)",
-                     (unsigned long long)host[2] << 32 | host[1]);
-            return ADAMA_ERR_INVALID_ARG;
-        }
+        e = clear(0);
+        if (e != cudaSuccess) return cuda_fail(ctx, "sync_status", e);
         snprintf(ctx->err, sizeof(ctx->err),
                  "device-side wait expired in the %s kernel (code %u, wait %u, tile %u)",
                  host[1] == adama::kWaitPolicyRing   ? "policy-loss"
@@ -1027,6 +1028,14 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
                                                      : "fused weight-gradient",
                  host[0], host[1], host[2]);
         return ADAMA_ERR_TIMEOUT;
+    }
+    const unsigned *target = host + adama::kStatusTarget;
+    if (target[0] != 0) {
+        e = clear(adama::kStatusTarget);
+        if (e != cudaSuccess) return cuda_fail(ctx, "sync_status", e);
+        snprintf(ctx->err, sizeof(ctx->err), "a row of logits had a target outside the vocabulary (row %llu)",
+                 (unsigned long long)target[2] << 32 | target[1]);
+        return ADAMA_ERR_INVALID_ARG;
     }
     return ADAMA_OK;
 }

@@ -49,10 +49,12 @@ FoldConstants make_fold_constants(double beta1, double beta2, int n_micro, unsig
 ApplyConstants make_apply_constants(double beta1, double beta2, double eps, int64_t t, double lr,
                                     int world = 1, bool sharded = false, double weight_decay = 0.0);
 
-// Status block in device memory (256 bytes): word 0 = first error code recorded
-// by a kernel (0 = none), word 1 = which wait, word 2 = tile (bad target: the row, low and high
-// half); rest reserved.
-enum DeviceErr : unsigned { kDevOk = 0, kDevTimeout = 1, kDevBadTarget = 2 };
+// Status block in device memory (256 bytes).  Words 0-3, an expired wait: word 0 = kDevTimeout (0 =
+// none) by the first kernel that records one, word 1 = which wait, word 2 = tile.  Words 4-7, a target
+// outside the vocabulary: word kStatusTarget = 1 by the first row that records one, the next two that row's
+// low and high half.  Apart, so that neither hides the other.  The rest is reserved.
+enum DeviceErr : unsigned { kDevOk = 0, kDevTimeout = 1 };
+constexpr int kStatusTarget = 4;
 // word 1 for the waits of the kernels that stream through a ring of bulk copies
 constexpr unsigned kWaitPolicyRing = 100, kWaitState8Ring = 101, kWaitStepRing = 102;
 

@@ -21,9 +21,9 @@ constexpr int kThreads = 512;  // that work on rows, in every kernel here
 constexpr int kWarps = kThreads / 32;
 
 __device__ __forceinline__ void record_bad_target(unsigned *status, int64_t row) {
-    if (atomicCAS(status, (unsigned)kDevOk, (unsigned)kDevBadTarget) == (unsigned)kDevOk) {
-        status[1] = (unsigned)row;
-        status[2] = (unsigned)(row >> 32);
+    if (atomicCAS(status + kStatusTarget, 0u, 1u) == 0u) {
+        status[kStatusTarget + 1] = (unsigned)row;
+        status[kStatusTarget + 2] = (unsigned)(row >> 32);
     }
 }
 
