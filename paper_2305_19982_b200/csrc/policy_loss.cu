@@ -157,6 +157,27 @@ __device__ __forceinline__ RowIn row_in(const PolicyArgs &a, int64_t row) {
     return r;
 }
 
+// exp(d) - d - 1, and exp(d) - 1.  Policies that are close have d of 1e-5 to 1e-2 and a KL of d^2/2: the
+// difference of exp(d) and d + 1 would leave noise of 6e-8 there.  Below 1/2 the exponential series without its
+// first two terms is summed instead (the first one left out is 2e-8 of the sum); from 1/2 on the
+// difference costs 1.2e-6 at most.
+__device__ __forceinline__ float kl_of(float d, float &less_one) {
+    if (fabsf(d) < 0.5f) {
+        float q = 1.f / 40320.f;
+        q = fmaf(q, d, 1.f / 5040.f);
+        q = fmaf(q, d, 1.f / 720.f);
+        q = fmaf(q, d, 1.f / 120.f);
+        q = fmaf(q, d, 1.f / 24.f);
+        q = fmaf(q, d, 1.f / 6.f);
+        q = fmaf(q, d, 0.5f);
+        const float kl = d * d * q;
+        less_one = d + kl;
+        return kl;
+    }
+    less_one = expf(d) - 1.f;
+    return less_one - d;
+}
+
 // One row's loss terms and its gradient: dlogits_j = unit*[j = target] + per_e*2^(k*(x_j - top)).
 struct RowOut {
     float logp, pg, kl, cut, unit, per_e;
@@ -172,9 +193,9 @@ __device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, 
     float slope = cut ? 0.f : -plain;
     o.kl = 0.f;
     if (a.ref_logp) {
-        const float d = in.ref - o.logp, e = expf(d);
-        o.kl = e - d - 1.f;
-        slope += a.kl_coef * (1.f - e);
+        float less_one;  // exp(d) - 1
+        o.kl = kl_of(in.ref - o.logp, less_one);
+        slope -= a.kl_coef * less_one;
     }
     if (r != r) o.pg = slope = r;  // a NaN log-probability stays visible
     o.unit = in.weight * slope * a.scale;
