@@ -422,7 +422,8 @@ ADAMA_API adama_status adama_token_logprobs(adama_ctx *ctx, const void *logits, 
  * logp as in adama_token_logprobs, A the advantage and w the row's weight:
  *     r  = exp(logp - old_logp)
  *     pg = -min(r*A, clamp(r, 1-clip_low, 1+clip_high)*A)
- *     d  = ref_logp - logp,  kl = exp(d) - d - 1            (0 without ref_logp)
+ *     d  = ref_logp - logp,  kl = exp(d) - d - 1            (0 without ref_logp; with kl_coef = 0 it is
+ *                                                            reported and has no part in loss and gradient)
  *     stats = sum over rows of w*{pg + kl_coef*kl, pg, kl, [r*A > the clamped product]}
  *     dlogits_j = w*logit_scale*c*([j = target] - p_j),
  *         c = (r*A <= the clamped product ? -r*A : 0) + kl_coef*(1 - exp(d))

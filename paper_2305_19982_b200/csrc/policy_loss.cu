@@ -195,7 +195,7 @@ __device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, 
     if (a.ref_logp) {
         float less_one;  // exp(d) - 1
         o.kl = kl_of(in.ref - o.logp, less_one);
-        slope -= a.kl_coef * less_one;
+        if (a.kl_coef != 0.f) slope -= a.kl_coef * less_one;  // a KL that is only watched may be infinite
     }
     if (r != r) o.pg = slope = r;  // a NaN log-probability stays visible
     o.unit = in.weight * slope * a.scale;
@@ -209,7 +209,7 @@ struct Sums {
 
     __device__ __forceinline__ void add(const PolicyArgs &a, const RowIn &in, const RowOut &o) {
         const double w = in.weight;
-        v[0] += w * (o.pg + (a.ref_logp ? a.kl_coef * o.kl : 0.f));
+        v[0] += w * (o.pg + (a.ref_logp && a.kl_coef != 0.f ? a.kl_coef * o.kl : 0.f));
         v[1] += w * o.pg;
         v[2] += w * o.kl;
         v[3] += w * o.cut;

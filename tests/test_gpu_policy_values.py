@@ -59,3 +59,16 @@ def test_equal_policies_have_no_kl_and_no_gradient():
     opt.policy_loss(x, targets, logp, torch.zeros(40, device="cuda"), torch.ones(40, device="cuda"), grad, stats,
                     ref_logp=logp, kl_coef=1.0)
     assert stats.tolist() == [0.0] * 4 and not bool(grad.any())
+
+
+@pytest.mark.parametrize("T,V", SHAPES)
+def test_kl_that_is_only_watched_does_not_reach_the_loss(T, V):
+    """kl_coef 0 with a reference that is far away, so that exp(ref - logp) overflows: the KL is infinite,
+    loss and gradient are those without a reference."""
+    opt, x, targets, logp = _rows(T, V, 5)
+    old, one = logp - 0.1, torch.ones(T, device="cuda")
+    grads, stats = [torch.empty(T, V, device="cuda") for _ in range(2)], [torch.empty(4, device="cuda") for _ in range(2)]
+    opt.policy_loss(x, targets, old, one, one, grads[0], stats[0])
+    opt.policy_loss(x, targets, old, one, one, grads[1], stats[1], ref_logp=logp + 100, kl_coef=0.0)
+    assert torch.equal(grads[0], grads[1]) and torch.equal(stats[0][:2], stats[1][:2])
+    assert float(stats[1][2]) == math.inf and math.isfinite(float(stats[1][0]))
