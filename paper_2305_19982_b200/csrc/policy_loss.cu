@@ -185,8 +185,10 @@ struct RowOut {
 __device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, const Stats &s, float x_target) {
     RowOut o;
     o.logp = logp_of(x_target, s, logf(s.sum), a.scale);
-    const float r = expf(o.logp - in.old), plain = r * in.adv;
-    const float clipped = fminf(fmaxf(r, a.ratio_min), a.ratio_max) * in.adv;
+    const float r = expf(o.logp - in.old);
+    // no advantage, no loss, also where the ratio overflows (a NaN ratio is seen to below)
+    const float plain = in.adv == 0.f ? 0.f : r * in.adv;
+    const float clipped = in.adv == 0.f ? 0.f : fminf(fmaxf(r, a.ratio_min), a.ratio_max) * in.adv;
     const bool cut = plain > clipped;
     o.pg = -(cut ? clipped : plain);
     o.cut = cut ? 1.f : 0.f;

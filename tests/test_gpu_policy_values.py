@@ -72,3 +72,15 @@ def test_kl_that_is_only_watched_does_not_reach_the_loss(T, V):
     opt.policy_loss(x, targets, old, one, one, grads[1], stats[1], ref_logp=logp + 100, kl_coef=0.0)
     assert torch.equal(grads[0], grads[1]) and torch.equal(stats[0][:2], stats[1][:2])
     assert float(stats[1][2]) == math.inf and math.isfinite(float(stats[1][0]))
+
+
+@pytest.mark.parametrize("T,V", SHAPES)
+def test_no_advantage_no_loss_however_large_the_ratio(T, V):
+    """exp(logp - old) = exp(100) overflows fp32; times an advantage of 0 it is 0.  A NaN ratio stays visible."""
+    opt, x, targets, logp = _rows(T, V, 6)
+    grad, stats = torch.full((T, V), 5.0, device="cuda"), torch.empty(4, device="cuda")
+    zero, one = torch.zeros(T, device="cuda"), torch.ones(T, device="cuda")
+    opt.policy_loss(x, targets, logp - 100, zero, one, grad, stats)
+    assert stats.tolist() == [0.0] * 4 and not bool(grad.any())
+    opt.policy_loss(x, targets, torch.full_like(logp, math.nan), zero, one, grad, stats)
+    assert math.isnan(float(stats[0])) and bool(torch.isnan(grad).all())
