@@ -405,7 +405,7 @@ ADAMA_API adama_status adama_grad_norm_multi(adama_ctx *ctx, const void *const *
                                              void *workspace, void *cuda_stream);
 
 /* Log-probability of one target per row of logits, with z = logit_scale * logits (logit_scale is
- * the inverse temperature):
+ * the inverse temperature, > 0 and at most 2.3e38):
  *     lse = log sum_j exp(z_j),  logp = z_target - lse,  entropy = lse - sum_j p_j z_j
  *   logits  : [rows, vocab] fp32 or bf16, row pitch ld elements (>= vocab), device, read-only;
  *             -inf entries have probability 0
@@ -436,7 +436,7 @@ ADAMA_API adama_status adama_token_logprobs(adama_ctx *ctx, const void *logits, 
  *   dlogits  : [rows, vocab] fp32 or bf16, pitch ld_dlogits, or NULL (loss and logp only)
  *   old_logp, ref_logp (or NULL), advantages, weights : rows fp32 each
  *   logp     : rows fp32, or NULL;   stats : 4 fp32;   workspace : ADAMA_WORKSPACE_BYTES
- * logit_scale > 0, 0 <= clip_low <= 1, clip_high >= 0, kl_coef finite.  Deterministic.
+ * logit_scale as there, 0 <= clip_low <= 1, clip_high >= 0, kl_coef finite.  Deterministic.
  * Errors: INVALID_ARG, MISALIGNED, CUDA; targets >= vocab as in adama_token_logprobs. */
 typedef struct adama_policy_args {
     const void *logits;

@@ -1,4 +1,5 @@
 // C ABI of libadama: context, argument checks, host-side constants, launches.
+#include <float.h>
 #include <math.h>
 #include <stdio.h>
 #include <string.h>
@@ -720,8 +721,9 @@ static adama_status check_logits(adama_ctx *ctx, const void *logits, adama_dtype
     if (dt != ADAMA_F32 && dt != ADAMA_BF16)
         return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: unknown dtype");
     if (rows > 0 && (!logits || !targets)) return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: null pointer");
-    if (!(logit_scale > 0.0) || !isfinite(logit_scale))
-        return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: logit_scale must be finite and > 0");
+    // the exponentials are taken to base 2: their factor, logit_scale*log2(e), has to be an fp32 number
+    if (!(logit_scale > 0.0) || !(logit_scale * 1.4426950408889634 <= FLT_MAX))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "logits: logit_scale must be > 0 and at most 2.3e38");
     if (!aligned_to(logits, dtype_size(dt)) || !aligned_to(targets, 8))
         return fail(ctx, ADAMA_ERR_MISALIGNED, "logits: pointer not aligned to its element size");
     return ADAMA_OK;

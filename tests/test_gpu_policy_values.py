@@ -84,3 +84,16 @@ def test_no_advantage_no_loss_however_large_the_ratio(T, V):
     assert stats.tolist() == [0.0] * 4 and not bool(grad.any())
     opt.policy_loss(x, targets, torch.full_like(logp, math.nan), zero, one, grad, stats)
     assert math.isnan(float(stats[0])) and bool(torch.isnan(grad).all())
+
+
+def test_a_scale_that_overflows_fp32_is_refused():
+    """2.5e38*log2(e), the factor of the exponentials, is beyond fp32."""
+    opt, x, targets, logp = _rows(4, 50, 7)
+    launches, one, stats = opt.launch_count, torch.ones(4, device="cuda"), torch.empty(4, device="cuda")
+    for scale in (2.5e38, 1e39, 1e300):
+        for call in (lambda: opt.token_logprobs(x, targets, logp, logit_scale=scale),
+                     lambda: opt.policy_loss(x, targets, logp, one, one, None, stats, logit_scale=scale)):
+            with pytest.raises(adama.AdamAError) as e:
+                call()
+            assert e.value.status == adama.Status.ERR_INVALID_ARG and "logit_scale" in str(e.value)
+    assert opt.launch_count == launches
