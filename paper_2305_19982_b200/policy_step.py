@@ -9,17 +9,20 @@ step; only library matrix products come between the calls:
     token_logprobs        log-probabilities of the sampled answers, under the sampling policy (old)
                           and the frozen one that the KL term holds on to (ref)
     policy_loss           clipped loss with KL term, and its gradient dlogits in bf16
+    grad_norm_multi       norm and clip factor of the gradients of the layers in front, left on the device
     linear_wgrad_fold     dlogits is the output layer's dY: its weight gradient goes straight into
-                          m, v and is never written; apply_bf16_copy updates that layer
-    grad_norm_multi       norm and clip factor of the other layers' gradients, left on the device
-    fold_apply8_multi     (or fold_apply_multi) their update in one pass, clipped, with the bf16
-                          copies that the next forward pass reads
+                          m, v and is never written, so it is neither in that norm nor clipped
+    fold_apply8_multi     (or fold_apply_multi) the update in one pass, the layers in front clipped,
+                          with the bf16 copies that the next forward pass reads
 
-Nothing waits for the host inside a step.  This module only sequences library calls and owns memory.
+A step whose gradients are not finite, or too large for v, leaves the whole model as it was: its factor is
+NaN, and nothing is folded into the output layer's moments.  Nothing waits for the host inside a step.
+This module only sequences library calls and owns memory.
 """
 from __future__ import annotations
 
 import argparse
+import math
 
 import torch
 
@@ -55,7 +58,11 @@ class PolicyStep:
             self.moments = State8List([State8.zeros(w.numel(), self.device) for w in (self.embed, self.inner)])
         else:
             self._m, self._v = (TensorList([torch.zeros_like(w) for w in (self.embed, self.inner)]) for _ in range(2))
+        # the output layer's last gradient is folded before its update, which then adds nothing
+        self._head = [TensorList([t]) for t in (self.head, torch.zeros_like(self.head_bf), self.head_m, self.head_v)]
+        self._head_copy = TensorList([self.head_bf])
         self.norm = torch.zeros(4, device=self.device)
+        self.sizes = torch.zeros(4, device=self.device)
         self.stats = torch.zeros(4, device=self.device)
 
     def forward(self, x: torch.Tensor, weights=None):
@@ -85,17 +92,24 @@ class PolicyStep:
         dl = dlogits[:, :self.vocab]
         opt.policy_loss(logits, y, old, advantages, weights, dl, self.stats, ref_logp=ref, kl_coef=self.kl_coef)
         dpre = (dlogits @ self.head_bf.t()) * (pre > 0)
-        opt.begin_minibatch(1)
-        opt.linear_wgrad_fold(h, dl, self.head_m[:, :self.vocab], self.head_v[:, :self.vocab])
         torch.mm(e.t(), dpre, out=self.grads[1])
         self.grads[0].copy_(torch.zeros_like(self.embed).index_add_(0, x, (dpre @ self.inner_bf.t()).float()))
         opt.grad_norm_multi(self._g, self.max_norm, self.norm)
+        # No entry of the output layer's gradient h' dlogits exceeds |h| |dlogits|, and so the square of the norm of
+        # both; v holds the entry's square.  Where that overflows, or the factor is NaN, the step is skipped.
+        opt.grad_norm_multi(TensorList([h, dlogits]), math.inf, self.sizes)
+        taken = torch.isfinite(self.sizes[0] ** 4) & torch.isfinite(self.norm[1])
+        self.norm[1].masked_fill_(~taken, math.nan)
+        head_factor = torch.where(taken, 1.0, math.nan)
+        h, dlogits = (torch.where(taken, t, 0.0) for t in (h, dlogits))
+        opt.begin_minibatch(1)
+        opt.linear_wgrad_fold(h, dlogits[:, :self.vocab], self.head_m[:, :self.vocab], self.head_v[:, :self.vocab])
         factor = self.norm[1:2]
         if self.states == 8:
             opt.fold_apply8_multi(self._w, self._g, self.moments, self.lr, w_bf16=self._copy, grad_factor=factor)
         else:
             opt.fold_apply_multi(self._w, self._g, self._m, self._v, self.lr, w_bf16=self._copy, grad_factor=factor)
-        opt.apply_bf16_copy(self.head, self.head_m, self.head_v, self.head_bf, self.lr)
+        opt.fold_apply_multi(*self._head, self.lr, w_bf16=self._head_copy, grad_factor=head_factor)
 
     def train(self, steps: int, tokens: int = 4096, every: int = 0):
         """`steps` rollouts with one update each; returns the mean reward of every rollout."""
