@@ -11,6 +11,7 @@
 
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"
+#include "policy_plan.h"
 #include "softmax_rows.cuh"
 #include "tensor_table.cuh"
 
@@ -51,8 +52,6 @@ __device__ __forceinline__ Stats group_join(Stats s, float k, Stats *slots, int 
 __device__ __forceinline__ float logp_of(float x_target, const Stats &s, float log_sum, float scale) {
     return fmaf(scale, x_target - s.top, -log_sum);
 }
-
-constexpr int kMaxCluster = 8;  // CTAs that may share a row
 
 // The slice of a row's units that CTA `rank` of 2^log_size takes (units < 2^29, so 32 bits hold it).
 __device__ __forceinline__ void slice_of(int units, int rank, int log_size, int &from, int &count) {
@@ -388,8 +387,6 @@ struct RowWriter {
 
 // One row at a time to a warp, 32 warps to an SM hide its latencies: 100000 x 2000 bf16 150 us (73 % of a
 // copy's rate), 333333 x 600 262 us (42 %), where a row's loss terms cost more than its elements.
-constexpr int kRowUnits = 8;  // units of a lane: rows of up to 4 KB
-
 template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 2)
 policy_loss_rows_kernel(const PolicyArgs a, float k) {
@@ -463,30 +460,6 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
 // between a row's statistics and its gradient lie the joins over warps and CTAs and the loss itself,
 // which one warp of its own does meanwhile, and nobody waits for them.  The ring therefore holds two
 // rows (slices).  One more warp issues the copies.
-
-// How the ring is cut: WORK threads compute, a stage holds two units of each, PER_SM such CTAs share an SM.
-template <int WORK, int STAGES, int PER_SM>
-struct RingCut {
-    static constexpr int kWork = WORK, kStages = STAGES, kPerSm = PER_SM;
-    static constexpr int kEach = 2;                              // units of a stage that a thread takes
-    static constexpr int kWarps = WORK / 32, kThreads = WORK + 64;
-    static constexpr int kProducerWarp = kWarps, kScalarWarp = kWarps + 1;
-    static constexpr int kStageUnits = kEach * WORK, kStageBytes = 16 * kStageUnits;
-    static constexpr int kSliceUnits = STAGES / 2 * kStageUnits;  // largest slice of which two fit
-
-    // stages of a slice times their units, in percent of the slice
-    static int fill_cost(int64_t slice) {
-        return (int)((slice + kStageUnits - 1) / kStageUnits * kStageUnits * 100 / slice);
-    }
-};
-// The shorter the slice, the fewer threads to it and the more CTAs to an SM: a row's joins and barriers
-// then cost fewer warps, and other rows' work hides its latencies (24390 x 8200 bf16: 238 us with 512
-// threads, 160 with 256, 132 with 128; 48828 x 4096: 149 with 128, 131 with 64).
-using Cut640 = RingCut<640, 11, 1>;  // 11 stages of 20 KB: slices of up to 6400 units
-using Cut512 = RingCut<512, 14, 1>;  // 14 of 16 KB: 7168
-using Cut256 = RingCut<256, 13, 2>;  // 13 of 8 KB: 3072
-using Cut128 = RingCut<128, 13, 4>;  // 13 of 4 KB: 1536
-using Cut64 = RingCut<64, 13, 8>;    // 13 of 2 KB: 768
 
 // What the gradient of a row needs.
 struct Verdict {
@@ -989,38 +962,21 @@ struct RingLaunch {
 template <typename T, typename O>
 cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
     const float k = (float)(a.scale_exact * kLog2e);
-    const int64_t units = a.vocab / kUnit<T>;
-    if (units <= 32 * kRowUnits) return policy_rows<T, O>(a, k, sm_count, stream);
-    // As few CTAs to a row as hold two of its slices.  Few rows are dealt out at once, one to a cluster as
-    // large as that and the row's length allow, which then has to hold one slice (33 x 131072 fp32: 8.9 us
-    // with 4 CTAs to a row, 10.9 with 8 in three turns).
-    using Ring = RingLaunch<T, O, Cut512>;
-    int cluster = 1;
-    while (cluster < kMaxCluster && (units + cluster - 1) / cluster > Cut512::kSliceUnits) cluster *= 2;
-    bool one_turn = false;
-    for (int c = kMaxCluster; c >= 1 && !one_turn; c /= 2) {
-        int most = 0;
-        const cudaError_t e = a.rows * c <= sm_count ? Ring::resident(c, sm_count, &most) : cudaSuccess;
-        if (e != cudaSuccess) return e;
-        const bool fits = (units + c - 1) / c <= Cut640::kStages * Cut640::kStageUnits;
-        if (a.rows <= most && fits && (c == 1 || units >= (int64_t)c * Cut512::kWork)) {
-            cluster = c;
-            one_turn = true;
-        }
+    PolicyPlan plan;
+    const int e = plan_policy(a.vocab / kUnit<T>, a.rows, sm_count, [&](PolicyForm form, int cluster, int *most) {
+        return (int)(form == kForm640 ? RingLaunch<T, O, Cut640>::resident(cluster, sm_count, most)
+                                      : RingLaunch<T, O, Cut512>::resident(cluster, sm_count, most));
+    }, plan);
+    if (e != 0) return (cudaError_t)e;
+    switch (plan.form) {
+        case kFormRows: return policy_rows<T, O>(a, k, sm_count, stream);
+        case kForm64: return RingLaunch<T, O, Cut64>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm128: return RingLaunch<T, O, Cut128>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm256: return RingLaunch<T, O, Cut256>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm512: return RingLaunch<T, O, Cut512>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm640: return RingLaunch<T, O, Cut640>::launch(a, k, plan.cluster, sm_count, stream);
+        case kFormLong: break;
     }
-    const int64_t slice = (units + cluster - 1) / cluster;
-    if (!one_turn && slice <= Cut64::kSliceUnits) return RingLaunch<T, O, Cut64>::launch(a, k, 1, sm_count, stream);
-    if (!one_turn && slice <= Cut128::kSliceUnits) return RingLaunch<T, O, Cut128>::launch(a, k, 1, sm_count, stream);
-    // (only whole rows: the halves of 6250 x 32000 in clusters take 129 us, whole rows with Cut512 123)
-    if (!one_turn && cluster == 1 && slice <= Cut256::kSliceUnits)
-        return RingLaunch<T, O, Cut256>::launch(a, k, 1, sm_count, stream);
-    // The two cuts of a whole SM: a stage that a row fills in part costs nearly as much as a full one, so the
-    // cut that fills better: 8192 x 50257 bf16 (6282 units, 114 % with Cut512, 102 % with Cut640) 260 and
-    // 256 us, 4096 of them with odd pitches 159 and 146; 8192 x 32000 (4000 units, 102 % and 128 %) 158 and
-    // 175 us.  On a tie the deeper ring.
-    if ((one_turn || slice <= Cut640::kSliceUnits) && Cut640::fill_cost(slice) < Cut512::fill_cost(slice))
-        return RingLaunch<T, O, Cut640>::launch(a, k, cluster, sm_count, stream);
-    if (one_turn || slice <= Cut512::kSliceUnits) return Ring::launch(a, k, cluster, sm_count, stream);
     policy_loss_long_kernel<T, O><<<grid_of(a.rows, (int64_t)sm_count * 4), kThreads, 0, stream>>>(a, k);
     return cudaGetLastError();
 }
