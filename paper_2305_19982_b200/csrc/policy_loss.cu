@@ -849,6 +849,24 @@ cudaError_t logprobs_groups(const LogprobArgs &a, float k, cudaStream_t stream) 
     return cudaGetLastError();
 }
 
+// CTAs of W warps, one row to each, that fit an SM.  Asked for once per device.
+template <typename T, int W, bool ENT>
+cudaError_t logprobs_resident(int *out) {
+    static std::atomic<int> known[64];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    int m = device < 64 ? known[device].load() : 0;
+    if (m == 0) {
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&m, token_logprobs_kernel<T, W, 1, ENT, false>, 32 * W, 0);
+        if (e != cudaSuccess) return e;
+        if (m < 1) m = 1;
+        if (device < 64) known[device].store(m);
+    }
+    *out = m;
+    return cudaSuccess;
+}
+
 int log2_of(int n) {
     int l = 0;
     while (1 << l < n) ++l;
@@ -888,12 +906,12 @@ cudaError_t logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
             while (cluster < kMaxCluster && a.rows * cluster * 2 <= sm_count && units >= cluster * 2 * kThreads) cluster *= 2;
         return cluster > 1 ? logprobs_cluster<T>(a, k, cluster, stream) : logprobs_groups<T, kWarps, 1>(a, k, stream);
     }
-    // More rows: 4 warps, of which the fewest wait at a row's end (1024 x 50257 bf16 22.0 / 24.3 / 25.3, 6000 x
-    // 20000 bf16 47.1 / 52.4 / 85.6); 8 for the numbers of rows that leave an SM with too few resident warps
-    // (450 x 50257 fp32 23.0 / 17.0 / 20.5), or at 4 warps with all its rows resident at once and so with more
-    // or fewer of them than the next SM (2048 x 128256 fp32 162.6 / 149.4 / 149.4).
-    return per_sm < 5 || (per_sm >= 10 && per_sm < 16) ? logprobs_groups<T, 8, 1>(a, k, stream)
-                                                       : logprobs_groups<T, 4, 1>(a, k, stream);
+    int resident4 = 0, resident8 = 0;
+    cudaError_t e = a.entropy ? logprobs_resident<T, 4, true>(&resident4) : logprobs_resident<T, 4, false>(&resident4);
+    if (e == cudaSuccess) e = a.entropy ? logprobs_resident<T, 8, true>(&resident8) : logprobs_resident<T, 8, false>(&resident8);
+    if (e != cudaSuccess) return e;
+    return warps_to_a_row(a.rows, sm_count, resident4, resident8) == 8 ? logprobs_groups<T, 8, 1>(a, k, stream)
+                                                                       : logprobs_groups<T, 4, 1>(a, k, stream);
 }
 
 template <typename T, typename O>
