@@ -92,10 +92,10 @@ grad_norm_kernel(const __grid_constant__ NormTable<CAP> tab, float max_norm, int
         ws->part[blockIdx.x] = sum;
         __threadfence();
         last = atomicAdd(&ws->ticket, 1u) == gridDim.x - 1;
+        if (last) __threadfence();  // the loads behind the barrier see what came before the other CTAs' tickets
     }
     __syncthreads();
     if (!last) return;
-    __threadfence();
     double all = 0.0;
     for (unsigned i = threadIdx.x; i < gridDim.x; i += kThreads) all += __ldcg(&ws->part[i]);
     all = block_sum(all, shared);

@@ -237,16 +237,17 @@ __device__ __forceinline__ void finish_stats(const PolicyArgs &a, const Sums &s,
     }
     if (count == 1) return;
     if (t < 32) {
-        if (t < 4) {
-            ws->part[4 * index + t] = sum;
-            __threadfence();
-        }
+        if (t < 4) ws->part[4 * index + t] = sum;
         __syncwarp();
-        if (t == 0) *last = atomicAdd(&ws->ticket, 1u) == count - 1;
+        if (t == 0) {  // this thread's fences cover the warp's stores before and, past the barrier, the CTA's loads behind
+            __threadfence();
+            const bool mine = atomicAdd(&ws->ticket, 1u) == count - 1;
+            if (mine) __threadfence();
+            *last = mine;
+        }
     }
     sync();
     if (!*last) return;
-    __threadfence();
     sum = 0.0;  // threads of one remainder mod 4 add up the same of the four sums
     for (unsigned i = t; i < 4 * count; i += THREADS) sum += __ldcg(&ws->part[i]);
     for (int o = 16; o >= 4; o >>= 1) sum += __shfl_down_sync(0xffffffffu, sum, o);

@@ -52,3 +52,16 @@ def test_the_verdict_on_a_row_waits_for_the_warp():
     arrive = next(i for i, line in enumerate(lines) if "barrier_arrive(shared_addr(&sh.ready" in line)
     begin = max(i for i in range(arrive) if lines[i] == "if (lane == 0) {")
     assert lines[begin - 1] == "__syncwarp();"
+
+
+@pytest.mark.parametrize("name", ["policy_loss.cu", "grad_norm.cu"])
+def test_the_thread_that_takes_the_ticket_fences_on_both_sides(name):
+    """Partial sums of other threads are stored before its fence, those of other blocks read behind one:
+    a fence of theirs before the warp or the block meets would not be ordered with the ticket."""
+    lines = _statements(name)
+    ticket = next(i for i, line in enumerate(lines) if "atomicAdd(&ws->ticket" in line)
+    assert lines[ticket - 1] == "__threadfence();" and lines[ticket + 1].startswith("if (") and "__threadfence();" in lines[ticket + 1]
+    before = lines[:ticket - 1]
+    stores = max(i for i, line in enumerate(before) if "ws->part[" in line)
+    owner = max(i for i, line in enumerate(before) if line.startswith("if (t == 0)") or line.startswith("if (threadIdx.x == 0)"))
+    assert owner < stores or "__syncwarp();" in before[stores:owner]
