@@ -320,7 +320,8 @@ ADAMA_API adama_status adama_apply_sharded_peers(adama_ctx *ctx, float *const *w
  *   grad_factor : NULL (1), or ONE fp32 in DEVICE memory that every gradient is multiplied by, e.g.
  *            adama_grad_norm.factor.  If it is NaN the kernel leaves w, m, v and the copies as they
  *            are (t has been counted all the same): a step with a non-finite gradient is skipped
- *            without a host round trip.
+ *            without a host round trip.  With N > 1 it scales the LAST gradient alone: the others are in m
+ *            and v already.  To clip a sum of micro-batches, or to skip it, sum the gradients first.
  * Any element-aligned pointers are accepted; 128-bit accesses are used for a tensor whose w, m, v
  * reach a 16-byte boundary after the same number of elements (at most 7) and whose gradient and copy
  * reach a 4-element boundary there, element accesses otherwise.  Tensors must not overlap.
@@ -339,7 +340,10 @@ ADAMA_API adama_status adama_fold_apply_multi(adama_ctx *ctx, const void *const 
  *                                             largest value 1.875
  * 2.03 B/param instead of 8.  All-zero codes and scales are the initial state m = v = 0.  Writing a
  * block puts its largest |m| and v at the largest code value, rounds the others to the nearest code
- * (ties to the even one), and never rounds a v > 0 to 0. */
+ * (ties to the even one), and never rounds a v > 0 to 0.  The relative error is 1/16 at most for a v within
+ * 31 binades of its block's largest, and for an m of 1/28672 of its block's largest |m| or more; smaller m lose
+ * precision step by step, and one under 1/458752 is held as 0 (until a gradient brings it back, such an
+ * entry's weight moves by the weight decay alone). */
 #define ADAMA_STATE8_BLOCK 256
 typedef struct adama_state8 {
     uint8_t *m_codes; /* n bytes */
@@ -389,7 +393,8 @@ ADAMA_API adama_status adama_state8_unpack_multi(adama_ctx *ctx, const adama_sta
  *     factor = max_norm/norm where norm > max_norm, else 1; NaN where norm is not finite
  * `accumulate` joins lists of different dtypes (or of several ranks, the caller having summed
  * sumsq) in one norm.  Squares are formed and summed in fp32 within up to 64 elements of a thread (13
- * roundings at most), in double from there on; entries beyond 1.8e19 count as infinite.  The result does not depend on
+ * roundings at most), in double from there on: entries from 1.8e19 on do, and many from 2.3e18 on may, count as
+ * infinite; entries below 1.1e-19 lose precision, below 2.6e-23 they add nothing.  The result does not depend on
  * scheduling.  An empty list gives norm 0, factor 1.  max_norm > 0, may be infinite (no clipping).
  * One launch for up to 1024 tensors, any element-aligned pointers.
  *   out : one adama_grad_norm in DEVICE memory, 8-byte aligned
@@ -436,7 +441,7 @@ ADAMA_API adama_status adama_token_logprobs(adama_ctx *ctx, const void *logits, 
  *   dlogits  : [rows, vocab] fp32 or bf16, pitch ld_dlogits, or NULL (loss and logp only)
  *   old_logp, ref_logp (or NULL), advantages, weights : rows fp32 each
  *   logp     : rows fp32, or NULL;   stats : 4 fp32;   workspace : ADAMA_WORKSPACE_BYTES
- * logit_scale as there, 0 <= clip_low <= 1, clip_high >= 0, kl_coef finite.  Deterministic.
+ * logit_scale as in adama_token_logprobs, 0 <= clip_low <= 1, clip_high >= 0, kl_coef finite.  Deterministic.
  * Errors: INVALID_ARG, MISALIGNED, CUDA; targets >= vocab as in adama_token_logprobs. */
 typedef struct adama_policy_args {
     const void *logits;

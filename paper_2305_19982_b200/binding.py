@@ -201,7 +201,8 @@ def _dev_ptr(t: torch.Tensor, dtype: torch.dtype, name: str) -> int:
 
 class TensorList:
     """Device pointers and sizes of a list of contiguous CUDA tensors, marshalled once for
-    repeated multi-tensor calls (keeps the tensors alive)."""
+    repeated multi-tensor calls (keeps the tensors alive).  Making one takes 0.5 us a tensor, more than
+    the call it goes to: keep it, and write gradients into the same tensors in every step."""
 
     def __init__(self, tensors, dtype=None):
         self.tensors = list(tensors)
@@ -619,7 +620,8 @@ class AdamA:
                          grad_factor: Optional[torch.Tensor] = None) -> None:
         """adama_fold_apply_multi: the mini-batch's last gradient and the update in one pass over
         lists of tensors (or TensorList objects).  `w_bf16` (list, entries may be None) receives
-        the weights as bf16; `grad_factor` is one fp32 on the device (NaN skips the step)."""
+        the weights as bf16; `grad_factor` is one fp32 on the device, which scales this last gradient
+        (NaN skips the update; what earlier micro-batches folded stays in m and v)."""
         ws, grads = self._list(ws, torch.float32), self._list(grads)
         ms, vs = self._list(ms, torch.float32), self._list(vs, torch.float32)
         if not ws.sizes == grads.sizes == ms.sizes == vs.sizes:

@@ -4,8 +4,8 @@
 // with g times an optional factor (gradient clipping) that lies in device memory.  With one
 // micro-batch a mini-batch this is a whole AdamW step: 26 B/param (bf16 gradient) instead of the
 // 18 + 24 of a fold and an apply.  Same arithmetic as those two, bit for bit.
-// Bound by HBM: 369 M parameters in 144 tensors (bf16 gradients, 9.6 GB) take 1504 us = 6.38 TB/s, 98 % of
-// a copy's rate; 30.7 M with the bf16 copy 135.5 us (97 %).  A list too short to stream is one launch's
+// Bound by HBM: 369 M parameters in 144 tensors (bf16 gradients, 9.6 GB) take 1478-1504 us = 6.38-6.49 TB/s, 99 to
+// 100 % of a copy's rate; 30.7 M with the bf16 copy 135.5 us (97 %).  A list too short to stream is one launch's
 // latency: 64 tensors of 1600 to 6400 elements 2.9 us.
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"

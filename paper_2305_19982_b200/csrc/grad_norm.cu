@@ -1,8 +1,9 @@
 // Global 2-norm of a list of gradients, and the clip factor that follows from it, left on the
 // device for the step that multiplies by it.  One pass, 2 or 4 B/element; each CTA's sum goes to
 // the workspace as a double, the last CTA to finish adds them in the CTAs' order, so that the
-// result does not depend on scheduling.  Bound by HBM: 369 M bf16 gradients take 107.9 us = 6.84 TB/s
-// (reads alone run above a copy's rate); 150 short tensors 4.9 us, two dependent reductions.
+// result does not depend on scheduling.  Bound by HBM: 369 M bf16 gradients take 107.4 us = 6.87 TB/s
+// (reads alone run above a copy's rate); 16 M 9.4 us, twice their floor: launch, first loads and two
+// dependent reductions are not yet hidden by so few bytes; 150 short tensors 5.0-5.5 us, nothing but these.
 #include "softmax_rows.cuh"
 #include "tensor_table.cuh"
 

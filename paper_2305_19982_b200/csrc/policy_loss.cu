@@ -7,7 +7,8 @@
 // A row is read once (loss: and its gradient written once).  Beside HBM the exponentials count, one per
 // element for the statistics and one for the gradient, at 16 per clock and SM.  Log-probabilities of 4096 rows
 // of 50304 bf16 with entropy: 69 us = 5.98 TB/s; loss and gradient of 8192 rows of 50257, a quarter of them
-// masked: 256 us = 5.6 TB/s, of 32768-wide rows 6.2 TB/s; one row of 50257 fp32: 3.8 us.
+// masked: 256 us = 5.6 TB/s, of 6103 rows of 32768, which fill the ring's stages, 117 us = 6.0 TB/s; the
+// log-probability of one row of 50257 fp32: 3.9 us.
 
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"
@@ -386,8 +387,10 @@ struct RowWriter {
 
 // ---- rows that fit a warp's registers -----------------------------------------------------------
 
-// One row at a time to a warp, 32 warps to an SM hide its latencies: 100000 x 2000 bf16 150 us (73 % of a
-// copy's rate), 333333 x 600 262 us (42 %), where a row's loss terms cost more than its elements.
+// One row at a time to a warp, 32 warps to an SM hide its latencies: 100000 x 2000 bf16 143 us (76 % of a
+// copy's rate), 333333 x 600 248 us (44 %).  What holds these back is no floor: all 32 lanes compute the row's
+// loss terms (a logarithm, two exponentials, a division) once per row, and a lane's eight units leave 64
+// registers too few (72 to 104 bytes spilled).
 template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 2)
 policy_loss_rows_kernel(const PolicyArgs a, float k) {

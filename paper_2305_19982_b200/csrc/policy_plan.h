@@ -98,7 +98,7 @@ int plan_policy(int64_t units, int64_t rows, int sm_count, Resident resident, Po
 // less of a last turn that is not full.  So 8 where that leaves fewer places unused, up to two turns of the
 // smaller ones; then turns no longer tell.  With entropy, us with 4 / 8 warps, fp32 of 128256: 740 rows 65.6 /
 // 57.4, 800 68.2 / 78.5, 1480 109.2 / 109.5, 1600 150.9 / 133.2, 2048 166.3 / 151.3, 2368 177.9 / 184.4; bf16 of
-// 50257: 592 rows 17.8 / 15.7, 1024 23.1 / 25.4, 1480 29.7 / 31.8, 2048 43.3 / 41.0, 4096 70.9 / 72.3.  Of 190 such
+// 50257: 592 rows 17.8 / 15.7, 1024 23.1 / 25.4, 1480 29.7 / 31.8, 2048 43.3 / 41.0, 4096 70.9 / 72.3.  Of 189 such
 // points (444 to 4096 rows of 13000 to 128256) the choice costs 0.3 % over the better of the two on average, at
 // most 8 % (3000 fp32 rows: 251.0 and 232.6); without entropy 0.4 % and 8 %.  16 warps are faster still at some
 // points (1600 and 3000 of those rows: 119.9 and 216.9) and slower at most.

@@ -2,7 +2,9 @@
 //     m = M * sm   M: e4m3 (sign, 4 exponent bits, 3 mantissa bits), largest 448
 //     v = V * sv   V: unsigned, 5 exponent bits, 3 mantissa bits, (1 + c%8/8) * 2^(c/8 - 31), largest 1.875
 // Adam divides m by sqrt(v), element by element, so both need relative, not absolute, precision:
-// 1/16 at most for m; for sqrt(v) half of v's 1/16, over the 31 binades of v that a block spans.
+// 1/16 at most for an m of 1/28672 of its block's largest or more (e4m3's normal numbers, 15 binades); below,
+// e4m3's subnormals lose precision, and an m under 1/458752 of the largest becomes 0.  For sqrt(v) half of v's
+// 1/16, over the 31 binades of v that a block spans.
 // A v that is not zero never becomes code 0 (it would divide m by eps alone): the smallest code
 // stands in.  The decay of Algorithm 2 multiplies the block's scale and leaves the codes alone:
 // 0.999 of a code value would round back to it for ever.
