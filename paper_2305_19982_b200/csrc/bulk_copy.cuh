@@ -4,6 +4,8 @@
 
 #include <stdint.h>
 
+#include "adama_internal.h"
+
 namespace adama {
 
 __device__ __forceinline__ uint32_t shared_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -40,16 +42,23 @@ constexpr unsigned long long kBulkWaitLimitNs = 2000000000ull;
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int *give_up) {
     if (barrier_poll(bar, parity)) return true;
     const unsigned long long t0 = now_ns();
+    bool late = false;
     for (uint32_t spins = 1;; ++spins) {
         if (barrier_poll(bar, parity)) return true;
         if ((spins & 0x3f) == 0) {
             if (*give_up) return false;
-            if (now_ns() - t0 > kBulkWaitLimitNs) {
+            if (late) {  // and not in these looks either: it is not this thread that was held up
                 *give_up = 1;
                 return false;
             }
+            late = now_ns() - t0 > kBulkWaitLimitNs;
         }
     }
+}
+
+// For one lane of every warp at its end: the warp whose wait ran out may be the last one of its CTA.
+__device__ __forceinline__ void report_expired_wait(const volatile int *give_up, unsigned *status, unsigned site) {
+    if (*give_up && atomicCAS(status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk) status[1] = site;
 }
 
 // `bytes` (a multiple of 16) from global `src` to shared `dst`, both 16-byte aligned

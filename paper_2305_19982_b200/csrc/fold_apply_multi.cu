@@ -232,6 +232,7 @@ fold_apply_ring_kernel(const __grid_constant__ StepTable<CAP> tab, FoldConstants
                 barrier_wait(shared_addr(&sh.full[slot]), parity, &none);
             }
         }
+        report_expired_wait(&sh.give_up, status, kWaitStepRing);
         return;
     }
     for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x, advance()) {
@@ -274,9 +275,7 @@ fold_apply_ring_kernel(const __grid_constant__ StepTable<CAP> tab, FoldConstants
         const size_t done = tab.bulk[t] ? base + loaded : head == kScalar ? base : end > base ? base + (end - base) / 4 * 4 : end;
         scalar_run(g, w, m, v, copy, done + tid, end, kRingWork, factor, f, c);
     }
-    if (tid == 0 && *(volatile int *)&sh.give_up &&
-        atomicCAS(status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
-        status[1] = kWaitStepRing;
+    if (lane == 0) report_expired_wait(&sh.give_up, status, kWaitStepRing);
 }
 
 // Elements before w, m, v are at a 16-byte boundary, the gradient at one too (bulk copies need it) or

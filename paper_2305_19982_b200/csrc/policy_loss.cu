@@ -562,6 +562,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                     c.slot = c.slot ? c.slot - 1 : kStages - 1;
                     barrier_wait(shared_addr(&sh.full[c.slot]), c.parity, &none);
                 }
+                report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
             }
         }
     } else if (warp == Cut::kScalarWarp) {
@@ -622,9 +623,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             if (has_extra && a.dlogits) y[extra] = out.value(x_extra, extra == in.target);
             ++n;
         }
-        if (lane == 0 && *(volatile int *)&sh.give_up &&
-            atomicCAS(a.status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
-            a.status[1] = kWaitPolicyRing;
+        if (lane == 0) report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
         __syncwarp();
         if (rank == 0) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, (unsigned)first, (unsigned)step);
     } else {
@@ -766,6 +765,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             ++n;
         }
         if (due >= 0) write_due();
+        if (lane == 0) report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
     }
     if (cluster > 1) {
         __syncwarp();

@@ -355,6 +355,7 @@ fold_apply8_ring_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f
                 barrier_wait(shared_addr(&sh.full[slot]), parity, &none);
             }
         }
+        if (lane == 0) report_expired_wait(&sh.give_up, status, kWaitState8Ring);
         return;
     }
     for (unsigned chunk = blockIdx.x; chunk < total; chunk += gridDim.x, advance()) {
@@ -390,9 +391,7 @@ fold_apply8_ring_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f
                 block_direct(static_cast<const G *>(tab.g[t]), tab.w[t], tab.copy[t], s, at, n, false, lane, factor, f, c);
         }
     }
-    if (threadIdx.x == 0 && *(volatile int *)&sh.give_up &&
-        atomicCAS(status, (unsigned)kDevOk, (unsigned)kDevTimeout) == (unsigned)kDevOk)
-        status[1] = kWaitState8Ring;
+    if (lane == 0) report_expired_wait(&sh.give_up, status, kWaitState8Ring);
 }
 
 template <int CAP>

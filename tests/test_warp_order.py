@@ -65,3 +65,24 @@ def test_the_thread_that_takes_the_ticket_fences_on_both_sides(name):
     stores = max(i for i, line in enumerate(before) if "ws->part[" in line)
     owner = max(i for i, line in enumerate(before) if line.startswith("if (t == 0)") or line.startswith("if (threadIdx.x == 0)"))
     assert owner < stores or "__syncwarp();" in before[stores:owner]
+
+
+@pytest.mark.parametrize("name,warps,threads", [("fold_apply_multi.cu", 1, 1), ("state8.cu", 2, 0), ("policy_loss.cu", 2, 1)])
+def test_whichever_warp_gives_up_reports_it(name, warps, threads):
+    """Not one chosen warp, which may have finished before: each role ends with a report, by one lane of the
+    warp, or by the one thread that issues the copies."""
+    calls = [line for line in _statements(name) if "report_expired_wait(" in line]
+    assert sum(line.startswith("if (lane == 0) report_expired_wait(") for line in calls) == warps
+    assert sum(line.startswith("report_expired_wait(") for line in calls) == threads
+    assert len(calls) == warps + threads
+
+
+def test_a_wait_looks_again_before_it_gives_up():
+    """A block that was held up itself for longer than the limit finds its barrier complete: the clock is read
+    last of all in a round of looks, and the flag is set a round later."""
+    lines = _statements("bulk_copy.cuh")
+    late = next(i for i, line in enumerate(lines) if line.startswith("late = now_ns() - t0 > kBulkWaitLimitNs"))
+    begin = max(i for i in range(late) if lines[i].startswith("for ("))
+    loop = lines[begin:late]
+    assert loop.index("if (barrier_poll(bar, parity)) return true;") < loop.index("*give_up = 1;")
+    assert any(line.startswith("if (late)") for line in loop) and sum("give_up = 1" in line for line in lines) == 1
