@@ -465,6 +465,114 @@ ADAMA_API adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args
  * caller who keeps a workspace per stream tells graphs apart by.  Ids are unique in the process. */
 ADAMA_API uint64_t adama_stream_capture_id(void *cuda_stream);
 
+/* ---- norms and embeddings ----------------------------------------------------------------- */
+
+/* Layer norm over the rows of a matrix:
+ *     mean = sum_j x_j / dim,  rstd = 1/sqrt(sum_j (x_j - mean)^2 / dim + eps)
+ *     y_j = (x_j - mean)*rstd*weight_j + bias_j
+ * in fp32, y rounded once.
+ *   x : [rows, dim] fp32 or bf16, row pitch ld_x elements (>= dim), read-only unless y is the same buffer
+ *   y : [rows, dim] fp32 or bf16, row pitch ld_y; may be x itself, with equal dtype and pitch
+ *   weight, bias : dim fp32 each, contiguous; bias may be NULL (0)
+ *   mean, rstd   : rows fp32 each, what the backward pass reads; each may be NULL
+ * Any dim >= 1, any element-aligned pointers and pitches.  eps >= 0.  rows = 0 is a no-op.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED (2^31 rows or more), CUDA. */
+typedef struct adama_layer_norm_args {
+    const void *x;
+    void *y;
+    adama_dtype x_dtype, y_dtype;
+    int64_t rows, dim, ld_x, ld_y;
+    const float *weight;
+    const float *bias;
+    double eps;
+    float *mean;
+    float *rstd;
+} adama_layer_norm_args;
+ADAMA_API adama_status adama_layer_norm(adama_ctx *ctx, const adama_layer_norm_args *args,
+                                        void *cuda_stream);
+
+/* Its backward pass.  With xhat = (x - mean)*rstd and g = dy*weight,
+ *     dx = rstd*(g - sum_j g_j / dim - xhat * sum_j g_j xhat_j / dim)
+ *     G_weight = sum over rows of dy*xhat,   G_bias = sum over rows of dy
+ * The two parameters' gradients are written (dweight, dbias), folded into their moments as adama_fold
+ * does (m += a*G, v += b*G^2; the sum over rows is complete before it is squared, and is never written),
+ * or both.
+ *   dy : [rows, dim] fp32 or bf16, pitch ld_dy;   x : as in the forward pass
+ *   dx : [rows, dim] of x's dtype, pitch ld_dx, or NULL; may be dy or x itself, with equal dtype and pitch
+ *   mean, rstd : of the forward pass
+ *   dweight, dbias : dim fp32 each, overwritten, or NULL
+ *   m_weight, v_weight, m_bias, v_bias : dim fp32 each, in place; a pair is given whole or not at all
+ *   workspace : adama_layer_norm_workspace(ctx, rows, dim) bytes of device memory, 16-byte aligned, that no
+ *               other call uses at the same time; its contents do not matter.  NULL where no parameter's
+ *               gradient is wanted and dim <= 8192
+ * With rows = 0 dweight and dbias are 0 and nothing else changes.  Deterministic.
+ * Errors: INVALID_ARG, BAD_STATE (moments without adama_begin_minibatch), MISALIGNED, UNSUPPORTED, CUDA. */
+typedef struct adama_layer_norm_backward_args {
+    const void *dy;
+    const void *x;
+    void *dx;
+    adama_dtype dy_dtype, x_dtype;
+    int64_t rows, dim, ld_dy, ld_x, ld_dx;
+    const float *weight;
+    const float *mean;
+    const float *rstd;
+    float *dweight;
+    float *dbias;
+    float *m_weight;
+    float *v_weight;
+    float *m_bias;
+    float *v_bias;
+    void *workspace;
+} adama_layer_norm_backward_args;
+ADAMA_API adama_status adama_layer_norm_backward(adama_ctx *ctx, const adama_layer_norm_backward_args *args,
+                                                 void *cuda_stream);
+/* Bytes of the workspace of such a call; 0 for arguments that it would refuse. */
+ADAMA_API size_t adama_layer_norm_workspace(const adama_ctx *ctx, int64_t rows, int64_t dim);
+
+/* Embedding lookup, out[t] = scale*table[ids[t]], rounded once.
+ *   ids   : tokens int64, device.  A negative one gives a row of zeros; one >= vocab gives NaN, and the
+ *           next adama_sync_status reports INVALID_ARG
+ *   table : [vocab, dim] fp32 or bf16, pitch ld_table;   out : [tokens, dim] fp32 or bf16, pitch ld_out
+ * Any dim >= 1, any element-aligned pointers and pitches.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+typedef struct adama_embedding_args {
+    const int64_t *ids;
+    const void *table;
+    void *out;
+    adama_dtype table_dtype, out_dtype;
+    int64_t tokens, vocab, dim, ld_table, ld_out;
+    double scale;
+} adama_embedding_args;
+ADAMA_API adama_status adama_embedding(adama_ctx *ctx, const adama_embedding_args *args, void *cuda_stream);
+
+/* Its gradient, G[i] = scale * sum over t with ids[t] = i of dy[t], summed in fp32 over tokens sorted by id
+ * (equal ones in their order, in groups that do not depend on scheduling):
+ *   - into a table: grad = G (rows without tokens become 0), or with `accumulate` grad = grad + G (rows
+ *     without tokens are left alone), rounded once; or
+ *   - into moments: m += a*G, v += b*G^2 as adama_fold.  Rows without tokens are not touched, so a call costs
+ *     its tokens, not the vocabulary; G is never written.
+ * ids < 0 have no part; ids >= vocab neither, and are reported as by adama_embedding.
+ *   dy   : [tokens, dim] fp32 or bf16, pitch ld_dy
+ *   grad : [vocab, dim] fp32 or bf16 (grad_dtype), pitch ld_grad;  m, v : the same in fp32, both with pitch
+ *          ld_grad.  Either grad is given or both moments are
+ *   workspace : adama_embedding_workspace(ctx, tokens, dim) bytes, as for adama_layer_norm_backward
+ * Errors: INVALID_ARG, BAD_STATE (moments without adama_begin_minibatch), MISALIGNED, UNSUPPORTED, CUDA. */
+typedef struct adama_embedding_grad_args {
+    const int64_t *ids;
+    const void *dy;
+    adama_dtype dy_dtype, grad_dtype;
+    int64_t tokens, vocab, dim, ld_dy, ld_grad;
+    double scale;
+    void *grad;
+    float *m;
+    float *v;
+    int64_t accumulate;
+    void *workspace;
+} adama_embedding_grad_args;
+ADAMA_API adama_status adama_embedding_grad(adama_ctx *ctx, const adama_embedding_grad_args *args,
+                                            void *cuda_stream);
+/* Bytes of the workspace of such a call; 0 for arguments that it would refuse. */
+ADAMA_API size_t adama_embedding_workspace(const adama_ctx *ctx, int64_t tokens, int64_t dim);
+
 /* ---- host-buffer variants (same arithmetic, copies included) --------------------------- */
 
 /* adama_fold with the gradient in HOST memory (pinned memory for full copy
@@ -599,7 +707,8 @@ ADAMA_API adama_status adama_set_weight_decay(adama_ctx *ctx, double weight_deca
 /* Waits for `cuda_stream`, then reads the device status block.  Returns ADAMA_OK,
  * ADAMA_ERR_TIMEOUT (a bounded wait inside a kernel expired: the fused weight gradient, a streamed
  * update or the policy loss, as adama_last_error says; what that call writes is incomplete),
- * ADAMA_ERR_INVALID_ARG (a row of adama_token_logprobs or adama_policy_loss had a target >= vocab) or
+ * ADAMA_ERR_INVALID_ARG (a row of adama_token_logprobs or adama_policy_loss had a target >= vocab, or an
+ * embedding call an id) or
  * ADAMA_ERR_CUDA.  Each call reports and clears one of them, an expired wait first: call again for the other. */
 ADAMA_API adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream);
 

@@ -28,6 +28,8 @@ EXPORTED_SYMBOLS = [
     "adama_version",
     "adama_fold_apply_multi", "adama_fold_apply8_multi", "adama_state8_pack_multi", "adama_state8_unpack_multi",
     "adama_grad_norm_multi", "adama_token_logprobs", "adama_policy_loss", "adama_stream_capture_id",
+    "adama_layer_norm", "adama_layer_norm_backward", "adama_layer_norm_workspace",
+    "adama_embedding", "adama_embedding_grad", "adama_embedding_workspace",
 ]
 
 
@@ -71,6 +73,13 @@ class _State8(ctypes.Structure):
 # adama_policy_args in native layout: logits, dlogits, two dtypes, rows, vocab, two pitches, five per-row
 # pointers, four doubles, logp, stats, workspace (packing costs a third of filling a ctypes structure)
 _POLICY_ARGS = struct.Struct("@PPii4qPPPPP4dPPP")
+
+
+# adama_layer_norm_args, adama_layer_norm_backward_args, adama_embedding_args, adama_embedding_grad_args
+_LAYER_NORM_ARGS = struct.Struct("@PPii4qPPdPP")
+_LAYER_NORM_BACKWARD_ARGS = struct.Struct("@PPPii5q10P")
+_EMBEDDING_ARGS = struct.Struct("@PPPii5qd")
+_EMBEDDING_GRAD_ARGS = struct.Struct("@PPii5qdPPPqP")
 
 
 class _Config(ctypes.Structure):
@@ -142,6 +151,11 @@ def load_library() -> ctypes.CDLL:
     L.adama_grad_norm_multi.argtypes = [vp, vp, ci, vp, ci, dbl, ci, vp, vp, vp]
     L.adama_token_logprobs.argtypes = [vp, vp, ci, i64, i64, i64, vp, dbl, vp, vp, vp, vp]
     L.adama_policy_loss.argtypes = [vp, ctypes.c_char_p, vp]
+    for name in ("layer_norm", "layer_norm_backward", "embedding", "embedding_grad"):
+        getattr(L, "adama_" + name).argtypes = [vp, ctypes.c_char_p, vp]
+    for name in ("layer_norm", "embedding"):
+        getattr(L, f"adama_{name}_workspace").argtypes = [vp, i64, i64]
+        getattr(L, f"adama_{name}_workspace").restype = sz
     L.adama_stream_capture_id.argtypes = [vp]
     L.adama_stream_capture_id.restype = ctypes.c_uint64
     L.adama_get_step.argtypes = [vp]
@@ -280,6 +294,7 @@ class AdamA:
         self._L = load_library()
         self._h = ctypes.c_void_p()
         self._workspaces, self._captured = {}, {}
+        self._scratches, self._captured_scratches, self._scratch_bytes = {}, {}, {}
         self.device = torch.device("cuda", int(device))
         cfg = _Config(beta1, beta2, eps, int(device),
                       (GRADS_PRESCALED if grads_prescaled else 0) |
@@ -734,6 +749,127 @@ class AdamA:
             _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream))
         self._check(self._L.adama_policy_loss(self._h, args, stream))
 
+    # -- norms and embeddings ----------------------------------------------------------------
+    def _scratch(self, stream: int, of: str, rows: int, dim: int) -> int:
+        """Workspace of a call over rows x dim, whose size adama_<of>_workspace gives: one buffer for each stream,
+        made anew where a call needs more; while the stream is being captured into a graph, one of that graph's
+        own from its memory.  What it holds between calls does not matter."""
+        need = self._scratch_bytes.get((of, rows, dim))
+        if need is None:
+            if len(self._scratch_bytes) >= 1024:
+                self._scratch_bytes.clear()
+            need = self._scratch_bytes[of, rows, dim] = max(16, getattr(self._L, f"adama_{of}_workspace")(self._h, rows, dim))
+        if stream:  # the legacy default stream cannot be captured
+            capture = self._L.adama_stream_capture_id(stream)
+            if capture:
+                known, t = self._captured_scratches.get(stream, (0, None))
+                if known != capture or t.numel() < need:
+                    t = torch.empty(need, dtype=torch.uint8, device=self.device)
+                    self._captured_scratches[stream] = (capture, t)
+                return t.data_ptr()
+        t = self._scratches.get(stream)
+        if t is None or t.numel() < need:
+            t = self._scratches[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return t.data_ptr()
+
+    @staticmethod
+    def _vector(t: Optional[torch.Tensor], n: int, name: str) -> int:
+        """Pointer of a contiguous fp32 vector of n elements; 0 for None."""
+        if t is None:
+            return 0
+        if t.dtype is torch.float32 and t.is_cuda and t.numel() == n and t.is_contiguous():
+            return t.data_ptr()
+        _dev_ptr(t, torch.float32, name)
+        raise ValueError(f"{name} must be contiguous with {n} elements")
+
+    def layer_norm(self, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor,
+                   mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, eps: float = 1e-5) -> None:
+        """adama_layer_norm: y = (x - mean)*rstd*weight + bias over the rows of `x` [rows, dim] (fp32 or bf16, as
+        is `y`, which may be `x` itself); `mean` and `rstd` (fp32) receive what the backward pass reads."""
+        ptr, dt, ld = self._rows(x, "x")
+        yptr, ydt, yld = self._rows(y, "y")
+        rows, dim = x.shape
+        if y.shape != x.shape:
+            raise ValueError("y must have the shape of x")
+        vector = self._vector
+        args = _LAYER_NORM_ARGS.pack(ptr, yptr, dt, ydt, rows, dim, ld, yld, vector(weight, dim, "weight"), vector(bias, dim, "bias"),
+                                     eps, vector(mean, rows, "mean"), vector(rstd, rows, "rstd"))
+        self._check(self._L.adama_layer_norm(self._h, args, _stream_ptr(self.device)))
+
+    def _layer_norm_backward(self, dy, x, weight, mean, rstd, dx, *params) -> None:
+        dyptr, dydt, dyld = self._rows(dy, "dy")
+        ptr, dt, ld = self._rows(x, "x")
+        rows, dim = x.shape
+        dxptr, dxld = 0, dim
+        if dx is not None:
+            if dx.dtype != x.dtype:
+                raise TypeError("dx must have the dtype of x")
+            dxptr, _, dxld = self._rows(dx, "dx")
+        if dy.shape != x.shape or (dx is not None and dx.shape != x.shape):
+            raise ValueError("dy and dx must have the shape of x")
+        vector, names = self._vector, ("dweight", "dbias", "m_weight", "v_weight", "m_bias", "v_bias")
+        stream = _stream_ptr(self.device)
+        args = _LAYER_NORM_BACKWARD_ARGS.pack(
+            dyptr, ptr, dxptr, dydt, dt, rows, dim, dyld, ld, dxld, vector(weight, dim, "weight"), vector(mean, rows, "mean"),
+            vector(rstd, rows, "rstd"), *[vector(t, dim, n) for t, n in zip(params, names)],
+            self._scratch(stream, "layer_norm", rows, dim))
+        self._check(self._L.adama_layer_norm_backward(self._h, args, stream))
+
+    def layer_norm_backward(self, dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                            dx: Optional[torch.Tensor], dweight: Optional[torch.Tensor] = None,
+                            dbias: Optional[torch.Tensor] = None) -> None:
+        """adama_layer_norm_backward: the gradient of `x` into `dx` (its dtype; may be `dy` or `x` itself, or
+        None), those of weight and bias into `dweight` and `dbias` (fp32; None where not wanted)."""
+        self._layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, None, None, None, None)
+
+    def layer_norm_backward_fold(self, dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                                 dx: Optional[torch.Tensor], m_weight: torch.Tensor, v_weight: torch.Tensor,
+                                 m_bias: Optional[torch.Tensor] = None, v_bias: Optional[torch.Tensor] = None) -> None:
+        """adama_layer_norm_backward with the parameters' gradients folded into their moments."""
+        self._layer_norm_backward(dy, x, weight, mean, rstd, dx, None, None, m_weight, v_weight, m_bias, v_bias)
+
+    def embedding(self, ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0) -> None:
+        """adama_embedding: out[t] = scale*table[ids[t]] (int64 ids; negative = a row of zeros)."""
+        ptr, dt, ld = self._rows(table, "table")
+        optr, odt, old = self._rows(out, "out")
+        vocab, dim = table.shape
+        tokens = out.shape[0]
+        if out.shape[1] != dim:
+            raise ValueError("out must be [tokens, dim]")
+        args = _EMBEDDING_ARGS.pack(self._per_row(ids, tokens, "ids", torch.int64), ptr, optr, dt, odt, tokens, vocab, dim, ld, old, scale)
+        self._check(self._L.adama_embedding(self._h, args, _stream_ptr(self.device)))
+
+    def _embedding_grad(self, ids, dy, target, v, scale, accumulate) -> None:
+        ptr, dt, ld = self._rows(dy, "dy")
+        tptr, tdt, tld = self._rows(target, "grad" if v is None else "m")
+        (tokens, dim), (vocab, width) = dy.shape, target.shape
+        if width != dim:
+            raise ValueError("rows of dy and of the table must have the same length")
+        vptr = 0
+        if v is not None:
+            vptr, vdt, vld = self._rows(v, "v")
+            if v.shape != target.shape or vld != tld:
+                raise ValueError("m and v must have one shape and one row pitch")
+            if tdt != F32 or vdt != F32:
+                raise TypeError("m and v must be float32")
+        stream = _stream_ptr(self.device)
+        args = _EMBEDDING_GRAD_ARGS.pack(
+            self._per_row(ids, tokens, "ids", torch.int64), ptr, dt, tdt, tokens, vocab, dim, ld, tld, scale,
+            tptr if v is None else 0, tptr if v is not None else 0, vptr, int(accumulate),
+            self._scratch(stream, "embedding", tokens, dim))
+        self._check(self._L.adama_embedding_grad(self._h, args, stream))
+
+    def embedding_grad(self, ids: torch.Tensor, dy: torch.Tensor, grad: torch.Tensor, scale: float = 1.0,
+                       accumulate: bool = False) -> None:
+        """adama_embedding_grad: the table's gradient into `grad` [vocab, dim] (fp32 or bf16), every row of it, or
+        with `accumulate` added to the rows that occur."""
+        self._embedding_grad(ids, dy, grad, None, scale, accumulate)
+
+    def embedding_grad_fold(self, ids: torch.Tensor, dy: torch.Tensor, m: torch.Tensor, v: torch.Tensor, scale: float = 1.0) -> None:
+        """adama_embedding_grad into moments: the table's gradient folded into `m` and `v` [vocab, dim] fp32, of
+        which only the rows that occur are touched."""
+        self._embedding_grad(ids, dy, m, v, scale, False)
+
     # -- host-buffer variants ---------------------------------------------------------------
     def fold_host(self, grad_host: torch.Tensor, m: torch.Tensor, v: torch.Tensor,
                   staging: torch.Tensor) -> None:
@@ -794,7 +930,7 @@ class AdamA:
 
     def sync_status(self) -> None:
         """Waits for the current stream and raises AdamAError: ERR_TIMEOUT if a bounded device-side wait
-        expired, else ERR_INVALID_ARG if a row of logits had a target outside the vocabulary.  One report
+        expired, else ERR_INVALID_ARG if a call was given a target or an id outside the vocabulary.  One report
         a call, which clears it."""
         self._check(self._L.adama_sync_status(self._h, _stream_ptr(self.device)))
 

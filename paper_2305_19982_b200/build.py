@@ -14,7 +14,8 @@ CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libadama.so"
 SOURCES = ["adama_api.cu", "fold_apply.cu", "multi_tensor.cu", "bias_grad.cu", "peer_apply.cu", "extensions.cu",
-           "wgrad_fold.cu", "fold_apply_multi.cu", "state8.cu", "grad_norm.cu", "policy_loss.cu"]
+           "wgrad_fold.cu", "fold_apply_multi.cu", "state8.cu", "grad_norm.cu", "policy_loss.cu",
+           "layer_norm.cu", "embedding.cu"]
 
 
 def _nvcc() -> str:
@@ -35,7 +36,7 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     """Compile every CUDA source of the library for sm_100a and link libadama.so."""
     if not force and not _stale():
         return LIB
-    cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo",
+    cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "--threads", "0",
            "-gencode", "arch=compute_100a,code=sm_100a",
            "-shared", "-Xcompiler", "-fPIC,-fvisibility=hidden",
            "-cudart", "static",

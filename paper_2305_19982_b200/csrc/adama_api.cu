@@ -810,6 +810,227 @@ adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args *p, void 
     return ADAMA_OK;
 }
 
+// ---- norms and embeddings ---------------------------------------------------------------------
+
+// A [rows, cols] matrix of a call: what is wrong with it, or OK.
+static adama_status check_matrix(adama_ctx *ctx, const char *call, const char *name, const void *p, adama_dtype dt,
+                                 int64_t rows, int64_t cols, int64_t ld) {
+    char msg[160];
+    adama_status st = ADAMA_OK;
+    const char *what = "";
+    if (dt != ADAMA_F32 && dt != ADAMA_BF16) {
+        st = ADAMA_ERR_INVALID_ARG;
+        what = "has an unknown dtype";
+    } else if (rows > 0 && !p) {
+        st = ADAMA_ERR_INVALID_ARG;
+        what = "is a null pointer";
+    } else if (ld < cols) {
+        st = ADAMA_ERR_INVALID_ARG;
+        what = "has a row pitch smaller than the row";
+    } else if (rows > 0 && ld > INT64_MAX / 8 / rows) {
+        st = ADAMA_ERR_UNSUPPORTED;
+        what = "is larger than the address space";
+    } else if (!aligned_to(p, dtype_size(dt))) {
+        st = ADAMA_ERR_MISALIGNED;
+        what = "is not aligned to its element size";
+    }
+    if (st == ADAMA_OK) return st;
+    snprintf(msg, sizeof(msg), "%s: %s %s", call, name, what);
+    return fail(ctx, st, msg);
+}
+
+static adama_status check_rows(adama_ctx *ctx, const char *call, int64_t rows, int64_t dim) {
+    char msg[96];
+    const bool large = rows > INT32_MAX || dim > INT32_MAX / 2;
+    if (rows >= 0 && dim >= 1 && !large) return ADAMA_OK;
+    snprintf(msg, sizeof(msg), large ? "%s: 2^31 rows or 2^30 columns or more" : "%s: bad shape", call);
+    return fail(ctx, large ? ADAMA_ERR_UNSUPPORTED : ADAMA_ERR_INVALID_ARG, msg);
+}
+
+adama_status adama_layer_norm(adama_ctx *ctx, const adama_layer_norm_args *p, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (!p) return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm: null arguments");
+    adama_status st = check_rows(ctx, "layer_norm", p->rows, p->dim);
+    if (st == ADAMA_OK) st = check_matrix(ctx, "layer_norm", "x", p->x, p->x_dtype, p->rows, p->dim, p->ld_x);
+    if (st == ADAMA_OK) st = check_matrix(ctx, "layer_norm", "y", p->y, p->y_dtype, p->rows, p->dim, p->ld_y);
+    if (st != ADAMA_OK) return st;
+    if (!p->weight) return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm: null weight");
+    if (!(p->eps >= 0.0) || !(p->eps <= FLT_MAX)) return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm: eps must be finite and >= 0");
+    if (p->y == p->x && p->rows > 0 && (p->y_dtype != p->x_dtype || p->ld_y != p->ld_x))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm: in place needs one dtype and one pitch");
+    if (!aligned_to(p->weight, 4) || !aligned_to(p->bias, 4) || !aligned_to(p->mean, 4) || !aligned_to(p->rstd, 4))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "layer_norm: pointer not aligned to 4 bytes");
+    if (p->rows == 0) return ADAMA_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    adama::NormArgs a;
+    a.x = p->x;
+    a.y = p->y;
+    a.x_dtype = p->x_dtype;
+    a.y_dtype = p->y_dtype;
+    a.rows = p->rows;
+    a.ld_x = p->ld_x;
+    a.ld_y = p->ld_y;
+    a.dim = (int)p->dim;
+    a.weight = p->weight;
+    a.bias = p->bias;
+    a.eps = (float)p->eps;
+    a.mean = p->mean;
+    a.rstd = p->rstd;
+    cudaError_t e = adama::launch_layer_norm(a, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(ctx, "layer_norm launch", e);
+    ctx->launches += 1;
+    return ADAMA_OK;
+}
+
+size_t adama_layer_norm_workspace(const adama_ctx *ctx, int64_t rows, int64_t dim) {
+    if (!ctx || rows < 0 || rows > INT32_MAX || dim < 1 || dim > INT32_MAX / 2) return 0;
+    return adama::norm_workspace_bytes(rows, (int)dim, ctx->sm_count);
+}
+
+adama_status adama_layer_norm_backward(adama_ctx *ctx, const adama_layer_norm_backward_args *p, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (!p) return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm_backward: null arguments");
+    const char *const call = "layer_norm_backward";
+    adama_status st = check_rows(ctx, call, p->rows, p->dim);
+    if (st == ADAMA_OK) st = check_matrix(ctx, call, "dy", p->dy, p->dy_dtype, p->rows, p->dim, p->ld_dy);
+    if (st == ADAMA_OK) st = check_matrix(ctx, call, "x", p->x, p->x_dtype, p->rows, p->dim, p->ld_x);
+    if (st == ADAMA_OK && p->dx) st = check_matrix(ctx, call, "dx", p->dx, p->x_dtype, p->rows, p->dim, p->ld_dx);
+    if (st != ADAMA_OK) return st;
+    if (!p->weight || (p->rows > 0 && (!p->mean || !p->rstd)))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm_backward: null weight, mean or rstd");
+    if ((p->m_weight == nullptr) != (p->v_weight == nullptr) || (p->m_bias == nullptr) != (p->v_bias == nullptr))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm_backward: moments are given in pairs");
+    const bool fold = p->m_weight || p->m_bias, params = fold || p->dweight || p->dbias;
+    if (fold && ctx->n_micro < 1)
+        return fail(ctx, ADAMA_ERR_BAD_STATE, "layer_norm_backward: adama_begin_minibatch has not been called");
+    if (p->rows > 0 && p->dx &&
+        ((p->dx == p->x && p->ld_dx != p->ld_x) || (p->dx == p->dy && (p->dy_dtype != p->x_dtype || p->ld_dx != p->ld_dy))))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm_backward: in place needs one dtype and one pitch");
+    const void *const singles[] = {p->weight, p->mean, p->rstd, p->dweight, p->dbias, p->m_weight, p->v_weight, p->m_bias, p->v_bias};
+    for (const void *q : singles)
+        if (!aligned_to(q, 4)) return fail(ctx, ADAMA_ERR_MISALIGNED, "layer_norm_backward: pointer not aligned to 4 bytes");
+    if (!aligned_to(p->workspace, 16)) return fail(ctx, ADAMA_ERR_MISALIGNED, "layer_norm_backward: workspace needs 16-byte alignment");
+    if (!p->workspace && (params || p->dim > 8192))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "layer_norm_backward: null workspace");
+    if (!params && (!p->dx || p->rows == 0)) return ADAMA_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    adama::NormBackArgs a;
+    a.dy = p->dy;
+    a.x = p->x;
+    a.dx = p->dx;
+    a.dy_dtype = p->dy_dtype;
+    a.x_dtype = p->x_dtype;
+    a.rows = p->rows;
+    a.ld_dy = p->ld_dy;
+    a.ld_x = p->ld_x;
+    a.ld_dx = p->ld_dx;
+    a.dim = (int)p->dim;
+    a.weight = p->weight;
+    a.mean = p->mean;
+    a.rstd = p->rstd;
+    a.inv_dim = (float)(1.0 / (double)p->dim);
+    a.dweight = p->dweight;
+    a.dbias = p->dbias;
+    a.m_weight = p->m_weight;
+    a.v_weight = p->v_weight;
+    a.m_bias = p->m_bias;
+    a.v_bias = p->v_bias;
+    a.fold = ctx->fold_c;
+    a.workspace = p->workspace;
+    a.parts = params ? static_cast<float *>(p->workspace) : nullptr;
+    int launches = 0;
+    cudaError_t e = adama::launch_layer_norm_backward(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream), &launches);
+    ctx->launches += launches;
+    return e == cudaSuccess ? ADAMA_OK : cuda_fail(ctx, "layer_norm_backward launch", e);
+}
+
+adama_status adama_embedding(adama_ctx *ctx, const adama_embedding_args *p, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (!p) return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding: null arguments");
+    adama_status st = check_rows(ctx, "embedding", p->tokens, p->dim);
+    if (st == ADAMA_OK && (p->vocab < 1 || p->vocab >= INT32_MAX))
+        st = fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding: vocab must be from 1 to 2^31-2");
+    if (st == ADAMA_OK) st = check_matrix(ctx, "embedding", "table", p->table, p->table_dtype, p->vocab, p->dim, p->ld_table);
+    if (st == ADAMA_OK) st = check_matrix(ctx, "embedding", "out", p->out, p->out_dtype, p->tokens, p->dim, p->ld_out);
+    if (st != ADAMA_OK) return st;
+    if (p->tokens > 0 && !p->ids) return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding: null ids");
+    if (!aligned_to(p->ids, 8)) return fail(ctx, ADAMA_ERR_MISALIGNED, "embedding: ids not aligned to 8 bytes");
+    if (!isfinite(p->scale) || !(fabs(p->scale) <= FLT_MAX))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding: scale must be a finite 32-bit number");
+    if (p->tokens == 0) return ADAMA_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    adama::EmbeddingArgs a;
+    a.ids = p->ids;
+    a.table = p->table;
+    a.out = p->out;
+    a.table_dtype = p->table_dtype;
+    a.out_dtype = p->out_dtype;
+    a.tokens = p->tokens;
+    a.vocab = p->vocab;
+    a.ld_table = p->ld_table;
+    a.ld_out = p->ld_out;
+    a.dim = (int)p->dim;
+    a.scale = (float)p->scale;
+    a.status = ctx->status_dev;
+    cudaError_t e = adama::launch_embedding(a, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(ctx, "embedding launch", e);
+    ctx->launches += 1;
+    return ADAMA_OK;
+}
+
+size_t adama_embedding_workspace(const adama_ctx *ctx, int64_t tokens, int64_t dim) {
+    if (!ctx || tokens < 0 || tokens > INT32_MAX || dim < 1 || dim > INT32_MAX / 2) return 0;
+    return adama::embedding_workspace_bytes(tokens, (int)dim, ctx->sm_count);
+}
+
+adama_status adama_embedding_grad(adama_ctx *ctx, const adama_embedding_grad_args *p, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (!p) return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding_grad: null arguments");
+    const char *const call = "embedding_grad";
+    adama_status st = check_rows(ctx, call, p->tokens, p->dim);
+    if (st == ADAMA_OK && (p->vocab < 1 || p->vocab >= INT32_MAX))
+        st = fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding_grad: vocab must be from 1 to 2^31-2");
+    if (st == ADAMA_OK) st = check_matrix(ctx, call, "dy", p->dy, p->dy_dtype, p->tokens, p->dim, p->ld_dy);
+    if (st != ADAMA_OK) return st;
+    const bool fold = p->m || p->v;
+    if (fold ? !p->m || !p->v || p->grad || p->accumulate : !p->grad)
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding_grad: either grad or both moments are given");
+    const adama_dtype dt = fold ? ADAMA_F32 : p->grad_dtype;
+    st = check_matrix(ctx, call, fold ? "m" : "grad", fold ? p->m : p->grad, dt, p->vocab, p->dim, p->ld_grad);
+    if (st == ADAMA_OK && fold) st = check_matrix(ctx, call, "v", p->v, dt, p->vocab, p->dim, p->ld_grad);
+    if (st != ADAMA_OK) return st;
+    if (fold && ctx->n_micro < 1)
+        return fail(ctx, ADAMA_ERR_BAD_STATE, "embedding_grad: adama_begin_minibatch has not been called");
+    if (p->tokens > 0 && (!p->ids || !p->workspace)) return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding_grad: null ids or workspace");
+    if (!aligned_to(p->ids, 8) || !aligned_to(p->workspace, 16))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "embedding_grad: ids need 8-byte, workspace 16-byte alignment");
+    if (!isfinite(p->scale) || !(fabs(p->scale) <= FLT_MAX))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding_grad: scale must be a finite 32-bit number");
+    DeviceGuard guard(ctx->cfg.device);
+    adama::EmbeddingGradArgs a = {};
+    a.ids = p->ids;
+    a.dy = p->dy;
+    a.dy_dtype = p->dy_dtype;
+    a.grad_dtype = dt;
+    a.tokens = p->tokens;
+    a.vocab = p->vocab;
+    a.ld_dy = p->ld_dy;
+    a.ld_grad = p->ld_grad;
+    a.dim = (int)p->dim;
+    a.scale = (float)p->scale;
+    a.accumulate = p->accumulate != 0;
+    a.grad = p->grad;
+    a.m = p->m;
+    a.v = p->v;
+    a.fold = ctx->fold_c;
+    a.workspace = p->workspace;
+    a.status = ctx->status_dev;
+    int launches = 0;
+    cudaError_t e = adama::launch_embedding_grad(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream), &launches);
+    ctx->launches += launches;
+    return e == cudaSuccess ? ADAMA_OK : cuda_fail(ctx, "embedding_grad launch", e);
+}
+
 // ---- host-buffer variants -------------------------------------------------------------------
 
 adama_status adama_fold_host(adama_ctx *ctx, const void *grad_host, adama_dtype gdt, float *m,
@@ -1035,7 +1256,7 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
     if (target[0] != 0) {
         e = clear(adama::kStatusTarget);
         if (e != cudaSuccess) return cuda_fail(ctx, "sync_status", e);
-        snprintf(ctx->err, sizeof(ctx->err), "a row of logits had a target outside the vocabulary (row %llu)",
+        snprintf(ctx->err, sizeof(ctx->err), "a target or an id lies outside the vocabulary (row %llu of its call)",
                  (unsigned long long)target[2] << 32 | target[1]);
         return ADAMA_ERR_INVALID_ARG;
     }

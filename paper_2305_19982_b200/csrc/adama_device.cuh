@@ -41,4 +41,12 @@ __device__ __forceinline__ void apply1(float &w, float &m, float &v, const Apply
     v = fmaf(v, c.beta2_hi, v * c.beta2_lo);
 }
 
+// A target or an id outside the vocabulary, in row `row` of a call.
+__device__ __forceinline__ void record_bad_target(unsigned *status, int64_t row) {
+    if (atomicCAS(status + kStatusTarget, 0u, 1u) == 0u) {
+        status[kStatusTarget + 1] = (unsigned)row;
+        status[kStatusTarget + 2] = (unsigned)(row >> 32);
+    }
+}
+
 }  // namespace adama

@@ -50,7 +50,7 @@ ApplyConstants make_apply_constants(double beta1, double beta2, double eps, int6
                                     int world = 1, bool sharded = false, double weight_decay = 0.0);
 
 // Status block in device memory (256 bytes).  Words 0-3, an expired wait: word 0 = kDevTimeout (0 =
-// none) by the first kernel that records one, word 1 = which wait, word 2 = tile.  Words 4-7, a target
+// none) by the first kernel that records one, word 1 = which wait, word 2 = tile.  Words 4-7, a target or an id
 // outside the vocabulary: word kStatusTarget = 1 by the first row that records one, the next two that row's
 // low and high half.  Apart, so that neither hides the other.  The rest is reserved.
 enum DeviceErr : unsigned { kDevOk = 0, kDevTimeout = 1 };
@@ -153,6 +153,68 @@ struct PolicyArgs {
     unsigned *status;
 };
 cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream);
+
+// layer norm (layer_norm.cu)
+struct NormArgs {
+    const void *x;
+    void *y;
+    adama_dtype x_dtype, y_dtype;
+    int64_t rows, ld_x, ld_y;
+    int dim;
+    const float *weight, *bias;  // bias may be null
+    float eps;
+    float *mean, *rstd;  // may be null
+};
+cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream);
+struct NormBackArgs {
+    const void *dy, *x;
+    void *dx;  // of x's type; may be null
+    adama_dtype dy_dtype, x_dtype;
+    int64_t rows, ld_dy, ld_x, ld_dx;
+    int dim;
+    const float *weight, *mean, *rstd;
+    float inv_dim;
+    float *dweight, *dbias;                          // each may be null
+    float *m_weight, *v_weight, *m_bias, *v_bias;    // pairs, each may be null
+    FoldConstants fold;
+    float *parts;  // the workspace, or null: no parameter's gradient is wanted
+    void *workspace;
+};
+size_t norm_workspace_bytes(int64_t rows, int dim, int sm_count);
+cudaError_t launch_layer_norm_backward(const NormBackArgs &a, int sm_count, cudaStream_t stream, int *launches);
+
+// embedding lookup and gradient (embedding.cu)
+struct EmbeddingArgs {
+    const int64_t *ids;
+    const void *table;
+    void *out;
+    adama_dtype table_dtype, out_dtype;
+    int64_t tokens, vocab, ld_table, ld_out;
+    int dim;
+    float scale;
+    unsigned *status;
+};
+cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream);
+struct EmbeddingGradArgs {
+    const int64_t *ids;
+    const void *dy;
+    adama_dtype dy_dtype, grad_dtype;
+    int64_t tokens, vocab, ld_dy, ld_grad;  // ld_grad: of grad, or of m and v
+    int dim;
+    float scale;
+    int accumulate;
+    void *grad;  // or:
+    float *m, *v;
+    FoldConstants fold;
+    void *workspace;
+    unsigned *status;
+    // parts of the workspace, set by the launch: sorted keys and their tokens, sums of runs that cross chunks
+    unsigned *keys, *order;
+    float *parts;
+    int64_t pad;
+};
+size_t embedding_workspace_bytes(int64_t tokens, int dim, int sm_count);
+cudaError_t launch_embedding_grad(EmbeddingGradArgs a, int sm_count, cudaStream_t stream, int *launches);
 
 // fused reduce-scatter + sharded apply + all-gather over peer-mapped buffers (peer_apply.cu)
 constexpr int kMaxPeers = 16;

@@ -1,0 +1,525 @@
+// Embedding lookup, out[t] = scale*table[ids[t]], and its gradient by sorted tokens:
+//     g[i] = scale * sum over the tokens t with ids[t] = i of dy[t]
+// written to a whole table (zeros in the other rows), added to one, or folded into the moments of the rows
+// that occur (m += a*g, v += b*g^2: the sum is complete before it is squared; a row without tokens has g = 0 and
+// is not touched, so that the traffic is that of the tokens, not of the vocabulary).
+//
+// The tokens are sorted by id, equal ones in their order.  The sorted tokens are cut into chunks; a warp takes
+// a chunk's columns 256 at a time and sums equal neighbours in registers, in fp32.  A run of equal tokens that
+// lies inside a chunk is finished there; the parts of one that crosses chunks go to the workspace, and a second
+// kernel adds them in order.  So a token that occurs thousands of times is spread over the card like any others,
+// no atomics are involved and results do not depend on scheduling.  Bound by HBM.
+#include "adama_device.cuh"
+#include "row_access.cuh"
+
+namespace adama {
+namespace {
+
+constexpr int kTile = 32 * kPiece;  // columns of a warp
+
+// ---- lookup --------------------------------------------------------------------------------------
+
+constexpr int kLookupWarps = 4;
+constexpr int kLookupPieces = 4;  // of a lane, all loaded before the first is stored
+
+template <typename T, typename O>
+__global__ void __launch_bounds__(32 * kLookupWarps)
+embedding_kernel(const EmbeddingArgs a, int groups) {
+    const int lane = threadIdx.x % 32;
+    const int64_t task = (int64_t)blockIdx.x * kLookupWarps + threadIdx.x / 32;
+    const int64_t token = task / groups;
+    const int first = (int)(task % groups) * kLookupPieces * kTile + lane * kPiece;
+    if (token >= a.tokens) return;
+    const int64_t id = a.ids[token];
+    const bool inside = id >= 0 && id < a.vocab;
+    const T *table = static_cast<const T *>(a.table);
+    const Extent all = extent_of(table, a.vocab, a.dim, a.ld_table);
+    O *out = static_cast<O *>(a.out) + token * a.ld_out;
+    float v[kLookupPieces][kPiece];
+    int count[kLookupPieces];
+#pragma unroll
+    for (int u = 0; u < kLookupPieces; ++u) {
+        const int c = first + u * kTile;
+        count[u] = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
+        load_piece(table + (inside ? id * a.ld_table : 0) + c, inside ? count[u] : 0, all, v[u]);
+    }
+    const float other = id < 0 ? 0.f : NAN;
+#pragma unroll
+    for (int u = 0; u < kLookupPieces; ++u) {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[u][i] = inside ? v[u][i] * a.scale : other;
+        store_run(out + first + u * kTile, v[u], count[u], 32);
+    }
+    if (!inside && id >= 0 && first == 0) record_bad_target(a.status, token);
+}
+
+// ---- sorting by id ---------------------------------------------------------------------------------
+// Ids outside the table get the key `vocab` and come last.
+
+__device__ __forceinline__ unsigned key_of(const EmbeddingGradArgs &a, int64_t t) {
+    const int64_t id = a.ids[t];
+    return id >= 0 && id < a.vocab ? (unsigned)id : (unsigned)a.vocab;
+}
+
+// Up to kRankTokens tokens: a token's place is the number of tokens that come before it, counted over all
+// of them.  32 tokens to a block, whose warps share the count.
+constexpr int kRankTokens = 8192;
+constexpr int kRankWarps = 8;
+constexpr int kRankTile = 2048;
+
+__global__ void __launch_bounds__(32 * kRankWarps)
+embedding_rank_kernel(const EmbeddingGradArgs a) {
+    __shared__ alignas(16) unsigned keys[kRankTile];
+    __shared__ int counts[kRankWarps][32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int t = blockIdx.x * 32 + lane, tokens = (int)a.tokens;
+    const unsigned mine = t < tokens ? key_of(a, t) : 0;
+    int before = 0;
+    for (int base = 0; base < tokens; base += kRankTile) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kRankTile; i += 32 * kRankWarps)
+            keys[i] = base + i < tokens ? key_of(a, base + i) : 0xffffffffu;
+        __syncthreads();
+        const int begin = warp * (kRankTile / kRankWarps);
+        for (int i = begin; i < begin + kRankTile / kRankWarps && base + i < tokens; i += 32) {
+            const int block = (base + i) / 32;
+            if (block != (int)blockIdx.x) {
+                const unsigned limit = mine + (block < (int)blockIdx.x ? 1u : 0u);  // equal ones in front count
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    const uint4 k = *reinterpret_cast<const uint4 *>(keys + i + j);
+                    before += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
+                }
+            } else {
+                for (int j = 0; j < 32; ++j) before += keys[i + j] < mine + (j < lane ? 1u : 0u);
+            }
+        }
+    }
+    counts[warp][lane] = before;
+    __syncthreads();
+    if (warp != 0 || t >= tokens) return;
+    int place = 0;
+    for (int i = 0; i < kRankWarps; ++i) place += counts[i][lane];
+    a.keys[place] = mine;
+    a.order[place] = (unsigned)t;
+    if (mine == (unsigned)a.vocab && a.ids[t] >= 0) record_bad_target(a.status, t);
+}
+
+// More: passes over digits of the key, from the lowest on, each of which keeps the order of equal digits.
+constexpr int kDigitBits = 9;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kSortWarps = 8;
+constexpr int kSortThreads = 32 * kSortWarps;
+constexpr int kSortBlocks = 64;  // at most
+
+struct SortPass {
+    const unsigned *keys, *order;  // null in the first pass: from the ids
+    unsigned *keys_out, *order_out;
+    int *counts;  // [blocks][digits]
+    int shift, mask, per;  // tokens of a block, a multiple of kSortThreads
+};
+__device__ __forceinline__ unsigned pass_key(const EmbeddingGradArgs &a, const SortPass &p, int64_t t) {
+    return p.keys ? p.keys[t] : key_of(a, t);
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+embedding_digits_kernel(const EmbeddingGradArgs a, const SortPass p) {
+    __shared__ int counts[kDigits];
+    for (int i = threadIdx.x; i < kDigits; i += kSortThreads) counts[i] = 0;
+    __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * p.per;
+    for (int64_t t = begin + threadIdx.x; t < begin + p.per && t < a.tokens; t += kSortThreads) {
+        const unsigned key = pass_key(a, p, t);
+        atomicAdd(&counts[key >> p.shift & p.mask], 1);
+        if (!p.keys && key == (unsigned)a.vocab && a.ids[t] >= 0) record_bad_target(a.status, t);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kDigits; i += kSortThreads) p.counts[blockIdx.x * kDigits + i] = counts[i];
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
+    __shared__ int place[kSortWarps][kDigits];  // where a warp's next token of a digit goes
+    __shared__ int scan[kSortThreads];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&place[0][0])[i] = 0;
+    __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * p.per + (int64_t)warp * (p.per / kSortWarps);
+    int64_t end = begin + p.per / kSortWarps;
+    if (end > a.tokens) end = a.tokens;
+    for (int64_t t = begin + lane; t < end; t += 32) atomicAdd(&place[warp][pass_key(a, p, t) >> p.shift & p.mask], 1);
+    __syncthreads();
+    // a thread has two neighbouring digits: tokens of smaller digits, and of its digits in blocks before this one
+    int total[2] = {0, 0}, earlier[2] = {0, 0};
+    for (int b = 0; b < (int)gridDim.x; ++b) {
+        const int2 n = *reinterpret_cast<const int2 *>(p.counts + b * kDigits + 2 * threadIdx.x);
+        if (b < (int)blockIdx.x) {
+            earlier[0] += n.x;
+            earlier[1] += n.y;
+        }
+        total[0] += n.x;
+        total[1] += n.y;
+    }
+    scan[threadIdx.x] = total[0] + total[1];
+    __syncthreads();
+    for (int o = 1; o < kSortThreads; o *= 2) {
+        const int x = (int)threadIdx.x >= o ? scan[threadIdx.x - o] : 0;
+        __syncthreads();
+        scan[threadIdx.x] += x;
+        __syncthreads();
+    }
+    int at = scan[threadIdx.x] - total[0] - total[1];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        int next = at + earlier[q];
+        for (int w = 0; w < kSortWarps; ++w) {
+            int &slot = place[w][2 * threadIdx.x + q];
+            const int n = slot;
+            slot = next;
+            next += n;
+        }
+        at += total[q];
+    }
+    __syncthreads();
+    for (int64_t base = begin; base < end; base += 32) {
+        const int64_t t = base + lane;
+        const unsigned key = t < end ? pass_key(a, p, t) : 0;
+        const unsigned token = t < end ? (p.order ? p.order[t] : (unsigned)t) : 0;
+        const int digit = t < end ? (int)(key >> p.shift & p.mask) : kDigits;
+        const unsigned same = __match_any_sync(0xffffffffu, digit);
+        const int rank = __popc(same & ((1u << lane) - 1));
+        int to = 0;
+        if (t < end) to = place[warp][digit] + rank;
+        __syncwarp();
+        if (t < end && rank == 0) place[warp][digit] += __popc(same);
+        __syncwarp();
+        if (t < end) {
+            p.keys_out[to] = key;
+            p.order_out[to] = token;
+        }
+    }
+}
+
+// ---- sums of equal tokens --------------------------------------------------------------------------
+
+enum GradMode { kWrite, kAdd, kFold };
+
+// What a finished sum meets in memory: loaded ahead of time.
+template <typename O, int MODE>
+struct Target {
+    float m[MODE == kWrite ? 1 : kPiece], v[MODE == kFold ? kPiece : 1];
+};
+template <typename O, int MODE>
+__device__ __forceinline__ void load_target(const EmbeddingGradArgs &a, unsigned key, int c, int count, Target<O, MODE> &t) {
+    if constexpr (MODE == kAdd) {
+        const O *grad = static_cast<const O *>(a.grad);
+        load_piece(grad + (int64_t)key * a.ld_grad + c, count, extent_of(grad, a.vocab, a.dim, a.ld_grad), t.m);
+    }
+    if constexpr (MODE == kFold) {
+        load_piece(a.m + (int64_t)key * a.ld_grad + c, count, extent_of(a.m, a.vocab, a.dim, a.ld_grad), t.m);
+        load_piece(a.v + (int64_t)key * a.ld_grad + c, count, extent_of(a.v, a.vocab, a.dim, a.ld_grad), t.v);
+    }
+}
+template <typename O, int MODE>
+__device__ __forceinline__ void finish(const EmbeddingGradArgs &a, unsigned key, int c, int count, const float (&sum)[kPiece],
+                                       Target<O, MODE> &t) {
+    float g[kPiece];
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) g[i] = sum[i] * a.scale;
+    if constexpr (MODE == kFold) {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) fold1(g[i], t.m[i], t.v[i], a.fold.a, a.fold.b);
+        store_run(a.m + (int64_t)key * a.ld_grad + c, t.m, count, 32);
+        store_run(a.v + (int64_t)key * a.ld_grad + c, t.v, count, 32);
+    } else {
+        if constexpr (MODE == kAdd) {
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) g[i] += t.m[i];
+        }
+        store_run(static_cast<O *>(a.grad) + (int64_t)key * a.ld_grad + c, g, count, 32);
+    }
+}
+
+// Part `slot` of chunk b: 0 continues the chunk before, 1 begins in b and goes on behind it.
+__device__ __forceinline__ float *part_of(const EmbeddingGradArgs &a, int64_t b, int slot) {
+    return a.parts + (2 * b + slot) * a.pad;
+}
+__device__ __forceinline__ void put_part(float *p, const float (&sum)[kPiece]) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+}
+__device__ __forceinline__ void add_part(const float *p, float (&sum)[kPiece]) {
+    const float4 x = __ldcg(reinterpret_cast<const float4 *>(p)), y = __ldcg(reinterpret_cast<const float4 *>(p) + 1);
+    sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+    sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+}
+
+constexpr int kGradWarps = 4;
+constexpr int kBatch = 4;  // tokens whose rows are loaded together
+
+template <typename O>
+__device__ __forceinline__ void zero_row(O *p, int n, int lane) {
+    constexpr int kPer = 16 / sizeof(O);
+    const int past = (int)(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(O));
+    const int head = past ? (kPer - past < n ? kPer - past : n) : 0, body = (n - head) / kPer, tail = head + body * kPer;
+    for (int i = lane; i < body; i += 32) reinterpret_cast<uint4 *>(p + head)[i] = make_uint4(0, 0, 0, 0);
+    if (lane < head) p[lane] = narrowed<O>(0.f);
+    if (lane < n - tail) p[tail + lane] = narrowed<O>(0.f);
+}
+
+// chunk: tokens of a warp, up to 32.  Blocks from sum_blocks on zero the rows that have no token.
+template <typename G, typename O, int MODE>
+__global__ void __launch_bounds__(32 * kGradWarps)
+embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned sum_blocks) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    if (MODE == kWrite && blockIdx.x >= sum_blocks) {
+        const int64_t first = ((int64_t)(blockIdx.x - sum_blocks) * kGradWarps + warp) * 32;
+        const int64_t row = first + lane;
+        int64_t lo = 0, hi = a.tokens;  // the first token whose key is not below the row
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if ((int64_t)a.keys[mid] < row) lo = mid + 1;
+            else hi = mid;
+        }
+        const bool empty = row < a.vocab && (lo == a.tokens || (int64_t)a.keys[lo] != row);
+        unsigned todo = __ballot_sync(0xffffffffu, empty);
+        for (; todo; todo &= todo - 1)
+            zero_row(static_cast<O *>(a.grad) + (first + __ffs(todo) - 1) * a.ld_grad, a.dim, lane);
+        return;
+    }
+    const int64_t task = (int64_t)blockIdx.x * kGradWarps + warp, b = task / tiles;
+    const int64_t start = b * chunk;
+    if (start >= a.tokens) return;
+    const int c = (int)(task % tiles) * kTile + lane * kPiece;
+    const int count = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
+    const int n = (int)(a.tokens - start < chunk ? a.tokens - start : chunk);
+    const unsigned none = 0xffffffffu, out = (unsigned)a.vocab;
+    const unsigned key = lane < n ? a.keys[start + lane] : none, token = lane < n ? a.order[start + lane] : 0;
+    const unsigned behind = start + n < a.tokens ? a.keys[start + n] : none;
+    const unsigned ahead = start > 0 ? a.keys[start - 1] : none;
+    unsigned next = __shfl_down_sync(0xffffffffu, key, 1);
+    if (lane == n - 1) next = behind;
+    const unsigned ends = __ballot_sync(0xffffffffu, lane < n && next != key);
+    const int live = __popc(__ballot_sync(0xffffffffu, lane < n && key != out));  // the others come last
+    bool open = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the first run continues the chunk before
+    const G *dy = static_cast<const G *>(a.dy);
+    const Extent all = extent_of(dy, a.tokens, a.dim, a.ld_dy);
+    float sum[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < live; j += kBatch) {
+        float x[kBatch][kPiece];
+        Target<O, MODE> target[kBatch];
+        unsigned k[kBatch];
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+            k[q] = __shfl_sync(0xffffffffu, key, (j + q) & 31);
+            const unsigned t = __shfl_sync(0xffffffffu, token, (j + q) & 31);
+            if (j + q < live) {
+                load_piece(dy + (int64_t)t * a.ld_dy + c, count, all, x[q]);
+                if (ends >> (j + q) & 1) load_target<O, MODE>(a, k[q], c, count, target[q]);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+            if (j + q < live) {
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) sum[i] += x[q][i];
+                if (ends >> (j + q) & 1) {
+                    if (open) {
+                        if (count) put_part(part_of(a, b, 0) + c, sum);
+                    } else {
+                        finish<O, MODE>(a, k[q], c, count, sum, target[q]);
+                    }
+                    open = false;
+#pragma unroll
+                    for (int i = 0; i < kPiece; ++i) sum[i] = 0.f;
+                }
+            }
+        }
+    }
+    if (live == n && !(ends >> (n - 1) & 1) && count) put_part(part_of(a, b, open ? 0 : 1) + c, sum);
+}
+
+// Runs that cross chunks: block x takes the one that begins in chunk x and goes on behind it, if there is one.
+constexpr int kJoinWarps = 8;
+constexpr int kJoinShort = 16;  // parts up to which a warp adds them alone
+
+template <typename O, int MODE>
+__global__ void __launch_bounds__(32 * kJoinWarps)
+embedding_join_kernel(const EmbeddingGradArgs a, int chunk, int tiles) {
+    __shared__ float slots[kJoinWarps][kTile];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int64_t b = blockIdx.x, start = b * chunk, end = start + chunk;
+    if (end >= a.tokens) return;
+    const unsigned key = a.keys[end - 1];
+    if (key == (unsigned)a.vocab || a.keys[end] != key) return;
+    if (start > 0 && a.keys[start - 1] == key && a.keys[start] == key) return;  // begins in an earlier chunk
+    int64_t last = b;  // the chunk in which the run ends
+    for (;;) {
+        const int64_t at = (last + 1 + lane) * chunk;
+        const unsigned more = __ballot_sync(0xffffffffu, at < a.tokens && a.keys[at] == key);
+        const int run = more == 0xffffffffu ? 32 : __ffs(~more) - 1;
+        last += run;
+        if (run < 32) break;
+    }
+    const int64_t parts = last - b;  // behind the first one
+    const int first_tile = blockIdx.y * kJoinWarps;
+    if (parts <= kJoinShort) {
+        const int tile = first_tile + warp;
+        if (tile >= tiles) return;
+        const int c = tile * kTile + lane * kPiece;
+        const int count = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
+        Target<O, MODE> target;
+        load_target<O, MODE>(a, key, c, count, target);
+        float sum[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (count) {
+            add_part(part_of(a, b, 1) + c, sum);
+#pragma unroll 4
+            for (int64_t i = b + 1; i <= last; ++i) add_part(part_of(a, i, 0) + c, sum);
+        }
+        finish<O, MODE>(a, key, c, count, sum, target);
+        return;
+    }
+    // long: the warps share the parts of a tile, one tile after the other
+    for (int tile = first_tile; tile < tiles && tile < first_tile + kJoinWarps; ++tile) {
+        const int c = tile * kTile + lane * kPiece;
+        const int count = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
+        const int64_t from = b + 1 + parts * warp / kJoinWarps, to = b + 1 + parts * (warp + 1) / kJoinWarps;
+        float sum[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (count) {
+            if (warp == 0) add_part(part_of(a, b, 1) + c, sum);
+#pragma unroll 8
+            for (int64_t i = from; i < to; ++i) add_part(part_of(a, i, 0) + c, sum);
+        }
+        put_part(&slots[warp][lane * kPiece], sum);
+        __syncthreads();
+        if (warp == 0) {
+            Target<O, MODE> target;
+            load_target<O, MODE>(a, key, c, count, target);
+            for (int w = 1; w < kJoinWarps; ++w)
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) sum[i] += slots[w][lane * kPiece + i];
+            finish<O, MODE>(a, key, c, count, sum, target);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- launches --------------------------------------------------------------------------------------
+
+template <typename T, typename O>
+cudaError_t lookup(const EmbeddingArgs &a, cudaStream_t stream) {
+    const int groups = (a.dim + kLookupPieces * kTile - 1) / (kLookupPieces * kTile);
+    const int64_t blocks = (a.tokens * groups + kLookupWarps - 1) / kLookupWarps;
+    embedding_kernel<T, O><<<(unsigned)blocks, 32 * kLookupWarps, 0, stream>>>(a, groups);
+    return cudaGetLastError();
+}
+
+// Sizes of the parts of the workspace, each a multiple of 16 bytes.
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+
+// Tokens to a chunk: as many as leave every SM a dozen warps, 32 at most (a lane each).
+int chunk_for(int64_t tokens, int tiles, int sm_count) {
+    int chunk = 32;
+    while (chunk > 8 && tokens * tiles / chunk < (int64_t)12 * sm_count) chunk /= 2;
+    return chunk;
+}
+struct GradPlan {
+    int tiles, chunk;
+    int64_t chunks, pad;
+    size_t list, parts;  // bytes of a list of the tokens, of the runs' parts
+    bool by_rank;
+};
+GradPlan plan_grad(int64_t tokens, int dim, int sm_count) {
+    GradPlan p;
+    p.tiles = (dim + kTile - 1) / kTile;
+    p.chunk = chunk_for(tokens, p.tiles, sm_count);
+    p.chunks = (tokens + p.chunk - 1) / p.chunk;
+    p.pad = ((int64_t)dim + kPiece - 1) / kPiece * kPiece;
+    p.list = up16((size_t)tokens * sizeof(unsigned));
+    p.parts = p.chunks > 1 ? (size_t)p.chunks * 2 * p.pad * sizeof(float) : 0;
+    p.by_rank = tokens <= kRankTokens;
+    return p;
+}
+
+cudaError_t sort_tokens(EmbeddingGradArgs &a, const GradPlan &p, unsigned char *ws, cudaStream_t stream, int *launches) {
+    unsigned *lists[4];
+    for (int i = 0; i < 4; ++i) lists[i] = reinterpret_cast<unsigned *>(ws + i * p.list);
+    a.keys = lists[0];
+    a.order = lists[1];
+    if (p.by_rank) {
+        embedding_rank_kernel<<<(unsigned)((a.tokens + 31) / 32), 32 * kRankWarps, 0, stream>>>(a);
+        *launches += 1;
+        return cudaGetLastError();
+    }
+    int bits = 1;
+    while (bits < 32 && a.vocab >> bits) ++bits;  // the key `vocab` included
+    const int passes = (bits + kDigitBits - 1) / kDigitBits, each = (bits + passes - 1) / passes;
+    SortPass s;
+    s.counts = reinterpret_cast<int *>(ws + 4 * p.list);
+    s.mask = (1 << each) - 1;
+    int64_t per = (a.tokens + kSortBlocks - 1) / kSortBlocks;
+    if (per < 2048) per = 2048;
+    s.per = (int)((per + kSortThreads - 1) / kSortThreads * kSortThreads);
+    const unsigned blocks = (unsigned)((a.tokens + s.per - 1) / s.per);
+    int to = passes % 2 ? 0 : 2;  // the last pass writes lists 0 and 1
+    s.keys = s.order = nullptr;
+    for (int i = 0; i < passes; ++i, to ^= 2) {
+        s.shift = i * each;
+        s.keys_out = lists[to];
+        s.order_out = lists[to + 1];
+        embedding_digits_kernel<<<blocks, kSortThreads, 0, stream>>>(a, s);
+        embedding_scatter_kernel<<<blocks, kSortThreads, 0, stream>>>(a, s);
+        *launches += 2;
+        s.keys = lists[to];
+        s.order = lists[to + 1];
+    }
+    return cudaGetLastError();
+}
+
+template <typename G, typename O, int MODE>
+cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t stream, int *launches) {
+    const unsigned sum_blocks = (unsigned)((p.chunks * p.tiles + kGradWarps - 1) / kGradWarps);
+    const unsigned zero_blocks = MODE == kWrite ? (unsigned)((a.vocab + 32 * kGradWarps - 1) / (32 * kGradWarps)) : 0;
+    if (sum_blocks + zero_blocks == 0) return cudaSuccess;
+    embedding_grad_kernel<G, O, MODE><<<sum_blocks + zero_blocks, 32 * kGradWarps, 0, stream>>>(a, p.chunk, p.tiles, sum_blocks);
+    *launches += 1;
+    if (p.chunks > 1) {
+        const dim3 grid((unsigned)(p.chunks - 1), (unsigned)((p.tiles + kJoinWarps - 1) / kJoinWarps));
+        embedding_join_kernel<O, MODE><<<grid, 32 * kJoinWarps, 0, stream>>>(a, p.chunk, p.tiles);
+        *launches += 1;
+    }
+    return cudaGetLastError();
+}
+template <typename G>
+cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t stream, int *launches) {
+    if (a.m) return sums<G, float, kFold>(a, p, stream, launches);
+    if (a.grad_dtype == ADAMA_F32) return a.accumulate ? sums<G, float, kAdd>(a, p, stream, launches) : sums<G, float, kWrite>(a, p, stream, launches);
+    return a.accumulate ? sums<G, __nv_bfloat16, kAdd>(a, p, stream, launches) : sums<G, __nv_bfloat16, kWrite>(a, p, stream, launches);
+}
+
+}  // namespace
+
+cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream) {
+    if (a.table_dtype == ADAMA_F32)
+        return a.out_dtype == ADAMA_F32 ? lookup<float, float>(a, stream) : lookup<float, __nv_bfloat16>(a, stream);
+    return a.out_dtype == ADAMA_F32 ? lookup<__nv_bfloat16, float>(a, stream) : lookup<__nv_bfloat16, __nv_bfloat16>(a, stream);
+}
+
+size_t embedding_workspace_bytes(int64_t tokens, int dim, int sm_count) {
+    const GradPlan p = plan_grad(tokens, dim, sm_count);
+    return p.list * (p.by_rank ? 2 : 4) + (p.by_rank ? 0 : kSortBlocks * kDigits * sizeof(int)) + p.parts;
+}
+
+cudaError_t launch_embedding_grad(EmbeddingGradArgs a, int sm_count, cudaStream_t stream, int *launches) {
+    const GradPlan p = plan_grad(a.tokens, a.dim, sm_count);
+    unsigned char *ws = static_cast<unsigned char *>(a.workspace);
+    a.pad = p.pad;
+    a.parts = reinterpret_cast<float *>(ws + p.list * (p.by_rank ? 2 : 4) + (p.by_rank ? 0 : kSortBlocks * kDigits * sizeof(int)));
+    if (a.tokens > 0) {
+        const cudaError_t e = sort_tokens(a, p, ws, stream, launches);
+        if (e != cudaSuccess) return e;
+    }
+    return a.dy_dtype == ADAMA_F32 ? sums<float>(a, p, stream, launches) : sums<__nv_bfloat16>(a, p, stream, launches);
+}
+
+}  // namespace adama

@@ -22,13 +22,6 @@ namespace {
 constexpr int kThreads = 512;  // that work on rows, in every kernel here
 constexpr int kWarps = kThreads / 32;
 
-__device__ __forceinline__ void record_bad_target(unsigned *status, int64_t row) {
-    if (atomicCAS(status + kStatusTarget, 0u, 1u) == 0u) {
-        status[kStatusTarget + 1] = (unsigned)row;
-        status[kStatusTarget + 2] = (unsigned)(row >> 32);
-    }
-}
-
 // Barrier of the W warps that share a row: group g of the CTA.
 template <int W>
 __device__ __forceinline__ void group_sync(int g) {
