@@ -380,7 +380,7 @@ ADAMA_API adama_status adama_state8_unpack_multi(adama_ctx *ctx, const adama_sta
                                                  float *const *m, float *const *v, const size_t *n,
                                                  int count, void *cuda_stream);
 
-/* Scratch of the two reductions below: caller-owned device memory, 16-byte aligned, zero-filled
+/* Scratch of the reductions below (norm, policy loss, distillation): caller-owned device memory, 16-byte aligned, zero-filled
  * once before its first use (each call leaves it ready for the next).  Calls that may overlap on the
  * GPU (different streams) need one each.  A call that is captured into a CUDA graph keeps the address:
  * give each graph a workspace of its own, with the zero-fill captured in the same graph before its first
@@ -460,6 +460,45 @@ typedef struct adama_policy_args {
 } adama_policy_args;
 ADAMA_API adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args *args,
                                          void *cuda_stream);
+
+/* Distillation from a teacher's top logits: the divergence of the student's distribution from a teacher's
+ * of which each row has `top` entries (logit, index) alone, and its gradient with respect to the student's
+ * logits.  With z = logit_scale*logits, log q = z - lse(z), and per entry i of a row with weight w
+ *     log p_i = logit_scale*teacher_logits_i - teacher_lse,  P = sum p_i
+ *     kl = sum p_i*(log p_i - log q_{ids_i})
+ *     stats = sum over rows of w*{kl, -sum p_i log q_{ids_i}, sum q_{ids_i}, P}
+ *     dlogits_j = w*logit_scale*(P*q_j - sum over the entries with ids_i = j of p_i)
+ * so that stats[0] is the loss and dlogits its gradient; w carries the mask, the normalisation, and 1/logit_scale^2
+ * where the temperature's square is wanted in front.  Without teacher_lse the entries' own log-sum takes its place:
+ * P = 1.  An entry with a negative index, or a teacher's logit of -inf, has p = 0; a row without any other has
+ * loss and gradient 0.  An index may occur more than once in a row: each entry has its own term.  A row with
+ * w = 0 is not read: its dlogits and loss are 0 and it adds nothing to stats.
+ *   logits, dlogits : as for adama_policy_loss (dlogits may be NULL, or logits itself)
+ *   teacher_logits  : [rows, top] fp32 or bf16, pitch ld_teacher;   ids : [rows, top] int64, pitch ld_ids
+ *   top         : 1 to ADAMA_DISTILL_TOP
+ *   teacher_lse : rows fp32 (of logit_scale times ALL the teacher's logits), or NULL
+ *   weights     : rows fp32;   loss : rows fp32 (kl of each row), or NULL;   stats : 4 fp32
+ *   workspace   : ADAMA_WORKSPACE_BYTES
+ * logit_scale as in adama_token_logprobs.  Deterministic.  A row with an index >= vocab becomes NaN and is reported
+ * as a target is.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED (top too large), CUDA. */
+#define ADAMA_DISTILL_TOP 128
+typedef struct adama_distill_args {
+    const void *logits;
+    void *dlogits;
+    adama_dtype logits_dtype, dlogits_dtype, teacher_dtype;
+    int top;
+    int64_t rows, vocab, ld_logits, ld_dlogits, ld_teacher, ld_ids;
+    const void *teacher_logits;
+    const int64_t *ids;
+    const float *teacher_lse;
+    const float *weights;
+    double logit_scale;
+    float *loss;
+    float *stats;
+    void *workspace;
+} adama_distill_args;
+ADAMA_API adama_status adama_distill_loss(adama_ctx *ctx, const adama_distill_args *args,
+                                          void *cuda_stream);
 
 /* The id of the capture that `cuda_stream` is taking part in, 0 if it is not being captured: what a
  * caller who keeps a workspace per stream tells graphs apart by.  Ids are unique in the process. */
@@ -708,7 +747,7 @@ ADAMA_API adama_status adama_set_weight_decay(adama_ctx *ctx, double weight_deca
  * ADAMA_ERR_TIMEOUT (a bounded wait inside a kernel expired: the fused weight gradient, a streamed
  * update or the policy loss, as adama_last_error says; what that call writes is incomplete),
  * ADAMA_ERR_INVALID_ARG (a row of adama_token_logprobs or adama_policy_loss had a target >= vocab, or an
- * embedding call an id) or
+ * embedding call or adama_distill_loss an index) or
  * ADAMA_ERR_CUDA.  Each call reports and clears one of them, an expired wait first: call again for the other. */
 ADAMA_API adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream);
 

@@ -29,7 +29,7 @@ EXPORTED_SYMBOLS = [
     "adama_fold_apply_multi", "adama_fold_apply8_multi", "adama_state8_pack_multi", "adama_state8_unpack_multi",
     "adama_grad_norm_multi", "adama_token_logprobs", "adama_policy_loss", "adama_stream_capture_id",
     "adama_layer_norm", "adama_layer_norm_backward", "adama_layer_norm_workspace",
-    "adama_embedding", "adama_embedding_grad", "adama_embedding_workspace",
+    "adama_embedding", "adama_embedding_grad", "adama_embedding_workspace", "adama_distill_loss",
 ]
 
 
@@ -75,6 +75,7 @@ class _State8(ctypes.Structure):
 _POLICY_ARGS = struct.Struct("@PPii4qPPPPP4dPPP")
 
 
+_DISTILL_ARGS = struct.Struct("@PPiiii6qPPPPdPPP")   # adama_distill_args
 # adama_layer_norm_args, adama_layer_norm_backward_args, adama_embedding_args, adama_embedding_grad_args
 _LAYER_NORM_ARGS = struct.Struct("@PPii4qPPdPP")
 _LAYER_NORM_BACKWARD_ARGS = struct.Struct("@PPPii5q10P")
@@ -151,7 +152,7 @@ def load_library() -> ctypes.CDLL:
     L.adama_grad_norm_multi.argtypes = [vp, vp, ci, vp, ci, dbl, ci, vp, vp, vp]
     L.adama_token_logprobs.argtypes = [vp, vp, ci, i64, i64, i64, vp, dbl, vp, vp, vp, vp]
     L.adama_policy_loss.argtypes = [vp, ctypes.c_char_p, vp]
-    for name in ("layer_norm", "layer_norm_backward", "embedding", "embedding_grad"):
+    for name in ("distill_loss", "layer_norm", "layer_norm_backward", "embedding", "embedding_grad"):
         getattr(L, "adama_" + name).argtypes = [vp, ctypes.c_char_p, vp]
     for name in ("layer_norm", "embedding"):
         getattr(L, f"adama_{name}_workspace").argtypes = [vp, i64, i64]
@@ -748,6 +749,37 @@ class AdamA:
             row(weights, rows, "weights"), logit_scale, clip_low, clip_high, kl_coef, row(logp, rows, "logp"),
             _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream))
         self._check(self._L.adama_policy_loss(self._h, args, stream))
+
+    def distill_loss(self, logits: torch.Tensor, teacher_logits: torch.Tensor, teacher_ids: torch.Tensor, weights: torch.Tensor,
+                     dlogits: Optional[torch.Tensor], stats: torch.Tensor, teacher_lse: Optional[torch.Tensor] = None,
+                     loss: Optional[torch.Tensor] = None, logit_scale: float = 1.0) -> None:
+        """adama_distill_loss: divergence from a teacher known by its top logits, `teacher_logits` [rows, top] (fp32 or
+        bf16) at the indices `teacher_ids` [rows, top] (int64; negative = no entry).  `stats` (4 fp32) receives {loss, cross
+        entropy, student's mass on the entries, teacher's mass}, each weighted by `weights`; `loss` each row's
+        divergence; `dlogits` (fp32 or bf16, `logits` itself, or None) the gradient.  Without `teacher_lse` the entries
+        are the whole of the teacher's distribution."""
+        ptr, dt, ld = self._rows(logits, "logits")
+        rows, vocab = logits.shape
+        dptr, ddt, dld = 0, dt, 0
+        if dlogits is not None:
+            if dlogits.shape != logits.shape:
+                raise ValueError("dlogits must have the shape of logits")
+            dptr, ddt, dld = self._rows(dlogits, "dlogits")
+        tptr, tdt, tld = self._rows(teacher_logits, "teacher_logits")
+        top = teacher_logits.shape[1]
+        if teacher_logits.shape[0] != rows or teacher_ids.shape != teacher_logits.shape:
+            raise ValueError("teacher_logits and teacher_ids must be [rows, top]")
+        if top > 1 and teacher_ids.stride(1) != 1:
+            raise ValueError("teacher_ids must have unit stride in its last dimension")
+        if stats.numel() != 4 or not stats.is_contiguous():
+            raise ValueError("stats must hold 4 contiguous float32 values")
+        stream = _stream_ptr(self.device)
+        row = self._per_row
+        args = _DISTILL_ARGS.pack(
+            ptr, dptr, dt, ddt, tdt, top, rows, vocab, ld, dld, tld, max(top, teacher_ids.stride(0)) if rows < 2 else teacher_ids.stride(0),
+            tptr, _dev_ptr(teacher_ids, torch.int64, "teacher_ids"), row(teacher_lse, rows, "teacher_lse"), row(weights, rows, "weights"),
+            logit_scale, row(loss, rows, "loss"), _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream))
+        self._check(self._L.adama_distill_loss(self._h, args, stream))
 
     # -- norms and embeddings ----------------------------------------------------------------
     def _scratch(self, stream: int, of: str, rows: int, dim: int) -> int:

@@ -810,6 +810,58 @@ adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args *p, void 
     return ADAMA_OK;
 }
 
+adama_status adama_distill_loss(adama_ctx *ctx, const adama_distill_args *p, void *cuda_stream) {
+    if (!ctx) return ADAMA_ERR_INVALID_ARG;
+    if (!p) return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: null arguments");
+    // (the entries' indices stand where the targets of the other calls do)
+    adama_status st = check_logits(ctx, p->logits, p->logits_dtype, p->rows, p->vocab, p->ld_logits, p->ids, p->logit_scale);
+    if (st != ADAMA_OK) return st;
+    if ((p->dlogits_dtype != ADAMA_F32 && p->dlogits_dtype != ADAMA_BF16) ||
+        (p->teacher_dtype != ADAMA_F32 && p->teacher_dtype != ADAMA_BF16))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: unknown dtype");
+    if (!p->stats || !p->workspace || (p->rows > 0 && (!p->teacher_logits || !p->weights)))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: null pointer");
+    if (p->top < 1) return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: a row needs an entry");
+    if (p->top > ADAMA_DISTILL_TOP) return fail(ctx, ADAMA_ERR_UNSUPPORTED, "distill_loss: more than 128 entries in a row");
+    if (p->ld_teacher < p->top || p->ld_ids < p->top || (p->dlogits && p->ld_dlogits < p->vocab))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: a row pitch smaller than the row");
+    if (p->dlogits == p->logits && p->rows > 0 &&
+        (p->dlogits_dtype != p->logits_dtype || p->ld_dlogits != p->ld_logits))
+        return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: in place needs one dtype and one pitch");
+    if (!aligned_to(p->dlogits, dtype_size(p->dlogits_dtype)) || !aligned_to(p->teacher_logits, dtype_size(p->teacher_dtype)) ||
+        !aligned_to(p->teacher_lse, 4) || !aligned_to(p->weights, 4) || !aligned_to(p->loss, 4) || !aligned_to(p->stats, 4) ||
+        !aligned_to(p->workspace, 16))
+        return fail(ctx, ADAMA_ERR_MISALIGNED, "distill_loss: pointer not aligned");
+    DeviceGuard guard(ctx->cfg.device);
+    adama::DistillArgs a;
+    a.logits = p->logits;
+    a.dlogits = p->dlogits;
+    a.logits_dtype = p->logits_dtype;
+    a.dlogits_dtype = p->dlogits_dtype;
+    a.teacher_dtype = p->teacher_dtype;
+    a.top = p->top;
+    a.rows = p->rows;
+    a.vocab = p->vocab;
+    a.ld_logits = p->ld_logits;
+    a.ld_dlogits = p->ld_dlogits;
+    a.ld_teacher = p->ld_teacher;
+    a.ld_ids = p->ld_ids;
+    a.teacher = p->teacher_logits;
+    a.ids = p->ids;
+    a.teacher_lse = p->teacher_lse;
+    a.weights = p->weights;
+    a.scale_exact = p->logit_scale;
+    a.scale = (float)p->logit_scale;
+    a.loss = p->loss;
+    a.stats = p->stats;
+    a.workspace = p->workspace;
+    a.status = ctx->status_dev;
+    cudaError_t e = adama::launch_distill_loss(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream));
+    if (e != cudaSuccess) return cuda_fail(ctx, "distill_loss launch", e);
+    ctx->launches += 1;
+    return ADAMA_OK;
+}
+
 // ---- norms and embeddings ---------------------------------------------------------------------
 
 // A [rows, cols] matrix of a call: what is wrong with it, or OK.
@@ -1245,7 +1297,7 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
         if (e != cudaSuccess) return cuda_fail(ctx, "sync_status", e);
         snprintf(ctx->err, sizeof(ctx->err),
                  "device-side wait expired in the %s kernel (code %u, wait %u, tile %u)",
-                 host[1] == adama::kWaitPolicyRing   ? "policy-loss"
+                 host[1] == adama::kWaitPolicyRing   ? "policy-loss or distillation"
                  : host[1] == adama::kWaitState8Ring ? "8-bit update"
                  : host[1] == adama::kWaitStepRing   ? "update"
                                                      : "fused weight-gradient",
@@ -1256,7 +1308,7 @@ adama_status adama_sync_status(adama_ctx *ctx, void *cuda_stream) {
     if (target[0] != 0) {
         e = clear(adama::kStatusTarget);
         if (e != cudaSuccess) return cuda_fail(ctx, "sync_status", e);
-        snprintf(ctx->err, sizeof(ctx->err), "a target or an id lies outside the vocabulary (row %llu of its call)",
+        snprintf(ctx->err, sizeof(ctx->err), "a target, an id or an index lies outside the vocabulary (row %llu of its call)",
                  (unsigned long long)target[2] << 32 | target[1]);
         return ADAMA_ERR_INVALID_ARG;
     }

@@ -153,6 +153,24 @@ struct PolicyArgs {
     unsigned *status;
 };
 cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream);
+struct DistillArgs {
+    const void *logits;
+    void *dlogits;  // may be null: no gradient
+    adama_dtype logits_dtype, dlogits_dtype, teacher_dtype;
+    int top;  // entries of a row
+    int64_t rows, vocab, ld_logits, ld_dlogits, ld_teacher, ld_ids;
+    const void *teacher;
+    const int64_t *ids;
+    const float *teacher_lse;  // may be null: the entries' own
+    const float *weights;
+    double scale_exact;
+    float scale;
+    float *loss;  // may be null
+    float *stats;
+    void *workspace;
+    unsigned *status;
+};
+cudaError_t launch_distill_loss(const DistillArgs &a, int sm_count, cudaStream_t stream);
 
 // layer norm (layer_norm.cu)
 struct NormArgs {

@@ -12,9 +12,11 @@
 
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"
-#include "policy_plan.h"
-#include "softmax_rows.cuh"
-#include "tensor_table.cuh"
+#include "distill.cuh"
+#include "logit_ring.cuh"
+#include "row_writer.cuh"
+
+#include <type_traits>
 
 namespace adama {
 namespace {
@@ -45,12 +47,6 @@ __device__ __forceinline__ Stats group_join(Stats s, float k, Stats *slots, int 
 // In natural units: the rounding of k does not show but through the sum.
 __device__ __forceinline__ float logp_of(float x_target, const Stats &s, float log_sum, float scale) {
     return fmaf(scale, x_target - s.top, -log_sum);
-}
-
-// The slice of a row's units that CTA `rank` of 2^log_size takes (units < 2^29, so 32 bits hold it).
-__device__ __forceinline__ void slice_of(int units, int rank, int log_size, int &from, int &count) {
-    from = (int)(((unsigned)units * (unsigned)rank) >> log_size);
-    count = (int)(((unsigned)units * (unsigned)(rank + 1)) >> log_size) - from;
 }
 
 __device__ __forceinline__ void store_peer(const Stats *slot, uint32_t rank, const Stats &s) {
@@ -150,6 +146,29 @@ __device__ __forceinline__ RowIn row_in(const PolicyArgs &a, int64_t row) {
     return r;
 }
 
+// Whether a row is read at all, in two steps: what decides it can be loaded ahead.
+struct PolicyMask {
+    float weight = 0.f;
+    int64_t target = -1;
+
+    __device__ __forceinline__ bool live() const { return weight != 0.f && target >= 0; }
+};
+__device__ __forceinline__ PolicyMask row_mask(const PolicyArgs &a, int64_t row) {
+    PolicyMask m;
+    m.weight = a.weights[row];
+    m.target = a.targets[row];
+    return m;
+}
+struct DistillMask {
+    float weight = 0.f;
+
+    __device__ __forceinline__ bool live() const { return weight != 0.f; }
+};
+__device__ __forceinline__ DistillMask row_mask(const DistillArgs &a, int64_t row) { return {a.weights[row]}; }
+
+template <typename Args>
+constexpr bool kDistill = std::is_same<Args, DistillArgs>::value;
+
 // exp(d) - d - 1, and exp(d) - 1.  Policies that are close have d of 1e-5 to 1e-2 and a KL of d^2/2: the
 // difference of exp(d) and d + 1 would leave noise of 6e-8 there.  Below 1/2 the exponential series without its
 // first two terms is summed instead (the first one left out is 2e-8 of the sum); from 1/2 on the
@@ -198,23 +217,14 @@ __device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, 
     return o;
 }
 
-// Sums of one thread over its rows; in double, so that their order does not show in fp32.
-struct Sums {
-    double v[4] = {0.0, 0.0, 0.0, 0.0};
-
-    __device__ __forceinline__ void add(const PolicyArgs &a, const RowIn &in, const RowOut &o) {
-        const double w = in.weight;
-        v[0] += w * (o.pg + (a.ref_logp && a.kl_coef != 0.f ? a.kl_coef * o.kl : 0.f));
-        v[1] += w * o.pg;
-        v[2] += w * o.kl;
-        v[3] += w * o.cut;
-    }
-};
+__device__ __forceinline__ void add_terms(Sums &sums, const PolicyArgs &a, const RowIn &in, const RowOut &o) {
+    sums.add(in.weight, o.pg + (a.ref_logp && a.kl_coef != 0.f ? a.kl_coef * o.kl : 0.f), o.pg, o.kl, o.cut);
+}
 
 // The leaders' sums -> the CTA's in the workspace -> stats, by the last CTA, in the CTAs' order.  All
 // THREADS call it; thread LEADER*i holds the sums of leader i.  CTA `index` of `count` that have sums.
-template <int THREADS, int LEADER>
-__device__ __forceinline__ void finish_stats(const PolicyArgs &a, const Sums &s, double (*slots)[4], volatile int *last,
+template <int THREADS, int LEADER, typename Args>
+__device__ __forceinline__ void finish_stats(const Args &a, const Sums &s, double (*slots)[4], volatile int *last,
                                              int t, unsigned index, unsigned count) {
     static_assert(THREADS / 32 <= kWarps, "slots");
     constexpr int kLeaders = THREADS / LEADER;
@@ -254,129 +264,6 @@ __device__ __forceinline__ void finish_stats(const PolicyArgs &a, const Sums &s,
     }
     if (t == 0) ws->ticket = 0;
 }
-
-template <typename O>
-__device__ __forceinline__ O narrow(float y);
-template <>
-__device__ __forceinline__ float narrow<float>(float y) { return y; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
-
-// N values as 32-bit words of their type
-__device__ __forceinline__ void to_words(const float (&v)[4], unsigned (&w)[4], float) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
-}
-__device__ __forceinline__ void to_words(const float (&v)[8], unsigned (&w)[8], float) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[i]);
-}
-__device__ __forceinline__ void to_words(const float (&v)[4], unsigned (&w)[2], __nv_bfloat16) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) w[i] = pack2_bf16(v[2 * i], v[2 * i + 1]);
-}
-__device__ __forceinline__ void to_words(const float (&v)[8], unsigned (&w)[4], __nv_bfloat16) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack2_bf16(v[2 * i], v[2 * i + 1]);
-}
-__device__ __forceinline__ void store_words(void *p, const unsigned (&w)[2]) { *static_cast<uint2 *>(p) = make_uint2(w[0], w[1]); }
-__device__ __forceinline__ void store_words(void *p, const unsigned (&w)[4]) {
-    *static_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store_words(void *p, const unsigned (&w)[8]) {
-    static_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    static_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-}
-
-// Zeros to p[0 .. n) by `threads` threads.
-template <typename O>
-__device__ __forceinline__ void fill_zeros(O *p, int64_t n, int t, int threads) {
-    constexpr int kPer = 16 / sizeof(O);
-    const int mis = (int)(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(O));
-    const int64_t head = mis ? (kPer - mis < n ? kPer - mis : n) : 0, body = (n - head) / kPer;
-    for (int64_t i = t; i < body; i += threads) reinterpret_cast<uint4 *>(p + head)[i] = make_uint4(0, 0, 0, 0);
-    const int64_t tail0 = head + body * kPer;
-    if (t < head) p[t] = narrow<O>(0.f);
-    if (t < n - tail0) p[tail0 + t] = narrow<O>(0.f);
-}
-
-// How a row's gradient is written.  The units are written without the target's extra term; the
-// thread that wrote the target's element writes it again, with the term.
-//
-// A unit's gradient is one aligned store where logits and gradient have the same alignment.  Where they
-// have not, a thread takes the window of N logits from `shift` on, which ends in the next unit: the
-// raw words of both are shifted into place before anything is computed, and only the first `shift`
-// elements of a slice and the last N - shift are stored one by one.  (Then logits and gradient are
-// different buffers: in place they share their pitch.)
-template <typename T, typename O>
-struct RowWriter {
-    static constexpr int N = kUnit<T>;
-    static constexpr int kWords = N * sizeof(O) / 4;             // a unit's gradient
-    static constexpr int kStoreWords = kWords < 4 ? kWords : 4;  // one store
-    int shift;  // elements between a unit's first one and the next aligned address; 0: aligned stores
-    float top, unit, per_e, k;
-
-    __device__ __forceinline__ RowWriter(const O *row, const RowShape &shape, float top_, float unit_, float per_e_, float k_)
-        : top(top_), unit(unit_), per_e(per_e_), k(k_) {
-        constexpr int kPer = kStoreWords * 4 / sizeof(O);
-        const int mis = (int)(reinterpret_cast<uintptr_t>(row + shape.head) % (kStoreWords * 4) / sizeof(O));
-        shift = mis ? kPer - mis : 0;
-    }
-    // the gradient of N logits
-    __device__ __forceinline__ void values(const uint4 &u, float (&v)[N]) const {
-        const Pair k2 = pair(k, k), per = pair(per_e, per_e);
-#pragma unroll
-        for (int q = 0; q < N / 2; ++q) {
-            float d0, d1;
-            split(mul2(unit_less<T>(u, q, top), k2), d0, d1);
-            split(mul2(pair(exp2_fast(d0), exp2_fast(d1)), per), v[2 * q], v[2 * q + 1]);
-        }
-    }
-    __device__ __forceinline__ void put(const uint4 &u, O *p) const {
-        float v[N];
-        values(u, v);
-        unsigned w[kWords];
-        to_words(v, w, O());
-        store_words(p, w);
-    }
-    // shift > 0: u goes to p; `first`: the slice begins with it, `last`: it ends with it, else `next` follows
-    __device__ __forceinline__ void put_shifted(const uint4 &u, const uint4 &next, O *p, bool first, bool last) const {
-        unsigned z[8] = {u.x, u.y, u.z, u.w, next.x, next.y, next.z, next.w};
-        const int words = shift * (int)sizeof(T) / 4;
-        if (words & 2) {
-#pragma unroll
-            for (int i = 0; i < 6; ++i) z[i] = z[i + 2];
-        }
-        if (words & 1) {
-#pragma unroll
-            for (int i = 0; i < 5; ++i) z[i] = z[i + 1];
-        }
-        if (sizeof(T) == 2 && (shift & 1)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) z[i] = __funnelshift_r(z[i], z[i + 1], 16);
-        }
-        if (!last) put(make_uint4(z[0], z[1], z[2], z[3]), p + shift);
-        if (first || last) {
-            float v[N];
-            values(u, v);
-#pragma unroll
-            for (int q = 0; q < N; ++q)
-                if (q < shift ? first : last) p[q] = narrow<O>(v[q]);
-        }
-    }
-    __device__ __forceinline__ O value(float x, bool is_target) const {
-        const float p = per_e * exp2_fast(k * (x - top));
-        return narrow<O>(is_target ? p + unit : p);
-    }
-    // Thread of a group of `threads` that wrote element j, of a slice of `count` units from unit `from`
-    // on that go round the threads; -1: it is not among the slice's units.
-    __device__ __forceinline__ int writer_of(const RowShape &shape, int64_t j, int from, int count, int threads) const {
-        const int64_t at = j - shape.head - (int64_t)from * N;
-        if (at < 0 || at >= (int64_t)count * N) return -1;
-        const int u = (int)(at / N);
-        return (at % N < shift && u > 0 ? u - 1 : u) % threads;
-    }
-};
 
 // ---- rows that fit a warp's registers -----------------------------------------------------------
 
@@ -423,7 +310,7 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
         __syncwarp();  // the gradient may replace the logits: no lane writes before all have read (a join alone orders no memory)
         const RowOut o = row_out(a, in, s, x_target);
         if (lane == 0) {
-            acc.add(a, in, o);
+            add_terms(acc, a, in, o);
             if (!inside) record_bad_target(a.status, row);
             if (a.logp) a.logp[row] = o.logp;
         }
@@ -449,6 +336,83 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
     finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
 }
 
+// The same for distillation: the warp's lanes hold the entries, too.
+template <typename T, typename O>
+__global__ void __launch_bounds__(kThreads, 2)
+distill_rows_kernel(const DistillArgs a, float k) {
+    __shared__ double sums[kWarps][4];
+    __shared__ int last;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    Sums acc;
+    for (int64_t row = (int64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (int64_t)gridDim.x * kWarps) {
+        const float weight = a.weights[row];
+        O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+        if (weight == 0.f) {
+            if (lane == 0 && a.loss) a.loss[row] = 0.f;
+            if (a.dlogits) fill_zeros(y, a.vocab, lane, 32);
+            continue;
+        }
+        const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+        const RowShape shape = row_shape(x, (int)a.vocab);
+        const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
+        const bool has_extra = lane < shape.head + shape.tail;
+        const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
+        const RawEntries raw = load_entries(a, row, lane);
+        uint4 u[kRowUnits];
+#pragma unroll
+        for (int i = 0; i < kRowUnits; ++i)
+            if (lane + 32 * i < shape.units) u[i] = ld_unit(body + lane + 32 * i);
+        const float x_extra = has_extra ? widen(x[extra]) : 0.f;
+        float x_at[kTopEach];
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e) x_at[e] = raw.id[e] >= 0 ? widen(x[raw.id[e]]) : 0.f;
+        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
+        Running<false> run;
+#pragma unroll
+        for (int i = 0; i < kRowUnits; ++i) {
+            if (lane + 32 * i < shape.units) {
+                const uint4 one[1] = {u[i]};
+                run.template add_units<T>(one, k);
+            }
+        }
+        if (has_extra) run.add_one(x_extra, k);
+        const Stats s = warp_join<false>(run.stats(), k);
+        const DistillOut o = distill_out(a, en, x_at, weight, s, k);
+        __syncwarp();  // the gradient may replace the logits: no lane writes before all have read
+        if (lane == 0) {
+            add_terms(acc, a, weight, en, o);
+            if (en.bad) record_bad_target(a.status, row);
+            if (a.loss) a.loss[row] = o.kl;
+        }
+        if (!a.dlogits) continue;
+        if (o.per_e == 0.f) {
+            fill_zeros(y, a.vocab, lane, 32);
+        } else {
+            const RowWriter<T, O> out(y, shape, s.top, 0.f, o.per_e, k);
+            O *p = y + shape.head + lane * kUnit<T>;
+            if (out.shift == 0) {
+#pragma unroll
+                for (int i = 0; i < kRowUnits; ++i)
+                    if (lane + 32 * i < shape.units) out.put(u[i], p + 32 * i * kUnit<T>);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRowUnits; ++i) {
+                    const int at = lane + 32 * i;
+                    if (at < shape.units)
+                        out.put_shifted(u[i], ld_unit(body + (at + 1 < shape.units ? at + 1 : at)), p + 32 * i * kUnit<T>, at == 0,
+                                        at + 1 == shape.units);
+                }
+            }
+            if (has_extra) y[extra] = out.value(x_extra, false);
+        }
+        __syncwarp();  // the entries' elements are written over
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e)
+            if (raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(en.bad ? CUDART_NAN_F : o.g[e]);
+    }
+    finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
+}
+
 // ---- longer rows: a ring in shared memory ------------------------------------------------------
 // A row, or its slice where a cluster of CTAs shares one, is brought to shared memory by bulk copies,
 // in stages; the statistics are taken from the stages as they arrive, then the gradient is computed
@@ -458,52 +422,9 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
 // which one warp of its own does meanwhile, and nobody waits for them.  The ring therefore holds two
 // rows (slices).  One more warp issues the copies.
 
-// What the gradient of a row needs.
-struct Verdict {
-    float top, unit, per_e, x_target;
-    int64_t target;
-    int writer;  // the thread that writes the target's element, or -1
-};
-
-// Two of each, for even and odd live rows: nobody is more than one row ahead.
-template <typename Cut>
-struct RingShared {
-    alignas(128) unsigned char stage[Cut::kStages][Cut::kStageBytes];
-    alignas(16) float4 peer[2][kMaxCluster];  // {top, sum, x_target} of the cluster's CTAs
-    Verdict verdict[2];
-    float2 slots[2][Cut::kWarps];             // {top, sum} of the warps
-    unsigned long long full[Cut::kStages], empty[Cut::kStages], joined[2], peered[2], ready[2];
-    double sums[1][4];
-    int last, give_up;
-};
-static_assert(sizeof(RingShared<Cut512>) + 128 <= 232448 && sizeof(RingShared<Cut640>) + 128 <= 232448, "shared memory of a CTA");
-static_assert(2 * (sizeof(RingShared<Cut256>) + 128 + 1024) <= 233472 &&
-                  4 * (sizeof(RingShared<Cut128>) + 128 + 1024) <= 233472 &&
-                  8 * (sizeof(RingShared<Cut64>) + 128 + 1024) <= 233472,
-              "shared memory of an SM");
-
-// Place in the ring: a stage, and the parity of the barrier phase that its current use completes.
-template <int STAGES>
-struct Cursor {
-    uint32_t slot = 0, parity = 0;
-
-    __device__ __forceinline__ void advance() {
-        if (++slot == STAGES) {
-            slot = 0;
-            parity ^= 1;
-        }
-    }
-};
-
-__device__ __forceinline__ Stats join2(const Stats &a, const Stats &b, float k) {
-    const float top = fmaxf(a.top, b.top);
-    const Stats p = raised(a, top, k), q = raised(b, top, k);
-    return {top, p.sum + q.sum, 0.f};
-}
-
-template <typename T, typename O, typename Cut>
+template <typename T, typename O, typename Cut, typename Args>
 __global__ void __launch_bounds__(Cut::kThreads, Cut::kPerSm)
-policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
+policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
     constexpr int kStages = Cut::kStages, kStageUnits = Cut::kStageUnits, kRingWork = Cut::kWork, kEach = Cut::kEach;
     extern __shared__ unsigned char raw[];
     RingShared<Cut> &sh = *reinterpret_cast<RingShared<Cut> *>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
@@ -521,6 +442,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             barrier_init(shared_addr(&sh.peered[i]), 1);
             barrier_init(shared_addr(&sh.ready[i]), 1);
         }
+        if (kDistill<Args>) barrier_init(shared_addr(&sh.done), Cut::kWarps);
         sh.give_up = 0;
         barrier_init_fence();
     }
@@ -532,7 +454,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             Cursor<kStages> c;
             uint32_t issued = 0;  // stages, up to kStages
             for (int64_t row = first; row < a.rows && !*(volatile int *)&sh.give_up; row += step) {
-                if (a.weights[row] == 0.f || a.targets[row] < 0) continue;
+                if (!row_mask(a, row).live()) continue;
                 const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
                 const RowShape shape = row_shape(x, (int)a.vocab);
                 int from, count;
@@ -560,61 +482,65 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
         }
     } else if (warp == Cut::kScalarWarp) {
         Sums acc;
-        uint32_t n = 0;  // live rows
-        RowIn next = {-1, 0.f, 0.f, 0.f, 0.f};
-        if (first < a.rows) next = row_in(a, first);
-        for (int64_t row = first; row < a.rows; row += step) {
-            const RowIn in = next;
-            if (row + step < a.rows) next = row_in(a, row + step);
-            if (!in.live()) {
-                if (lane == 0 && rank == 0 && a.logp) a.logp[row] = 0.f;
-                continue;
-            }
-            const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
-            const RowShape shape = row_shape(x, (int)a.vocab);
-            int from, count;
-            slice_of(shape.units, rank, log_cluster, from, count);
-            const int b = n & 1;
-            const uint32_t parity = n >> 1 & 1;
-            const bool inside = in.target < a.vocab, has_extra = rank == 0 && lane < shape.head + shape.tail;
-            const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
-            // the gradient may replace the logits: what is read here travels with this CTA's message,
-            // before which nobody writes
-            float x_target = rank == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
-            const float x_extra = has_extra ? widen(x[extra]) : -CUDART_INF_F;
-            Running<false> run;
-            run.add_one(x_extra, k);
-            barrier_wait(shared_addr(&sh.joined[b]), parity, &sh.give_up);
-            const Stats none = {-CUDART_INF_F, 0.f, 0.f};
-            Stats s = none;
-            if (lane < Cut::kWarps) s = {sh.slots[b][lane].x, sh.slots[b][lane].y, 0.f};
-            s = warp_join<false>(join2(s, run.stats(), k), k);
-            if (cluster > 1) {
-                const uint32_t bar = shared_addr(&sh.peered[b]);
-                if (lane == 0) barrier_expect(bar, 16u * cluster);
-                if (lane < cluster) send16(shared_addr(&sh.peer[b][rank]), bar, lane, s.top, s.sum, x_target, 0.f);
-                barrier_wait(bar, parity, &sh.give_up);
-                float4 q = make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
-                if (lane < cluster) q = sh.peer[b][lane];
-                x_target = __shfl_sync(0xffffffffu, q.z, 0);
-                s = warp_join<false>({q.x, q.y, 0.f}, k);
-            }
-            const RowOut o = row_out(a, in, s, x_target);
-            O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
-            const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
-            __syncwarp();  // all lanes have read x_target, which the verdict's readers may overwrite
-            if (lane == 0) {
-                const int writer = inside ? out.writer_of(shape, in.target, from, count, kRingWork) : -1;
-                sh.verdict[b] = {s.top, o.unit, o.per_e, x_target, in.target, writer};
-                barrier_arrive(shared_addr(&sh.ready[b]));
-                if (rank == 0) {
-                    acc.add(a, in, o);
-                    if (a.logp) a.logp[row] = o.logp;
-                    if (!inside) record_bad_target(a.status, row);
+        if constexpr (kDistill<Args>) {
+            distill_verdicts<T, O>(a, k, sh, lane, rank, log_cluster, first, step, acc);
+        } else {
+            uint32_t n = 0;  // live rows
+            RowIn next = {-1, 0.f, 0.f, 0.f, 0.f};
+            if (first < a.rows) next = row_in(a, first);
+            for (int64_t row = first; row < a.rows; row += step) {
+                const RowIn in = next;
+                if (row + step < a.rows) next = row_in(a, row + step);
+                if (!in.live()) {
+                    if (lane == 0 && rank == 0 && a.logp) a.logp[row] = 0.f;
+                    continue;
                 }
+                const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+                const RowShape shape = row_shape(x, (int)a.vocab);
+                int from, count;
+                slice_of(shape.units, rank, log_cluster, from, count);
+                const int b = n & 1;
+                const uint32_t parity = n >> 1 & 1;
+                const bool inside = in.target < a.vocab, has_extra = rank == 0 && lane < shape.head + shape.tail;
+                const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
+                // the gradient may replace the logits: what is read here travels with this CTA's message,
+                // before which nobody writes
+                float x_target = rank == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
+                const float x_extra = has_extra ? widen(x[extra]) : -CUDART_INF_F;
+                Running<false> run;
+                run.add_one(x_extra, k);
+                barrier_wait(shared_addr(&sh.joined[b]), parity, &sh.give_up);
+                const Stats none = {-CUDART_INF_F, 0.f, 0.f};
+                Stats s = none;
+                if (lane < Cut::kWarps) s = {sh.slots[b][lane].x, sh.slots[b][lane].y, 0.f};
+                s = warp_join<false>(join2(s, run.stats(), k), k);
+                if (cluster > 1) {
+                    const uint32_t bar = shared_addr(&sh.peered[b]);
+                    if (lane == 0) barrier_expect(bar, 16u * cluster);
+                    if (lane < cluster) send16(shared_addr(&sh.peer[b][rank]), bar, lane, s.top, s.sum, x_target, 0.f);
+                    barrier_wait(bar, parity, &sh.give_up);
+                    float4 q = make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+                    if (lane < cluster) q = sh.peer[b][lane];
+                    x_target = __shfl_sync(0xffffffffu, q.z, 0);
+                    s = warp_join<false>({q.x, q.y, 0.f}, k);
+                }
+                const RowOut o = row_out(a, in, s, x_target);
+                O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+                const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
+                __syncwarp();  // all lanes have read x_target, which the verdict's readers may overwrite
+                if (lane == 0) {
+                    const int writer = inside ? out.writer_of(shape, in.target, from, count, kRingWork) : -1;
+                    sh.verdict[b] = {s.top, o.unit, o.per_e, x_target, in.target, writer};
+                    barrier_arrive(shared_addr(&sh.ready[b]));
+                    if (rank == 0) {
+                        add_terms(acc, a, in, o);
+                        if (a.logp) a.logp[row] = o.logp;
+                        if (!inside) record_bad_target(a.status, row);
+                    }
+                }
+                if (has_extra && a.dlogits) y[extra] = out.value(x_extra, extra == in.target);
+                ++n;
             }
-            if (has_extra && a.dlogits) y[extra] = out.value(x_extra, extra == in.target);
-            ++n;
         }
         if (lane == 0) report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
         __syncwarp();
@@ -638,7 +564,14 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 if (lane == 0) barrier_arrive(shared_addr(&sh.empty[at_stage.slot]));
             };
             O *p = y + shape.head + (int64_t)(from + t) * kUnit<T>;
-            if (!a.dlogits || !ok) {
+            bool skip = !a.dlogits || !ok;
+            if constexpr (kDistill<Args>) {
+                if (!skip && q.per_e == 0.f) {  // a row without entries, whatever its logits
+                    fill_zeros(y + shape.head + (int64_t)from * kUnit<T>, (int64_t)count * kUnit<T>, t, kRingWork);
+                    skip = true;
+                }
+            }
+            if (skip) {
                 for (int at = 0; at < count; at += kStageUnits, at_stage.advance()) release();
                 return;
             }
@@ -689,18 +622,11 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             }
             if (t == q.writer) y[q.target] = out.value(q.x_target, true);
         };
-        float next_weight = 0.f;
-        int64_t next_target = -1;
-        if (first < a.rows) {
-            next_weight = a.weights[first];
-            next_target = a.targets[first];
-        }
+        decltype(row_mask(a, first)) next;
+        if (first < a.rows) next = row_mask(a, first);
         for (int64_t row = first; row < a.rows; row += step) {
-            const bool live = next_weight != 0.f && next_target >= 0;
-            if (row + step < a.rows) {
-                next_weight = a.weights[row + step];
-                next_target = a.targets[row + step];
-            }
+            const bool live = next.live();
+            if (row + step < a.rows) next = row_mask(a, row + step);
             const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
             const RowShape new_shape = row_shape(x, (int)a.vocab);
             int new_from, new_count;
@@ -745,6 +671,7 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
                 }
             }
             const Stats s = warp_join<false>(run.stats(), k);
+            if (kDistill<Args>) __syncwarp();  // the arrival also says that row n-2 has been written
             if (lane == 0) {
                 sh.slots[n & 1][warp] = make_float2(s.top, s.sum);
                 barrier_arrive(shared_addr(&sh.joined[n & 1]));
@@ -758,6 +685,10 @@ policy_loss_ring_kernel(const PolicyArgs a, float k, int log_cluster) {
             ++n;
         }
         if (due >= 0) write_due();
+        if (kDistill<Args>) {
+            __syncwarp();
+            if (lane == 0) barrier_arrive(shared_addr(&sh.done));
+        }
         if (lane == 0) report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
     }
     if (cluster > 1) {
@@ -800,7 +731,7 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
             top = s.top;
             o = row_out(a, in, s, x_target);
             if (t == 0) {
-                acc.add(a, in, o);
+                add_terms(acc, a, in, o);
                 if (!inside) record_bad_target(a.status, row);
             }
         }
@@ -825,6 +756,74 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
             }
         }
         group_sync<kWarps>(0);  // the slots are used again
+    }
+    finish_stats<kThreads, kThreads>(a, acc, sums, &last, t, blockIdx.x, gridDim.x);
+}
+
+// The same for distillation: every warp makes the row's terms, the first one writes the entries' elements.
+template <typename T, typename O>
+__global__ void __launch_bounds__(kThreads)
+distill_long_kernel(const DistillArgs a, float k) {
+    __shared__ Stats shared[kWarps];
+    __shared__ double sums[kWarps][4];
+    __shared__ int last;
+    const int t = threadIdx.x, lane = t % 32;
+    Sums acc;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const float weight = a.weights[row];
+        const bool live = weight != 0.f;
+        const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+        O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+        const RowShape shape = row_shape(x, (int)a.vocab);
+        const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
+        const bool has_extra = t < shape.head + shape.tail;
+        const int extra = has_extra ? extra_index<T>(shape, t) : 0;
+        if (!live) {
+            if (t == 0 && a.loss) a.loss[row] = 0.f;
+            if (a.dlogits) fill_zeros(y, a.vocab, t, kThreads);
+            continue;
+        }
+        const RawEntries raw = load_entries(a, row, lane);
+        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
+        float x_at[kTopEach];
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e) x_at[e] = raw.id[e] >= 0 ? widen(x[raw.id[e]]) : 0.f;
+        const float x_extra = has_extra ? widen(x[extra]) : 0.f;
+        Running<false> run;
+        for (int i = t; i < shape.units; i += kThreads) {
+            const uint4 u[1] = {ld_unit(body + i)};
+            run.template add_units<T>(u, k);
+        }
+        if (has_extra) run.add_one(x_extra, k);
+        const Stats s = group_join<kWarps, false>(run.stats(), k, shared, 0);
+        const DistillOut o = distill_out(a, en, x_at, weight, s, k);
+        if (t == 0) {
+            add_terms(acc, a, weight, en, o);
+            if (en.bad) record_bad_target(a.status, row);
+            if (a.loss) a.loss[row] = o.kl;
+        }
+        group_sync<kWarps>(0);  // all warps have read their logits, and the slots are used again
+        if (!a.dlogits) continue;
+        if (o.per_e == 0.f) {
+            fill_zeros(y, a.vocab, t, kThreads);
+        } else {
+            const RowWriter<T, O> out(y, shape, s.top, 0.f, o.per_e, k);
+            O *p = y + shape.head;
+            if (out.shift == 0) {
+                for (int i = t; i < shape.units; i += kThreads) out.put(ld_unit(body + i), p + (int64_t)i * kUnit<T>);
+            } else {
+                for (int i = t; i < shape.units; i += kThreads)
+                    out.put_shifted(ld_unit(body + i), ld_unit(body + (i + 1 < shape.units ? i + 1 : i)),
+                                    p + (int64_t)i * kUnit<T>, i == 0, i + 1 == shape.units);
+            }
+            if (has_extra) y[extra] = out.value(x_extra, false);
+        }
+        group_sync<kWarps>(0);  // the entries' elements are written over
+        if (t < 32) {
+#pragma unroll
+            for (int e = 0; e < kTopEach; ++e)
+                if (raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(en.bad ? CUDART_NAN_F : o.g[e]);
+        }
     }
     finish_stats<kThreads, kThreads>(a, acc, sums, &last, t, blockIdx.x, gridDim.x);
 }
@@ -912,12 +911,23 @@ cudaError_t logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
 }
 
 template <typename T, typename O>
-cudaError_t policy_rows(const PolicyArgs &a, float k, int sm_count, cudaStream_t stream) {
-    policy_loss_rows_kernel<T, O><<<grid_of((a.rows + kWarps - 1) / kWarps, (int64_t)sm_count * 2), kThreads, 0, stream>>>(a, k);
-    return cudaGetLastError();
+void launch_rows(const PolicyArgs &a, float k, unsigned grid, cudaStream_t stream) {
+    policy_loss_rows_kernel<T, O><<<grid, kThreads, 0, stream>>>(a, k);
+}
+template <typename T, typename O>
+void launch_rows(const DistillArgs &a, float k, unsigned grid, cudaStream_t stream) {
+    distill_rows_kernel<T, O><<<grid, kThreads, 0, stream>>>(a, k);
+}
+template <typename T, typename O>
+void launch_long(const PolicyArgs &a, float k, unsigned grid, cudaStream_t stream) {
+    policy_loss_long_kernel<T, O><<<grid, kThreads, 0, stream>>>(a, k);
+}
+template <typename T, typename O>
+void launch_long(const DistillArgs &a, float k, unsigned grid, cudaStream_t stream) {
+    distill_long_kernel<T, O><<<grid, kThreads, 0, stream>>>(a, k);
 }
 
-template <typename T, typename O, typename Cut>
+template <typename T, typename O, typename Cut, typename Args>
 struct RingLaunch {
     static constexpr int kBytes = (int)sizeof(RingShared<Cut>) + 128;
     cudaLaunchConfig_t cfg = {};
@@ -937,7 +947,7 @@ struct RingLaunch {
 
     static cudaError_t prepare() {
         static std::atomic<unsigned long long> ready{0};
-        return allow_shared(policy_loss_ring_kernel<T, O, Cut>, kBytes, ready);
+        return allow_shared(policy_loss_ring_kernel<T, O, Cut, Args>, kBytes, ready);
     }
     // Clusters that run at a time.  A GPC's SMs need not be a multiple of the cluster's (132 of 148 SMs
     // take part in clusters of 4, 120 in clusters of 8), and a cluster that waits for its turn would leave
@@ -956,7 +966,7 @@ struct RingLaunch {
             e = prepare();
             if (e != cudaSuccess) return e;
             RingLaunch l(cluster, sm_count * Cut::kPerSm / cluster, nullptr);
-            e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O, Cut>, &l.cfg);
+            e = cudaOccupancyMaxActiveClusters(&m, policy_loss_ring_kernel<T, O, Cut, Args>, &l.cfg);
             if (e != cudaSuccess) return e;
             if (m < 1) m = 1;
             if (slot) slot->store(m);
@@ -964,36 +974,44 @@ struct RingLaunch {
         *out = m;
         return cudaSuccess;
     }
-    static cudaError_t launch(const PolicyArgs &a, float k, int cluster, int sm_count, cudaStream_t stream) {
+    static cudaError_t launch(const Args &a, float k, int cluster, int sm_count, cudaStream_t stream) {
         int most = 0;
         cudaError_t e = prepare();
         if (e == cudaSuccess) e = resident(cluster, sm_count, &most);
         if (e != cudaSuccess) return e;
         RingLaunch l(cluster, a.rows < 1 ? 1 : a.rows < most ? a.rows : most, stream);
-        return cudaLaunchKernelEx(&l.cfg, policy_loss_ring_kernel<T, O, Cut>, a, k, log2_of(cluster));
+        return cudaLaunchKernelEx(&l.cfg, policy_loss_ring_kernel<T, O, Cut, Args>, a, k, log2_of(cluster));
     }
 };
 
-template <typename T, typename O>
-cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
+// A loss and its gradient: the policy loss's arguments or the distillation's.
+template <typename T, typename O, typename Args>
+cudaError_t loss(const Args &a, int sm_count, cudaStream_t stream) {
     const float k = (float)(a.scale_exact * kLog2e);
     PolicyPlan plan;
     const int e = plan_policy(a.vocab / kUnit<T>, a.rows, sm_count, [&](PolicyForm form, int cluster, int *most) {
-        return (int)(form == kForm640 ? RingLaunch<T, O, Cut640>::resident(cluster, sm_count, most)
-                                      : RingLaunch<T, O, Cut512>::resident(cluster, sm_count, most));
+        return (int)(form == kForm640 ? RingLaunch<T, O, Cut640, Args>::resident(cluster, sm_count, most)
+                                      : RingLaunch<T, O, Cut512, Args>::resident(cluster, sm_count, most));
     }, plan);
     if (e != 0) return (cudaError_t)e;
     switch (plan.form) {
-        case kFormRows: return policy_rows<T, O>(a, k, sm_count, stream);
-        case kForm64: return RingLaunch<T, O, Cut64>::launch(a, k, plan.cluster, sm_count, stream);
-        case kForm128: return RingLaunch<T, O, Cut128>::launch(a, k, plan.cluster, sm_count, stream);
-        case kForm256: return RingLaunch<T, O, Cut256>::launch(a, k, plan.cluster, sm_count, stream);
-        case kForm512: return RingLaunch<T, O, Cut512>::launch(a, k, plan.cluster, sm_count, stream);
-        case kForm640: return RingLaunch<T, O, Cut640>::launch(a, k, plan.cluster, sm_count, stream);
-        case kFormLong: break;
+        case kForm64: return RingLaunch<T, O, Cut64, Args>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm128: return RingLaunch<T, O, Cut128, Args>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm256: return RingLaunch<T, O, Cut256, Args>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm512: return RingLaunch<T, O, Cut512, Args>::launch(a, k, plan.cluster, sm_count, stream);
+        case kForm640: return RingLaunch<T, O, Cut640, Args>::launch(a, k, plan.cluster, sm_count, stream);
+        case kFormRows: launch_rows<T, O>(a, k, grid_of((a.rows + kWarps - 1) / kWarps, (int64_t)sm_count * 2), stream); break;
+        case kFormLong: launch_long<T, O>(a, k, grid_of(a.rows, (int64_t)sm_count * 4), stream); break;
     }
-    policy_loss_long_kernel<T, O><<<grid_of(a.rows, (int64_t)sm_count * 4), kThreads, 0, stream>>>(a, k);
     return cudaGetLastError();
+}
+
+template <typename Args>
+cudaError_t any_loss(const Args &a, int sm_count, cudaStream_t stream) {
+    if (a.logits_dtype == ADAMA_F32)
+        return a.dlogits_dtype == ADAMA_F32 ? loss<float, float>(a, sm_count, stream) : loss<float, __nv_bfloat16>(a, sm_count, stream);
+    return a.dlogits_dtype == ADAMA_F32 ? loss<__nv_bfloat16, float>(a, sm_count, stream)
+                                        : loss<__nv_bfloat16, __nv_bfloat16>(a, sm_count, stream);
 }
 
 }  // namespace
@@ -1001,13 +1019,7 @@ cudaError_t policy(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
 cudaError_t launch_token_logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
     return a.dtype == ADAMA_F32 ? logprobs<float>(a, sm_count, stream) : logprobs<__nv_bfloat16>(a, sm_count, stream);
 }
-
-cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
-    if (a.logits_dtype == ADAMA_F32)
-        return a.dlogits_dtype == ADAMA_F32 ? policy<float, float>(a, sm_count, stream)
-                                            : policy<float, __nv_bfloat16>(a, sm_count, stream);
-    return a.dlogits_dtype == ADAMA_F32 ? policy<__nv_bfloat16, float>(a, sm_count, stream)
-                                        : policy<__nv_bfloat16, __nv_bfloat16>(a, sm_count, stream);
-}
+cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream) { return any_loss(a, sm_count, stream); }
+cudaError_t launch_distill_loss(const DistillArgs &a, int sm_count, cudaStream_t stream) { return any_loss(a, sm_count, stream); }
 
 }  // namespace adama
