@@ -19,19 +19,22 @@ struct RawEntries {
     int id[kTopEach];
     float t[kTopEach];
 };
+// Whether a warp has entries at 32*e: most rows have fewer than 128, and the warp that deals with them works alone.
+__device__ __forceinline__ bool in_use(const DistillArgs &a, int e) { return e == 0 || 32 * e < a.top; }
+
 __device__ __forceinline__ RawEntries load_entries(const DistillArgs &a, int64_t row, int lane) {
     RawEntries r;
+    const int64_t *ids = a.ids + row * a.ld_ids + lane;
+    const int64_t at = row * a.ld_teacher + lane;
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e) {
         r.id[e] = -1;
         r.t[e] = -CUDART_INF_F;
-        const int i = 32 * e + lane;
-        if (i < a.top) {
-            const int64_t id = a.ids[row * a.ld_ids + i];
+        if (in_use(a, e) && 32 * e + lane < a.top) {
+            const int64_t id = ids[32 * e];
             r.id[e] = id < 0 ? -1 : id < a.vocab ? (int)id : -2;
-            const int64_t at = row * a.ld_teacher + i;
-            r.t[e] = a.teacher_dtype == ADAMA_F32 ? static_cast<const float *>(a.teacher)[at]
-                                                  : widen(static_cast<const __nv_bfloat16 *>(a.teacher)[at]);
+            r.t[e] = a.teacher_dtype == ADAMA_F32 ? static_cast<const float *>(a.teacher)[at + 32 * e]
+                                                  : widen(static_cast<const __nv_bfloat16 *>(a.teacher)[at + 32 * e]);
         }
     }
     return r;
@@ -57,32 +60,33 @@ struct Entries {
     float mass;            // P; NaN where an index lies outside the vocabulary
     bool bad;
 };
-__device__ __forceinline__ Entries entries_of(const DistillArgs &a, const RawEntries &raw, float lse, int lane) {
+__device__ __forceinline__ Entries entries_of(const DistillArgs &a, const RawEntries &raw, float lse) {
     Entries r;
     bool bad = false;
     float top = -CUDART_INF_F;
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e) {
-        bad |= raw.id[e] == -2;
         r.id[e] = raw.id[e] < 0 ? -1 : raw.id[e];
-        if (r.id[e] >= 0) top = fmaxf(top, raw.t[e] != raw.t[e] ? CUDART_INF_F : raw.t[e]);  // a NaN shows below
+        r.p[e] = r.logp[e] = 0.f;
+        if (in_use(a, e)) {
+            bad |= raw.id[e] == -2;
+            if (r.id[e] >= 0) top = fmaxf(top, raw.t[e] != raw.t[e] ? CUDART_INF_F : raw.t[e]);  // a NaN shows below
+        }
     }
     r.bad = __any_sync(0xffffffffu, bad);
-    top = warp_max(top);
-    float offset = -lse;  // log p = s*t + offset, or s*(t - top) + offset
+    float offset = -lse, ref = 0.f;  // log p = s*(t - ref) + offset
     if (!a.teacher_lse) {
+        ref = warp_max(top);
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e)
-            if (r.id[e] >= 0 && top != -CUDART_INF_F) sum += expf(a.scale * (raw.t[e] - top));
+            if (in_use(a, e) && r.id[e] >= 0 && ref != -CUDART_INF_F) sum += expf(a.scale * (raw.t[e] - ref));
         offset = -logf(warp_sum(sum));
     }
-    const float ref = a.teacher_lse ? 0.f : top;
     float mass = 0.f;
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e) {
-        r.p[e] = r.logp[e] = 0.f;
-        if (r.id[e] >= 0 && raw.t[e] != -CUDART_INF_F) {
+        if (in_use(a, e) && r.id[e] >= 0 && raw.t[e] != -CUDART_INF_F) {
             r.logp[e] = fmaf(a.scale, raw.t[e] - ref, offset);
             r.p[e] = expf(r.logp[e]);
         }
@@ -93,25 +97,27 @@ __device__ __forceinline__ Entries entries_of(const DistillArgs &a, const RawEnt
     if (r.bad) r.mass = CUDART_NAN_F;
     // The same index twice: rare, but its element has one gradient.  First whether there is any.
     bool twice = false;
-    int sets = 0;
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e)
-        if (32 * e < a.top) {
-            sets = e + 1;
+        if (in_use(a, e)) {
             const unsigned same = __match_any_sync(0xffffffffu, r.id[e]);
             twice |= r.id[e] >= 0 && (same & (same - 1)) != 0;
         }
-    for (int l = 0; sets > 1 && l < 32; ++l) {
 #pragma unroll
-        for (int f = 0; f < kTopEach - 1; ++f)
-            if (f + 1 < sets) {
-                const int id = __shfl_sync(0xffffffffu, r.id[f], l);
+    for (int f = 0; f < kTopEach - 1; ++f)
+        if (in_use(a, f + 1)) {
+            const int id = r.id[f] < 0 ? -2 : r.id[f];
+#pragma unroll 8
+            for (int l = 0; l < 32; ++l) {
+                const int other = __shfl_sync(0xffffffffu, id, l);
 #pragma unroll
-                for (int e = f + 1; e < kTopEach; ++e) twice |= id >= 0 && r.id[e] == id;
+                for (int e = f + 1; e < kTopEach; ++e) twice |= r.id[e] == other;
             }
-    }
+        }
     if (__any_sync(0xffffffffu, twice)) {
-        float own[kTopEach] = {};
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e) r.own[e] = 0.f;
+#pragma unroll 1
         for (int l = 0; l < 32; ++l)
 #pragma unroll
             for (int f = 0; f < kTopEach; ++f) {
@@ -119,42 +125,43 @@ __device__ __forceinline__ Entries entries_of(const DistillArgs &a, const RawEnt
                 const float p = __shfl_sync(0xffffffffu, r.p[f], l);
 #pragma unroll
                 for (int e = 0; e < kTopEach; ++e)
-                    if (r.id[e] == id) own[e] += p;
+                    if (r.id[e] == id) r.own[e] += p;
             }
-#pragma unroll
-        for (int e = 0; e < kTopEach; ++e) r.own[e] = own[e];
     }
     return r;
 }
 
-// A row's loss terms, and what its gradient needs; g: of the entries' elements.
+// What all but the entries' elements of a row's gradient are made of.
+__device__ __forceinline__ float per_e_of(const DistillArgs &a, float mass, float weight, float sum) {
+    return mass == 0.f ? 0.f : weight * a.scale * mass / sum;  // no entry: nothing to learn, whatever the logits
+}
+
+// A row's loss terms; g: the gradient of the entries' elements.
 struct DistillOut {
     float kl, cross, held;  // held: the student's mass on the entries
-    float per_e;
     float g[kTopEach];
 };
 __device__ __forceinline__ DistillOut distill_out(const DistillArgs &a, const Entries &en, const float (&x)[kTopEach], float weight,
-                                                  const Stats &s, float k) {
+                                                  float top, float sum, float k) {
     DistillOut o;
-    const float log_sum = logf(s.sum), unit = weight * a.scale, inv = 1.f / s.sum;
+    const float log_sum = logf(sum), unit = weight * a.scale, inv = 1.f / sum;
     float kl = 0.f, cross = 0.f, held = 0.f;
 #pragma unroll
-    for (int e = 0; e < kTopEach; ++e) {
-        const float d = x[e] - s.top, logq = fmaf(a.scale, d, -log_sum);
-        const float q = exp2_fast(k * d) * inv;
-        o.g[e] = unit * fmaf(en.mass, q, -en.own[e]);
-        if (en.id[e] >= 0) held += q;
-        if (en.p[e] != 0.f) {  // no probability, no loss, also where the student has none either
-            kl = fmaf(en.p[e], en.logp[e] - logq, kl);
-            cross = fmaf(-en.p[e], logq, cross);
+    for (int e = 0; e < kTopEach; ++e)
+        if (in_use(a, e)) {
+            const float d = x[e] - top, logq = fmaf(a.scale, d, -log_sum);
+            const float q = exp2_fast(k * d) * inv;
+            o.g[e] = en.bad ? CUDART_NAN_F : unit * fmaf(en.mass, q, -en.own[e]);
+            if (en.id[e] >= 0) held += q;
+            if (en.p[e] != 0.f) {  // no probability, no loss, also where the student has none either
+                kl = fmaf(en.p[e], en.logp[e] - logq, kl);
+                cross = fmaf(-en.p[e], logq, cross);
+            }
         }
-    }
     o.kl = warp_sum(kl);
     o.cross = warp_sum(cross);
     o.held = warp_sum(held);
     if (en.bad) o.kl = o.cross = o.held = CUDART_NAN_F;
-    o.per_e = unit * en.mass * inv;
-    if (en.mass == 0.f) o.per_e = 0.f;  // no entry: nothing to learn, whatever the logits
     return o;
 }
 
@@ -175,7 +182,7 @@ __device__ __forceinline__ void write_patches(const DistillArgs &a, const Patche
     O *y = static_cast<O *>(a.dlogits) + p.row * a.ld_dlogits;
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e)
-        if (p.id[e] >= 0) y[p.id[e]] = narrow<O>(p.g[e]);
+        if (in_use(a, e) && p.id[e] >= 0) y[p.id[e]] = narrow<O>(p.g[e]);
 }
 
 // In the ring's warp of its own: joins, loss terms, verdicts.  The working warps have written row n-2 when they
@@ -187,15 +194,18 @@ __device__ __forceinline__ void distill_verdicts(const DistillArgs &a, float k, 
     const int cluster = 1 << log_cluster;
     uint32_t n = 0;  // live rows
     Patches waiting[2];
-    float next_weight = 0.f, next_lse = 0.f;
+    // a row's weight is loaded two rows ahead, its entries one: loads that nobody waits for
+    float after_weight = 0.f, next_weight = 0.f, next_lse = 0.f;
     RawEntries next = {};
     const auto look_ahead = [&](int64_t row) {
-        next_weight = row < a.rows ? a.weights[row] : 0.f;
+        next_weight = after_weight;
+        after_weight = row + step < a.rows ? a.weights[row + step] : 0.f;
         if (next_weight != 0.f) {
             next = load_entries(a, row, lane);
             if (a.teacher_lse) next_lse = a.teacher_lse[row];
         }
     };
+    after_weight = first < a.rows ? a.weights[first] : 0.f;
     look_ahead(first);
     for (int64_t row = first; row < a.rows; row += step) {
         const float weight = next_weight, lse = next_lse;
@@ -222,13 +232,13 @@ __device__ __forceinline__ void distill_verdicts(const DistillArgs &a, float k, 
             const int j = raw.id[e];
             mine[e] = j >= 0 && ((j >= begin && j < end) || (rank == 0 && (j < shape.head || j >= body_end)));
             x_at[e] = 0.f;
-            if (j >= 0 && (rank == 0 || mine[e])) x_at[e] = widen(x[j]);
+            if (in_use(a, e) && j >= 0 && (rank == 0 || mine[e])) x_at[e] = widen(x[j]);
         }
         const bool has_extra = rank == 0 && lane < shape.head + shape.tail;
         const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
         const float x_extra = has_extra ? widen(x[extra]) : -CUDART_INF_F;
         look_ahead(row + step);
-        const Entries en = entries_of(a, raw, lse, lane);
+        const Entries en = entries_of(a, raw, lse);
         Running<false> run;
         run.add_one(x_extra, k);
         float seen = x_at[0];  // of all that this warp has read
@@ -249,21 +259,22 @@ __device__ __forceinline__ void distill_verdicts(const DistillArgs &a, float k, 
             if (lane < cluster) q = sh.peer[b][lane];
             s = warp_join<false>({q.x, q.y, 0.f}, k);
         }
-        const DistillOut o = distill_out(a, en, x_at, weight, s, k);
+        const float per_e = per_e_of(a, en.mass, weight, s.sum);
         __syncwarp();  // all lanes have read their logits, which the verdict's readers may overwrite
         if (lane == 0) {
-            sh.verdict[b] = {s.top, 0.f, o.per_e, 0.f, -1, -1};
+            sh.verdict[b] = {s.top, 0.f, per_e, seen, -1, -1};
             barrier_arrive(shared_addr(&sh.ready[b]));
-            if (rank == 0) {
-                add_terms(acc, a, weight, en, o);
-                if (a.loss) a.loss[row] = o.kl;
-                if (en.bad) record_bad_target(a.status, row);
-            }
+        }
+        const DistillOut o = distill_out(a, en, x_at, weight, s.top, s.sum, k);  // while the others write
+        if (lane == 0 && rank == 0) {
+            add_terms(acc, a, weight, en, o);
+            if (a.loss) a.loss[row] = o.kl;
+            if (en.bad) record_bad_target(a.status, row);
         }
         if (a.dlogits) {
             if (has_extra) {
                 O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
-                y[extra] = narrow<O>(o.per_e == 0.f ? 0.f : o.per_e * exp2_fast(k * (x_extra - s.top)));
+                y[extra] = narrow<O>(per_e == 0.f ? 0.f : per_e * exp2_fast(k * (x_extra - s.top)));
             }
             __syncwarp();  // (an extra may be an entry's)
             if (n >= 2) write_patches<O>(a, waiting[0]);
@@ -272,7 +283,7 @@ __device__ __forceinline__ void distill_verdicts(const DistillArgs &a, float k, 
 #pragma unroll
             for (int e = 0; e < kTopEach; ++e) {
                 waiting[1].id[e] = mine[e] ? raw.id[e] : -1;
-                waiting[1].g[e] = en.bad ? CUDART_NAN_F : o.g[e];
+                waiting[1].g[e] = o.g[e];
             }
         }
         ++n;

@@ -366,7 +366,7 @@ distill_rows_kernel(const DistillArgs a, float k) {
         float x_at[kTopEach];
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e) x_at[e] = raw.id[e] >= 0 ? widen(x[raw.id[e]]) : 0.f;
-        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
+        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f);
         Running<false> run;
 #pragma unroll
         for (int i = 0; i < kRowUnits; ++i) {
@@ -377,7 +377,8 @@ distill_rows_kernel(const DistillArgs a, float k) {
         }
         if (has_extra) run.add_one(x_extra, k);
         const Stats s = warp_join<false>(run.stats(), k);
-        const DistillOut o = distill_out(a, en, x_at, weight, s, k);
+        const DistillOut o = distill_out(a, en, x_at, weight, s.top, s.sum, k);
+        const float per_e = per_e_of(a, en.mass, weight, s.sum);
         __syncwarp();  // the gradient may replace the logits: no lane writes before all have read
         if (lane == 0) {
             add_terms(acc, a, weight, en, o);
@@ -385,10 +386,10 @@ distill_rows_kernel(const DistillArgs a, float k) {
             if (a.loss) a.loss[row] = o.kl;
         }
         if (!a.dlogits) continue;
-        if (o.per_e == 0.f) {
+        if (per_e == 0.f) {
             fill_zeros(y, a.vocab, lane, 32);
         } else {
-            const RowWriter<T, O> out(y, shape, s.top, 0.f, o.per_e, k);
+            const RowWriter<T, O> out(y, shape, s.top, 0.f, per_e, k);
             O *p = y + shape.head + lane * kUnit<T>;
             if (out.shift == 0) {
 #pragma unroll
@@ -408,7 +409,7 @@ distill_rows_kernel(const DistillArgs a, float k) {
         __syncwarp();  // the entries' elements are written over
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e)
-            if (raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(en.bad ? CUDART_NAN_F : o.g[e]);
+            if (in_use(a, e) && raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(o.g[e]);
     }
     finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
 }
@@ -577,18 +578,26 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             }
             if (out.shift == 0) {
                 int at = 0;
+                // Stages are given back behind the stores that use what was read from them: a load that has been issued
+                // need not have read yet when a lane's arrival is seen, and the stage is then filled anew under it.
                 for (; count - at >= 2 * kStageUnits; at += 2 * kStageUnits, p += 2 * kStageUnits * kUnit<T>) {
                     uint4 u[2 * kEach];
+                    Cursor<kStages> second = at_stage;
+                    second.advance();
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]) + t;
+                        const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[j ? second.slot : at_stage.slot]) + t;
 #pragma unroll
                         for (int i = 0; i < kEach; ++i) u[j * kEach + i] = units[i * kRingWork];
-                        release();
-                        at_stage.advance();
                     }
 #pragma unroll
-                    for (int i = 0; i < 2 * kEach; ++i) out.put(u[i], p + i * kRingWork * kUnit<T>);
+                    for (int i = 0; i < 2 * kEach; ++i) {
+                        out.put(u[i], p + i * kRingWork * kUnit<T>);
+                        if (i + 1 == kEach || i + 1 == 2 * kEach) {
+                            release();
+                            at_stage.advance();
+                        }
+                    }
                 }
                 for (; at < count; at += kStageUnits, at_stage.advance(), p += kStageUnits * kUnit<T>) {
                     const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]) + t;
@@ -784,7 +793,7 @@ distill_long_kernel(const DistillArgs a, float k) {
             continue;
         }
         const RawEntries raw = load_entries(a, row, lane);
-        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
+        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f);
         float x_at[kTopEach];
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e) x_at[e] = raw.id[e] >= 0 ? widen(x[raw.id[e]]) : 0.f;
@@ -796,7 +805,8 @@ distill_long_kernel(const DistillArgs a, float k) {
         }
         if (has_extra) run.add_one(x_extra, k);
         const Stats s = group_join<kWarps, false>(run.stats(), k, shared, 0);
-        const DistillOut o = distill_out(a, en, x_at, weight, s, k);
+        const DistillOut o = distill_out(a, en, x_at, weight, s.top, s.sum, k);
+        const float per_e = per_e_of(a, en.mass, weight, s.sum);
         if (t == 0) {
             add_terms(acc, a, weight, en, o);
             if (en.bad) record_bad_target(a.status, row);
@@ -804,10 +814,10 @@ distill_long_kernel(const DistillArgs a, float k) {
         }
         group_sync<kWarps>(0);  // all warps have read their logits, and the slots are used again
         if (!a.dlogits) continue;
-        if (o.per_e == 0.f) {
+        if (per_e == 0.f) {
             fill_zeros(y, a.vocab, t, kThreads);
         } else {
-            const RowWriter<T, O> out(y, shape, s.top, 0.f, o.per_e, k);
+            const RowWriter<T, O> out(y, shape, s.top, 0.f, per_e, k);
             O *p = y + shape.head;
             if (out.shift == 0) {
                 for (int i = t; i < shape.units; i += kThreads) out.put(ld_unit(body + i), p + (int64_t)i * kUnit<T>);
@@ -822,7 +832,7 @@ distill_long_kernel(const DistillArgs a, float k) {
         if (t < 32) {
 #pragma unroll
             for (int e = 0; e < kTopEach; ++e)
-                if (raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(en.bad ? CUDART_NAN_F : o.g[e]);
+                if (in_use(a, e) && raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(o.g[e]);
         }
     }
     finish_stats<kThreads, kThreads>(a, acc, sums, &last, t, blockIdx.x, gridDim.x);
