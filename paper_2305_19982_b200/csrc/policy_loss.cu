@@ -357,16 +357,22 @@ distill_rows_kernel(const DistillArgs a, float k) {
         const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
         const bool has_extra = lane < shape.head + shape.tail;
         const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
-        const RawEntries raw = load_entries(a, row, lane);
+        RawEntries raw = {};
+        load_entries(a, row, lane, raw);
         uint4 u[kRowUnits];
 #pragma unroll
         for (int i = 0; i < kRowUnits; ++i)
             if (lane + 32 * i < shape.units) u[i] = ld_unit(body + lane + 32 * i);
         const float x_extra = has_extra ? widen(x[extra]) : 0.f;
+        Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
         float x_at[kTopEach];
+        bool mine[kTopEach];
 #pragma unroll
-        for (int e = 0; e < kTopEach; ++e) x_at[e] = raw.id[e] >= 0 ? widen(x[raw.id[e]]) : 0.f;
-        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f);
+        for (int e = 0; e < kTopEach; ++e) {
+            mine[e] = en.id[e] >= 0;
+            x_at[e] = mine[e] ? widen(x[en.id[e]]) : 0.f;
+        }
+        if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
         Running<false> run;
 #pragma unroll
         for (int i = 0; i < kRowUnits; ++i) {
@@ -377,14 +383,15 @@ distill_rows_kernel(const DistillArgs a, float k) {
         }
         if (has_extra) run.add_one(x_extra, k);
         const Stats s = warp_join<false>(run.stats(), k);
-        const DistillOut o = distill_out(a, en, x_at, weight, s.top, s.sum, k);
+        const DistillOut o = distill_out(a, en, x_at, mine, weight, s.top, s.sum, k);
         const float per_e = per_e_of(a, en.mass, weight, s.sum);
         __syncwarp();  // the gradient may replace the logits: no lane writes before all have read
-        if (lane == 0) {
-            add_terms(acc, a, weight, en, o);
-            if (en.bad) record_bad_target(a.status, row);
-            if (a.loss) a.loss[row] = o.kl;
+        add_terms(acc, weight, en, o, lane == 0);
+        if (a.loss) {
+            const float kl = warp_sum(o.kl);
+            if (lane == 0) a.loss[row] = kl;
         }
+        if (lane == 0 && en.bad) record_bad_target(a.status, row);
         if (!a.dlogits) continue;
         if (per_e == 0.f) {
             fill_zeros(y, a.vocab, lane, 32);
@@ -409,8 +416,9 @@ distill_rows_kernel(const DistillArgs a, float k) {
         __syncwarp();  // the entries' elements are written over
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e)
-            if (in_use(a, e) && raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(o.g[e]);
+            if (in_use(a, e) && en.id[e] >= 0) y[en.id[e]] = narrow<O>(o.g[e]);
     }
+    sum_lanes(acc);
     finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
 }
 
@@ -545,7 +553,8 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
         }
         if (lane == 0) report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
         __syncwarp();
-        if (rank == 0) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, (unsigned)first, (unsigned)step);
+        if (kDistill<Args>) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, blockIdx.x, gridDim.x);  // every CTA has some
+        else if (rank == 0) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, (unsigned)first, (unsigned)step);
     } else {
         Cursor<kStages> c;
         uint32_t n = 0;              // live rows whose statistics have been taken
@@ -792,11 +801,17 @@ distill_long_kernel(const DistillArgs a, float k) {
             if (a.dlogits) fill_zeros(y, a.vocab, t, kThreads);
             continue;
         }
-        const RawEntries raw = load_entries(a, row, lane);
-        const Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f);
+        RawEntries raw = {};
+        load_entries(a, row, lane, raw);
+        Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
         float x_at[kTopEach];
+        bool mine[kTopEach];
 #pragma unroll
-        for (int e = 0; e < kTopEach; ++e) x_at[e] = raw.id[e] >= 0 ? widen(x[raw.id[e]]) : 0.f;
+        for (int e = 0; e < kTopEach; ++e) {
+            mine[e] = en.id[e] >= 0;
+            x_at[e] = mine[e] ? widen(x[en.id[e]]) : 0.f;
+        }
+        if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
         const float x_extra = has_extra ? widen(x[extra]) : 0.f;
         Running<false> run;
         for (int i = t; i < shape.units; i += kThreads) {
@@ -805,12 +820,15 @@ distill_long_kernel(const DistillArgs a, float k) {
         }
         if (has_extra) run.add_one(x_extra, k);
         const Stats s = group_join<kWarps, false>(run.stats(), k, shared, 0);
-        const DistillOut o = distill_out(a, en, x_at, weight, s.top, s.sum, k);
+        const DistillOut o = distill_out(a, en, x_at, mine, weight, s.top, s.sum, k);
         const float per_e = per_e_of(a, en.mass, weight, s.sum);
-        if (t == 0) {
-            add_terms(acc, a, weight, en, o);
-            if (en.bad) record_bad_target(a.status, row);
-            if (a.loss) a.loss[row] = o.kl;
+        if (t < 32) {
+            add_terms(acc, weight, en, o, t == 0);
+            const float kl = warp_sum(o.kl);
+            if (t == 0) {
+                if (en.bad) record_bad_target(a.status, row);
+                if (a.loss) a.loss[row] = kl;
+            }
         }
         group_sync<kWarps>(0);  // all warps have read their logits, and the slots are used again
         if (!a.dlogits) continue;
@@ -832,9 +850,10 @@ distill_long_kernel(const DistillArgs a, float k) {
         if (t < 32) {
 #pragma unroll
             for (int e = 0; e < kTopEach; ++e)
-                if (in_use(a, e) && raw.id[e] >= 0) y[raw.id[e]] = narrow<O>(o.g[e]);
+                if (in_use(a, e) && en.id[e] >= 0) y[en.id[e]] = narrow<O>(o.g[e]);
         }
     }
+    sum_lanes(acc);  // (the first warp has them)
     finish_stats<kThreads, kThreads>(a, acc, sums, &last, t, blockIdx.x, gridDim.x);
 }
 
