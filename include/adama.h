@@ -478,7 +478,9 @@ ADAMA_API adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args
  *   top         : 1 to ADAMA_DISTILL_TOP
  *   teacher_lse : rows fp32 (of logit_scale times ALL the teacher's logits), or NULL
  *   weights     : rows fp32;   loss : rows fp32 (kl of each row), or NULL;   stats : 4 fp32
- *   workspace   : ADAMA_WORKSPACE_BYTES
+ *   workspace   : ADAMA_WORKSPACE_BYTES, as for adama_policy_loss
+ *   scratch     : adama_distill_scratch(ctx, rows, top) bytes of device memory, 16-byte aligned, that no other call
+ *                 uses at the same time; its contents do not matter
  * logit_scale as in adama_token_logprobs.  Deterministic.  A row with an index >= vocab becomes NaN and is reported
  * as a target is.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED (top too large), CUDA. */
 #define ADAMA_DISTILL_TOP 128
@@ -496,9 +498,12 @@ typedef struct adama_distill_args {
     float *loss;
     float *stats;
     void *workspace;
+    void *scratch;
 } adama_distill_args;
 ADAMA_API adama_status adama_distill_loss(adama_ctx *ctx, const adama_distill_args *args,
                                           void *cuda_stream);
+/* Bytes of the scratch of such a call; 0 for arguments that it would refuse. */
+ADAMA_API size_t adama_distill_scratch(const adama_ctx *ctx, int64_t rows, int64_t top);
 
 /* The id of the capture that `cuda_stream` is taking part in, 0 if it is not being captured: what a
  * caller who keeps a workspace per stream tells graphs apart by.  Ids are unique in the process. */

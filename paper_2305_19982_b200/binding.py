@@ -29,7 +29,7 @@ EXPORTED_SYMBOLS = [
     "adama_fold_apply_multi", "adama_fold_apply8_multi", "adama_state8_pack_multi", "adama_state8_unpack_multi",
     "adama_grad_norm_multi", "adama_token_logprobs", "adama_policy_loss", "adama_stream_capture_id",
     "adama_layer_norm", "adama_layer_norm_backward", "adama_layer_norm_workspace",
-    "adama_embedding", "adama_embedding_grad", "adama_embedding_workspace", "adama_distill_loss",
+    "adama_embedding", "adama_embedding_grad", "adama_embedding_workspace", "adama_distill_loss", "adama_distill_scratch",
 ]
 
 
@@ -75,7 +75,7 @@ class _State8(ctypes.Structure):
 _POLICY_ARGS = struct.Struct("@PPii4qPPPPP4dPPP")
 
 
-_DISTILL_ARGS = struct.Struct("@PPiiii6qPPPPdPPP")   # adama_distill_args
+_DISTILL_ARGS = struct.Struct("@PPiiii6qPPPPdPPPP")   # adama_distill_args
 # adama_layer_norm_args, adama_layer_norm_backward_args, adama_embedding_args, adama_embedding_grad_args
 _LAYER_NORM_ARGS = struct.Struct("@PPii4qPPdPP")
 _LAYER_NORM_BACKWARD_ARGS = struct.Struct("@PPPii5q10P")
@@ -154,9 +154,9 @@ def load_library() -> ctypes.CDLL:
     L.adama_policy_loss.argtypes = [vp, ctypes.c_char_p, vp]
     for name in ("distill_loss", "layer_norm", "layer_norm_backward", "embedding", "embedding_grad"):
         getattr(L, "adama_" + name).argtypes = [vp, ctypes.c_char_p, vp]
-    for name in ("layer_norm", "embedding"):
-        getattr(L, f"adama_{name}_workspace").argtypes = [vp, i64, i64]
-        getattr(L, f"adama_{name}_workspace").restype = sz
+    for name in ("layer_norm_workspace", "embedding_workspace", "distill_scratch"):
+        getattr(L, "adama_" + name).argtypes = [vp, i64, i64]
+        getattr(L, "adama_" + name).restype = sz
     L.adama_stream_capture_id.argtypes = [vp]
     L.adama_stream_capture_id.restype = ctypes.c_uint64
     L.adama_get_step.argtypes = [vp]
@@ -778,19 +778,20 @@ class AdamA:
         args = _DISTILL_ARGS.pack(
             ptr, dptr, dt, ddt, tdt, top, rows, vocab, ld, dld, tld, max(top, teacher_ids.stride(0)) if rows < 2 else teacher_ids.stride(0),
             tptr, _dev_ptr(teacher_ids, torch.int64, "teacher_ids"), row(teacher_lse, rows, "teacher_lse"), row(weights, rows, "weights"),
-            logit_scale, row(loss, rows, "loss"), _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream))
+            logit_scale, row(loss, rows, "loss"), _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream),
+            self._scratch(stream, "distill_scratch", rows, top))
         self._check(self._L.adama_distill_loss(self._h, args, stream))
 
     # -- norms and embeddings ----------------------------------------------------------------
     def _scratch(self, stream: int, of: str, rows: int, dim: int) -> int:
-        """Workspace of a call over rows x dim, whose size adama_<of>_workspace gives: one buffer for each stream,
+        """Workspace of a call over rows x dim, whose size adama_<of> gives: one buffer for each stream,
         made anew where a call needs more; while the stream is being captured into a graph, one of that graph's
         own from its memory.  What it holds between calls does not matter."""
         need = self._scratch_bytes.get((of, rows, dim))
         if need is None:
             if len(self._scratch_bytes) >= 1024:
                 self._scratch_bytes.clear()
-            need = self._scratch_bytes[of, rows, dim] = max(16, getattr(self._L, f"adama_{of}_workspace")(self._h, rows, dim))
+            need = self._scratch_bytes[of, rows, dim] = max(16, getattr(self._L, "adama_" + of)(self._h, rows, dim))
         if stream:  # the legacy default stream cannot be captured
             capture = self._L.adama_stream_capture_id(stream)
             if capture:
@@ -844,7 +845,7 @@ class AdamA:
         args = _LAYER_NORM_BACKWARD_ARGS.pack(
             dyptr, ptr, dxptr, dydt, dt, rows, dim, dyld, ld, dxld, vector(weight, dim, "weight"), vector(mean, rows, "mean"),
             vector(rstd, rows, "rstd"), *[vector(t, dim, n) for t, n in zip(params, names)],
-            self._scratch(stream, "layer_norm", rows, dim))
+            self._scratch(stream, "layer_norm_workspace", rows, dim))
         self._check(self._L.adama_layer_norm_backward(self._h, args, stream))
 
     def layer_norm_backward(self, dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -888,7 +889,7 @@ class AdamA:
         args = _EMBEDDING_GRAD_ARGS.pack(
             self._per_row(ids, tokens, "ids", torch.int64), ptr, dt, tdt, tokens, vocab, dim, ld, tld, scale,
             tptr if v is None else 0, tptr if v is not None else 0, vptr, int(accumulate),
-            self._scratch(stream, "embedding", tokens, dim))
+            self._scratch(stream, "embedding_workspace", tokens, dim))
         self._check(self._L.adama_embedding_grad(self._h, args, stream))
 
     def embedding_grad(self, ids: torch.Tensor, dy: torch.Tensor, grad: torch.Tensor, scale: float = 1.0,

@@ -819,7 +819,7 @@ adama_status adama_distill_loss(adama_ctx *ctx, const adama_distill_args *p, voi
     if ((p->dlogits_dtype != ADAMA_F32 && p->dlogits_dtype != ADAMA_BF16) ||
         (p->teacher_dtype != ADAMA_F32 && p->teacher_dtype != ADAMA_BF16))
         return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: unknown dtype");
-    if (!p->stats || !p->workspace || (p->rows > 0 && (!p->teacher_logits || !p->weights)))
+    if (!p->stats || !p->workspace || (p->rows > 0 && (!p->teacher_logits || !p->weights || !p->scratch)))
         return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: null pointer");
     if (p->top < 1) return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: a row needs an entry");
     if (p->top > ADAMA_DISTILL_TOP) return fail(ctx, ADAMA_ERR_UNSUPPORTED, "distill_loss: more than 128 entries in a row");
@@ -830,10 +830,10 @@ adama_status adama_distill_loss(adama_ctx *ctx, const adama_distill_args *p, voi
         return fail(ctx, ADAMA_ERR_INVALID_ARG, "distill_loss: in place needs one dtype and one pitch");
     if (!aligned_to(p->dlogits, dtype_size(p->dlogits_dtype)) || !aligned_to(p->teacher_logits, dtype_size(p->teacher_dtype)) ||
         !aligned_to(p->teacher_lse, 4) || !aligned_to(p->weights, 4) || !aligned_to(p->loss, 4) || !aligned_to(p->stats, 4) ||
-        !aligned_to(p->workspace, 16))
+        !aligned_to(p->workspace, 16) || !aligned_to(p->scratch, 16))
         return fail(ctx, ADAMA_ERR_MISALIGNED, "distill_loss: pointer not aligned");
     DeviceGuard guard(ctx->cfg.device);
-    adama::DistillArgs a;
+    adama::DistillArgs a = {};
     a.logits = p->logits;
     a.dlogits = p->dlogits;
     a.logits_dtype = p->logits_dtype;
@@ -856,10 +856,15 @@ adama_status adama_distill_loss(adama_ctx *ctx, const adama_distill_args *p, voi
     a.stats = p->stats;
     a.workspace = p->workspace;
     a.status = ctx->status_dev;
-    cudaError_t e = adama::launch_distill_loss(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream));
-    if (e != cudaSuccess) return cuda_fail(ctx, "distill_loss launch", e);
-    ctx->launches += 1;
-    return ADAMA_OK;
+    int launches = 0;
+    cudaError_t e = adama::launch_distill_loss(a, p->scratch, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream), &launches);
+    ctx->launches += launches;
+    return e == cudaSuccess ? ADAMA_OK : cuda_fail(ctx, "distill_loss launch", e);
+}
+
+size_t adama_distill_scratch(const adama_ctx *ctx, int64_t rows, int64_t top) {
+    if (!ctx || rows < 0 || rows > INT32_MAX || top < 1 || top > ADAMA_DISTILL_TOP) return 0;
+    return adama::distill_scratch_bytes(rows, (int)top);
 }
 
 // ---- norms and embeddings ---------------------------------------------------------------------

@@ -169,8 +169,12 @@ struct DistillArgs {
     float *stats;
     void *workspace;
     unsigned *status;
+    // parts of the scratch, set by the launch: {x, p, own, index} of each entry, {mass, sum p log p} and {top, sum} of each row
+    float4 *entries;
+    float2 *masses, *row_stats;
 };
-cudaError_t launch_distill_loss(const DistillArgs &a, int sm_count, cudaStream_t stream);
+size_t distill_scratch_bytes(int64_t rows, int top);
+cudaError_t launch_distill_loss(DistillArgs a, void *scratch, int sm_count, cudaStream_t stream, int *launches);
 
 // layer norm (layer_norm.cu)
 struct NormArgs {

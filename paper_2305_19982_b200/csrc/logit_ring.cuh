@@ -39,7 +39,7 @@ struct RingShared {
     alignas(16) float4 peer[2][kMaxCluster];  // {top, sum, x_target} of the cluster's CTAs
     Verdict verdict[2];
     float2 slots[2][Cut::kWarps];             // {top, sum} of the warps
-    unsigned long long full[Cut::kStages], empty[Cut::kStages], joined[2], peered[2], ready[2], done;
+    unsigned long long full[Cut::kStages], empty[Cut::kStages], joined[2], peered[2], ready[2];
     double sums[1][4];
     int last, give_up;
 };

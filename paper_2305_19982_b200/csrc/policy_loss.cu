@@ -166,6 +166,15 @@ struct DistillMask {
 };
 __device__ __forceinline__ DistillMask row_mask(const DistillArgs &a, int64_t row) { return {a.weights[row]}; }
 
+// The same of a distilled row, as the kernels for any loss see it: no target, but the teacher's mass.
+struct DistillIn {
+    int64_t target = -1;
+    float weight = 0.f, mass = 0.f;
+
+    __device__ __forceinline__ bool live() const { return weight != 0.f; }
+};
+__device__ __forceinline__ DistillIn row_in(const DistillArgs &a, int64_t row) { return {-1, a.weights[row], a.masses[row].x}; }
+
 template <typename Args>
 constexpr bool kDistill = std::is_same<Args, DistillArgs>::value;
 
@@ -215,6 +224,10 @@ __device__ __forceinline__ RowOut row_out(const PolicyArgs &a, const RowIn &in, 
     o.unit = in.weight * slope * a.scale;
     o.per_e = __fdividef(-o.unit, s.sum);  // 2 ulp; sum >= 1 or NaN
     return o;
+}
+
+__device__ __forceinline__ RowOut row_out(const DistillArgs &a, const DistillIn &in, const Stats &s, float) {
+    return {0.f, 0.f, 0.f, 0.f, 0.f, per_e_of(a, in.mass, in.weight, s.sum)};
 }
 
 __device__ __forceinline__ void add_terms(Sums &sums, const PolicyArgs &a, const RowIn &in, const RowOut &o) {
@@ -366,12 +379,8 @@ distill_rows_kernel(const DistillArgs a, float k) {
         const float x_extra = has_extra ? widen(x[extra]) : 0.f;
         Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
         float x_at[kTopEach];
-        bool mine[kTopEach];
 #pragma unroll
-        for (int e = 0; e < kTopEach; ++e) {
-            mine[e] = en.id[e] >= 0;
-            x_at[e] = mine[e] ? widen(x[en.id[e]]) : 0.f;
-        }
+        for (int e = 0; e < kTopEach; ++e) x_at[e] = en.id[e] >= 0 ? widen(x[en.id[e]]) : 0.f;
         if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
         Running<false> run;
 #pragma unroll
@@ -383,12 +392,22 @@ distill_rows_kernel(const DistillArgs a, float k) {
         }
         if (has_extra) run.add_one(x_extra, k);
         const Stats s = warp_join<false>(run.stats(), k);
-        const DistillOut o = distill_out(a, en, x_at, mine, weight, s.top, s.sum, k);
-        const float per_e = per_e_of(a, en.mass, weight, s.sum);
+        const float per_e = per_e_of(a, en.mass, weight, s.sum), log_sum = logf(s.sum), inv = 1.f / s.sum;
+        float kl = en.inner, cross = 0.f, held = 0.f, g[kTopEach];
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e)
+            if (in_use(a, e) && en.id[e] >= 0) {
+                const EntryTerms o = entry_terms(x_at[e], en.p[e], en.own[e], en.mass, a.scale, weight * a.scale, s.top, log_sum, inv, k);
+                cross += o.cross;
+                held += o.held;
+                g[e] = o.g;
+            }
+        kl += cross;
+        if (en.bad) kl = cross = held = CUDART_NAN_F;
         __syncwarp();  // the gradient may replace the logits: no lane writes before all have read
-        add_terms(acc, weight, en, o, lane == 0);
+        acc.add(weight, kl, cross, held, lane == 0 ? en.mass : 0.f);
         if (a.loss) {
-            const float kl = warp_sum(o.kl);
+            kl = warp_sum(kl);
             if (lane == 0) a.loss[row] = kl;
         }
         if (lane == 0 && en.bad) record_bad_target(a.status, row);
@@ -416,7 +435,7 @@ distill_rows_kernel(const DistillArgs a, float k) {
         __syncwarp();  // the entries' elements are written over
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e)
-            if (in_use(a, e) && en.id[e] >= 0) y[en.id[e]] = narrow<O>(o.g[e]);
+            if (in_use(a, e) && en.id[e] >= 0) y[en.id[e]] = narrow<O>(g[e]);
     }
     sum_lanes(acc);
     finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
@@ -451,7 +470,6 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             barrier_init(shared_addr(&sh.peered[i]), 1);
             barrier_init(shared_addr(&sh.ready[i]), 1);
         }
-        if (kDistill<Args>) barrier_init(shared_addr(&sh.done), Cut::kWarps);
         sh.give_up = 0;
         barrier_init_fence();
     }
@@ -491,70 +509,74 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
         }
     } else if (warp == Cut::kScalarWarp) {
         Sums acc;
-        if constexpr (kDistill<Args>) {
-            distill_verdicts<T, O>(a, k, sh, lane, rank, log_cluster, first, step, acc);
-        } else {
-            uint32_t n = 0;  // live rows
-            RowIn next = {-1, 0.f, 0.f, 0.f, 0.f};
-            if (first < a.rows) next = row_in(a, first);
-            for (int64_t row = first; row < a.rows; row += step) {
-                const RowIn in = next;
-                if (row + step < a.rows) next = row_in(a, row + step);
-                if (!in.live()) {
+        uint32_t n = 0;  // live rows
+        decltype(row_in(a, first)) next = {};
+        if (first < a.rows) next = row_in(a, first);
+        for (int64_t row = first; row < a.rows; row += step) {
+            const auto in = next;
+            if (row + step < a.rows) next = row_in(a, row + step);
+            if (!in.live()) {
+                if constexpr (!kDistill<Args>) {
                     if (lane == 0 && rank == 0 && a.logp) a.logp[row] = 0.f;
-                    continue;
                 }
-                const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
-                const RowShape shape = row_shape(x, (int)a.vocab);
-                int from, count;
-                slice_of(shape.units, rank, log_cluster, from, count);
-                const int b = n & 1;
-                const uint32_t parity = n >> 1 & 1;
-                const bool inside = in.target < a.vocab, has_extra = rank == 0 && lane < shape.head + shape.tail;
-                const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
-                // the gradient may replace the logits: what is read here travels with this CTA's message,
-                // before which nobody writes
-                float x_target = rank == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
-                const float x_extra = has_extra ? widen(x[extra]) : -CUDART_INF_F;
-                Running<false> run;
-                run.add_one(x_extra, k);
-                barrier_wait(shared_addr(&sh.joined[b]), parity, &sh.give_up);
-                const Stats none = {-CUDART_INF_F, 0.f, 0.f};
-                Stats s = none;
-                if (lane < Cut::kWarps) s = {sh.slots[b][lane].x, sh.slots[b][lane].y, 0.f};
-                s = warp_join<false>(join2(s, run.stats(), k), k);
-                if (cluster > 1) {
-                    const uint32_t bar = shared_addr(&sh.peered[b]);
-                    if (lane == 0) barrier_expect(bar, 16u * cluster);
-                    if (lane < cluster) send16(shared_addr(&sh.peer[b][rank]), bar, lane, s.top, s.sum, x_target, 0.f);
-                    barrier_wait(bar, parity, &sh.give_up);
-                    float4 q = make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
-                    if (lane < cluster) q = sh.peer[b][lane];
-                    x_target = __shfl_sync(0xffffffffu, q.z, 0);
-                    s = warp_join<false>({q.x, q.y, 0.f}, k);
-                }
-                const RowOut o = row_out(a, in, s, x_target);
-                O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
-                const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
-                __syncwarp();  // all lanes have read x_target, which the verdict's readers may overwrite
-                if (lane == 0) {
-                    const int writer = inside ? out.writer_of(shape, in.target, from, count, kRingWork) : -1;
-                    sh.verdict[b] = {s.top, o.unit, o.per_e, x_target, in.target, writer};
-                    barrier_arrive(shared_addr(&sh.ready[b]));
-                    if (rank == 0) {
-                        add_terms(acc, a, in, o);
-                        if (a.logp) a.logp[row] = o.logp;
-                        if (!inside) record_bad_target(a.status, row);
-                    }
-                }
-                if (has_extra && a.dlogits) y[extra] = out.value(x_extra, extra == in.target);
-                ++n;
+                continue;
             }
+            const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+            const RowShape shape = row_shape(x, (int)a.vocab);
+            int from, count;
+            slice_of(shape.units, rank, log_cluster, from, count);
+            const int b = n & 1;
+            const uint32_t parity = n >> 1 & 1;
+            const bool inside = !kDistill<Args> && in.target < a.vocab, has_extra = rank == 0 && lane < shape.head + shape.tail;
+            const int extra = has_extra ? extra_index<T>(shape, lane) : 0;
+            // the gradient may replace the logits: what is read here travels with this CTA's message,
+            // before which nobody writes
+            float x_target = rank == 0 && inside ? widen(x[in.target]) : CUDART_NAN_F;
+            const float x_extra = has_extra ? widen(x[extra]) : -CUDART_INF_F;
+            Running<false> run;
+            run.add_one(x_extra, k);
+            barrier_wait(shared_addr(&sh.joined[b]), parity, &sh.give_up);
+            const Stats none = {-CUDART_INF_F, 0.f, 0.f};
+            Stats s = none;
+            if (lane < Cut::kWarps) s = {sh.slots[b][lane].x, sh.slots[b][lane].y, 0.f};
+            s = warp_join<false>(join2(s, run.stats(), k), k);
+            if (cluster > 1) {
+                const uint32_t bar = shared_addr(&sh.peered[b]);
+                if (lane == 0) barrier_expect(bar, 16u * cluster);
+                if (lane < cluster) send16(shared_addr(&sh.peer[b][rank]), bar, lane, s.top, s.sum, x_target, 0.f);
+                barrier_wait(bar, parity, &sh.give_up);
+                float4 q = make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+                if (lane < cluster) q = sh.peer[b][lane];
+                x_target = __shfl_sync(0xffffffffu, q.z, 0);
+                s = warp_join<false>({q.x, q.y, 0.f}, k);
+            }
+            const RowOut o = row_out(a, in, s, x_target);
+            O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+            const RowWriter<T, O> out(y, shape, s.top, o.unit, o.per_e, k);
+            __syncwarp();  // all lanes have read x_target, which the verdict's readers may overwrite
+            if (lane == 0) {
+                const int writer = inside ? out.writer_of(shape, in.target, from, count, kRingWork) : -1;
+                sh.verdict[b] = {s.top, o.unit, o.per_e, x_target, in.target, writer};
+                barrier_arrive(shared_addr(&sh.ready[b]));
+                if constexpr (kDistill<Args>) {
+                    if (rank == 0) a.row_stats[row] = make_float2(s.top, s.sum);
+                } else if (rank == 0) {
+                    add_terms(acc, a, in, o);
+                    if (a.logp) a.logp[row] = o.logp;
+                    if (!inside) record_bad_target(a.status, row);
+                }
+            }
+            if (has_extra && a.dlogits) {
+                if (kDistill<Args> && o.per_e == 0.f) y[extra] = narrow<O>(0.f);
+                else y[extra] = out.value(x_extra, extra == in.target);
+            }
+            ++n;
         }
         if (lane == 0) report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
         __syncwarp();
-        if (kDistill<Args>) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, blockIdx.x, gridDim.x);  // every CTA has some
-        else if (rank == 0) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, (unsigned)first, (unsigned)step);
+        if constexpr (!kDistill<Args>) {
+            if (rank == 0) finish_stats<32, 32>(a, acc, sh.sums, &sh.last, lane, (unsigned)first, (unsigned)step);
+        }
     } else {
         Cursor<kStages> c;
         uint32_t n = 0;              // live rows whose statistics have been taken
@@ -689,7 +711,6 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
                 }
             }
             const Stats s = warp_join<false>(run.stats(), k);
-            if (kDistill<Args>) __syncwarp();  // the arrival also says that row n-2 has been written
             if (lane == 0) {
                 sh.slots[n & 1][warp] = make_float2(s.top, s.sum);
                 barrier_arrive(shared_addr(&sh.joined[n & 1]));
@@ -703,10 +724,6 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             ++n;
         }
         if (due >= 0) write_due();
-        if (kDistill<Args>) {
-            __syncwarp();
-            if (lane == 0) barrier_arrive(shared_addr(&sh.done));
-        }
         if (lane == 0) report_expired_wait(&sh.give_up, a.status, kWaitPolicyRing);
     }
     if (cluster > 1) {
@@ -778,40 +795,24 @@ policy_loss_long_kernel(const PolicyArgs a, float k) {
     finish_stats<kThreads, kThreads>(a, acc, sums, &last, t, blockIdx.x, gridDim.x);
 }
 
-// The same for distillation: every warp makes the row's terms, the first one writes the entries' elements.
+// The same for distillation.
 template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads)
 distill_long_kernel(const DistillArgs a, float k) {
     __shared__ Stats shared[kWarps];
-    __shared__ double sums[kWarps][4];
-    __shared__ int last;
-    const int t = threadIdx.x, lane = t % 32;
-    Sums acc;
+    const int t = threadIdx.x;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const float weight = a.weights[row];
-        const bool live = weight != 0.f;
+        const DistillIn in = row_in(a, row);
         const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
         O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+        if (!in.live()) {
+            if (a.dlogits) fill_zeros(y, a.vocab, t, kThreads);
+            continue;
+        }
         const RowShape shape = row_shape(x, (int)a.vocab);
         const uint4 *body = reinterpret_cast<const uint4 *>(x + shape.head);
         const bool has_extra = t < shape.head + shape.tail;
         const int extra = has_extra ? extra_index<T>(shape, t) : 0;
-        if (!live) {
-            if (t == 0 && a.loss) a.loss[row] = 0.f;
-            if (a.dlogits) fill_zeros(y, a.vocab, t, kThreads);
-            continue;
-        }
-        RawEntries raw = {};
-        load_entries(a, row, lane, raw);
-        Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
-        float x_at[kTopEach];
-        bool mine[kTopEach];
-#pragma unroll
-        for (int e = 0; e < kTopEach; ++e) {
-            mine[e] = en.id[e] >= 0;
-            x_at[e] = mine[e] ? widen(x[en.id[e]]) : 0.f;
-        }
-        if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
         const float x_extra = has_extra ? widen(x[extra]) : 0.f;
         Running<false> run;
         for (int i = t; i < shape.units; i += kThreads) {
@@ -820,41 +821,97 @@ distill_long_kernel(const DistillArgs a, float k) {
         }
         if (has_extra) run.add_one(x_extra, k);
         const Stats s = group_join<kWarps, false>(run.stats(), k, shared, 0);
-        const DistillOut o = distill_out(a, en, x_at, mine, weight, s.top, s.sum, k);
-        const float per_e = per_e_of(a, en.mass, weight, s.sum);
-        if (t < 32) {
-            add_terms(acc, weight, en, o, t == 0);
-            const float kl = warp_sum(o.kl);
-            if (t == 0) {
-                if (en.bad) record_bad_target(a.status, row);
-                if (a.loss) a.loss[row] = kl;
-            }
-        }
-        group_sync<kWarps>(0);  // all warps have read their logits, and the slots are used again
+        const RowOut o = row_out(a, in, s, 0.f);
+        if (t == 0) a.row_stats[row] = make_float2(s.top, s.sum);
+        group_sync<kWarps>(0);  // the slots are used again
         if (!a.dlogits) continue;
-        if (per_e == 0.f) {
+        if (o.per_e == 0.f) {
             fill_zeros(y, a.vocab, t, kThreads);
-        } else {
-            const RowWriter<T, O> out(y, shape, s.top, 0.f, per_e, k);
-            O *p = y + shape.head;
-            if (out.shift == 0) {
-                for (int i = t; i < shape.units; i += kThreads) out.put(ld_unit(body + i), p + (int64_t)i * kUnit<T>);
-            } else {
-                for (int i = t; i < shape.units; i += kThreads)
-                    out.put_shifted(ld_unit(body + i), ld_unit(body + (i + 1 < shape.units ? i + 1 : i)),
-                                    p + (int64_t)i * kUnit<T>, i == 0, i + 1 == shape.units);
-            }
-            if (has_extra) y[extra] = out.value(x_extra, false);
+            continue;
         }
-        group_sync<kWarps>(0);  // the entries' elements are written over
-        if (t < 32) {
+        const RowWriter<T, O> out(y, shape, s.top, 0.f, o.per_e, k);
+        O *p = y + shape.head;
+        if (out.shift == 0) {
+            for (int i = t; i < shape.units; i += kThreads) out.put(ld_unit(body + i), p + (int64_t)i * kUnit<T>);
+        } else {
+            for (int i = t; i < shape.units; i += kThreads)
+                out.put_shifted(ld_unit(body + i), ld_unit(body + (i + 1 < shape.units ? i + 1 : i)),
+                                p + (int64_t)i * kUnit<T>, i == 0, i + 1 == shape.units);
+        }
+        if (has_extra) y[extra] = out.value(x_extra, false);
+    }
+}
+
+// ---- a distilled row's entries, before and after the row -----------------------------------------
+
+constexpr int kEntryWarps = 8;  // a row to each
+
+template <typename T>
+__global__ void __launch_bounds__(32 * kEntryWarps)
+distill_teacher_kernel(const DistillArgs a) {
+    const int lane = threadIdx.x % 32;
+    const int64_t row = (int64_t)blockIdx.x * kEntryWarps + threadIdx.x / 32;
+    if (row >= a.rows || a.weights[row] == 0.f) return;
+    RawEntries raw = {};
+    load_entries(a, row, lane, raw);
+    const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
+    float x_at[kTopEach];
 #pragma unroll
-            for (int e = 0; e < kTopEach; ++e)
-                if (in_use(a, e) && en.id[e] >= 0) y[en.id[e]] = narrow<O>(o.g[e]);
+    for (int e = 0; e < kTopEach; ++e) {
+        x_at[e] = 0.f;
+        if (in_use(a, e) && 32 * e + lane < a.top && raw.id[e] >= 0 && raw.id[e] < a.vocab) x_at[e] = widen(x[raw.id[e]]);
+    }
+    Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
+    if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
+#pragma unroll
+    for (int e = 0; e < kTopEach; ++e)
+        if (32 * e + lane < a.top) a.entries[row * a.top + 32 * e + lane] = make_float4(x_at[e], en.p[e], en.own[e], __int_as_float(en.id[e]));
+    const float inner = warp_sum(en.inner);
+    if (lane == 0) {
+        a.masses[row] = make_float2(en.mass, inner);
+        if (en.bad) record_bad_target(a.status, row);
+    }
+}
+
+template <typename O>
+__global__ void __launch_bounds__(32 * kEntryWarps)
+distill_entries_kernel(const DistillArgs a, float k) {
+    __shared__ double sums[kEntryWarps][4];
+    __shared__ int last;
+    const int lane = threadIdx.x % 32;
+    Sums acc;
+    for (int64_t row = (int64_t)blockIdx.x * kEntryWarps + threadIdx.x / 32; row < a.rows; row += (int64_t)gridDim.x * kEntryWarps) {
+        const float weight = a.weights[row];
+        if (weight == 0.f) {
+            if (lane == 0 && a.loss) a.loss[row] = 0.f;
+            continue;
+        }
+        const float2 of_row = a.row_stats[row], of_teacher = a.masses[row];
+        const float log_sum = logf(of_row.y), inv = 1.f / of_row.y, mass = of_teacher.x;
+        O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
+        float cross = 0.f, held = 0.f;
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e)
+            if (32 * e + lane < a.top) {
+                const float4 q = a.entries[row * a.top + 32 * e + lane];
+                const int id = __float_as_int(q.w);
+                if (id >= 0) {
+                    const EntryTerms o = entry_terms(q.x, q.y, q.z, mass, a.scale, weight * a.scale, of_row.x, log_sum, inv, k);
+                    cross += o.cross;
+                    held += o.held;
+                    if (a.dlogits) y[id] = narrow<O>(o.g);
+                }
+            }
+        if (mass != mass) cross = held = mass;
+        const float kl = cross + (lane == 0 ? of_teacher.y : 0.f);
+        acc.add(weight, kl, cross, held, lane == 0 ? mass : 0.f);
+        if (a.loss) {
+            const float all = warp_sum(kl);
+            if (lane == 0) a.loss[row] = all;
         }
     }
-    sum_lanes(acc);  // (the first warp has them)
-    finish_stats<kThreads, kThreads>(a, acc, sums, &last, t, blockIdx.x, gridDim.x);
+    sum_lanes(acc);
+    finish_stats<32 * kEntryWarps, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
 }
 
 // ---- launches --------------------------------------------------------------------------------------
@@ -1035,12 +1092,21 @@ cudaError_t loss(const Args &a, int sm_count, cudaStream_t stream) {
     return cudaGetLastError();
 }
 
-template <typename Args>
-cudaError_t any_loss(const Args &a, int sm_count, cudaStream_t stream) {
-    if (a.logits_dtype == ADAMA_F32)
-        return a.dlogits_dtype == ADAMA_F32 ? loss<float, float>(a, sm_count, stream) : loss<float, __nv_bfloat16>(a, sm_count, stream);
-    return a.dlogits_dtype == ADAMA_F32 ? loss<__nv_bfloat16, float>(a, sm_count, stream)
-                                        : loss<__nv_bfloat16, __nv_bfloat16>(a, sm_count, stream);
+// Distillation: rows that a warp holds in one kernel, others in three.
+template <typename T, typename O>
+cudaError_t distill(const DistillArgs &a, int sm_count, cudaStream_t stream, int *launches) {
+    const unsigned rows = (unsigned)((a.rows + kEntryWarps - 1) / kEntryWarps);
+    const bool whole = a.vocab / kUnit<T> <= 32 * kRowUnits;
+    if (!whole && a.rows > 0) distill_teacher_kernel<T><<<rows, 32 * kEntryWarps, 0, stream>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) e = loss<T, O>(a, sm_count, stream);
+    if (e != cudaSuccess) return e;
+    *launches += whole ? 1 : a.rows > 0 ? 3 : 2;
+    if (!whole) {
+        const unsigned grid = grid_of(rows, (int64_t)sm_count * 4);
+        distill_entries_kernel<O><<<grid, 32 * kEntryWarps, 0, stream>>>(a, (float)(a.scale_exact * kLog2e));
+    }
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -1048,7 +1114,25 @@ cudaError_t any_loss(const Args &a, int sm_count, cudaStream_t stream) {
 cudaError_t launch_token_logprobs(const LogprobArgs &a, int sm_count, cudaStream_t stream) {
     return a.dtype == ADAMA_F32 ? logprobs<float>(a, sm_count, stream) : logprobs<__nv_bfloat16>(a, sm_count, stream);
 }
-cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream) { return any_loss(a, sm_count, stream); }
-cudaError_t launch_distill_loss(const DistillArgs &a, int sm_count, cudaStream_t stream) { return any_loss(a, sm_count, stream); }
+
+cudaError_t launch_policy_loss(const PolicyArgs &a, int sm_count, cudaStream_t stream) {
+    if (a.logits_dtype == ADAMA_F32)
+        return a.dlogits_dtype == ADAMA_F32 ? loss<float, float>(a, sm_count, stream) : loss<float, __nv_bfloat16>(a, sm_count, stream);
+    return a.dlogits_dtype == ADAMA_F32 ? loss<__nv_bfloat16, float>(a, sm_count, stream)
+                                        : loss<__nv_bfloat16, __nv_bfloat16>(a, sm_count, stream);
+}
+
+size_t distill_scratch_bytes(int64_t rows, int top) { return (size_t)rows * (top * sizeof(float4) + 2 * sizeof(float2)); }
+
+cudaError_t launch_distill_loss(DistillArgs a, void *scratch, int sm_count, cudaStream_t stream, int *launches) {
+    a.entries = static_cast<float4 *>(scratch);
+    a.masses = reinterpret_cast<float2 *>(a.entries + a.rows * a.top);
+    a.row_stats = a.masses + a.rows;
+    if (a.logits_dtype == ADAMA_F32)
+        return a.dlogits_dtype == ADAMA_F32 ? distill<float, float>(a, sm_count, stream, launches)
+                                            : distill<float, __nv_bfloat16>(a, sm_count, stream, launches);
+    return a.dlogits_dtype == ADAMA_F32 ? distill<__nv_bfloat16, float>(a, sm_count, stream, launches)
+                                        : distill<__nv_bfloat16, __nv_bfloat16>(a, sm_count, stream, launches);
+}
 
 }  // namespace adama
