@@ -933,7 +933,7 @@ adama_status adama_layer_norm(adama_ctx *ctx, const adama_layer_norm_args *p, vo
     a.eps = (float)p->eps;
     a.mean = p->mean;
     a.rstd = p->rstd;
-    cudaError_t e = adama::launch_layer_norm(a, static_cast<cudaStream_t>(cuda_stream));
+    cudaError_t e = adama::launch_layer_norm(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream));
     if (e != cudaSuccess) return cuda_fail(ctx, "layer_norm launch", e);
     ctx->launches += 1;
     return ADAMA_OK;

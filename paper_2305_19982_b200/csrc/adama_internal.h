@@ -187,7 +187,7 @@ struct NormArgs {
     float eps;
     float *mean, *rstd;  // may be null
 };
-cudaError_t launch_layer_norm(const NormArgs &a, cudaStream_t stream);
+cudaError_t launch_layer_norm(const NormArgs &a, int sm_count, cudaStream_t stream);
 struct NormBackArgs {
     const void *dy, *x;
     void *dx;  // of x's type; may be null

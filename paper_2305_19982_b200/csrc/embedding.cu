@@ -41,14 +41,14 @@ embedding_kernel(const EmbeddingArgs a, int groups) {
     for (int u = 0; u < kLookupPieces; ++u) {
         const int c = first + u * kTile;
         count[u] = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
-        load_piece(table + (inside ? id * a.ld_table : 0) + c, inside ? count[u] : 0, all, v[u]);
+        load_piece<false>(table + (inside ? id * a.ld_table : 0) + c, inside ? count[u] : 0, all, v[u]);
     }
     const float other = id < 0 ? 0.f : NAN;
 #pragma unroll
     for (int u = 0; u < kLookupPieces; ++u) {
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) v[u][i] = inside ? v[u][i] * a.scale : other;
-        store_run(out + first + u * kTile, v[u], count[u], 32);
+        store_run<false>(out + first + u * kTile, v[u], count[u], 32);
     }
     if (!inside && id >= 0 && first == 0) record_bad_target(a.status, token);
 }
@@ -213,11 +213,11 @@ template <typename O, int MODE>
 __device__ __forceinline__ void load_target(const EmbeddingGradArgs &a, unsigned key, int c, int count, Target<O, MODE> &t) {
     if constexpr (MODE == kAdd) {
         const O *grad = static_cast<const O *>(a.grad);
-        load_piece(grad + (int64_t)key * a.ld_grad + c, count, extent_of(grad, a.vocab, a.dim, a.ld_grad), t.m);
+        load_piece<false>(grad + (int64_t)key * a.ld_grad + c, count, extent_of(grad, a.vocab, a.dim, a.ld_grad), t.m);
     }
     if constexpr (MODE == kFold) {
-        load_piece(a.m + (int64_t)key * a.ld_grad + c, count, extent_of(a.m, a.vocab, a.dim, a.ld_grad), t.m);
-        load_piece(a.v + (int64_t)key * a.ld_grad + c, count, extent_of(a.v, a.vocab, a.dim, a.ld_grad), t.v);
+        load_piece<false>(a.m + (int64_t)key * a.ld_grad + c, count, extent_of(a.m, a.vocab, a.dim, a.ld_grad), t.m);
+        load_piece<false>(a.v + (int64_t)key * a.ld_grad + c, count, extent_of(a.v, a.vocab, a.dim, a.ld_grad), t.v);
     }
 }
 template <typename O, int MODE>
@@ -229,14 +229,14 @@ __device__ __forceinline__ void finish(const EmbeddingGradArgs &a, unsigned key,
     if constexpr (MODE == kFold) {
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) fold1(g[i], t.m[i], t.v[i], a.fold.a, a.fold.b);
-        store_run(a.m + (int64_t)key * a.ld_grad + c, t.m, count, 32);
-        store_run(a.v + (int64_t)key * a.ld_grad + c, t.v, count, 32);
+        store_run<false>(a.m + (int64_t)key * a.ld_grad + c, t.m, count, 32);
+        store_run<false>(a.v + (int64_t)key * a.ld_grad + c, t.v, count, 32);
     } else {
         if constexpr (MODE == kAdd) {
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) g[i] += t.m[i];
         }
-        store_run(static_cast<O *>(a.grad) + (int64_t)key * a.ld_grad + c, g, count, 32);
+        store_run<false>(static_cast<O *>(a.grad) + (int64_t)key * a.ld_grad + c, g, count, 32);
     }
 }
 
@@ -314,7 +314,7 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
             k[q] = __shfl_sync(0xffffffffu, key, (j + q) & 31);
             const unsigned t = __shfl_sync(0xffffffffu, token, (j + q) & 31);
             if (j + q < live) {
-                load_piece(dy + (int64_t)t * a.ld_dy + c, count, all, x[q]);
+                load_piece<false>(dy + (int64_t)t * a.ld_dy + c, count, all, x[q]);
                 if (ends >> (j + q) & 1) load_target<O, MODE>(a, k[q], c, count, target[q]);
             }
         }

@@ -69,28 +69,67 @@ __device__ __forceinline__ void widen_words(const unsigned *z, float (&v)[kPiece
     for (int i = 0; i < kPiece; ++i) v[i] = __uint_as_float(z[i]);
 }
 
-// Elements p[0 .. count), count <= 8, as fp32; zeros behind them.
-template <typename T>
-__device__ __forceinline__ void load_piece(const T *p, int count, const Extent &all, float (&v)[kPiece]) {
-    constexpr int kWords = kPiece * sizeof(T) / 4;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~(uintptr_t)15;
-    if (count == kPiece && base == at) {
-        unsigned z[kWords];
-        load_words(z, reinterpret_cast<const unsigned char *>(p));
-        widen_words(z, v, T());
-    } else if (count == kPiece && base >= all.begin && base + 4 * kWords + 16 <= all.end) {
-        unsigned z[kWords + 4];
-        load_words(z, reinterpret_cast<const unsigned char *>(base));
-        move_words(z, (int)(at - base) / 4);
-        if (sizeof(T) == 2 && (at & 2)) {
+// A piece on its way: loads are issued for all of a thread's pieces before the first one is looked at.  EVEN: all
+// rows begin on 16-byte boundaries and are whole pieces long.  Otherwise the 16-byte units that a piece
+// touches are loaded, one more than it is long, as far as they lie in the matrix.
+template <typename T, bool EVEN>
+struct Piece {
+    static constexpr int kWords = kPiece * sizeof(T) / 4;
+    unsigned z[kWords + (EVEN ? 0 : 4)];
+
+    __device__ __forceinline__ void load(const T *p, int count, const Extent &all) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = EVEN ? at : at & ~(uintptr_t)15;
 #pragma unroll
-            for (int i = 0; i < kWords; ++i) z[i] = __funnelshift_r(z[i], z[i + 1], 16);
+        for (int i = 0; i < (int)(sizeof(z) / 16); ++i) {
+            const uintptr_t unit = base + 16 * i;
+            const bool wanted = EVEN ? count != 0 : unit < at + count * sizeof(T) && unit >= all.begin && unit + 16 <= all.end;
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (wanted) u = ld16(reinterpret_cast<const void *>(unit));
+            z[4 * i] = u.x;
+            z[4 * i + 1] = u.y;
+            z[4 * i + 2] = u.z;
+            z[4 * i + 3] = u.w;
         }
-        widen_words(z, v, T());
-    } else {
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) v[i] = i < count ? widen(p[i]) : 0.f;
     }
+    // its elements as fp32, zeros from `count` on
+    __device__ __forceinline__ void get(const T *p, int count, const Extent &all, float (&v)[kPiece]) const {
+        if constexpr (EVEN) {
+            widen_words(z, v, T());
+        } else {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~(uintptr_t)15;
+            unsigned y[kWords + 4];
+#pragma unroll
+            for (int i = 0; i < kWords + 4; ++i) y[i] = z[i];
+            move_words(y, (int)(at - base) / 4);
+            if (sizeof(T) == 2 && (at & 2)) {
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) y[i] = __funnelshift_r(y[i], y[i + 1], 16);
+            }
+            widen_words(y, v, T());
+            if (count != kPiece) {
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i)
+                    if (i >= count) v[i] = 0.f;
+            }
+            const uintptr_t end = (at + count * sizeof(T) + 15) & ~(uintptr_t)15;
+            if (count != 0 && (base < all.begin || end > all.end)) {  // at the matrix's ends a unit lies outside in part
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) v[i] = i < count ? widen(p[i]) : 0.f;
+            }
+        }
+    }
+};
+
+template <bool EVEN, typename T>
+__device__ __forceinline__ void load_piece(const T *p, int count, const Extent &all, float (&v)[kPiece]) {
+    Piece<T, EVEN> q;
+    q.load(p, count, all);
+    q.get(p, count, all, v);
+}
+
+// Whether rows of a matrix are even in that sense.
+inline bool even_rows(const void *p, int64_t cols, int64_t ld, int size) {
+    return aligned(p, 16) && cols % kPiece == 0 && ld * size % 16 == 0;
 }
 
 __device__ __forceinline__ void pack_words(const float (&v)[kPiece], unsigned (&w)[4], __nv_bfloat16) {
@@ -109,11 +148,19 @@ __device__ __forceinline__ void pack_words(const float (&v)[kPiece], unsigned (&
 // `count` elements that go to p (8, fewer at the row's end, 0 behind it).  All 32 lanes of a warp call it.
 // Where p is not on a 16-byte boundary a lane stores the eight elements from the next boundary on, of which
 // its neighbour has the last ones; only a run's ends are stored one by one.
-template <typename O>
+template <bool EVEN, typename O>
 __device__ __forceinline__ void store_run(O *p, const float (&v)[kPiece], int count, int lanes) {
     constexpr int kWords = kPiece * sizeof(O) / 4;
     unsigned w[kWords];
     pack_words(v, w, O());
+    if constexpr (EVEN) {
+        if (count != 0) {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i)
+                reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        }
+        return;
+    }
     const int past = (int)(reinterpret_cast<uintptr_t>(p) & 15);
     const int shift = past ? (16 - past) / (int)sizeof(O) : 0;  // elements before the boundary
     if (!__any_sync(0xffffffffu, shift != 0 && count > 0)) {
