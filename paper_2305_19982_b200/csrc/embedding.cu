@@ -10,6 +10,7 @@
 // kernel adds them in order.  So a token that occurs thousands of times is spread over the card like any others,
 // no atomics are involved and results do not depend on scheduling.  Bound by HBM.
 #include "adama_device.cuh"
+#include "chained.cuh"
 #include "row_access.cuh"
 
 namespace adama {
@@ -22,35 +23,32 @@ constexpr int kTile = 32 * kPiece;  // columns of a warp
 constexpr int kLookupWarps = 4;
 constexpr int kLookupPieces = 4;  // of a lane, all loaded before the first is stored
 
-template <typename T, typename O>
+template <typename T, typename O, bool EVEN>
 __global__ void __launch_bounds__(32 * kLookupWarps)
 embedding_kernel(const EmbeddingArgs a, int groups) {
     const int lane = threadIdx.x % 32;
     const int64_t task = (int64_t)blockIdx.x * kLookupWarps + threadIdx.x / 32;
     const int64_t token = task / groups;
-    const int first = (int)(task % groups) * kLookupPieces * kTile + lane * kPiece;
+    const int first = (int)(task - token * groups) * kLookupPieces * kTile;
     if (token >= a.tokens) return;
     const int64_t id = a.ids[token];
     const bool inside = id >= 0 && id < a.vocab;
-    const T *table = static_cast<const T *>(a.table);
-    const Extent all = extent_of(table, a.vocab, a.dim, a.ld_table);
-    O *out = static_cast<O *>(a.out) + token * a.ld_out;
-    float v[kLookupPieces][kPiece];
-    int count[kLookupPieces];
+    const Columns<EVEN> c = {lane, 32, a.dim - first};
+    const T *row = static_cast<const T *>(a.table) + (inside ? id * a.ld_table : 0) + first;
+    O *out = static_cast<O *>(a.out) + token * a.ld_out + first;
+    Piece<T, EVEN> raw[kLookupPieces];
 #pragma unroll
-    for (int u = 0; u < kLookupPieces; ++u) {
-        const int c = first + u * kTile;
-        count[u] = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
-        load_piece<false>(table + (inside ? id * a.ld_table : 0) + c, inside ? count[u] : 0, all, v[u]);
-    }
+    for (int u = 0; u < kLookupPieces; ++u) raw[u].load(row, c, u, inside);
     const float other = id < 0 ? 0.f : NAN;
 #pragma unroll
     for (int u = 0; u < kLookupPieces; ++u) {
+        float v[kPiece];
+        raw[u].get(v);
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) v[u][i] = inside ? v[u][i] * a.scale : other;
-        store_run<false>(out + first + u * kTile, v[u], count[u], 32);
+        for (int i = 0; i < kPiece; ++i) v[i] = inside ? v[i] * a.scale : other;
+        store_piece(out, c, u, true, v);
     }
-    if (!inside && id >= 0 && first == 0) record_bad_target(a.status, token);
+    if (!inside && id >= 0 && first == 0 && lane == 0) record_bad_target(a.status, token);
 }
 
 // ---- sorting by id ---------------------------------------------------------------------------------
@@ -69,6 +67,7 @@ constexpr int kRankTile = 2048;
 
 __global__ void __launch_bounds__(32 * kRankWarps)
 embedding_rank_kernel(const EmbeddingGradArgs a) {
+    let_next_start();
     __shared__ alignas(16) unsigned keys[kRankTile];
     __shared__ int counts[kRankWarps][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -204,58 +203,50 @@ embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
 
 enum GradMode { kWrite, kAdd, kFold };
 
-// What a finished sum meets in memory: loaded ahead of time.
-template <typename O, int MODE>
+// A warp's columns of one tile, and what a finished sum meets there in memory: loaded ahead of time.
+template <typename O, int MODE, bool EVEN>
 struct Target {
-    float m[MODE == kWrite ? 1 : kPiece], v[MODE == kFold ? kPiece : 1];
-};
-template <typename O, int MODE>
-__device__ __forceinline__ void load_target(const EmbeddingGradArgs &a, unsigned key, int c, int count, Target<O, MODE> &t) {
-    if constexpr (MODE == kAdd) {
-        const O *grad = static_cast<const O *>(a.grad);
-        load_piece<false>(grad + (int64_t)key * a.ld_grad + c, count, extent_of(grad, a.vocab, a.dim, a.ld_grad), t.m);
-    }
-    if constexpr (MODE == kFold) {
-        load_piece<false>(a.m + (int64_t)key * a.ld_grad + c, count, extent_of(a.m, a.vocab, a.dim, a.ld_grad), t.m);
-        load_piece<false>(a.v + (int64_t)key * a.ld_grad + c, count, extent_of(a.v, a.vocab, a.dim, a.ld_grad), t.v);
-    }
-}
-template <typename O, int MODE>
-__device__ __forceinline__ void finish(const EmbeddingGradArgs &a, unsigned key, int c, int count, const float (&sum)[kPiece],
-                                       Target<O, MODE> &t) {
-    float g[kPiece];
-#pragma unroll
-    for (int i = 0; i < kPiece; ++i) g[i] = sum[i] * a.scale;
-    if constexpr (MODE == kFold) {
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) fold1(g[i], t.m[i], t.v[i], a.fold.a, a.fold.b);
-        store_run<false>(a.m + (int64_t)key * a.ld_grad + c, t.m, count, 32);
-        store_run<false>(a.v + (int64_t)key * a.ld_grad + c, t.v, count, 32);
-    } else {
-        if constexpr (MODE == kAdd) {
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i) g[i] += t.m[i];
+    Piece<O, EVEN> m;      // of kAdd: the table; of kFold: the moments
+    Piece<float, EVEN> v;
+
+    __device__ __forceinline__ void load(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN> &c, bool wanted) {
+        const int64_t at = (int64_t)key * a.ld_grad + first;
+        if constexpr (MODE == kAdd) m.load(static_cast<const O *>(a.grad) + (wanted ? at : 0), c, 0, wanted);
+        if constexpr (MODE == kFold) {
+            m.load(a.m + (wanted ? at : 0), c, 0, wanted);
+            v.load(a.v + (wanted ? at : 0), c, 0, wanted);
         }
-        store_run<false>(static_cast<O *>(a.grad) + (int64_t)key * a.ld_grad + c, g, count, 32);
     }
-}
+    __device__ __forceinline__ void finish(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN> &c,
+                                           const float (&sum)[kPiece]) const {
+        const int64_t at = (int64_t)key * a.ld_grad + first;
+        float g[kPiece], x[kPiece], y[kPiece];
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) g[i] = sum[i] * a.scale;
+        if constexpr (MODE == kFold) {
+            m.get(x);
+            v.get(y);
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) fold1(g[i], x[i], y[i], a.fold.a, a.fold.b);
+            store_piece(a.m + at, c, 0, true, x);
+            store_piece(a.v + at, c, 0, true, y);
+        } else {
+            if constexpr (MODE == kAdd) {
+                m.get(x);
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) g[i] += x[i];
+            }
+            store_piece(static_cast<O *>(a.grad) + at, c, 0, true, g);
+        }
+    }
+};
 
 // Part `slot` of chunk b: 0 continues the chunk before, 1 begins in b and goes on behind it.
 __device__ __forceinline__ float *part_of(const EmbeddingGradArgs &a, int64_t b, int slot) {
     return a.parts + (2 * b + slot) * a.pad;
 }
-__device__ __forceinline__ void put_part(float *p, const float (&sum)[kPiece]) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
-}
-__device__ __forceinline__ void add_part(const float *p, float (&sum)[kPiece]) {
-    const float4 x = __ldcg(reinterpret_cast<const float4 *>(p)), y = __ldcg(reinterpret_cast<const float4 *>(p) + 1);
-    sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-    sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
-}
 
 constexpr int kGradWarps = 4;
-constexpr int kBatch = 4;  // tokens whose rows are loaded together
 
 template <typename O>
 __device__ __forceinline__ void zero_row(O *p, int n, int lane) {
@@ -266,32 +257,36 @@ __device__ __forceinline__ void zero_row(O *p, int n, int lane) {
     if (lane < head) p[lane] = narrowed<O>(0.f);
     if (lane < n - tail) p[tail + lane] = narrowed<O>(0.f);
 }
+constexpr int kZeroRows = 8;  // rows of a warp, of those that may have no token
 
-// chunk: tokens of a warp, up to 32.  Blocks from sum_blocks on zero the rows that have no token.
-template <typename G, typename O, int MODE>
-__global__ void __launch_bounds__(32 * kGradWarps)
-embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned sum_blocks) {
+// chunk: tokens of a warp, up to 32.  The first zero_blocks blocks zero the rows that have no token.
+template <typename G, typename O, int MODE, bool EVEN>
+__global__ void __launch_bounds__(32 * kGradWarps, MODE == kFold ? 4 : 5)
+embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned zero_blocks) {
+    constexpr int kBatch = MODE == kWrite ? 8 : 4;  // tokens whose rows are loaded together
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    if (MODE == kWrite && blockIdx.x >= sum_blocks) {
-        const int64_t first = ((int64_t)(blockIdx.x - sum_blocks) * kGradWarps + warp) * 32;
+    let_next_start();
+    wait_for_previous();
+    if (MODE == kWrite && blockIdx.x < zero_blocks) {
+        const int64_t first = ((int64_t)blockIdx.x * kGradWarps + warp) * kZeroRows;
         const int64_t row = first + lane;
-        int64_t lo = 0, hi = a.tokens;  // the first token whose key is not below the row
+        int64_t lo = 0, hi = lane < kZeroRows ? a.tokens : 0;  // the first token whose key is not below the row
         while (lo < hi) {
             const int64_t mid = (lo + hi) / 2;
             if ((int64_t)a.keys[mid] < row) lo = mid + 1;
             else hi = mid;
         }
-        const bool empty = row < a.vocab && (lo == a.tokens || (int64_t)a.keys[lo] != row);
+        const bool empty = lane < kZeroRows && row < a.vocab && (lo == a.tokens || (int64_t)a.keys[lo] != row);
         unsigned todo = __ballot_sync(0xffffffffu, empty);
         for (; todo; todo &= todo - 1)
             zero_row(static_cast<O *>(a.grad) + (first + __ffs(todo) - 1) * a.ld_grad, a.dim, lane);
         return;
     }
-    const int64_t task = (int64_t)blockIdx.x * kGradWarps + warp, b = task / tiles;
+    const int64_t task = (int64_t)(blockIdx.x - zero_blocks) * kGradWarps + warp, b = task / tiles;
     const int64_t start = b * chunk;
     if (start >= a.tokens) return;
-    const int c = (int)(task % tiles) * kTile + lane * kPiece;
-    const int count = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
+    const int tile = (int)(task - b * tiles) * kTile;
+    const Columns<EVEN> c = {lane, 32, a.dim - tile};
     const int n = (int)(a.tokens - start < chunk ? a.tokens - start : chunk);
     const unsigned none = 0xffffffffu, out = (unsigned)a.vocab;
     const unsigned key = lane < n ? a.keys[start + lane] : none, token = lane < n ? a.order[start + lane] : 0;
@@ -302,103 +297,106 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     const unsigned ends = __ballot_sync(0xffffffffu, lane < n && next != key);
     const int live = __popc(__ballot_sync(0xffffffffu, lane < n && key != out));  // the others come last
     bool open = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the first run continues the chunk before
-    const G *dy = static_cast<const G *>(a.dy);
-    const Extent all = extent_of(dy, a.tokens, a.dim, a.ld_dy);
+    const G *dy = static_cast<const G *>(a.dy) + tile;
     float sum[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int j = 0; j < live; j += kBatch) {
-        float x[kBatch][kPiece];
-        Target<O, MODE> target[kBatch];
+        Piece<G, EVEN> raw[kBatch];
+        Target<O, MODE, EVEN> target[kBatch];
         unsigned k[kBatch];
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
+            const bool in = j + q < live;
             k[q] = __shfl_sync(0xffffffffu, key, (j + q) & 31);
             const unsigned t = __shfl_sync(0xffffffffu, token, (j + q) & 31);
-            if (j + q < live) {
-                load_piece<false>(dy + (int64_t)t * a.ld_dy + c, count, all, x[q]);
-                if (ends >> (j + q) & 1) load_target<O, MODE>(a, k[q], c, count, target[q]);
-            }
+            raw[q].load(dy + (in ? (int64_t)t * a.ld_dy : 0), c, 0, in);
+            target[q].load(a, k[q], tile, c, in && (ends >> (j + q) & 1));
         }
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
-            if (j + q < live) {
+            float x[kPiece];
+            raw[q].get(x);
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) sum[i] += x[q][i];
-                if (ends >> (j + q) & 1) {
-                    if (open) {
-                        if (count) put_part(part_of(a, b, 0) + c, sum);
-                    } else {
-                        finish<O, MODE>(a, k[q], c, count, sum, target[q]);
-                    }
-                    open = false;
+            for (int i = 0; i < kPiece; ++i) sum[i] += x[i];
+            if (j + q < live && (ends >> (j + q) & 1)) {
+                if (open) store_piece(part_of(a, b, 0) + tile, c, 0, true, sum);
+                else target[q].finish(a, k[q], tile, c, sum);
+                open = false;
 #pragma unroll
-                    for (int i = 0; i < kPiece; ++i) sum[i] = 0.f;
-                }
+                for (int i = 0; i < kPiece; ++i) sum[i] = 0.f;
             }
         }
     }
-    if (live == n && !(ends >> (n - 1) & 1) && count) put_part(part_of(a, b, open ? 0 : 1) + c, sum);
+    if (live == n && !(ends >> (n - 1) & 1)) store_piece(part_of(a, b, open ? 0 : 1) + tile, c, 0, true, sum);
 }
 
 // Runs that cross chunks: block x takes the one that begins in chunk x and goes on behind it, if there is one.
 constexpr int kJoinWarps = 8;
 constexpr int kJoinShort = 16;  // parts up to which a warp adds them alone
 
-template <typename O, int MODE>
+template <typename O, int MODE, bool EVEN>
 __global__ void __launch_bounds__(32 * kJoinWarps)
 embedding_join_kernel(const EmbeddingGradArgs a, int chunk, int tiles) {
     __shared__ float slots[kJoinWarps][kTile];
+    wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t b = blockIdx.x, start = b * chunk, end = start + chunk;
     if (end >= a.tokens) return;
-    const unsigned key = a.keys[end - 1];
-    if (key == (unsigned)a.vocab || a.keys[end] != key) return;
-    if (start > 0 && a.keys[start - 1] == key && a.keys[start] == key) return;  // begins in an earlier chunk
+    const unsigned key = a.keys[end - 1], after = a.keys[end], before = start > 0 ? a.keys[start - 1] : 0xffffffffu;
+    const int64_t first_at = (b + 1 + lane) * chunk;
+    const unsigned first_key = first_at < a.tokens ? a.keys[first_at] : 0xffffffffu;
+    if (key == (unsigned)a.vocab || after != key || before == key) return;  // (one that began in an earlier chunk fills this one)
     int64_t last = b;  // the chunk in which the run ends
-    for (;;) {
+    for (bool more_to_see = true, first = true; more_to_see; first = false) {
         const int64_t at = (last + 1 + lane) * chunk;
-        const unsigned more = __ballot_sync(0xffffffffu, at < a.tokens && a.keys[at] == key);
+        const unsigned more = __ballot_sync(0xffffffffu, first ? first_key == key : at < a.tokens && a.keys[at] == key);
         const int run = more == 0xffffffffu ? 32 : __ffs(~more) - 1;
         last += run;
-        if (run < 32) break;
+        more_to_see = run == 32;
     }
     const int64_t parts = last - b;  // behind the first one
     const int first_tile = blockIdx.y * kJoinWarps;
     if (parts <= kJoinShort) {
-        const int tile = first_tile + warp;
-        if (tile >= tiles) return;
-        const int c = tile * kTile + lane * kPiece;
-        const int count = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
-        Target<O, MODE> target;
-        load_target<O, MODE>(a, key, c, count, target);
-        float sum[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (count) {
-            add_part(part_of(a, b, 1) + c, sum);
+        if (first_tile + warp >= tiles) return;
+        const int tile = (first_tile + warp) * kTile;
+        const Columns<EVEN> c = {lane, 32, a.dim - tile};
+        Target<O, MODE, EVEN> target;
+        target.load(a, key, tile, c, true);
+        float sum[kPiece];
+        load_piece<float>(part_of(a, b, 1) + tile, c, 0, true, sum);
 #pragma unroll 4
-            for (int64_t i = b + 1; i <= last; ++i) add_part(part_of(a, i, 0) + c, sum);
+        for (int64_t i = b + 1; i <= last; ++i) {
+            float x[kPiece];
+            load_piece<float>(part_of(a, i, 0) + tile, c, 0, true, x);
+#pragma unroll
+            for (int q = 0; q < kPiece; ++q) sum[q] += x[q];
         }
-        finish<O, MODE>(a, key, c, count, sum, target);
+        target.finish(a, key, tile, c, sum);
         return;
     }
     // long: the warps share the parts of a tile, one tile after the other
-    for (int tile = first_tile; tile < tiles && tile < first_tile + kJoinWarps; ++tile) {
-        const int c = tile * kTile + lane * kPiece;
-        const int count = c < a.dim ? (a.dim - c < kPiece ? a.dim - c : kPiece) : 0;
+    for (int i = first_tile; i < tiles && i < first_tile + kJoinWarps; ++i) {
+        const int tile = i * kTile;
+        const Columns<EVEN> c = {lane, 32, a.dim - tile};
         const int64_t from = b + 1 + parts * warp / kJoinWarps, to = b + 1 + parts * (warp + 1) / kJoinWarps;
-        float sum[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (count) {
-            if (warp == 0) add_part(part_of(a, b, 1) + c, sum);
-#pragma unroll 8
-            for (int64_t i = from; i < to; ++i) add_part(part_of(a, i, 0) + c, sum);
+        float sum[kPiece];
+        load_piece<float>(part_of(a, b, 1) + tile, c, 0, warp == 0, sum);
+#pragma unroll 4
+        for (int64_t j = from; j < to; ++j) {
+            float x[kPiece];
+            load_piece<float>(part_of(a, j, 0) + tile, c, 0, true, x);
+#pragma unroll
+            for (int q = 0; q < kPiece; ++q) sum[q] += x[q];
         }
-        put_part(&slots[warp][lane * kPiece], sum);
+#pragma unroll
+        for (int q = 0; q < kPiece; ++q) slots[warp][q * 32 + lane] = sum[q];
         __syncthreads();
         if (warp == 0) {
-            Target<O, MODE> target;
-            load_target<O, MODE>(a, key, c, count, target);
+            Target<O, MODE, EVEN> target;
+            target.load(a, key, tile, c, true);
             for (int w = 1; w < kJoinWarps; ++w)
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) sum[i] += slots[w][lane * kPiece + i];
-            finish<O, MODE>(a, key, c, count, sum, target);
+                for (int q = 0; q < kPiece; ++q) sum[q] += slots[w][q * 32 + lane];
+            target.finish(a, key, tile, c, sum);
         }
         __syncthreads();
     }
@@ -409,8 +407,11 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk, int tiles) {
 template <typename T, typename O>
 cudaError_t lookup(const EmbeddingArgs &a, cudaStream_t stream) {
     const int groups = (a.dim + kLookupPieces * kTile - 1) / (kLookupPieces * kTile);
-    const int64_t blocks = (a.tokens * groups + kLookupWarps - 1) / kLookupWarps;
-    embedding_kernel<T, O><<<(unsigned)blocks, 32 * kLookupWarps, 0, stream>>>(a, groups);
+    const unsigned blocks = (unsigned)((a.tokens * groups + kLookupWarps - 1) / kLookupWarps);
+    if (even_rows(a.table, a.dim, a.ld_table, sizeof(T)) && even_rows(a.out, a.dim, a.ld_out, sizeof(O)))
+        embedding_kernel<T, O, true><<<blocks, 32 * kLookupWarps, 0, stream>>>(a, groups);
+    else
+        embedding_kernel<T, O, false><<<blocks, 32 * kLookupWarps, 0, stream>>>(a, groups);
     return cudaGetLastError();
 }
 
@@ -476,24 +477,39 @@ cudaError_t sort_tokens(EmbeddingGradArgs &a, const GradPlan &p, unsigned char *
     return cudaGetLastError();
 }
 
-template <typename G, typename O, int MODE>
+template <typename G, typename O, int MODE, bool EVEN>
 cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t stream, int *launches) {
-    const unsigned sum_blocks = (unsigned)((p.chunks * p.tiles + kGradWarps - 1) / kGradWarps);
-    const unsigned zero_blocks = MODE == kWrite ? (unsigned)((a.vocab + 32 * kGradWarps - 1) / (32 * kGradWarps)) : 0;
+    const int64_t sum_blocks = (p.chunks * p.tiles + kGradWarps - 1) / kGradWarps;
+    const int64_t zero_blocks = MODE == kWrite ? (a.vocab + kZeroRows * kGradWarps - 1) / (kZeroRows * kGradWarps) : 0;
     if (sum_blocks + zero_blocks == 0) return cudaSuccess;
-    embedding_grad_kernel<G, O, MODE><<<sum_blocks + zero_blocks, 32 * kGradWarps, 0, stream>>>(a, p.chunk, p.tiles, sum_blocks);
+    const dim3 grid((unsigned)(sum_blocks + zero_blocks)), block(32 * kGradWarps);
+    cudaError_t e;
+    if (a.tokens > 0) {
+        e = launch_chained(embedding_grad_kernel<G, O, MODE, EVEN>, grid, block, 0, stream, a, p.chunk, p.tiles, (unsigned)zero_blocks);
+    } else {  // no sort in front
+        embedding_grad_kernel<G, O, MODE, EVEN><<<grid, block, 0, stream>>>(a, p.chunk, p.tiles, (unsigned)zero_blocks);
+        e = cudaGetLastError();
+    }
+    if (e != cudaSuccess) return e;
     *launches += 1;
     if (p.chunks > 1) {
-        const dim3 grid((unsigned)(p.chunks - 1), (unsigned)((p.tiles + kJoinWarps - 1) / kJoinWarps));
-        embedding_join_kernel<O, MODE><<<grid, 32 * kJoinWarps, 0, stream>>>(a, p.chunk, p.tiles);
+        const dim3 joins((unsigned)(p.chunks - 1), (unsigned)((p.tiles + kJoinWarps - 1) / kJoinWarps));
+        e = launch_chained(embedding_join_kernel<O, MODE, EVEN>, joins, dim3(32 * kJoinWarps), 0, stream, a, p.chunk, p.tiles);
         *launches += 1;
     }
-    return cudaGetLastError();
+    return e;
+}
+template <typename G, typename O, int MODE>
+cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t stream, int *launches) {
+    const bool even = even_rows(a.dy, a.dim, a.ld_dy, sizeof(G)) &&
+                      (MODE == kFold ? even_rows(a.m, a.dim, a.ld_grad, 4) && aligned(a.v, 16) : even_rows(a.grad, a.dim, a.ld_grad, sizeof(O)));
+    return even ? sums<G, O, MODE, true>(a, p, stream, launches) : sums<G, O, MODE, false>(a, p, stream, launches);
 }
 template <typename G>
 cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t stream, int *launches) {
     if (a.m) return sums<G, float, kFold>(a, p, stream, launches);
-    if (a.grad_dtype == ADAMA_F32) return a.accumulate ? sums<G, float, kAdd>(a, p, stream, launches) : sums<G, float, kWrite>(a, p, stream, launches);
+    if (a.grad_dtype == ADAMA_F32)
+        return a.accumulate ? sums<G, float, kAdd>(a, p, stream, launches) : sums<G, float, kWrite>(a, p, stream, launches);
     return a.accumulate ? sums<G, __nv_bfloat16, kAdd>(a, p, stream, launches) : sums<G, __nv_bfloat16, kWrite>(a, p, stream, launches);
 }
 

@@ -12,170 +12,214 @@
 #include "chained.cuh"
 #include "row_access.cuh"
 #include "softmax_rows.cuh"
+#include "tensor_table.cuh"
 
 namespace adama {
 namespace {
 
-// ---- groups of threads that share a row ---------------------------------------------------------
-// Up to 32 lanes of a warp (a power of two), or the whole block.
+// ---- threads that share a row -------------------------------------------------------------------
+// Up to 32 lanes of a warp (a power of two), or some warps of a block.
 
 __device__ __forceinline__ float lanes_sum(float x, int lanes) {
     for (int o = lanes / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-
-// The sums of N values over the row's group, in every thread.
-template <bool BLOCK, int N>
-__device__ __forceinline__ void group_sums(float (&x)[N], int lanes, float (*slots)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = lanes_sum(x[i], BLOCK ? 32 : lanes);
-    if (!BLOCK) return;
-    const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
-    if (lane == 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) slots[threadIdx.x / 32][i] = x[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = lanes_sum(lane < warps ? slots[lane][i] : 0.f, 32);
-    __syncthreads();
+__device__ __forceinline__ float pair_sum(Pair p) {
+    float a, b;
+    split(p, a, b);
+    return a + b;
 }
 
-__device__ __forceinline__ int piece_count(int column, int dim) {
-    return column + kPiece <= dim ? kPiece : column < dim ? dim - column : 0;
+// Warps of a block that share rows: `warps` to a row, several such groups side by side.
+struct Group {
+    int warps, index, count, t;
+
+    __device__ __forceinline__ explicit Group(int w)
+        : warps(w), index((int)threadIdx.x / 32 / w), count((int)blockDim.x / 32 / w), t((int)threadIdx.x - index * 32 * w) {}
+    __device__ __forceinline__ void sync() const {
+        if (warps == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + index), "r"(32 * warps) : "memory");
+    }
+    // The sum of x over the group, in every thread.  `slots`: one for each warp of the block, used again no sooner than
+    // behind another sync of the group.
+    __device__ __forceinline__ float sum(float x, float *slots) const {
+        x = lanes_sum(x, 32);
+        if (warps == 1) return x;
+        if (threadIdx.x % 32 == 0) slots[threadIdx.x / 32] = x;
+        sync();
+        x = 0.f;
+        for (int i = 0; i < warps; ++i) x += slots[index * warps + i];
+        return x;
+    }
+};
+
+constexpr int kGroupWarps = 16;  // of a block, at most
+constexpr int kAhead = 3;        // rows of a thread on their way, of even ones
+
+// A row's elements as fp32, and its distances from the mean.
+template <bool EVEN>
+__device__ __forceinline__ float sum_of(const float (&v)[kPiece]) {
+    Pair s = 0;
+#pragma unroll
+    for (int i = 0; i < kPiece; i += 2) s = add2(s, pair(v[i], v[i + 1]));
+    return pair_sum(s);
+}
+template <bool EVEN>
+__device__ __forceinline__ float centre(float (&v)[kPiece], const Columns<EVEN> &c, int u, float mean) {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i)
+        if (!c.has(u, i)) v[i] = mean;  // columns that the row does not have lie at no distance
+    Pair s = 0;
+#pragma unroll
+    for (int i = 0; i < kPiece; i += 2) {
+        const Pair d = add2(pair(v[i], v[i + 1]), pair(-mean, -mean));
+        s = fma2(d, d, s);
+        split(d, v[i], v[i + 1]);
+    }
+    return pair_sum(s);
+}
+__device__ __forceinline__ void scale_shift(float (&v)[kPiece], float rstd, const float (&w)[kPiece], const float (&b)[kPiece]) {
+#pragma unroll
+    for (int i = 0; i < kPiece; i += 2)
+        split(fma2(mul2(pair(v[i], v[i + 1]), pair(rstd, rstd)), pair(w[i], w[i + 1]), pair(b[i], b[i + 1])), v[i], v[i + 1]);
 }
 
 // ---- forward -------------------------------------------------------------------------------------
 
-// U pieces to a thread.  BLOCK: a row to a block, else to `lanes` lanes of a warp.  Exchanges between lanes are the
-// dearest instructions here, and a row takes two chains of them in every warp that shares it: so a lane takes many
-// pieces where there are rows enough for all SMs (4096 x 1600 fp32 to bf16: 17.3 us with one piece to a thread, @FWD@).
-template <typename T, typename O, int U, bool BLOCK, bool EVEN>
-__global__ void __launch_bounds__(BLOCK ? (U <= 2 ? 1024 : 256) : 128)
-layer_norm_kernel(const NormArgs a, int lanes) {
-    __shared__ float slots[32][1];
-    const int width = BLOCK ? (int)blockDim.x : lanes, t = threadIdx.x % width;
-    const int64_t row = BLOCK ? blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / lanes) + threadIdx.x / lanes;
+// Rows of up to 256 elements: `lanes` lanes to a row, one piece to a lane.
+constexpr int kShortThreads = 128;
+
+template <typename T, typename O, bool EVEN>
+__global__ void __launch_bounds__(kShortThreads)
+layer_norm_short_kernel(const NormArgs a, int lanes) {
+    const Columns<EVEN> c = {(int)threadIdx.x % lanes, lanes, a.dim};
+    const int64_t row = (int64_t)blockIdx.x * (kShortThreads / lanes) + threadIdx.x / lanes;
     const bool live = row < a.rows;
-    const T *x = static_cast<const T *>(a.x);
-    const Extent all = extent_of(x, a.rows, a.dim, a.ld_x);
-    x += (live ? row : 0) * a.ld_x;
-    Piece<T, EVEN> raw[U];
-    float v[U][kPiece];
-    int count[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int c = (t + u * width) * kPiece;
-        count[u] = live ? piece_count(c, a.dim) : 0;
-        raw[u].load(x + c, count[u], all);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u].get(x + (t + u * width) * kPiece, count[u], all, v[u]);
-    Pair sums = 0;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < kPiece; i += 2) sums = add2(sums, pair(v[u][i], v[u][i + 1]));
-    float s[1], other;
-    split(sums, s[0], other);
-    s[0] += other;
-    group_sums<BLOCK, 1>(s, lanes, slots);
-    const float mean = s[0] / (float)a.dim;  // (a product with 1/D would move the mean of equal values)
-    sums = 0;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (count[u] != kPiece) {  // elements behind the row: no distance from the mean
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i)
-                if (i >= count[u]) v[u][i] = mean;
-        }
-#pragma unroll
-        for (int i = 0; i < kPiece; i += 2) {
-            const Pair d = add2(pair(v[u][i], v[u][i + 1]), pair(-mean, -mean));
-            sums = fma2(d, d, sums);
-            split(d, v[u][i], v[u][i + 1]);
-        }
-    }
-    split(sums, s[0], other);
-    s[0] += other;
-    group_sums<BLOCK, 1>(s, lanes, slots);
-    const float rstd = 1.f / sqrtf(s[0] / (float)a.dim + a.eps);
-    if (t == 0 && live) {
+    float v[kPiece], w[kPiece], b[kPiece];
+    Piece<T, EVEN> raw;
+    Piece<float, EVEN> raw_w, raw_b;
+    raw.load(static_cast<const T *>(a.x) + (live ? row : 0) * a.ld_x, c, 0, live);
+    raw_w.load(a.weight, c, 0, live);
+    raw_b.load(a.bias, c, 0, live && a.bias);
+    raw.get(v);
+    const float mean = lanes_sum(sum_of<EVEN>(v), lanes) / (float)a.dim;  // (a product with 1/D would move the mean of equal values)
+    const float rstd = 1.f / sqrtf(lanes_sum(centre(v, c, 0, mean), lanes) / (float)a.dim + a.eps);
+    if (c.t == 0 && live) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
     }
-    const Extent params_w = {reinterpret_cast<uintptr_t>(a.weight), reinterpret_cast<uintptr_t>(a.weight + a.dim)};
-    const Extent params_b = {reinterpret_cast<uintptr_t>(a.bias), reinterpret_cast<uintptr_t>(a.bias + a.dim)};
-    O *y = static_cast<O *>(a.y) + (live ? row : 0) * a.ld_y;
+    raw_w.get(w);
+    raw_b.get(b);
+    scale_shift(v, rstd, w, b);
+    store_piece(static_cast<O *>(a.y) + (live ? row : 0) * a.ld_y, c, 0, live, v);
+}
+
+// Longer rows: a group of warps walks rows, U pieces to a thread, weight and bias in registers, the next rows on their
+// way.  (One row to a block that ends with it: @FWD@.)
+template <typename T, typename O, int U, bool EVEN>
+__global__ void __launch_bounds__(32 * kGroupWarps)
+layer_norm_kernel(const NormArgs a, int warps) {
+    extern __shared__ uint4 ahead[];  // [rows ahead][U][units of a piece][threads]
+    __shared__ float slots[2][kGroupWarps];
+    constexpr int kUnits = Piece<T, true>::kUnits;
+    const Group group(warps);
+    const Columns<EVEN> c = {group.t, 32 * warps, a.dim};
+    const T *x0 = static_cast<const T *>(a.x);
+    const int64_t step = (int64_t)gridDim.x * group.count;
+    int64_t row = (int64_t)blockIdx.x * group.count + group.index;
+    const auto slot = [&](int stage, int u, int i) { return ahead + ((stage * U + u) * kUnits + i) * blockDim.x + threadIdx.x; };
+    const auto send_for = [&](int64_t r, int stage) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (r < a.rows && c.has(u, 0)) {
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i)
+                    copy16((uint32_t)__cvta_generic_to_shared(slot(stage, u, i)), reinterpret_cast<const uint4 *>(x0 + r * a.ld_x + c.at(u, 0)) + i);
+            }
+        copies_end_group();
+    };
+    Piece<T, EVEN> next[U];
+    if constexpr (EVEN) {
+        for (int i = 0; i < kAhead; ++i) send_for(row + i * step, i);
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u].load(x0 + (row < a.rows ? row : 0) * a.ld_x, c, u, row < a.rows);
+    }
+    float w[U][kPiece], b[U][kPiece];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int c = (t + u * width) * kPiece;
-        float w[kPiece], b[kPiece];
-        Piece<float, EVEN> raw_w, raw_b;
-        raw_w.load(a.weight + c, count[u], params_w);
-        raw_b.load(a.bias + c, a.bias ? count[u] : 0, params_b);
-        raw_w.get(a.weight + c, count[u], params_w, w);
-        raw_b.get(a.bias + c, a.bias ? count[u] : 0, params_b, b);
+        load_piece(a.weight, c, u, true, w[u]);
+        load_piece(a.bias, c, u, a.bias != nullptr, b[u]);
+    }
+    for (int stage = 0; row < a.rows; row += step, stage = stage + 1 == kAhead ? 0 : stage + 1) {
+        float v[U][kPiece], s = 0.f;
+        if constexpr (EVEN) {
+            copies_wait<kAhead - 1>();
 #pragma unroll
-        for (int i = 0; i < kPiece; i += 2) {
-            const Pair xhat = mul2(pair(v[u][i], v[u][i + 1]), pair(rstd, rstd));
-            split(fma2(xhat, pair(w[i], w[i + 1]), pair(b[i], b[i + 1])), v[u][i], v[u][i + 1]);
+            for (int u = 0; u < U; ++u)
+                if (c.has(u, 0)) {
+#pragma unroll
+                    for (int i = 0; i < kUnits; ++i) next[u].even[i] = *slot(stage, u, i);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kUnits; ++i) next[u].even[i] = make_uint4(0, 0, 0, 0);
+                }
         }
-        store_run<EVEN>(y + c, v[u], count[u], BLOCK ? 32 : lanes);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            next[u].get(v[u]);
+            s += sum_of<EVEN>(v[u]);
+        }
+        if constexpr (!EVEN) {
+            const int64_t r = row + step;
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u].load(x0 + (r < a.rows ? r : 0) * a.ld_x, c, u, r < a.rows);
+        }
+        const float mean = group.sum(s, slots[0]) / (float)a.dim;
+        if constexpr (EVEN) send_for(row + kAhead * step, stage);  // what was there has been summed up
+        s = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) s += centre(v[u], c, u, mean);
+        const float rstd = 1.f / sqrtf(group.sum(s, slots[1]) / (float)a.dim + a.eps);
+        if (c.t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        O *y = static_cast<O *>(a.y) + row * a.ld_y;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            scale_shift(v[u], rstd, w[u], b[u]);
+            store_piece(y, c, u, true, v[u]);
+        }
     }
 }
 
-// Rows that no block holds in registers: read three times, from L2 if they stay there.
+// Rows that no group holds in registers: read three times, from L2 if they stay there.
 constexpr int kLongThreads = 512;
 
 template <typename T, typename O>
 __global__ void __launch_bounds__(kLongThreads)
 layer_norm_long_kernel(const NormArgs a) {
-    __shared__ float slots[32][1];
+    __shared__ float slots[2][kGroupWarps];
+    const Group group(kGroupWarps);
     const int64_t row = blockIdx.x;
-    const T *x = static_cast<const T *>(a.x);
-    const Extent all = extent_of(x, a.rows, a.dim, a.ld_x);
-    x += row * a.ld_x;
-    constexpr int kStep = kLongThreads * kPiece;
-    const int first = threadIdx.x * kPiece;
-    float s[1] = {0.f}, v[kPiece];
-    for (int64_t c = first; c < a.dim; c += kStep) {
-        load_piece<false>(x + c, piece_count((int)c, a.dim), all, v);
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) s[0] += v[i];
+    const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
+    float s = 0.f;
+    for (int c = threadIdx.x; c < a.dim; c += kLongThreads) s += widen(x[c]);
+    const float mean = group.sum(s, slots[0]) / (float)a.dim;
+    s = 0.f;
+    for (int c = threadIdx.x; c < a.dim; c += kLongThreads) {
+        const float d = widen(x[c]) - mean;
+        s = fmaf(d, d, s);
     }
-    group_sums<true, 1>(s, 32, slots);
-    const float mean = s[0] / (float)a.dim;  // (a product with 1/D would move the mean of equal values)
-    s[0] = 0.f;
-    for (int64_t c = first; c < a.dim; c += kStep) {
-        const int count = piece_count((int)c, a.dim);
-        load_piece<false>(x + c, count, all, v);
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) {
-            const float d = i < count ? v[i] - mean : 0.f;
-            s[0] = fmaf(d, d, s[0]);
-        }
-    }
-    group_sums<true, 1>(s, 32, slots);
-    const float rstd = 1.f / sqrtf(s[0] / (float)a.dim + a.eps);
+    const float rstd = 1.f / sqrtf(group.sum(s, slots[1]) / (float)a.dim + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
     }
     O *y = static_cast<O *>(a.y) + row * a.ld_y;
-    const Extent params_w = {reinterpret_cast<uintptr_t>(a.weight), reinterpret_cast<uintptr_t>(a.weight + a.dim)};
-    const Extent params_b = {reinterpret_cast<uintptr_t>(a.bias), reinterpret_cast<uintptr_t>(a.bias + a.dim)};
-    for (int64_t c0 = 0; c0 < a.dim; c0 += kStep) {  // whole warps: they store together
-        const int64_t c = c0 + first;
-        const int count = c < a.dim ? piece_count((int)c, a.dim) : 0;
-        float w[kPiece], b[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        load_piece<false>(x + c, count, all, v);
-        load_piece<false>(a.weight + c, count, params_w, w);
-        if (a.bias) load_piece<false>(a.bias + c, count, params_b, b);
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) v[i] = fmaf((v[i] - mean) * rstd, w[i], b[i]);
-        store_run<false>(y + c, v, count, 32);
-    }
+    for (int c = threadIdx.x; c < a.dim; c += kLongThreads)
+        y[c] = narrowed<O>(fmaf((widen(x[c]) - mean) * rstd, a.weight[c], a.bias ? a.bias[c] : 0.f));
 }
 
 // ---- backward ------------------------------------------------------------------------------------
@@ -183,33 +227,14 @@ layer_norm_long_kernel(const NormArgs a) {
 // A block's sums in the workspace: dweight, then dbias, each padded to whole pieces.
 __host__ __device__ inline int64_t padded(int dim) { return ((int64_t)dim + kPiece - 1) / kPiece * kPiece; }
 
-// The sums of N values (2 or 4) over a warp, each in the lanes whose upper bits are its number: values are
-// traded for other values' halves, six exchanges instead of twenty for four of them.
-template <int N>
-__device__ __forceinline__ float traded_sums(const float (&v)[N], int lane) {
-    static_assert(N == 2 || N == 4, "values");
-    const bool high = lane & 16, odd = lane & 8;
-    float c = (high ? v[N / 2] : v[0]) + __shfl_xor_sync(0xffffffffu, high ? v[0] : v[N / 2], 16);
-    if (N == 4) {
-        const float b = (high ? v[N - 1] : v[1]) + __shfl_xor_sync(0xffffffffu, high ? v[1] : v[N - 1], 16);
-        c = (odd ? b : c) + __shfl_xor_sync(0xffffffffu, odd ? c : b, 8);
-    } else {
-        c += __shfl_xor_sync(0xffffffffu, c, 8);
-    }
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-    return c;
-}
-
 // Sums over rows, of a thread's columns.
 struct PieceSums {
     Pair dw[kPiece / 2], db[kPiece / 2];
 };
-
 __device__ __forceinline__ Pair xhat_of(float x0, float x1, float mean, float rstd) {
     return mul2(add2(pair(x0, x1), pair(-mean, -mean)), pair(rstd, rstd));
 }
-// A piece's part in its columns' sums and in its row's two.  Elements behind the row are 0 in dy and add nothing.
+// A piece's part in its columns' sums and in its row's two.  Columns that the row does not have are 0 in dy and add nothing.
 __device__ __forceinline__ void take_piece(const float (&x)[kPiece], const float (&dy)[kPiece], const float (&w)[kPiece], float mean, float rstd,
                                            PieceSums &sums, Pair &s1, Pair &s2) {
 #pragma unroll
@@ -232,19 +257,15 @@ __device__ __forceinline__ void piece_dx(const float (&x)[kPiece], const float (
         split(mul2(fma2(xhat, pair(-s2, -s2), g), pair(rstd, rstd)), dx[2 * i], dx[2 * i + 1]);
     }
 }
-__device__ __forceinline__ void store_sums(float *p, const Pair (&v)[kPiece / 2], bool add) {
-    float4 q[2];
+// A piece's sums to a vector of all columns, or in addition to what is there.
+template <bool EVEN>
+__device__ __forceinline__ void put_sums(float *to, const Columns<EVEN> &c, int u, const Pair (&v)[kPiece / 2], bool add) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        q[h] = add ? reinterpret_cast<const float4 *>(p)[h] : make_float4(0.f, 0.f, 0.f, 0.f);
-        float a, b;
-        split(v[2 * h], a, b);
-        q[h].x += a;
-        q[h].y += b;
-        split(v[2 * h + 1], a, b);
-        q[h].z += a;
-        q[h].w += b;
-        reinterpret_cast<float4 *>(p)[h] = q[h];
+    for (int i = 0; i < kPiece / 2; ++i) {
+        float p, q;
+        split(v[i], p, q);
+        if (c.has(u, 2 * i)) to[c.at(u, 2 * i)] = add ? to[c.at(u, 2 * i)] + p : p;
+        if (c.has(u, 2 * i + 1)) to[c.at(u, 2 * i + 1)] = add ? to[c.at(u, 2 * i + 1)] + q : q;
     }
 }
 
@@ -253,47 +274,47 @@ constexpr int kLanesThreads = 256;
 
 template <typename T, typename G, bool EVEN>
 __global__ void __launch_bounds__(kLanesThreads)
-layer_norm_backward_lanes_kernel(const NormBackArgs a, int lanes) {
-    __shared__ alignas(16) float total[2 * 32 * kPiece];
+layer_norm_backward_short_kernel(const NormBackArgs a, int lanes) {
+    __shared__ float total[2 * 32 * kPiece];
     let_next_start();
-    const int t = threadIdx.x % lanes, groups = kLanesThreads / lanes, c = t * kPiece, count = piece_count(c, a.dim);
+    const Columns<EVEN> c = {(int)threadIdx.x % lanes, lanes, a.dim};
+    const int groups = kLanesThreads / lanes;
     const T *x0 = static_cast<const T *>(a.x);
     const G *dy0 = static_cast<const G *>(a.dy);
-    const Extent x_all = extent_of(x0, a.rows, a.dim, a.ld_x), dy_all = extent_of(dy0, a.rows, a.dim, a.ld_dy);
-    const Extent params_w = {reinterpret_cast<uintptr_t>(a.weight), reinterpret_cast<uintptr_t>(a.weight + a.dim)};
     float w[kPiece];
-    load_piece<EVEN>(a.weight + c, count, params_w, w);
+    load_piece(a.weight, c, 0, true, w);
     PieceSums sums = {};
-    // all lanes of a warp go round together, the last rows of some being none
-    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += (int64_t)gridDim.x * groups) {
-        const int64_t row = base + threadIdx.x / lanes;
+    const int64_t step = (int64_t)gridDim.x * groups;
+    Piece<T, EVEN> next_x;
+    Piece<G, EVEN> next_dy;
+    float next_mean = 0.f, next_rstd = 0.f;
+    const auto send_for = [&](int64_t row) {
         const bool live = row < a.rows;
-        const int n = live ? count : 0;
+        next_x.load(x0 + (live ? row * a.ld_x : 0), c, 0, live);
+        next_dy.load(dy0 + (live ? row * a.ld_dy : 0), c, 0, live);
+        next_mean = live ? a.mean[row] : 0.f;
+        next_rstd = live ? a.rstd[row] : 0.f;
+    };
+    send_for((int64_t)blockIdx.x * groups + threadIdx.x / lanes);
+    // all lanes of a warp go round together, the last rows of some being none
+    for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += step) {
+        const int64_t row = base + threadIdx.x / lanes;
         float x[kPiece], dy[kPiece];
-        Piece<T, EVEN> raw_x;
-        Piece<G, EVEN> raw_dy;
-        const T *px = x0 + (live ? row * a.ld_x : 0) + c;
-        const G *pdy = dy0 + (live ? row * a.ld_dy : 0) + c;
-        raw_x.load(px, n, x_all);
-        raw_dy.load(pdy, n, dy_all);
-        const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
-        raw_x.get(px, n, x_all, x);
-        raw_dy.get(pdy, n, dy_all, dy);
+        next_x.get(x);
+        next_dy.get(dy);
+        const float mean = next_mean, rstd = next_rstd;
+        send_for(row + step);
         Pair p1 = 0, p2 = 0;
         take_piece(x, dy, w, mean, rstd, sums, p1, p2);
         if (!a.dx) continue;
-        float s1, s2, other;
-        split(p1, s1, other);
-        s1 = lanes_sum(s1 + other, lanes) * a.inv_dim;
-        split(p2, s2, other);
-        s2 = lanes_sum(s2 + other, lanes) * a.inv_dim;
+        const float s1 = lanes_sum(pair_sum(p1), lanes) * a.inv_dim, s2 = lanes_sum(pair_sum(p2), lanes) * a.inv_dim;
         float dx[kPiece];
         piece_dx(x, dy, w, mean, rstd, s1, s2, dx);
-        store_run<EVEN>(static_cast<T *>(a.dx) + (live ? row * a.ld_dx : 0) + c, dx, n, lanes);
+        const bool live = row < a.rows;
+        store_piece(static_cast<T *>(a.dx) + (live ? row * a.ld_dx : 0), c, 0, live, dx);
     }
     if (!a.parts) return;
     // the rows of a warp by exchange, the warps one after the other in shared memory
-    const int cols = lanes * kPiece;
 #pragma unroll
     for (int i = 0; i < kPiece / 2; ++i)
         for (int o = lanes; o < 32; o <<= 1) {
@@ -302,8 +323,8 @@ layer_norm_backward_lanes_kernel(const NormBackArgs a, int lanes) {
         }
     for (int warp = 0; warp < kLanesThreads / 32; ++warp) {
         if ((int)threadIdx.x / 32 == warp && (int)threadIdx.x % 32 < lanes) {
-            store_sums(total + c, sums.dw, warp > 0);
-            store_sums(total + cols + c, sums.db, warp > 0);
+            put_sums(total, c, 0, sums.dw, warp > 0);
+            put_sums(total + 32 * kPiece, c, 0, sums.db, warp > 0);
         }
         __syncthreads();
     }
@@ -311,124 +332,149 @@ layer_norm_backward_lanes_kernel(const NormBackArgs a, int lanes) {
     float *part = a.parts + (int64_t)blockIdx.x * 2 * pad;
     for (int i = threadIdx.x; i < a.dim; i += kLanesThreads) {
         part[i] = total[i];
-        part[pad + i] = total[cols + i];
+        part[pad + i] = total[32 * kPiece + i];
     }
 }
 
-// Longer rows: W warps to a row, two pieces to a thread, of ROWS rows at a time; the groups of a block join their sums
-// in shared memory, so that one set of them leaves an SM.
-constexpr int kBackPieces = 2;     // U
-constexpr int kBackWarps = 16;     // of a block
-
-template <typename T, typename G, int ROWS, bool EVEN>
-__global__ void __launch_bounds__(32 * kBackWarps)
+// Longer rows: a group of warps walks rows, U pieces to a thread, the next rows on their way (to registers, of uneven rows,
+// with one piece to a thread).  The groups of a block join their sums in shared memory, so that one set of them leaves an SM.
+template <typename T, typename G, int U, bool EVEN>
+__global__ void __launch_bounds__(32 * kGroupWarps)
 layer_norm_backward_kernel(const NormBackArgs a, int warps) {
-    constexpr int U = kBackPieces;
-    extern __shared__ __align__(16) float joined[];  // two sums of each column, where a block has several groups
-    __shared__ alignas(16) float slots[2][kBackWarps][2 * ROWS];
+    constexpr int kUnitsX = Piece<T, true>::kUnits, kUnits = kUnitsX + Piece<G, true>::kUnits;
+    constexpr bool kNext = !EVEN && U == 1;
+    extern __shared__ uint4 ahead[];  // [rows ahead][U][units of both pieces][threads]; at the end two sums of each column
+    __shared__ float slots[2][kGroupWarps][2];
     let_next_start();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, group = warp / warps, groups = (int)blockDim.x / 32 / warps;
-    const int width = 32 * warps, t = threadIdx.x - group * width;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const Group group(warps);
+    const Columns<EVEN> c = {group.t, 32 * warps, a.dim};
     const T *x0 = static_cast<const T *>(a.x);
     const G *dy0 = static_cast<const G *>(a.dy);
-    const Extent x_all = extent_of(x0, a.rows, a.dim, a.ld_x), dy_all = extent_of(dy0, a.rows, a.dim, a.ld_dy);
-    const Extent params_w = {reinterpret_cast<uintptr_t>(a.weight), reinterpret_cast<uintptr_t>(a.weight + a.dim)};
+    const int64_t step = (int64_t)gridDim.x * group.count;
+    int64_t row = (int64_t)blockIdx.x * group.count + group.index;
+    const auto slot = [&](int stage, int u, int i) { return ahead + ((stage * U + u) * kUnits + i) * blockDim.x + threadIdx.x; };
+    const auto send_for = [&](int64_t r, int stage) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (r < a.rows && c.has(u, 0)) {
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i)
+                    copy16((uint32_t)__cvta_generic_to_shared(slot(stage, u, i)),
+                           i < kUnitsX ? reinterpret_cast<const uint4 *>(x0 + r * a.ld_x + c.at(u, 0)) + i
+                                       : reinterpret_cast<const uint4 *>(dy0 + r * a.ld_dy + c.at(u, 0)) + (i - kUnitsX));
+            }
+        copies_end_group();
+    };
+    Piece<T, EVEN> raw_x[U], next_x[U];
+    Piece<G, EVEN> raw_dy[U], next_dy[U];
+    float next_mean = 0.f, next_rstd = 0.f;
+    const auto load = [&](int64_t r, Piece<T, EVEN> (&px)[U], Piece<G, EVEN> (&pdy)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            px[u].load(x0 + (r < a.rows ? r * a.ld_x : 0), c, u, r < a.rows);
+            pdy[u].load(dy0 + (r < a.rows ? r * a.ld_dy : 0), c, u, r < a.rows);
+        }
+    };
+    if constexpr (EVEN) {
+        for (int i = 0; i < kAhead; ++i) send_for(row + i * step, i);
+    } else if constexpr (kNext) {
+        load(row, next_x, next_dy);
+    }
+    if (row < a.rows) {
+        next_mean = a.mean[row];
+        next_rstd = a.rstd[row];
+    }
     float w[U][kPiece];
     PieceSums sums[U] = {};
-    int count[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int c = (t + u * width) * kPiece;
-        count[u] = piece_count(c, a.dim);
-        load_piece<EVEN>(a.weight + c, count[u], params_w, w[u]);
-    }
-    const int64_t stride = (int64_t)gridDim.x * groups;
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * groups + group; row < a.rows; row += ROWS * stride, turn ^= 1) {
-        Piece<T, EVEN> raw_x[ROWS][U];
-        Piece<G, EVEN> raw_dy[ROWS][U];
-        const T *px[ROWS];
-        const G *pdy[ROWS];
-        float mean[ROWS], rstd[ROWS], v[2 * ROWS];
-        bool live[ROWS];
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const int64_t at = row + r * stride;
-            live[r] = at < a.rows;
-            px[r] = x0 + (live[r] ? at * a.ld_x : 0) + t * kPiece;
-            pdy[r] = dy0 + (live[r] ? at * a.ld_dy : 0) + t * kPiece;
+    for (int u = 0; u < U; ++u) load_piece(a.weight, c, u, true, w[u]);
+    for (int stage = 0, turn = 0; row < a.rows; row += step, stage = stage + 1 == kAhead ? 0 : stage + 1, turn ^= 1) {
+        const float mean = next_mean, rstd = next_rstd;
+        if (row + step < a.rows) {
+            next_mean = a.mean[row + step];
+            next_rstd = a.rstd[row + step];
+        }
+        if constexpr (EVEN) {
+            copies_wait<kAhead - 1>();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                raw_x[r][u].load(px[r] + u * width * kPiece, live[r] ? count[u] : 0, x_all);
-                raw_dy[r][u].load(pdy[r] + u * width * kPiece, live[r] ? count[u] : 0, dy_all);
-            }
-            mean[r] = live[r] ? a.mean[at] : 0.f;
-            rstd[r] = live[r] ? a.rstd[at] : 0.f;
-        }
+                const bool has = c.has(u, 0);
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            Pair s1 = 0, s2 = 0;
-            float other;
+                for (int i = 0; i < kUnits; ++i) {
+                    const uint4 q = has ? *slot(stage, u, i) : make_uint4(0, 0, 0, 0);
+                    if (i < kUnitsX) raw_x[u].even[i < kUnitsX ? i : 0] = q;
+                    else raw_dy[u].even[i < kUnitsX ? 0 : i - kUnitsX] = q;
+                }
+            }
+        } else if constexpr (kNext) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                float x[kPiece], dy[kPiece];
-                raw_x[r][u].get(px[r] + u * width * kPiece, live[r] ? count[u] : 0, x_all, x);
-                raw_dy[r][u].get(pdy[r] + u * width * kPiece, live[r] ? count[u] : 0, dy_all, dy);
-                take_piece(x, dy, w[u], mean[r], rstd[r], sums[u], s1, s2);
+                raw_x[u] = next_x[u];
+                raw_dy[u] = next_dy[u];
             }
-            split(s1, v[2 * r], other);
-            v[2 * r] += other;
-            split(s2, v[2 * r + 1], other);
-            v[2 * r + 1] += other;
+            load(row + step, next_x, next_dy);
+        } else {
+            load(row, raw_x, raw_dy);
         }
-        if (!a.dx) continue;
-        const float mine = traded_sums(v, lane);
-        if (lane % (16 / ROWS) == 0) slots[turn][warp][lane / (16 / ROWS)] = mine;
-        if (warps == 1) __syncwarp();
-        else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(width) : "memory");
-        float all[2 * ROWS] = {};
-        for (int i = 0; i < warps; ++i) {
+        Pair p1 = 0, p2 = 0;
 #pragma unroll
-            for (int q = 0; q < 2 * ROWS; ++q) all[q] += slots[turn][group * warps + i][q];
+        for (int u = 0; u < U; ++u) {
+            float x[kPiece], dy[kPiece];
+            raw_x[u].get(x);
+            raw_dy[u].get(dy);
+            take_piece(x, dy, w[u], mean, rstd, sums[u], p1, p2);
         }
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            T *dx = static_cast<T *>(a.dx) + (live[r] ? (row + r * stride) * a.ld_dx : 0) + t * kPiece;
+        if (a.dx) {
+            // two sums over a warp: each half of it takes one
+            const float s1 = pair_sum(p1), s2 = pair_sum(p2);
+            float s = (lane & 16 ? s2 : s1) + __shfl_xor_sync(0xffffffffu, lane & 16 ? s1 : s2, 16);
+            s = lanes_sum(s, 16);
+            if (lane % 16 == 0) slots[turn][warp][lane / 16] = s;
+            group.sync();
+            float m1 = 0.f, m2 = 0.f;
+            for (int i = 0; i < warps; ++i) {
+                const float2 q = *reinterpret_cast<const float2 *>(slots[turn][group.index * warps + i]);
+                m1 += q.x;
+                m2 += q.y;
+            }
+            m1 *= a.inv_dim;
+            m2 *= a.inv_dim;
+            T *dx = static_cast<T *>(a.dx) + row * a.ld_dx;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float x[kPiece], dy[kPiece], out[kPiece];
-                raw_x[r][u].get(px[r] + u * width * kPiece, live[r] ? count[u] : 0, x_all, x);
-                raw_dy[r][u].get(pdy[r] + u * width * kPiece, live[r] ? count[u] : 0, dy_all, dy);
-                piece_dx(x, dy, w[u], mean[r], rstd[r], all[2 * r] * a.inv_dim, all[2 * r + 1] * a.inv_dim, out);
-                store_run<EVEN>(dx + u * width * kPiece, out, live[r] ? count[u] : 0, 32);
+                raw_x[u].get(x);
+                raw_dy[u].get(dy);
+                piece_dx(x, dy, w[u], mean, rstd, m1, m2, out);
+                store_piece(dx, c, u, true, out);
             }
         }
+        if constexpr (EVEN) send_for(row + kAhead * step, stage);  // behind the last use of what was there
     }
     if (!a.parts) return;
     const int64_t pad = padded(a.dim);
-    float *part = a.parts + (int64_t)blockIdx.x * 2 * pad;
-    for (int q = 0; q < groups; ++q) {
-        if (q == group) {
-            float *to = q + 1 == groups ? part : joined;
+    float *part = a.parts + (int64_t)blockIdx.x * 2 * pad, *joined = reinterpret_cast<float *>(ahead);
+    __syncthreads();  // all copies have been waited for by those who sent for them
+    for (int q = 0; q < group.count; ++q) {
+        if (q == group.index) {
+            const bool last = q + 1 == group.count;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int64_t c = (int64_t)(t + u * width) * kPiece;
-                if (count[u] == 0) continue;
-                if (q > 0 && q + 1 == groups) {  // the last one brings them out
+                if (q > 0 && last) {  // the last group brings the sums out
 #pragma unroll
                     for (int i = 0; i < kPiece / 2; ++i) {
-                        const float2 dw = *reinterpret_cast<const float2 *>(joined + c + 2 * i);
-                        const float2 db = *reinterpret_cast<const float2 *>(joined + pad + c + 2 * i);
-                        sums[u].dw[i] = add2(sums[u].dw[i], pair(dw.x, dw.y));
-                        sums[u].db[i] = add2(sums[u].db[i], pair(db.x, db.y));
+                        const int at0 = c.at(u, 2 * i), at1 = c.at(u, 2 * i + 1);
+                        const bool has0 = c.has(u, 2 * i), has1 = c.has(u, 2 * i + 1);
+                        sums[u].dw[i] = add2(sums[u].dw[i], pair(has0 ? joined[at0] : 0.f, has1 ? joined[at1] : 0.f));
+                        sums[u].db[i] = add2(sums[u].db[i], pair(has0 ? joined[pad + at0] : 0.f, has1 ? joined[pad + at1] : 0.f));
                     }
                 }
-                const bool add = q > 0 && q + 1 < groups;
-                store_sums(to + c, sums[u].dw, add);
-                store_sums(to + pad + c, sums[u].db, add);
+                put_sums(last ? part : joined, c, u, sums[u].dw, q > 0 && !last);
+                put_sums((last ? part : joined) + pad, c, u, sums[u].db, q > 0 && !last);
             }
         }
-        if (q + 1 < groups) __syncthreads();
+        if (q + 1 < group.count) __syncthreads();
     }
 }
 
@@ -436,66 +482,61 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
 template <typename T, typename G>
 __global__ void __launch_bounds__(kLongThreads)
 layer_norm_row_sums_kernel(const NormBackArgs a, float2 *sums) {
-    __shared__ float slots[32][2];
+    __shared__ float slots[2][kGroupWarps];
+    const Group group(kGroupWarps);
     const int64_t row = blockIdx.x;
-    const T *x = static_cast<const T *>(a.x);
-    const G *dy = static_cast<const G *>(a.dy);
-    const Extent x_all = extent_of(x, a.rows, a.dim, a.ld_x), dy_all = extent_of(dy, a.rows, a.dim, a.ld_dy);
-    const Extent params_w = {reinterpret_cast<uintptr_t>(a.weight), reinterpret_cast<uintptr_t>(a.weight + a.dim)};
+    const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
+    const G *dy = static_cast<const G *>(a.dy) + row * a.ld_dy;
     const float mean = a.mean[row], rstd = a.rstd[row];
-    float s[2] = {0.f, 0.f};
-    for (int64_t c = threadIdx.x * kPiece; c < a.dim; c += kLongThreads * kPiece) {
-        const int count = piece_count((int)c, a.dim);
-        float v[kPiece], g[kPiece], w[kPiece];
-        load_piece<false>(x + row * a.ld_x + c, count, x_all, v);
-        load_piece<false>(dy + row * a.ld_dy + c, count, dy_all, g);
-        load_piece<false>(a.weight + c, count, params_w, w);
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i)
-            if (i < count) {
-                s[0] = fmaf(g[i], w[i], s[0]);
-                s[1] = fmaf(g[i] * w[i], (v[i] - mean) * rstd, s[1]);
-            }
+    float s1 = 0.f, s2 = 0.f;
+    for (int c = threadIdx.x; c < a.dim; c += kLongThreads) {
+        const float g = widen(dy[c]) * a.weight[c];
+        s1 += g;
+        s2 = fmaf(g, (widen(x[c]) - mean) * rstd, s2);
     }
-    group_sums<true, 2>(s, 32, slots);
-    if (threadIdx.x == 0) sums[row] = make_float2(s[0] * a.inv_dim, s[1] * a.inv_dim);
+    s1 = group.sum(s1, slots[0]);
+    s2 = group.sum(s2, slots[1]);
+    if (threadIdx.x == 0) sums[row] = make_float2(s1 * a.inv_dim, s2 * a.inv_dim);
 }
+
+constexpr int kTileColumns = 2;  // of a thread, kLanesThreads apart
 
 template <typename T, typename G>
 __global__ void __launch_bounds__(kLanesThreads)
 layer_norm_tiles_kernel(const NormBackArgs a, const float2 *sums) {
-    const int c = (blockIdx.x * kLanesThreads + threadIdx.x) * kPiece, count = piece_count(c, a.dim);
+    const int c0 = blockIdx.x * kTileColumns * kLanesThreads + threadIdx.x;
     const T *x0 = static_cast<const T *>(a.x);
     const G *dy0 = static_cast<const G *>(a.dy);
-    const Extent x_all = extent_of(x0, a.rows, a.dim, a.ld_x), dy_all = extent_of(dy0, a.rows, a.dim, a.ld_dy);
-    const Extent params_w = {reinterpret_cast<uintptr_t>(a.weight), reinterpret_cast<uintptr_t>(a.weight + a.dim)};
-    float w[kPiece], dw[kPiece], db[kPiece];
-    load_piece<false>(a.weight + c, count, params_w, w);
+    T *dx0 = static_cast<T *>(a.dx);
+    float w[kTileColumns], dw[kTileColumns], db[kTileColumns];
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) dw[i] = db[i] = 0.f;
+    for (int i = 0; i < kTileColumns; ++i) {
+        w[i] = c0 + i * kLanesThreads < a.dim ? a.weight[c0 + i * kLanesThreads] : 0.f;
+        dw[i] = db[i] = 0.f;
+    }
+#pragma unroll 4
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        float x[kPiece], g[kPiece], out[kPiece];
-        load_piece<false>(x0 + row * a.ld_x + c, count, x_all, x);
-        load_piece<false>(dy0 + row * a.ld_dy + c, count, dy_all, g);
         const float mean = a.mean[row], rstd = a.rstd[row];
         const float2 s = a.dx ? sums[row] : make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) {
-            const float xhat = (x[i] - mean) * rstd;
-            db[i] += g[i];
-            dw[i] = fmaf(g[i], xhat, dw[i]);
-            out[i] = rstd * (g[i] * w[i] - fmaf(xhat, s.y, s.x));
+        for (int i = 0; i < kTileColumns; ++i) {
+            const int c = c0 + i * kLanesThreads;
+            if (c >= a.dim) continue;
+            const float g = widen(dy0[row * a.ld_dy + c]), xhat = (widen(x0[row * a.ld_x + c]) - mean) * rstd;
+            db[i] += g;
+            dw[i] = fmaf(g, xhat, dw[i]);
+            if (a.dx) dx0[row * a.ld_dx + c] = narrowed<T>(rstd * (g * w[i] - fmaf(xhat, s.y, s.x)));
         }
-        if (a.dx) store_run<false>(static_cast<T *>(a.dx) + row * a.ld_dx + c, out, count, 32);
     }
     if (!a.parts) return;
     float *part = a.parts + (int64_t)blockIdx.y * 2 * padded(a.dim);
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i)
-        if (i < count) {
-            part[c + i] = dw[i];
-            part[padded(a.dim) + c + i] = db[i];
-        }
+    for (int i = 0; i < kTileColumns; ++i) {
+        const int c = c0 + i * kLanesThreads;
+        if (c >= a.dim) continue;
+        part[c] = dw[i];
+        part[padded(a.dim) + c] = db[i];
+    }
 }
 
 // The blocks' sums, 32 columns to a block; warps take every 16th, then the warps' sums in their order.
@@ -532,34 +573,46 @@ int lanes_for(int pieces) {
     while (lanes < pieces) lanes *= 2;
     return lanes;
 }
+constexpr int kLongPieces = 64 * kGroupWarps;  // longer rows are read more than once
+
+// How a call over rows of up to kLongPieces pieces runs: pieces to a thread, warps to a row, rows side by side.
+struct RowPlan {
+    int pieces, each, warps, groups;
+};
 
 template <typename T, typename O, int U, bool EVEN>
-void forward_rows(const NormArgs &a, int pieces, cudaStream_t stream) {
-    const int warps = (pieces + 32 * U - 1) / (32 * U);
-    if (warps == 1) layer_norm_kernel<T, O, U, false, EVEN><<<(unsigned)((a.rows + 3) / 4), 128, 0, stream>>>(a, 32);
-    else layer_norm_kernel<T, O, U, true, EVEN><<<(unsigned)a.rows, 32 * warps, 0, stream>>>(a, 32);
+cudaError_t forward_groups(const NormArgs &a, const RowPlan &p, int sm_count, cudaStream_t stream) {
+    constexpr int kResident = 768;  // threads of an SM that 80 registers allow
+    const int threads = 32 * p.warps * p.groups;
+    const size_t shared = EVEN ? (size_t)kAhead * U * Piece<T, true>::kUnits * threads * 16 : 0;
+    const unsigned grid = grid_for((size_t)a.rows, (size_t)p.groups, sm_count, threads < kResident ? kResident / threads : 1);
+    if (shared > 40 * 1024) {  // with the static part, more than a kernel has unasked
+        static std::atomic<unsigned long long> ready{0};
+        const cudaError_t e = allow_shared(layer_norm_kernel<T, O, U, EVEN>, 160 * 1024, ready);
+        if (e != cudaSuccess) return e;
+    }
+    layer_norm_kernel<T, O, U, EVEN><<<grid, threads, shared, stream>>>(a, p.warps);
+    return cudaGetLastError();
 }
 
 template <typename T, typename O, bool EVEN>
 cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
-    const int pieces = (int)(padded(a.dim) / kPiece);
-    // as many pieces to a lane as leave every SM a dozen warps
-    const auto enough = [&](int u) { return a.rows * ((pieces + 32 * u - 1) / (32 * u)) >= 12 * (int64_t)sm_count; };
-    if (pieces <= 32) {
-        const int lanes = lanes_for(pieces), rows = 128 / lanes;
-        layer_norm_kernel<T, O, 1, false, EVEN><<<(unsigned)((a.rows + rows - 1) / rows), 128, 0, stream>>>(a, lanes);
-    } else if (pieces > 2048) {
-        layer_norm_long_kernel<T, O><<<(unsigned)a.rows, kLongThreads, 0, stream>>>(a);
-    } else if (EVEN && pieces > 128 && enough(8)) {
-        forward_rows<T, O, EVEN ? 8 : 4, EVEN>(a, pieces, stream);
-    } else if (pieces > 64 && pieces <= 1024 && enough(4)) {
-        forward_rows<T, O, 4, EVEN>(a, pieces, stream);
-    } else if (pieces > 1024 || enough(2)) {
-        forward_rows<T, O, 2, EVEN>(a, pieces, stream);
-    } else {
-        forward_rows<T, O, 1, EVEN>(a, pieces, stream);
+    RowPlan p;
+    p.pieces = (int)(padded(a.dim) / kPiece);
+    if (p.pieces <= 32) {
+        const int lanes = lanes_for(p.pieces), rows = kShortThreads / lanes;
+        layer_norm_short_kernel<T, O, EVEN><<<(unsigned)((a.rows + rows - 1) / rows), kShortThreads, 0, stream>>>(a, lanes);
+        return cudaGetLastError();
     }
-    return cudaGetLastError();
+    if (p.pieces > kLongPieces) {
+        layer_norm_long_kernel<T, O><<<(unsigned)a.rows, kLongThreads, 0, stream>>>(a);
+        return cudaGetLastError();
+    }
+    // few rows: more threads to each
+    p.each = p.pieces > 32 * kGroupWarps || a.rows >= 2 * (int64_t)sm_count ? 2 : 1;
+    p.warps = (p.pieces + 32 * p.each - 1) / (32 * p.each);
+    p.groups = p.warps < 4 && a.rows >= 2 * (int64_t)sm_count ? 4 / p.warps : 1;
+    return p.each == 2 ? forward_groups<T, O, 2, EVEN>(a, p, sm_count, stream) : forward_groups<T, O, 1, EVEN>(a, p, sm_count, stream);
 }
 template <typename T, typename O>
 cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
@@ -569,31 +622,28 @@ cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
 }
 
 // Blocks of the backward pass, whose sums the workspace holds; behind them two sums of each row where rows are long.
-struct BackPlan {
-    int pieces, warps, groups;  // warps to a row, rows side by side in a block
+struct BackPlan : RowPlan {
     bool is_long;
     int64_t parts;
-    size_t shared;
 };
-BackPlan plan_back(int64_t rows, int dim, int sm_count) {
+BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even) {
     BackPlan p;
     p.pieces = (int)(padded(dim) / kPiece);
-    p.warps = (p.pieces + 32 * kBackPieces - 1) / (32 * kBackPieces);
+    p.each = p.pieces > 32 * kGroupWarps || (even && rows >= 2 * (int64_t)sm_count) ? 2 : 1;
+    p.warps = (p.pieces + 32 * p.each - 1) / (32 * p.each);
     p.groups = 1;
-    p.is_long = p.warps > kBackWarps;
-    p.shared = 0;
+    p.is_long = p.pieces > kLongPieces;
     int64_t most = sm_count;
     if (p.pieces <= 32) {
         p.groups = kLanesThreads / lanes_for(p.pieces);
         most = 4 * (int64_t)sm_count;
     } else if (p.is_long) {
-        const int64_t tiles = (p.pieces + kLanesThreads - 1) / kLanesThreads;
+        const int64_t tiles = (dim + kTileColumns * kLanesThreads - 1) / (kTileColumns * kLanesThreads);
         most = (4 * (int64_t)sm_count + tiles - 1) / tiles;
     } else {
         // as many rows to a block as it has warps for, fewer where that would leave SMs without any
-        p.groups = kBackWarps / p.warps;
+        p.groups = kGroupWarps / p.warps;
         while (p.groups > 1 && rows < (int64_t)sm_count * p.groups) p.groups -= 1;
-        if (p.groups > 1) p.shared = (size_t)2 * padded(dim) * sizeof(float);
     }
     p.parts = (rows + p.groups - 1) / p.groups;
     if (p.parts > most) p.parts = most;
@@ -601,51 +651,66 @@ BackPlan plan_back(int64_t rows, int dim, int sm_count) {
     return p;
 }
 
+template <typename T, typename G, int U, bool EVEN>
+cudaError_t back_groups(const NormBackArgs &a, const BackPlan &p, cudaStream_t stream) {
+    const int threads = 32 * p.warps * p.groups;
+    size_t shared = EVEN ? (size_t)kAhead * U * (Piece<T, true>::kUnits + Piece<G, true>::kUnits) * threads * 16 : 0;
+    const size_t joined = p.groups > 1 && a.parts ? (size_t)2 * padded(a.dim) * sizeof(float) : 0;
+    if (shared < joined) shared = joined;
+    if (shared > 40 * 1024) {  // with the static part, more than a kernel has unasked
+        static std::atomic<unsigned long long> ready{0};
+        const cudaError_t e = allow_shared(layer_norm_backward_kernel<T, G, U, EVEN>, 200 * 1024, ready);
+        if (e != cudaSuccess) return e;
+    }
+    layer_norm_backward_kernel<T, G, U, EVEN><<<(unsigned)p.parts, threads, shared, stream>>>(a, p.warps);
+    return cudaGetLastError();
+}
 template <typename T, typename G, bool EVEN>
-void launch_back(const NormBackArgs &a, const BackPlan &p, cudaStream_t stream) {
-    // two rows at a time where their pieces leave registers for it
-    constexpr int kRows = EVEN && sizeof(T) == 2 && sizeof(G) == 2 ? 2 : 1;
-    const unsigned grid = (unsigned)p.parts;
-    if (p.pieces <= 32) layer_norm_backward_lanes_kernel<T, G, EVEN><<<grid, kLanesThreads, 0, stream>>>(a, lanes_for(p.pieces));
-    else layer_norm_backward_kernel<T, G, kRows, EVEN><<<grid, 32 * p.warps * p.groups, p.shared, stream>>>(a, p.warps);
+cudaError_t launch_back(const NormBackArgs &a, const BackPlan &p, cudaStream_t stream) {
+    if (p.pieces <= 32) {
+        layer_norm_backward_short_kernel<T, G, EVEN><<<(unsigned)p.parts, kLanesThreads, 0, stream>>>(a, lanes_for(p.pieces));
+        return cudaGetLastError();
+    }
+    return p.each == 2 ? back_groups<T, G, 2, EVEN>(a, p, stream) : back_groups<T, G, 1, EVEN>(a, p, stream);
 }
 
 template <typename T, typename G>
 cudaError_t backward(const NormBackArgs &a, int sm_count, cudaStream_t stream, int *launches) {
-    const BackPlan p = plan_back(a.rows, a.dim, sm_count);
-    const unsigned grid = (unsigned)p.parts;
+    const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T)) && even_rows(a.dy, a.dim, a.ld_dy, sizeof(G)) &&
+                      (!a.dx || even_rows(a.dx, a.dim, a.ld_dx, sizeof(T))) && aligned(a.weight, 16);
+    const BackPlan p = plan_back(a.rows, a.dim, sm_count, even);
+    cudaError_t e = cudaSuccess;
     if (a.rows > 0) {
         if (p.is_long) {
             float2 *sums = reinterpret_cast<float2 *>(static_cast<float *>(a.workspace) + p.parts * 2 * padded(a.dim));
             if (a.dx) layer_norm_row_sums_kernel<T, G><<<(unsigned)a.rows, kLongThreads, 0, stream>>>(a, sums);
-            const dim3 tiles((unsigned)((p.pieces + kLanesThreads - 1) / kLanesThreads), grid);
+            const dim3 tiles((unsigned)((a.dim + kTileColumns * kLanesThreads - 1) / (kTileColumns * kLanesThreads)), (unsigned)p.parts);
             layer_norm_tiles_kernel<T, G><<<tiles, kLanesThreads, 0, stream>>>(a, sums);
+            e = cudaGetLastError();
         } else {
-            const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T)) && even_rows(a.dy, a.dim, a.ld_dy, sizeof(G)) &&
-                              (!a.dx || even_rows(a.dx, a.dim, a.ld_dx, sizeof(T))) && aligned(a.weight, 16);
-            if (even) launch_back<T, G, true>(a, p, stream);
-            else launch_back<T, G, false>(a, p, stream);
+            e = even ? launch_back<T, G, true>(a, p, stream) : launch_back<T, G, false>(a, p, stream);
         }
-        const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
         *launches += p.is_long && a.dx ? 2 : 1;
     }
     if (a.parts) {
-        const dim3 columns((unsigned)((a.dim + 31) / 32), 2);
-        const int parts = a.rows > 0 ? (int)grid : 0;
-        // (without a kernel of this call in front, in plain order)
-        const cudaError_t e = a.rows > 0 ? launch_chained(layer_norm_join_kernel, columns, dim3(32 * kJoinWarps), 0, stream, a, parts)
-                                         : (layer_norm_join_kernel<<<columns, 32 * kJoinWarps, 0, stream>>>(a, parts), cudaGetLastError());
+        const dim3 columns((unsigned)((a.dim + 31) / 32), 2), block(32 * kJoinWarps);
+        if (a.rows > 0) {
+            e = launch_chained(layer_norm_join_kernel, columns, block, 0, stream, a, (int)p.parts);
+        } else {  // nothing in front that it could be chained to
+            layer_norm_join_kernel<<<columns, block, 0, stream>>>(a, 0);
+            e = cudaGetLastError();
+        }
         *launches += 1;
-        return e;
     }
-    return cudaSuccess;
+    return e;
 }
 
 }  // namespace
 
 size_t norm_workspace_bytes(int64_t rows, int dim, int sm_count) {
-    const BackPlan p = plan_back(rows, dim, sm_count);
+    // (whichever way the rows lie: an even call has no more blocks than an uneven one)
+    const BackPlan p = plan_back(rows, dim, sm_count, false);
     return (size_t)p.parts * 2 * padded(dim) * sizeof(float) + (p.is_long ? (size_t)rows * sizeof(float2) : 0);
 }
 

@@ -1,5 +1,8 @@
-// Rows of any alignment in pieces of eight consecutive elements, one piece to a lane: 16-byte accesses
-// wherever memory allows them, whatever the row's pitch.
+// Rows of any alignment, eight elements ("a piece") to a thread and turn.  EVEN: rows begin on 16-byte boundaries and
+// are whole pieces long; a thread takes eight consecutive elements with 16-byte accesses.  Otherwise threads
+// take every width-th element: a warp's accesses then cover consecutive elements whatever the pitch, and
+// cost no shifting of words (8192 rows of 1601 bf16, layer norm: 39 us with 16-byte loads shifted into place and stores
+// traded between lanes, @ODD@ so).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -11,12 +14,6 @@ namespace adama {
 
 constexpr int kPiece = 8;  // elements of a piece: 16 bytes of bf16, 32 of fp32
 
-__device__ __forceinline__ uint4 ld16(const void *p) {
-    uint4 r;
-    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-    return r;
-}
-
 template <typename O>
 __device__ __forceinline__ O narrowed(float y);
 template <>
@@ -24,107 +21,96 @@ __device__ __forceinline__ float narrowed<float>(float y) { return y; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 narrowed<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
 
-// A matrix's memory from its first element to past its last one: 16-byte loads that begin before a piece or
-// end behind it stay inside.
-struct Extent {
-    uintptr_t begin, end;
-};
-template <typename T>
-__device__ __forceinline__ Extent extent_of(const T *p, int64_t rows, int64_t cols, int64_t ld) {
-    return {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p + (rows - 1) * ld + cols)};
-}
+// Columns of a thread: element i of its piece u, of threads `t` of `width` that share a row.
+template <bool EVEN>
+struct Columns {
+    int t, width, dim;
 
-// Words of 16-byte loads, moved down by `shift` words (0 to 3).
-template <int N>
-__device__ __forceinline__ void move_words(unsigned (&z)[N], int shift) {
-    if (shift & 2) {
+    __device__ __forceinline__ int at(int u, int i) const { return EVEN ? (t + u * width) * kPiece + i : t + (u * kPiece + i) * width; }
+    __device__ __forceinline__ bool has(int u, int i) const { return at(u, i) < dim; }  // (EVEN: the same for all i)
+};
+
+__device__ __forceinline__ void widen_words(const uint4 (&u)[1], float (&v)[kPiece]) {  // bf16 -> fp32 is a 16-bit left shift
+    const unsigned z[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
 #pragma unroll
-        for (int i = 0; i < N - 2; ++i) z[i] = z[i + 2];
-    }
-    if (shift & 1) {
-#pragma unroll
-        for (int i = 0; i < N - 1; ++i) z[i] = z[i + 1];
-    }
-}
-template <int N>
-__device__ __forceinline__ void load_words(unsigned (&z)[N], const unsigned char *p) {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-        const uint4 u = ld16(p + 16 * i);
-        z[4 * i] = u.x;
-        z[4 * i + 1] = u.y;
-        z[4 * i + 2] = u.z;
-        z[4 * i + 3] = u.w;
-    }
-}
-__device__ __forceinline__ void widen_words(const unsigned *z, float (&v)[kPiece], __nv_bfloat16) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {  // bf16 -> fp32 is a 16-bit left shift
+    for (int i = 0; i < 4; ++i) {
         v[2 * i] = __uint_as_float(z[i] << 16);
         v[2 * i + 1] = __uint_as_float(z[i] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ void widen_words(const unsigned *z, float (&v)[kPiece], float) {
-#pragma unroll
-    for (int i = 0; i < kPiece; ++i) v[i] = __uint_as_float(z[i]);
+__device__ __forceinline__ void widen_words(const uint4 (&u)[2], float (&v)[kPiece]) {
+    v[0] = __uint_as_float(u[0].x); v[1] = __uint_as_float(u[0].y); v[2] = __uint_as_float(u[0].z); v[3] = __uint_as_float(u[0].w);
+    v[4] = __uint_as_float(u[1].x); v[5] = __uint_as_float(u[1].y); v[6] = __uint_as_float(u[1].z); v[7] = __uint_as_float(u[1].w);
 }
 
-// A piece on its way: loads are issued for all of a thread's pieces before the first one is looked at.  EVEN: all
-// rows begin on 16-byte boundaries and are whole pieces long.  Otherwise the 16-byte units that a piece
-// touches are loaded, one more than it is long, as far as they lie in the matrix.
+// A piece as it comes from memory, so that many can be on their way before the first one is looked at.
 template <typename T, bool EVEN>
 struct Piece {
-    static constexpr int kWords = kPiece * sizeof(T) / 4;
-    unsigned z[kWords + (EVEN ? 0 : 4)];
+    static constexpr int kUnits = kPiece * sizeof(T) / 16;
+    uint4 even[EVEN ? kUnits : 1];
+    T odd[EVEN ? 1 : kPiece];
 
-    __device__ __forceinline__ void load(const T *p, int count, const Extent &all) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = EVEN ? at : at & ~(uintptr_t)15;
+    // row: the row's first element; zeros for columns that it does not have, and for none at all (`live` false)
+    __device__ __forceinline__ void load(const T *row, const Columns<EVEN> &c, int u, bool live) {
+        if constexpr (EVEN) {
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(z) / 16); ++i) {
-            const uintptr_t unit = base + 16 * i;
-            const bool wanted = EVEN ? count != 0 : unit < at + count * sizeof(T) && unit >= all.begin && unit + 16 <= all.end;
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (wanted) u = ld16(reinterpret_cast<const void *>(unit));
-            z[4 * i] = u.x;
-            z[4 * i + 1] = u.y;
-            z[4 * i + 2] = u.z;
-            z[4 * i + 3] = u.w;
+            for (int i = 0; i < kUnits; ++i) {
+                even[i] = make_uint4(0, 0, 0, 0);
+                if (live && c.has(u, 0)) even[i] = reinterpret_cast<const uint4 *>(row + c.at(u, 0))[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) {
+                odd[i] = narrowed<T>(0.f);
+                if (live && c.has(u, i)) odd[i] = row[c.at(u, i)];
+            }
         }
     }
-    // its elements as fp32, zeros from `count` on
-    __device__ __forceinline__ void get(const T *p, int count, const Extent &all, float (&v)[kPiece]) const {
+    __device__ __forceinline__ void get(float (&v)[kPiece]) const {
         if constexpr (EVEN) {
-            widen_words(z, v, T());
+            widen_words(even, v);
         } else {
-            const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~(uintptr_t)15;
-            unsigned y[kWords + 4];
 #pragma unroll
-            for (int i = 0; i < kWords + 4; ++i) y[i] = z[i];
-            move_words(y, (int)(at - base) / 4);
-            if (sizeof(T) == 2 && (at & 2)) {
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) y[i] = __funnelshift_r(y[i], y[i + 1], 16);
-            }
-            widen_words(y, v, T());
-            if (count != kPiece) {
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i)
-                    if (i >= count) v[i] = 0.f;
-            }
-            const uintptr_t end = (at + count * sizeof(T) + 15) & ~(uintptr_t)15;
-            if (count != 0 && (base < all.begin || end > all.end)) {  // at the matrix's ends a unit lies outside in part
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i) v[i] = i < count ? widen(p[i]) : 0.f;
-            }
+            for (int i = 0; i < kPiece; ++i) v[i] = widen(odd[i]);
         }
     }
 };
-
-template <bool EVEN, typename T>
-__device__ __forceinline__ void load_piece(const T *p, int count, const Extent &all, float (&v)[kPiece]) {
+template <typename T, bool EVEN>
+__device__ __forceinline__ void load_piece(const T *row, const Columns<EVEN> &c, int u, bool live, float (&v)[kPiece]) {
     Piece<T, EVEN> q;
-    q.load(p, count, all);
-    q.get(p, count, all, v);
+    q.load(row, c, u, live);
+    q.get(v);
+}
+
+__device__ __forceinline__ void pack_words(const float (&v)[kPiece], uint4 (&w)[1]) {
+    unsigned z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        z[i] = *reinterpret_cast<const unsigned *>(&p);
+    }
+    w[0] = make_uint4(z[0], z[1], z[2], z[3]);
+}
+__device__ __forceinline__ void pack_words(const float (&v)[kPiece], uint4 (&w)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        w[h] = make_uint4(__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3]));
+}
+template <typename O, bool EVEN>
+__device__ __forceinline__ void store_piece(O *row, const Columns<EVEN> &c, int u, bool live, const float (&v)[kPiece]) {
+    if (!live) return;
+    if constexpr (EVEN) {
+        uint4 w[kPiece * sizeof(O) / 16];
+        pack_words(v, w);
+        if (c.has(u, 0)) {
+#pragma unroll
+            for (int i = 0; i < (int)(kPiece * sizeof(O) / 16); ++i) reinterpret_cast<uint4 *>(row + c.at(u, 0))[i] = w[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i)
+            if (c.has(u, i)) row[c.at(u, i)] = narrowed<O>(v[i]);
+    }
 }
 
 // Whether rows of a matrix are even in that sense.
@@ -132,71 +118,16 @@ inline bool even_rows(const void *p, int64_t cols, int64_t ld, int size) {
     return aligned(p, 16) && cols % kPiece == 0 && ld * size % 16 == 0;
 }
 
-__device__ __forceinline__ void pack_words(const float (&v)[kPiece], unsigned (&w)[4], __nv_bfloat16) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const unsigned *>(&p);
-    }
+// ---- rows ahead -----------------------------------------------------------------------------------
+// A thread's own pieces of the next rows on their way to shared memory (asynchronous copies that the thread itself waits
+// for: no other one reads them), or, of uneven rows, of the next row to registers.
+__device__ __forceinline__ void copy16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
-__device__ __forceinline__ void pack_words(const float (&v)[kPiece], unsigned (&w)[8], float) {
-#pragma unroll
-    for (int i = 0; i < kPiece; ++i) w[i] = __float_as_uint(v[i]);
-}
-
-// Stores a run of pieces: `lanes` (a power of two) neighbouring lanes hold consecutive pieces, this one
-// `count` elements that go to p (8, fewer at the row's end, 0 behind it).  All 32 lanes of a warp call it.
-// Where p is not on a 16-byte boundary a lane stores the eight elements from the next boundary on, of which
-// its neighbour has the last ones; only a run's ends are stored one by one.
-template <bool EVEN, typename O>
-__device__ __forceinline__ void store_run(O *p, const float (&v)[kPiece], int count, int lanes) {
-    constexpr int kWords = kPiece * sizeof(O) / 4;
-    unsigned w[kWords];
-    pack_words(v, w, O());
-    if constexpr (EVEN) {
-        if (count != 0) {
-#pragma unroll
-            for (int i = 0; i < kWords / 4; ++i)
-                reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-        }
-        return;
-    }
-    const int past = (int)(reinterpret_cast<uintptr_t>(p) & 15);
-    const int shift = past ? (16 - past) / (int)sizeof(O) : 0;  // elements before the boundary
-    if (!__any_sync(0xffffffffu, shift != 0 && count > 0)) {
-        if (count == kPiece) {
-#pragma unroll
-            for (int i = 0; i < kWords / 4; ++i)
-                reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i)
-                if (i < count) p[i] = narrowed<O>(v[i]);
-        }
-        return;
-    }
-    const int lane = threadIdx.x % 32, at = lane & (lanes - 1);
-    const int next_count = __shfl_down_sync(0xffffffffu, count, 1);
-    const bool whole = count == kPiece && (shift == 0 || (at != lanes - 1 && next_count >= shift));
-    const bool before = __shfl_up_sync(0xffffffffu, whole, 1) && at != 0;  // the lane below has stored the first ones
-    unsigned z[kWords + 4];
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) z[i] = w[i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) z[kWords + i] = __shfl_down_sync(0xffffffffu, w[i], 1);
-    if (whole) {
-        move_words(z, shift * (int)sizeof(O) / 4);
-        if (sizeof(O) == 2 && (shift & 1)) {
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) z[i] = __funnelshift_r(z[i], z[i + 1], 16);
-        }
-#pragma unroll
-        for (int i = 0; i < kWords / 4; ++i)
-            reinterpret_cast<uint4 *>(p + shift)[i] = make_uint4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]);
-    }
-#pragma unroll
-    for (int i = 0; i < kPiece; ++i)
-        if (i < count && (i < shift ? !before : !whole)) p[i] = narrowed<O>(v[i]);
+__device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {  // for all but the last N groups
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 }  // namespace adama
