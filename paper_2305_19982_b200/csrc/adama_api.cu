@@ -931,6 +931,7 @@ adama_status adama_layer_norm(adama_ctx *ctx, const adama_layer_norm_args *p, vo
     a.weight = p->weight;
     a.bias = p->bias;
     a.eps = (float)p->eps;
+    a.inv_dim = (float)(1.0 / (double)p->dim);
     a.mean = p->mean;
     a.rstd = p->rstd;
     cudaError_t e = adama::launch_layer_norm(a, ctx->sm_count, static_cast<cudaStream_t>(cuda_stream));

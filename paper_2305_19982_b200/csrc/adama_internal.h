@@ -184,7 +184,7 @@ struct NormArgs {
     int64_t rows, ld_x, ld_y;
     int dim;
     const float *weight, *bias;  // bias may be null
-    float eps;
+    float eps, inv_dim;
     float *mean, *rstd;  // may be null
 };
 cudaError_t launch_layer_norm(const NormArgs &a, int sm_count, cudaStream_t stream);

@@ -33,7 +33,7 @@ embedding_kernel(const EmbeddingArgs a, int groups) {
     if (token >= a.tokens) return;
     const int64_t id = a.ids[token];
     const bool inside = id >= 0 && id < a.vocab;
-    const Columns<EVEN> c = {lane, 32, a.dim - first};
+    const Columns<EVEN, 32> c = {lane, 32, a.dim - first};
     const T *row = static_cast<const T *>(a.table) + (inside ? id * a.ld_table : 0) + first;
     O *out = static_cast<O *>(a.out) + token * a.ld_out + first;
     Piece<T, EVEN> raw[kLookupPieces];
@@ -42,10 +42,9 @@ embedding_kernel(const EmbeddingArgs a, int groups) {
     const float other = id < 0 ? 0.f : NAN;
 #pragma unroll
     for (int u = 0; u < kLookupPieces; ++u) {
-        float v[kPiece];
-        raw[u].get(v);
+        Vec v = raw[u].get();
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) v[i] = inside ? v[i] * a.scale : other;
+        for (int i = 0; i < kPiece / 2; ++i) v.p[i] = inside ? mul2(v.p[i], pair(a.scale, a.scale)) : pair(other, other);
         store_piece(out, c, u, true, v);
     }
     if (!inside && id >= 0 && first == 0 && lane == 0) record_bad_target(a.status, token);
@@ -209,7 +208,7 @@ struct Target {
     Piece<O, EVEN> m;      // of kAdd: the table; of kFold: the moments
     Piece<float, EVEN> v;
 
-    __device__ __forceinline__ void load(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN> &c, bool wanted) {
+    __device__ __forceinline__ void load(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN, 32> &c, bool wanted) {
         const int64_t at = (int64_t)key * a.ld_grad + first;
         if constexpr (MODE == kAdd) m.load(static_cast<const O *>(a.grad) + (wanted ? at : 0), c, 0, wanted);
         if constexpr (MODE == kFold) {
@@ -217,29 +216,35 @@ struct Target {
             v.load(a.v + (wanted ? at : 0), c, 0, wanted);
         }
     }
-    __device__ __forceinline__ void finish(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN> &c,
-                                           const float (&sum)[kPiece]) const {
+    __device__ __forceinline__ void finish(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN, 32> &c,
+                                           const Vec &sum) const {
         const int64_t at = (int64_t)key * a.ld_grad + first;
-        float g[kPiece], x[kPiece], y[kPiece];
+        Vec g;
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) g[i] = sum[i] * a.scale;
+        for (int i = 0; i < kPiece / 2; ++i) g.p[i] = mul2(sum.p[i], pair(a.scale, a.scale));
         if constexpr (MODE == kFold) {
-            m.get(x);
-            v.get(y);
+            Vec x = m.get(), y = v.get();
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) fold1(g[i], x[i], y[i], a.fold.a, a.fold.b);
+            for (int i = 0; i < kPiece / 2; ++i) {
+                x.p[i] = fma2(pair(a.fold.a, a.fold.a), g.p[i], x.p[i]);  // as fold1
+                y.p[i] = fma2(mul2(pair(a.fold.b, a.fold.b), g.p[i]), g.p[i], y.p[i]);
+            }
             store_piece(a.m + at, c, 0, true, x);
             store_piece(a.v + at, c, 0, true, y);
         } else {
             if constexpr (MODE == kAdd) {
-                m.get(x);
+                const Vec x = m.get();
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) g[i] += x[i];
+                for (int i = 0; i < kPiece / 2; ++i) g.p[i] = add2(g.p[i], x.p[i]);
             }
             store_piece(static_cast<O *>(a.grad) + at, c, 0, true, g);
         }
     }
 };
+__device__ __forceinline__ void add_to(Vec &sum, const Vec &x) {
+#pragma unroll
+    for (int i = 0; i < kPiece / 2; ++i) sum.p[i] = add2(sum.p[i], x.p[i]);
+}
 
 // Part `slot` of chunk b: 0 continues the chunk before, 1 begins in b and goes on behind it.
 __device__ __forceinline__ float *part_of(const EmbeddingGradArgs &a, int64_t b, int slot) {
@@ -286,7 +291,7 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     const int64_t start = b * chunk;
     if (start >= a.tokens) return;
     const int tile = (int)(task - b * tiles) * kTile;
-    const Columns<EVEN> c = {lane, 32, a.dim - tile};
+    const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
     const int n = (int)(a.tokens - start < chunk ? a.tokens - start : chunk);
     const unsigned none = 0xffffffffu, out = (unsigned)a.vocab;
     const unsigned key = lane < n ? a.keys[start + lane] : none, token = lane < n ? a.order[start + lane] : 0;
@@ -298,7 +303,7 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     const int live = __popc(__ballot_sync(0xffffffffu, lane < n && key != out));  // the others come last
     bool open = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the first run continues the chunk before
     const G *dy = static_cast<const G *>(a.dy) + tile;
-    float sum[kPiece] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    Vec sum = zeros();
     for (int j = 0; j < live; j += kBatch) {
         Piece<G, EVEN> raw[kBatch];
         Target<O, MODE, EVEN> target[kBatch];
@@ -313,16 +318,12 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
         }
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
-            float x[kPiece];
-            raw[q].get(x);
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i) sum[i] += x[i];
+            add_to(sum, raw[q].get());
             if (j + q < live && (ends >> (j + q) & 1)) {
                 if (open) store_piece(part_of(a, b, 0) + tile, c, 0, true, sum);
                 else target[q].finish(a, k[q], tile, c, sum);
                 open = false;
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i) sum[i] = 0.f;
+                sum = zeros();
             }
         }
     }
@@ -336,7 +337,7 @@ constexpr int kJoinShort = 16;  // parts up to which a warp adds them alone
 template <typename O, int MODE, bool EVEN>
 __global__ void __launch_bounds__(32 * kJoinWarps)
 embedding_join_kernel(const EmbeddingGradArgs a, int chunk, int tiles) {
-    __shared__ float slots[kJoinWarps][kTile];
+    __shared__ Pair slots[kJoinWarps][kTile / 2];
     wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t b = blockIdx.x, start = b * chunk, end = start + chunk;
@@ -358,44 +359,32 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk, int tiles) {
     if (parts <= kJoinShort) {
         if (first_tile + warp >= tiles) return;
         const int tile = (first_tile + warp) * kTile;
-        const Columns<EVEN> c = {lane, 32, a.dim - tile};
+        const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
         Target<O, MODE, EVEN> target;
         target.load(a, key, tile, c, true);
-        float sum[kPiece];
-        load_piece<float>(part_of(a, b, 1) + tile, c, 0, true, sum);
+        Vec sum = load_piece<float>(part_of(a, b, 1) + tile, c, 0, true);
 #pragma unroll 4
-        for (int64_t i = b + 1; i <= last; ++i) {
-            float x[kPiece];
-            load_piece<float>(part_of(a, i, 0) + tile, c, 0, true, x);
-#pragma unroll
-            for (int q = 0; q < kPiece; ++q) sum[q] += x[q];
-        }
+        for (int64_t i = b + 1; i <= last; ++i) add_to(sum, load_piece<float>(part_of(a, i, 0) + tile, c, 0, true));
         target.finish(a, key, tile, c, sum);
         return;
     }
     // long: the warps share the parts of a tile, one tile after the other
     for (int i = first_tile; i < tiles && i < first_tile + kJoinWarps; ++i) {
         const int tile = i * kTile;
-        const Columns<EVEN> c = {lane, 32, a.dim - tile};
+        const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
         const int64_t from = b + 1 + parts * warp / kJoinWarps, to = b + 1 + parts * (warp + 1) / kJoinWarps;
-        float sum[kPiece];
-        load_piece<float>(part_of(a, b, 1) + tile, c, 0, warp == 0, sum);
+        Vec sum = load_piece<float>(part_of(a, b, 1) + tile, c, 0, warp == 0);
 #pragma unroll 4
-        for (int64_t j = from; j < to; ++j) {
-            float x[kPiece];
-            load_piece<float>(part_of(a, j, 0) + tile, c, 0, true, x);
+        for (int64_t j = from; j < to; ++j) add_to(sum, load_piece<float>(part_of(a, j, 0) + tile, c, 0, true));
 #pragma unroll
-            for (int q = 0; q < kPiece; ++q) sum[q] += x[q];
-        }
-#pragma unroll
-        for (int q = 0; q < kPiece; ++q) slots[warp][q * 32 + lane] = sum[q];
+        for (int q = 0; q < kPiece / 2; ++q) slots[warp][q * 32 + lane] = sum.p[q];
         __syncthreads();
         if (warp == 0) {
             Target<O, MODE, EVEN> target;
             target.load(a, key, tile, c, true);
             for (int w = 1; w < kJoinWarps; ++w)
 #pragma unroll
-                for (int q = 0; q < kPiece; ++q) sum[q] += slots[w][q * 32 + lane];
+                for (int q = 0; q < kPiece / 2; ++q) sum.p[q] = add2(sum.p[q], slots[w][q * 32 + lane]);
             target.finish(a, key, tile, c, sum);
         }
         __syncthreads();

@@ -24,12 +24,6 @@ __device__ __forceinline__ float lanes_sum(float x, int lanes) {
     for (int o = lanes / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-__device__ __forceinline__ float pair_sum(Pair p) {
-    float a, b;
-    split(p, a, b);
-    return a + b;
-}
-
 // Warps of a block that share rows: `warps` to a row, several such groups side by side.
 struct Group {
     int warps, index, count, t;
@@ -48,40 +42,47 @@ struct Group {
         if (threadIdx.x % 32 == 0) slots[threadIdx.x / 32] = x;
         sync();
         x = 0.f;
+#pragma unroll 4
         for (int i = 0; i < warps; ++i) x += slots[index * warps + i];
         return x;
     }
 };
 
-constexpr int kGroupWarps = 16;  // of a block, at most
-constexpr int kAhead = 3;        // rows of a thread on their way, of even ones
+// s/n for a whole number n, without a division's length: a product, and what it lacks.  (The product alone would
+// move the mean of equal values.)
+__device__ __forceinline__ float share(float s, float n, float inv_n) {
+    const float q = s * inv_n, lack = fmaf(-q, n, s);
+    return lack == lack ? fmaf(lack, inv_n, q) : q;  // (an infinite sum stays one)
+}
 
-// A row's elements as fp32, and its distances from the mean.
-template <bool EVEN>
-__device__ __forceinline__ float sum_of(const float (&v)[kPiece]) {
-    Pair s = 0;
-#pragma unroll
-    for (int i = 0; i < kPiece; i += 2) s = add2(s, pair(v[i], v[i + 1]));
-    return pair_sum(s);
+constexpr int kGroupWarps = 16;  // of a block, at most
+
+__device__ __forceinline__ Vec sum_of(const Vec &a, const Vec &b) {
+    return {{add2(a.p[0], b.p[0]), add2(a.p[1], b.p[1]), add2(a.p[2], b.p[2]), add2(a.p[3], b.p[3])}};
 }
-template <bool EVEN>
-__device__ __forceinline__ float centre(float (&v)[kPiece], const Columns<EVEN> &c, int u, float mean) {
+__device__ __forceinline__ Pair sum_of(const Vec &v) { return add2(add2(v.p[0], v.p[1]), add2(v.p[2], v.p[3])); }
+// v becomes its distance from the mean; returns that squared, summed.  Columns that the row does not have lie at none.
+template <bool EVEN, int W>
+__device__ __forceinline__ Pair centre(Vec &v, const Columns<EVEN, W> &c, int u, float mean) {
+    if constexpr (!EVEN) {
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i)
-        if (!c.has(u, i)) v[i] = mean;  // columns that the row does not have lie at no distance
-    Pair s = 0;
-#pragma unroll
-    for (int i = 0; i < kPiece; i += 2) {
-        const Pair d = add2(pair(v[i], v[i + 1]), pair(-mean, -mean));
-        s = fma2(d, d, s);
-        split(d, v[i], v[i + 1]);
+        for (int i = 0; i < kPiece / 2; ++i) {
+            float a, b;
+            split(v.p[i], a, b);
+            v.p[i] = pair(c.has(u, 2 * i) ? a : mean, c.has(u, 2 * i + 1) ? b : mean);
+        }
     }
-    return pair_sum(s);
-}
-__device__ __forceinline__ void scale_shift(float (&v)[kPiece], float rstd, const float (&w)[kPiece], const float (&b)[kPiece]) {
+    Pair s = 0;
 #pragma unroll
-    for (int i = 0; i < kPiece; i += 2)
-        split(fma2(mul2(pair(v[i], v[i + 1]), pair(rstd, rstd)), pair(w[i], w[i + 1]), pair(b[i], b[i + 1])), v[i], v[i + 1]);
+    for (int i = 0; i < kPiece / 2; ++i) {
+        v.p[i] = add2(v.p[i], pair(-mean, -mean));
+        s = fma2(v.p[i], v.p[i], s);
+    }
+    return EVEN && !c.has(u, 0) ? 0 : s;
+}
+__device__ __forceinline__ void scale_shift(Vec &v, float rstd, const Vec &w, const Vec &b) {
+#pragma unroll
+    for (int i = 0; i < kPiece / 2; ++i) v.p[i] = fma2(mul2(v.p[i], pair(rstd, rstd)), w.p[i], b.p[i]);
 }
 
 // ---- forward -------------------------------------------------------------------------------------
@@ -95,92 +96,97 @@ layer_norm_short_kernel(const NormArgs a, int lanes) {
     const Columns<EVEN> c = {(int)threadIdx.x % lanes, lanes, a.dim};
     const int64_t row = (int64_t)blockIdx.x * (kShortThreads / lanes) + threadIdx.x / lanes;
     const bool live = row < a.rows;
-    float v[kPiece], w[kPiece], b[kPiece];
     Piece<T, EVEN> raw;
     Piece<float, EVEN> raw_w, raw_b;
     raw.load(static_cast<const T *>(a.x) + (live ? row : 0) * a.ld_x, c, 0, live);
     raw_w.load(a.weight, c, 0, live);
     raw_b.load(a.bias, c, 0, live && a.bias);
-    raw.get(v);
-    const float mean = lanes_sum(sum_of<EVEN>(v), lanes) / (float)a.dim;  // (a product with 1/D would move the mean of equal values)
-    const float rstd = 1.f / sqrtf(lanes_sum(centre(v, c, 0, mean), lanes) / (float)a.dim + a.eps);
+    Vec v = raw.get();
+    const float n = (float)a.dim, mean = share(lanes_sum(pair_sum(sum_of(v)), lanes), n, a.inv_dim);
+    const float rstd = __frsqrt_rn(share(lanes_sum(pair_sum(centre(v, c, 0, mean)), lanes), n, a.inv_dim) + a.eps);
     if (c.t == 0 && live) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
     }
-    raw_w.get(w);
-    raw_b.get(b);
-    scale_shift(v, rstd, w, b);
+    scale_shift(v, rstd, raw_w.get(), raw_b.get());
     store_piece(static_cast<O *>(a.y) + (live ? row : 0) * a.ld_y, c, 0, live, v);
 }
 
-// Longer rows: a group of warps walks rows, U pieces to a thread, weight and bias in registers, the next rows on their
-// way.  (One row to a block that ends with it: @FWD@.)
-template <typename T, typename O, int U, bool EVEN>
+// Longer rows: a group of warps walks rows, U pieces to a thread; weight and bias lie in shared memory, as do the next
+// rows of a thread, which are on their way while it works on one.  A row costs a warp some 200 instructions beside those of
+// its elements, and exchanges between lanes and warps wait for each other: so few warps share a row, with many pieces
+// to a thread, where there are rows enough (4096 x 1600 fp32 to bf16: four warps to a row 20 us, one @FWD@).
+constexpr int kAhead = 2;  // rows of a thread on their way, of even ones
+
+template <typename T, typename O, int U, bool EVEN, int WARPS>
 __global__ void __launch_bounds__(32 * kGroupWarps)
 layer_norm_kernel(const NormArgs a, int warps) {
-    extern __shared__ uint4 ahead[];  // [rows ahead][U][units of a piece][threads]
+    extern __shared__ uint4 shared[];  // even: [pieces][2][threads of a row] of weight, of bias, then [rows ahead][U][units][threads]
     __shared__ float slots[2][kGroupWarps];
     constexpr int kUnits = Piece<T, true>::kUnits;
-    const Group group(warps);
-    const Columns<EVEN> c = {group.t, 32 * warps, a.dim};
+    const Group group(WARPS ? WARPS : warps);
+    const Columns<EVEN, 32 * WARPS> c = {group.t, 32 * warps, a.dim};
     const T *x0 = static_cast<const T *>(a.x);
     const int64_t step = (int64_t)gridDim.x * group.count;
     int64_t row = (int64_t)blockIdx.x * group.count + group.index;
+    uint4 *const params = shared, *const ahead = shared + 4 * U * c.width();
+    float *const odd_params = reinterpret_cast<float *>(shared);  // uneven: weight, bias
     const auto slot = [&](int stage, int u, int i) { return ahead + ((stage * U + u) * kUnits + i) * blockDim.x + threadIdx.x; };
     const auto send_for = [&](int64_t r, int stage) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r < a.rows && c.has(u, 0)) {
-#pragma unroll
-                for (int i = 0; i < kUnits; ++i)
-                    copy16((uint32_t)__cvta_generic_to_shared(slot(stage, u, i)), reinterpret_cast<const uint4 *>(x0 + r * a.ld_x + c.at(u, 0)) + i);
-            }
-        copies_end_group();
-    };
-    Piece<T, EVEN> next[U];
-    if constexpr (EVEN) {
-        for (int i = 0; i < kAhead; ++i) send_for(row + i * step, i);
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u) next[u].load(x0 + (row < a.rows ? row : 0) * a.ld_x, c, u, row < a.rows);
-    }
-    float w[U][kPiece], b[U][kPiece];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        load_piece(a.weight, c, u, true, w[u]);
-        load_piece(a.bias, c, u, a.bias != nullptr, b[u]);
-    }
-    for (int stage = 0; row < a.rows; row += step, stage = stage + 1 == kAhead ? 0 : stage + 1) {
-        float v[U][kPiece], s = 0.f;
-        if constexpr (EVEN) {
-            copies_wait<kAhead - 1>();
+        if (r < a.rows) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(x0 + r * a.ld_x) + c.t * kUnits;
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (c.has(u, 0)) {
 #pragma unroll
-                    for (int i = 0; i < kUnits; ++i) next[u].even[i] = *slot(stage, u, i);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kUnits; ++i) next[u].even[i] = make_uint4(0, 0, 0, 0);
+                    for (int i = 0; i < kUnits; ++i)
+                        copy16((uint32_t)__cvta_generic_to_shared(slot(stage, u, i)), from + u * c.width() * kUnits + i);
                 }
+        }
+        copies_end_group();
+    };
+    if constexpr (EVEN) {
+        for (int i = 0; i < kAhead; ++i) send_for(row + i * step, i);
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+        for (int i = threadIdx.x; i < 2 * U * c.width(); i += blockDim.x) {
+            const int piece = i / 2, at = ((piece / c.width()) * 2 + i % 2) * c.width() + piece % c.width();
+            const bool has = piece * kPiece < a.dim;
+            params[at] = has ? reinterpret_cast<const uint4 *>(a.weight)[i] : zero;
+            params[2 * U * c.width() + at] = has && a.bias ? reinterpret_cast<const uint4 *>(a.bias)[i] : zero;
+        }
+    } else {
+        for (int i = threadIdx.x; i < a.dim; i += blockDim.x) {
+            odd_params[i] = a.weight[i];
+            odd_params[a.dim + i] = a.bias ? a.bias[i] : 0.f;
+        }
+    }
+    __syncthreads();
+    const float n = (float)a.dim;
+    for (int stage = 0; row < a.rows; row += step, stage = stage + 1 == kAhead ? 0 : stage + 1) {
+        Vec v[U];
+        Pair s = 0;
+        Piece<T, EVEN> raw[U];
+        if constexpr (EVEN) {
+            copies_wait<kAhead - 1>();
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i) raw[u].even[i] = c.has(u, 0) ? *slot(stage, u, i) : make_uint4(0, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u].load(x0 + row * a.ld_x, c, u, true);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            next[u].get(v[u]);
-            s += sum_of<EVEN>(v[u]);
+            v[u] = raw[u].get();
+            s = add2(s, sum_of(v[u]));
         }
-        if constexpr (!EVEN) {
-            const int64_t r = row + step;
-#pragma unroll
-            for (int u = 0; u < U; ++u) next[u].load(x0 + (r < a.rows ? r : 0) * a.ld_x, c, u, r < a.rows);
-        }
-        const float mean = group.sum(s, slots[0]) / (float)a.dim;
+        const float mean = share(group.sum(pair_sum(s), slots[0]), n, a.inv_dim);
         if constexpr (EVEN) send_for(row + kAhead * step, stage);  // what was there has been summed up
-        s = 0.f;
+        s = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) s += centre(v[u], c, u, mean);
-        const float rstd = 1.f / sqrtf(group.sum(s, slots[1]) / (float)a.dim + a.eps);
+        for (int u = 0; u < U; ++u) s = add2(s, centre(v[u], c, u, mean));
+        const float rstd = __frsqrt_rn(share(group.sum(pair_sum(s), slots[1]), n, a.inv_dim) + a.eps);
         if (c.t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
@@ -188,7 +194,20 @@ layer_norm_kernel(const NormArgs a, int warps) {
         O *y = static_cast<O *>(a.y) + row * a.ld_y;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            scale_shift(v[u], rstd, w[u], b[u]);
+            Vec w, b;
+            if constexpr (EVEN) {
+                uint4 q[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) q[i] = params[(u * 2 + i) * c.width() + c.t];
+                w = widened(q);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) q[i] = params[(2 * U + u * 2 + i) * c.width() + c.t];
+                b = widened(q);
+            } else {
+                w = load_piece(odd_params, c, u, true);
+                b = load_piece(odd_params + a.dim, c, u, true);
+            }
+            scale_shift(v[u], rstd, w, b);
             store_piece(y, c, u, true, v[u]);
         }
     }
@@ -206,13 +225,13 @@ layer_norm_long_kernel(const NormArgs a) {
     const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
     float s = 0.f;
     for (int c = threadIdx.x; c < a.dim; c += kLongThreads) s += widen(x[c]);
-    const float mean = group.sum(s, slots[0]) / (float)a.dim;
+    const float n = (float)a.dim, mean = share(group.sum(s, slots[0]), n, a.inv_dim);
     s = 0.f;
     for (int c = threadIdx.x; c < a.dim; c += kLongThreads) {
         const float d = widen(x[c]) - mean;
         s = fmaf(d, d, s);
     }
-    const float rstd = 1.f / sqrtf(group.sum(s, slots[1]) / (float)a.dim + a.eps);
+    const float rstd = __frsqrt_rn(share(group.sum(s, slots[1]), n, a.inv_dim) + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -229,44 +248,31 @@ __host__ __device__ inline int64_t padded(int dim) { return ((int64_t)dim + kPie
 
 // Sums over rows, of a thread's columns.
 struct PieceSums {
-    Pair dw[kPiece / 2], db[kPiece / 2];
+    Vec dw, db;
 };
-__device__ __forceinline__ Pair xhat_of(float x0, float x1, float mean, float rstd) {
-    return mul2(add2(pair(x0, x1), pair(-mean, -mean)), pair(rstd, rstd));
-}
+__device__ __forceinline__ Pair xhat_of(Pair x, float mean, float rstd) { return mul2(add2(x, pair(-mean, -mean)), pair(rstd, rstd)); }
 // A piece's part in its columns' sums and in its row's two.  Columns that the row does not have are 0 in dy and add nothing.
-__device__ __forceinline__ void take_piece(const float (&x)[kPiece], const float (&dy)[kPiece], const float (&w)[kPiece], float mean, float rstd,
-                                           PieceSums &sums, Pair &s1, Pair &s2) {
+__device__ __forceinline__ void take_piece(const Vec &x, const Vec &dy, const Vec &w, float mean, float rstd, PieceSums &sums, Pair &s1, Pair &s2) {
 #pragma unroll
     for (int i = 0; i < kPiece / 2; ++i) {
-        const Pair d = pair(dy[2 * i], dy[2 * i + 1]), xhat = xhat_of(x[2 * i], x[2 * i + 1], mean, rstd);
-        sums.db[i] = add2(sums.db[i], d);
-        sums.dw[i] = fma2(d, xhat, sums.dw[i]);
-        const Pair g = mul2(d, pair(w[2 * i], w[2 * i + 1]));
+        const Pair xhat = xhat_of(x.p[i], mean, rstd);
+        sums.db.p[i] = add2(sums.db.p[i], dy.p[i]);
+        sums.dw.p[i] = fma2(dy.p[i], xhat, sums.dw.p[i]);
+        const Pair g = mul2(dy.p[i], w.p[i]);
         s1 = add2(s1, g);
         s2 = fma2(g, xhat, s2);
     }
 }
 // dx of a piece; s1, s2: the row's sums divided by its length.  (Computed anew rather than kept: registers are dearer.)
-__device__ __forceinline__ void piece_dx(const float (&x)[kPiece], const float (&dy)[kPiece], const float (&w)[kPiece], float mean, float rstd,
-                                         float s1, float s2, float (&dx)[kPiece]) {
+__device__ __forceinline__ Vec piece_dx(const Vec &x, const Vec &dy, const Vec &w, float mean, float rstd, float s1, float s2) {
+    Vec dx;
 #pragma unroll
     for (int i = 0; i < kPiece / 2; ++i) {
-        const Pair xhat = xhat_of(x[2 * i], x[2 * i + 1], mean, rstd);
-        const Pair g = fma2(pair(dy[2 * i], dy[2 * i + 1]), pair(w[2 * i], w[2 * i + 1]), pair(-s1, -s1));
-        split(mul2(fma2(xhat, pair(-s2, -s2), g), pair(rstd, rstd)), dx[2 * i], dx[2 * i + 1]);
+        const Pair xhat = xhat_of(x.p[i], mean, rstd);
+        const Pair g = fma2(dy.p[i], w.p[i], pair(-s1, -s1));
+        dx.p[i] = mul2(fma2(xhat, pair(-s2, -s2), g), pair(rstd, rstd));
     }
-}
-// A piece's sums to a vector of all columns, or in addition to what is there.
-template <bool EVEN>
-__device__ __forceinline__ void put_sums(float *to, const Columns<EVEN> &c, int u, const Pair (&v)[kPiece / 2], bool add) {
-#pragma unroll
-    for (int i = 0; i < kPiece / 2; ++i) {
-        float p, q;
-        split(v[i], p, q);
-        if (c.has(u, 2 * i)) to[c.at(u, 2 * i)] = add ? to[c.at(u, 2 * i)] + p : p;
-        if (c.has(u, 2 * i + 1)) to[c.at(u, 2 * i + 1)] = add ? to[c.at(u, 2 * i + 1)] + q : q;
-    }
+    return dx;
 }
 
 // Rows of up to 256 elements: `lanes` lanes to a row, one piece to a lane.
@@ -275,14 +281,13 @@ constexpr int kLanesThreads = 256;
 template <typename T, typename G, bool EVEN>
 __global__ void __launch_bounds__(kLanesThreads)
 layer_norm_backward_short_kernel(const NormBackArgs a, int lanes) {
-    __shared__ float total[2 * 32 * kPiece];
+    __shared__ alignas(16) float total[2 * 32 * kPiece];
     let_next_start();
     const Columns<EVEN> c = {(int)threadIdx.x % lanes, lanes, a.dim};
     const int groups = kLanesThreads / lanes;
     const T *x0 = static_cast<const T *>(a.x);
     const G *dy0 = static_cast<const G *>(a.dy);
-    float w[kPiece];
-    load_piece(a.weight, c, 0, true, w);
+    const Vec w = load_piece(a.weight, c, 0, true);
     PieceSums sums = {};
     const int64_t step = (int64_t)gridDim.x * groups;
     Piece<T, EVEN> next_x;
@@ -299,32 +304,29 @@ layer_norm_backward_short_kernel(const NormBackArgs a, int lanes) {
     // all lanes of a warp go round together, the last rows of some being none
     for (int64_t base = (int64_t)blockIdx.x * groups; base < a.rows; base += step) {
         const int64_t row = base + threadIdx.x / lanes;
-        float x[kPiece], dy[kPiece];
-        next_x.get(x);
-        next_dy.get(dy);
+        const Vec x = next_x.get(), dy = next_dy.get();
         const float mean = next_mean, rstd = next_rstd;
         send_for(row + step);
         Pair p1 = 0, p2 = 0;
         take_piece(x, dy, w, mean, rstd, sums, p1, p2);
         if (!a.dx) continue;
         const float s1 = lanes_sum(pair_sum(p1), lanes) * a.inv_dim, s2 = lanes_sum(pair_sum(p2), lanes) * a.inv_dim;
-        float dx[kPiece];
-        piece_dx(x, dy, w, mean, rstd, s1, s2, dx);
         const bool live = row < a.rows;
-        store_piece(static_cast<T *>(a.dx) + (live ? row * a.ld_dx : 0), c, 0, live, dx);
+        store_piece(static_cast<T *>(a.dx) + (live ? row * a.ld_dx : 0), c, 0, live, piece_dx(x, dy, w, mean, rstd, s1, s2));
     }
     if (!a.parts) return;
     // the rows of a warp by exchange, the warps one after the other in shared memory
 #pragma unroll
     for (int i = 0; i < kPiece / 2; ++i)
         for (int o = lanes; o < 32; o <<= 1) {
-            sums.dw[i] = add2(sums.dw[i], __shfl_xor_sync(0xffffffffu, sums.dw[i], o));
-            sums.db[i] = add2(sums.db[i], __shfl_xor_sync(0xffffffffu, sums.db[i], o));
+            sums.dw.p[i] = add2(sums.dw.p[i], __shfl_xor_sync(0xffffffffu, sums.dw.p[i], o));
+            sums.db.p[i] = add2(sums.db.p[i], __shfl_xor_sync(0xffffffffu, sums.db.p[i], o));
         }
     for (int warp = 0; warp < kLanesThreads / 32; ++warp) {
         if ((int)threadIdx.x / 32 == warp && (int)threadIdx.x % 32 < lanes) {
-            put_sums(total, c, 0, sums.dw, warp > 0);
-            put_sums(total + 32 * kPiece, c, 0, sums.db, warp > 0);
+            const Vec none = zeros(), dw = warp > 0 ? load_piece(total, c, 0, true) : none, db = warp > 0 ? load_piece(total + 32 * kPiece, c, 0, true) : none;
+            store_piece(total, c, 0, true, sum_of(sums.dw, dw));
+            store_piece(total + 32 * kPiece, c, 0, true, sum_of(sums.db, db));
         }
         __syncthreads();
     }
@@ -336,121 +338,156 @@ layer_norm_backward_short_kernel(const NormBackArgs a, int lanes) {
     }
 }
 
-// Longer rows: a group of warps walks rows, U pieces to a thread, the next rows on their way (to registers, of uneven rows,
-// with one piece to a thread).  The groups of a block join their sums in shared memory, so that one set of them leaves an SM.
-template <typename T, typename G, int U, bool EVEN>
+// The sums of four values over a warp, each in the lanes whose bits 4 and 3 are its number: values are traded
+// for other values' halves, six exchanges instead of twenty.
+__device__ __forceinline__ float traded_sums(const float (&v)[4], int lane) {
+    const bool high = lane & 16, odd = lane & 8;
+    const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, high ? v[0] : v[2], 16);
+    const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, high ? v[1] : v[3], 16);
+    float c = (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+    return c;
+}
+
+// Longer rows: a group of warps takes two rows at a time, U pieces of each to a thread; even rows lie in shared memory, where
+// the next ones are on their way, and are read from there once for the sums and once for dx.  The groups of a block join
+// their sums over rows in shared memory, so that one set of them leaves an SM.
+constexpr int kPairsAhead = 2;
+
+template <typename T, typename G, int U, bool EVEN, int WARPS>
 __global__ void __launch_bounds__(32 * kGroupWarps)
 layer_norm_backward_kernel(const NormBackArgs a, int warps) {
     constexpr int kUnitsX = Piece<T, true>::kUnits, kUnits = kUnitsX + Piece<G, true>::kUnits;
-    constexpr bool kNext = !EVEN && U == 1;
-    extern __shared__ uint4 ahead[];  // [rows ahead][U][units of both pieces][threads]; at the end two sums of each column
-    __shared__ float slots[2][kGroupWarps][2];
+    extern __shared__ uint4 ahead[];  // [pairs ahead][2][U][units of both pieces][threads]; at the end two sums of each column
+    __shared__ alignas(16) float slots[2][kGroupWarps][4];
     let_next_start();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const Group group(warps);
-    const Columns<EVEN> c = {group.t, 32 * warps, a.dim};
+    const Group group(WARPS ? WARPS : warps);
+    const Columns<EVEN, 32 * WARPS> c = {group.t, 32 * warps, a.dim};
     const T *x0 = static_cast<const T *>(a.x);
     const G *dy0 = static_cast<const G *>(a.dy);
-    const int64_t step = (int64_t)gridDim.x * group.count;
+    const int64_t step = (int64_t)gridDim.x * group.count;  // of a group's rows; it takes rows row and row + step together
     int64_t row = (int64_t)blockIdx.x * group.count + group.index;
-    const auto slot = [&](int stage, int u, int i) { return ahead + ((stage * U + u) * kUnits + i) * blockDim.x + threadIdx.x; };
-    const auto send_for = [&](int64_t r, int stage) {
+    const auto slot = [&](int stage, int r, int u, int i) { return ahead + (((stage * 2 + r) * U + u) * kUnits + i) * blockDim.x + threadIdx.x; };
+    const auto send_for = [&](int64_t first, int stage) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r < a.rows && c.has(u, 0)) {
+        for (int r = 0; r < 2; ++r) {
+            const int64_t at = first + r * step;
+            if (at >= a.rows) continue;
+            const uint4 *fx = reinterpret_cast<const uint4 *>(x0 + at * a.ld_x) + c.t * kUnitsX;
+            const uint4 *fdy = reinterpret_cast<const uint4 *>(dy0 + at * a.ld_dy) + c.t * (kUnits - kUnitsX);
 #pragma unroll
-                for (int i = 0; i < kUnits; ++i)
-                    copy16((uint32_t)__cvta_generic_to_shared(slot(stage, u, i)),
-                           i < kUnitsX ? reinterpret_cast<const uint4 *>(x0 + r * a.ld_x + c.at(u, 0)) + i
-                                       : reinterpret_cast<const uint4 *>(dy0 + r * a.ld_dy + c.at(u, 0)) + (i - kUnitsX));
-            }
+            for (int u = 0; u < U; ++u)
+                if (c.has(u, 0)) {
+#pragma unroll
+                    for (int i = 0; i < kUnits; ++i)
+                        copy16((uint32_t)__cvta_generic_to_shared(slot(stage, r, u, i)),
+                               i < kUnitsX ? fx + u * c.width() * kUnitsX + i : fdy + u * c.width() * (kUnits - kUnitsX) + (i - kUnitsX));
+                }
+        }
         copies_end_group();
     };
-    Piece<T, EVEN> raw_x[U], next_x[U];
-    Piece<G, EVEN> raw_dy[U], next_dy[U];
-    float next_mean = 0.f, next_rstd = 0.f;
-    const auto load = [&](int64_t r, Piece<T, EVEN> (&px)[U], Piece<G, EVEN> (&pdy)[U]) {
+    float next_mean[2] = {}, next_rstd[2] = {};
+    const auto look_up = [&](int64_t first) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            px[u].load(x0 + (r < a.rows ? r * a.ld_x : 0), c, u, r < a.rows);
-            pdy[u].load(dy0 + (r < a.rows ? r * a.ld_dy : 0), c, u, r < a.rows);
+        for (int r = 0; r < 2; ++r) {
+            const int64_t at = first + r * step;
+            next_mean[r] = at < a.rows ? a.mean[at] : 0.f;
+            next_rstd[r] = at < a.rows ? a.rstd[at] : 0.f;
         }
     };
     if constexpr (EVEN) {
-        for (int i = 0; i < kAhead; ++i) send_for(row + i * step, i);
-    } else if constexpr (kNext) {
-        load(row, next_x, next_dy);
+        for (int i = 0; i < kPairsAhead; ++i) send_for(row + 2 * i * step, i);
     }
-    if (row < a.rows) {
-        next_mean = a.mean[row];
-        next_rstd = a.rstd[row];
-    }
-    float w[U][kPiece];
+    look_up(row);
+    Vec w[U];
     PieceSums sums[U] = {};
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_piece(a.weight, c, u, true, w[u]);
-    for (int stage = 0, turn = 0; row < a.rows; row += step, stage = stage + 1 == kAhead ? 0 : stage + 1, turn ^= 1) {
-        const float mean = next_mean, rstd = next_rstd;
-        if (row + step < a.rows) {
-            next_mean = a.mean[row + step];
-            next_rstd = a.rstd[row + step];
+    for (int u = 0; u < U; ++u) w[u] = load_piece(a.weight, c, u, true);
+    Piece<T, EVEN> odd_x[EVEN ? 1 : 2][U];
+    Piece<G, EVEN> odd_dy[EVEN ? 1 : 2][U];
+    // a piece of the pair's row r
+    const auto get = [&](int stage, int r, int u, bool live, Vec &x, Vec &dy) {
+        if constexpr (EVEN) {
+            Piece<T, true> px;
+            Piece<G, true> pdy;
+            const bool has = live && c.has(u, 0);
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const uint4 q = has ? *slot(stage, r, u, i) : make_uint4(0, 0, 0, 0);
+                if (i < kUnitsX) px.even[i < kUnitsX ? i : 0] = q;
+                else pdy.even[i < kUnitsX ? 0 : i - kUnitsX] = q;
+            }
+            x = px.get();
+            dy = pdy.get();
+        } else {
+            x = odd_x[r][u].get();
+            dy = odd_dy[r][u].get();
+        }
+    };
+    for (int stage = 0, turn = 0; row < a.rows; row += 2 * step, stage = stage + 1 == kPairsAhead ? 0 : stage + 1, turn ^= 1) {
+        float mean[2], rstd[2], v[4];
+        const bool both = row + step < a.rows;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            mean[r] = next_mean[r];
+            rstd[r] = next_rstd[r];
         }
         if constexpr (EVEN) {
-            copies_wait<kAhead - 1>();
+            copies_wait<kPairsAhead - 1>();
+        } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const bool has = c.has(u, 0);
+            for (int r = 0; r < 2; ++r) {
+                const bool live = r == 0 || both;
+                const int64_t at = live ? row + r * step : 0;
 #pragma unroll
-                for (int i = 0; i < kUnits; ++i) {
-                    const uint4 q = has ? *slot(stage, u, i) : make_uint4(0, 0, 0, 0);
-                    if (i < kUnitsX) raw_x[u].even[i < kUnitsX ? i : 0] = q;
-                    else raw_dy[u].even[i < kUnitsX ? 0 : i - kUnitsX] = q;
+                for (int u = 0; u < U; ++u) {
+                    odd_x[r][u].load(x0 + at * a.ld_x, c, u, live);
+                    odd_dy[r][u].load(dy0 + at * a.ld_dy, c, u, live);
                 }
             }
-        } else if constexpr (kNext) {
+        }
+        look_up(row + 2 * step);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            Pair p1 = 0, p2 = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                raw_x[u] = next_x[u];
-                raw_dy[u] = next_dy[u];
+                Vec x, dy;
+                get(stage, r, u, r == 0 || both, x, dy);
+                take_piece(x, dy, w[u], mean[r], rstd[r], sums[u], p1, p2);
             }
-            load(row + step, next_x, next_dy);
-        } else {
-            load(row, raw_x, raw_dy);
-        }
-        Pair p1 = 0, p2 = 0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[kPiece], dy[kPiece];
-            raw_x[u].get(x);
-            raw_dy[u].get(dy);
-            take_piece(x, dy, w[u], mean, rstd, sums[u], p1, p2);
+            v[2 * r] = pair_sum(p1);
+            v[2 * r + 1] = pair_sum(p2);
         }
         if (a.dx) {
-            // two sums over a warp: each half of it takes one
-            const float s1 = pair_sum(p1), s2 = pair_sum(p2);
-            float s = (lane & 16 ? s2 : s1) + __shfl_xor_sync(0xffffffffu, lane & 16 ? s1 : s2, 16);
-            s = lanes_sum(s, 16);
-            if (lane % 16 == 0) slots[turn][warp][lane / 16] = s;
+            const float mine = traded_sums(v, lane);
+            if (lane % 8 == 0) slots[turn][warp][lane / 8] = mine;
             group.sync();
-            float m1 = 0.f, m2 = 0.f;
+            float4 all = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
             for (int i = 0; i < warps; ++i) {
-                const float2 q = *reinterpret_cast<const float2 *>(slots[turn][group.index * warps + i]);
-                m1 += q.x;
-                m2 += q.y;
+                const float4 q = *reinterpret_cast<const float4 *>(slots[turn][group.index * warps + i]);
+                all.x += q.x;
+                all.y += q.y;
+                all.z += q.z;
+                all.w += q.w;
             }
-            m1 *= a.inv_dim;
-            m2 *= a.inv_dim;
-            T *dx = static_cast<T *>(a.dx) + row * a.ld_dx;
+            const float m1[2] = {all.x * a.inv_dim, all.z * a.inv_dim}, m2[2] = {all.y * a.inv_dim, all.w * a.inv_dim};
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float x[kPiece], dy[kPiece], out[kPiece];
-                raw_x[u].get(x);
-                raw_dy[u].get(dy);
-                piece_dx(x, dy, w[u], mean, rstd, m1, m2, out);
-                store_piece(dx, c, u, true, out);
+            for (int r = 0; r < 2; ++r) {
+                if (r == 1 && !both) continue;
+                T *dx = static_cast<T *>(a.dx) + (row + r * step) * a.ld_dx;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    Vec x, dy;
+                    get(stage, r, u, true, x, dy);
+                    store_piece(dx, c, u, true, piece_dx(x, dy, w[u], mean[r], rstd[r], m1[r], m2[r]));
+                }
             }
         }
-        if constexpr (EVEN) send_for(row + kAhead * step, stage);  // behind the last use of what was there
+        if constexpr (EVEN) send_for(row + 2 * kPairsAhead * step, stage);  // behind the last use of what was there
     }
     if (!a.parts) return;
     const int64_t pad = padded(a.dim);
@@ -459,19 +496,16 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
     for (int q = 0; q < group.count; ++q) {
         if (q == group.index) {
             const bool last = q + 1 == group.count;
+            float *to = last ? part : joined;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (q > 0 && last) {  // the last group brings the sums out
-#pragma unroll
-                    for (int i = 0; i < kPiece / 2; ++i) {
-                        const int at0 = c.at(u, 2 * i), at1 = c.at(u, 2 * i + 1);
-                        const bool has0 = c.has(u, 2 * i), has1 = c.has(u, 2 * i + 1);
-                        sums[u].dw[i] = add2(sums[u].dw[i], pair(has0 ? joined[at0] : 0.f, has1 ? joined[at1] : 0.f));
-                        sums[u].db[i] = add2(sums[u].db[i], pair(has0 ? joined[pad + at0] : 0.f, has1 ? joined[pad + at1] : 0.f));
-                    }
+            for (int u = 0; u < U; ++u) {  // the last group brings the sums out
+                Vec dw = sums[u].dw, db = sums[u].db;
+                if (q > 0) {
+                    dw = sum_of(dw, load_piece(joined, c, u, true));
+                    db = sum_of(db, load_piece(joined + pad, c, u, true));
                 }
-                put_sums(last ? part : joined, c, u, sums[u].dw, q > 0 && !last);
-                put_sums((last ? part : joined) + pad, c, u, sums[u].db, q > 0 && !last);
+                store_piece(to, c, u, true, dw);
+                store_piece(to + pad, c, u, true, db);
             }
         }
         if (q + 1 < group.count) __syncthreads();
@@ -580,45 +614,84 @@ struct RowPlan {
     int pieces, each, warps, groups;
 };
 
-template <typename T, typename O, int U, bool EVEN>
+template <typename T, typename O, int U, bool EVEN, int WARPS>
 cudaError_t forward_groups(const NormArgs &a, const RowPlan &p, int sm_count, cudaStream_t stream) {
-    constexpr int kResident = 768;  // threads of an SM that 80 registers allow
     const int threads = 32 * p.warps * p.groups;
-    const size_t shared = EVEN ? (size_t)kAhead * U * Piece<T, true>::kUnits * threads * 16 : 0;
-    const unsigned grid = grid_for((size_t)a.rows, (size_t)p.groups, sm_count, threads < kResident ? kResident / threads : 1);
+    const size_t params = EVEN ? (size_t)64 * U * 32 * p.warps : (size_t)8 * a.dim;
+    const size_t shared = params + (EVEN ? (size_t)kAhead * U * Piece<T, true>::kUnits * threads * 16 : 0);
     if (shared > 40 * 1024) {  // with the static part, more than a kernel has unasked
         static std::atomic<unsigned long long> ready{0};
-        const cudaError_t e = allow_shared(layer_norm_kernel<T, O, U, EVEN>, 160 * 1024, ready);
+        const cudaError_t e = allow_shared(layer_norm_kernel<T, O, U, EVEN, WARPS>, 200 * 1024, ready);
         if (e != cudaSuccess) return e;
     }
-    layer_norm_kernel<T, O, U, EVEN><<<grid, threads, shared, stream>>>(a, p.warps);
+    const unsigned grid = grid_for((size_t)a.rows, (size_t)p.groups, sm_count, 1);
+    layer_norm_kernel<T, O, U, EVEN, WARPS><<<grid, threads, shared, stream>>>(a, p.warps);
     return cudaGetLastError();
 }
 
-template <typename T, typename O, bool EVEN>
-cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
+// Pieces to a thread and warps to a row: as many pieces as leave every SM eight warps, up to `most`; warps rounded up to
+// a power of two where the compiler has to know them.
+RowPlan plan_rows(int64_t rows, int pieces, int sm_count, int most, bool power) {
     RowPlan p;
-    p.pieces = (int)(padded(a.dim) / kPiece);
-    if (p.pieces <= 32) {
-        const int lanes = lanes_for(p.pieces), rows = kShortThreads / lanes;
-        layer_norm_short_kernel<T, O, EVEN><<<(unsigned)((a.rows + rows - 1) / rows), kShortThreads, 0, stream>>>(a, lanes);
+    p.pieces = pieces;
+    const auto warps_with = [&](int each) {
+        int w = (pieces + 32 * each - 1) / (32 * each);
+        while (power && (w & (w - 1))) ++w;
+        return w;
+    };
+    p.each = most;
+    while (p.each > 1 && (pieces <= 16 * p.each || rows * warps_with(p.each) < 8 * (int64_t)sm_count) && warps_with(p.each / 2) <= kGroupWarps)
+        p.each /= 2;
+    p.warps = warps_with(p.each);
+    p.groups = 1;
+    return p;
+}
+
+template <typename T, typename O>
+cudaError_t forward_even(const NormArgs &a, RowPlan &p, int sm_count, cudaStream_t stream) {
+    switch (p.each) {
+        case 8: return forward_groups<T, O, 8, true, 0>(a, p, sm_count, stream);
+        case 4: return forward_groups<T, O, 4, true, 0>(a, p, sm_count, stream);
+        case 2: return forward_groups<T, O, 2, true, 0>(a, p, sm_count, stream);
+        default: return forward_groups<T, O, 1, true, 0>(a, p, sm_count, stream);
+    }
+}
+template <typename T, typename O, int U>
+cudaError_t forward_odd(const NormArgs &a, RowPlan &p, int sm_count, cudaStream_t stream) {
+    switch (p.warps) {
+        case 1: return forward_groups<T, O, U, false, 1>(a, p, sm_count, stream);
+        case 2: return forward_groups<T, O, U, false, 2>(a, p, sm_count, stream);
+        case 4: return forward_groups<T, O, U, false, 4>(a, p, sm_count, stream);
+        case 8: return forward_groups<T, O, U, false, 8>(a, p, sm_count, stream);
+        default: return forward_groups<T, O, U, false, 16>(a, p, sm_count, stream);
+    }
+}
+
+template <typename T, typename O>
+cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
+    const int pieces = (int)(padded(a.dim) / kPiece);
+    const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T)) && even_rows(a.y, a.dim, a.ld_y, sizeof(O)) && aligned(a.weight, 16) &&
+                      aligned(a.bias, 16);
+    if (pieces <= 32) {
+        const int lanes = lanes_for(pieces), rows = kShortThreads / lanes;
+        const unsigned grid = (unsigned)((a.rows + rows - 1) / rows);
+        if (even) layer_norm_short_kernel<T, O, true><<<grid, kShortThreads, 0, stream>>>(a, lanes);
+        else layer_norm_short_kernel<T, O, false><<<grid, kShortThreads, 0, stream>>>(a, lanes);
         return cudaGetLastError();
     }
-    if (p.pieces > kLongPieces) {
+    if (pieces > kLongPieces) {
         layer_norm_long_kernel<T, O><<<(unsigned)a.rows, kLongThreads, 0, stream>>>(a);
         return cudaGetLastError();
     }
-    // few rows: more threads to each
-    p.each = p.pieces > 32 * kGroupWarps || a.rows >= 2 * (int64_t)sm_count ? 2 : 1;
-    p.warps = (p.pieces + 32 * p.each - 1) / (32 * p.each);
-    p.groups = p.warps < 4 && a.rows >= 2 * (int64_t)sm_count ? 4 / p.warps : 1;
-    return p.each == 2 ? forward_groups<T, O, 2, EVEN>(a, p, sm_count, stream) : forward_groups<T, O, 1, EVEN>(a, p, sm_count, stream);
-}
-template <typename T, typename O>
-cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
-    const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T)) && even_rows(a.y, a.dim, a.ld_y, sizeof(O)) && aligned(a.weight, 16) &&
-                      aligned(a.bias, 16);
-    return even ? forward<T, O, true>(a, sm_count, stream) : forward<T, O, false>(a, sm_count, stream);
+    // (uneven: four pieces where there are rows enough for that, else one or two)
+    RowPlan p = plan_rows(a.rows, pieces, sm_count, even ? 8 : 4, !even);
+    // rows side by side in a block, as many as its warps and an SM's shared memory have room for
+    const int most = even && sizeof(T) == 4 && p.each == 8 ? kGroupWarps / 2 : kGroupWarps;
+    p.groups = most / p.warps < 1 ? 1 : most / p.warps;
+    while (p.groups > 1 && a.rows < (int64_t)sm_count * p.groups) p.groups -= 1;
+    if (even) return forward_even<T, O>(a, p, sm_count, stream);
+    return p.each == 4 ? forward_odd<T, O, 4>(a, p, sm_count, stream)
+                       : p.each == 2 ? forward_odd<T, O, 2>(a, p, sm_count, stream) : forward_odd<T, O, 1>(a, p, sm_count, stream);
 }
 
 // Blocks of the backward pass, whose sums the workspace holds; behind them two sums of each row where rows are long.
@@ -626,11 +699,12 @@ struct BackPlan : RowPlan {
     bool is_long;
     int64_t parts;
 };
-BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even) {
+BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even, bool wide) {
     BackPlan p;
     p.pieces = (int)(padded(dim) / kPiece);
     p.each = p.pieces > 32 * kGroupWarps || (even && rows >= 2 * (int64_t)sm_count) ? 2 : 1;
     p.warps = (p.pieces + 32 * p.each - 1) / (32 * p.each);
+    while (!even && p.pieces > 32 && (p.warps & (p.warps - 1))) ++p.warps;  // the compiler has to know them
     p.groups = 1;
     p.is_long = p.pieces > kLongPieces;
     int64_t most = sm_count;
@@ -641,8 +715,9 @@ BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even) {
         const int64_t tiles = (dim + kTileColumns * kLanesThreads - 1) / (kTileColumns * kLanesThreads);
         most = (4 * (int64_t)sm_count + tiles - 1) / tiles;
     } else {
-        // as many rows to a block as it has warps for, fewer where that would leave SMs without any
-        p.groups = kGroupWarps / p.warps;
+        // as many groups to a block as it has warps for (half as many, where even rows in fp32 fill shared memory), fewer where that
+        // would leave SMs without any
+        p.groups = (wide && p.warps <= kGroupWarps / 2 ? kGroupWarps / 2 : kGroupWarps) / p.warps;
         while (p.groups > 1 && rows < (int64_t)sm_count * p.groups) p.groups -= 1;
     }
     p.parts = (rows + p.groups - 1) / p.groups;
@@ -651,18 +726,24 @@ BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even) {
     return p;
 }
 
-template <typename T, typename G, int U, bool EVEN>
+constexpr size_t kBackShared = 200 * 1024;
+template <typename T, typename G>
+size_t bytes_ahead(int each, int threads) {
+    return (size_t)kPairsAhead * 2 * each * (Piece<T, true>::kUnits + Piece<G, true>::kUnits) * threads * 16;
+}
+
+template <typename T, typename G, int U, bool EVEN, int WARPS>
 cudaError_t back_groups(const NormBackArgs &a, const BackPlan &p, cudaStream_t stream) {
     const int threads = 32 * p.warps * p.groups;
-    size_t shared = EVEN ? (size_t)kAhead * U * (Piece<T, true>::kUnits + Piece<G, true>::kUnits) * threads * 16 : 0;
+    size_t shared = EVEN ? bytes_ahead<T, G>(U, threads) : 0;
     const size_t joined = p.groups > 1 && a.parts ? (size_t)2 * padded(a.dim) * sizeof(float) : 0;
     if (shared < joined) shared = joined;
     if (shared > 40 * 1024) {  // with the static part, more than a kernel has unasked
         static std::atomic<unsigned long long> ready{0};
-        const cudaError_t e = allow_shared(layer_norm_backward_kernel<T, G, U, EVEN>, 200 * 1024, ready);
+        const cudaError_t e = allow_shared(layer_norm_backward_kernel<T, G, U, EVEN, WARPS>, kBackShared, ready);
         if (e != cudaSuccess) return e;
     }
-    layer_norm_backward_kernel<T, G, U, EVEN><<<(unsigned)p.parts, threads, shared, stream>>>(a, p.warps);
+    layer_norm_backward_kernel<T, G, U, EVEN, WARPS><<<(unsigned)p.parts, threads, shared, stream>>>(a, p.warps);
     return cudaGetLastError();
 }
 template <typename T, typename G, bool EVEN>
@@ -671,14 +752,25 @@ cudaError_t launch_back(const NormBackArgs &a, const BackPlan &p, cudaStream_t s
         layer_norm_backward_short_kernel<T, G, EVEN><<<(unsigned)p.parts, kLanesThreads, 0, stream>>>(a, lanes_for(p.pieces));
         return cudaGetLastError();
     }
-    return p.each == 2 ? back_groups<T, G, 2, EVEN>(a, p, stream) : back_groups<T, G, 1, EVEN>(a, p, stream);
+    if constexpr (EVEN) {
+        return p.each == 2 ? back_groups<T, G, 2, true, 0>(a, p, stream) : back_groups<T, G, 1, true, 0>(a, p, stream);
+    } else {
+        if (p.each == 2) return back_groups<T, G, 2, false, 16>(a, p, stream);  // rows of over 512 pieces
+        switch (p.warps) {
+            case 2: return back_groups<T, G, 1, false, 2>(a, p, stream);
+            case 4: return back_groups<T, G, 1, false, 4>(a, p, stream);
+            case 8: return back_groups<T, G, 1, false, 8>(a, p, stream);
+            default: return back_groups<T, G, 1, false, 16>(a, p, stream);
+        }
+    }
 }
 
 template <typename T, typename G>
 cudaError_t backward(const NormBackArgs &a, int sm_count, cudaStream_t stream, int *launches) {
     const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T)) && even_rows(a.dy, a.dim, a.ld_dy, sizeof(G)) &&
-                      (!a.dx || even_rows(a.dx, a.dim, a.ld_dx, sizeof(T))) && aligned(a.weight, 16);
-    const BackPlan p = plan_back(a.rows, a.dim, sm_count, even);
+                      (!a.dx || even_rows(a.dx, a.dim, a.ld_dx, sizeof(T))) && aligned(a.weight, 16) &&
+                      bytes_ahead<T, G>(2, a.dim / (2 * kPiece)) <= kBackShared - 8192;  // (the longest rows of fp32 go the other way)
+    const BackPlan p = plan_back(a.rows, a.dim, sm_count, even, even && sizeof(T) + sizeof(G) > 4);
     cudaError_t e = cudaSuccess;
     if (a.rows > 0) {
         if (p.is_long) {
@@ -710,7 +802,7 @@ cudaError_t backward(const NormBackArgs &a, int sm_count, cudaStream_t stream, i
 
 size_t norm_workspace_bytes(int64_t rows, int dim, int sm_count) {
     // (whichever way the rows lie: an even call has no more blocks than an uneven one)
-    const BackPlan p = plan_back(rows, dim, sm_count, false);
+    const BackPlan p = plan_back(rows, dim, sm_count, false, false);
     return (size_t)p.parts * 2 * padded(dim) * sizeof(float) + (p.is_long ? (size_t)rows * sizeof(float2) : 0);
 }
 

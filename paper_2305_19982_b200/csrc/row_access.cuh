@@ -8,11 +8,22 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
-#include "stream_access.cuh"
+#include "softmax_rows.cuh"
 
 namespace adama {
 
 constexpr int kPiece = 8;  // elements of a piece: 16 bytes of bf16, 32 of fp32
+
+// Eight elements as fp32, two to a register pair.
+struct Vec {
+    Pair p[kPiece / 2];
+};
+__device__ __forceinline__ Vec zeros() { return {{0, 0, 0, 0}}; }
+__device__ __forceinline__ float pair_sum(Pair p) {
+    float a, b;
+    split(p, a, b);
+    return a + b;
+}
 
 template <typename O>
 __device__ __forceinline__ O narrowed(float y);
@@ -21,26 +32,34 @@ __device__ __forceinline__ float narrowed<float>(float y) { return y; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 narrowed<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
 
-// Columns of a thread: element i of its piece u, of threads `t` of `width` that share a row.
-template <bool EVEN>
+// Columns of a thread: element i of its piece u, of threads `t` of a row's `width`.  W: that width, known to the
+// compiler (0: it is not), so that uneven rows' accesses need no address of their own each.
+template <bool EVEN, int W = 0>
 struct Columns {
-    int t, width, dim;
+    int t, threads, dim;
 
-    __device__ __forceinline__ int at(int u, int i) const { return EVEN ? (t + u * width) * kPiece + i : t + (u * kPiece + i) * width; }
-    __device__ __forceinline__ bool has(int u, int i) const { return at(u, i) < dim; }  // (EVEN: the same for all i)
+    __device__ __forceinline__ int width() const { return W ? W : threads; }
+    __device__ __forceinline__ int at(int u, int i) const { return EVEN ? (t + u * width()) * kPiece + i : t + (u * kPiece + i) * width(); }
+    __device__ __forceinline__ bool has(int u, int i) const {  // (EVEN: the same for all i)
+        return EVEN ? (t + u * width()) * kPiece < dim : t < dim - (u * kPiece + i) * width();
+    }
 };
 
-__device__ __forceinline__ void widen_words(const uint4 (&u)[1], float (&v)[kPiece]) {  // bf16 -> fp32 is a 16-bit left shift
+__device__ __forceinline__ Vec widened(const uint4 (&u)[1]) {  // bf16 -> fp32 is a 16-bit left shift
     const unsigned z[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+    Vec v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(z[i] << 16);
-        v[2 * i + 1] = __uint_as_float(z[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) v.p[i] = pair(__uint_as_float(z[i] << 16), __uint_as_float(z[i] & 0xffff0000u));
+    return v;
 }
-__device__ __forceinline__ void widen_words(const uint4 (&u)[2], float (&v)[kPiece]) {
-    v[0] = __uint_as_float(u[0].x); v[1] = __uint_as_float(u[0].y); v[2] = __uint_as_float(u[0].z); v[3] = __uint_as_float(u[0].w);
-    v[4] = __uint_as_float(u[1].x); v[5] = __uint_as_float(u[1].y); v[6] = __uint_as_float(u[1].z); v[7] = __uint_as_float(u[1].w);
+__device__ __forceinline__ Vec widened(const uint4 (&u)[2]) {
+    Vec v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        v.p[2 * h] = pair(__uint_as_float(u[h].x), __uint_as_float(u[h].y));
+        v.p[2 * h + 1] = pair(__uint_as_float(u[h].z), __uint_as_float(u[h].w));
+    }
+    return v;
 }
 
 // A piece as it comes from memory, so that many can be on their way before the first one is looked at.
@@ -51,65 +70,81 @@ struct Piece {
     T odd[EVEN ? 1 : kPiece];
 
     // row: the row's first element; zeros for columns that it does not have, and for none at all (`live` false)
-    __device__ __forceinline__ void load(const T *row, const Columns<EVEN> &c, int u, bool live) {
+    template <int W>
+    __device__ __forceinline__ void load(const T *row, const Columns<EVEN, W> &c, int u, bool live) {
         if constexpr (EVEN) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(row + c.at(u, 0));
 #pragma unroll
-            for (int i = 0; i < kUnits; ++i) {
-                even[i] = make_uint4(0, 0, 0, 0);
-                if (live && c.has(u, 0)) even[i] = reinterpret_cast<const uint4 *>(row + c.at(u, 0))[i];
+            for (int i = 0; i < kUnits; ++i) even[i] = make_uint4(0, 0, 0, 0);
+            if (live && c.has(u, 0)) {
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i) even[i] = from[i];
             }
         } else {
+            const T *from = row + c.t;
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) {
                 odd[i] = narrowed<T>(0.f);
-                if (live && c.has(u, i)) odd[i] = row[c.at(u, i)];
+                if (live && c.has(u, i)) odd[i] = from[(u * kPiece + i) * c.width()];
             }
         }
     }
-    __device__ __forceinline__ void get(float (&v)[kPiece]) const {
+    __device__ __forceinline__ Vec get() const {
         if constexpr (EVEN) {
-            widen_words(even, v);
+            return widened(even);
         } else {
+            Vec v;
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) v[i] = widen(odd[i]);
+            for (int i = 0; i < kPiece / 2; ++i) v.p[i] = pair(widen(odd[2 * i]), widen(odd[2 * i + 1]));
+            return v;
         }
     }
 };
-template <typename T, bool EVEN>
-__device__ __forceinline__ void load_piece(const T *row, const Columns<EVEN> &c, int u, bool live, float (&v)[kPiece]) {
+template <typename T, bool EVEN, int W>
+__device__ __forceinline__ Vec load_piece(const T *row, const Columns<EVEN, W> &c, int u, bool live) {
     Piece<T, EVEN> q;
     q.load(row, c, u, live);
-    q.get(v);
+    return q.get();
 }
 
-__device__ __forceinline__ void pack_words(const float (&v)[kPiece], uint4 (&w)[1]) {
+__device__ __forceinline__ void pack_words(const Vec &v, uint4 (&w)[1]) {
     unsigned z[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        z[i] = *reinterpret_cast<const unsigned *>(&p);
+        float a, b;
+        split(v.p[i], a, b);
+        const __nv_bfloat162 q = __floats2bfloat162_rn(a, b);
+        z[i] = *reinterpret_cast<const unsigned *>(&q);
     }
     w[0] = make_uint4(z[0], z[1], z[2], z[3]);
 }
-__device__ __forceinline__ void pack_words(const float (&v)[kPiece], uint4 (&w)[2]) {
+__device__ __forceinline__ void pack_words(const Vec &v, uint4 (&w)[2]) {
+    float a[kPiece];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split(v.p[i], a[2 * i], a[2 * i + 1]);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        w[h] = make_uint4(__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3]));
+        w[h] = make_uint4(__float_as_uint(a[4 * h]), __float_as_uint(a[4 * h + 1]), __float_as_uint(a[4 * h + 2]), __float_as_uint(a[4 * h + 3]));
 }
-template <typename O, bool EVEN>
-__device__ __forceinline__ void store_piece(O *row, const Columns<EVEN> &c, int u, bool live, const float (&v)[kPiece]) {
-    if (!live) return;
+template <typename O, bool EVEN, int W>
+__device__ __forceinline__ void store_piece(O *row, const Columns<EVEN, W> &c, int u, bool live, const Vec &v) {
     if constexpr (EVEN) {
         uint4 w[kPiece * sizeof(O) / 16];
         pack_words(v, w);
-        if (c.has(u, 0)) {
+        if (live && c.has(u, 0)) {
+            uint4 *to = reinterpret_cast<uint4 *>(row + c.at(u, 0));
 #pragma unroll
-            for (int i = 0; i < (int)(kPiece * sizeof(O) / 16); ++i) reinterpret_cast<uint4 *>(row + c.at(u, 0))[i] = w[i];
+            for (int i = 0; i < (int)(kPiece * sizeof(O) / 16); ++i) to[i] = w[i];
         }
     } else {
+        O *to = row + c.t;
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i)
-            if (c.has(u, i)) row[c.at(u, i)] = narrowed<O>(v[i]);
+        for (int i = 0; i < kPiece / 2; ++i) {
+            float a, b;
+            split(v.p[i], a, b);
+            if (live && c.has(u, 2 * i)) to[(u * kPiece + 2 * i) * c.width()] = narrowed<O>(a);
+            if (live && c.has(u, 2 * i + 1)) to[(u * kPiece + 2 * i + 1) * c.width()] = narrowed<O>(b);
+        }
     }
 }
 
