@@ -7,7 +7,8 @@
 // The tokens are sorted by id, equal ones in their order.  The sorted tokens are cut into chunks; a warp takes
 // a chunk's columns 256 at a time and sums equal neighbours in registers, in fp32.  A run of equal tokens that
 // lies inside a chunk is finished there; the parts of one that crosses chunks go to the workspace, and a second
-// kernel adds them in order.  So a token that occurs thousands of times is spread over the card like any others,
+// kernel adds them in order; one that only reaches into the next chunk is finished by the warp that has its
+// beginning.  So a token that occurs thousands of times is spread over the card like any others,
 // no atomics are involved and results do not depend on scheduling.  Bound by HBM.
 #include "adama_device.cuh"
 #include "chained.cuh"
@@ -61,75 +62,80 @@ __device__ __forceinline__ unsigned key_of(const EmbeddingGradArgs &a, int64_t t
 // Up to kRankTokens tokens: a token's place is the number of tokens that come before it, counted over all
 // of them.  32 tokens to a block, whose warps share the count.
 constexpr int kRankTokens = 8192;
-constexpr int kRankWarps = 8;
-constexpr int kRankTile = 2048;
+constexpr int kRankWarps = 16;
 
 __global__ void __launch_bounds__(32 * kRankWarps)
 embedding_rank_kernel(const EmbeddingGradArgs a) {
-    let_next_start();
-    __shared__ alignas(16) unsigned keys[kRankTile];
+    __shared__ alignas(16) unsigned keys[kRankTokens];
     __shared__ int counts[kRankWarps][32];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int t = blockIdx.x * 32 + lane, tokens = (int)a.tokens;
-    const unsigned mine = t < tokens ? key_of(a, t) : 0;
+    let_next_start();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, tokens = (int)a.tokens;
+    const int groups = (tokens + 31) / 32;  // of 32 tokens
+#pragma unroll 8
+    for (int i = threadIdx.x; i < 32 * groups; i += 32 * kRankWarps) keys[i] = i < tokens ? key_of(a, i) : 0xffffffffu;
+    __syncthreads();
+    const int t = blockIdx.x * 32 + lane;
+    const unsigned mine = keys[t];
     int before = 0;
-    for (int base = 0; base < tokens; base += kRankTile) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kRankTile; i += 32 * kRankWarps)
-            keys[i] = base + i < tokens ? key_of(a, base + i) : 0xffffffffu;
-        __syncthreads();
-        const int begin = warp * (kRankTile / kRankWarps);
-        for (int i = begin; i < begin + kRankTile / kRankWarps && base + i < tokens; i += 32) {
-            const int block = (base + i) / 32;
-            if (block != (int)blockIdx.x) {
-                const unsigned limit = mine + (block < (int)blockIdx.x ? 1u : 0u);  // equal ones in front count
+    for (int g = warp; g < groups; g += kRankWarps) {
+        if (g != (int)blockIdx.x) {
+            const unsigned limit = mine + (g < (int)blockIdx.x ? 1u : 0u);  // equal ones in front count
 #pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    const uint4 k = *reinterpret_cast<const uint4 *>(keys + i + j);
-                    before += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
-                }
-            } else {
-                for (int j = 0; j < 32; ++j) before += keys[i + j] < mine + (j < lane ? 1u : 0u);
+            for (int j = 0; j < 32; j += 4) {
+                const uint4 k = *reinterpret_cast<const uint4 *>(keys + 32 * g + j);
+                before += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
             }
+        } else {
+            for (int j = 0; j < 32; ++j) before += keys[32 * g + j] < mine + (j < lane ? 1u : 0u);
         }
     }
     counts[warp][lane] = before;
     __syncthreads();
     if (warp != 0 || t >= tokens) return;
     int place = 0;
+#pragma unroll
     for (int i = 0; i < kRankWarps; ++i) place += counts[i][lane];
     a.keys[place] = mine;
     a.order[place] = (unsigned)t;
     if (mine == (unsigned)a.vocab && a.ids[t] >= 0) record_bad_target(a.status, t);
 }
 
-// More: passes over digits of the key, from the lowest on, each of which keeps the order of equal digits.
+// More: passes over digits of the key, from the lowest on, each of which keeps the order of equal digits.  A block
+// has neighbouring tokens; how many of each digit every block has is counted ahead of a pass (of the first one by a kernel
+// of its own, of the others as the tokens get their new places).
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortWarps = 8;
 constexpr int kSortThreads = 32 * kSortWarps;
 constexpr int kSortBlocks = 64;  // at most
+constexpr int kSortPasses = 4;   // for keys of 31 bits and the one behind them
+constexpr int kRounds = 4;       // of 32 tokens, loaded together
 
 struct SortPass {
     const unsigned *keys, *order;  // null in the first pass: from the ids
     unsigned *keys_out, *order_out;
-    int *counts;  // [blocks][digits]
-    int shift, mask, per;  // tokens of a block, a multiple of kSortThreads
+    int *counts, *next_counts;  // [blocks][digits]; next: null in the last pass
+    int shift, next_shift, mask;
+    int per;  // tokens of a block, a multiple of kSortThreads
 };
 __device__ __forceinline__ unsigned pass_key(const EmbeddingGradArgs &a, const SortPass &p, int64_t t) {
     return p.keys ? p.keys[t] : key_of(a, t);
 }
 
+// Counts for the first pass; the other passes' counts (`others` ints behind them) become 0.
 __global__ void __launch_bounds__(kSortThreads)
-embedding_digits_kernel(const EmbeddingGradArgs a, const SortPass p) {
+embedding_digits_kernel(const EmbeddingGradArgs a, const SortPass p, int *others, int other_ints) {
     __shared__ int counts[kDigits];
+    let_next_start();
     for (int i = threadIdx.x; i < kDigits; i += kSortThreads) counts[i] = 0;
+    for (int i = blockIdx.x * kSortThreads + threadIdx.x; i < other_ints; i += gridDim.x * kSortThreads) others[i] = 0;
     __syncthreads();
     const int64_t begin = (int64_t)blockIdx.x * p.per;
+#pragma unroll 4
     for (int64_t t = begin + threadIdx.x; t < begin + p.per && t < a.tokens; t += kSortThreads) {
-        const unsigned key = pass_key(a, p, t);
+        const unsigned key = key_of(a, t);
         atomicAdd(&counts[key >> p.shift & p.mask], 1);
-        if (!p.keys && key == (unsigned)a.vocab && a.ids[t] >= 0) record_bad_target(a.status, t);
+        if (key == (unsigned)a.vocab && a.ids[t] >= 0) record_bad_target(a.status, t);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kDigits; i += kSortThreads) p.counts[blockIdx.x * kDigits + i] = counts[i];
@@ -138,17 +144,33 @@ embedding_digits_kernel(const EmbeddingGradArgs a, const SortPass p) {
 __global__ void __launch_bounds__(kSortThreads)
 embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
     __shared__ int place[kSortWarps][kDigits];  // where a warp's next token of a digit goes
-    __shared__ int scan[kSortThreads];
+    __shared__ int warp_total[kSortWarps];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&place[0][0])[i] = 0;
+    let_next_start();
+    wait_for_previous();
     __syncthreads();
     const int64_t begin = (int64_t)blockIdx.x * p.per + (int64_t)warp * (p.per / kSortWarps);
     int64_t end = begin + p.per / kSortWarps;
     if (end > a.tokens) end = a.tokens;
-    for (int64_t t = begin + lane; t < end; t += 32) atomicAdd(&place[warp][pass_key(a, p, t) >> p.shift & p.mask], 1);
-    __syncthreads();
+    unsigned key[kRounds], token[kRounds];
+    const auto load = [&](int64_t base) {
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const int64_t t = base + 32 * i + lane;
+            key[i] = t < end ? pass_key(a, p, t) : 0;
+            token[i] = t < end ? (p.order ? p.order[t] : (unsigned)t) : 0;
+        }
+    };
+    for (int64_t base = begin; base < end; base += 32 * kRounds) {
+        load(base);
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i)
+            if (base + 32 * i + lane < end) atomicAdd(&place[warp][key[i] >> p.shift & p.mask], 1);
+    }
     // a thread has two neighbouring digits: tokens of smaller digits, and of its digits in blocks before this one
     int total[2] = {0, 0}, earlier[2] = {0, 0};
+#pragma unroll 8
     for (int b = 0; b < (int)gridDim.x; ++b) {
         const int2 n = *reinterpret_cast<const int2 *>(p.counts + b * kDigits + 2 * threadIdx.x);
         if (b < (int)blockIdx.x) {
@@ -158,18 +180,20 @@ embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
         total[0] += n.x;
         total[1] += n.y;
     }
-    scan[threadIdx.x] = total[0] + total[1];
-    __syncthreads();
-    for (int o = 1; o < kSortThreads; o *= 2) {
-        const int x = (int)threadIdx.x >= o ? scan[threadIdx.x - o] : 0;
-        __syncthreads();
-        scan[threadIdx.x] += x;
-        __syncthreads();
+    int at = total[0] + total[1];
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int x = __shfl_up_sync(0xffffffffu, at, o);
+        if (lane >= o) at += x;
     }
-    int at = scan[threadIdx.x] - total[0] - total[1];
+    if (lane == 31) warp_total[warp] = at;
+    __syncthreads();
+    at -= total[0] + total[1];
+    for (int w = 0; w < warp; ++w) at += warp_total[w];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         int next = at + earlier[q];
+#pragma unroll
         for (int w = 0; w < kSortWarps; ++w) {
             int &slot = place[w][2 * threadIdx.x + q];
             const int n = slot;
@@ -179,21 +203,24 @@ embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
         at += total[q];
     }
     __syncthreads();
-    for (int64_t base = begin; base < end; base += 32) {
-        const int64_t t = base + lane;
-        const unsigned key = t < end ? pass_key(a, p, t) : 0;
-        const unsigned token = t < end ? (p.order ? p.order[t] : (unsigned)t) : 0;
-        const int digit = t < end ? (int)(key >> p.shift & p.mask) : kDigits;
-        const unsigned same = __match_any_sync(0xffffffffu, digit);
-        const int rank = __popc(same & ((1u << lane) - 1));
-        int to = 0;
-        if (t < end) to = place[warp][digit] + rank;
-        __syncwarp();
-        if (t < end && rank == 0) place[warp][digit] += __popc(same);
-        __syncwarp();
-        if (t < end) {
-            p.keys_out[to] = key;
-            p.order_out[to] = token;
+    for (int64_t base = begin; base < end; base += 32 * kRounds) {
+        if (begin + 32 * kRounds < end) load(base);  // else they are still here
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const bool in = base + 32 * i + lane < end;
+            const int digit = in ? (int)(key[i] >> p.shift & p.mask) : kDigits;
+            const unsigned same = __match_any_sync(0xffffffffu, digit);
+            const int rank = __popc(same & ((1u << lane) - 1));
+            int to = 0;
+            if (in) to = place[warp][digit] + rank;
+            __syncwarp();
+            if (in && rank == 0) place[warp][digit] += __popc(same);
+            __syncwarp();
+            if (in) {
+                p.keys_out[to] = key[i];
+                p.order_out[to] = token[i];
+                if (p.next_counts) atomicAdd(p.next_counts + to / p.per * kDigits + (key[i] >> p.next_shift & p.mask), 1);
+            }
         }
     }
 }
@@ -295,31 +322,48 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     const int n = (int)(a.tokens - start < chunk ? a.tokens - start : chunk);
     const unsigned none = 0xffffffffu, out = (unsigned)a.vocab;
     const unsigned key = lane < n ? a.keys[start + lane] : none, token = lane < n ? a.order[start + lane] : 0;
-    const unsigned behind = start + n < a.tokens ? a.keys[start + n] : none;
+    const bool more = start + n + lane < a.tokens && lane < chunk;  // the next chunk's
+    const unsigned key2 = more ? a.keys[start + n + lane] : none, token2 = more ? a.order[start + n + lane] : 0;
     const unsigned ahead = start > 0 ? a.keys[start - 1] : none;
+    const unsigned far_ahead = start > chunk ? a.keys[start - chunk - 1] : none;
+    const unsigned behind = __shfl_sync(0xffffffffu, key2, 0), first_key = __shfl_sync(0xffffffffu, key, 0);
+    const unsigned last_key = __shfl_sync(0xffffffffu, key, n - 1);
     unsigned next = __shfl_down_sync(0xffffffffu, key, 1);
     if (lane == n - 1) next = behind;
-    const unsigned ends = __ballot_sync(0xffffffffu, lane < n && next != key);
+    unsigned ends = __ballot_sync(0xffffffffu, lane < n && next != key);
     const int live = __popc(__ballot_sync(0xffffffffu, lane < n && key != out));  // the others come last
-    bool open = __shfl_sync(0xffffffffu, key, 0) == ahead;  // the first run continues the chunk before
+    bool open = first_key == ahead;  // the first run continues the chunk before
+    int j = 0;
+    if (open && ends && far_ahead != first_key && __ffs(ends) < chunk) {  // begun there and ended here, not filling the chunk: its warp sees to it
+        j = __ffs(ends);
+        open = false;
+    }
+    // the last run's tokens in the next chunk, where it begins here and does not fill that
+    const bool goes_on = live == n && !(ends >> (n - 1) & 1) && !(open && ends == 0);
+    int extra = goes_on ? __popc(__ballot_sync(0xffffffffu, key2 == last_key)) : 0;
+    if (extra == chunk) extra = 0;
+    const int count = live + extra;
     const G *dy = static_cast<const G *>(a.dy) + tile;
     Vec sum = zeros();
-    for (int j = 0; j < live; j += kBatch) {
+    for (; j < count; j += kBatch) {
         Piece<G, EVEN> raw[kBatch];
         Target<O, MODE, EVEN> target[kBatch];
         unsigned k[kBatch];
+        bool last[kBatch];
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
-            const bool in = j + q < live;
-            k[q] = __shfl_sync(0xffffffffu, key, (j + q) & 31);
-            const unsigned t = __shfl_sync(0xffffffffu, token, (j + q) & 31);
-            raw[q].load(dy + (in ? (int64_t)t * a.ld_dy : 0), c, 0, in);
-            target[q].load(a, k[q], tile, c, in && (ends >> (j + q) & 1));
+            const int at = j + q;
+            const bool in = at < count;
+            const unsigned t1 = __shfl_sync(0xffffffffu, token, at & 31), t2 = __shfl_sync(0xffffffffu, token2, (at - n) & 31);
+            k[q] = __shfl_sync(0xffffffffu, key, at < n ? at : n - 1);  // (those behind have the last one's)
+            last[q] = in && (at < n ? ends >> at & 1 : at + 1 == count);
+            raw[q].load(dy + (in ? (int64_t)(at < n ? t1 : t2) * a.ld_dy : 0), c, 0, in);
+            target[q].load(a, k[q], tile, c, last[q]);
         }
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
             add_to(sum, raw[q].get());
-            if (j + q < live && (ends >> (j + q) & 1)) {
+            if (last[q]) {
                 if (open) store_piece(part_of(a, b, 0) + tile, c, 0, true, sum);
                 else target[q].finish(a, k[q], tile, c, sum);
                 open = false;
@@ -327,10 +371,10 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
             }
         }
     }
-    if (live == n && !(ends >> (n - 1) & 1)) store_piece(part_of(a, b, open ? 0 : 1) + tile, c, 0, true, sum);
+    if (live == n && extra == 0 && !(ends >> (n - 1) & 1)) store_piece(part_of(a, b, open ? 0 : 1) + tile, c, 0, true, sum);
 }
 
-// Runs that cross chunks: block x takes the one that begins in chunk x and goes on behind it, if there is one.
+// Runs that fill chunks: block x takes the one that begins in chunk x and fills the next one, if there is one.
 constexpr int kJoinWarps = 8;
 constexpr int kJoinShort = 16;  // parts up to which a warp adds them alone
 
@@ -342,7 +386,9 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk, int tiles) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t b = blockIdx.x, start = b * chunk, end = start + chunk;
     if (end >= a.tokens) return;
-    const unsigned key = a.keys[end - 1], after = a.keys[end], before = start > 0 ? a.keys[start - 1] : 0xffffffffu;
+    // the key behind the next chunk's last but one place: without it the run does not fill that chunk
+    const unsigned key = a.keys[end - 1], after = end + chunk <= a.tokens ? a.keys[end + chunk - 1] : 0xffffffffu;
+    const unsigned before = start > 0 ? a.keys[start - 1] : 0xffffffffu;
     const int64_t first_at = (b + 1 + lane) * chunk;
     const unsigned first_key = first_at < a.tokens ? a.keys[first_at] : 0xffffffffu;
     if (key == (unsigned)a.vocab || after != key || before == key) return;  // (one that began in an earlier chunk fills this one)
@@ -444,26 +490,32 @@ cudaError_t sort_tokens(EmbeddingGradArgs &a, const GradPlan &p, unsigned char *
     int bits = 1;
     while (bits < 32 && a.vocab >> bits) ++bits;  // the key `vocab` included
     const int passes = (bits + kDigitBits - 1) / kDigitBits, each = (bits + passes - 1) / passes;
-    SortPass s;
-    s.counts = reinterpret_cast<int *>(ws + 4 * p.list);
+    int *counts = reinterpret_cast<int *>(ws + 4 * p.list);
+    SortPass s = {};
     s.mask = (1 << each) - 1;
     int64_t per = (a.tokens + kSortBlocks - 1) / kSortBlocks;
-    if (per < 2048) per = 2048;
+    if (per < 1024) per = 1024;
     s.per = (int)((per + kSortThreads - 1) / kSortThreads * kSortThreads);
     const unsigned blocks = (unsigned)((a.tokens + s.per - 1) / s.per);
+    constexpr int kInts = kSortBlocks * kDigits;  // counts of a pass
+    s.counts = counts;
+    embedding_digits_kernel<<<blocks, kSortThreads, 0, stream>>>(a, s, counts + kInts, (passes - 1) * kInts);
+    cudaError_t e = cudaGetLastError();
+    *launches += 1;
     int to = passes % 2 ? 0 : 2;  // the last pass writes lists 0 and 1
-    s.keys = s.order = nullptr;
-    for (int i = 0; i < passes; ++i, to ^= 2) {
+    for (int i = 0; i < passes && e == cudaSuccess; ++i, to ^= 2) {
+        s.counts = counts + i * kInts;
+        s.next_counts = i + 1 < passes ? counts + (i + 1) * kInts : nullptr;
         s.shift = i * each;
+        s.next_shift = (i + 1) * each;
         s.keys_out = lists[to];
         s.order_out = lists[to + 1];
-        embedding_digits_kernel<<<blocks, kSortThreads, 0, stream>>>(a, s);
-        embedding_scatter_kernel<<<blocks, kSortThreads, 0, stream>>>(a, s);
-        *launches += 2;
+        e = launch_chained(embedding_scatter_kernel, dim3(blocks), dim3(kSortThreads), 0, stream, a, s);
+        *launches += 1;
         s.keys = lists[to];
         s.order = lists[to + 1];
     }
-    return cudaGetLastError();
+    return e;
 }
 
 template <typename G, typename O, int MODE, bool EVEN>
@@ -512,14 +564,14 @@ cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream) {
 
 size_t embedding_workspace_bytes(int64_t tokens, int dim, int sm_count) {
     const GradPlan p = plan_grad(tokens, dim, sm_count);
-    return p.list * (p.by_rank ? 2 : 4) + (p.by_rank ? 0 : kSortBlocks * kDigits * sizeof(int)) + p.parts;
+    return p.list * (p.by_rank ? 2 : 4) + (p.by_rank ? 0 : kSortPasses * kSortBlocks * kDigits * sizeof(int)) + p.parts;
 }
 
 cudaError_t launch_embedding_grad(EmbeddingGradArgs a, int sm_count, cudaStream_t stream, int *launches) {
     const GradPlan p = plan_grad(a.tokens, a.dim, sm_count);
     unsigned char *ws = static_cast<unsigned char *>(a.workspace);
     a.pad = p.pad;
-    a.parts = reinterpret_cast<float *>(ws + p.list * (p.by_rank ? 2 : 4) + (p.by_rank ? 0 : kSortBlocks * kDigits * sizeof(int)));
+    a.parts = reinterpret_cast<float *>(ws + p.list * (p.by_rank ? 2 : 4) + (p.by_rank ? 0 : kSortPasses * kSortBlocks * kDigits * sizeof(int)));
     if (a.tokens > 0) {
         const cudaError_t e = sort_tokens(a, p, ws, stream, launches);
         if (e != cudaSuccess) return e;

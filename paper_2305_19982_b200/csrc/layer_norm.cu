@@ -684,10 +684,9 @@ cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
         return cudaGetLastError();
     }
     // (uneven: four pieces where there are rows enough for that, else one or two)
-    RowPlan p = plan_rows(a.rows, pieces, sm_count, even ? 8 : 4, !even);
+    RowPlan p = plan_rows(a.rows, pieces, sm_count, even && sizeof(T) == 2 ? 8 : 4, !even);
     // rows side by side in a block, as many as its warps and an SM's shared memory have room for
-    const int most = even && sizeof(T) == 4 && p.each == 8 ? kGroupWarps / 2 : kGroupWarps;
-    p.groups = most / p.warps < 1 ? 1 : most / p.warps;
+    p.groups = kGroupWarps / p.warps;
     while (p.groups > 1 && a.rows < (int64_t)sm_count * p.groups) p.groups -= 1;
     if (even) return forward_even<T, O>(a, p, sm_count, stream);
     return p.each == 4 ? forward_odd<T, O, 4>(a, p, sm_count, stream)

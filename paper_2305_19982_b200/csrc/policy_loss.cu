@@ -12,6 +12,7 @@
 
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"
+#include "chained.cuh"
 #include "distill.cuh"
 #include "logit_ring.cuh"
 #include "row_writer.cuh"
@@ -508,6 +509,10 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             }
         }
     } else if (warp == Cut::kScalarWarp) {
+        if constexpr (kDistill<Args>) {
+            let_next_start();
+            wait_for_previous();  // for the teacher's masses; the others need nothing that was not there before that kernel
+        }
         Sums acc;
         uint32_t n = 0;  // live rows
         decltype(row_in(a, first)) next = {};
@@ -844,28 +849,32 @@ distill_long_kernel(const DistillArgs a, float k) {
 
 // ---- a distilled row's entries, before and after the row -----------------------------------------
 
-constexpr int kEntryWarps = 8;  // a row to each
+constexpr int kEntryWarps = 8;  // a row to each at a time
 
 template <typename T>
 __global__ void __launch_bounds__(32 * kEntryWarps)
 distill_teacher_kernel(const DistillArgs a) {
+    let_next_start();
     const int lane = threadIdx.x % 32;
     const int64_t row = (int64_t)blockIdx.x * kEntryWarps + threadIdx.x / 32;
-    if (row >= a.rows || a.weights[row] == 0.f) return;
+    if (row >= a.rows) return;
     RawEntries raw = {};
-    load_entries(a, row, lane, raw);
+    load_entries(a, row, lane, raw);  // whether the row counts or not: its weight is not waited for
+    const float lse = a.teacher_lse ? a.teacher_lse[row] : 0.f;
+    if (a.weights[row] == 0.f) return;
     const T *x = static_cast<const T *>(a.logits) + row * a.ld_logits;
-    float x_at[kTopEach];
+    T x_at[kTopEach];
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e) {
-        x_at[e] = 0.f;
-        if (in_use(a, e) && 32 * e + lane < a.top && raw.id[e] >= 0 && raw.id[e] < a.vocab) x_at[e] = widen(x[raw.id[e]]);
+        x_at[e] = narrow<T>(0.f);
+        if (in_use(a, e) && 32 * e + lane < a.top && raw.id[e] >= 0 && raw.id[e] < a.vocab) x_at[e] = x[raw.id[e]];
     }
-    Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
+    Entries en = entries_of(a, raw, lse, lane);
     if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e)
-        if (32 * e + lane < a.top) a.entries[row * a.top + 32 * e + lane] = make_float4(x_at[e], en.p[e], en.own[e], __int_as_float(en.id[e]));
+        if (32 * e + lane < a.top)
+            a.entries[row * a.top + 32 * e + lane] = make_float4(widen(x_at[e]), en.p[e], en.own[e], __int_as_float(en.id[e]));
     const float inner = warp_sum(en.inner);
     if (lane == 0) {
         a.masses[row] = make_float2(en.mass, inner);
@@ -878,25 +887,29 @@ __global__ void __launch_bounds__(32 * kEntryWarps)
 distill_entries_kernel(const DistillArgs a, float k) {
     __shared__ double sums[kEntryWarps][4];
     __shared__ int last;
+    wait_for_previous();
     const int lane = threadIdx.x % 32;
     Sums acc;
     for (int64_t row = (int64_t)blockIdx.x * kEntryWarps + threadIdx.x / 32; row < a.rows; row += (int64_t)gridDim.x * kEntryWarps) {
         const float weight = a.weights[row];
+        float4 q[kTopEach];  // (what a row without weight left there is not used)
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e)
+            if (32 * e + lane < a.top) q[e] = a.entries[row * a.top + 32 * e + lane];
+        const float2 of_row = a.row_stats[row], of_teacher = a.masses[row];
         if (weight == 0.f) {
             if (lane == 0 && a.loss) a.loss[row] = 0.f;
             continue;
         }
-        const float2 of_row = a.row_stats[row], of_teacher = a.masses[row];
         const float log_sum = logf(of_row.y), inv = 1.f / of_row.y, mass = of_teacher.x;
         O *y = static_cast<O *>(a.dlogits) + row * a.ld_dlogits;
         float cross = 0.f, held = 0.f;
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e)
             if (32 * e + lane < a.top) {
-                const float4 q = a.entries[row * a.top + 32 * e + lane];
-                const int id = __float_as_int(q.w);
+                const int id = __float_as_int(q[e].w);
                 if (id >= 0) {
-                    const EntryTerms o = entry_terms(q.x, q.y, q.z, mass, a.scale, weight * a.scale, of_row.x, log_sum, inv, k);
+                    const EntryTerms o = entry_terms(q[e].x, q[e].y, q[e].z, mass, a.scale, weight * a.scale, of_row.x, log_sum, inv, k);
                     cross += o.cross;
                     held += o.held;
                     if (a.dlogits) y[id] = narrow<O>(o.g);
@@ -1017,16 +1030,18 @@ template <typename T, typename O, typename Cut, typename Args>
 struct RingLaunch {
     static constexpr int kBytes = (int)sizeof(RingShared<Cut>) + 128;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr;
+    cudaLaunchAttribute attr[2];
 
     RingLaunch(int cluster, int64_t clusters, cudaStream_t stream) {
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim = {(unsigned)cluster, 1, 1};
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim = {(unsigned)cluster, 1, 1};
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // distillation: behind its first kernel
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.gridDim = dim3((unsigned)(clusters * cluster));
         cfg.blockDim = dim3(Cut::kThreads);
         cfg.dynamicSmemBytes = kBytes;
         cfg.stream = stream;
-        cfg.attrs = &attr;
+        cfg.attrs = attr;
         cfg.numAttrs = 1;
     }
     RingLaunch(const RingLaunch &) = delete;  // cfg points at attr
@@ -1066,6 +1081,7 @@ struct RingLaunch {
         if (e == cudaSuccess) e = resident(cluster, sm_count, &most);
         if (e != cudaSuccess) return e;
         RingLaunch l(cluster, a.rows < 1 ? 1 : a.rows < most ? a.rows : most, stream);
+        if (kDistill<Args> && a.rows > 0) l.cfg.numAttrs = 2;
         return cudaLaunchKernelEx(&l.cfg, policy_loss_ring_kernel<T, O, Cut, Args>, a, k, log2_of(cluster));
     }
 };
@@ -1103,8 +1119,8 @@ cudaError_t distill(const DistillArgs &a, int sm_count, cudaStream_t stream, int
     if (e != cudaSuccess) return e;
     *launches += whole ? 1 : a.rows > 0 ? 3 : 2;
     if (!whole) {
-        const unsigned grid = grid_of(rows, (int64_t)sm_count * 4);
-        distill_entries_kernel<O><<<grid, 32 * kEntryWarps, 0, stream>>>(a, (float)(a.scale_exact * kLog2e));
+        const unsigned grid = grid_of(rows, (int64_t)sm_count * 2);
+        return launch_chained(distill_entries_kernel<O>, dim3(grid), dim3(32 * kEntryWarps), 0, stream, a, (float)(a.scale_exact * kLog2e));
     }
     return cudaGetLastError();
 }
