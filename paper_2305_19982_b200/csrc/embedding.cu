@@ -13,6 +13,7 @@
 #include "adama_device.cuh"
 #include "chained.cuh"
 #include "row_access.cuh"
+#include "tensor_table.cuh"
 
 namespace adama {
 namespace {
@@ -170,7 +171,7 @@ embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
     }
     // a thread has two neighbouring digits: tokens of smaller digits, and of its digits in blocks before this one
     int total[2] = {0, 0}, earlier[2] = {0, 0};
-#pragma unroll 8
+#pragma unroll 16
     for (int b = 0; b < (int)gridDim.x; ++b) {
         const int2 n = *reinterpret_cast<const int2 *>(p.counts + b * kDigits + 2 * threadIdx.x);
         if (b < (int)blockIdx.x) {
@@ -229,28 +230,28 @@ embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
 
 enum GradMode { kWrite, kAdd, kFold };
 
-// A warp's columns of one tile, and what a finished sum meets there in memory: loaded ahead of time.
+// What a finished sum of a warp's columns of one tile meets in memory.
 template <typename O, int MODE, bool EVEN>
 struct Target {
-    Piece<O, EVEN> m;      // of kAdd: the table; of kFold: the moments
-    Piece<float, EVEN> v;
+    using First = Slot<O, EVEN>;       // of kAdd: the table; of kFold: m, then v behind it
+    static constexpr int kBytes = MODE == kAdd ? First::kBytes : MODE == kFold ? 2 * First::kBytes : 0;
+    const EmbeddingGradArgs &a;
+    int64_t at;  // of the row's tile
 
-    __device__ __forceinline__ void load(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN, 32> &c, bool wanted) {
-        const int64_t at = (int64_t)key * a.ld_grad + first;
-        if constexpr (MODE == kAdd) m.load(static_cast<const O *>(a.grad) + (wanted ? at : 0), c, 0, wanted);
+    __device__ __forceinline__ Target(const EmbeddingGradArgs &args, unsigned key, int tile) : a(args), at((int64_t)key * args.ld_grad + tile) {}
+    __device__ __forceinline__ void send_for(unsigned char *slot, const Columns<EVEN, 32> &c, int lane) const {
+        if constexpr (MODE == kAdd) First::send_for(slot, static_cast<const O *>(a.grad) + at, c, lane);
         if constexpr (MODE == kFold) {
-            m.load(a.m + (wanted ? at : 0), c, 0, wanted);
-            v.load(a.v + (wanted ? at : 0), c, 0, wanted);
+            First::send_for(slot, a.m + at, c, lane);
+            First::send_for(slot + First::kBytes, a.v + at, c, lane);
         }
     }
-    __device__ __forceinline__ void finish(const EmbeddingGradArgs &a, unsigned key, int first, const Columns<EVEN, 32> &c,
-                                           const Vec &sum) const {
-        const int64_t at = (int64_t)key * a.ld_grad + first;
+    __device__ __forceinline__ void finish(const unsigned char *slot, const Columns<EVEN, 32> &c, int lane, const Vec &sum) const {
         Vec g;
 #pragma unroll
         for (int i = 0; i < kPiece / 2; ++i) g.p[i] = mul2(sum.p[i], pair(a.scale, a.scale));
         if constexpr (MODE == kFold) {
-            Vec x = m.get(), y = v.get();
+            Vec x = First::get(slot, a.m + at, c, lane), y = First::get(slot + First::kBytes, a.v + at, c, lane);
 #pragma unroll
             for (int i = 0; i < kPiece / 2; ++i) {
                 x.p[i] = fma2(pair(a.fold.a, a.fold.a), g.p[i], x.p[i]);  // as fold1
@@ -260,7 +261,7 @@ struct Target {
             store_piece(a.v + at, c, 0, true, y);
         } else {
             if constexpr (MODE == kAdd) {
-                const Vec x = m.get();
+                const Vec x = First::get(slot, static_cast<const O *>(a.grad) + at, c, lane);
 #pragma unroll
                 for (int i = 0; i < kPiece / 2; ++i) g.p[i] = add2(g.p[i], x.p[i]);
             }
@@ -291,11 +292,19 @@ __device__ __forceinline__ void zero_row(O *p, int n, int lane) {
 }
 constexpr int kZeroRows = 8;  // rows of a warp, of those that may have no token
 
-// chunk: tokens of a warp, up to 32.  The first zero_blocks blocks zero the rows that have no token.
+// chunk: tokens of a warp, up to 16: a lane each for them and for the next chunk's.  The first zero_blocks blocks zero the rows that have no token.
+// A warp's tokens are on their way to shared memory some at a time, with what their sums will meet; the loop over them is
+// not unrolled (a batch of four in registers cost little calls 10 us of fetching instructions).
+template <int MODE>
+constexpr int kDepthOf = MODE == kWrite ? 6 : 4;
+
 template <typename G, typename O, int MODE, bool EVEN>
-__global__ void __launch_bounds__(32 * kGradWarps, MODE == kFold ? 4 : 5)
+__global__ void __launch_bounds__(32 * kGradWarps, 8)
 embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned zero_blocks) {
-    constexpr int kBatch = MODE == kWrite ? 8 : 4;  // tokens whose rows are loaded together
+    using Given = Slot<G, EVEN>;
+    using Meets = Target<O, MODE, EVEN>;
+    constexpr int kSlot = Given::kBytes + Meets::kBytes, kDepth = kDepthOf<MODE>;
+    extern __shared__ __align__(16) unsigned char slots[];  // [warps][kDepth][kSlot]
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     let_next_start();
     wait_for_previous();
@@ -321,15 +330,13 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
     const int n = (int)(a.tokens - start < chunk ? a.tokens - start : chunk);
     const unsigned none = 0xffffffffu, out = (unsigned)a.vocab;
-    const unsigned key = lane < n ? a.keys[start + lane] : none, token = lane < n ? a.order[start + lane] : 0;
-    const bool more = start + n + lane < a.tokens && lane < chunk;  // the next chunk's
-    const unsigned key2 = more ? a.keys[start + n + lane] : none, token2 = more ? a.order[start + n + lane] : 0;
+    const bool there = lane < 2 * chunk && start + lane < a.tokens;  // its tokens, then the next chunk's
+    const unsigned key = there ? a.keys[start + lane] : none, token = there ? a.order[start + lane] : 0;
     const unsigned ahead = start > 0 ? a.keys[start - 1] : none;
     const unsigned far_ahead = start > chunk ? a.keys[start - chunk - 1] : none;
-    const unsigned behind = __shfl_sync(0xffffffffu, key2, 0), first_key = __shfl_sync(0xffffffffu, key, 0);
-    const unsigned last_key = __shfl_sync(0xffffffffu, key, n - 1);
+    const unsigned first_key = __shfl_sync(0xffffffffu, key, 0), last_key = __shfl_sync(0xffffffffu, key, n - 1);
     unsigned next = __shfl_down_sync(0xffffffffu, key, 1);
-    if (lane == n - 1) next = behind;
+    if (lane == 31) next = none;
     unsigned ends = __ballot_sync(0xffffffffu, lane < n && next != key);
     const int live = __popc(__ballot_sync(0xffffffffu, lane < n && key != out));  // the others come last
     bool open = first_key == ahead;  // the first run continues the chunk before
@@ -340,98 +347,112 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     }
     // the last run's tokens in the next chunk, where it begins here and does not fill that
     const bool goes_on = live == n && !(ends >> (n - 1) & 1) && !(open && ends == 0);
-    int extra = goes_on ? __popc(__ballot_sync(0xffffffffu, key2 == last_key)) : 0;
+    int extra = goes_on ? __popc(__ballot_sync(0xffffffffu, lane >= n && key == last_key)) : 0;
     if (extra == chunk) extra = 0;
     const int count = live + extra;
+    if (extra) ends |= 1u << (count - 1);
     const G *dy = static_cast<const G *>(a.dy) + tile;
     Vec sum = zeros();
-    for (; j < count; j += kBatch) {
-        Piece<G, EVEN> raw[kBatch];
-        Target<O, MODE, EVEN> target[kBatch];
-        unsigned k[kBatch];
-        bool last[kBatch];
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q) {
-            const int at = j + q;
-            const bool in = at < count;
-            const unsigned t1 = __shfl_sync(0xffffffffu, token, at & 31), t2 = __shfl_sync(0xffffffffu, token2, (at - n) & 31);
-            k[q] = __shfl_sync(0xffffffffu, key, at < n ? at : n - 1);  // (those behind have the last one's)
-            last[q] = in && (at < n ? ends >> at & 1 : at + 1 == count);
-            raw[q].load(dy + (in ? (int64_t)(at < n ? t1 : t2) * a.ld_dy : 0), c, 0, in);
-            target[q].load(a, k[q], tile, c, last[q]);
+    unsigned char *const mine = slots + warp * (kDepth * kSlot);
+    const auto send_for = [&](int at, int slot) {
+        const unsigned t = __shfl_sync(0xffffffffu, token, at & 31), k = __shfl_sync(0xffffffffu, key, at & 31);
+        if (at < count) {
+            Given::send_for(mine + slot * kSlot, dy + (int64_t)t * a.ld_dy, c, lane);
+            if (MODE != kWrite && (ends >> at & 1)) Meets(a, k, tile).send_for(mine + slot * kSlot + Given::kBytes, c, lane);
         }
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q) {
-            add_to(sum, raw[q].get());
-            if (last[q]) {
-                if (open) store_piece(part_of(a, b, 0) + tile, c, 0, true, sum);
-                else target[q].finish(a, k[q], tile, c, sum);
-                open = false;
-                sum = zeros();
-            }
+        copies_end_group();
+    };
+    for (int i = 0; i < kDepth; ++i) send_for(j + i, i);
+    int slot = 0;
+#pragma unroll 1
+    for (; j < count; ++j) {
+        const unsigned t = __shfl_sync(0xffffffffu, token, j), k = __shfl_sync(0xffffffffu, key, j);
+        copies_wait<kDepth - 1>();
+        add_to(sum, Given::get(mine + slot * kSlot, dy + (int64_t)t * a.ld_dy, c, lane));
+        if (ends >> j & 1) {
+            if (open) store_piece(part_of(a, b, 0) + tile, c, 0, true, sum);
+            else Meets(a, k, tile).finish(mine + slot * kSlot + Given::kBytes, c, lane, sum);
+            open = false;
+            sum = zeros();
         }
+        __syncwarp();
+        send_for(j + kDepth, slot);  // behind the last use of what was there
+        slot = slot + 1 == kDepth ? 0 : slot + 1;
     }
     if (live == n && extra == 0 && !(ends >> (n - 1) & 1)) store_piece(part_of(a, b, open ? 0 : 1) + tile, c, 0, true, sum);
 }
 
-// Runs that fill chunks: block x takes the one that begins in chunk x and fills the next one, if there is one.
+// Runs that fill chunks: a block looks at 32 chunks for those that begin one, and joins the parts of these for one tile;
+// a warp to each, or the block to one of many parts.
 constexpr int kJoinWarps = 8;
-constexpr int kJoinShort = 16;  // parts up to which a warp adds them alone
+constexpr int kJoinAlone = 12;  // parts up to which a warp adds them alone
 
 template <typename O, int MODE, bool EVEN>
 __global__ void __launch_bounds__(32 * kJoinWarps)
-embedding_join_kernel(const EmbeddingGradArgs a, int chunk, int tiles) {
-    __shared__ Pair slots[kJoinWarps][kTile / 2];
+embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
+    using Meets = Target<O, MODE, EVEN>;
+    __shared__ Pair sums[kJoinWarps][kTile / 2];
+    __shared__ alignas(16) unsigned char slots[kJoinWarps][Meets::kBytes ? Meets::kBytes : 16];
+    __shared__ int64_t last_of[32];
     wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int64_t b = blockIdx.x, start = b * chunk, end = start + chunk;
-    if (end >= a.tokens) return;
-    // the key behind the next chunk's last but one place: without it the run does not fill that chunk
-    const unsigned key = a.keys[end - 1], after = end + chunk <= a.tokens ? a.keys[end + chunk - 1] : 0xffffffffu;
-    const unsigned before = start > 0 ? a.keys[start - 1] : 0xffffffffu;
-    const int64_t first_at = (b + 1 + lane) * chunk;
-    const unsigned first_key = first_at < a.tokens ? a.keys[first_at] : 0xffffffffu;
-    if (key == (unsigned)a.vocab || after != key || before == key) return;  // (one that began in an earlier chunk fills this one)
-    int64_t last = b;  // the chunk in which the run ends
-    for (bool more_to_see = true, first = true; more_to_see; first = false) {
-        const int64_t at = (last + 1 + lane) * chunk;
-        const unsigned more = __ballot_sync(0xffffffffu, first ? first_key == key : at < a.tokens && a.keys[at] == key);
-        const int run = more == 0xffffffffu ? 32 : __ffs(~more) - 1;
-        last += run;
-        more_to_see = run == 32;
-    }
-    const int64_t parts = last - b;  // behind the first one
-    const int first_tile = blockIdx.y * kJoinWarps;
-    if (parts <= kJoinShort) {
-        if (first_tile + warp >= tiles) return;
-        const int tile = (first_tile + warp) * kTile;
-        const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
-        Target<O, MODE, EVEN> target;
-        target.load(a, key, tile, c, true);
-        Vec sum = load_piece<float>(part_of(a, b, 1) + tile, c, 0, true);
+    const int tile = blockIdx.y * kTile;
+    const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
+    const unsigned none = 0xffffffffu;
+    const int64_t first = (int64_t)blockIdx.x * 32, start = (first + lane) * chunk, end = start + chunk;
+    // it begins one that fills the next chunk: the same key at its own end and at that chunk's, another one in front of it
+    const unsigned key = end <= a.tokens ? a.keys[end - 1] : none, far = end + chunk <= a.tokens ? a.keys[end + chunk - 1] : none - 1;
+    const unsigned before = start > 0 && start <= a.tokens ? a.keys[start - 1] : none;
+    unsigned todo = __ballot_sync(none, key == far && key != before && key != (unsigned)a.vocab);
+    if (todo == 0) return;  // (all warps see the same)
+    const auto sum_parts = [&](Vec &sum, int64_t from, int64_t to) {
 #pragma unroll 4
-        for (int64_t i = b + 1; i <= last; ++i) add_to(sum, load_piece<float>(part_of(a, i, 0) + tile, c, 0, true));
-        target.finish(a, key, tile, c, sum);
-        return;
+        for (int64_t i = from; i < to; ++i) add_to(sum, load_piece(part_of(a, i, 0) + tile, c, 0, true));
+    };
+    unsigned of_block = 0;
+    for (int turn = 0; todo; todo &= todo - 1, ++turn) {
+        const int which = __ffs(todo) - 1;
+        const unsigned k = __shfl_sync(none, key, which);
+        const int64_t b = first + which;
+        int64_t last = b;  // the chunk in which the run ends
+        for (int run = 32; run == 32; last += run) {
+            const int64_t at = (last + 1 + lane) * chunk;
+            const unsigned more = __ballot_sync(none, at < a.tokens && a.keys[at] == k);
+            run = more == none ? 32 : __ffs(~more) - 1;
+        }
+        if (last - b > kJoinAlone) {
+            of_block |= 1u << which;
+            last_of[which] = last;  // (every warp writes the same)
+            continue;
+        }
+        if (turn % kJoinWarps != warp) continue;
+        const Meets meets(a, k, tile);
+        meets.send_for(slots[warp], c, lane);
+        copies_end_group();
+        Vec sum = load_piece(part_of(a, b, 1) + tile, c, 0, true);
+        sum_parts(sum, b + 1, last + 1);
+        copies_wait<0>();
+        meets.finish(slots[warp], c, lane, sum);
+        __syncwarp();
     }
-    // long: the warps share the parts of a tile, one tile after the other
-    for (int i = first_tile; i < tiles && i < first_tile + kJoinWarps; ++i) {
-        const int tile = i * kTile;
-        const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
-        const int64_t from = b + 1 + parts * warp / kJoinWarps, to = b + 1 + parts * (warp + 1) / kJoinWarps;
-        Vec sum = load_piece<float>(part_of(a, b, 1) + tile, c, 0, warp == 0);
-#pragma unroll 4
-        for (int64_t j = from; j < to; ++j) add_to(sum, load_piece<float>(part_of(a, j, 0) + tile, c, 0, true));
+    for (; of_block; of_block &= of_block - 1) {
+        const int which = __ffs(of_block) - 1;
+        const unsigned k = __shfl_sync(none, key, which);
+        const int64_t b = first + which, parts = last_of[which] - b;
+        Vec sum = warp == 0 ? load_piece(part_of(a, b, 1) + tile, c, 0, true) : zeros();
+        sum_parts(sum, b + 1 + parts * warp / kJoinWarps, b + 1 + parts * (warp + 1) / kJoinWarps);
 #pragma unroll
-        for (int q = 0; q < kPiece / 2; ++q) slots[warp][q * 32 + lane] = sum.p[q];
+        for (int q = 0; q < kPiece / 2; ++q) sums[warp][q * 32 + lane] = sum.p[q];
         __syncthreads();
         if (warp == 0) {
-            Target<O, MODE, EVEN> target;
-            target.load(a, key, tile, c, true);
+            const Meets meets(a, k, tile);
+            meets.send_for(slots[0], c, lane);
+            copies_end_group();
             for (int w = 1; w < kJoinWarps; ++w)
 #pragma unroll
-                for (int q = 0; q < kPiece / 2; ++q) sum.p[q] = add2(sum.p[q], slots[w][q * 32 + lane]);
-            target.finish(a, key, tile, c, sum);
+                for (int q = 0; q < kPiece / 2; ++q) sum.p[q] = add2(sum.p[q], sums[w][q * 32 + lane]);
+            copies_wait<0>();
+            meets.finish(slots[0], c, lane, sum);
         }
         __syncthreads();
     }
@@ -453,12 +474,8 @@ cudaError_t lookup(const EmbeddingArgs &a, cudaStream_t stream) {
 // Sizes of the parts of the workspace, each a multiple of 16 bytes.
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
-// Tokens to a chunk: as many as leave every SM a dozen warps, 32 at most (a lane each).
-int chunk_for(int64_t tokens, int tiles, int sm_count) {
-    int chunk = 32;
-    while (chunk > 8 && tokens * tiles / chunk < (int64_t)12 * sm_count) chunk /= 2;
-    return chunk;
-}
+// Tokens to a chunk: 16 where that makes several rounds of warps.
+int chunk_for(int64_t tokens, int tiles, int sm_count) { return tokens * tiles / 16 < (int64_t)48 * sm_count ? 8 : 16; }
 struct GradPlan {
     int tiles, chunk;
     int64_t chunks, pad;
@@ -524,18 +541,24 @@ cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t str
     const int64_t zero_blocks = MODE == kWrite ? (a.vocab + kZeroRows * kGradWarps - 1) / (kZeroRows * kGradWarps) : 0;
     if (sum_blocks + zero_blocks == 0) return cudaSuccess;
     const dim3 grid((unsigned)(sum_blocks + zero_blocks)), block(32 * kGradWarps);
-    cudaError_t e;
+    const size_t shared = (size_t)kGradWarps * kDepthOf<MODE> * (Slot<G, EVEN>::kBytes + Target<O, MODE, EVEN>::kBytes);
+    cudaError_t e = cudaSuccess;
+    if (shared > 40 * 1024) {  // more than a kernel has unasked
+        static std::atomic<unsigned long long> ready{0};
+        e = allow_shared(embedding_grad_kernel<G, O, MODE, EVEN>, (int)shared, ready);
+        if (e != cudaSuccess) return e;
+    }
     if (a.tokens > 0) {
-        e = launch_chained(embedding_grad_kernel<G, O, MODE, EVEN>, grid, block, 0, stream, a, p.chunk, p.tiles, (unsigned)zero_blocks);
+        e = launch_chained(embedding_grad_kernel<G, O, MODE, EVEN>, grid, block, shared, stream, a, p.chunk, p.tiles, (unsigned)zero_blocks);
     } else {  // no sort in front
-        embedding_grad_kernel<G, O, MODE, EVEN><<<grid, block, 0, stream>>>(a, p.chunk, p.tiles, (unsigned)zero_blocks);
+        embedding_grad_kernel<G, O, MODE, EVEN><<<grid, block, shared, stream>>>(a, p.chunk, p.tiles, (unsigned)zero_blocks);
         e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
     *launches += 1;
     if (p.chunks > 1) {
-        const dim3 joins((unsigned)(p.chunks - 1), (unsigned)((p.tiles + kJoinWarps - 1) / kJoinWarps));
-        e = launch_chained(embedding_join_kernel<O, MODE, EVEN>, joins, dim3(32 * kJoinWarps), 0, stream, a, p.chunk, p.tiles);
+        const dim3 joins((unsigned)((p.chunks + 31) / 32), (unsigned)p.tiles);
+        e = launch_chained(embedding_join_kernel<O, MODE, EVEN>, joins, dim3(32 * kJoinWarps), 0, stream, a, p.chunk);
         *launches += 1;
     }
     return e;

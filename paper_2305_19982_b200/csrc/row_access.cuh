@@ -75,10 +75,9 @@ struct Piece {
         if constexpr (EVEN) {
             const uint4 *from = reinterpret_cast<const uint4 *>(row + c.at(u, 0));
 #pragma unroll
-            for (int i = 0; i < kUnits; ++i) even[i] = make_uint4(0, 0, 0, 0);
-            if (live && c.has(u, 0)) {
-#pragma unroll
-                for (int i = 0; i < kUnits; ++i) even[i] = from[i];
+            for (int i = 0; i < kUnits; ++i) {
+                even[i] = make_uint4(0, 0, 0, 0);
+                if (live && c.has(u, 0)) even[i] = from[i];
             }
         } else {
             const T *from = row + c.t;
@@ -153,16 +152,59 @@ inline bool even_rows(const void *p, int64_t cols, int64_t ld, int size) {
     return aligned(p, 16) && cols % kPiece == 0 && ld * size % 16 == 0;
 }
 
-// ---- rows ahead -----------------------------------------------------------------------------------
-// A thread's own pieces of the next rows on their way to shared memory (asynchronous copies that the thread itself waits
-// for: no other one reads them), or, of uneven rows, of the next row to registers.
+// ---- pieces ahead ----------------------------------------------------------------------------------
+// Asynchronous copies to shared memory that the thread itself waits for: no other one reads them.
 __device__ __forceinline__ void copy16(uint32_t to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void *from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() {  // for all but the last N groups
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+
+// A lane's piece in a slot of its warp's, which is kBytes long.  Two-byte elements of uneven rows cannot come that way.
+template <typename T, bool EVEN>
+struct Slot {
+    static constexpr bool kCopied = EVEN || sizeof(T) == 4;
+    static constexpr int kBytes = kCopied ? 32 * kPiece * (int)sizeof(T) : 0;
+    static constexpr int kUnits = kPiece * sizeof(T) / 16;
+
+    template <int W>
+    static __device__ __forceinline__ void send_for(unsigned char *slot, const T *row, const Columns<EVEN, W> &c, int lane) {
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
+        if constexpr (EVEN) {
+            if (c.has(0, 0)) {
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i) copy16(to + (32 * i + lane) * 16, reinterpret_cast<const uint4 *>(row + c.at(0, 0)) + i);
+            }
+        } else if constexpr (kCopied) {
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i)
+                if (c.has(0, i)) copy4(to + (32 * i + lane) * 4, row + c.at(0, i));
+        }
+    }
+    template <int W>
+    static __device__ __forceinline__ Vec get(const unsigned char *slot, const T *row, const Columns<EVEN, W> &c, int lane) {
+        if constexpr (EVEN) {
+            uint4 u[kUnits];
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) u[i] = c.has(0, 0) ? reinterpret_cast<const uint4 *>(slot)[32 * i + lane] : make_uint4(0, 0, 0, 0);
+            return widened(u);
+        } else if constexpr (kCopied) {
+            Vec v;
+            const float *f = reinterpret_cast<const float *>(slot) + lane;
+#pragma unroll
+            for (int i = 0; i < kPiece / 2; ++i)
+                v.p[i] = pair(c.has(0, 2 * i) ? f[64 * i] : 0.f, c.has(0, 2 * i + 1) ? f[64 * i + 32] : 0.f);
+            return v;
+        } else {
+            return load_piece(row, c, 0, true);
+        }
+    }
+};
 
 }  // namespace adama
