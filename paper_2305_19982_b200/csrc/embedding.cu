@@ -35,7 +35,7 @@ embedding_kernel(const EmbeddingArgs a, int groups) {
     if (token >= a.tokens) return;
     const int64_t id = a.ids[token];
     const bool inside = id >= 0 && id < a.vocab;
-    const Columns<EVEN, 32> c = {lane, 32, a.dim - first};
+    const Columns<EVEN, together(sizeof(T), sizeof(O)), 32> c = {lane, 32, a.dim - first};
     const T *row = static_cast<const T *>(a.table) + (inside ? id * a.ld_table : 0) + first;
     O *out = static_cast<O *>(a.out) + token * a.ld_out + first;
     Piece<T, EVEN> raw[kLookupPieces];
@@ -231,27 +231,27 @@ embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
 enum GradMode { kWrite, kAdd, kFold };
 
 // What a finished sum of a warp's columns of one tile meets in memory.
-template <typename O, int MODE, bool EVEN>
+template <typename O, int MODE, bool EVEN, int N>
 struct Target {
     using First = Slot<O, EVEN>;       // of kAdd: the table; of kFold: m, then v behind it
-    static constexpr int kBytes = MODE == kAdd ? First::kBytes : MODE == kFold ? 2 * First::kBytes : 0;
+    static constexpr int kBytes = 32 * (MODE == kAdd ? First::kBytes : MODE == kFold ? 2 * First::kBytes : 0);
     const EmbeddingGradArgs &a;
     int64_t at;  // of the row's tile
 
     __device__ __forceinline__ Target(const EmbeddingGradArgs &args, unsigned key, int tile) : a(args), at((int64_t)key * args.ld_grad + tile) {}
-    __device__ __forceinline__ void send_for(unsigned char *slot, const Columns<EVEN, 32> &c, int lane) const {
-        if constexpr (MODE == kAdd) First::send_for(slot, static_cast<const O *>(a.grad) + at, c, lane);
+    __device__ __forceinline__ void send_for(unsigned char *slot, const Columns<EVEN, N, 32> &c, int lane) const {
+        if constexpr (MODE == kAdd) First::send_for(slot, static_cast<const O *>(a.grad) + at, c, 0, lane, 32);
         if constexpr (MODE == kFold) {
-            First::send_for(slot, a.m + at, c, lane);
-            First::send_for(slot + First::kBytes, a.v + at, c, lane);
+            First::send_for(slot, a.m + at, c, 0, lane, 32);
+            First::send_for(slot + 32 * First::kBytes, a.v + at, c, 0, lane, 32);
         }
     }
-    __device__ __forceinline__ void finish(const unsigned char *slot, const Columns<EVEN, 32> &c, int lane, const Vec &sum) const {
+    __device__ __forceinline__ void finish(const unsigned char *slot, const Columns<EVEN, N, 32> &c, int lane, const Vec &sum) const {
         Vec g;
 #pragma unroll
         for (int i = 0; i < kPiece / 2; ++i) g.p[i] = mul2(sum.p[i], pair(a.scale, a.scale));
         if constexpr (MODE == kFold) {
-            Vec x = First::get(slot, a.m + at, c, lane), y = First::get(slot + First::kBytes, a.v + at, c, lane);
+            Vec x = First::get(slot, a.m + at, c, 0, lane, 32), y = First::get(slot + 32 * First::kBytes, a.v + at, c, 0, lane, 32);
 #pragma unroll
             for (int i = 0; i < kPiece / 2; ++i) {
                 x.p[i] = fma2(pair(a.fold.a, a.fold.a), g.p[i], x.p[i]);  // as fold1
@@ -261,7 +261,7 @@ struct Target {
             store_piece(a.v + at, c, 0, true, y);
         } else {
             if constexpr (MODE == kAdd) {
-                const Vec x = First::get(slot, static_cast<const O *>(a.grad) + at, c, lane);
+                const Vec x = First::get(slot, static_cast<const O *>(a.grad) + at, c, 0, lane, 32);
 #pragma unroll
                 for (int i = 0; i < kPiece / 2; ++i) g.p[i] = add2(g.p[i], x.p[i]);
             }
@@ -302,12 +302,13 @@ template <typename G, typename O, int MODE, bool EVEN>
 __global__ void __launch_bounds__(32 * kGradWarps, 8)
 embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned zero_blocks) {
     using Given = Slot<G, EVEN>;
-    using Meets = Target<O, MODE, EVEN>;
-    constexpr int kSlot = Given::kBytes + Meets::kBytes, kDepth = kDepthOf<MODE>;
+    constexpr int N = together(sizeof(G), sizeof(O));
+    using Meets = Target<O, MODE, EVEN, N>;
+    constexpr int kGiven = 32 * Given::kBytes, kSlot = kGiven + Meets::kBytes, kDepth = kDepthOf<MODE>;
     extern __shared__ __align__(16) unsigned char slots[];  // [warps][kDepth][kSlot]
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    let_next_start();
     wait_for_previous();
+    let_next_start();  // the sorted tokens are there for the next kernel, too
     if (MODE == kWrite && blockIdx.x < zero_blocks) {
         const int64_t first = ((int64_t)blockIdx.x * kGradWarps + warp) * kZeroRows;
         const int64_t row = first + lane;
@@ -327,7 +328,7 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     const int64_t start = b * chunk;
     if (start >= a.tokens) return;
     const int tile = (int)(task - b * tiles) * kTile;
-    const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
+    const Columns<EVEN, N, 32> c = {lane, 32, a.dim - tile};
     const int n = (int)(a.tokens - start < chunk ? a.tokens - start : chunk);
     const unsigned none = 0xffffffffu, out = (unsigned)a.vocab;
     const bool there = lane < 2 * chunk && start + lane < a.tokens;  // its tokens, then the next chunk's
@@ -357,8 +358,8 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     const auto send_for = [&](int at, int slot) {
         const unsigned t = __shfl_sync(0xffffffffu, token, at & 31), k = __shfl_sync(0xffffffffu, key, at & 31);
         if (at < count) {
-            Given::send_for(mine + slot * kSlot, dy + (int64_t)t * a.ld_dy, c, lane);
-            if (MODE != kWrite && (ends >> at & 1)) Meets(a, k, tile).send_for(mine + slot * kSlot + Given::kBytes, c, lane);
+            Given::send_for(mine + slot * kSlot, dy + (int64_t)t * a.ld_dy, c, 0, lane, 32);
+            if (MODE != kWrite && (ends >> at & 1)) Meets(a, k, tile).send_for(mine + slot * kSlot + kGiven, c, lane);
         }
         copies_end_group();
     };
@@ -368,10 +369,10 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
     for (; j < count; ++j) {
         const unsigned t = __shfl_sync(0xffffffffu, token, j), k = __shfl_sync(0xffffffffu, key, j);
         copies_wait<kDepth - 1>();
-        add_to(sum, Given::get(mine + slot * kSlot, dy + (int64_t)t * a.ld_dy, c, lane));
+        add_to(sum, Given::get(mine + slot * kSlot, dy + (int64_t)t * a.ld_dy, c, 0, lane, 32));
         if (ends >> j & 1) {
             if (open) store_piece(part_of(a, b, 0) + tile, c, 0, true, sum);
-            else Meets(a, k, tile).finish(mine + slot * kSlot + Given::kBytes, c, lane, sum);
+            else Meets(a, k, tile).finish(mine + slot * kSlot + kGiven, c, lane, sum);
             open = false;
             sum = zeros();
         }
@@ -387,57 +388,61 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
 constexpr int kJoinWarps = 8;
 constexpr int kJoinAlone = 12;  // parts up to which a warp adds them alone
 
-template <typename O, int MODE, bool EVEN>
+template <typename O, int MODE, bool EVEN, int N>
 __global__ void __launch_bounds__(32 * kJoinWarps)
 embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
-    using Meets = Target<O, MODE, EVEN>;
+    using Meets = Target<O, MODE, EVEN, N>;
     __shared__ Pair sums[kJoinWarps][kTile / 2];
     __shared__ alignas(16) unsigned char slots[kJoinWarps][Meets::kBytes ? Meets::kBytes : 16];
     __shared__ int64_t last_of[32];
-    wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int tile = blockIdx.y * kTile;
-    const Columns<EVEN, 32> c = {lane, 32, a.dim - tile};
+    const Columns<EVEN, N, 32> c = {lane, 32, a.dim - tile};
     const unsigned none = 0xffffffffu;
     const int64_t first = (int64_t)blockIdx.x * 32, start = (first + lane) * chunk, end = start + chunk;
-    // it begins one that fills the next chunk: the same key at its own end and at that chunk's, another one in front of it
+    // The sort has ended when this kernel may start (the sums wait for it first): the runs are looked up while the sums are
+    // still being made, and what the first one of a warp will meet is sent for.  A run begins in a chunk and fills the
+    // next one: the same key at its own end and at that chunk's, another one in front of it.
     const unsigned key = end <= a.tokens ? a.keys[end - 1] : none, far = end + chunk <= a.tokens ? a.keys[end + chunk - 1] : none - 1;
     const unsigned before = start > 0 && start <= a.tokens ? a.keys[start - 1] : none;
-    unsigned todo = __ballot_sync(none, key == far && key != before && key != (unsigned)a.vocab);
-    if (todo == 0) return;  // (all warps see the same)
-    const auto sum_parts = [&](Vec &sum, int64_t from, int64_t to) {
-#pragma unroll 4
-        for (int64_t i = from; i < to; ++i) add_to(sum, load_piece(part_of(a, i, 0) + tile, c, 0, true));
-    };
-    unsigned of_block = 0;
-    for (int turn = 0; todo; todo &= todo - 1, ++turn) {
+    unsigned todo = __ballot_sync(none, key == far && key != before && key != (unsigned)a.vocab), of_warp = 0, of_block = 0;
+    for (int turn = 0; todo; todo &= todo - 1) {  // (all warps see the same)
         const int which = __ffs(todo) - 1;
         const unsigned k = __shfl_sync(none, key, which);
-        const int64_t b = first + which;
-        int64_t last = b;  // the chunk in which the run ends
+        int64_t last = first + which;  // the chunk in which the run ends
         for (int run = 32; run == 32; last += run) {
             const int64_t at = (last + 1 + lane) * chunk;
             const unsigned more = __ballot_sync(none, at < a.tokens && a.keys[at] == k);
             run = more == none ? 32 : __ffs(~more) - 1;
         }
-        if (last - b > kJoinAlone) {
-            of_block |= 1u << which;
-            last_of[which] = last;  // (every warp writes the same)
-            continue;
+        if (lane == 0) last_of[which] = last;  // (every warp writes the same)
+        if (last - first - which > kJoinAlone) of_block |= 1u << which;
+        else if (turn++ % kJoinWarps == warp) of_warp |= 1u << which;
+    }
+    __syncwarp();
+    const int ahead = of_warp ? __ffs(of_warp) - 1 : -1;
+    if (ahead >= 0) Meets(a, __shfl_sync(none, key, ahead), tile).send_for(slots[warp], c, lane);
+    copies_end_group();
+    wait_for_previous();
+    const auto sum_parts = [&](Vec &sum, int64_t from, int64_t to) {
+#pragma unroll 4
+        for (int64_t i = from; i < to; ++i) add_to(sum, load_piece(part_of(a, i, 0) + tile, c, 0, true));
+    };
+    for (; of_warp; of_warp &= of_warp - 1) {
+        const int which = __ffs(of_warp) - 1;
+        const Meets meets(a, __shfl_sync(none, key, which), tile);
+        if (which != ahead) {
+            meets.send_for(slots[warp], c, lane);
+            copies_end_group();
         }
-        if (turn % kJoinWarps != warp) continue;
-        const Meets meets(a, k, tile);
-        meets.send_for(slots[warp], c, lane);
-        copies_end_group();
-        Vec sum = load_piece(part_of(a, b, 1) + tile, c, 0, true);
-        sum_parts(sum, b + 1, last + 1);
+        Vec sum = load_piece(part_of(a, first + which, 1) + tile, c, 0, true);
+        sum_parts(sum, first + which + 1, last_of[which] + 1);
         copies_wait<0>();
         meets.finish(slots[warp], c, lane, sum);
-        __syncwarp();
     }
+    copies_wait<0>();
     for (; of_block; of_block &= of_block - 1) {
         const int which = __ffs(of_block) - 1;
-        const unsigned k = __shfl_sync(none, key, which);
         const int64_t b = first + which, parts = last_of[which] - b;
         Vec sum = warp == 0 ? load_piece(part_of(a, b, 1) + tile, c, 0, true) : zeros();
         sum_parts(sum, b + 1 + parts * warp / kJoinWarps, b + 1 + parts * (warp + 1) / kJoinWarps);
@@ -445,7 +450,7 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
         for (int q = 0; q < kPiece / 2; ++q) sums[warp][q * 32 + lane] = sum.p[q];
         __syncthreads();
         if (warp == 0) {
-            const Meets meets(a, k, tile);
+            const Meets meets(a, __shfl_sync(none, key, which), tile);
             meets.send_for(slots[0], c, lane);
             copies_end_group();
             for (int w = 1; w < kJoinWarps; ++w)
@@ -541,7 +546,7 @@ cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t str
     const int64_t zero_blocks = MODE == kWrite ? (a.vocab + kZeroRows * kGradWarps - 1) / (kZeroRows * kGradWarps) : 0;
     if (sum_blocks + zero_blocks == 0) return cudaSuccess;
     const dim3 grid((unsigned)(sum_blocks + zero_blocks)), block(32 * kGradWarps);
-    const size_t shared = (size_t)kGradWarps * kDepthOf<MODE> * (Slot<G, EVEN>::kBytes + Target<O, MODE, EVEN>::kBytes);
+    const size_t shared = (size_t)kGradWarps * kDepthOf<MODE> * (32 * Slot<G, EVEN>::kBytes + Target<O, MODE, EVEN, 8>::kBytes);
     cudaError_t e = cudaSuccess;
     if (shared > 40 * 1024) {  // more than a kernel has unasked
         static std::atomic<unsigned long long> ready{0};
@@ -558,7 +563,7 @@ cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t str
     *launches += 1;
     if (p.chunks > 1) {
         const dim3 joins((unsigned)((p.chunks + 31) / 32), (unsigned)p.tiles);
-        e = launch_chained(embedding_join_kernel<O, MODE, EVEN>, joins, dim3(32 * kJoinWarps), 0, stream, a, p.chunk);
+        e = launch_chained(embedding_join_kernel<O, MODE, EVEN, together(sizeof(G), sizeof(O))>, joins, dim3(32 * kJoinWarps), 0, stream, a, p.chunk);
         *launches += 1;
     }
     return e;

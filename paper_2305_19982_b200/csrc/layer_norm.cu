@@ -62,8 +62,8 @@ __device__ __forceinline__ Vec sum_of(const Vec &a, const Vec &b) {
 }
 __device__ __forceinline__ Pair sum_of(const Vec &v) { return add2(add2(v.p[0], v.p[1]), add2(v.p[2], v.p[3])); }
 // v becomes its distance from the mean; returns that squared, summed.  Columns that the row does not have lie at none.
-template <bool EVEN, int W>
-__device__ __forceinline__ Pair centre(Vec &v, const Columns<EVEN, W> &c, int u, float mean) {
+template <bool EVEN, int N, int W>
+__device__ __forceinline__ Pair centre(Vec &v, const Columns<EVEN, N, W> &c, int u, float mean) {
     if constexpr (!EVEN) {
 #pragma unroll
         for (int i = 0; i < kPiece / 2; ++i) {
@@ -72,13 +72,13 @@ __device__ __forceinline__ Pair centre(Vec &v, const Columns<EVEN, W> &c, int u,
             v.p[i] = pair(c.has(u, 2 * i) ? a : mean, c.has(u, 2 * i + 1) ? b : mean);
         }
     }
-    Pair s = 0;
+    Pair s[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < kPiece / 2; ++i) {
         v.p[i] = add2(v.p[i], pair(-mean, -mean));
-        s = fma2(v.p[i], v.p[i], s);
+        s[i / 2] = fma2(v.p[i], v.p[i], s[i / 2]);
     }
-    return EVEN && !c.has(u, 0) ? 0 : s;
+    return add2(EVEN && !c.has(u, 0) ? 0 : s[0], EVEN && !c.has(u, kPiece / 2) ? 0 : s[1]);
 }
 __device__ __forceinline__ void scale_shift(Vec &v, float rstd, const Vec &w, const Vec &b) {
 #pragma unroll
@@ -93,7 +93,7 @@ constexpr int kShortThreads = 128;
 template <typename T, typename O, bool EVEN>
 __global__ void __launch_bounds__(kShortThreads)
 layer_norm_short_kernel(const NormArgs a, int lanes) {
-    const Columns<EVEN> c = {(int)threadIdx.x % lanes, lanes, a.dim};
+    const Columns<EVEN, together(sizeof(T), sizeof(O))> c = {(int)threadIdx.x % lanes, lanes, a.dim};
     const int64_t row = (int64_t)blockIdx.x * (kShortThreads / lanes) + threadIdx.x / lanes;
     const bool live = row < a.rows;
     Piece<T, EVEN> raw;
@@ -123,25 +123,21 @@ __global__ void __launch_bounds__(32 * kGroupWarps)
 layer_norm_kernel(const NormArgs a, int warps) {
     extern __shared__ uint4 shared[];  // even: [pieces][2][threads of a row] of weight, of bias, then [rows ahead][U][units][threads]
     __shared__ float slots[2][kGroupWarps];
-    constexpr int kUnits = Piece<T, true>::kUnits;
+    constexpr int N = together(sizeof(T), sizeof(O));
+    using Ahead = Slot<T, EVEN>;
     const Group group(WARPS ? WARPS : warps);
-    const Columns<EVEN, 32 * WARPS> c = {group.t, 32 * warps, a.dim};
+    const Columns<EVEN, N, 32 * WARPS> c = {group.t, 32 * warps, a.dim};
     const T *x0 = static_cast<const T *>(a.x);
     const int64_t step = (int64_t)gridDim.x * group.count;
     int64_t row = (int64_t)blockIdx.x * group.count + group.index;
-    uint4 *const params = shared, *const ahead = shared + 4 * U * c.width();
+    uint4 *const params = shared;
+    unsigned char *const ahead = reinterpret_cast<unsigned char *>(shared + 4 * U * c.width());
     float *const odd_params = reinterpret_cast<float *>(shared);  // uneven: weight, bias
-    const auto slot = [&](int stage, int u, int i) { return ahead + ((stage * U + u) * kUnits + i) * blockDim.x + threadIdx.x; };
+    const auto slot = [&](int stage, int u) { return ahead + (stage * U + u) * (int)blockDim.x * Ahead::kBytes; };
     const auto send_for = [&](int64_t r, int stage) {
         if (r < a.rows) {
-            const uint4 *from = reinterpret_cast<const uint4 *>(x0 + r * a.ld_x) + c.t * kUnits;
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (c.has(u, 0)) {
-#pragma unroll
-                    for (int i = 0; i < kUnits; ++i)
-                        copy16((uint32_t)__cvta_generic_to_shared(slot(stage, u, i)), from + u * c.width() * kUnits + i);
-                }
+            for (int u = 0; u < U; ++u) Ahead::send_for(slot(stage, u), x0 + r * a.ld_x, c, u, threadIdx.x, blockDim.x);
         }
         copies_end_group();
     };
@@ -149,8 +145,9 @@ layer_norm_kernel(const NormArgs a, int warps) {
         for (int i = 0; i < kAhead; ++i) send_for(row + i * step, i);
         const uint4 zero = make_uint4(0, 0, 0, 0);
         for (int i = threadIdx.x; i < 2 * U * c.width(); i += blockDim.x) {
-            const int piece = i / 2, at = ((piece / c.width()) * 2 + i % 2) * c.width() + piece % c.width();
-            const bool has = piece * kPiece < a.dim;
+            // fours of columns, in the order in which a piece's halves lie
+            const int piece = i / 2, at = N == 4 ? i : ((piece / c.width()) * 2 + i % 2) * c.width() + piece % c.width();
+            const bool has = i * 4 < a.dim;
             params[at] = has ? reinterpret_cast<const uint4 *>(a.weight)[i] : zero;
             params[2 * U * c.width() + at] = has && a.bias ? reinterpret_cast<const uint4 *>(a.bias)[i] : zero;
         }
@@ -165,22 +162,19 @@ layer_norm_kernel(const NormArgs a, int warps) {
     for (int stage = 0; row < a.rows; row += step, stage = stage + 1 == kAhead ? 0 : stage + 1) {
         Vec v[U];
         Pair s = 0;
-        Piece<T, EVEN> raw[U];
         if constexpr (EVEN) {
             copies_wait<kAhead - 1>();
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < kUnits; ++i) raw[u].even[i] = c.has(u, 0) ? *slot(stage, u, i) : make_uint4(0, 0, 0, 0);
+            for (int u = 0; u < U; ++u) v[u] = Ahead::get(slot(stage, u), x0, c, u, threadIdx.x, blockDim.x);
         } else {
+            Piece<T, EVEN> raw[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) raw[u].load(x0 + row * a.ld_x, c, u, true);
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = raw[u].get();
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            v[u] = raw[u].get();
-            s = add2(s, sum_of(v[u]));
-        }
+        for (int u = 0; u < U; ++u) s = add2(s, sum_of(v[u]));
         const float mean = share(group.sum(pair_sum(s), slots[0]), n, a.inv_dim);
         if constexpr (EVEN) send_for(row + kAhead * step, stage);  // what was there has been summed up
         s = 0;
@@ -283,7 +277,7 @@ __global__ void __launch_bounds__(kLanesThreads)
 layer_norm_backward_short_kernel(const NormBackArgs a, int lanes) {
     __shared__ alignas(16) float total[2 * 32 * kPiece];
     let_next_start();
-    const Columns<EVEN> c = {(int)threadIdx.x % lanes, lanes, a.dim};
+    const Columns<EVEN, together(sizeof(T), sizeof(G))> c = {(int)threadIdx.x % lanes, lanes, a.dim};
     const int groups = kLanesThreads / lanes;
     const T *x0 = static_cast<const T *>(a.x);
     const G *dy0 = static_cast<const G *>(a.dy);
@@ -358,33 +352,31 @@ constexpr int kPairsAhead = 2;
 template <typename T, typename G, int U, bool EVEN, int WARPS>
 __global__ void __launch_bounds__(32 * kGroupWarps)
 layer_norm_backward_kernel(const NormBackArgs a, int warps) {
-    constexpr int kUnitsX = Piece<T, true>::kUnits, kUnits = kUnitsX + Piece<G, true>::kUnits;
-    extern __shared__ uint4 ahead[];  // [pairs ahead][2][U][units of both pieces][threads]; at the end two sums of each column
+    constexpr int N = together(sizeof(T), sizeof(G));
+    using AheadX = Slot<T, EVEN>;
+    using AheadDy = Slot<G, EVEN>;
+    constexpr int kBytes = AheadX::kBytes + AheadDy::kBytes;
+    extern __shared__ __align__(16) unsigned char ahead[];  // [pairs ahead][2][U][both pieces of all threads]; at the end two sums of each column
     __shared__ alignas(16) float slots[2][kGroupWarps][4];
     let_next_start();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const Group group(WARPS ? WARPS : warps);
-    const Columns<EVEN, 32 * WARPS> c = {group.t, 32 * warps, a.dim};
+    const Columns<EVEN, N, 32 * WARPS> c = {group.t, 32 * warps, a.dim};
     const T *x0 = static_cast<const T *>(a.x);
     const G *dy0 = static_cast<const G *>(a.dy);
     const int64_t step = (int64_t)gridDim.x * group.count;  // of a group's rows; it takes rows row and row + step together
     int64_t row = (int64_t)blockIdx.x * group.count + group.index;
-    const auto slot = [&](int stage, int r, int u, int i) { return ahead + (((stage * 2 + r) * U + u) * kUnits + i) * blockDim.x + threadIdx.x; };
+    const auto slot = [&](int stage, int r, int u) { return ahead + ((stage * 2 + r) * U + u) * (int)blockDim.x * kBytes; };
     const auto send_for = [&](int64_t first, int stage) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const int64_t at = first + r * step;
             if (at >= a.rows) continue;
-            const uint4 *fx = reinterpret_cast<const uint4 *>(x0 + at * a.ld_x) + c.t * kUnitsX;
-            const uint4 *fdy = reinterpret_cast<const uint4 *>(dy0 + at * a.ld_dy) + c.t * (kUnits - kUnitsX);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (c.has(u, 0)) {
-#pragma unroll
-                    for (int i = 0; i < kUnits; ++i)
-                        copy16((uint32_t)__cvta_generic_to_shared(slot(stage, r, u, i)),
-                               i < kUnitsX ? fx + u * c.width() * kUnitsX + i : fdy + u * c.width() * (kUnits - kUnitsX) + (i - kUnitsX));
-                }
+            for (int u = 0; u < U; ++u) {
+                AheadX::send_for(slot(stage, r, u), x0 + at * a.ld_x, c, u, threadIdx.x, blockDim.x);
+                AheadDy::send_for(slot(stage, r, u) + blockDim.x * AheadX::kBytes, dy0 + at * a.ld_dy, c, u, threadIdx.x, blockDim.x);
+            }
         }
         copies_end_group();
     };
@@ -410,17 +402,8 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
     // a piece of the pair's row r
     const auto get = [&](int stage, int r, int u, bool live, Vec &x, Vec &dy) {
         if constexpr (EVEN) {
-            Piece<T, true> px;
-            Piece<G, true> pdy;
-            const bool has = live && c.has(u, 0);
-#pragma unroll
-            for (int i = 0; i < kUnits; ++i) {
-                const uint4 q = has ? *slot(stage, r, u, i) : make_uint4(0, 0, 0, 0);
-                if (i < kUnitsX) px.even[i < kUnitsX ? i : 0] = q;
-                else pdy.even[i < kUnitsX ? 0 : i - kUnitsX] = q;
-            }
-            x = px.get();
-            dy = pdy.get();
+            x = AheadX::get(slot(stage, r, u), x0, c, u, threadIdx.x, blockDim.x, live);
+            dy = AheadDy::get(slot(stage, r, u) + blockDim.x * AheadX::kBytes, dy0, c, u, threadIdx.x, blockDim.x, live);
         } else {
             x = odd_x[r][u].get();
             dy = odd_dy[r][u].get();

@@ -1,5 +1,7 @@
 // Rows of any alignment, eight elements ("a piece") to a thread and turn.  EVEN: rows begin on 16-byte boundaries and
-// are whole pieces long; a thread takes eight consecutive elements with 16-byte accesses.  Otherwise threads
+// are whole pieces long; a thread takes eight consecutive elements, or twice four where some of the matrices are fp32, so
+// that a warp's accesses cover consecutive 8 or 16 bytes of each lane (fp32 in eights leaves half of every 32-byte
+// sector to a second access).  Otherwise threads
 // take every width-th element: a warp's accesses then cover consecutive elements whatever the pitch, and
 // cost no shifting of words (8192 rows of 1601 bf16, layer norm: 39 us with 16-byte loads shifted into place and stores
 // traded between lanes, @ODD@ so).
@@ -32,16 +34,22 @@ __device__ __forceinline__ float narrowed<float>(float y) { return y; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 narrowed<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
 
-// Columns of a thread: element i of its piece u, of threads `t` of a row's `width`.  W: that width, known to the
-// compiler (0: it is not), so that uneven rows' accesses need no address of their own each.
-template <bool EVEN, int W = 0>
+// Elements that lie together in a piece of even rows whose matrices have elements of these sizes.
+__host__ __device__ constexpr int together(size_t a, size_t b = 2, size_t c = 2) { return a == 2 && b == 2 && c == 2 ? 8 : 4; }
+
+// Columns of a thread: element i of its piece u, of threads `t` of a row's `width`; N elements lie together.  W: that
+// width, known to the compiler (0: it is not), so that uneven rows' accesses need no address of their own each.
+template <bool EVEN, int N, int W = 0>
 struct Columns {
+    static constexpr int kTogether = N, kParts = kPiece / N;
     int t, threads, dim;
 
     __device__ __forceinline__ int width() const { return W ? W : threads; }
-    __device__ __forceinline__ int at(int u, int i) const { return EVEN ? (t + u * width()) * kPiece + i : t + (u * kPiece + i) * width(); }
-    __device__ __forceinline__ bool has(int u, int i) const {  // (EVEN: the same for all i)
-        return EVEN ? (t + u * width()) * kPiece < dim : t < dim - (u * kPiece + i) * width();
+    __device__ __forceinline__ int at(int u, int i) const {
+        return EVEN ? (t + (u * kParts + i / N) * width()) * N + i % N : t + (u * kPiece + i) * width();
+    }
+    __device__ __forceinline__ bool has(int u, int i) const {  // (EVEN: the same for elements that lie together)
+        return EVEN ? (t + (u * kParts + i / N) * width()) * N < dim : t < dim - (u * kPiece + i) * width();
     }
 };
 
@@ -70,14 +78,21 @@ struct Piece {
     T odd[EVEN ? 1 : kPiece];
 
     // row: the row's first element; zeros for columns that it does not have, and for none at all (`live` false)
-    template <int W>
-    __device__ __forceinline__ void load(const T *row, const Columns<EVEN, W> &c, int u, bool live) {
+    template <int N, int W>
+    __device__ __forceinline__ void load(const T *row, const Columns<EVEN, N, W> &c, int u, bool live) {
         if constexpr (EVEN) {
-            const uint4 *from = reinterpret_cast<const uint4 *>(row + c.at(u, 0));
 #pragma unroll
-            for (int i = 0; i < kUnits; ++i) {
-                even[i] = make_uint4(0, 0, 0, 0);
-                if (live && c.has(u, 0)) even[i] = from[i];
+            for (int i = 0; i < kUnits; ++i) even[i] = make_uint4(0, 0, 0, 0);
+            if constexpr (N * sizeof(T) == 8) {
+                uint2 q[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (live && c.has(u, N * i)) q[i] = *reinterpret_cast<const uint2 *>(row + c.at(u, N * i));
+                even[0] = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i)
+                    if (live && c.has(u, kPiece / kUnits * i)) even[i] = *reinterpret_cast<const uint4 *>(row + c.at(u, kPiece / kUnits * i));
             }
         } else {
             const T *from = row + c.t;
@@ -99,8 +114,8 @@ struct Piece {
         }
     }
 };
-template <typename T, bool EVEN, int W>
-__device__ __forceinline__ Vec load_piece(const T *row, const Columns<EVEN, W> &c, int u, bool live) {
+template <typename T, bool EVEN, int N, int W>
+__device__ __forceinline__ Vec load_piece(const T *row, const Columns<EVEN, N, W> &c, int u, bool live) {
     Piece<T, EVEN> q;
     q.load(row, c, u, live);
     return q.get();
@@ -125,15 +140,19 @@ __device__ __forceinline__ void pack_words(const Vec &v, uint4 (&w)[2]) {
     for (int h = 0; h < 2; ++h)
         w[h] = make_uint4(__float_as_uint(a[4 * h]), __float_as_uint(a[4 * h + 1]), __float_as_uint(a[4 * h + 2]), __float_as_uint(a[4 * h + 3]));
 }
-template <typename O, bool EVEN, int W>
-__device__ __forceinline__ void store_piece(O *row, const Columns<EVEN, W> &c, int u, bool live, const Vec &v) {
+template <typename O, bool EVEN, int N, int W>
+__device__ __forceinline__ void store_piece(O *row, const Columns<EVEN, N, W> &c, int u, bool live, const Vec &v) {
     if constexpr (EVEN) {
-        uint4 w[kPiece * sizeof(O) / 16];
+        constexpr int kUnits = kPiece * sizeof(O) / 16;
+        uint4 w[kUnits];
         pack_words(v, w);
-        if (live && c.has(u, 0)) {
-            uint4 *to = reinterpret_cast<uint4 *>(row + c.at(u, 0));
+        if constexpr (N * sizeof(O) == 8) {
+            if (live && c.has(u, 0)) *reinterpret_cast<uint2 *>(row + c.at(u, 0)) = make_uint2(w[0].x, w[0].y);
+            if (live && c.has(u, N)) *reinterpret_cast<uint2 *>(row + c.at(u, N)) = make_uint2(w[0].z, w[0].w);
+        } else {
 #pragma unroll
-            for (int i = 0; i < (int)(kPiece * sizeof(O) / 16); ++i) to[i] = w[i];
+            for (int i = 0; i < kUnits; ++i)
+                if (live && c.has(u, kPiece / kUnits * i)) *reinterpret_cast<uint4 *>(row + c.at(u, kPiece / kUnits * i)) = w[i];
         }
     } else {
         O *to = row + c.t;
@@ -157,6 +176,9 @@ inline bool even_rows(const void *p, int64_t cols, int64_t ld, int size) {
 __device__ __forceinline__ void copy16(uint32_t to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copy8(uint32_t to, const void *from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
 __device__ __forceinline__ void copy4(uint32_t to, const void *from) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
@@ -166,43 +188,60 @@ __device__ __forceinline__ void copies_wait() {  // for all but the last N group
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// A lane's piece in a slot of its warp's, which is kBytes long.  Two-byte elements of uneven rows cannot come that way.
+// Thread `t` of `threads` that share a slot of kBytes * threads: its piece of a row.  Two-byte elements of uneven rows
+// cannot come that way, and are loaded when they are wanted.
 template <typename T, bool EVEN>
 struct Slot {
     static constexpr bool kCopied = EVEN || sizeof(T) == 4;
-    static constexpr int kBytes = kCopied ? 32 * kPiece * (int)sizeof(T) : 0;
+    static constexpr int kBytes = kCopied ? kPiece * (int)sizeof(T) : 0;
     static constexpr int kUnits = kPiece * sizeof(T) / 16;
 
-    template <int W>
-    static __device__ __forceinline__ void send_for(unsigned char *slot, const T *row, const Columns<EVEN, W> &c, int lane) {
+    template <int N, int W>
+    static __device__ __forceinline__ void send_for(unsigned char *slot, const T *row, const Columns<EVEN, N, W> &c, int u, int t, int threads) {
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
-        if constexpr (EVEN) {
-            if (c.has(0, 0)) {
+        if constexpr (EVEN && N * sizeof(T) == 8) {
 #pragma unroll
-                for (int i = 0; i < kUnits; ++i) copy16(to + (32 * i + lane) * 16, reinterpret_cast<const uint4 *>(row + c.at(0, 0)) + i);
-            }
+            for (int i = 0; i < 2; ++i)
+                if (c.has(u, N * i)) copy8(to + (threads * i + t) * 8, row + c.at(u, N * i));
+        } else if constexpr (EVEN) {
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i)
+                if (c.has(u, kPiece / kUnits * i)) copy16(to + (threads * i + t) * 16, row + c.at(u, kPiece / kUnits * i));
         } else if constexpr (kCopied) {
 #pragma unroll
             for (int i = 0; i < kPiece; ++i)
-                if (c.has(0, i)) copy4(to + (32 * i + lane) * 4, row + c.at(0, i));
+                if (c.has(u, i)) copy4(to + (threads * i + t) * 4, row + c.at(u, i));
         }
     }
-    template <int W>
-    static __device__ __forceinline__ Vec get(const unsigned char *slot, const T *row, const Columns<EVEN, W> &c, int lane) {
+    // (live false: zeros, whatever lies there)
+    template <int N, int W>
+    static __device__ __forceinline__ Vec get(const unsigned char *slot, const T *row, const Columns<EVEN, N, W> &c, int u, int t, int threads,
+                                              bool live = true) {
         if constexpr (EVEN) {
-            uint4 u[kUnits];
+            uint4 w[kUnits];
+            if constexpr (N * sizeof(T) == 8) {
+                uint2 q[2] = {make_uint2(0, 0), make_uint2(0, 0)};
 #pragma unroll
-            for (int i = 0; i < kUnits; ++i) u[i] = c.has(0, 0) ? reinterpret_cast<const uint4 *>(slot)[32 * i + lane] : make_uint4(0, 0, 0, 0);
-            return widened(u);
+                for (int i = 0; i < 2; ++i)
+                    if (live && c.has(u, N * i)) q[i] = reinterpret_cast<const uint2 *>(slot)[threads * i + t];
+                w[0] = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kUnits; ++i) {
+                    w[i] = make_uint4(0, 0, 0, 0);
+                    if (live && c.has(u, kPiece / kUnits * i)) w[i] = reinterpret_cast<const uint4 *>(slot)[threads * i + t];
+                }
+            }
+            return widened(w);
         } else if constexpr (kCopied) {
             Vec v;
-            const float *f = reinterpret_cast<const float *>(slot) + lane;
+            const float *f = reinterpret_cast<const float *>(slot) + t;
 #pragma unroll
             for (int i = 0; i < kPiece / 2; ++i)
-                v.p[i] = pair(c.has(0, 2 * i) ? f[64 * i] : 0.f, c.has(0, 2 * i + 1) ? f[64 * i + 32] : 0.f);
+                v.p[i] = pair(live && c.has(u, 2 * i) ? f[2 * i * threads] : 0.f, live && c.has(u, 2 * i + 1) ? f[(2 * i + 1) * threads] : 0.f);
             return v;
         } else {
-            return load_piece(row, c, 0, true);
+            return load_piece(row, c, u, live);
         }
     }
 };
