@@ -142,7 +142,11 @@ layer_norm_kernel(const NormArgs a, int warps) {
         copies_end_group();
     };
     if constexpr (EVEN) {
-        for (int i = 0; i < kAhead; ++i) send_for(row + i * step, i);
+        for (int i = 0; i < kAhead; ++i) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) Ahead::clear(slot(i, u), c, u, threadIdx.x, blockDim.x);
+            send_for(row + i * step, i);
+        }
         const uint4 zero = make_uint4(0, 0, 0, 0);
         for (int i = threadIdx.x; i < 2 * U * c.width(); i += blockDim.x) {
             // fours of columns, in the order in which a piece's halves lie
@@ -390,7 +394,16 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
         }
     };
     if constexpr (EVEN) {
-        for (int i = 0; i < kPairsAhead; ++i) send_for(row + 2 * i * step, i);
+        for (int i = 0; i < kPairsAhead; ++i) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    AheadX::clear(slot(i, r, u), c, u, threadIdx.x, blockDim.x);
+                    AheadDy::clear(slot(i, r, u) + blockDim.x * AheadX::kBytes, c, u, threadIdx.x, blockDim.x);
+                }
+            send_for(row + 2 * i * step, i);
+        }
     }
     look_up(row);
     Vec w[U];
@@ -400,10 +413,10 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
     Piece<T, EVEN> odd_x[EVEN ? 1 : 2][U];
     Piece<G, EVEN> odd_dy[EVEN ? 1 : 2][U];
     // a piece of the pair's row r
-    const auto get = [&](int stage, int r, int u, bool live, Vec &x, Vec &dy) {
+    const auto get = [&](int stage, int r, int u, Vec &x, Vec &dy) {
         if constexpr (EVEN) {
-            x = AheadX::get(slot(stage, r, u), x0, c, u, threadIdx.x, blockDim.x, live);
-            dy = AheadDy::get(slot(stage, r, u) + blockDim.x * AheadX::kBytes, dy0, c, u, threadIdx.x, blockDim.x, live);
+            x = AheadX::get(slot(stage, r, u), x0, c, u, threadIdx.x, blockDim.x);
+            dy = AheadDy::get(slot(stage, r, u) + blockDim.x * AheadX::kBytes, dy0, c, u, threadIdx.x, blockDim.x);
         } else {
             x = odd_x[r][u].get();
             dy = odd_dy[r][u].get();
@@ -432,13 +445,15 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
             }
         }
         look_up(row + 2 * step);
+        v[2] = v[3] = 0.f;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
+            if (r == 1 && !both) continue;
             Pair p1 = 0, p2 = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 Vec x, dy;
-                get(stage, r, u, r == 0 || both, x, dy);
+                get(stage, r, u, x, dy);
                 take_piece(x, dy, w[u], mean[r], rstd[r], sums[u], p1, p2);
             }
             v[2 * r] = pair_sum(p1);
@@ -465,7 +480,7 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     Vec x, dy;
-                    get(stage, r, u, true, x, dy);
+                    get(stage, r, u, x, dy);
                     store_piece(dx, c, u, true, piece_dx(x, dy, w[u], mean[r], rstd[r], m1[r], m2[r]));
                 }
             }

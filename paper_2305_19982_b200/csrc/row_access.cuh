@@ -213,35 +213,39 @@ struct Slot {
                 if (c.has(u, i)) copy4(to + (threads * i + t) * 4, row + c.at(u, i));
         }
     }
-    // (live false: zeros, whatever lies there)
+    // Zeros where nothing will be sent to, so that get need not ask which columns there are.
     template <int N, int W>
-    static __device__ __forceinline__ Vec get(const unsigned char *slot, const T *row, const Columns<EVEN, N, W> &c, int u, int t, int threads,
-                                              bool live = true) {
+    static __device__ __forceinline__ void clear(unsigned char *slot, const Columns<EVEN, N, W> &c, int u, int t, int threads) {
+        if constexpr (kCopied) {
+            constexpr int kEach = EVEN ? (N * sizeof(T) == 8 ? 2 : kUnits) : kPiece, kLen = kBytes / kEach;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (!c.has(u, kPiece / kEach * i)) {
+#pragma unroll
+                    for (int q = 0; q < kLen / 4; ++q) reinterpret_cast<unsigned *>(slot)[(threads * i + t) * (kLen / 4) + q] = 0;
+                }
+        }
+    }
+    template <int N, int W>
+    static __device__ __forceinline__ Vec get(const unsigned char *slot, const T *row, const Columns<EVEN, N, W> &c, int u, int t, int threads) {
         if constexpr (EVEN) {
             uint4 w[kUnits];
             if constexpr (N * sizeof(T) == 8) {
-                uint2 q[2] = {make_uint2(0, 0), make_uint2(0, 0)};
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (live && c.has(u, N * i)) q[i] = reinterpret_cast<const uint2 *>(slot)[threads * i + t];
-                w[0] = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
+                const uint2 p = reinterpret_cast<const uint2 *>(slot)[t], q = reinterpret_cast<const uint2 *>(slot)[threads + t];
+                w[0] = make_uint4(p.x, p.y, q.x, q.y);
             } else {
 #pragma unroll
-                for (int i = 0; i < kUnits; ++i) {
-                    w[i] = make_uint4(0, 0, 0, 0);
-                    if (live && c.has(u, kPiece / kUnits * i)) w[i] = reinterpret_cast<const uint4 *>(slot)[threads * i + t];
-                }
+                for (int i = 0; i < kUnits; ++i) w[i] = reinterpret_cast<const uint4 *>(slot)[threads * i + t];
             }
             return widened(w);
         } else if constexpr (kCopied) {
             Vec v;
             const float *f = reinterpret_cast<const float *>(slot) + t;
 #pragma unroll
-            for (int i = 0; i < kPiece / 2; ++i)
-                v.p[i] = pair(live && c.has(u, 2 * i) ? f[2 * i * threads] : 0.f, live && c.has(u, 2 * i + 1) ? f[(2 * i + 1) * threads] : 0.f);
+            for (int i = 0; i < kPiece / 2; ++i) v.p[i] = pair(f[2 * i * threads], f[(2 * i + 1) * threads]);
             return v;
         } else {
-            return load_piece(row, c, u, live);
+            return load_piece(row, c, u, true);
         }
     }
 };
