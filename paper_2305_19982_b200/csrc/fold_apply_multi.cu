@@ -253,12 +253,13 @@ fold_apply_ring_kernel(const __grid_constant__ StepTable<CAP> tab, FoldConstants
             r.m = *reinterpret_cast<const float4 *>(st.m + 4 * tid);
             r.v = *reinterpret_cast<const float4 *>(st.v + 4 * tid);
         }
-        __syncwarp();
-        if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
         if (mine) {
             step4(r.g, factor, r.w, r.m, r.v, f, c);
             store4(w, m, v, copy, base + 4 * tid, r.w, r.m, r.v);
         }
+        // behind the stores that use what was read: a load that has been issued need not have read yet when the arrival is seen
+        __syncwarp();
+        if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
         if (loaded == kRingChunk && (k > 0 || head == 0)) continue;
         // before the first boundary, behind the last whole unit, or all of an unaligned tensor's chunk
         if (k == 0 && head != kScalar && tid < head && (size_t)tid < n) scalar_element(g, w, m, v, copy, tid, factor, f, c);

@@ -379,9 +379,11 @@ fold_apply8_ring_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f
             x.vc = load_codes(st.v + o);
             x.sm = st.sm[warp];
             x.sv = st.sv[warp];
+            const float2 top = x.update(factor, f, c);
+            // behind the arithmetic that uses what was read: a load that has been issued need not have read yet when the
+            // arrival is seen
             __syncwarp();
             if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
-            const float2 top = x.update(factor, f, c);
             x.store_wide(s, tab.w[t], tab.copy[t], at + 4 * lane);
             Block8::store_scales(s, blk, top, lane, c);
         } else {
