@@ -470,7 +470,8 @@ ADAMA_API adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args
  *     dlogits_j = w*logit_scale*(P*q_j - sum over the entries with ids_i = j of p_i)
  * so that stats[0] is the loss and dlogits its gradient; w carries the mask, the normalisation, and 1/logit_scale^2
  * where the temperature's square is wanted in front.  Without teacher_lse the entries' own log-sum takes its place:
- * P = 1.  An entry with a negative index, or a teacher's logit of -inf, has p = 0; a row without any other has
+ * P = 1.  (With it, and P < 1, the terms are the entries' part of the divergence, which alone may be below 0.)  An
+ * entry with a negative index, or a teacher's logit of -inf, has p = 0; a row without any other has
  * loss and gradient 0.  An index may occur more than once in a row: each entry has its own term.  A row with
  * w = 0 is not read: its dlogits and loss are 0 and it adds nothing to stats.
  *   logits, dlogits : as for adama_policy_loss (dlogits may be NULL, or logits itself)
@@ -599,7 +600,7 @@ ADAMA_API adama_status adama_embedding(adama_ctx *ctx, const adama_embedding_arg
  *   grad : [vocab, dim] fp32 or bf16 (grad_dtype), pitch ld_grad;  m, v : the same in fp32, both with pitch
  *          ld_grad.  Either grad is given or both moments are
  *   workspace : adama_embedding_workspace(ctx, tokens, dim) bytes, as for adama_layer_norm_backward
- * Errors: INVALID_ARG, BAD_STATE (moments without adama_begin_minibatch), MISALIGNED, UNSUPPORTED, CUDA. */
+ * Errors: INVALID_ARG, BAD_STATE (moments without adama_begin_minibatch), MISALIGNED, UNSUPPORTED (dim > 2^23), CUDA. */
 typedef struct adama_embedding_grad_args {
     const int64_t *ids;
     const void *dy;

@@ -1036,8 +1036,10 @@ adama_status adama_embedding(adama_ctx *ctx, const adama_embedding_args *p, void
     return ADAMA_OK;
 }
 
+constexpr int64_t kEmbeddingDim = 1 << 23;  // of the gradient: its sums are joined in a grid with a row for 256 columns
+
 size_t adama_embedding_workspace(const adama_ctx *ctx, int64_t tokens, int64_t dim) {
-    if (!ctx || tokens < 0 || tokens > INT32_MAX || dim < 1 || dim > INT32_MAX / 2) return 0;
+    if (!ctx || tokens < 0 || tokens > INT32_MAX || dim < 1 || dim > kEmbeddingDim) return 0;
     return adama::embedding_workspace_bytes(tokens, (int)dim, ctx->sm_count);
 }
 
@@ -1046,6 +1048,7 @@ adama_status adama_embedding_grad(adama_ctx *ctx, const adama_embedding_grad_arg
     if (!p) return fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding_grad: null arguments");
     const char *const call = "embedding_grad";
     adama_status st = check_rows(ctx, call, p->tokens, p->dim);
+    if (st == ADAMA_OK && p->dim > kEmbeddingDim) st = fail(ctx, ADAMA_ERR_UNSUPPORTED, "embedding_grad: more than 2^23 columns");
     if (st == ADAMA_OK && (p->vocab < 1 || p->vocab >= INT32_MAX))
         st = fail(ctx, ADAMA_ERR_INVALID_ARG, "embedding_grad: vocab must be from 1 to 2^31-2");
     if (st == ADAMA_OK) st = check_matrix(ctx, call, "dy", p->dy, p->dy_dtype, p->tokens, p->dim, p->ld_dy);

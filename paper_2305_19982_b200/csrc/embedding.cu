@@ -402,9 +402,10 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
     const int64_t first = (int64_t)blockIdx.x * 32, start = (first + lane) * chunk, end = start + chunk;
     // The sort has ended when this kernel may start (the sums wait for it first): the runs are looked up while the sums are
     // still being made, and what the first one of a warp will meet is sent for.  A run begins in a chunk and fills the
-    // next one: the same key at its own end and at that chunk's, another one in front of it.
-    const unsigned key = end <= a.tokens ? a.keys[end - 1] : none, far = end + chunk <= a.tokens ? a.keys[end + chunk - 1] : none - 1;
-    const unsigned before = start > 0 && start <= a.tokens ? a.keys[start - 1] : none;
+    // next one: the same key at its own end and at that chunk's, another one in front of it.  (The keys come from L2: it is the
+    // sums that have waited for the sort, not this kernel.)
+    const unsigned key = end <= a.tokens ? __ldcg(a.keys + end - 1) : none, far = end + chunk <= a.tokens ? __ldcg(a.keys + end + chunk - 1) : none - 1;
+    const unsigned before = start > 0 && start <= a.tokens ? __ldcg(a.keys + start - 1) : none;
     unsigned todo = __ballot_sync(none, key == far && key != before && key != (unsigned)a.vocab), of_warp = 0, of_block = 0;
     for (int turn = 0; todo; todo &= todo - 1) {  // (all warps see the same)
         const int which = __ffs(todo) - 1;
@@ -412,7 +413,7 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
         int64_t last = first + which;  // the chunk in which the run ends
         for (int run = 32; run == 32; last += run) {
             const int64_t at = (last + 1 + lane) * chunk;
-            const unsigned more = __ballot_sync(none, at < a.tokens && a.keys[at] == k);
+            const unsigned more = __ballot_sync(none, at < a.tokens && __ldcg(a.keys + at) == k);
             run = more == none ? 32 : __ffs(~more) - 1;
         }
         if (lane == 0) last_of[which] = last;  // (every warp writes the same)

@@ -115,7 +115,7 @@ layer_norm_short_kernel(const NormArgs a, int lanes) {
 // Longer rows: a group of warps walks rows, U pieces to a thread; weight and bias lie in shared memory, as do the next
 // rows of a thread, which are on their way while it works on one.  A row costs a warp some 200 instructions beside those of
 // its elements, and exchanges between lanes and warps wait for each other: so few warps share a row, with many pieces
-// to a thread, where there are rows enough (4096 x 1600 fp32 to bf16: four warps to a row 20 us, one @FWD@).
+// to a thread, where there are rows enough (4096 x 1600 fp32 to bf16: four warps to a row 20 us, two 13).
 constexpr int kAhead = 2;  // rows of a thread on their way, of even ones
 
 template <typename T, typename O, int U, bool EVEN, int WARPS>

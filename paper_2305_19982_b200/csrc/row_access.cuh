@@ -4,7 +4,7 @@
 // sector to a second access).  Otherwise threads
 // take every width-th element: a warp's accesses then cover consecutive elements whatever the pitch, and
 // cost no shifting of words (8192 rows of 1601 bf16, layer norm: 39 us with 16-byte loads shifted into place and stores
-// traded between lanes, @ODD@ so).
+// traded between lanes, 24 so).
 #pragma once
 
 #include <cuda_bf16.h>
