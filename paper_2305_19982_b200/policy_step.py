@@ -6,6 +6,8 @@ A small next-token policy (embedding, one hidden layer, output layer) is trained
 in which the answer to token x is (7*x + 3) mod vocab.  It stands for the last part of a language model's
 step; only library matrix products come between the calls:
 
+    embedding             the inputs' rows of the table, and in the backward pass
+    embedding_grad        the table's gradient: rows of equal tokens summed in fp32, in one fixed order
     token_logprobs        log-probabilities of the sampled answers, under the sampling policy (old)
                           and the frozen one that the KL term holds on to (ref)
     policy_loss           clipped loss with KL term, and its gradient dlogits in bf16
@@ -68,7 +70,8 @@ class PolicyStep:
     def forward(self, x: torch.Tensor, weights=None):
         """Activations and logits [tokens, vocab] (bf16, aligned rows) of the inputs x."""
         embed, inner, head = weights if weights is not None else (self.embed_bf, self.inner_bf, self.head_bf)
-        e = embed[x]
+        e = torch.empty(x.numel(), embed.shape[1], dtype=embed.dtype, device=self.device)
+        self.opt.embedding(x, embed, e)
         pre = e @ inner
         h = torch.relu(pre)
         return e, pre, h, (h @ head)[:, :self.vocab]
@@ -93,7 +96,7 @@ class PolicyStep:
         opt.policy_loss(logits, y, old, advantages, weights, dl, self.stats, ref_logp=ref, kl_coef=self.kl_coef)
         dpre = (dlogits @ self.head_bf.t()) * (pre > 0)
         torch.mm(e.t(), dpre, out=self.grads[1])
-        self.grads[0].copy_(torch.zeros_like(self.embed).index_add_(0, x, (dpre @ self.inner_bf.t()).float()))
+        opt.embedding_grad(x, dpre @ self.inner_bf.t(), self.grads[0])
         opt.grad_norm_multi(self._g, self.max_norm, self.norm)
         # No entry of the output layer's gradient h' dlogits exceeds |h| |dlogits|, and so the square of the norm of
         # both; v holds the entry's square.  Where that overflows, or the factor is NaN, the step is skipped.
