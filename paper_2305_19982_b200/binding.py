@@ -692,17 +692,20 @@ class AdamA:
             _dev_ptr(out, torch.float32, "out"), self._workspace(stream), stream))
 
     @staticmethod
-    def _rows(t: torch.Tensor, name: str):
-        """(pointer, dtype, pitch) of a [rows, vocab] tensor with unit stride in its last dimension."""
-        shape, stride, dt = t.shape, t.stride(), _DTYPES.get(t.dtype)
-        if len(shape) != 2:
-            raise ValueError(f"{name} must be [rows, vocab]")
+    def _matrix(t: torch.Tensor, name: str):
+        """(pointer, dtype, pitch, rows, columns) of a [rows, columns] tensor with unit stride in its last dimension."""
+        dt = _DTYPES.get(t.dtype)
         if dt is None:
             raise TypeError(f"{name} must be float32 or bfloat16")
-        rows, vocab = shape
-        if vocab > 1 and stride[1] != 1:
+        if t.ndim != 2:
+            raise ValueError(f"{name} must be [rows, columns]")
+        rows, cols = t.shape
+        ld, step = t.stride()
+        if step != 1 and cols > 1:
             raise ValueError(f"{name} must have unit stride in its last dimension")
-        return _dev_ptr(t, t.dtype, name), dt, stride[0] if rows > 1 else max(vocab, stride[0])
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor")
+        return t.data_ptr(), dt, ld if rows > 1 or ld > cols else cols, rows, cols
 
     @staticmethod
     def _per_row(t: Optional[torch.Tensor], rows: int, name: str, dtype=torch.float32):
@@ -718,8 +721,7 @@ class AdamA:
                        logit_scale: float = 1.0) -> None:
         """adama_token_logprobs: log-probability of `targets` (int64; negative = ignored) under the
         rows of `logits` (fp32 or bf16), written to `logp`; log-sum-exp and entropy on request."""
-        ptr, dt, ld = self._rows(logits, "logits")
-        rows, vocab = logits.shape
+        ptr, dt, ld, rows, vocab = self._matrix(logits, "logits")
         self._check(self._L.adama_token_logprobs(
             self._h, ptr, dt, rows, vocab, ld, self._per_row(targets, rows, "targets", torch.int64),
             float(logit_scale), self._per_row(logp, rows, "logp"), self._per_row(lse, rows, "lse"),
@@ -732,13 +734,12 @@ class AdamA:
                     kl_coef: float = 0.0, logit_scale: float = 1.0) -> None:
         """adama_policy_loss: `stats` (4 fp32) receives {loss, policy part, KL, clipped share}, each
         weighted by `weights`; `dlogits` (fp32 or bf16, `logits` itself, or None) the gradient."""
-        ptr, dt, ld = self._rows(logits, "logits")
-        rows, vocab = logits.shape
+        ptr, dt, ld, rows, vocab = self._matrix(logits, "logits")
         dptr, ddt, dld = 0, dt, 0
         if dlogits is not None:
-            if dlogits.shape != logits.shape:
+            dptr, ddt, dld, drows, dvocab = self._matrix(dlogits, "dlogits")
+            if drows != rows or dvocab != vocab:
                 raise ValueError("dlogits must have the shape of logits")
-            dptr, ddt, dld = self._rows(dlogits, "dlogits")
         if stats.numel() != 4 or not stats.is_contiguous():
             raise ValueError("stats must hold 4 contiguous float32 values")
         stream = _stream_ptr(self.device)
@@ -758,25 +759,24 @@ class AdamA:
         entropy, student's mass on the entries, teacher's mass}, each weighted by `weights`; `loss` each row's
         divergence; `dlogits` (fp32 or bf16, `logits` itself, or None) the gradient.  Without `teacher_lse` the entries
         are the whole of the teacher's distribution."""
-        ptr, dt, ld = self._rows(logits, "logits")
-        rows, vocab = logits.shape
+        ptr, dt, ld, rows, vocab = self._matrix(logits, "logits")
         dptr, ddt, dld = 0, dt, 0
         if dlogits is not None:
-            if dlogits.shape != logits.shape:
+            dptr, ddt, dld, drows, dvocab = self._matrix(dlogits, "dlogits")
+            if drows != rows or dvocab != vocab:
                 raise ValueError("dlogits must have the shape of logits")
-            dptr, ddt, dld = self._rows(dlogits, "dlogits")
-        tptr, tdt, tld = self._rows(teacher_logits, "teacher_logits")
-        top = teacher_logits.shape[1]
-        if teacher_logits.shape[0] != rows or teacher_ids.shape != teacher_logits.shape:
+        tptr, tdt, tld, trows, top = self._matrix(teacher_logits, "teacher_logits")
+        if trows != rows or teacher_ids.shape != (rows, top):
             raise ValueError("teacher_logits and teacher_ids must be [rows, top]")
-        if top > 1 and teacher_ids.stride(1) != 1:
+        ild, step = teacher_ids.stride()
+        if step != 1 and top > 1:
             raise ValueError("teacher_ids must have unit stride in its last dimension")
         if stats.numel() != 4 or not stats.is_contiguous():
             raise ValueError("stats must hold 4 contiguous float32 values")
         stream = _stream_ptr(self.device)
         row = self._per_row
         args = _DISTILL_ARGS.pack(
-            ptr, dptr, dt, ddt, tdt, top, rows, vocab, ld, dld, tld, max(top, teacher_ids.stride(0)) if rows < 2 else teacher_ids.stride(0),
+            ptr, dptr, dt, ddt, tdt, top, rows, vocab, ld, dld, tld, ild if rows > 1 or ild > top else top,
             tptr, _dev_ptr(teacher_ids, torch.int64, "teacher_ids"), row(teacher_lse, rows, "teacher_lse"), row(weights, rows, "weights"),
             logit_scale, row(loss, rows, "loss"), _dev_ptr(stats, torch.float32, "stats"), self._workspace(stream),
             self._scratch(stream, "distill_scratch", rows, top))
@@ -819,10 +819,9 @@ class AdamA:
                    mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, eps: float = 1e-5) -> None:
         """adama_layer_norm: y = (x - mean)*rstd*weight + bias over the rows of `x` [rows, dim] (fp32 or bf16, as
         is `y`, which may be `x` itself); `mean` and `rstd` (fp32) receive what the backward pass reads."""
-        ptr, dt, ld = self._rows(x, "x")
-        yptr, ydt, yld = self._rows(y, "y")
-        rows, dim = x.shape
-        if y.shape != x.shape:
+        ptr, dt, ld, rows, dim = self._matrix(x, "x")
+        yptr, ydt, yld, yrows, ydim = self._matrix(y, "y")
+        if yrows != rows or ydim != dim:
             raise ValueError("y must have the shape of x")
         vector = self._vector
         args = _LAYER_NORM_ARGS.pack(ptr, yptr, dt, ydt, rows, dim, ld, yld, vector(weight, dim, "weight"), vector(bias, dim, "bias"),
@@ -830,15 +829,12 @@ class AdamA:
         self._check(self._L.adama_layer_norm(self._h, args, _stream_ptr(self.device)))
 
     def _layer_norm_backward(self, dy, x, weight, mean, rstd, dx, *params) -> None:
-        dyptr, dydt, dyld = self._rows(dy, "dy")
-        ptr, dt, ld = self._rows(x, "x")
-        rows, dim = x.shape
-        dxptr, dxld = 0, dim
-        if dx is not None:
-            if dx.dtype != x.dtype:
-                raise TypeError("dx must have the dtype of x")
-            dxptr, _, dxld = self._rows(dx, "dx")
-        if dy.shape != x.shape or (dx is not None and dx.shape != x.shape):
+        dyptr, dydt, dyld, dyrows, dydim = self._matrix(dy, "dy")
+        ptr, dt, ld, rows, dim = self._matrix(x, "x")
+        dxptr, dxdt, dxld, dxrows, dxdim = (0, dt, dim, rows, dim) if dx is None else self._matrix(dx, "dx")
+        if dxdt != dt:
+            raise TypeError("dx must have the dtype of x")
+        if dyrows != rows or dydim != dim or dxrows != rows or dxdim != dim:
             raise ValueError("dy and dx must have the shape of x")
         vector, names = self._vector, ("dweight", "dbias", "m_weight", "v_weight", "m_bias", "v_bias")
         stream = _stream_ptr(self.device)
@@ -863,25 +859,22 @@ class AdamA:
 
     def embedding(self, ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0) -> None:
         """adama_embedding: out[t] = scale*table[ids[t]] (int64 ids; negative = a row of zeros)."""
-        ptr, dt, ld = self._rows(table, "table")
-        optr, odt, old = self._rows(out, "out")
-        vocab, dim = table.shape
-        tokens = out.shape[0]
-        if out.shape[1] != dim:
+        ptr, dt, ld, vocab, dim = self._matrix(table, "table")
+        optr, odt, old, tokens, width = self._matrix(out, "out")
+        if width != dim:
             raise ValueError("out must be [tokens, dim]")
         args = _EMBEDDING_ARGS.pack(self._per_row(ids, tokens, "ids", torch.int64), ptr, optr, dt, odt, tokens, vocab, dim, ld, old, scale)
         self._check(self._L.adama_embedding(self._h, args, _stream_ptr(self.device)))
 
     def _embedding_grad(self, ids, dy, target, v, scale, accumulate) -> None:
-        ptr, dt, ld = self._rows(dy, "dy")
-        tptr, tdt, tld = self._rows(target, "grad" if v is None else "m")
-        (tokens, dim), (vocab, width) = dy.shape, target.shape
+        ptr, dt, ld, tokens, dim = self._matrix(dy, "dy")
+        tptr, tdt, tld, vocab, width = self._matrix(target, "grad" if v is None else "m")
         if width != dim:
             raise ValueError("rows of dy and of the table must have the same length")
         vptr = 0
         if v is not None:
-            vptr, vdt, vld = self._rows(v, "v")
-            if v.shape != target.shape or vld != tld:
+            vptr, vdt, vld, vrows, vdim = self._matrix(v, "v")
+            if vrows != vocab or vdim != dim or vld != tld:
                 raise ValueError("m and v must have one shape and one row pitch")
             if tdt != F32 or vdt != F32:
                 raise TypeError("m and v must be float32")
