@@ -577,10 +577,14 @@ constexpr int kJoinWarps = 16;
 __global__ void __launch_bounds__(32 * kJoinWarps)
 layer_norm_join_kernel(const NormBackArgs a, int parts) {
     __shared__ float slots[kJoinWarps][32];
-    wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const bool of_bias = blockIdx.y == 1;
     const int c = blockIdx.x * 32 + lane;
+    float *g = of_bias ? a.dbias : a.dweight, *m = of_bias ? a.m_bias : a.m_weight, *v = of_bias ? a.v_bias : a.v_weight;
+    const bool writes = warp == 0 && c < a.dim;
+    float m_c = 0.f, v_c = 0.f;
+    if (m && writes) m_c = __ldcg(m + c), v_c = __ldcg(v + c);  // what the kernel before this one leaves alone
+    wait_for_previous();
     const int64_t pad = padded(a.dim);
     const float *from = a.parts + (of_bias ? pad : 0) + c;
     float s = 0.f;
@@ -590,12 +594,16 @@ layer_norm_join_kernel(const NormBackArgs a, int parts) {
     }
     slots[warp][lane] = s;
     __syncthreads();
-    if (warp != 0 || c >= a.dim) return;
+    if (!writes) return;
     s = 0.f;
+#pragma unroll
     for (int i = 0; i < kJoinWarps; ++i) s += slots[i][lane];
-    float *g = of_bias ? a.dbias : a.dweight, *m = of_bias ? a.m_bias : a.m_weight, *v = of_bias ? a.v_bias : a.v_weight;
     if (g) g[c] = s;
-    if (m) fold1(s, m[c], v[c], a.fold.a, a.fold.b);
+    if (m) {
+        fold1(s, m_c, v_c, a.fold.a, a.fold.b);
+        m[c] = m_c;
+        v[c] = v_c;
+    }
 }
 
 // ---- launches --------------------------------------------------------------------------------------
