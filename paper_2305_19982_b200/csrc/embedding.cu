@@ -470,7 +470,8 @@ template <typename T, typename O>
 cudaError_t lookup(const EmbeddingArgs &a, cudaStream_t stream) {
     const int groups = (a.dim + kLookupPieces * kTile - 1) / (kLookupPieces * kTile);
     const unsigned blocks = (unsigned)((a.tokens * groups + kLookupWarps - 1) / kLookupWarps);
-    if (even_rows(a.table, a.dim, a.ld_table, sizeof(T)) && even_rows(a.out, a.dim, a.ld_out, sizeof(O)))
+    constexpr int N = together(sizeof(T), sizeof(O));
+    if (even_rows(a.table, a.dim, a.ld_table, sizeof(T), N) && even_rows(a.out, a.dim, a.ld_out, sizeof(O), N))
         embedding_kernel<T, O, true><<<blocks, 32 * kLookupWarps, 0, stream>>>(a, groups);
     else
         embedding_kernel<T, O, false><<<blocks, 32 * kLookupWarps, 0, stream>>>(a, groups);
@@ -571,8 +572,9 @@ cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t str
 }
 template <typename G, typename O, int MODE>
 cudaError_t sums(const EmbeddingGradArgs &a, const GradPlan &p, cudaStream_t stream, int *launches) {
-    const bool even = even_rows(a.dy, a.dim, a.ld_dy, sizeof(G)) &&
-                      (MODE == kFold ? even_rows(a.m, a.dim, a.ld_grad, 4) && aligned(a.v, 16) : even_rows(a.grad, a.dim, a.ld_grad, sizeof(O)));
+    constexpr int N = together(sizeof(G), sizeof(O));
+    const bool even = even_rows(a.dy, a.dim, a.ld_dy, sizeof(G), N) &&
+                      (MODE == kFold ? even_rows(a.m, a.dim, a.ld_grad, 4, N) && aligned(a.v, 16) : even_rows(a.grad, a.dim, a.ld_grad, sizeof(O), N));
     return even ? sums<G, O, MODE, true>(a, p, stream, launches) : sums<G, O, MODE, false>(a, p, stream, launches);
 }
 template <typename G>

@@ -676,7 +676,8 @@ cudaError_t forward_odd(const NormArgs &a, RowPlan &p, int sm_count, cudaStream_
 template <typename T, typename O>
 cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
     const int pieces = (int)(padded(a.dim) / kPiece);
-    const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T)) && even_rows(a.y, a.dim, a.ld_y, sizeof(O)) && aligned(a.weight, 16) &&
+    constexpr int N = together(sizeof(T), sizeof(O));
+    const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T), N) && even_rows(a.y, a.dim, a.ld_y, sizeof(O), N) && aligned(a.weight, 16) &&
                       aligned(a.bias, 16);
     if (pieces <= 32) {
         const int lanes = lanes_for(pieces), rows = kShortThreads / lanes;
@@ -772,10 +773,14 @@ cudaError_t launch_back(const NormBackArgs &a, const BackPlan &p, cudaStream_t s
 
 template <typename T, typename G>
 cudaError_t backward(const NormBackArgs &a, int sm_count, cudaStream_t stream, int *launches) {
-    const bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T)) && even_rows(a.dy, a.dim, a.ld_dy, sizeof(G)) &&
-                      (!a.dx || even_rows(a.dx, a.dim, a.ld_dx, sizeof(T))) && aligned(a.weight, 16) &&
-                      bytes_ahead<T, G>(2, a.dim / (2 * kPiece)) <= kBackShared - 8192;  // (the longest rows of fp32 go the other way)
-    const BackPlan p = plan_back(a.rows, a.dim, sm_count, even, even && sizeof(T) + sizeof(G) > 4);
+    constexpr int N = together(sizeof(T), sizeof(G));
+    bool even = even_rows(a.x, a.dim, a.ld_x, sizeof(T), N) && even_rows(a.dy, a.dim, a.ld_dy, sizeof(G), N) &&
+                (!a.dx || even_rows(a.dx, a.dim, a.ld_dx, sizeof(T), N)) && aligned(a.weight, 16);
+    BackPlan p = plan_back(a.rows, a.dim, sm_count, even, even && sizeof(T) + sizeof(G) > 4);
+    if (even && !p.is_long && p.pieces > 32 && bytes_ahead<T, G>(p.each, 32 * p.warps * p.groups) > kBackShared) {
+        even = false;  // the longest rows of fp32 go the other way
+        p = plan_back(a.rows, a.dim, sm_count, false, false);
+    }
     cudaError_t e = cudaSuccess;
     if (a.rows > 0) {
         if (p.is_long) {

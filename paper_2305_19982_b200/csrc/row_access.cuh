@@ -1,7 +1,7 @@
-// Rows of any alignment, eight elements ("a piece") to a thread and turn.  EVEN: rows begin on 16-byte boundaries and
-// are whole pieces long; a thread takes eight consecutive elements, or twice four where some of the matrices are fp32, so
-// that a warp's accesses cover consecutive 8 or 16 bytes of each lane (fp32 in eights leaves half of every 32-byte
-// sector to a second access).  Otherwise threads
+// Rows of any alignment, eight elements ("a piece") to a thread and turn.  EVEN: a thread takes eight consecutive elements,
+// or twice four where some of the matrices are fp32, so that a warp's accesses cover consecutive 8 or 16 bytes of each
+// lane (fp32 in eights leaves half of every 32-byte sector to a second access); rows are whole eights or fours long
+// and begin on boundaries of as many elements.  Otherwise threads
 // take every width-th element: a warp's accesses then cover consecutive elements whatever the pitch, and
 // cost no shifting of words (8192 rows of 1601 bf16, layer norm: 39 us with 16-byte loads shifted into place and stores
 // traded between lanes, 24 so).
@@ -166,9 +166,9 @@ __device__ __forceinline__ void store_piece(O *row, const Columns<EVEN, N, W> &c
     }
 }
 
-// Whether rows of a matrix are even in that sense.
-inline bool even_rows(const void *p, int64_t cols, int64_t ld, int size) {
-    return aligned(p, 16) && cols % kPiece == 0 && ld * size % 16 == 0;
+// Whether rows of a matrix are even in that sense, n elements lying together.
+inline bool even_rows(const void *p, int64_t cols, int64_t ld, int size, int n) {
+    return aligned(p, n * size) && cols % n == 0 && ld % n == 0;
 }
 
 // ---- pieces ahead ----------------------------------------------------------------------------------

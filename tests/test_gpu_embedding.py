@@ -62,7 +62,7 @@ def _sums(ids, dy, V, scale):
     return G, (n[:, None] + 1) * U * add(dy.abs()) * abs(scale), n > 0
 
 
-SHAPES = [(1, 1, 1), (1, 5, 7), (3, 2, 8), (9, 100, 9), (32, 11, 256), (33, 1000, 257), (131, 1003, 250), (200, 40, 1600), (700, 5000, 1601), (1500, 37, 33)]
+SHAPES = [(1, 1, 1), (1, 5, 7), (3, 2, 8), (9, 100, 9), (32, 11, 256), (33, 1000, 257), (131, 1003, 250), (200, 40, 1600), (700, 5000, 1601), (1500, 37, 33), (33, 50, 4), (131, 1003, 252), (200, 40, 1028)]
 
 
 @pytest.mark.parametrize("tt,ot", TYPES)
@@ -107,7 +107,7 @@ def test_gradient(T, V, D, gt, dt, kind, pitch, offset):
 
 
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("T,V,D,kind", [(1, 3, 5, "text"), (77, 50, 257, "padded"), (900, 2000, 1600, "text"), (3000, 999, 301, "one"), (64, 64, 8, "distinct"),
+@pytest.mark.parametrize("T,V,D,kind", [(1, 3, 5, "text"), (77, 50, 257, "padded"), (900, 2000, 1600, "text"), (3000, 999, 301, "one"), (3000, 999, 300, "one"), (500, 60, 1028, "text"), (64, 64, 8, "distinct"),
                                         (8192, 600, 24, "text"), (8193, 600, 24, "text")])
 def test_folded_into_moments(T, V, D, kind, dt):
     opt = adama.AdamA()

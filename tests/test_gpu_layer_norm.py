@@ -69,7 +69,7 @@ def _reference_back(dy, x, w, mean, rstd):
 
 
 SHAPES = [(1, 1), (3, 2), (1, 7), (9, 8), (70, 9), (33, 31), (300, 64), (5, 257), (2, 1600), (301, 1000), (7, 1601), (40, 4099), (3, 8192),
-          (3, 8193), (2, 16384), (2, 16390), (65, 16401)]
+          (3, 8193), (2, 16384), (2, 16390), (65, 16401), (9, 4), (70, 12), (33, 260), (301, 1004), (40, 4100), (300, 6152), (2, 8188)]
 
 
 @pytest.mark.parametrize("xt,yt", TYPES)
