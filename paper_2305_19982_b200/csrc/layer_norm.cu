@@ -573,6 +573,7 @@ layer_norm_tiles_kernel(const NormBackArgs a, const float2 *sums) {
 
 // The blocks' sums, 32 columns to a block; warps take every 16th, then the warps' sums in their order.
 constexpr int kJoinWarps = 16;
+constexpr int kJoinLoads = 10;  // of a thread, together: those of 148 blocks at once
 
 __global__ void __launch_bounds__(32 * kJoinWarps)
 layer_norm_join_kernel(const NormBackArgs a, int parts) {
@@ -586,11 +587,14 @@ layer_norm_join_kernel(const NormBackArgs a, int parts) {
     if (m && writes) m_c = __ldcg(m + c), v_c = __ldcg(v + c);  // what the kernel before this one leaves alone
     wait_for_previous();
     const int64_t pad = padded(a.dim);
-    const float *from = a.parts + (of_bias ? pad : 0) + c;
+    const float *from = a.parts + (of_bias ? pad : 0) + min(c, a.dim - 1);
     float s = 0.f;
-    if (c < a.dim) {
-#pragma unroll 8
-        for (int i = warp; i < parts; i += kJoinWarps) s += __ldcg(from + (int64_t)i * 2 * pad);
+    for (int first = warp; first < parts; first += kJoinLoads * kJoinWarps) {
+        float q[kJoinLoads];  // (of a part that there is, and used or not: a load with a condition would wait for the one before)
+#pragma unroll
+        for (int j = 0; j < kJoinLoads; ++j) q[j] = __ldcg(from + (int64_t)min(first + j * kJoinWarps, parts - 1) * 2 * pad);
+#pragma unroll
+        for (int j = 0; j < kJoinLoads; ++j) s += first + j * kJoinWarps < parts ? q[j] : 0.f;
     }
     slots[warp][lane] = s;
     __syncthreads();
