@@ -55,10 +55,11 @@ embedding_kernel(const EmbeddingArgs a, int groups) {
 // ---- sorting by id ---------------------------------------------------------------------------------
 // Ids outside the table get the key `vocab` and come last.
 
-__device__ __forceinline__ unsigned key_of(const EmbeddingGradArgs &a, int64_t t) {
-    const int64_t id = a.ids[t];
+__device__ __forceinline__ unsigned key_of(const EmbeddingGradArgs &a, int64_t id) {
     return id >= 0 && id < a.vocab ? (unsigned)id : (unsigned)a.vocab;
 }
+// Several of a thread's tokens are loaded together, the last token again where there are no more: a load with a condition
+// waits for the one before it.
 
 // Up to kRankTokens tokens: a token's place is the number of tokens that come before it, counted over all
 // of them.  32 tokens to a block, whose warps share the count.
@@ -72,8 +73,17 @@ embedding_rank_kernel(const EmbeddingGradArgs a) {
     let_next_start();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, tokens = (int)a.tokens;
     const int groups = (tokens + 31) / 32;  // of 32 tokens
-#pragma unroll 8
-    for (int i = threadIdx.x; i < 32 * groups; i += 32 * kRankWarps) keys[i] = i < tokens ? key_of(a, i) : 0xffffffffu;
+    constexpr int kThreads = 32 * kRankWarps, kLoads = 4;
+    for (int first = threadIdx.x; first < 32 * groups; first += kLoads * kThreads) {
+        int64_t id[kLoads];
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) id[q] = a.ids[min(first + q * kThreads, tokens - 1)];
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int i = first + q * kThreads;
+            if (i < 32 * groups) keys[i] = i < tokens ? key_of(a, id[q]) : 0xffffffffu;
+        }
+    }
     __syncthreads();
     const int t = blockIdx.x * 32 + lane;
     const unsigned mine = keys[t];
@@ -119,9 +129,6 @@ struct SortPass {
     int shift, next_shift, mask;
     int per;  // tokens of a block, a multiple of kSortThreads
 };
-__device__ __forceinline__ unsigned pass_key(const EmbeddingGradArgs &a, const SortPass &p, int64_t t) {
-    return p.keys ? p.keys[t] : key_of(a, t);
-}
 
 // Counts for the first pass; the other passes' counts (`others` ints behind them) become 0.
 __global__ void __launch_bounds__(kSortThreads)
@@ -131,12 +138,18 @@ embedding_digits_kernel(const EmbeddingGradArgs a, const SortPass p, int *others
     for (int i = threadIdx.x; i < kDigits; i += kSortThreads) counts[i] = 0;
     for (int i = blockIdx.x * kSortThreads + threadIdx.x; i < other_ints; i += gridDim.x * kSortThreads) others[i] = 0;
     __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * p.per;
-#pragma unroll 4
-    for (int64_t t = begin + threadIdx.x; t < begin + p.per && t < a.tokens; t += kSortThreads) {
-        const unsigned key = key_of(a, t);
-        atomicAdd(&counts[key >> p.shift & p.mask], 1);
-        if (key == (unsigned)a.vocab && a.ids[t] >= 0) record_bad_target(a.status, t);
+    const int64_t begin = (int64_t)blockIdx.x * p.per, end = begin + p.per < a.tokens ? begin + p.per : a.tokens;
+    for (int64_t first = begin + threadIdx.x; first < end; first += kRounds * kSortThreads) {
+        int64_t id[kRounds];
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q) id[q] = a.ids[min(first + q * kSortThreads, end - 1)];
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q)
+            if (first + q * kSortThreads < end) {
+                const unsigned key = key_of(a, id[q]);
+                atomicAdd(&counts[key >> p.shift & p.mask], 1);
+                if (key == (unsigned)a.vocab && id[q] >= 0) record_bad_target(a.status, first + q * kSortThreads);
+            }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kDigits; i += kSortThreads) p.counts[blockIdx.x * kDigits + i] = counts[i];
@@ -156,11 +169,22 @@ embedding_scatter_kernel(const EmbeddingGradArgs a, const SortPass p) {
     if (end > a.tokens) end = a.tokens;
     unsigned key[kRounds], token[kRounds];
     const auto load = [&](int64_t base) {
+        if (p.keys) {
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i) {
-            const int64_t t = base + 32 * i + lane;
-            key[i] = t < end ? pass_key(a, p, t) : 0;
-            token[i] = t < end ? (p.order ? p.order[t] : (unsigned)t) : 0;
+            for (int i = 0; i < kRounds; ++i) {
+                const int64_t t = min(base + 32 * i + lane, end - 1);
+                key[i] = p.keys[t];
+                token[i] = p.order[t];
+            }
+        } else {
+            int64_t id[kRounds];
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) id[i] = a.ids[min(base + 32 * i + lane, end - 1)];
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) {
+                key[i] = key_of(a, id[i]);
+                token[i] = (unsigned)(base + 32 * i + lane);
+            }
         }
     };
     for (int64_t base = begin; base < end; base += 32 * kRounds) {
@@ -274,9 +298,20 @@ __device__ __forceinline__ void add_to(Vec &sum, const Vec &x) {
     for (int i = 0; i < kPiece / 2; ++i) sum.p[i] = add2(sum.p[i], x.p[i]);
 }
 
-// Part `slot` of chunk b: 0 continues the chunk before, 1 begins in b and goes on behind it.
-__device__ __forceinline__ float *part_of(const EmbeddingGradArgs &a, int64_t b, int slot) {
-    return a.parts + (2 * b + slot) * a.pad;
+// Part `slot` of chunk b: 0 continues the chunk before, 1 begins in b and goes on behind it.  A tile of it lies by lanes, whatever
+// columns they have, so that none asks which there are.
+__device__ __forceinline__ uint4 *part_of(const EmbeddingGradArgs &a, int64_t b, int slot, int tile) {
+    return reinterpret_cast<uint4 *>(a.parts + (2 * b + slot) * a.pad + tile);
+}
+__device__ __forceinline__ void store_part(uint4 *part, int lane, const Vec &sum) {
+    uint4 w[2];
+    pack_words(sum, w);
+    part[lane] = w[0];
+    part[32 + lane] = w[1];
+}
+__device__ __forceinline__ Vec load_part(const uint4 *part, int lane) {
+    const uint4 w[2] = {part[lane], part[32 + lane]};
+    return widened(w);
 }
 
 constexpr int kGradWarps = 4;
@@ -371,7 +406,7 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
         copies_wait<kDepth - 1>();
         add_to(sum, Given::get(mine + slot * kSlot, dy + (int64_t)t * a.ld_dy, c, 0, lane, 32));
         if (ends >> j & 1) {
-            if (open) store_piece(part_of(a, b, 0) + tile, c, 0, true, sum);
+            if (open) store_part(part_of(a, b, 0, tile), lane, sum);
             else Meets(a, k, tile).finish(mine + slot * kSlot + kGiven, c, lane, sum);
             open = false;
             sum = zeros();
@@ -380,13 +415,14 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
         send_for(j + kDepth, slot);  // behind the last use of what was there
         slot = slot + 1 == kDepth ? 0 : slot + 1;
     }
-    if (live == n && extra == 0 && !(ends >> (n - 1) & 1)) store_piece(part_of(a, b, open ? 0 : 1) + tile, c, 0, true, sum);
+    if (live == n && extra == 0 && !(ends >> (n - 1) & 1)) store_part(part_of(a, b, open ? 0 : 1, tile), lane, sum);
 }
 
 // Runs that fill chunks: a block looks at 32 chunks for those that begin one, and joins the parts of these for one tile;
 // a warp to each, or the block to one of many parts.
 constexpr int kJoinWarps = 8;
 constexpr int kJoinAlone = 12;  // parts up to which a warp adds them alone
+constexpr int kJoinLoads = 4;   // parts of a lane, together
 
 template <typename O, int MODE, bool EVEN, int N>
 __global__ void __launch_bounds__(32 * kJoinWarps)
@@ -410,12 +446,17 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
     for (int turn = 0; todo; todo &= todo - 1) {  // (all warps see the same)
         const int which = __ffs(todo) - 1;
         const unsigned k = __shfl_sync(none, key, which);
-        int64_t last = first + which;  // the chunk in which the run ends
-        for (int run = 32; run == 32; last += run) {
-            const int64_t at = (last + 1 + lane) * chunk;
-            const unsigned more = __ballot_sync(none, at < a.tokens && __ldcg(a.keys + at) == k);
-            run = more == none ? 32 : __ffs(~more) - 1;
-        }
+        // the chunk in which the run ends, among the next 32 or, of a long run, by ever closer looks at 32 places
+        int64_t last = first + which, end_chunk = (a.tokens + chunk - 1) / chunk, apart = 1;
+        do {
+            const int64_t at = (last + (lane + 1) * apart) * chunk;
+            const unsigned more = __ballot_sync(none, at < a.tokens && __ldcg(a.keys + min(at, a.tokens - 1)) == k);
+            const int run = more == none ? 32 : __ffs(~more) - 1;
+            last += run * apart;
+            if (apart == 1 && run < 32) break;
+            if (run < 32 && last + apart < end_chunk) end_chunk = last + apart;  // it ends before that one
+            apart = (end_chunk - last + 31) / 32;
+        } while (end_chunk - last > 1);
         if (lane == 0) last_of[which] = last;  // (every warp writes the same)
         if (last - first - which > kJoinAlone) of_block |= 1u << which;
         else if (turn++ % kJoinWarps == warp) of_warp |= 1u << which;
@@ -425,9 +466,17 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
     if (ahead >= 0) Meets(a, __shfl_sync(none, key, ahead), tile).send_for(slots[warp], c, lane);
     copies_end_group();
     wait_for_previous();
+    // (a turn's last parts are loaded again where there are no more: a load with a condition waits for the one before it)
     const auto sum_parts = [&](Vec &sum, int64_t from, int64_t to) {
-#pragma unroll 4
-        for (int64_t i = from; i < to; ++i) add_to(sum, load_piece(part_of(a, i, 0) + tile, c, 0, true));
+        for (; from < to; from += kJoinLoads) {
+            Vec q[kJoinLoads];
+#pragma unroll
+            for (int j = 0; j < kJoinLoads; ++j) q[j] = load_part(part_of(a, min(from + j, to - 1), 0, tile), lane);
+#pragma unroll
+            for (int j = 0; j < kJoinLoads; ++j)
+#pragma unroll
+                for (int i = 0; i < kPiece / 2; ++i) sum.p[i] = add2(sum.p[i], from + j < to ? q[j].p[i] : 0);
+        }
     };
     for (; of_warp; of_warp &= of_warp - 1) {
         const int which = __ffs(of_warp) - 1;
@@ -436,7 +485,7 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
             meets.send_for(slots[warp], c, lane);
             copies_end_group();
         }
-        Vec sum = load_piece(part_of(a, first + which, 1) + tile, c, 0, true);
+        Vec sum = load_part(part_of(a, first + which, 1, tile), lane);
         sum_parts(sum, first + which + 1, last_of[which] + 1);
         copies_wait<0>();
         meets.finish(slots[warp], c, lane, sum);
@@ -445,7 +494,7 @@ embedding_join_kernel(const EmbeddingGradArgs a, int chunk) {
     for (; of_block; of_block &= of_block - 1) {
         const int which = __ffs(of_block) - 1;
         const int64_t b = first + which, parts = last_of[which] - b;
-        Vec sum = warp == 0 ? load_piece(part_of(a, b, 1) + tile, c, 0, true) : zeros();
+        Vec sum = warp == 0 ? load_part(part_of(a, b, 1, tile), lane) : zeros();
         sum_parts(sum, b + 1 + parts * warp / kJoinWarps, b + 1 + parts * (warp + 1) / kJoinWarps);
 #pragma unroll
         for (int q = 0; q < kPiece / 2; ++q) sums[warp][q * 32 + lane] = sum.p[q];
@@ -494,7 +543,7 @@ GradPlan plan_grad(int64_t tokens, int dim, int sm_count) {
     p.tiles = (dim + kTile - 1) / kTile;
     p.chunk = chunk_for(tokens, p.tiles, sm_count);
     p.chunks = (tokens + p.chunk - 1) / p.chunk;
-    p.pad = ((int64_t)dim + kPiece - 1) / kPiece * kPiece;
+    p.pad = (int64_t)p.tiles * kTile;
     p.list = up16((size_t)tokens * sizeof(unsigned));
     p.parts = p.chunks > 1 ? (size_t)p.chunks * 2 * p.pad * sizeof(float) : 0;
     p.by_rank = tokens <= kRankTokens;
