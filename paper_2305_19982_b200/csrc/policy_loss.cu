@@ -596,9 +596,10 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             O *y = static_cast<O *>(a.dlogits) + due * a.ld_dlogits;
             const RowWriter<T, O> out(y, shape, q.top, q.unit, q.per_e, k);
             Cursor<kStages> at_stage = due_at;
-            const auto release = [&]() {
+            const unsigned zero = (unsigned)log_cluster >> 8;  // which the compiler does not know
+            const auto release = [&](unsigned was_read = 0) {
                 __syncwarp();
-                if (lane == 0) barrier_arrive(shared_addr(&sh.empty[at_stage.slot]));
+                if (lane == 0) barrier_arrive(shared_addr(&sh.empty[at_stage.slot]) + was_read);
             };
             O *p = y + shape.head + (int64_t)(from + t) * kUnit<T>;
             bool skip = !a.dlogits || !ok;
@@ -614,8 +615,9 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             }
             if (out.shift == 0) {
                 int at = 0;
-                // Stages are given back behind the stores that use what was read from them: a load that has been issued
-                // need not have read yet when a lane's arrival is seen, and the stage is then filled anew under it.
+                // A stage is given back when it has been read, not when its loads have been issued: a load that is still on its
+                // way when a lane's arrival is seen would find the stage filled anew.  So the arrival's address is made to
+                // depend on what was read; elsewhere it stands behind the stores.
                 for (; count - at >= 2 * kStageUnits; at += 2 * kStageUnits, p += 2 * kStageUnits * kUnit<T>) {
                     uint4 u[2 * kEach];
                     Cursor<kStages> second = at_stage;
@@ -627,27 +629,33 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
                         for (int i = 0; i < kEach; ++i) u[j * kEach + i] = units[i * kRingWork];
                     }
 #pragma unroll
-                    for (int i = 0; i < 2 * kEach; ++i) {
-                        out.put(u[i], p + i * kRingWork * kUnit<T>);
-                        if (i + 1 == kEach || i + 1 == 2 * kEach) {
-                            release();
-                            at_stage.advance();
-                        }
+                    for (int j = 0; j < 2; ++j) {
+                        unsigned read = 0;
+#pragma unroll
+                        for (int i = 0; i < kEach; ++i) read ^= u[j * kEach + i].x;
+                        release(read & zero);
+                        at_stage.advance();
                     }
+#pragma unroll
+                    for (int i = 0; i < 2 * kEach; ++i) out.put(u[i], p + i * kRingWork * kUnit<T>);
                 }
                 for (; at < count; at += kStageUnits, at_stage.advance(), p += kStageUnits * kUnit<T>) {
                     const uint4 *units = reinterpret_cast<const uint4 *>(sh.stage[at_stage.slot]) + t;
                     if (count - at >= kStageUnits) {
                         uint4 u[kEach];
+                        unsigned read = 0;
 #pragma unroll
                         for (int i = 0; i < kEach; ++i) u[i] = units[i * kRingWork];
+#pragma unroll
+                        for (int i = 0; i < kEach; ++i) read ^= u[i].x;
+                        release(read & zero);
 #pragma unroll
                         for (int i = 0; i < kEach; ++i) out.put(u[i], p + i * kRingWork * kUnit<T>);
                     } else {
 #pragma unroll 1
                         for (int i = 0; i < count - at - t; i += kRingWork) out.put(units[i], p + i * kUnit<T>);
+                        release();
                     }
-                    release();
                 }
             } else {
                 for (int at = 0; at < count; at += kStageUnits, p += kStageUnits * kUnit<T>) {

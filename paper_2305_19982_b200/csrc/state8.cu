@@ -379,11 +379,13 @@ fold_apply8_ring_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f
             x.vc = load_codes(st.v + o);
             x.sm = st.sm[warp];
             x.sv = st.sv[warp];
+            // The stage is given back when it has been read, not when its loads have been issued (one that is still on its way
+            // when the arrival is seen would find the stage filled anew): behind the exchange of the blocks' largest moments,
+            // and at an address that depends on the weights, which have no part in that.  The zero is not known to the compiler.
+            const unsigned read = (__float_as_uint(x.w[0]) ^ __float_as_uint(x.w[4])) & (unsigned)(n >> 63);
             const float2 top = x.update(factor, f, c);
-            // behind the arithmetic that uses what was read: a load that has been issued need not have read yet when the
-            // arrival is seen
             __syncwarp();
-            if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]));
+            if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]) + read);
             x.store_wide(s, tab.w[t], tab.copy[t], at + 4 * lane);
             Block8::store_scales(s, blk, top, lane, c);
         } else {
