@@ -8,8 +8,12 @@
 // a chunk's columns 256 at a time and sums equal neighbours in registers, in fp32.  A run of equal tokens that
 // lies inside a chunk is finished there; the parts of one that crosses chunks go to the workspace, and a second
 // kernel adds them in order; one that only reaches into the next chunk is finished by the warp that has its
-// beginning.  So a token that occurs thousands of times is spread over the card like any others,
-// no atomics are involved and results do not depend on scheduling.  Bound by HBM.
+// beginning.  So a token that occurs thousands of times is spread over the card like any others, no sum is made by
+// atomics (the counts of the sort are, and whole numbers do not care for an order), and results do not depend on scheduling.
+//
+// The lookup of 16384 x 4096 bf16 takes 32 us = 5.6 TB/s, bound by HBM (7 x 1600: 2.1 us).  Gradients: 32768 x 4096 bf16 into a
+// whole bf16 table of 32000 rows 113 us = 4.6 TB/s; 60000 x 1024 fp32 added 92 us = 5.1 TB/s; 4096 x 1600 bf16 folded 24 us =
+// 2.8 TB/s: short ones are four or five kernels that wait for each other, each some 4 us long.
 #include "adama_device.cuh"
 #include "chained.cuh"
 #include "row_access.cuh"
@@ -62,8 +66,9 @@ __device__ __forceinline__ unsigned key_of(const EmbeddingGradArgs &a, int64_t i
 // waits for the one before it.
 
 // Up to kRankTokens tokens: a token's place is the number of tokens that come before it, counted over all
-// of them.  32 tokens to a block, whose warps share the count.
-constexpr int kRankTokens = 8192;
+// of them.  32 tokens to a block, whose warps share the count.  (The whole gradient by this and by the digits below: 4096 x 1600 of
+// 50257 ids 24 and 29 us, 5500 x 256 20 and 20, 8000 x 256 25 and 21; 4096 x 64 of 500 ids, which one pass sorts, 14 and 13.)
+constexpr int kRankTokens = 5120;
 constexpr int kRankWarps = 16;
 
 __global__ void __launch_bounds__(32 * kRankWarps)
@@ -421,7 +426,8 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
 // Runs that fill chunks: a block looks at 32 chunks for those that begin one, and joins the parts of these for one tile;
 // a warp to each, or the block to one of many parts.
 constexpr int kJoinWarps = 8;
-constexpr int kJoinAlone = 12;  // parts up to which a warp adds them alone
+// parts up to which a warp adds them alone (32768 x 4096: 113 us, up to 4 113, up to 40 125; 4096 x 1600: 24, 25, 25)
+constexpr int kJoinAlone = 12;
 constexpr int kJoinLoads = 4;   // parts of a lane, together
 
 template <typename O, int MODE, bool EVEN, int N>
@@ -530,8 +536,9 @@ cudaError_t lookup(const EmbeddingArgs &a, cudaStream_t stream) {
 // Sizes of the parts of the workspace, each a multiple of 16 bytes.
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
-// Tokens to a chunk: 16 where that makes several rounds of warps.
-int chunk_for(int64_t tokens, int tiles, int sm_count) { return tokens * tiles / 16 < (int64_t)48 * sm_count ? 8 : 16; }
+// Tokens to a chunk: 16 where that makes warps enough.  (With 8 and with 16: 32768 x 4096 127 and 113 us, 65536 x 256 52 and 48,
+// 4096 x 1600 24.0 and 24.8, 8000 x 256 25 and 29.)
+int chunk_for(int64_t tokens, int tiles, int sm_count) { return tokens * tiles / 16 < (int64_t)14 * sm_count ? 8 : 16; }
 struct GradPlan {
     int tiles, chunk;
     int64_t chunks, pad;

@@ -7,7 +7,13 @@
 // no precision.  In the backward pass a thread keeps its columns for all rows of its block, with their two sums
 // in registers; the blocks' sums go to the workspace, and a second, short kernel adds them in the blocks' order
 // and writes the parameters' gradients or folds them into their moments (m += a*g, v += b*g^2: the sum over
-// rows is complete before it is squared).  Nothing depends on scheduling.  Bound by HBM.
+// rows is complete before it is squared).  Nothing depends on scheduling.
+//
+// Bound by HBM where there is enough to do: 16384 x 4096 bf16 takes 48 us forward = 5.6 TB/s, 75 us backward = 5.4 TB/s.  4096 x 1600
+// is one wave, in which launch, first rows, sums across warps and the last rows come in sequence: 13 us forward (fp32 to
+// bf16, floor 6), 17 us backward with the moments (floor 6).  One row: 2.8 us.  Rows that are not even (row_access.cuh) are bound
+// by instructions, an element to an access: 8192 x 1601 bf16 24 us forward, 39 backward (floors 8 and 12).  Bringing them to
+// shared memory by the 16 bytes made them slower (17696 x 760 39 -> 57): it is not latency that they wait for.
 #include "adama_device.cuh"
 #include "chained.cuh"
 #include "row_access.cuh"
@@ -640,7 +646,8 @@ cudaError_t forward_groups(const NormArgs &a, const RowPlan &p, int sm_count, cu
 }
 
 // Pieces to a thread and warps to a row: as many pieces as leave every SM eight warps, up to `most`; warps rounded up to
-// a power of two where the compiler has to know them.
+// a power of two where the compiler has to know them.  (With 8, 4 and 2 pieces, bf16: 16384 x 4096 48, 56 and 72 us; 8192 x 1024 13.0,
+// 11.0 and 11.7, taken 4; 30000 x 512 28, 21 and 16, taken 2; 700 x 4096 6.9, 6.2 and 6.9.)
 RowPlan plan_rows(int64_t rows, int pieces, int sm_count, int most, bool power) {
     RowPlan p;
     p.pieces = pieces;
@@ -712,6 +719,7 @@ struct BackPlan : RowPlan {
 BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even, bool wide) {
     BackPlan p;
     p.pieces = (int)(padded(dim) / kPiece);
+    // two pieces to a thread (16384 x 4096 bf16 75 us, one 102; 32816 x 512 31, 36; 4096 x 1600 17.1, 16.4), one where there are few rows
     p.each = p.pieces > 32 * kGroupWarps || (even && rows >= 2 * (int64_t)sm_count) ? 2 : 1;
     p.warps = (p.pieces + 32 * p.each - 1) / (32 * p.each);
     while (!even && p.pieces > 32 && (p.warps & (p.warps - 1))) ++p.warps;  // the compiler has to know them
@@ -725,8 +733,8 @@ BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even, bool wide) {
         const int64_t tiles = (dim + kTileColumns * kLanesThreads - 1) / (kTileColumns * kLanesThreads);
         most = (4 * (int64_t)sm_count + tiles - 1) / tiles;
     } else {
-        // as many groups to a block as it has warps for (half as many, where even rows in fp32 fill shared memory), fewer where that
-        // would leave SMs without any
+        // as many groups to a block as it has warps for (half as many, where even rows in fp32 fill shared memory: 4096 x 4096 38 us, else
+        // 57), fewer where that would leave SMs without any
         p.groups = (wide && p.warps <= kGroupWarps / 2 ? kGroupWarps / 2 : kGroupWarps) / p.warps;
         while (p.groups > 1 && rows < (int64_t)sm_count * p.groups) p.groups -= 1;
     }

@@ -35,7 +35,7 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 narrowed<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
 
 // Elements that lie together in a piece of even rows whose matrices have elements of these sizes.
-__host__ __device__ constexpr int together(size_t a, size_t b = 2, size_t c = 2) { return a == 2 && b == 2 && c == 2 ? 8 : 4; }
+__host__ __device__ constexpr int together(size_t a, size_t b) { return a == 2 && b == 2 ? 8 : 4; }
 
 // Columns of a thread: element i of its piece u, of threads `t` of a row's `width`; N elements lie together.  W: that
 // width, known to the compiler (0: it is not), so that uneven rows' accesses need no address of their own each.

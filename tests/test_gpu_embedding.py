@@ -128,7 +128,7 @@ def test_folded_into_moments(T, V, D, kind, dt):
     _outside_untouched(vb, v)
 
 
-@pytest.mark.parametrize("T,V", [(8192, 50257), (8193, 50257), (20_000, 300), (70_001, 131_072), (200_000, 511), (9000, 512), (9000, 1), (12_345, 300_000)])
+@pytest.mark.parametrize("T,V", [(5120, 50257), (5121, 50257), (8192, 50257), (8193, 50257), (20_000, 300), (70_001, 131_072), (200_000, 511), (9000, 512), (9000, 1), (12_345, 300_000)])
 @pytest.mark.parametrize("kind", ["text", "padded", "one", "sorted"])
 def test_either_way_of_sorting(T, V, kind):
     """Whole numbers: sums are exact in any order, so a token in a wrong place shows."""
