@@ -26,16 +26,21 @@ struct RawEntries {
     unsigned t[kTopEach];  // fp32 or bf16
 };
 __device__ __forceinline__ void load_entries(const DistillArgs &a, int64_t row, int lane, RawEntries &r) {
-    const int64_t *ids = a.ids + row * a.ld_ids + lane;
-    const int64_t at = row * a.ld_teacher + lane;
-    const bool wide = a.teacher_dtype == ADAMA_F32;
+    // (the last entry again where there are no more: a load with a condition of its own waits for the one before it)
+    const int64_t *ids = a.ids + row * a.ld_ids;
+    const int64_t first = row * a.ld_teacher;
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e)
-        if (in_use(a, e) && 32 * e + lane < a.top) {
-            r.id[e] = ids[32 * e];
-            if (wide) r.t[e] = static_cast<const unsigned *>(a.teacher)[at + 32 * e];
-            else r.t[e] = static_cast<const unsigned short *>(a.teacher)[at + 32 * e];
-        }
+        if (in_use(a, e)) r.id[e] = ids[min(32 * e + lane, a.top - 1)];
+    if (a.teacher_dtype == ADAMA_F32) {
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e)
+            if (in_use(a, e)) r.t[e] = static_cast<const unsigned *>(a.teacher)[first + min(32 * e + lane, a.top - 1)];
+    } else {
+#pragma unroll
+        for (int e = 0; e < kTopEach; ++e)
+            if (in_use(a, e)) r.t[e] = static_cast<const unsigned short *>(a.teacher)[first + min(32 * e + lane, a.top - 1)];
+    }
 }
 
 __device__ __forceinline__ float warp_sum(float x) {

@@ -877,7 +877,7 @@ distill_teacher_kernel(const DistillArgs a) {
 #pragma unroll
     for (int e = 0; e < kTopEach; ++e) {
         x_at[e] = narrow<T>(0.f);
-        if (in_use(a, e) && 32 * e + lane < a.top && raw.id[e] >= 0 && raw.id[e] < a.vocab) x_at[e] = x[raw.id[e]];
+        if (in_use(a, e)) x_at[e] = x[min(max(raw.id[e], (int64_t)0), a.vocab - 1)];  // (used where there is an entry)
     }
     Entries en = entries_of(a, raw, lse, lane);
     if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
@@ -1129,7 +1129,7 @@ cudaError_t distill(const DistillArgs &a, int sm_count, cudaStream_t stream, int
     if (e != cudaSuccess) return e;
     *launches += whole ? 1 : a.rows > 0 ? 3 : 2;
     if (!whole) {
-        const unsigned grid = grid_of(rows, (int64_t)sm_count * 2);
+        const unsigned grid = grid_of(rows, (int64_t)sm_count * 4);
         return launch_chained(distill_entries_kernel<O>, dim3(grid), dim3(32 * kEntryWarps), 0, stream, a, (float)(a.scale_exact * kLog2e));
     }
     return cudaGetLastError();
