@@ -383,7 +383,7 @@ distill_rows_kernel(const DistillArgs a, float k) {
         Entries en = entries_of(a, raw, a.teacher_lse ? a.teacher_lse[row] : 0.f, lane);
         float x_at[kTopEach];
 #pragma unroll
-        for (int e = 0; e < kTopEach; ++e) x_at[e] = en.id[e] >= 0 ? widen(x[en.id[e]]) : 0.f;
+        for (int e = 0; e < kTopEach; ++e) x_at[e] = in_use(a, e) ? widen(x[max(en.id[e], 0)]) : 0.f;
         if (any_twice(a, en)) join_twice(en.id, en.p, en.own);
         Running<false> run;
 #pragma unroll
@@ -905,7 +905,7 @@ distill_entries_kernel(const DistillArgs a, float k) {
         float4 q[kTopEach];  // (what a row without weight left there is not used)
 #pragma unroll
         for (int e = 0; e < kTopEach; ++e)
-            if (32 * e + lane < a.top) q[e] = a.entries[row * a.top + 32 * e + lane];
+            if (in_use(a, e)) q[e] = a.entries[row * a.top + min(32 * e + lane, a.top - 1)];
         const float2 of_row = a.row_stats[row], of_teacher = a.masses[row];
         if (weight == 0.f) {
             if (lane == 0 && a.loss) a.loss[row] = 0.f;
