@@ -10,7 +10,7 @@
 // of 50304 bf16 with entropy: 69 us = 5.98 TB/s; loss and gradient of 8192 rows of 50257, a quarter of them
 // masked: 252 us = 5.7 TB/s, of 6103 rows of 32768, which fill the ring's stages, 123 us = 5.7 TB/s; the
 // log-probability of one row of 50257 fp32: 3.9 us.  Distillation of 4096 x 50257 bf16 from 64 entries, a quarter masked:
-// 153 us = 4.7 TB/s, of 24 x 32000 fp32 10.3 us, in three kernels.
+// 150 us = 4.8 TB/s, of 24 x 32000 fp32 10.3 us, in three kernels.
 
 #include "adama_device.cuh"
 #include "bulk_copy.cuh"
