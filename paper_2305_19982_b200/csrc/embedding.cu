@@ -17,6 +17,7 @@
 #include "adama_device.cuh"
 #include "chained.cuh"
 #include "row_access.cuh"
+#include "row_writer.cuh"
 #include "tensor_table.cuh"
 
 namespace adama {
@@ -321,15 +322,6 @@ __device__ __forceinline__ Vec load_part(const uint4 *part, int lane) {
 
 constexpr int kGradWarps = 4;
 
-template <typename O>
-__device__ __forceinline__ void zero_row(O *p, int n, int lane) {
-    constexpr int kPer = 16 / sizeof(O);
-    const int past = (int)(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(O));
-    const int head = past ? (kPer - past < n ? kPer - past : n) : 0, body = (n - head) / kPer, tail = head + body * kPer;
-    for (int i = lane; i < body; i += 32) reinterpret_cast<uint4 *>(p + head)[i] = make_uint4(0, 0, 0, 0);
-    if (lane < head) p[lane] = narrowed<O>(0.f);
-    if (lane < n - tail) p[tail + lane] = narrowed<O>(0.f);
-}
 constexpr int kZeroRows = 8;  // rows of a warp, of those that may have no token
 
 // chunk: tokens of a warp, up to 16: a lane each for them and for the next chunk's.  The first zero_blocks blocks zero the rows that have no token.
@@ -361,7 +353,7 @@ embedding_grad_kernel(const EmbeddingGradArgs a, int chunk, int tiles, unsigned 
         const bool empty = lane < kZeroRows && row < a.vocab && (lo == a.tokens || (int64_t)a.keys[lo] != row);
         unsigned todo = __ballot_sync(0xffffffffu, empty);
         for (; todo; todo &= todo - 1)
-            zero_row(static_cast<O *>(a.grad) + (first + __ffs(todo) - 1) * a.ld_grad, a.dim, lane);
+            fill_zeros(static_cast<O *>(a.grad) + (first + __ffs(todo) - 1) * a.ld_grad, a.dim, lane, 32);
         return;
     }
     const int64_t task = (int64_t)(blockIdx.x - zero_blocks) * kGradWarps + warp, b = task / tiles;

@@ -242,7 +242,7 @@ layer_norm_long_kernel(const NormArgs a) {
     }
     O *y = static_cast<O *>(a.y) + row * a.ld_y;
     for (int c = threadIdx.x; c < a.dim; c += kLongThreads)
-        y[c] = narrowed<O>(fmaf((widen(x[c]) - mean) * rstd, a.weight[c], a.bias ? a.bias[c] : 0.f));
+        y[c] = narrow<O>(fmaf((widen(x[c]) - mean) * rstd, a.weight[c], a.bias ? a.bias[c] : 0.f));
 }
 
 // ---- backward ------------------------------------------------------------------------------------
@@ -563,7 +563,7 @@ layer_norm_tiles_kernel(const NormBackArgs a, const float2 *sums) {
             const float g = widen(dy0[row * a.ld_dy + c]), xhat = (widen(x0[row * a.ld_x + c]) - mean) * rstd;
             db[i] += g;
             dw[i] = fmaf(g, xhat, dw[i]);
-            if (a.dx) dx0[row * a.ld_dx + c] = narrowed<T>(rstd * (g * w[i] - fmaf(xhat, s.y, s.x)));
+            if (a.dx) dx0[row * a.ld_dx + c] = narrow<T>(rstd * (g * w[i] - fmaf(xhat, s.y, s.x)));
         }
     }
     if (!a.parts) return;

@@ -27,13 +27,6 @@ __device__ __forceinline__ float pair_sum(Pair p) {
     return a + b;
 }
 
-template <typename O>
-__device__ __forceinline__ O narrowed(float y);
-template <>
-__device__ __forceinline__ float narrowed<float>(float y) { return y; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 narrowed<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
-
 // Elements that lie together in a piece of even rows whose matrices have elements of these sizes.
 __host__ __device__ constexpr int together(size_t a, size_t b) { return a == 2 && b == 2 ? 8 : 4; }
 
@@ -98,7 +91,7 @@ struct Piece {
             const T *from = row + c.t;
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) {
-                odd[i] = narrowed<T>(0.f);
+                odd[i] = narrow<T>(0.f);
                 if (live && c.has(u, i)) odd[i] = from[(u * kPiece + i) * c.width()];
             }
         }
@@ -160,8 +153,8 @@ __device__ __forceinline__ void store_piece(O *row, const Columns<EVEN, N, W> &c
         for (int i = 0; i < kPiece / 2; ++i) {
             float a, b;
             split(v.p[i], a, b);
-            if (live && c.has(u, 2 * i)) to[(u * kPiece + 2 * i) * c.width()] = narrowed<O>(a);
-            if (live && c.has(u, 2 * i + 1)) to[(u * kPiece + 2 * i + 1) * c.width()] = narrowed<O>(b);
+            if (live && c.has(u, 2 * i)) to[(u * kPiece + 2 * i) * c.width()] = narrow<O>(a);
+            if (live && c.has(u, 2 * i + 1)) to[(u * kPiece + 2 * i + 1) * c.width()] = narrow<O>(b);
         }
     }
 }

@@ -6,13 +6,6 @@
 
 namespace adama {
 
-template <typename O>
-__device__ __forceinline__ O narrow(float y);
-template <>
-__device__ __forceinline__ float narrow<float>(float y) { return y; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
-
 // N values as 32-bit words of their type
 __device__ __forceinline__ void to_words(const float (&v)[4], unsigned (&w)[4], float) {
 #pragma unroll

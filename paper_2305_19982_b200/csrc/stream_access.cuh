@@ -57,6 +57,12 @@ __device__ __forceinline__ Grad4 load_grad4(const __nv_bfloat16 *g, size_t i4) {
 }
 __device__ __forceinline__ float widen(float g) { return g; }
 __device__ __forceinline__ float widen(__nv_bfloat16 g) { return __bfloat162float(g); }
+template <typename O>
+__device__ __forceinline__ O narrow(float y);
+template <>
+__device__ __forceinline__ float narrow<float>(float y) { return y; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 

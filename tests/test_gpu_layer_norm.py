@@ -1,10 +1,11 @@
 """Layer norm (adama_layer_norm) and its backward pass (adama_layer_norm_backward) against the formulas in 64 bits.
 
-Tolerances, u = 2^-24.  A sum over a row of D elements adds at most 8*ceil(D/4096) + 8 of them in a thread and
-meets 10 more levels in warp and block: its error is at most K = (8*ceil(D/4096) + 24)*u of the mean magnitude.
+Tolerances, u = 2^-24.  A sum over a row of D elements passes through at most 8*ceil(D/4096) + 3 additions in a thread, 5 between lanes
+and 16 over warps: its error is at most K = (8*ceil(D/4096) + 24)*u of the mean magnitude.
     y: mean K*mean|x|, rstd relative K, the operations behind them 4u: |w|*(|xhat|*(K + 4u) + rstd*K*mean|x|) + 4u*(|w xhat| + |b|)
     dx: rstd*(K*(mean|g| + |xhat|*mean|g xhat|) + 8u*(|g| + |s1| + |xhat s2|))   (mean and rstd are inputs)
-    dweight, dbias: a block adds R/blocks rows one after the other, the blocks' sums meet 16 ways: (R/64 + 64)*u*sum|.|
+    dweight, dbias: a thread adds its block's rows one after the other (R/64 of them at most, where blocks are fewer than rows), then
+        come at most 16 sums in a block, 19 of blocks and 16 of these: (R/64 + 64)*u*sum|.|
 and half a last place of the output's type each."""
 import numpy as np
 import pytest
