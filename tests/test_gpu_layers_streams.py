@@ -182,3 +182,59 @@ def test_rows_of_the_gradient_are_refused_from_a_length_on():
     opt.embedding(ids, wide + 2.5, out)
     assert bool((out == 2.5).all())
     opt.sync_status()
+
+
+@pytest.mark.parametrize("T", [1, 50, 9000])
+@pytest.mark.parametrize("D", [5, 64, 1028])
+def test_a_batch_of_nothing_but_padding(T, D):
+    opt = adama.AdamA()
+    opt.begin_minibatch(1)
+    ids = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+    dy, table = torch.full((T, D), float("nan"), device="cuda"), torch.full((77, D), 3.0, device="cuda")
+    out = torch.full((T, D), 7.0, device="cuda")
+    opt.embedding(ids, table, out)
+    assert not bool(out.any())
+    m, v, grad = (torch.full((77, D), 3.0, device="cuda") for _ in range(3))
+    opt.embedding_grad_fold(ids, dy, m, v)
+    opt.embedding_grad(ids, dy, grad, accumulate=True)
+    assert all(torch.equal(t, table) for t in (m, v, grad))
+    opt.embedding_grad(ids, dy, grad)
+    assert not bool(grad.any())
+    # a distillation of which no row counts
+    logits, d = torch.full((T, 3 * D), float("nan"), device="cuda"), torch.full((T, 3 * D), 7.0, device="cuda")
+    stats, loss = torch.full((4,), 7.0, device="cuda"), torch.full((T,), 7.0, device="cuda")
+    opt.distill_loss(logits, dy[:, :5], ids[:, None].expand(T, 5).contiguous(), torch.zeros(T, device="cuda"), d, stats, loss=loss)
+    assert not bool(d.any()) and not bool(stats.any()) and not bool(loss.any())
+    opt.sync_status()
+
+
+def test_calls_from_several_threads():
+    """A context and a stream to each thread, the same inputs."""
+    import threading
+    x, w, ids, dy = _rand((500, 1600), 1), _rand((1600,), 2), (torch.arange(500) % 37).cuda(), _rand((500, 1600), 3)
+    results, errors = [], []
+
+    def work():
+        try:
+            opt, y, grad = adama.AdamA(), torch.empty_like(x), torch.empty(37, 1600, device="cuda")
+            mean, rstd = torch.empty(2, 500, device="cuda")
+            dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(50):
+                    opt.layer_norm(x, w, None, y, mean, rstd)
+                    opt.layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db)
+                    opt.embedding_grad(ids, dy, grad)
+                torch.cuda.current_stream().synchronize()
+            opt.sync_status()
+            results.append((y, dx, dw, db, grad))
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    assert all(torch.equal(a, b) for r in results[1:] for a, b in zip(r, results[0]))
