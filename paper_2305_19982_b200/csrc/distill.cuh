@@ -163,8 +163,9 @@ __device__ __forceinline__ EntryTerms entry_terms(float x, float p, float own, f
                                                   float inv, float k) {
     EntryTerms t;
     const float d = x - top, q = exp2_fast(k * d) * inv;
-    t.held = mass == mass ? q : mass;
-    t.g = unit * fmaf(mass, q, -own);
+    // no mass: nothing to learn here either, and no NaN of the student's row (fmaxf leaves it out) in any sum
+    t.held = mass == 0.f ? fmaxf(q, 0.f) : mass == mass ? q : mass;
+    t.g = mass == 0.f ? 0.f : unit * fmaf(mass, q, -own);
     t.cross = p != 0.f ? p * (log_sum - scale * d) : 0.f;  // no probability, no loss, also where the student has none either
     if (mass != mass) t.cross = mass;
     return t;
