@@ -473,8 +473,8 @@ ADAMA_API adama_status adama_policy_loss(adama_ctx *ctx, const adama_policy_args
  * P = 1.  (With it, and P < 1, the terms are the entries' part of the divergence, which alone may be below 0.)  An
  * entry with a negative index, or a teacher's logit of -inf, has p = 0; a row without any other (P = 0) has
  * loss and gradient 0 whatever its logits, and adds 0 to every sum where these are not finite.  An index may occur more
- * than once in a row: each entry has its own term.  A row with w = 0 is not read: its
- * dlogits and loss are 0 and it adds nothing to stats.
+ * than once in a row: each entry has its own term.  A row with w = 0 has dlogits and loss 0 and adds nothing to stats:
+ * its logits are not read, and nothing that is read of its entries is used.
  *   logits, dlogits : as for adama_policy_loss (dlogits may be NULL, or logits itself)
  *   teacher_logits  : [rows, top] fp32 or bf16, pitch ld_teacher;   ids : [rows, top] int64, pitch ld_ids
  *   top         : 1 to ADAMA_DISTILL_TOP
