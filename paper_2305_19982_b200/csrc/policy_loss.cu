@@ -599,10 +599,20 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             const RowWriter<T, O> out(y, shape, q.top, q.unit, q.per_e, k);
             Cursor<kStages> at_stage = due_at;
             const unsigned zero = (unsigned)log_cluster >> 8;  // which the compiler does not know
-            const auto release = [&](unsigned was_read = 0) {
+            // A stage is given back when it has been read, not when its loads have been issued: a load that is still on its way
+            // when the arrival is seen would find the stage filled anew.  So it is given back behind the stores of what was
+            // read, or as soon as that has come, by an arrival whose address depends on it: a vote, since one lane arrives
+            // for all of the warp, and lanes may run apart.  (4096 x 50257 bf16 distilled: 151 us so, 157 behind the stores.)
+            // A stage is given back when it has been read, not when its loads have been issued: a load that is still on its way
+            // when the arrival is seen would find the stage filled anew.  So it is given back behind the stores of what was
+            // read, or as soon as that has come, by an arrival whose address depends on it.  One lane arrives for its warp, and
+            // lanes may run apart, so it is a vote of all lanes that the address depends on.  (8192 x 50257 bf16: 252 us, 261
+            // behind the stores; 252 with the arriving lane's own words alone.)
+            const auto release = [&](unsigned nothing = 0u) {
                 __syncwarp();
-                if (lane == 0) barrier_arrive(shared_addr(&sh.empty[at_stage.slot]) + was_read);
+                if (lane == 0) barrier_arrive(shared_addr(&sh.empty[at_stage.slot]) + nothing);
             };
+            const auto once_read = [&](unsigned read) { return (unsigned)__any_sync(0xffffffffu, (read & zero) != 0u); };  // 0
             O *p = y + shape.head + (int64_t)(from + t) * kUnit<T>;
             bool skip = !a.dlogits || !ok;
             if constexpr (kDistill<Args>) {
@@ -617,9 +627,6 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
             }
             if (out.shift == 0) {
                 int at = 0;
-                // A stage is given back when it has been read, not when its loads have been issued: a load that is still on its
-                // way when a lane's arrival is seen would find the stage filled anew.  So the arrival's address is made to
-                // depend on what was read; elsewhere it stands behind the stores.
                 for (; count - at >= 2 * kStageUnits; at += 2 * kStageUnits, p += 2 * kStageUnits * kUnit<T>) {
                     uint4 u[2 * kEach];
                     Cursor<kStages> second = at_stage;
@@ -630,14 +637,14 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
 #pragma unroll
                         for (int i = 0; i < kEach; ++i) u[j * kEach + i] = units[i * kRingWork];
                     }
+                    unsigned read = 0;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        unsigned read = 0;
-#pragma unroll
-                        for (int i = 0; i < kEach; ++i) read ^= u[j * kEach + i].x;
-                        release(read & zero);
-                        at_stage.advance();
-                    }
+                    for (int i = 0; i < 2 * kEach; ++i) read ^= u[i].x;
+                    const unsigned nothing = once_read(read);
+                    release(nothing);
+                    at_stage.advance();
+                    release(nothing);
+                    at_stage.advance();
 #pragma unroll
                     for (int i = 0; i < 2 * kEach; ++i) out.put(u[i], p + i * kRingWork * kUnit<T>);
                 }
@@ -650,7 +657,8 @@ policy_loss_ring_kernel(const Args a, float k, int log_cluster) {
                         for (int i = 0; i < kEach; ++i) u[i] = units[i * kRingWork];
 #pragma unroll
                         for (int i = 0; i < kEach; ++i) read ^= u[i].x;
-                        release(read & zero);
+                        const unsigned nothing = once_read(read);
+                        release(nothing);
 #pragma unroll
                         for (int i = 0; i < kEach; ++i) out.put(u[i], p + i * kRingWork * kUnit<T>);
                     } else {
