@@ -380,12 +380,14 @@ fold_apply8_ring_kernel(const __grid_constant__ Table8<CAP> tab, FoldConstants f
             x.sm = st.sm[warp];
             x.sv = st.sv[warp];
             // The stage is given back when it has been read, not when its loads have been issued (one that is still on its way
-            // when the arrival is seen would find the stage filled anew): behind the exchange of the blocks' largest moments,
-            // and at an address that depends on the weights, which have no part in that.  The zero is not known to the compiler.
-            const unsigned read = (__float_as_uint(x.w[0]) ^ __float_as_uint(x.w[4])) & (unsigned)(n >> 63);
+            // when the arrival is seen would find the stage filled anew): at an address that depends on a vote of all lanes
+            // (one arrives for its warp, and lanes may run apart) on their weights and on the blocks' largest moments, which
+            // gradients, codes and scales have gone into.  The zero is not known to the compiler.
+            const unsigned weights = __float_as_uint(x.w[0]) ^ __float_as_uint(x.w[4]), zero = (unsigned)(n >> 63);
             const float2 top = x.update(factor, f, c);
+            const unsigned nothing = __any_sync(0xffffffffu, ((weights ^ __float_as_uint(top.x) ^ __float_as_uint(top.y)) & zero) != 0u);
             __syncwarp();
-            if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]) + read);
+            if (lane == 0) barrier_arrive(shared_addr(&sh.empty[slot]) + nothing);
             x.store_wide(s, tab.w[t], tab.copy[t], at + 4 * lane);
             Block8::store_scales(s, blk, top, lane, c);
         } else {

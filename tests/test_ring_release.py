@@ -32,6 +32,13 @@ def test_rows_of_logits():
     assert body[plain[0]].startswith("for (int at = 0; at < count;") and all("out.put" in " ".join(body[i - 3:i]) for i in plain[1:])
 
 
+def test_8_bit_updates():
+    lines = _statements("state8.cu")
+    at = next(i for i, line in enumerate(lines) if "barrier_arrive(" in line and "+ nothing" in line)
+    assert lines[at - 1] == "__syncwarp();" and re.match(r"const unsigned nothing = %s;$" % VOTE, lines[at - 2])
+    assert all(part in lines[at - 2] for part in ("weights", "top.x", "top.y"))
+
+
 def test_32_bit_updates():
     """Nothing is read of the stage behind the last store of what was read from it."""
     lines = _statements("fold_apply_multi.cu")
