@@ -664,23 +664,33 @@ RowPlan plan_rows(int64_t rows, int pieces, int sm_count, int most, bool power) 
     return p;
 }
 
+constexpr int most_even(size_t size) { return size == 2 ? 8 : 4; }  // pieces of even rows to a thread, x's elements of that size
+constexpr int kMostOdd = 4;
+
 template <typename T, typename O>
 cudaError_t forward_even(const NormArgs &a, RowPlan &p, int sm_count, cudaStream_t stream) {
+    if constexpr (most_even(sizeof(T)) == 8) {
+        if (p.each == 8) return forward_groups<T, O, 8, true, 0>(a, p, sm_count, stream);
+    }
     switch (p.each) {
-        case 8: return forward_groups<T, O, 8, true, 0>(a, p, sm_count, stream);
         case 4: return forward_groups<T, O, 4, true, 0>(a, p, sm_count, stream);
         case 2: return forward_groups<T, O, 2, true, 0>(a, p, sm_count, stream);
         default: return forward_groups<T, O, 1, true, 0>(a, p, sm_count, stream);
     }
 }
+// (rows here have over 32 pieces and up to kLongPieces: one piece to a thread takes two warps at least, four take eight at most)
 template <typename T, typename O, int U>
 cudaError_t forward_odd(const NormArgs &a, RowPlan &p, int sm_count, cudaStream_t stream) {
+    if constexpr (U > 1) {
+        if (p.warps == 1) return forward_groups<T, O, U, false, 1>(a, p, sm_count, stream);
+    }
+    if constexpr (kLongPieces > 32 * 8 * U) {
+        if (p.warps == 16) return forward_groups<T, O, U, false, 16>(a, p, sm_count, stream);
+    }
     switch (p.warps) {
-        case 1: return forward_groups<T, O, U, false, 1>(a, p, sm_count, stream);
         case 2: return forward_groups<T, O, U, false, 2>(a, p, sm_count, stream);
         case 4: return forward_groups<T, O, U, false, 4>(a, p, sm_count, stream);
-        case 8: return forward_groups<T, O, U, false, 8>(a, p, sm_count, stream);
-        default: return forward_groups<T, O, U, false, 16>(a, p, sm_count, stream);
+        default: return forward_groups<T, O, U, false, 8>(a, p, sm_count, stream);
     }
 }
 
@@ -702,7 +712,7 @@ cudaError_t forward(const NormArgs &a, int sm_count, cudaStream_t stream) {
         return cudaGetLastError();
     }
     // (uneven: four pieces where there are rows enough for that, else one or two)
-    RowPlan p = plan_rows(a.rows, pieces, sm_count, even && sizeof(T) == 2 ? 8 : 4, !even);
+    RowPlan p = plan_rows(a.rows, pieces, sm_count, even ? most_even(sizeof(T)) : kMostOdd, !even);
     // rows side by side in a block, as many as its warps and an SM's shared memory have room for
     p.groups = kGroupWarps / p.warps;
     while (p.groups > 1 && a.rows < (int64_t)sm_count * p.groups) p.groups -= 1;

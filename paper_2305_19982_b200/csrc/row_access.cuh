@@ -209,15 +209,14 @@ struct Slot {
     // Zeros where nothing will be sent to, so that get need not ask which columns there are.
     template <int N, int W>
     static __device__ __forceinline__ void clear(unsigned char *slot, const Columns<EVEN, N, W> &c, int u, int t, int threads) {
-        if constexpr (kCopied) {
-            constexpr int kEach = EVEN ? (N * sizeof(T) == 8 ? 2 : kUnits) : kPiece, kLen = kBytes / kEach;
+        static_assert(EVEN, "uneven rows are not cleared");
+        constexpr int kEach = N * sizeof(T) == 8 ? 2 : kUnits, kLen = kBytes / kEach;
 #pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                if (!c.has(u, kPiece / kEach * i)) {
+        for (int i = 0; i < kEach; ++i)
+            if (!c.has(u, kPiece / kEach * i)) {
 #pragma unroll
-                    for (int q = 0; q < kLen / 4; ++q) reinterpret_cast<unsigned *>(slot)[(threads * i + t) * (kLen / 4) + q] = 0;
-                }
-        }
+                for (int q = 0; q < kLen / 4; ++q) reinterpret_cast<unsigned *>(slot)[(threads * i + t) * (kLen / 4) + q] = 0;
+            }
     }
     template <int N, int W>
     static __device__ __forceinline__ Vec get(const unsigned char *slot, const T *row, const Columns<EVEN, N, W> &c, int u, int t, int threads) {
