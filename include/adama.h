@@ -504,7 +504,7 @@ typedef struct adama_distill_args {
 } adama_distill_args;
 ADAMA_API adama_status adama_distill_loss(adama_ctx *ctx, const adama_distill_args *args,
                                           void *cuda_stream);
-/* Bytes of the scratch of such a call; 0 for arguments that it would refuse. */
+/* Bytes of the scratch of such a call, rows*(16*top + 16); 0 for arguments that it would refuse. */
 ADAMA_API size_t adama_distill_scratch(const adama_ctx *ctx, int64_t rows, int64_t top);
 
 /* The id of the capture that `cuda_stream` is taking part in, 0 if it is not being captured: what a
@@ -572,7 +572,8 @@ typedef struct adama_layer_norm_backward_args {
 } adama_layer_norm_backward_args;
 ADAMA_API adama_status adama_layer_norm_backward(adama_ctx *ctx, const adama_layer_norm_backward_args *args,
                                                  void *cuda_stream);
-/* Bytes of the workspace of such a call; 0 for arguments that it would refuse. */
+/* Bytes of the workspace of such a call: the two sums of each column for each block of rows, at most 8*dim for an SM (twice that
+ * up to 256 columns), and 8 for each row where dim > 8192; 0 for arguments that it would refuse. */
 ADAMA_API size_t adama_layer_norm_workspace(const adama_ctx *ctx, int64_t rows, int64_t dim);
 
 /* Embedding lookup, out[t] = scale*table[ids[t]], rounded once.
@@ -616,7 +617,9 @@ typedef struct adama_embedding_grad_args {
 } adama_embedding_grad_args;
 ADAMA_API adama_status adama_embedding_grad(adama_ctx *ctx, const adama_embedding_grad_args *args,
                                             void *cuda_stream);
-/* Bytes of the workspace of such a call; 0 for arguments that it would refuse. */
+/* Bytes of the workspace of such a call, 0 for arguments that it would refuse: the sorted tokens (8 bytes each, over 5120
+ * tokens 16 and 512 KB), and room for the fp32 sums of runs of equal tokens that cross chunks, two for each chunk of 16 tokens (of 8,
+ * where there are few): tokens*dim/2 bytes (tokens*dim), dim rounded up to 256, whatever the tokens are.  32768 x 4096: 68 MB. */
 ADAMA_API size_t adama_embedding_workspace(const adama_ctx *ctx, int64_t tokens, int64_t dim);
 
 /* ---- host-buffer variants (same arithmetic, copies included) --------------------------- */

@@ -785,8 +785,9 @@ class AdamA:
     # -- norms and embeddings ----------------------------------------------------------------
     def _scratch(self, stream: int, of: str, rows: int, dim: int) -> int:
         """Workspace of a call over rows x dim, whose size adama_<of> gives: one buffer for each stream,
-        made anew where a call needs more; while the stream is being captured into a graph, one of that graph's
-        own from its memory.  What it holds between calls does not matter."""
+        made anew where a call needs more and kept as long as the context; while the stream is being captured into a
+        graph, one of that graph's own from its memory.  What it holds between calls does not matter.  The largest is
+        embedding_grad's, up to tokens*dim/2 bytes (include/adama.h)."""
         need = self._scratch_bytes.get((of, rows, dim))
         if need is None:
             if len(self._scratch_bytes) >= 1024:

@@ -5,7 +5,7 @@
 // All but the entries' own elements have the form that the kernels write for any loss, per_e * 2^(k*(x - top)).
 // Rows that a warp holds are dealt with whole.  For longer ones a short kernel takes the teacher's side and the
 // entries' logits ahead of the main one, which leaves each row's top and sum; a third one makes the loss terms and
-// writes the entries' elements over, at 16 bytes an entry to L2 and back.  (4096 x 50257 bf16, 64 entries: 150 us.  When it took 157, the
+// writes the entries' elements over, at 16 bytes an entry to L2 and back.  (4096 x 50257 bf16, 64 entries: 151 us.  When it took 157, the
 // main kernel doing all of it gained nothing: 160 us with one warp for the entries between a row's statistics and its gradient, 156
 // with all of them, but 24 rows of 32000 then took 12.3 instead of 10.3.)
 #pragma once

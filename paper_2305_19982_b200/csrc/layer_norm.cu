@@ -11,7 +11,8 @@
 //
 // Bound by HBM where there is enough to do: 16384 x 4096 bf16 takes 48 us forward = 5.6 TB/s, 75 us backward = 5.4 TB/s.  4096 x 1600
 // is one wave, in which launch, first rows, sums across warps and the last rows come in sequence: 13 us forward (fp32 to
-// bf16, floor 6), 17 us backward with the moments (floor 6).  One row: 2.8 us.  Rows that are not even (row_access.cuh) are bound
+// bf16, floor 6), 17 us backward with the moments (floor 6).  Its 200 pieces take 256 places (four to a lane of two warps forward,
+// two of four backward), and forward 1184 groups go round four times for 3.5 turns of rows.  One row: 2.8 us.  Rows that are not even (row_access.cuh) are bound
 // by instructions, an element to an access: 8192 x 1601 bf16 24 us forward, 39 backward (floors 8 and 12).  Bringing them to
 // shared memory by the 16 bytes made them slower (17696 x 760 39 -> 57): it is not latency that they wait for.
 #include "adama_device.cuh"
@@ -217,7 +218,8 @@ layer_norm_kernel(const NormArgs a, int warps) {
     }
 }
 
-// Rows that no group holds in registers: read three times, from L2 if they stay there.
+// Rows that no group holds in registers: read three times, from L2 if they stay there, an element to an access.
+// 2048 x 12288 bf16 48 us (floor 15), fp32 57 (31); 2048 x 14336 bf16 54 (18).
 constexpr int kLongThreads = 512;
 
 template <typename T, typename O>
@@ -516,7 +518,8 @@ layer_norm_backward_kernel(const NormBackArgs a, int warps) {
     }
 }
 
-// Rows too long for that: the two sums of each row first, then columns by the tile.
+// Rows too long for that: the two sums of each row first, then columns by the tile, an element to an access; x and dy are
+// read twice.  2048 x 12288 bf16 136 us (floor 23), fp32 153 (46); 2048 x 14336 bf16 154 (27).
 template <typename T, typename G>
 __global__ void __launch_bounds__(kLongThreads)
 layer_norm_row_sums_kernel(const NormBackArgs a, float2 *sums) {
@@ -729,7 +732,8 @@ struct BackPlan : RowPlan {
 BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even, bool wide) {
     BackPlan p;
     p.pieces = (int)(padded(dim) / kPiece);
-    // two pieces to a thread (16384 x 4096 bf16 75 us, one 102; 32816 x 512 31, 36; 4096 x 1600 17.1, 16.4), one where there are few rows
+    // two pieces to a thread (16384 x 4096 bf16 75 us, one 102; 32816 x 512 31, 36), one where there are few rows.  (One is better for some
+    // rows that two leave places empty in: 4096 x 1600, seven warps of one piece 16.4 us, four of two 17.1.)
     p.each = p.pieces > 32 * kGroupWarps || (even && rows >= 2 * (int64_t)sm_count) ? 2 : 1;
     p.warps = (p.pieces + 32 * p.each - 1) / (32 * p.each);
     while (!even && p.pieces > 32 && (p.warps & (p.warps - 1))) ++p.warps;  // the compiler has to know them
@@ -738,7 +742,9 @@ BackPlan plan_back(int64_t rows, int dim, int sm_count, bool even, bool wide) {
     int64_t most = sm_count;
     if (p.pieces <= 32) {
         p.groups = kLanesThreads / lanes_for(p.pieces);
-        most = 2 * (int64_t)sm_count;  // as many as an SM has registers for (60000 x 256 bf16: 28 us, with one 42, with four 32)
+        // two to an SM.  Three fit, too (72 to 80 registers), and are better where there are many long rows alone: 60000 x 256 bf16 27.8 us
+        // with two, 24.7 with three (one 42, four 32), 65536 x 128 17.4 and 16.2; 23327 x 224 12.4 and 13.4, 15035 x 56 7.3 and 8.3
+        most = 2 * (int64_t)sm_count;
     } else if (p.is_long) {
         const int64_t tiles = (dim + kTileColumns * kLanesThreads - 1) / (kTileColumns * kLanesThreads);
         most = (4 * (int64_t)sm_count + tiles - 1) / tiles;

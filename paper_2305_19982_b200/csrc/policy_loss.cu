@@ -8,7 +8,7 @@
 // A row is read once (loss: and its gradient written once).  Beside HBM the exponentials count, one per
 // element for the statistics and one for the gradient, at 16 per clock and SM.  Log-probabilities of 4096 rows
 // of 50304 bf16 with entropy: 69 us = 5.98 TB/s; loss and gradient of 8192 rows of 50257, a quarter of them
-// masked: 252 us = 5.7 TB/s, of 6103 rows of 32768, which fill the ring's stages, 123 us = 5.7 TB/s; the
+// masked: 252 us = 5.7 TB/s, of 6103 rows of 32768, which fill the ring's stages, 119 us = 5.9 TB/s; the
 // log-probability of one row of 50257 fp32: 3.9 us.  Distillation of 4096 x 50257 bf16 from 64 entries, a quarter masked:
 // 150 us = 4.8 TB/s, of 24 x 32000 fp32 10.3 us, in three kernels.
 
@@ -283,8 +283,8 @@ __device__ __forceinline__ void finish_stats(const Args &a, const Sums &s, doubl
 
 // ---- rows that fit a warp's registers -----------------------------------------------------------
 
-// One row at a time to a warp, 32 warps to an SM hide its latencies: 100000 x 2000 bf16 143 us (76 % of a
-// copy's rate), 333333 x 600 248 us (44 %).  What holds these back is no floor: all 32 lanes compute the row's
+// One row at a time to a warp, 32 warps to an SM hide its latencies: 100000 x 2000 bf16 144 us (75 % of a
+// copy's rate), 333333 x 600 246 us (44 %).  What holds these back is no floor: all 32 lanes compute the row's
 // loss terms (a logarithm, two exponentials, a division) once per row, and a lane's eight units leave 64
 // registers too few (72 to 104 bytes spilled).
 template <typename T, typename O>
@@ -352,7 +352,9 @@ policy_loss_rows_kernel(const PolicyArgs a, float k) {
     finish_stats<kThreads, 32>(a, acc, sums, &last, threadIdx.x, blockIdx.x, gridDim.x);
 }
 
-// The same for distillation: the warp's lanes hold the entries, too.
+// The same for distillation: the warp's lanes hold the entries, too.  100000 x 2000 bf16 from 64 entries 231 us (50 % of a copy's
+// rate), 333333 x 600 from 20 entries 387 (30 %): a warp does a row's loads, two exchanges, teacher's side, loss terms and
+// stores one after the other, and 64 registers to a thread are too few here as well (128 to 152 bytes spilled).
 template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 2)
 distill_rows_kernel(const DistillArgs a, float k) {

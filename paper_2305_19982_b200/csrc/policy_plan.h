@@ -26,8 +26,8 @@ struct RingCut {
     }
 };
 // The shorter the slice, the fewer threads to it and the more CTAs to an SM: a row's joins and barriers
-// then cost fewer warps, and other rows' work hides its latencies (24390 x 8200 bf16: 238 us with 512
-// threads, 160 with 256, 132 with 128; 48828 x 4096: 149 with 128, 131 with 64).
+// then cost fewer warps, and other rows' work hides its latencies (24390 x 8200 bf16: 250 us with 512
+// threads, 160 with 256, 134 with 128; 48828 x 4096: 151 with 128, 132 with 64; 8333 x 24000: 139 with 512, 131 with 256).
 using Cut640 = RingCut<640, 11, 1>;  // 11 stages of 20 KB: slices of up to 6400 units
 using Cut512 = RingCut<512, 14, 1>;  // 14 of 16 KB: 7168
 using Cut256 = RingCut<256, 13, 2>;  // 13 of 8 KB: 3072
@@ -37,8 +37,8 @@ using Cut64 = RingCut<64, 13, 8>;    // 13 of 2 KB: 768
 enum PolicyForm { kFormRows, kForm64, kForm128, kForm256, kForm512, kForm640, kFormLong };
 
 // The cut of a whole SM: a stage that a row fills in part costs nearly as much as a full one, so the cut
-// that fills better: 8192 x 50257 bf16 (6282 units, 114 % with Cut512, 102 % with Cut640) 260 and 256 us,
-// 4096 of them with odd pitches 159 and 146; 8192 x 32000 (4000 units, 102 % and 128 %) 158 and 175 us.  On
+// that fills better: 8192 x 50257 bf16 (6282 units, 114 % with Cut512, 102 % with Cut640) 259 and 251 us,
+// 4096 of them with odd pitches 159 and 147; 8192 x 32000 (4000 units, 102 % and 128 %) 160 and 168 us.  On
 // a tie the deeper ring.
 inline PolicyForm whole_sm_cut(int64_t slice) {
     return Cut640::fill_cost(slice) < Cut512::fill_cost(slice) ? kForm640 : kForm512;
@@ -57,7 +57,7 @@ int plan_policy(int64_t units, int64_t rows, int sm_count, Resident resident, Po
     plan = {kFormRows, 1, false};
     if (units <= 32 * kRowUnits) return 0;
     // As few CTAs to a row as hold two of its slices.  Few rows are dealt out at once, one to a cluster as
-    // large as that and the row's length allow, which then has to hold one slice (33 x 131072 fp32: 8.9 us
+    // large as that and the row's length allow, which then has to hold one slice (33 x 131072 fp32: 10.0 us
     // with 4 CTAs to a row, 10.9 with 8 in three turns).  A second row would wait in such a ring for ever:
     // what is asked about is the cut that will be launched.
     while (plan.cluster < kMaxCluster && (units + plan.cluster - 1) / plan.cluster > Cut512::kSliceUnits) plan.cluster *= 2;
@@ -82,7 +82,7 @@ int plan_policy(int64_t units, int64_t rows, int sm_count, Resident resident, Po
     } else if (slice <= Cut128::kSliceUnits) {
         plan.form = kForm128;
     } else if (plan.cluster == 1 && slice <= Cut256::kSliceUnits) {
-        // (only whole rows: the halves of 6250 x 32000 in clusters take 129 us, whole rows with Cut512 123)
+        // (only whole rows: the halves of 6250 x 32000 in clusters take 131 us, whole rows with Cut512 124)
         plan.form = kForm256;
     } else if (slice <= Cut640::kSliceUnits && whole_sm_cut(slice) == kForm640) {
         plan.form = kForm640;
